@@ -96,7 +96,9 @@ typedef struct {
 #define ENTMAX_ATTN_STATUS_SCORED_STEPS 5  /* ... and steps it still scored (both 0 without ALiBi slopes)          */
 #define ENTMAX_ATTN_FLAG_WAIT_EXPIRED 1    /* a bounded on-chip wait ran out; outputs of that call are invalid */
 #define ENTMAX_ATTN_FLAG_BAD_SCALE 2       /* some c_i was not finite                                          */
-#define ENTMAX_ATTN_FLAG_BAD_LENGTH 4      /* entmax_attn_decode_fwd: some kv_len[b] outside [q_len, kv_capacity] */
+#define ENTMAX_ATTN_FLAG_BAD_LENGTH 4      /* entmax_attn_decode_fwd: some kv_len[b] outside [q_len, kv_capacity];
+                                              entmax_attn_paged_*: a sequence's lengths do not fit (see there)     */
+#define ENTMAX_ATTN_FLAG_BAD_PAGE 8        /* entmax_attn_paged_*: a page number outside the pool                  */
 
 /* Bytes of scratch the caller must pass to entmax_attn_fwd (is_bwd = 0) or entmax_attn_bwd
  * (is_bwd = 1) for these params.  Returns 0 if the params are invalid.  No paper counterpart: the
@@ -294,6 +296,86 @@ int entmax_attn_decode_fwd(const entmax_attn_decode_params* params, const void* 
                            const int32_t* kv_len, const float* beta, const float* gamma, const float* delta,
                            const float* alibi_slopes, void* o, float* tau, int32_t* support_size, void* workspace,
                            size_t workspace_bytes, int32_t* device_status, void* cuda_stream);
+
+/* Serving from a paged key/value cache.  (The paper has no counterpart: it does not describe serving.)  Keys and values live in a pool of
+ * pages of page_size tokens each; a sequence's pages may be anywhere in the pool, and several sequences may share pages they only
+ * read.  Position p of sequence b is slot p % page_size of page block_table[b][p / page_size].
+ *   batch         sequences
+ *   page_size     tokens per page: a power of two, 16 .. 65536
+ *   num_pages     pages in the pool; max_pages: entries in a row of the block table, max_pages * page_size <= ENTMAX_ATTN_PAGED_MAX_KV
+ *   table_stride  elements between the rows of the block table (>= max_pages)
+ *   stride_*      elements between pages, slots of a page and K/V heads of a slot, for K and V alike (multiples of 8, at least head_dim;
+ *                 head_dim innermost): [pages, slots, heads, d] and [pages, heads, slots, d] pools both fit, and so do views of one
+ *                 pool that holds K and V side by side
+ * New tokens are packed: the rows cu_q[b] .. cu_q[b+1] - 1 of q (k, v) are the last tokens of sequence b, kv_len[b] counts everything
+ * the sequence has including them, so new token t sits at position kv_len[b] - (cu_q[b+1] - cu_q[b]) + t.
+ *   cu_q          in, device int32 [batch + 1], ascending from 0; rows behind cu_q[batch] are left alone.  NULL: every sequence
+ *                 has total_q / batch new tokens (total_q a multiple of batch)
+ *   kv_len        in, device int32 [batch]
+ *   block_table   in, device int32 [batch][table_stride]; entries of pages a sequence does not reach are not read
+ * Lengths and page numbers are device data and checked there.  A sequence whose kv_len is smaller than its number of new tokens or
+ * larger than what the call can hold sets ENTMAX_ATTN_FLAG_BAD_LENGTH and is left out; a page number outside the pool sets
+ * ENTMAX_ATTN_FLAG_BAD_PAGE, is not read or written, and leaves the results of its sequence unspecified (finite). */
+#define ENTMAX_ATTN_PAGED_MAX_KV (1 << 24)
+typedef struct {
+  int32_t batch, kv_heads, head_dim;                 /* head_dim in {64, 128}                                  */
+  int32_t page_size, num_pages, max_pages;
+  int64_t table_stride;
+  int64_t stride_page, stride_token, stride_head;
+} entmax_attn_paged_cache;
+
+/* Rotates new queries and keys to their positions and appends keys and values to the cache.  Per row x (one token, one head) the first
+ * rot_dim elements are taken in pairs, (i, i + rot_dim/2) or, interleaved, (2i, 2i + 1), and turned by the angle of the token's position:
+ *   x'_first = x_first cos - x_second sin,  x'_second = x_second cos + x_first sin     (float32, rounded to bfloat16 once)
+ *   rotation      in, device float32 [rot_positions][rot_dim], 16-byte aligned: cosines of the rot_dim/2 pairs, then sines; NULL with
+ *                 rot_dim = 0 (nothing is turned).  rot_dim: a multiple of 16, at most head_dim
+ *   q             in, device bf16 [total_q, q_heads, head_dim] with strides, or NULL (q_heads = 0: only keys and values)
+ *   k, v          in, device bf16 [total_q, kv_heads, head_dim] with strides (e.g. views of one fused projection)
+ *   q_out         out, device bf16 [total_q, q_heads, head_dim] with strides; may be q itself with q's strides
+ *   k_cache, v_cache   in/out, device bf16: the slots of the new tokens are written, nothing else
+ * Strides in elements, multiples of 8 and at least head_dim; 16-byte aligned pointers.  A sequence with kv_len above
+ * max_pages * page_size or rot_positions is left out (ENTMAX_ATTN_FLAG_BAD_LENGTH): neither its queries nor its slots are written.  New tokens of two
+ * sequences must not meet in the same slot (a page that both append to): one of the two would be kept, not determined which. */
+typedef struct {
+  int32_t total_q, q_heads;
+  int32_t rot_dim, rot_positions, interleaved;
+  int64_t q_stride_t, q_stride_h, k_stride_t, k_stride_h, v_stride_t, v_stride_h, out_stride_t, out_stride_h;
+} entmax_attn_paged_append_params;
+int entmax_attn_paged_append(const entmax_attn_paged_cache* cache, const entmax_attn_paged_append_params* params, const void* q,
+                             const void* k, const void* v, const float* rotation, const int32_t* cu_q, const int32_t* kv_len,
+                             const int32_t* block_table, void* q_out, void* k_cache, void* v_cache, int32_t* device_status,
+                             void* cuda_stream);
+
+/* Attention of new tokens over the cache, which already holds their own keys and values: one token per sequence (decoding), a few (checking
+ * proposed tokens), a chunk of a prompt or a whole prompt, mixed in one call.  Query heads kv_head * g .. kv_head * g + g - 1, g = q_heads /
+ * kv_heads <= 128, share a K/V head.  The token at position pos sees the keys j <= pos and is row pos of the full causal problem: Eq. 1 on
+ * s_j = c (sm_scale <q,k_j> - m_h (pos - j)), c from Eq. "asentmax" with n = pos + 1 (c = delta_h for n = 1).
+ *   q             in,  device bf16 [total_q, q_heads, head_dim] with strides (multiples of 8, at least head_dim)
+ *   beta, gamma, delta   in, device float32 [q_heads]; all three or none (c = 1)
+ *   alibi_slopes  in,  device float32 [q_heads] or NULL
+ *   o             out, device bf16 [total_q, q_heads, head_dim] contiguous
+ *   tau           out, device float32 [total_q, q_heads]
+ *   support_size  out, device int32 [total_q, q_heads] or NULL: number of keys with p > 0
+ *   max_q_len, max_kv_len   the most new tokens and the longest kv_len of any sequence of the call (0: not known).  They size the workspace and
+ *                 the launches; a sequence beyond them is left out (ENTMAX_ATTN_FLAG_BAD_LENGTH)
+ *   workspace     device scratch, 256-byte aligned, >= entmax_attn_paged_workspace_bytes(cache, params, cu_q == NULL) bytes
+ * The rows of a sequence that is left out get O = 0, tau = -inf, support size 0.  K is read once per K/V head (chunks: once
+ * per 256 rows of a head's group), V only on the support.  Results are bitwise reproducible, and slots past a sequence's length may hold anything.
+ * Errors as for entmax_attn_fwd; bf16 only. */
+typedef struct {
+  int32_t total_q, q_heads;
+  int32_t max_q_len, max_kv_len;
+  float alpha;                                        /* 1 < alpha <= 64                                        */
+  float sm_scale;                                     /* 0 means 1/sqrt(head_dim)                               */
+  int64_t q_stride_t, q_stride_h;
+} entmax_attn_paged_params;
+size_t entmax_attn_paged_workspace_bytes(const entmax_attn_paged_cache* cache, const entmax_attn_paged_params* params,
+                                         int uniform);
+int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const entmax_attn_paged_params* params, const void* q,
+                          const void* k_cache, const void* v_cache, const int32_t* cu_q, const int32_t* kv_len,
+                          const int32_t* block_table, const float* beta, const float* gamma, const float* delta,
+                          const float* alibi_slopes, void* o, float* tau, int32_t* support_size, void* workspace,
+                          size_t workspace_bytes, int32_t* device_status, void* cuda_stream);
 
 /* Forward pass for callers that cannot provide a workspace.  (The paper has no counterpart: it does
  * not discuss memory management.)

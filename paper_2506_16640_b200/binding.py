@@ -6,6 +6,7 @@ library is missing or a call is rejected, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -19,7 +20,8 @@ DTYPE_BF16, DTYPE_FP32 = 0, 1
 STATUS_WORDS = 8
 STATUS_FLAGS, STATUS_DENSE_ROWS, STATUS_TILE_SWEEPS, STATUS_TILES = 0, 1, 2, 3
 STATUS_SKIPPED_STEPS, STATUS_SCORED_STEPS = 4, 5
-FLAG_WAIT_EXPIRED, FLAG_BAD_SCALE, FLAG_BAD_LENGTH = 1, 2, 4
+FLAG_WAIT_EXPIRED, FLAG_BAD_SCALE, FLAG_BAD_LENGTH, FLAG_BAD_PAGE = 1, 2, 4, 8
+PAGED_MAX_KV = 1 << 24
 
 
 class Params(ctypes.Structure):
@@ -40,6 +42,27 @@ class ProjParams(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("seq", ctypes.c_int32), ("d_model", ctypes.c_int32),
                 ("x_dtype", ctypes.c_int32), ("causal", ctypes.c_int32), ("n_mode", ctypes.c_int32),
                 ("gamma_range", ctypes.c_float)]
+
+
+class PagedCache(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("table_stride", ctypes.c_int64), ("stride_page", ctypes.c_int64), ("stride_token", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64)]
+
+
+class PagedAppendParams(ctypes.Structure):
+    _fields_ = [("total_q", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("rot_positions", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("q_stride_t", ctypes.c_int64),
+                ("q_stride_h", ctypes.c_int64), ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
+                ("v_stride_t", ctypes.c_int64), ("v_stride_h", ctypes.c_int64), ("out_stride_t", ctypes.c_int64),
+                ("out_stride_h", ctypes.c_int64)]
+
+
+class PagedParams(ctypes.Structure):
+    _fields_ = [("total_q", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("max_q_len", ctypes.c_int32),
+                ("max_kv_len", ctypes.c_int32), ("alpha", ctypes.c_float), ("sm_scale", ctypes.c_float),
+                ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64)]
 
 
 class WsLayout(ctypes.Structure):
@@ -99,6 +122,14 @@ def load():
         lib.entmax_attn_decode_workspace_bytes.argtypes = [dp]
         lib.entmax_attn_decode_fwd.restype = ctypes.c_int
         lib.entmax_attn_decode_fwd.argtypes = [dp, vp, vp, vp, ip, fp, fp, fp, fp, vp, fp, ip, vp, ctypes.c_size_t, ip, vp]
+        cp, ap, gp = ctypes.POINTER(PagedCache), ctypes.POINTER(PagedAppendParams), ctypes.POINTER(PagedParams)
+        lib.entmax_attn_paged_append.restype = ctypes.c_int
+        lib.entmax_attn_paged_append.argtypes = [cp, ap, vp, vp, vp, fp, ip, ip, ip, vp, vp, vp, ip, vp]
+        lib.entmax_attn_paged_workspace_bytes.restype = ctypes.c_size_t
+        lib.entmax_attn_paged_workspace_bytes.argtypes = [cp, gp, ctypes.c_int]
+        lib.entmax_attn_paged_fwd.restype = ctypes.c_int
+        lib.entmax_attn_paged_fwd.argtypes = [cp, gp, vp, vp, vp, ip, ip, ip, fp, fp, fp, fp, vp, fp, ip, vp, ctypes.c_size_t,
+                                              ip, vp]
         lib.entmax_attn_saved_bytes.restype = ctypes.c_size_t
         lib.entmax_attn_saved_bytes.argtypes = [pp]
         lib.entmax_attn_save_supports.restype = ctypes.c_int
@@ -249,6 +280,153 @@ def entmax_attn_decode_fwd(q, k, v, alpha, kv_len=None, beta=None, gamma=None, d
                                        _ptr(support_size), _ptr(workspace), workspace.numel(), _ptr(status),
                                        _stream_ptr(stream))
     _check(rc, "entmax_attn_decode_fwd")
+    return o, tau, support_size
+
+
+def rotation_table(positions: int, rot_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """float32 [positions, rot_dim] for entmax_attn_paged_append: cosines, then sines, of position * base^(-2i / rot_dim), computed in
+    64 bits (in 32 the angle of a position near 10^6 is off by 0.03)."""
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    angle = torch.arange(positions, dtype=torch.float64)[:, None] * base ** (-2.0 * i / rot_dim)
+    return torch.cat([angle.cos(), angle.sin()], 1).to(torch.float32).to(device)
+
+
+def _row_strides(name, x, heads, d):
+    """(token, head) strides of a bf16 [tokens, heads, d] tensor; a dimension of one element has no stride of its own."""
+    if x.dim() != 3 or x.dtype != torch.bfloat16 or x.shape[1] != heads or x.shape[2] != d or x.stride(2) != 1:
+        raise EntmaxAttnError("%s must be a bfloat16 [tokens, %d, %d] tensor with the last dimension contiguous" % (name, heads, d))
+    return x.stride(0) if x.shape[0] > 1 else heads * d, x.stride(1) if heads > 1 else d
+
+
+def _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, total_q, device):
+    if k_cache.dim() != 4 or k_cache.dtype != torch.bfloat16 or k_cache.stride(3) != 1:
+        raise EntmaxAttnError("%s: k_cache must be a bfloat16 [pages, page_size, kv_heads, head_dim] tensor, head_dim contiguous" % what)
+    if v_cache.shape != k_cache.shape or v_cache.stride() != k_cache.stride() or v_cache.dtype != k_cache.dtype:
+        raise EntmaxAttnError("%s: k_cache and v_cache must share shape, strides and dtype" % what)
+    if block_table.dim() != 2 or block_table.dtype != torch.int32 or block_table.stride(1) != 1 and block_table.shape[1] > 1:
+        raise EntmaxAttnError("%s: block_table must be an int32 [batch, max_pages] tensor with contiguous rows" % what)
+    B, max_pages = block_table.shape
+    if kv_len.shape != (B,) or kv_len.dtype != torch.int32 or not kv_len.is_contiguous():
+        raise EntmaxAttnError("%s: kv_len must be a contiguous int32 [batch] tensor" % what)
+    if cu_q is not None and (cu_q.shape != (B + 1,) or cu_q.dtype != torch.int32 or not cu_q.is_contiguous()):
+        raise EntmaxAttnError("%s: cu_q must be a contiguous int32 [batch + 1] tensor" % what)
+    if cu_q is None and B and total_q % B:
+        raise EntmaxAttnError("%s: without cu_q the number of new tokens must be a multiple of the batch" % what)
+    for t in (k_cache, v_cache, block_table, kv_len, cu_q):
+        if t is not None and t.device != device:
+            raise EntmaxAttnError("%s: all tensors must be on one device" % what)
+    P, ps, KH, D = k_cache.shape
+    return PagedCache(B, KH, D, ps, P, max_pages, block_table.stride(0) if B > 1 else max_pages,
+                      k_cache.stride(0) if P > 1 else ps * KH * D, k_cache.stride(1), k_cache.stride(2) if KH > 1 else D)
+
+
+def _check_scale(what, H, device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and (t.shape != (H,) or t.dtype != torch.float32 or not t.is_contiguous() or t.device != device):
+            raise EntmaxAttnError("%s: %s must be a contiguous float32 [%d] tensor on the device of q" % (what, name, H))
+
+
+def _on_device(device):
+    """The launches go to the current device's context: made the tensors' own for the call where it is another."""
+    if device.type != "cuda":
+        raise EntmaxAttnError("CUDA tensors only (there is no CPU fallback)")
+    return torch.cuda.device(device) if device.index != torch._C._cuda_getDevice() else contextlib.nullcontext()
+
+
+def _check_status(what, status, device):
+    if status is not None and (status.dtype != torch.int32 or status.numel() < STATUS_WORDS or not status.is_contiguous() or
+                               status.device != device):
+        raise EntmaxAttnError("%s: status must be a contiguous int32 tensor of %d words on the device of q" % (what, STATUS_WORDS))
+
+
+def entmax_attn_paged_append(q, k, v, k_cache, v_cache, block_table, kv_len, cu_q=None, *, rotation=None, interleaved=False,
+                             q_out=None, status=None, stream=None):
+    """Rotates new queries and keys to their positions and appends keys and values to a paged cache, in one pass.
+
+    q [T, H, d] (or None), k, v [T, kv_heads, d]: the new tokens' rows, bf16, any strides with d contiguous; k_cache, v_cache
+    [pages, page_size, kv_heads, d], written in place (a [pages, kv_heads, page_size, d] pool as its transpose(1, 2));
+    block_table int32 [B, max_pages]; kv_len int32 [B], new tokens included; cu_q int32 [B + 1]: rows cu_q[b] .. cu_q[b+1] - 1
+    are sequence b's (None: T / B each).  rotation: float32 [positions, rot_dim] (rotation_table) or None; interleaved: pairs
+    (2i, 2i + 1) instead of (i, i + rot_dim / 2).  Returns the rotated q (q_out; may be q itself)."""
+    what = "entmax_attn_paged_append"
+    T, KH, D = k.shape if k.dim() == 3 else (0, 0, 0)
+    ks, vs = _row_strides("k", k, KH, D), _row_strides("v", v, KH, D)
+    cache = _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, T, k.device)
+    if (cache.kv_heads, cache.head_dim) != (KH, D) or v.shape != k.shape or v.device != k.device:
+        raise EntmaxAttnError("%s: k, v and the cache disagree on tokens, kv_heads, head_dim or device" % what)
+    H, qs, os_ = 0, (D, D), (D, D)
+    if q is not None:
+        H = q.shape[1] if q.dim() == 3 else 0
+        qs = _row_strides("q", q, H, D)
+        if q_out is None:
+            q_out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+        os_ = _row_strides("q_out", q_out, H, D)
+        if q.shape[0] != T or q_out.shape != q.shape or q.device != k.device or q_out.device != k.device:
+            raise EntmaxAttnError("%s: q, q_out and k disagree on tokens or device" % what)
+    elif q_out is not None:
+        raise EntmaxAttnError("%s: q_out without q" % what)
+    rot_pos, rot = 0, 0
+    if rotation is not None:
+        if rotation.dim() != 2 or rotation.dtype != torch.float32 or not rotation.is_contiguous() or rotation.device != k.device:
+            raise EntmaxAttnError("%s: rotation must be a contiguous float32 [positions, rot_dim] tensor on the device of k" % what)
+        rot_pos, rot = rotation.shape
+    _check_status(what, status, k.device)
+    if T == 0:
+        return q_out
+    params = PagedAppendParams(T, H, rot, rot_pos, int(bool(interleaved)), *qs, *ks, *vs, *os_)
+    with _on_device(k.device):
+        rc = load().entmax_attn_paged_append(ctypes.byref(cache), ctypes.byref(params), _ptr(q), _ptr(k), _ptr(v), _ptr(rotation),
+                                             _ptr(cu_q), _ptr(kv_len), _ptr(block_table), _ptr(q_out), _ptr(k_cache), _ptr(v_cache),
+                                             _ptr(status), _stream_ptr(stream))
+    _check(rc, what)
+    return q_out
+
+
+def _paged_params(q, alpha, sm_scale, max_q_len, max_kv_len):
+    T, H, D = q.shape if q.dim() == 3 else (0, 0, 0)
+    return PagedParams(T, H, int(max_q_len), int(max_kv_len), float(alpha), float(sm_scale), *_row_strides("q", q, H, D))
+
+
+def entmax_attn_paged_workspace_bytes(cache: PagedCache, params: PagedParams, uniform: bool) -> int:
+    return int(load().entmax_attn_paged_workspace_bytes(ctypes.byref(cache), ctypes.byref(params), int(bool(uniform))))
+
+
+def entmax_attn_paged_fwd(q, k_cache, v_cache, alpha, block_table, kv_len, cu_q=None, beta=None, gamma=None, delta=None, *,
+                          alibi_slopes=None, sm_scale=0.0, max_q_len=0, max_kv_len=0, o=None, tau=None, support_size=None,
+                          workspace=None, status=None, stream=None):
+    """Attention of new tokens over a paged cache that already holds their keys and values: q [T, H, d] bf16, packed as in
+    entmax_attn_paged_append, H a multiple of the cache's kv_heads (query heads h * H / kv_heads .. share K/V head h).  One new
+    token per sequence, a chunk, or whole prompts, mixed as they come.  max_q_len, max_kv_len: the most new tokens and the
+    longest kv_len of the call, where the caller knows them (they size the workspace and the launches).
+    Returns (o [T, H, d], tau [T, H], support_size [T, H])."""
+    what = "entmax_attn_paged_fwd"
+    params = _paged_params(q, alpha, sm_scale, max_q_len, max_kv_len)
+    T, H, D = q.shape
+    device = q.device
+    cache = _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, T, device)
+    if cache.head_dim != D:
+        raise EntmaxAttnError("%s: q and the cache disagree on head_dim" % what)
+    _check_scale(what, H, device, beta=beta, gamma=gamma, delta=delta, alibi_slopes=alibi_slopes)
+    _check_status(what, status, device)
+    o = torch.empty((T, H, D), dtype=q.dtype, device=device) if o is None else o
+    tau = torch.empty((T, H), dtype=torch.float32, device=device) if tau is None else tau
+    support_size = torch.empty((T, H), dtype=torch.int32, device=device) if support_size is None else support_size
+    for name, t, shape, dtype in (("o", o, (T, H, D), torch.bfloat16), ("tau", tau, (T, H), torch.float32),
+                                  ("support_size", support_size, (T, H), torch.int32)):
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.device != device:
+            raise EntmaxAttnError("%s: %s must be a contiguous %s %s tensor on the device of q" % (what, name, dtype, list(shape)))
+    if T == 0:
+        return o, tau, support_size
+    with _on_device(device):
+        if workspace is None:
+            nbytes = entmax_attn_paged_workspace_bytes(cache, params, cu_q is None)
+            # (0: the parameters are refused below, with the reason)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        rc = load().entmax_attn_paged_fwd(ctypes.byref(cache), ctypes.byref(params), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(cu_q),
+                                          _ptr(kv_len), _ptr(block_table), _ptr(beta), _ptr(gamma), _ptr(delta), _ptr(alibi_slopes),
+                                          _ptr(o), _ptr(tau), _ptr(support_size), _ptr(workspace), workspace.numel(), _ptr(status),
+                                          _stream_ptr(stream))
+    _check(rc, what)
     return o, tau, support_size
 
 

@@ -313,6 +313,11 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
+// Host: a bf16 tensor of four dimensions (D, n1, n2, n3), D contiguous and the others at element strides s1, s2, s3, as a tensor map
+// with boxes of 64 columns (one 128-byte swizzle row) by box1 by box2 rows; 128-byte swizzle, what lies outside is read as zero.
+// Defined in tile_fwd_sm100.cu, like the next ones.
+cudaError_t make_box_map(CUtensorMap* map, const void* base, int D, int n1, int n2, int n3, int64_t s1, int64_t s2, int64_t s3,
+                         int box1, int box2);
 // Host: a bf16 [B,H,N,D] tensor with element strides (sb, sh, sn) as a 4-D tensor map (D, N, H, B), box
 // 64 columns (one 128-byte swizzle row) by box_rows rows, 128-byte swizzle, out-of-range rows read as zero.
 // Defined in tile_fwd_sm100.cu.

@@ -1,0 +1,427 @@
+"""Serving from a paged cache: entmax_attn_paged_append and entmax_attn_paged_fwd against their definitions in 64 bits.
+
+Tolerances: tests/paged.py derives them row by row from the roundings a float32 evaluation makes."""
+import numpy as np
+import pytest
+import torch
+
+import paged
+from paper_2506_16640_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+def _problem(new, lens, H, KH, d, page, seed=0, sigma=1.0, layout="tokens", rows_behind=0, plant=True):
+    """Packed queries and a filled pool; some keys match a query, so that supports of one and of many keys occur."""
+    g = torch.Generator().manual_seed(seed)
+    T = sum(new)
+    q = (torch.randn((T + rows_behind, H, d), generator=g) * sigma).to(torch.bfloat16)
+    keys = [(torch.randn((n, KH, d), generator=g) * sigma).to(torch.bfloat16) for n in lens]
+    values = [torch.randn((n, KH, d), generator=g).to(torch.bfloat16) for n in lens]
+    t = 0
+    for b, n in enumerate(new):
+        for i in range(0, n if plant else 0, 3):
+            x = q[t + i, (i // 3) % H].float()
+            at = int(torch.randint(0, lens[b] - n + i + 1, (1,), generator=g))
+            keys[b][at, ((i // 3) % H) // (H // KH)] = (2.5 * d ** 0.5 * x / x.norm()).to(torch.bfloat16)
+        t += n
+    kc, vc, table = paged.pool(keys, values, page, d, KH, seed, "cuda", layout=layout)
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+    return dict(q=q.cuda(), keys=keys, values=values, kc=kc, vc=vc, table=table, cu=cu,
+                lens=torch.tensor(lens, dtype=torch.int32, device="cuda"), new=list(new), kv=list(lens), H=H, KH=KH, d=d)
+
+
+def _scales(H, seed, kind):
+    g = torch.Generator().manual_seed(1000 + seed)
+    if kind is None:
+        return None
+    if kind == "cool":                        # low temperatures: supports of one or two keys
+        return [torch.full((H,), x) for x in (1.5, 1.2, 2.0)]
+    return [0.5 + torch.rand(H, generator=g) for _ in range(3)]
+
+
+def _run(pr, alpha, scale=None, slopes=None, **kw):
+    status = torch.full((binding.STATUS_WORDS,), -1, dtype=torch.int32, device="cuda")
+    sc = [t.cuda() for t in scale] if scale is not None else [None] * 3
+    al = torch.tensor(slopes, dtype=torch.float32, device="cuda") if slopes is not None else None
+    out = binding.entmax_attn_paged_fwd(pr["q"], pr["kc"], pr["vc"], alpha, pr["table"], pr["lens"], kw.pop("cu", pr["cu"]), *sc,
+                                        alibi_slopes=al, status=status, **kw)
+    torch.cuda.synchronize()
+    return (*out, int(status[0]))
+
+
+def _check(pr, alpha, got, scale=None, slopes=None, skip=(), sm_scale=None):
+    o, tau, supp, flags = got
+    assert flags == 0
+    o, tau, supp = o.cpu().double(), tau.cpu().double(), supp.cpu()
+    R = pr["H"] // pr["KH"]
+    q = pr["q"].cpu()
+    t = 0
+    for b, (n, L) in enumerate(zip(pr["new"], pr["kv"])):
+        for h in range(pr["H"]) if n and b not in skip else ():
+            sc = None if scale is None else [s[h] for s in scale]
+            m = 0.0 if slopes is None else slopes[h]
+            ro, rt, to, tt, lo, hi = paged.attend(q[t:t + n, h], pr["keys"][b][:, h // R], pr["values"][b][:, h // R], L - n, alpha, sc, m,
+                                                  sm_scale)
+            et, eo = (tau[t:t + n, h] - rt).abs() / tt, (o[t:t + n, h] - ro).abs() / to
+            assert float(et.max()) <= 1.0, ("tau", b, h, int(et.argmax()), float(et.max()))
+            assert float(eo.max()) <= 1.0, ("o", b, h, int(eo.max(1)[0].argmax()), float(eo.max()))
+            s = supp[t:t + n, h]
+            assert bool(((s >= lo) & (s <= hi)).all()), ("support", b, h)
+        t += n
+
+
+LENGTHS = [1, 2, 15, 16, 17, 127, 128, 129, 255, 256, 257, 700, 1500]
+
+
+@pytest.mark.parametrize("H,KH,d,page", [(4, 4, 64, 16), (6, 2, 128, 32), (8, 1, 64, 64), (16, 1, 128, 128), (4, 2, 128, 256), (20, 1, 64, 16)])
+def test_single_tokens(H, KH, d, page):
+    pr = _problem([1] * len(LENGTHS), LENGTHS, H, KH, d, page, seed=H)
+    sc = _scales(H, 1, "length")
+    got = _run(pr, 1.5, sc)
+    _check(pr, 1.5, got, sc)
+    same = _run(pr, 1.5, sc, cu=None, max_q_len=1, max_kv_len=max(LENGTHS))
+    for x, y in zip(got[:2], same[:2]):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("alpha", [1.25, 1.5, 1.7, 2.0, 3.0])
+@pytest.mark.parametrize("kind", [None, "length", "cool"])
+def test_alphas_and_temperatures(alpha, kind):
+    pr = _problem([1, 3, 40], [900, 333, 640], 4, 2, 64, 16, seed=3)
+    sc = _scales(4, 2, kind)
+    _check(pr, alpha, _run(pr, alpha, sc), sc)
+
+
+@pytest.mark.parametrize("new,lens,H,KH,d,page", [
+    ([5, 1, 0, 3, 8], [700, 1, 90, 3, 8], 8, 2, 128, 32),            # a few tokens each, an idle sequence, nothing but new tokens
+    ([9, 17, 33], [33, 17, 400], 3, 1, 64, 16),                      # on both sides of the 32 rows where the kernels change over
+    ([200, 1, 64, 33], [200, 513, 300, 1025], 4, 4, 64, 64),         # whole prompts among single tokens
+    ([130, 259], [1000, 259], 6, 2, 128, 16),                        # groups of three: 126 rows to a tile
+    ([300], [300], 8, 1, 64, 128),
+    ([77, 500], [1111, 1536], 2, 1, 128, 256),
+    ([3, 70], [200, 71], 40, 1, 64, 16),                             # more query heads to a K/V head than the few-row kernel takes
+    ([2, 5], [300, 6], 128, 1, 64, 32),
+])
+def test_chunks(new, lens, H, KH, d, page):
+    pr = _problem(new, lens, H, KH, d, page, seed=len(new) + H)
+    sc = _scales(H, 4, "length")
+    got = _run(pr, 1.5, sc)
+    _check(pr, 1.5, got, sc)
+    hinted = _run(pr, 1.5, sc, max_q_len=max(new), max_kv_len=max(lens))
+    _check(pr, 1.5, hinted, sc)
+
+
+@pytest.mark.parametrize("new,lens", [([1, 1], [600, 40]), ([4, 120], [64, 500])])
+def test_alibi(new, lens):
+    pr = _problem(new, lens, 4, 2, 64, 16, seed=7)
+    slopes = [0.5, 0.0, 0.0625, 0.0]
+    sc = _scales(4, 5, "length")
+    for alpha in (1.5, 2.0):
+        _check(pr, alpha, _run(pr, alpha, sc, slopes), sc, slopes)
+
+
+@pytest.mark.parametrize("new", [1, 150])
+def test_equal_logits_see_every_key(new):
+    # q = 0: every visible key weighs 1/n, far more of them than any list holds
+    pr = _problem([new, 1], [2600, 700], 2, 1, 64, 16, plant=False)
+    pr["q"].zero_()
+    o, tau, supp, flags = got = _run(pr, 1.5)
+    _check(pr, 1.5, got)
+    n = torch.arange(2600 - new + 1, 2601, dtype=torch.float64)
+    assert torch.allclose(tau[:new, 0].cpu().double(), -n.pow(-0.5), rtol=1e-5)
+    assert torch.equal(supp[:new, 0].cpu().long(), n.long())
+
+
+@pytest.mark.parametrize("sigma", [0.02, 0.3])
+def test_flat_rows(sigma):
+    pr = _problem([1, 90], [2000, 1300], 4, 2, 64, 32, sigma=sigma, plant=False)
+    for alpha in (1.25, 1.5, 2.0):
+        _check(pr, alpha, _run(pr, alpha))
+
+
+@pytest.mark.parametrize("layout", ["tokens", "heads", "fused"])
+@pytest.mark.parametrize("new,lens", [([1, 1, 1], [100, 31, 257]), ([100, 2], [257, 40])])
+def test_layouts_and_strided_queries(layout, new, lens):
+    pr = _problem(new, lens, 4, 2, 64, 32, layout=layout)
+    T = sum(new)
+    wide = torch.full((T, 4 + 3, 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide[:, 2:6] = pr["q"]
+    want = _run(pr, 1.5)
+    pr["q"] = wide[:, 2:6]
+    got = _run(pr, 1.5)
+    _check(pr, 1.5, got)
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_rows_behind_the_last_sequence_stay():
+    for new, lens in (([1, 2], [50, 70]), ([60, 1], [300, 9])):
+        pr = _problem(new, lens, 4, 2, 64, 16, rows_behind=9)
+        T = sum(new)
+        o = torch.full((T + 9, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        tau = torch.full((T + 9, 4), 7.0, device="cuda")
+        supp = torch.full((T + 9, 4), 7, dtype=torch.int32, device="cuda")
+        got = _run(pr, 1.5, o=o, tau=tau, support_size=supp)
+        _check(pr, 1.5, got)
+        assert bool((o[T:] == 7).all() and (tau[T:] == 7).all() and (supp[T:] == 7).all())
+
+
+def test_workspace_in_slices():
+    # a table with room for 2^20 tokens and no bound on the lengths given: the rows' share of the workspace covers a few blocks at a time
+    new, lens = [40, 1, 700, 1], [300, 90, 700, 33]
+    pr = _problem(new, lens, 4, 2, 64, 16)
+    wide = torch.full((len(new), (1 << 20) // 16), -1, dtype=torch.int32, device="cuda")
+    wide[:, :pr["table"].shape[1]] = pr["table"]
+    want = _run(pr, 1.5)
+    pr["table"] = wide
+    got = _run(pr, 1.5)
+    _check(pr, 1.5, got)
+    assert torch.equal(want[1], got[1])
+
+
+@pytest.mark.parametrize("new,lens,bad", [([1, 1, 1], [5, 0, 40], 1), ([1, 1, 1], [5, 49, 40], 1), ([3, 60, 1], [40, 30, 9], 1),
+                                          ([3, 60, 1], [40, 65, 9], 1)])
+def test_lengths_that_do_not_fit(new, lens, bad):
+    # the sequence is left out and reported, the others are served (48 tokens of room, or 64 with the chunk)
+    room = 48 if max(new) == 1 else 64
+    ok = [min(max(n, L), room) for n, L in zip(new, lens)]
+    pr = _problem(new, ok, 4, 2, 64, 16)
+    pr["table"] = pr["table"][:, :room // 16].contiguous()
+    pr["lens"] = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, tau, supp, flags = _run(pr, 1.5)
+    assert flags == binding.FLAG_BAD_LENGTH
+    a, e = sum(new[:bad]), sum(new[:bad + 1])
+    assert bool((o[a:e] == 0).all() and torch.isneginf(tau[a:e]).all() and (supp[a:e] == 0).all())
+    pr["kv"] = lens
+    _check(pr, 1.5, (o, tau, supp, 0), skip=(bad,))
+
+
+@pytest.mark.parametrize("new", [[1, 1], [50, 1]])
+def test_pages_outside_the_pool(new):
+    lens = [200, 100]
+    pr = _problem(new, lens, 4, 2, 64, 16)
+    good = _run(pr, 1.5)
+    for bad in (-1, pr["kc"].shape[0], 2 ** 31 - 1):
+        pr["table"][0, 3] = bad
+        o, tau, supp, flags = _run(pr, 1.5)
+        assert flags == binding.FLAG_BAD_PAGE
+        assert bool(torch.isfinite(o).all() and torch.isfinite(tau).all())
+        assert torch.equal(o[new[0]:], good[0][new[0]:]) and torch.equal(tau[new[0]:], good[1][new[0]:])
+
+
+def test_offsets_beyond_32_bits():
+    # a pool of more than 2^32 bytes, the sequence's pages at its end
+    d, KH, page = 128, 2, 256
+    n = (1 << 32) // (page * KH * d * 2) + 40
+    pr = _problem([1, 70], [300, 500], 4, KH, d, page)
+    kc = torch.zeros((n, page, KH, d), dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros_like(kc)
+    m = pr["kc"].shape[0]
+    kc[n - m:], vc[n - m:] = pr["kc"], pr["vc"]
+    pr["table"] = torch.where(pr["table"] < m, pr["table"] + (n - m), pr["table"])
+    pr["kc"], pr["vc"] = kc, vc
+    _check(pr, 1.5, _run(pr, 1.5))
+
+
+def test_repeats_are_bit_equal():
+    pr = _problem([1, 5, 300], [900, 128, 900], 8, 2, 128, 16)
+    a = _run(pr, 1.5)
+    for _ in range(3):
+        b = _run(pr, 1.5)
+        assert all(torch.equal(x, y) for x, y in zip(a[:3], b[:3]))
+
+
+def test_graph_replay_and_second_stream():
+    pr = _problem([1, 1, 90], [64, 200, 300], 4, 2, 64, 16)
+    sc = [t.cuda() for t in _scales(4, 1, "length")]
+    o = torch.empty((92, 4, 64), dtype=torch.bfloat16, device="cuda")
+    tau = torch.empty((92, 4), device="cuda")
+    side = torch.cuda.Stream()
+
+    def call():
+        binding.entmax_attn_paged_fwd(pr["q"], pr["kc"], pr["vc"], 1.5, pr["table"], pr["lens"], pr["cu"], *sc, o=o, tau=tau)
+
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    side.synchronize()
+    eager = o.clone(), tau.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    o.zero_()
+    tau.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(o, eager[0]) and torch.equal(tau, eager[1])
+    # other lengths through the same graph: one token less of the first sequences' past
+    pr["lens"][:2] -= 1
+    g.replay()
+    torch.cuda.synchronize()
+    again = o.clone()
+    call()
+    torch.cuda.synchronize()
+    assert torch.equal(again, o) and not torch.equal(o[:2], eager[0][:2])
+
+
+# ------------------------------------------------------------------------------------------------ append
+def _append_problem(new, lens, H, KH, d, page, seed=0, layout="tokens"):
+    g = torch.Generator().manual_seed(seed)
+    T = sum(new)
+    qkv = torch.randn((T, H + 2 * KH, d), generator=g).to(torch.bfloat16)
+    past = [torch.randn((n, KH, d), generator=g).to(torch.bfloat16) for n in lens]
+    kc, vc, table = paged.pool(past, [-x for x in past], page, d, KH, seed, "cuda", fill=5.0, layout=layout)
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+    return qkv.cuda(), kc, vc, table, cu, torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+
+def _check_append(qkv, H, KH, new, lens, page, rotation, interleaved, before, after, table, q_out):
+    x = qkv.cpu()
+    want_k, want_v = before[0].cpu().clone(), before[1].cpu().clone()
+    tol_k = torch.zeros(want_k.shape, dtype=torch.float64)
+    exact_k = want_k.double()
+    t = 0
+    for b, (n, L) in enumerate(zip(new, lens)):
+        pos = torch.arange(L - n, L)
+        rows = x[t:t + n]
+        turned = rows[:, :H + KH].double() if rotation is None else paged.rotate(rows[:, :H + KH], rotation.cpu(), pos, interleaved)
+        # two products and a sum in float32 (or fused), one rounding to bf16
+        tol = 2.0 ** -8 * turned.abs() + 4 * 2.0 ** -24 * 2 * rows[:, :H + KH].double().abs().amax(-1, keepdim=True)
+        if rotation is None:
+            tol = torch.zeros_like(tol)
+        if q_out is not None:
+            assert bool(((q_out[t:t + n].cpu().double() - turned[:, :H]).abs() <= tol[:, :H]).all())
+        pg, slot = table[b].cpu().long()[pos // page], pos % page
+        exact_k[pg, slot], tol_k[pg, slot] = turned[:, H:], tol[:, H:]
+        want_v[pg, slot] = rows[:, H + KH:]
+        t += n
+    assert bool(((after[0].cpu().double() - exact_k).abs() <= tol_k).all())
+    assert torch.equal(after[1].cpu(), want_v)
+
+
+@pytest.mark.parametrize("rot,interleaved", [(0, False), (16, False), (64, False), (64, True), (32, True)])
+@pytest.mark.parametrize("new,lens,H,KH,d,page,layout", [
+    ([1, 1, 1], [1, 16, 300], 4, 4, 64, 16, "tokens"),
+    ([1, 0, 37, 5], [17, 40, 37, 129], 6, 2, 128, 32, "heads"),
+    ([130, 1], [200, 256], 32, 8, 128, 64, "fused"),
+    ([3], [3], 1, 1, 64, 16, "tokens"),
+])
+def test_append(rot, interleaved, new, lens, H, KH, d, page, layout):
+    qkv, kc, vc, table, cu, kv_len = _append_problem(new, lens, H, KH, d, page, layout=layout)
+    rotation = binding.rotation_table(max(lens), rot) if rot else None
+    before = kc.clone(), vc.clone()
+    status = torch.full((binding.STATUS_WORDS,), -1, dtype=torch.int32, device="cuda")
+    q = binding.entmax_attn_paged_append(qkv[:, :H], qkv[:, H:H + KH], qkv[:, H + KH:], kc, vc, table, kv_len, cu, rotation=rotation,
+                                         interleaved=interleaved, status=status)
+    torch.cuda.synchronize()
+    assert int(status[0]) == 0
+    _check_append(qkv, H, KH, new, lens, page, rotation, interleaved, before, (kc, vc), table, q)
+
+
+def test_append_in_place_without_queries_and_uniform():
+    new, lens, H, KH, d, page = [2, 2, 2], [30, 2, 65], 4, 2, 64, 16
+    qkv, kc, vc, table, cu, kv_len = _append_problem(new, lens, H, KH, d, page)
+    rotation = binding.rotation_table(80, 64)
+    before = kc.clone(), vc.clone()
+    src = qkv.clone()
+    q = src[:, :H]
+    out = binding.entmax_attn_paged_append(q, src[:, H:H + KH], src[:, H + KH:], kc, vc, table, kv_len, None, rotation=rotation, q_out=q)
+    torch.cuda.synchronize()
+    assert out.data_ptr() == q.data_ptr()
+    _check_append(qkv, H, KH, new, lens, page, rotation, False, before, (kc, vc), table, out)
+    assert torch.equal(src[:, H:], qkv[:, H:])
+    k2, v2 = before[0].clone(), before[1].clone()
+    assert binding.entmax_attn_paged_append(None, qkv[:, H:H + KH], qkv[:, H + KH:], k2, v2, table, kv_len, cu, rotation=rotation) is None
+    torch.cuda.synchronize()
+    assert torch.equal(k2, kc) and torch.equal(v2, vc)
+
+
+def test_append_at_far_positions():
+    # 64-bit angles: at position 10^6 a float32 angle is off by 0.03
+    L, page = 1_000_003, 4096
+    g = torch.Generator().manual_seed(5)
+    qkv = torch.randn((3, 3, 64), generator=g).to(torch.bfloat16).cuda()
+    table = torch.full((1, -(-L // page)), -1, dtype=torch.int32, device="cuda")
+    table[0, -1] = 0                                        # only the last page is there: the others are not touched
+    kc = torch.zeros((1, page, 1, 64), dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros_like(kc)
+    rotation = binding.rotation_table(L, 64)
+    kv_len = torch.tensor([L], dtype=torch.int32, device="cuda")
+    q = binding.entmax_attn_paged_append(qkv[:, :1], qkv[:, 1:2], qkv[:, 2:], kc, vc, table, kv_len, rotation=rotation)
+    pos = torch.arange(L - 3, L)
+    i = torch.arange(32, dtype=torch.float64)
+    angle = pos.double()[:, None] * 10000.0 ** (-2 * i / 64)
+    x = qkv[:, :2].cpu().double()
+    turned = torch.cat([x[..., :32] * angle.cos()[:, None] - x[..., 32:] * angle.sin()[:, None],
+                        x[..., 32:] * angle.cos()[:, None] + x[..., :32] * angle.sin()[:, None]], -1)
+    # the table's own rounding (2^-24 of each cosine and sine) beside the arithmetic's
+    tol = 2.0 ** -8 * turned.abs() + 8 * 2.0 ** -24 * 2 * x.abs().amax(-1, keepdim=True)
+    assert bool(((q.cpu().double() - turned[:, :1]).abs() <= tol[:, :1]).all())
+    assert bool(((kc[0, pos % page].cpu().double() - turned[:, 1:]).abs() <= tol[:, 1:]).all())
+    assert torch.equal(vc[0, pos % page], qkv[:, 2:])
+
+
+def test_append_leaves_out_what_does_not_fit():
+    new, lens, H, KH, d, page = [2, 3, 1, 1], [30, 33, 20, 10], 4, 2, 64, 16
+    qkv, kc, vc, table, cu, kv_len = _append_problem(new, lens, H, KH, d, page)
+    before = kc.clone(), vc.clone()
+    table = table[:, :2].contiguous()                       # room for 32 tokens: the second sequence does not fit
+    bad = table.clone()
+    bad[2, 1] = kc.shape[0]                                 # the third one's page is not in the pool
+    q = torch.full((7, H, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    status = torch.zeros(binding.STATUS_WORDS, dtype=torch.int32, device="cuda")
+    binding.entmax_attn_paged_append(qkv[:, :H], qkv[:, H:H + KH], qkv[:, H + KH:], kc, vc, bad, kv_len, cu, q_out=q, status=status)
+    torch.cuda.synchronize()
+    assert int(status[0]) == binding.FLAG_BAD_LENGTH | binding.FLAG_BAD_PAGE
+    assert bool((q[2:5] == 9).all()) and torch.equal(q[:2], qkv[:2, :H]) and torch.equal(q[5:], qkv[5:, :H])
+    want = before[0].clone(), before[1].clone()
+    for b, t0, n, L in ((0, 0, 2, 30), (3, 6, 1, 10)):
+        for i in range(n):
+            p = L - n + i
+            want[0][table[b, p // page].long(), p % page] = qkv[t0 + i, H:H + KH]
+            want[1][table[b, p // page].long(), p % page] = qkv[t0 + i, H + KH:]
+    assert torch.equal(kc, want[0]) and torch.equal(vc, want[1])
+
+
+# ------------------------------------------------------------------------------------------------ together
+@pytest.mark.parametrize("H,KH,d,page", [(4, 2, 64, 16), (6, 6, 128, 32)])
+def test_prompt_chunks_then_single_tokens_equal_the_whole_sequence(H, KH, d, page):
+    """A prompt in two chunks, then tokens one by one, two sequences at different points: every output equals the full causal problem's row
+    (entmax_attn_fwd on the rotated tokens), within the two paths' tolerances for the same inputs."""
+    N, B = 150, 2
+    g = torch.Generator().manual_seed(11)
+    qkv = torch.randn((B, N, H + 2 * KH, d), generator=g).to(torch.bfloat16).cuda()
+    rotation = binding.rotation_table(N, d)
+    sc = [t.cuda() for t in _scales(H, 3, "length")]
+    pages = -(-N // page)
+    kc = torch.full((B * pages + 1, page, KH, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    vc = torch.full_like(kc, float("nan"))
+    table = torch.randperm(B * pages, generator=g).to(torch.int32).view(B, pages).cuda()
+    steps = [(64, 40), (50, 1), (1, 60), (1, 1)] + [(1, 1)] * 30
+    at = [0, 0]
+    rotated_q = torch.zeros((B, N, H, d), dtype=torch.bfloat16, device="cuda")
+    outs = torch.zeros((B, N, H, d), dtype=torch.bfloat16, device="cuda")
+    taus = torch.zeros((B, N, H), device="cuda")
+    for new in steps:
+        rows = torch.cat([qkv[b, at[b]:at[b] + new[b]] for b in range(B)])
+        cu = torch.tensor([0, new[0], sum(new)], dtype=torch.int32, device="cuda")
+        at = [at[b] + new[b] for b in range(B)]
+        kv_len = torch.tensor(at, dtype=torch.int32, device="cuda")
+        q = binding.entmax_attn_paged_append(rows[:, :H], rows[:, H:H + KH], rows[:, H + KH:], kc, vc, table, kv_len, cu, rotation=rotation)
+        o, tau, _ = binding.entmax_attn_paged_fwd(q, kc, vc, 1.5, table, kv_len, cu, *sc, max_q_len=max(new), max_kv_len=max(at))
+        for b, t0 in ((0, 0), (1, new[0])):
+            where = slice(at[b] - new[b], at[b])
+            rotated_q[b, where], outs[b, where], taus[b, where] = q[t0:t0 + new[b]], o[t0:t0 + new[b]], tau[t0:t0 + new[b]]
+    for b in range(B):
+        n = at[b]
+        flat = table[b].long()
+        k = kc[flat].flatten(0, 1)[:n].transpose(0, 1).repeat_interleave(H // KH, 0)[None].contiguous()
+        v = vc[flat].flatten(0, 1)[:n].transpose(0, 1).repeat_interleave(H // KH, 0)[None].contiguous()
+        q = rotated_q[b, :n].transpose(0, 1)[None].contiguous()
+        o, tau = binding.entmax_attn_fwd(q, k, v, 1.5, True, *sc)
+        for h in range(H):
+            ro, rt, to, tt, _, _ = paged.attend(q[0, h].cpu(), k[0, h].cpu(), v[0, h].cpu(), 0, 1.5, [s[h].cpu() for s in sc])
+            assert bool(((taus[b, :n, h].cpu().double() - rt).abs() <= tt).all())
+            assert bool(((outs[b, :n, h].cpu().double() - ro).abs() <= to).all())
+            assert bool(((tau[0, h].cpu().double() - taus[b, :n, h].cpu().double()).abs() <= 2 * tt).all())
+            assert bool(((o[0, h].cpu().double() - outs[b, :n, h].cpu().double()).abs() <= 2 * to).all())
