@@ -6,7 +6,6 @@ library is missing or a call is rejected, an exception is raised.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -291,6 +290,25 @@ def rotation_table(positions: int, rot_dim: int, base: float = 10000.0, device="
     return torch.cat([angle.cos(), angle.sin()], 1).to(torch.float32).to(device)
 
 
+# The paged calls sit in a serving loop, one of each per layer and step, where checking some forty shapes, strides and dtypes and filling in
+# the parameter structures took 20 of the 30 us a small call needed.  All of that depends on the tensors' layouts alone, so it is done
+# once per combination of layouts and looked up afterwards (nothing of the tensors themselves is kept).  Hashing the layouts costs as much as
+# the checks did, so they are found under a few of their numbers and compared.
+_layouts: dict = {}
+_LAYOUTS_KEPT = 512
+
+
+def _layout_of(*tensors):
+    return tuple([None if t is None else (t.dtype, t.shape, t.stride(), t.get_device()) for t in tensors])
+
+
+def _keep(where, key, value):
+    if len(_layouts) >= _LAYOUTS_KEPT:
+        _layouts.clear()
+    _layouts[where] = key, value
+    return value
+
+
 def _row_strides(name, x, heads, d):
     """(token, head) strides of a bf16 [tokens, heads, d] tensor; a dimension of one element has no stride of its own."""
     if x.dim() != 3 or x.dtype != torch.bfloat16 or x.shape[1] != heads or x.shape[2] != d or x.stride(2) != 1:
@@ -298,7 +316,7 @@ def _row_strides(name, x, heads, d):
     return x.stride(0) if x.shape[0] > 1 else heads * d, x.stride(1) if heads > 1 else d
 
 
-def _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, total_q, device):
+def _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, status, total_q, device):
     if k_cache.dim() != 4 or k_cache.dtype != torch.bfloat16 or k_cache.stride(3) != 1:
         raise EntmaxAttnError("%s: k_cache must be a bfloat16 [pages, page_size, kv_heads, head_dim] tensor, head_dim contiguous" % what)
     if v_cache.shape != k_cache.shape or v_cache.stride() != k_cache.stride() or v_cache.dtype != k_cache.dtype:
@@ -312,7 +330,9 @@ def _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, total_q, dev
         raise EntmaxAttnError("%s: cu_q must be a contiguous int32 [batch + 1] tensor" % what)
     if cu_q is None and B and total_q % B:
         raise EntmaxAttnError("%s: without cu_q the number of new tokens must be a multiple of the batch" % what)
-    for t in (k_cache, v_cache, block_table, kv_len, cu_q):
+    if status is not None and (status.dtype != torch.int32 or status.numel() < STATUS_WORDS or not status.is_contiguous()):
+        raise EntmaxAttnError("%s: status must be a contiguous int32 tensor of %d words" % (what, STATUS_WORDS))
+    for t in (k_cache, v_cache, block_table, kv_len, cu_q, status):
         if t is not None and t.device != device:
             raise EntmaxAttnError("%s: all tensors must be on one device" % what)
     P, ps, KH, D = k_cache.shape
@@ -320,23 +340,43 @@ def _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, total_q, dev
                       k_cache.stride(0) if P > 1 else ps * KH * D, k_cache.stride(1), k_cache.stride(2) if KH > 1 else D)
 
 
-def _check_scale(what, H, device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and (t.shape != (H,) or t.dtype != torch.float32 or not t.is_contiguous() or t.device != device):
-            raise EntmaxAttnError("%s: %s must be a contiguous float32 [%d] tensor on the device of q" % (what, name, H))
-
-
 def _on_device(device):
     """The launches go to the current device's context: made the tensors' own for the call where it is another."""
-    if device.type != "cuda":
+    if device < 0:
         raise EntmaxAttnError("CUDA tensors only (there is no CPU fallback)")
-    return torch.cuda.device(device) if device.index != torch._C._cuda_getDevice() else contextlib.nullcontext()
+    return torch.cuda.device(device) if device != torch._C._cuda_getDevice() else None
 
 
-def _check_status(what, status, device):
-    if status is not None and (status.dtype != torch.int32 or status.numel() < STATUS_WORDS or not status.is_contiguous() or
-                               status.device != device):
-        raise EntmaxAttnError("%s: status must be a contiguous int32 tensor of %d words on the device of q" % (what, STATUS_WORDS))
+def _call_on(device, fn, *args):
+    guard = _on_device(device)
+    if guard is None:
+        return fn(*args)
+    with guard:
+        return fn(*args)
+
+
+def _append_layout(what, q, k, v, k_cache, v_cache, block_table, kv_len, cu_q, rotation, interleaved, q_out, status):
+    T, KH, D = k.shape if k.dim() == 3 else (0, 0, 0)
+    ks, vs = _row_strides("k", k, KH, D), _row_strides("v", v, KH, D)
+    cache = _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, status, T, k.device)
+    if (cache.kv_heads, cache.head_dim) != (KH, D) or v.shape != k.shape or v.device != k.device:
+        raise EntmaxAttnError("%s: k, v and the cache disagree on tokens, kv_heads, head_dim or device" % what)
+    H, qs, os_ = 0, (D, D), (D, D)
+    if q is not None:
+        H = q.shape[1] if q.dim() == 3 else 0
+        qs = _row_strides("q", q, H, D)
+        os_ = (H * D, D) if q_out is None else _row_strides("q_out", q_out, H, D)
+        if q.shape[0] != T or q.device != k.device or q_out is not None and (q_out.shape != q.shape or q_out.device != k.device):
+            raise EntmaxAttnError("%s: q, q_out and k disagree on tokens or device" % what)
+    elif q_out is not None:
+        raise EntmaxAttnError("%s: q_out without q" % what)
+    rot_pos, rot = 0, 0
+    if rotation is not None:
+        if rotation.dim() != 2 or rotation.dtype != torch.float32 or not rotation.is_contiguous() or rotation.device != k.device:
+            raise EntmaxAttnError("%s: rotation must be a contiguous float32 [positions, rot_dim] tensor on the device of k" % what)
+        rot_pos, rot = rotation.shape
+    params = PagedAppendParams(T, H, rot, rot_pos, int(bool(interleaved)), *qs, *ks, *vs, *os_)
+    return ctypes.byref(cache), ctypes.byref(params), T, H, D
 
 
 def entmax_attn_paged_append(q, k, v, k_cache, v_cache, block_table, kv_len, cu_q=None, *, rotation=None, interleaved=False,
@@ -349,46 +389,44 @@ def entmax_attn_paged_append(q, k, v, k_cache, v_cache, block_table, kv_len, cu_
     are sequence b's (None: T / B each).  rotation: float32 [positions, rot_dim] (rotation_table) or None; interleaved: pairs
     (2i, 2i + 1) instead of (i, i + rot_dim / 2).  Returns the rotated q (q_out; may be q itself)."""
     what = "entmax_attn_paged_append"
-    T, KH, D = k.shape if k.dim() == 3 else (0, 0, 0)
-    ks, vs = _row_strides("k", k, KH, D), _row_strides("v", v, KH, D)
-    cache = _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, T, k.device)
-    if (cache.kv_heads, cache.head_dim) != (KH, D) or v.shape != k.shape or v.device != k.device:
-        raise EntmaxAttnError("%s: k, v and the cache disagree on tokens, kv_heads, head_dim or device" % what)
-    H, qs, os_ = 0, (D, D), (D, D)
-    if q is not None:
-        H = q.shape[1] if q.dim() == 3 else 0
-        qs = _row_strides("q", q, H, D)
-        if q_out is None:
-            q_out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
-        os_ = _row_strides("q_out", q_out, H, D)
-        if q.shape[0] != T or q_out.shape != q.shape or q.device != k.device or q_out.device != k.device:
-            raise EntmaxAttnError("%s: q, q_out and k disagree on tokens or device" % what)
-    elif q_out is not None:
-        raise EntmaxAttnError("%s: q_out without q" % what)
-    rot_pos, rot = 0, 0
-    if rotation is not None:
-        if rotation.dim() != 2 or rotation.dtype != torch.float32 or not rotation.is_contiguous() or rotation.device != k.device:
-            raise EntmaxAttnError("%s: rotation must be a contiguous float32 [positions, rot_dim] tensor on the device of k" % what)
-        rot_pos, rot = rotation.shape
-    _check_status(what, status, k.device)
+    where = (what, k.numel(), k_cache.numel(), block_table.numel())
+    key = (interleaved, _layout_of(q, k, v, k_cache, v_cache, block_table, kv_len, cu_q, rotation, q_out, status))
+    known = _layouts.get(where)
+    cache, params, T, H, D = known[1] if known is not None and known[0] == key else _keep(where, key, _append_layout(
+        what, q, k, v, k_cache, v_cache, block_table, kv_len, cu_q, rotation, interleaved, q_out, status))
+    device = k.get_device()
+    if q is not None and q_out is None:
+        q_out = q.new_empty((T, H, D))
     if T == 0:
         return q_out
-    params = PagedAppendParams(T, H, rot, rot_pos, int(bool(interleaved)), *qs, *ks, *vs, *os_)
-    with _on_device(k.device):
-        rc = load().entmax_attn_paged_append(ctypes.byref(cache), ctypes.byref(params), _ptr(q), _ptr(k), _ptr(v), _ptr(rotation),
-                                             _ptr(cu_q), _ptr(kv_len), _ptr(block_table), _ptr(q_out), _ptr(k_cache), _ptr(v_cache),
-                                             _ptr(status), _stream_ptr(stream))
+    rc = _call_on(device, lambda: load().entmax_attn_paged_append(
+        cache, params, _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(rotation), _ptr(cu_q), kv_len.data_ptr(), block_table.data_ptr(), _ptr(q_out),
+        k_cache.data_ptr(), v_cache.data_ptr(), _ptr(status), _stream_ptr(stream)))
     _check(rc, what)
     return q_out
 
 
-def _paged_params(q, alpha, sm_scale, max_q_len, max_kv_len):
-    T, H, D = q.shape if q.dim() == 3 else (0, 0, 0)
-    return PagedParams(T, H, int(max_q_len), int(max_kv_len), float(alpha), float(sm_scale), *_row_strides("q", q, H, D))
-
-
 def entmax_attn_paged_workspace_bytes(cache: PagedCache, params: PagedParams, uniform: bool) -> int:
     return int(load().entmax_attn_paged_workspace_bytes(ctypes.byref(cache), ctypes.byref(params), int(bool(uniform))))
+
+
+def _paged_layout(what, q, k_cache, v_cache, alpha, block_table, kv_len, cu_q, beta, gamma, delta, alibi_slopes, sm_scale, max_q_len,
+                  max_kv_len, o, tau, support_size, status):
+    T, H, D = q.shape if q.dim() == 3 else (0, 0, 0)
+    params = PagedParams(T, H, int(max_q_len), int(max_kv_len), float(alpha), float(sm_scale), *_row_strides("q", q, H, D))
+    device = q.device
+    cache = _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, status, T, device)
+    if cache.head_dim != D:
+        raise EntmaxAttnError("%s: q and the cache disagree on head_dim" % what)
+    for name, t in (("beta", beta), ("gamma", gamma), ("delta", delta), ("alibi_slopes", alibi_slopes)):
+        if t is not None and (t.shape != (H,) or t.dtype != torch.float32 or not t.is_contiguous() or t.device != device):
+            raise EntmaxAttnError("%s: %s must be a contiguous float32 [%d] tensor on the device of q" % (what, name, H))
+    for name, t, shape, dtype in (("o", o, (T, H, D), torch.bfloat16), ("tau", tau, (T, H), torch.float32),
+                                  ("support_size", support_size, (T, H), torch.int32)):
+        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.device != device):
+            raise EntmaxAttnError("%s: %s must be a contiguous %s %s tensor on the device of q" % (what, name, dtype, list(shape)))
+    # (0 bytes: parameters that the call itself refuses, with the reason)
+    return (ctypes.byref(cache), ctypes.byref(params), T, H, D, entmax_attn_paged_workspace_bytes(cache, params, cu_q is None) if T else 0)
 
 
 def entmax_attn_paged_fwd(q, k_cache, v_cache, alpha, block_table, kv_len, cu_q=None, beta=None, gamma=None, delta=None, *,
@@ -398,34 +436,28 @@ def entmax_attn_paged_fwd(q, k_cache, v_cache, alpha, block_table, kv_len, cu_q=
     entmax_attn_paged_append, H a multiple of the cache's kv_heads (query heads h * H / kv_heads .. share K/V head h).  One new
     token per sequence, a chunk, or whole prompts, mixed as they come.  max_q_len, max_kv_len: the most new tokens and the
     longest kv_len of the call, where the caller knows them (they size the workspace and the launches).
-    Returns (o [T, H, d], tau [T, H], support_size [T, H])."""
+    Returns (o [T, H, d], tau [T, H], support_size [T, H] or None where no tensor was given for it)."""
     what = "entmax_attn_paged_fwd"
-    params = _paged_params(q, alpha, sm_scale, max_q_len, max_kv_len)
-    T, H, D = q.shape
-    device = q.device
-    cache = _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, T, device)
-    if cache.head_dim != D:
-        raise EntmaxAttnError("%s: q and the cache disagree on head_dim" % what)
-    _check_scale(what, H, device, beta=beta, gamma=gamma, delta=delta, alibi_slopes=alibi_slopes)
-    _check_status(what, status, device)
-    o = torch.empty((T, H, D), dtype=q.dtype, device=device) if o is None else o
-    tau = torch.empty((T, H), dtype=torch.float32, device=device) if tau is None else tau
-    support_size = torch.empty((T, H), dtype=torch.int32, device=device) if support_size is None else support_size
-    for name, t, shape, dtype in (("o", o, (T, H, D), torch.bfloat16), ("tau", tau, (T, H), torch.float32),
-                                  ("support_size", support_size, (T, H), torch.int32)):
-        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.device != device:
-            raise EntmaxAttnError("%s: %s must be a contiguous %s %s tensor on the device of q" % (what, name, dtype, list(shape)))
+    where = (what, q.numel(), k_cache.numel(), block_table.numel(), max_q_len, max_kv_len)
+    key = (alpha, sm_scale, _layout_of(q, k_cache, v_cache, block_table, kv_len, cu_q, beta, gamma, delta, alibi_slopes, o, tau, support_size,
+                                       status))
+    known = _layouts.get(where)
+    cache, params, T, H, D, nbytes = known[1] if known is not None and known[0] == key else _keep(where, key, _paged_layout(
+        what, q, k_cache, v_cache, alpha, block_table, kv_len, cu_q, beta, gamma, delta, alibi_slopes, sm_scale, max_q_len, max_kv_len, o,
+        tau, support_size, status))
+    device = q.get_device()
+    if o is None:
+        o = q.new_empty((T, H, D))
+    if tau is None:
+        tau = q.new_empty((T, H), dtype=torch.float32)
     if T == 0:
         return o, tau, support_size
-    with _on_device(device):
-        if workspace is None:
-            nbytes = entmax_attn_paged_workspace_bytes(cache, params, cu_q is None)
-            # (0: the parameters are refused below, with the reason)
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        rc = load().entmax_attn_paged_fwd(ctypes.byref(cache), ctypes.byref(params), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(cu_q),
-                                          _ptr(kv_len), _ptr(block_table), _ptr(beta), _ptr(gamma), _ptr(delta), _ptr(alibi_slopes),
-                                          _ptr(o), _ptr(tau), _ptr(support_size), _ptr(workspace), workspace.numel(), _ptr(status),
-                                          _stream_ptr(stream))
+    if workspace is None:
+        workspace = q.new_empty(nbytes, dtype=torch.uint8)
+    rc = _call_on(device, lambda: load().entmax_attn_paged_fwd(
+        cache, params, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(cu_q), kv_len.data_ptr(), block_table.data_ptr(), _ptr(beta),
+        _ptr(gamma), _ptr(delta), _ptr(alibi_slopes), o.data_ptr(), tau.data_ptr(), _ptr(support_size), workspace.data_ptr(),
+        workspace.numel(), _ptr(status), _stream_ptr(stream)))
     _check(rc, what)
     return o, tau, support_size
 

@@ -59,19 +59,41 @@ __device__ __forceinline__ int find_seq(const PagedCache& c, int x, int div, int
   return lo;
 }
 
+// Sequence and first token of block `blk` of blocks of `tokens` new tokens, by the whole warp.  Block ids run over the sequences with one
+// to spare each: sequence b has the ids from cu_q[b] / tokens + b on, at least as many as it has blocks (then t0 >= n).
+__device__ __forceinline__ int find_block(const PagedCache& c, int blk, int tokens, int& t0) {
+  int b;
+  if (c.cu_q) {
+    b = find_seq(c, blk, tokens, 1);
+    t0 = (blk - (clamped_cu(c, b) / tokens + b)) * tokens;
+  } else {
+    const int per = (c.T / c.B + tokens - 1) / tokens;
+    b = blk / per;
+    t0 = (blk - b * per) * tokens;
+  }
+  return b;
+}
+
 // Host: checks of the cache description shared by the entry points (defined in paged_append.cu).
 int check_paged_cache(const entmax_attn_paged_cache* cache, int total_q, PagedCache* out);
 
 // ------------------------------------------------------------------------------------------- attention
-// Rows are handled in units of (block of new tokens, K/V head): block token t and query head kv_head * G + g form row
-// t * G + g of the unit, which the score kernels leave in the workspace as
-//   group_max[row][group]    maximum over the 32 keys of a group (Eq. 1's units, -inf where none is visible)
-//   scores[row][key]         y = (alpha-1) s of every key of the groups whose maximum is above some lower bound of
-//                            y_max - 1 (and possibly of others); the other groups are not written
-// Two kernels fill it.  "few": one block per sequence with at most few_rows rows, keys as the M side of the MMA.  "many":
-// blocks of kManyTiles * tile_tokens tokens of the longer chunks, query rows as the M side.
+// Rows are handled in units of (new tokens, K/V head): token t of the unit and query head kv_head * G + g form row t * G + g of it.  Of its
+// scores y = (alpha-1) s (Eq. 1's units) the score kernels leave in the workspace what can matter: every key above some lower bound of the
+// row's threshold is there.  Two kernels, two forms:
+//   "few": a unit is a sequence with at most few_rows rows.
+//       group_max[unit][group][row]   the maximum over each group of 32 keys (-inf: none visible)
+//       scores[row][key]              the scores of the groups whose maximum is above a bound of y_max - 1; other groups are not written
+//                                     (some may be)
+//   "many": a unit is a block of kManyTiles * tile_tokens tokens of a longer chunk, its keys are split among many_splits work items, and the
+//       item whose first K tile is lo keeps records of eight neighbouring keys, those with a value above the bound it had then, in key order:
+//       scores[row][256 lo + 8 i ..]  the values, before the scaling by |a|      record_key[row][32 lo + i]  the first key
+//       row_info[unit][split][row]    {number of records, the bound the item ended with, |a|, -}
+//       (room for every key: a row of flat logits keeps them all)
 constexpr int kGroupKeys = 32;
+constexpr int kManyKeys = 256;
 constexpr int kManyTiles = 2;
+constexpr int kFewSeqs = 256;   // sequences a launch of the "few" kernel takes
 
 struct PagedArgs {
   PagedCache c;
@@ -79,19 +101,22 @@ struct PagedArgs {
   int expo_class;
   float expo, alpha_m1, sm_scale;
   const float *beta, *gamma, *delta, *alibi;
+  int sms;
   int max_q, max_kv;          // longest chunk and sequence that are served (longer: FLAG_BAD_LENGTH)
   int few_rows;               // a sequence with n * G <= few_rows is the "few" kernel's (0: none is)
   int few_slots;              // row slots of a unit there
   int tile_tokens;            // "many": new tokens per 128-row tile, 128 / G
   int many_slots;             // row slots of a unit there
-  int many_blocks;            // bound on the number of blocks: T / block_tokens + B
-  int few_chunks;             // CTAs per unit of the "few" kernel
+  int many_blocks;            // bound on the number of blocks: ceil(T / block_tokens) + B - 1
   int many_splits;            // work items per unit of the "many" kernel, each a share of the keys
   size_t score_stride;        // floats per row of scores
-  int group_stride;           // floats per row of group_max
+  int groups, tiles;          // groups of 32 and tiles of 256 keys that a row has room for
   float* scores;
   float* group_max;
-  int32_t* counter;
+  int32_t* record_key;
+  float4* row_info;
+  int32_t* counters;          // [0]: work items handed out by the "many" kernel, [1]: rows in spilled
+  int32_t* spilled;           // rows whose candidates did not fit the list of the kernel that takes eight lanes per row
   __nv_bfloat16* o;
   float* tau;
   int32_t* support;
@@ -103,6 +128,17 @@ __device__ __forceinline__ bool paged_ok(const PagedArgs& a, const PagedSeq& s) 
   return s.len >= s.n && s.len <= a.max_kv && s.n <= a.max_q;
 }
 __device__ __forceinline__ bool paged_few(const PagedArgs& a, const PagedSeq& s) { return (long long)s.n * a.G <= a.few_rows; }
+
+// y^e and y^(e-1) of y >= 0, the exponent class known at compile time (kExpoGeneral: any)
+template <int EC>
+__device__ __forceinline__ void powers(float y, float expo, float& ye, float& ye1) {
+  pow_pair_c<EC>(y, y > 0.f, expo, ye, ye1);
+}
+// A lower bound of a threshold from an iterate that came from the left: a hair below it for the rounding
+__device__ __forceinline__ float bound_below(float tau) { return tau - 1e-5f * fmaxf(1.0f, fabsf(tau)); }
+
+// K tiles of 256 keys that work item `split` of a unit takes (of `tiles` that its last row sees): lo .. hi - 1
+__device__ __forceinline__ int split_begin(int tiles, int split, int splits) { return (int)((long long)tiles * split / splits); }
 
 // (alpha-1) c sm_scale of a query at position pos, c = delta + beta (ln n)^gamma with n = pos + 1 (delta for n = 1; 1 without
 // scale parameters)
@@ -128,7 +164,7 @@ __device__ __forceinline__ void write_unserved(const PagedArgs& a, const PagedSe
   }
 }
 
-cudaError_t launch_paged_few(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int unit0, int units,
+cudaError_t launch_paged_few(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int seq0, int seqs,
                              cudaStream_t stream);
 cudaError_t launch_paged_many(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int block0, int blocks,
                               cudaStream_t stream);

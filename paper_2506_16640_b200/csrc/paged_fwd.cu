@@ -1,10 +1,14 @@
-// Attention of new tokens over a paged key/value cache: the row solve behind the score kernels (paged_scores_sm100.cu), and the entry
+// Attention of new tokens over a paged key/value cache: the row solves behind the score kernels (paged_scores_sm100.cu), and the entry
 // points.
 //
-// A row of the workspace holds the maxima of its groups of 32 keys and the scores of the groups that can matter.  W warps take a
-// row: y_max from the maxima; the keys above y_max - 1 (App. A: tau >= y_max - 1) out of the groups whose maximum is above it, into shared
-// memory; Newton from the left on them; p = [y - tau]_+^e; O = sum_j p_j v_j as a gather of V rows through the block table.  A row with more
-// candidates than the list holds walks its groups in the workspace instead.  All sums are taken in a fixed order.
+// A row's largest score and a lower bound of its threshold come first: tau >= y_max - 1 (App. A), and the threshold of any subset of the keys is
+// a bound too.  The keys above the bound are collected from what the score kernels left, into shared memory; Newton from the left on them;
+// p = [y - tau]_+^e; O = sum_j p_j v_j as a gather of V rows through the block table (asked for from memory as soon as a key is a
+// candidate).  All sums are taken in a fixed order.
+//   rows8   eight lanes per row: a record or a group's 32 scores and a V row are a coalesced access of eight lanes, sums take three
+//           shuffles, and a warp has four rows' chains of dependent loads under way.  Rows with more than kList8 candidates are listed for
+//   row     a CTA per row, for those and for calls of few or very long rows.
+#include <atomic>
 #include <cmath>
 
 #include "paged.cuh"
@@ -13,87 +17,391 @@ namespace entmax {
 
 namespace {
 
-constexpr int kMaxNewtonP = 64;
 
-template <int PER>
-__device__ __forceinline__ void load_packed_row(const __nv_bfloat16* p, uint32_t (&w)[PER / 2]) {
-  if constexpr (PER == 4) {
-    const uint2 raw = *reinterpret_cast<const uint2*>(p);
-    w[0] = raw.x;
-    w[1] = raw.y;
-  } else {
-    w[0] = *reinterpret_cast<const uint32_t*>(p);
-  }
-}
-__device__ __forceinline__ float packed_at(const uint32_t* w, int e) {
-  return __uint_as_float((e & 1) ? (w[e >> 1] & 0xffff0000u) : (w[e >> 1] << 16));
-}
-
-template <int W>
-struct SolveShape {
-  static constexpr int kRowsPerCta = W == 1 ? 4 : 1;
-  static constexpr int kThreads = 32 * W * kRowsPerCta;
-  static constexpr int kSeg = W == 1 ? 512 : 256;          // list entries of a warp
+// Eight lanes' share of a V or O row: 16-byte pieces sl, sl + 8 (head_dim 128)
+template <int D>
+struct Share {
+  uint4 w[D / 64];
 };
-
-// The new token and head of row slot r of a unit
-struct RowOf {
-  PagedSeq s;
-  int b, kvh, tok, g;
-  bool served;
-};
-template <bool kMany>
-__device__ __forceinline__ RowOf row_of(const PagedArgs& a, int first, int unit, int r) {
-  RowOf w;
-  w.kvh = unit % a.c.KH;
-  const int at = first + unit / a.c.KH;
-  int t0 = 0;
-  if constexpr (kMany) {
-    const int block_tokens = kManyTiles * a.tile_tokens;
-    if (a.c.cu_q) {
-      w.b = find_seq(a.c, at, block_tokens, 1);
-      t0 = (at - (clamped_cu(a.c, w.b) / block_tokens + w.b)) * block_tokens;
-    } else {
-      const int per = (a.c.T / a.c.B + block_tokens - 1) / block_tokens;
-      w.b = at / per;
-      t0 = (at - w.b * per) * block_tokens;
+template <int D>
+__device__ __forceinline__ void add_share(float (&acc)[D / 8], float p, const Share<D>& x) {
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) {
+    const uint32_t w[4] = {x.w[c].x, x.w[c].y, x.w[c].z, x.w[c].w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc[8 * c + 2 * e] = fmaf(p, __uint_as_float(w[e] << 16), acc[8 * c + 2 * e]);
+      acc[8 * c + 2 * e + 1] = fmaf(p, __uint_as_float(w[e] & 0xffff0000u), acc[8 * c + 2 * e + 1]);
     }
-  } else {
-    w.b = at;
   }
-  w.served = w.b < a.c.B && t0 >= 0;
-  if (!w.served) return w;
-  w.s = paged_seq(a.c, w.b);
-  w.tok = t0 + r / a.G;
-  w.g = r % a.G;
-  w.served = w.tok < w.s.n && paged_ok(a, w.s) && paged_few(a, w.s) != kMany;
-  return w;
+}
+template <int D>
+__device__ __forceinline__ void store_share(__nv_bfloat16* row, int sl, const float (&acc)[D / 8]) {
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __nv_bfloat162 t = __floats2bfloat162_rn(acc[8 * c + 2 * e], acc[8 * c + 2 * e + 1]);
+      w[e] = *reinterpret_cast<const uint32_t*>(&t);
+    }
+    *reinterpret_cast<uint4*>(row + 64 * c + 8 * sl) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
 }
 
-template <int D, int W, bool kMany>
-__global__ void __launch_bounds__(SolveShape<W>::kThreads) paged_solve_kernel(const __grid_constant__ PagedArgs a,
-                                                                            const __nv_bfloat16* __restrict__ v, int first,
-                                                                            long long n_rows) {
-  pdl_begin();
-  using S = SolveShape<W>;
-  constexpr int PER = D / 32;
-  __shared__ float list_y[S::kRowsPerCta * W * S::kSeg];
-  __shared__ int list_j[S::kRowsPerCta * W * S::kSeg];
-  __shared__ float2 red[2][W];
-  __shared__ float opart[W == 1 ? 1 : W][D];
-  const int lane = threadIdx.x & 31;
-  const int warp = W == 1 ? 0 : threadIdx.x >> 5;          // of the row
-  const long long row = W == 1 ? (long long)blockIdx.x * S::kRowsPerCta + (threadIdx.x >> 5) : blockIdx.x;
-  if (row >= n_rows) return;
-  const int slots = kMany ? a.many_slots : a.few_slots;
-  const int unit = (int)(row / slots), r = (int)(row - (long long)unit * slots);
-  const RowOf w = row_of<kMany>(a, first, unit, r);
-  if (!w.served) return;
-  const int pos = w.s.len - w.s.n + w.tok;
-  const int groups = pos / kGroupKeys + 1;
-  const float* max_row = a.group_max + (size_t)row * a.group_stride;
-  const float* y_row = a.scores + (size_t)row * a.score_stride;
+// Where V row j of a sequence is, in elements from the K/V head's first (-1: its page is not in the pool)
+struct Pages {
+  const int32_t* table;
+  int shift, n_pages;
+  long long s_page, s_tok;
+  __device__ __forceinline__ long long at(int j) const {
+    const int page = table[j >> shift];
+    if ((unsigned)page >= (unsigned)n_pages) return -1;
+    return (long long)page * s_page + (long long)(j & ((1 << shift) - 1)) * s_tok;
+  }
+};
+__device__ __forceinline__ Pages pages_of(const PagedCache& c, int b) {
+  return Pages{c.table + (long long)b * c.table_stride, c.ps_shift, c.n_pages, c.s_page, c.s_tok};
+}
+// (a V row is one or two 128-byte lines)
+template <int D>
+__device__ __forceinline__ void prefetch_row(const __nv_bfloat16* p) {
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+  if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + 64));
+}
 
+// One step of the threshold iteration on the candidates from their sums.  Returns false when st.tau is final.  e >= 1: Newton on the e-norm,
+// from the left; the rounding of a long step over many keys can pass the root, and a step back from there lands at or before it.
+__device__ __forceinline__ bool solve_step(TauIter& st, float s0, float s1, int expo_class, float expo) {
+  if (expo < 1.0f) return tau_iter_update(st, s0, s1, expo_class, expo, 1e-7f);
+  if (!(s1 > 0.f)) return false;
+  const float step = threshold_step(s0, s1, expo_class, expo);
+  st.tau += step;
+  return fabsf(step) > 1e-7f * fmaxf(1.0f, fabsf(st.tau));
+}
+constexpr int kMaxSteps = 64;
+constexpr int kBoundSteps = 5;       // steps towards the threshold of the cells' maxima
+constexpr int kFewCandidateCells = 8;   // groups above y_max - 1 up to which that bound is not looked for
+
+// What the "many" kernel kept of a row: a list of records per work item that had keys of the row
+struct Records {
+  const float* values;                  // [256 lo + 8 i]
+  const int32_t* keys;                  // [32 lo + i]
+  const float4* info;                   // [split][slot]
+  int slots, splits, tiles;             // tiles: of the unit
+  __device__ __forceinline__ int begin(int split) const { return split_begin(tiles, split, splits); }
+};
+__device__ __forceinline__ Records records_of(const PagedArgs& a, const PagedSeq& s, int t0, int unit, int r, size_t row) {
+  const int last = min(t0 + kManyTiles * a.tile_tokens, s.n) - 1;
+  return Records{a.scores + row * a.score_stride, a.record_key + row * (size_t)(a.tiles * 32),
+                 a.row_info + (size_t)unit * a.many_splits * a.many_slots + r, a.many_slots, a.many_splits,
+                 (s.len - s.n + last) / kManyKeys + 1};
+}
+
+// ================================================================================================ rows8
+constexpr int kList8 = 96;           // candidates of a row
+constexpr int kSteps8 = 8;           // loads of eight groups, or of four records, whose maxima stay in registers
+constexpr int kWarps8 = 8;
+constexpr int kRows8 = 4 * kWarps8;  // rows of a CTA
+
+__device__ __forceinline__ float sum8(float x) {
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+template <int D, int EC, bool kMany>
+__global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __grid_constant__ PagedArgs a,
+                                                                      const __nv_bfloat16* __restrict__ v, int first, int units) {
+  pdl_begin();
+  __shared__ float list_y[kRows8][kList8];
+  __shared__ long long list_at[kRows8][kList8];
+  const int lane = threadIdx.x & 31, sl = lane & 7, sub = lane >> 3, sub_bit = 8 * sub;
+  const int slots = kMany ? a.many_slots : a.few_slots;
+  const int cta_row = (threadIdx.x >> 3);
+  int unit, r;
+  if constexpr (kMany) {
+    const int per = (slots + kRows8 - 1) / kRows8;         // CTAs of a unit
+    unit = blockIdx.x / per;
+    r = (blockIdx.x - unit * per) * kRows8 + cta_row;
+  } else {
+    const long long row = (long long)blockIdx.x * kRows8 + cta_row;
+    unit = (int)(row / slots);
+    r = (int)(row - (long long)unit * slots);
+  }
+  // ---- which row this is
+  int b, t0 = 0;
+  const int kvh = unit % a.c.KH;
+  b = first + unit / a.c.KH;
+  if constexpr (kMany) b = find_block(a.c, b, kManyTiles * a.tile_tokens, t0);
+  bool live = unit < units && r < slots && b < a.c.B && t0 >= 0;
+  PagedSeq s = {0, 0, 0};
+  if (live) s = paged_seq(a.c, b);
+  const int tok = t0 + r / a.G;
+  live = live && tok < s.n && paged_ok(a, s) && paged_few(a, s) != kMany;
+  if (!__any_sync(0xffffffffu, live)) return;
+  const int pos = s.len - s.n + tok;
+  const size_t row = (size_t)unit * slots + r;
+  const Pages pages = pages_of(a.c, live ? b : 0);
+  const __nv_bfloat16* v_head = v + (long long)kvh * a.c.s_head;
+  float* my_y = list_y[cta_row];
+  long long* my_at = list_at[cta_row];
+  int cnt = 0;
+  // appends those of this lane's four keys from `key` on that are above the bound to the row's list, lane by lane
+  auto append = [&](const float (&y)[4], int key, float floor_y) {
+    int mine = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine += y[e] > floor_y ? 1 : 0;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, upto, o, 8);
+      if (sl >= o) upto += up;
+    }
+    int at = cnt + upto - mine;
+    cnt += __shfl_sync(0xffffffffu, upto, 7, 8);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (y[e] > floor_y) {
+        if (at < kList8) {
+          const long long off = pages.at(key + e);
+          if (off >= 0) prefetch_row<D>(v_head + off);
+          my_y[at] = y[e];
+          my_at[at] = off;
+        }
+        ++at;
+      }
+    }
+  };
+  // A threshold of maxima of different keys alone, by a few steps from the left of floor_y (any iterate is a bound; a hair below it for the
+  // rounding).  for_maxima(f): f(a maximum) for all of this lane's.  c = 1, alpha = 1.5, 32768 keys N(0, 1): 585 keys above
+  // y_max - 1, about 50 above the bound of the maxima of 128 cells.
+  auto raise = [&](float floor_y, int few, auto&& for_maxima) -> float {
+    if (a.expo < 1.0f) return floor_y;
+    int n = 0;
+    for_maxima([&](float m) { n += m > floor_y ? 1 : 0; });
+    n = (int)sum8((float)n);
+    if (!__any_sync(0xffffffffu, n > few)) return floor_y;
+    float tau = floor_y;
+    for (int it = 0; it < kBoundSteps; ++it) {
+      float s0 = 0.f, s1 = 0.f;
+      for_maxima([&](float m) {
+        float ye, ye1;
+        powers<EC>(fmaxf(m - tau, 0.f), a.expo, ye, ye1);
+        s0 += ye;
+        s1 += ye1;
+      });
+      s0 = sum8(s0);
+      s1 = sum8(s1);
+      const bool go = s0 > 1.01f && s1 > 0.f;
+      if (go) tau += threshold_step(s0, s1, EC, a.expo);
+      if (!__any_sync(0xffffffffu, go)) break;
+    }
+    return fmaxf(floor_y, bound_below(tau));
+  };
+
+  // ---- candidates; loops run for the longest of the warp's four rows
+  float ymax = -INFINITY, floor_y;
+  if constexpr (kMany) {
+    const Records rec = records_of(a, s, t0, unit, r, row);
+    int splits = 0;                                         // work items that had keys of the row
+    if (live)
+      while (splits < rec.splits && rec.begin(splits) <= pos / kManyKeys) ++splits;
+    float mag = 0.f, bound = -INFINITY;
+    auto count = [&](int i) {                               // records of item i (0 where there was none)
+      if (i >= splits || rec.begin(i) == rec.begin(i + 1)) return 0;
+      const float4 info = rec.info[(size_t)i * rec.slots];
+      mag = info.z;
+      bound = fmaxf(bound, info.y);
+      return __float_as_int(info.x);
+    };
+    // f(this lane's four values, its first key) for every four records: two lanes to a record
+    const int n_first = count(0);
+    const int most_splits = __reduce_max_sync(0xffffffffu, splits);
+    float4 kept[kSteps8];
+#pragma unroll
+    for (int i = 0; i < kSteps8; ++i) {
+      const int at = 4 * i + (sl >> 1);
+      kept[i] = at < n_first ? *reinterpret_cast<const float4*>(rec.values + 8 * at + 4 * (sl & 1))
+                             : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    }
+    auto scaled = [&](const float4& z, float (&y)[4]) {
+      y[0] = mag * z.x; y[1] = mag * z.y; y[2] = mag * z.z; y[3] = mag * z.w;
+    };
+    auto for_records = [&](auto&& f) {
+      for (int i = 0; i < most_splits; ++i) {
+        const int n = i == 0 ? n_first : count(i), lo = i < splits ? rec.begin(i) : 0;
+        const int steps = (__reduce_max_sync(0xffffffffu, n) + 3) / 4;
+        float y[4];
+        int st = 0;
+        if (i == 0) {
+#pragma unroll
+          for (int u = 0; u < kSteps8; ++u) {
+            if (u < steps) {
+              const int at = 4 * u + (sl >> 1);
+              scaled(kept[u], y);
+              f(y, lo * 32 + at, at < n);
+            }
+          }
+          st = kSteps8;
+        }
+        for (; st < steps; ++st) {
+          const int at = 4 * st + (sl >> 1);
+          float4 z = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+          if (at < n) z = *reinterpret_cast<const float4*>(rec.values + (size_t)lo * kManyKeys + 8 * at + 4 * (sl & 1));
+          scaled(z, y);
+          f(y, lo * 32 + at, at < n);
+        }
+      }
+    };
+    for_records([&](const float (&y)[4], int, bool) { ymax = fmaxf(ymax, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))); });
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) ymax = fmaxf(ymax, __shfl_xor_sync(0xffffffffu, ymax, o));
+    floor_y = fmaxf(ymax - 1.0f, bound);
+    floor_y = raise(floor_y, kList8 / 4, [&](auto&& f) {
+      for_records([&](const float (&y)[4], int, bool) { f(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))); });
+    });
+    for_records([&](const float (&y)[4], int at, bool on) {
+      const bool any = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])) > floor_y;
+      if (!__any_sync(0xffffffffu, any)) return;
+      append(y, any && on ? rec.keys[at] + 4 * (sl & 1) : 0, floor_y);
+    });
+  } else {
+    const int groups = live ? pos / kGroupKeys + 1 : 0;
+    const float* max_row = a.group_max + (size_t)unit * a.groups * slots + r;
+    const float* y_row = a.scores + row * a.score_stride;
+    const int steps = (__reduce_max_sync(0xffffffffu, groups) + 7) / 8;
+    float kept[kSteps8];
+#pragma unroll
+    for (int i = 0; i < kSteps8; ++i) {
+      const int g = 8 * i + sl;
+      kept[i] = g < groups ? max_row[(size_t)g * slots] : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps8; ++i) ymax = fmaxf(ymax, kept[i]);
+    for (int i = kSteps8; i < steps; i += 4) {
+      float m[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int g = 8 * (i + u) + sl;
+        m[u] = g < groups ? max_row[(size_t)g * slots] : -INFINITY;
+      }
+      ymax = fmaxf(ymax, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) ymax = fmaxf(ymax, __shfl_xor_sync(0xffffffffu, ymax, o));
+    // f(this lane's maximum of groups 8 i .. 8 i + 7, i)
+    auto for_groups = [&](auto&& f) {
+#pragma unroll
+      for (int i = 0; i < kSteps8; ++i)
+        if (i < steps) f(kept[i], i);
+      for (int i = kSteps8; i < steps; ++i) {
+        const int g = 8 * i + sl;
+        f(g < groups ? max_row[(size_t)g * slots] : -INFINITY, i);
+      }
+    };
+    floor_y = raise(ymax - 1.0f, kFewCandidateCells, [&](auto&& f) { for_groups([&](float m, int) { f(m); }); });
+    for_groups([&](float m, int i) {
+      unsigned bits = (__ballot_sync(0xffffffffu, m > floor_y) >> sub_bit) & 0xffu;
+      while (__any_sync(0xffffffffu, bits != 0u)) {
+        const int key0 = (8 * i + __ffs(bits) - 1) * kGroupKeys + 4 * sl;
+        float4 y4 = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (bits) y4 = *reinterpret_cast<const float4*>(y_row + key0);
+        bits &= bits - 1;
+        const float y[4] = {y4.x, y4.y, y4.z, y4.w};
+        append(y, key0, floor_y);
+      }
+    });
+  }
+  if (live && cnt > kList8) {
+    if (sl == 0) a.spilled[atomicAdd(a.counters + 1, 1)] = (int)row;
+    live = false;
+  }
+  if (!live) cnt = 0;
+  __syncwarp();
+
+  // ---- threshold
+  const int longest = __reduce_max_sync(0xffffffffu, cnt);
+  TauIter st;
+  st.tau = st.lo = floor_y;
+  st.hi = ymax;
+  bool done = !live;
+  for (int it = 0; it < kMaxSteps; ++it) {
+    float s0 = 0.f, s1 = 0.f;
+    for (int e = sl; e < longest; e += 8) {
+      float ye, ye1;
+      powers<EC>(e < cnt ? fmaxf(my_y[e] - st.tau, 0.f) : 0.f, a.expo, ye, ye1);
+      s0 += ye;
+      s1 += ye1;
+    }
+    s0 = sum8(s0);
+    s1 = sum8(s1);
+    if (!done) done = !solve_step(st, s0, s1, EC, a.expo);
+    if (__all_sync(0xffffffffu, done)) break;
+  }
+  const float tau = st.tau;
+  int support = 0;
+  for (int e = sl; e < cnt; e += 8) {
+    const float d = fmaxf(my_y[e] - tau, 0.f);
+    float p, p1;
+    powers<EC>(d, a.expo, p, p1);
+    support += d > 0.f ? 1 : 0;
+    my_y[e] = my_at[e] >= 0 ? p : 0.f;                      // (a page that is not there counts as zeros)
+  }
+  support = (int)sum8((float)support);
+  __syncwarp();
+
+  // ---- O = sum_j p_j v_j, four V rows of each of the warp's rows in flight
+  float acc[D / 8];
+#pragma unroll
+  for (int e = 0; e < D / 8; ++e) acc[e] = 0.f;
+  for (int e0 = 0; e0 < cnt; e0 += 4) {
+    float p[4];
+    Share<D> x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      p[u] = e0 + u < cnt ? my_y[e0 + u] : 0.f;
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        x[u].w[c] = make_uint4(0u, 0u, 0u, 0u);
+        if (p[u] > 0.f) x[u].w[c] = *reinterpret_cast<const uint4*>(v_head + my_at[e0 + u] + 64 * c + 8 * sl);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) add_share<D>(acc, p[u], x[u]);
+  }
+  if (live) {
+    const size_t out = (size_t)(s.q0 + tok) * a.H + kvh * a.G + r % a.G;
+    store_share<D>(a.o + out * D, sl, acc);
+    if (sl == 0) {
+      a.tau[out] = tau;
+      if (a.support) a.support[out] = support;
+    }
+  }
+}
+
+// ================================================================================================== row
+constexpr int kRowWarps = 8;
+constexpr int kSeg = 256;            // list entries of a warp
+constexpr int kChunks = 8;           // chunks of 32 groups of a warp whose maxima stay in shared memory
+
+// kSpilled: the rows listed by rows8, by CTAs that stay; otherwise a CTA for every row slot
+template <int D, bool kMany, bool kSpilled>
+__global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_kernel(const __grid_constant__ PagedArgs a,
+                                                                     const __nv_bfloat16* __restrict__ v, int first) {
+  pdl_begin();
+  constexpr int W = kRowWarps;
+  __shared__ float list_y[W][kSeg];
+  __shared__ int list_j[W][kSeg];
+  __shared__ float maxima[W][kChunks * 32];
+  __shared__ float2 red[2][W];
+  __shared__ float opart[W][D];
+  const int lane = threadIdx.x & 31, sl = lane & 7, warp = threadIdx.x >> 5;
+  const int slots = kMany ? a.many_slots : a.few_slots;
+  const int n_rows = kSpilled ? a.counters[1] : 0;
+  float* my_max = maxima[warp];
+  float* my_y = list_y[warp];
+  int* my_j = list_j[warp];
   int red_slot = 0;
   // sums over the row's warps in a fixed order; every thread gets them
   auto row_sum2 = [&](float x, float y) {
@@ -102,198 +410,324 @@ __global__ void __launch_bounds__(SolveShape<W>::kThreads) paged_solve_kernel(co
       x += __shfl_xor_sync(0xffffffffu, x, o);
       y += __shfl_xor_sync(0xffffffffu, y, o);
     }
-    if constexpr (W > 1) {
-      if (lane == 0) red[red_slot][warp] = make_float2(x, y);
-      __syncthreads();
-      x = 0.f; y = 0.f;
+    if (lane == 0) red[red_slot][warp] = make_float2(x, y);
+    __syncthreads();
+    x = 0.f; y = 0.f;
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        x += red[red_slot][i].x;
-        y += red[red_slot][i].y;
-      }
-      red_slot ^= 1;
+    for (int i = 0; i < W; ++i) {
+      x += red[red_slot][i].x;
+      y += red[red_slot][i].y;
     }
+    red_slot ^= 1;
     return make_float2(x, y);
   };
 
-  // ---- y_max; a warp looks at 32 groups together
-  float ymax = -INFINITY;
-  for (int g0 = warp * 32; g0 < groups; g0 += 32 * W * 4) {
-    float m[4];
+  for (int n = blockIdx.x;; n += gridDim.x) {
+    if (kSpilled && n >= n_rows) break;
+    const int row = kSpilled ? a.spilled[n] : n;
+    const int unit = row / slots, r = row - unit * slots;
+    // ---- which row this is
+    int t0 = 0;
+    const int kvh = unit % a.c.KH;
+    int b = first + unit / a.c.KH;
+    if constexpr (kMany) b = find_block(a.c, b, kManyTiles * a.tile_tokens, t0);
+    if (b >= a.c.B || t0 < 0) break;                       // (no row; never so for listed ones)
+    const PagedSeq s = paged_seq(a.c, b);
+    const int tok = t0 + r / a.G;
+    if (tok >= s.n || !paged_ok(a, s) || paged_few(a, s) == kMany) break;
+    const int pos = s.len - s.n + tok;
+    const Pages pages = pages_of(a.c, b);
+    const __nv_bfloat16* v_head = v + (long long)kvh * a.c.s_head;
+    const float* y_row = a.scores + (size_t)row * a.score_stride;
+    float ymax = -INFINITY, floor_y = -INFINITY;
+
+    // for_keys(f): f(y, key) with a key per lane (y = -inf: none) for all keys of this warp that are kept and can be in the support
+    const int groups = pos / kGroupKeys + 1;
+    const float* max_row = a.group_max + (size_t)unit * a.groups * slots + r;
+    // few: group g is warp g mod W's, 32 of a warp's groups are a chunk (so that short rows and runs of neighbouring candidates are
+    // spread over the warps)
+    const int chunks = (groups + 32 * W - 1) / (32 * W);
+    auto max_at = [&](int i) -> float {                    // this lane's group of the warp's chunk i
+      if (i < kChunks) return my_max[i * 32 + lane];
+      const int g = (i * 32 + lane) * W + warp;
+      return g < groups ? max_row[(size_t)g * slots] : -INFINITY;
+    };
+    Records rec;
+    if constexpr (kMany) rec = records_of(a, s, t0, unit, r, row);
+    auto for_keys = [&](auto&& f) {
+      if constexpr (!kMany) {
+        for (int i = 0; i < chunks; ++i) {
+          unsigned todo = __ballot_sync(0xffffffffu, max_at(i) > floor_y);
+          while (todo) {
+            int at[4];
+            float y[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int g = g0 + u * 32 * W + lane;
-      m[u] = g < groups ? max_row[g] : -INFINITY;
+            for (int u = 0; u < 4; ++u) {
+              at[u] = -1;
+              y[u] = -INFINITY;
+              if (todo) {
+                at[u] = ((i * 32 + __ffs(todo) - 1) * W + warp) * kGroupKeys + lane;
+                todo &= todo - 1;
+                y[u] = y_row[at[u]];
+              }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              if (at[u] >= 0) f(y[u], at[u]);
+          }
+        }
+      } else {
+        // four records of a work item are a warp's step
+        for (int i = 0; i < rec.splits && rec.begin(i) <= pos / kManyKeys; ++i) {
+          const int lo = rec.begin(i);
+          if (lo == rec.begin(i + 1)) continue;
+          const float4 info = rec.info[(size_t)i * rec.slots];
+          const int n = __float_as_int(info.x);
+          for (int st = 4 * warp; st < n; st += 16 * W) {
+            float y[4];
+            int key[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int at = st + 4 * W * u + (lane >> 3);
+              y[u] = -INFINITY;
+              key[u] = 0;
+              if (at < n) {
+                y[u] = info.z * y_row[(size_t)lo * kManyKeys + 8 * at + sl];
+                key[u] = rec.keys[lo * 32 + at] + sl;
+              }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              if (st + 4 * W * u < n) f(y[u], key[u]);
+          }
+        }
+      }
+    };
+
+    // ---- y_max
+    if constexpr (!kMany) {
+      float m[kChunks];
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+        const int g = (i * 32 + lane) * W + warp;
+        m[i] = g < groups ? max_row[(size_t)g * slots] : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+        my_max[i * 32 + lane] = m[i];
+        ymax = fmaxf(ymax, m[i]);
+      }
+      for (int i = kChunks; i < chunks; ++i) ymax = fmaxf(ymax, max_at(i));
+    } else {
+      for_keys([&](float y, int) { ymax = fmaxf(ymax, y); });
     }
-    ymax = fmaxf(ymax, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
-  }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) ymax = fmaxf(ymax, __shfl_xor_sync(0xffffffffu, ymax, o));
-  if constexpr (W > 1) {
-    if (lane == 0) red[1][warp].x = ymax;
+    for (int o = 16; o > 0; o >>= 1) ymax = fmaxf(ymax, __shfl_xor_sync(0xffffffffu, ymax, o));
+    if (lane == 0) red[red_slot][warp].x = ymax;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < W; ++i) ymax = fmaxf(ymax, red[1][i].x);
-  }
-  const float floor_y = ymax - 1.0f;
+    for (int i = 0; i < W; ++i) ymax = fmaxf(ymax, red[red_slot][i].x);
+    red_slot ^= 1;
+    floor_y = ymax - 1.0f;
+    if constexpr (kMany) {
+      for (int i = 0; i < rec.splits && rec.begin(i) <= pos / kManyKeys; ++i)
+        if (rec.begin(i) < rec.begin(i + 1)) floor_y = fmaxf(floor_y, rec.info[(size_t)i * rec.slots].y);
+    }
 
-  // f(y of 32 keys, first key) for every group of this warp that can hold a key of the support, four in flight
-  auto for_groups = [&](auto&& f) {
-    for (int g0 = warp * 32; g0 < groups; g0 += 32 * W) {
-      const int g = g0 + lane;
-      unsigned todo = __ballot_sync(0xffffffffu, g < groups && max_row[g] > floor_y);
-      while (todo) {
-        int at[4];
-        float y[4];
+    // ---- the threshold of the groups' largest keys as a bound (see rows8)
+    if (!kMany && a.expo >= 1.0f) {
+      int cand = 0;
+      for (int i = 0; i < chunks; ++i) cand += __popc(__ballot_sync(0xffffffffu, max_at(i) > floor_y));
+      cand = (int)row_sum2(lane == 0 ? (float)cand : 0.f, 0.f).x;
+      float tau = floor_y;
+      for (int it = 0; it < kBoundSteps && cand > kFewCandidateCells; ++it) {
+        float s0 = 0.f, s1 = 0.f;
+        for (int i = 0; i < chunks; ++i) {
+          const float d = max_at(i) - tau;
+          if (d > 0.f) {
+            float ye, ye1;
+            pow_pair(d, a.expo_class, a.expo, ye, ye1);
+            s0 += ye;
+            s1 += ye1;
+          }
+        }
+        const float2 sum = row_sum2(s0, s1);
+        if (!(sum.x > 1.01f) || !(sum.y > 0.f)) break;
+        tau += threshold_step(sum.x, sum.y, a.expo_class, a.expo);
+      }
+      floor_y = fmaxf(floor_y, bound_below(tau));
+    }
+
+    // ---- candidates
+    int cnt = 0;
+    for_keys([&](float y, int key) {
+      const unsigned m = __ballot_sync(0xffffffffu, y > floor_y);
+      const int at = cnt + __popc(m & ((1u << lane) - 1u));
+      if (y > floor_y && at < kSeg) {
+        my_y[at] = y;
+        my_j[at] = key;
+        const long long off = pages.at(key);
+        if (off >= 0) prefetch_row<D>(v_head + off);
+      }
+      cnt += __popc(m);
+    });
+    const bool walk = __syncthreads_or(cnt > kSeg);         // more than the lists hold: the kept keys are walked every time
+
+    // ---- threshold
+    TauIter st;
+    st.tau = st.lo = floor_y;
+    st.hi = ymax;
+    for (int it = 0; it < kMaxSteps; ++it) {
+      float s0 = 0.f, s1 = 0.f;
+      auto add = [&](float y) {
+        const float d = y - st.tau;
+        if (d > 0.f) {
+          float ye, ye1;
+          pow_pair(d, a.expo_class, a.expo, ye, ye1);
+          s0 += ye;
+          s1 += ye1;
+        }
+      };
+      if (!walk) {
+        for (int e = lane; e < cnt; e += 32) add(my_y[e]);
+      } else {
+        for_keys([&](float y, int) { add(y); });
+      }
+      const float2 sum = row_sum2(s0, s1);
+      if (!solve_step(st, sum.x, sum.y, a.expo_class, a.expo)) break;
+    }
+    const float tau = st.tau;
+
+    // ---- O = sum_j p_j v_j: a key per eight lanes, sixteen V rows of a warp in flight
+    float acc[D / 8];
+#pragma unroll
+    for (int e = 0; e < D / 8; ++e) acc[e] = 0.f;
+    int support = 0;
+    auto gather = [&](float y, int j) {                     // a key per lane (y = -inf: none)
+      const float d = y - tau;
+      float p = 0.f, p1;
+      long long off = -1;
+      if (d > 0.f) {
+        pow_pair(d, a.expo_class, a.expo, p, p1);
+        off = pages.at(j);
+      }
+      const unsigned m = __ballot_sync(0xffffffffu, d > 0.f);
+      support += __popc(m);
+      // (the eight lanes of a key take the set bits of their own octet of the mask, so no bit is looked for twice)
+#pragma unroll
+      for (int e0 = 0; e0 < 8; e0 += 4) {
+        if (((m >> e0) & 0x0f0f0f0fu) == 0u) continue;
+        float px[4];
+        Share<D> x[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          at[u] = -1;
-          y[u] = -INFINITY;
-          if (todo) {
-            at[u] = (g0 + __ffs(todo) - 1) * kGroupKeys;
-            todo &= todo - 1;
-            y[u] = y_row[at[u] + lane];
+          const int src = (lane & 24) + e0 + u;
+          px[u] = __shfl_sync(0xffffffffu, p, src);
+          const long long at = __shfl_sync(0xffffffffu, off, src);
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) {
+            x[u].w[c] = make_uint4(0u, 0u, 0u, 0u);
+            if (at >= 0) x[u].w[c] = *reinterpret_cast<const uint4*>(v_head + at + 64 * c + 8 * sl);
           }
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (at[u] >= 0) f(y[u], at[u]);
-      }
-    }
-  };
-
-  // ---- candidates
-  const int seg = (W == 1 ? (int)(threadIdx.x >> 5) : warp) * S::kSeg;
-  int cnt = 0;
-  for_groups([&](float y, int key0) {
-    const unsigned m = __ballot_sync(0xffffffffu, y > floor_y);
-    const int at = cnt + __popc(m & ((1u << lane) - 1u));
-    if (y > floor_y && at < S::kSeg) {
-      list_y[seg + at] = y;
-      list_j[seg + at] = key0 + lane;
-    }
-    cnt += __popc(m);
-  });
-  bool spilled = cnt > S::kSeg;
-  if constexpr (W > 1) spilled = __syncthreads_or(spilled);
-  __syncwarp();
-
-  // ---- threshold: Newton from the left on f(tau) = sum [y - tau]_+^e - 1 (bracketed for e < 1)
-  TauIter st;
-  st.tau = st.lo = floor_y;
-  st.hi = ymax;
-  for (int it = 0; it < kMaxNewtonP; ++it) {
-    float s0 = 0.f, s1 = 0.f;
-    auto add = [&](float y) {
-      const float d = y - st.tau;
-      if (d > 0.f) {
-        float ye, ye1;
-        pow_pair(d, a.expo_class, a.expo, ye, ye1);
-        s0 += ye;
-        s1 += ye1;
+        for (int u = 0; u < 4; ++u) add_share<D>(acc, px[u], x[u]);
       }
     };
-    if (!spilled) {
-      for (int e = lane; e < cnt; e += 32) add(list_y[seg + e]);
-    } else {
-      for_groups([&](float y, int) { add(y); });
-    }
-    const float2 s = row_sum2(s0, s1);
-    if (!tau_iter_update(st, s.x, s.y, a.expo_class, a.expo, 1e-7f)) break;
-  }
-  const float tau = st.tau;
-
-  // ---- O = sum_j p_j v_j, four V rows in flight
-  float acc[PER];
-#pragma unroll
-  for (int e = 0; e < PER; ++e) acc[e] = 0.f;
-  int support = 0;
-  const __nv_bfloat16* v_head = v + (long long)w.kvh * a.c.s_head + lane * PER;
-  const int32_t* pages = a.c.table + (long long)w.b * a.c.table_stride;
-  auto gather = [&](float y, int j) {                       // a key per lane (y = -inf: none)
-    const float d = y - tau;
-    float p = 0.f, p1;
-    long long off = -1;
-    if (d > 0.f) {
-      pow_pair(d, a.expo_class, a.expo, p, p1);
-      const int page = pages[j >> a.c.ps_shift];
-      if ((unsigned)page < (unsigned)a.c.n_pages)
-        off = (long long)page * a.c.s_page + (long long)(j & ((1 << a.c.ps_shift) - 1)) * a.c.s_tok;
-    }
-    unsigned m = __ballot_sync(0xffffffffu, d > 0.f);
-    support += __popc(m);
-    while (m) {
-      float pj[4];
-      uint32_t vw[4][PER / 2];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int src = m ? __ffs(m) - 1 : 0;
-        pj[u] = __shfl_sync(0xffffffffu, p, src);
-        const long long at = __shfl_sync(0xffffffffu, off, src);
-#pragma unroll
-        for (int e = 0; e < PER / 2; ++e) vw[u][e] = 0u;
-        if (m && at >= 0) load_packed_row<PER>(v_head + at, vw[u]);
-        m &= m - 1;
+    if (!walk) {
+      for (int e0 = 0; e0 < cnt; e0 += 32) {
+        const int e = e0 + lane;
+        gather(e < cnt ? my_y[e] : -INFINITY, e < cnt ? my_j[e] : 0);
       }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int e = 0; e < PER; ++e) acc[e] = fmaf(pj[u], packed_at(vw[u], e), acc[e]);
+    } else {
+      for_keys([&](float y, int key) { gather(y, key); });
     }
-  };
-  if (!spilled) {
-    for (int e0 = 0; e0 < cnt; e0 += 32) {
-      const int e = e0 + lane;
-      gather(e < cnt ? list_y[seg + e] : -INFINITY, e < cnt ? list_j[seg + e] : 0);
-    }
-  } else {
-    for_groups([&](float y, int key0) { gather(y, key0 + lane); });
-  }
-
-  const size_t out = (size_t)(w.s.q0 + w.tok) * a.H + w.kvh * a.G + w.g;
-  if constexpr (W == 1) {
-    store_slice<PER>(a.o + out * D + lane * PER, acc);
-    if (lane == 0) {
-      a.tau[out] = tau;
-      if (a.support) a.support[out] = support;
-    }
-  } else {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) opart[warp][lane * PER + e] = acc[e];
-    const float2 n = row_sum2(lane == 0 ? (float)support : 0.f, 0.f);     // (a barrier; counts stay below 2^24)
+    for (int e = 0; e < D / 8; ++e) {
+      acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 8);
+      acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 16);
+    }
+    if (lane < 8) {
+#pragma unroll
+      for (int e = 0; e < D / 8; ++e) opart[warp][(e >> 3) * 64 + 8 * sl + (e & 7)] = acc[e];
+    }
+    const float2 total = row_sum2(lane == 0 ? (float)support : 0.f, 0.f);   // (a barrier; counts stay below 2^24)
+    const size_t out = (size_t)(s.q0 + tok) * a.H + kvh * a.G + r % a.G;
     if ((int)threadIdx.x < D) {
-      float s = 0.f;
+      float o = 0.f;
 #pragma unroll
-      for (int i = 0; i < W; ++i) s += opart[i][threadIdx.x];
-      a.o[out * D + threadIdx.x] = __float2bfloat16(s);
+      for (int i = 0; i < W; ++i) o += opart[i][threadIdx.x];
+      a.o[out * D + threadIdx.x] = __float2bfloat16(o);
     }
     if (threadIdx.x == 0) {
       a.tau[out] = tau;
-      if (a.support) a.support[out] = (int)n.x;
+      if (a.support) a.support[out] = (int)total.x;
     }
+    if (!kSpilled) break;
+    __syncthreads();                                        // (opart is read before the next row writes it)
   }
 }
 
+template <int D, bool kMany>
+cudaError_t launch_solve_d(const PagedArgs& a, const __nv_bfloat16* v, int first, int units, bool rows8, cudaStream_t stream) {
+  const int slots = kMany ? a.many_slots : a.few_slots;
+  const long long rows = (long long)units * slots;
+  if (!rows8) return launch_kernel(paged_row_kernel<D, kMany, false>, (unsigned)rows, 32 * kRowWarps, 0, stream, a, v, first);
+  const unsigned ctas = (unsigned)(kMany ? (long long)units * ((slots + kRows8 - 1) / kRows8) : (rows + kRows8 - 1) / kRows8);
+  cudaError_t err;
+#define ENTMAX_ROWS8(EC) launch_kernel(paged_rows8_kernel<D, EC, kMany>, ctas, 32 * kWarps8, 0, stream, a, v, first, units)
+  switch (a.expo_class) {
+    case kExpo2: err = ENTMAX_ROWS8(kExpo2); break;
+    case kExpo1: err = ENTMAX_ROWS8(kExpo1); break;
+    case kExpo4: err = ENTMAX_ROWS8(kExpo4); break;
+    default: err = ENTMAX_ROWS8(kExpoGeneral); break;
+  }
+#undef ENTMAX_ROWS8
+  if (err != cudaSuccess) return err;
+  return launch_kernel(paged_row_kernel<D, kMany, true>, 4 * 148, 32 * kRowWarps, 0, stream, a, v, first);
+}
+
+// Eight lanes per row where there are rows enough to fill the machine that way, or where a row is short
+bool solve_by_rows8(const PagedArgs& a, bool many, long long rows) {
+  return a.max_kv <= (many ? 65536 : 8192) && (rows >= 8 * 148 || a.max_kv <= 2048);
+}
 template <bool kMany>
-cudaError_t launch_solve(const PagedArgs& a, const void* v, int first, long long units, cudaStream_t stream) {
-  const long long rows = units * (kMany ? a.many_slots : a.few_slots);
+cudaError_t launch_solve(const PagedArgs& a, const void* v, int first, int units, cudaStream_t stream) {
   const __nv_bfloat16* vb = static_cast<const __nv_bfloat16*>(v);
-  const bool one = a.max_kv <= 1024 || (rows >= 4096 && a.max_kv <= 65536);
-#define ENTMAX_PAGED_SOLVE(D, W)                                                                                               \
-  launch_kernel(paged_solve_kernel<D, W, kMany>, (unsigned)((rows + SolveShape<W>::kRowsPerCta - 1) / SolveShape<W>::kRowsPerCta), \
-                SolveShape<W>::kThreads, 0, stream, a, vb, first, rows)
-  if (a.c.D == 64) return one ? ENTMAX_PAGED_SOLVE(64, 1) : ENTMAX_PAGED_SOLVE(64, 8);
-  return one ? ENTMAX_PAGED_SOLVE(128, 1) : ENTMAX_PAGED_SOLVE(128, 8);
-#undef ENTMAX_PAGED_SOLVE
+  const long long rows = (long long)units * (kMany ? a.many_slots : a.few_slots);
+  const bool rows8 = solve_by_rows8(a, kMany, rows);
+  return a.c.D == 64 ? launch_solve_d<64, kMany>(a, vb, first, units, rows8, stream)
+                     : launch_solve_d<128, kMany>(a, vb, first, units, rows8, stream);
 }
 
 // ------------------------------------------------------------------------------------------------ host
 constexpr size_t kSliceBytes = (size_t)4 << 30;     // scores held at a time (at least one sequence's or block's)
 constexpr int kFewRows = 32;
+constexpr int kFewWorth = 8;
+
+// The current device's compute capability (major) and SMs, looked up once per device
+cudaError_t device_facts(int* major, int* sms) {
+  static std::atomic<int> known[64];               // major << 16 | sms; 0: not looked up yet
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  int v = dev >= 0 && dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (v == 0) {
+    int m = 0, n = 0;
+    err = cudaDeviceGetAttribute(&m, cudaDevAttrComputeCapabilityMajor, dev);
+    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (err != cudaSuccess) return err;
+    v = m << 16 | n;
+    if (dev >= 0 && dev < 64) known[dev].store(v, std::memory_order_relaxed);
+  }
+  *major = v >> 16;
+  *sms = v & 0xffff;
+  return cudaSuccess;
+}
 
 struct PagedPlan {
-  size_t scores, group_max, total;
-  int few_seqs;          // sequences to a slice of the "few" kernel
+  size_t scores, group_max, record_key, row_info, spilled, total;
+  int few_seqs;          // sequences to a slice of the "few" kernel (at most kFewSeqs)
   int many_blocks;       // blocks to a slice of the "many" kernel
   bool few, many;
 };
@@ -321,11 +755,14 @@ int plan_paged(const entmax_attn_paged_cache* cache, const entmax_attn_paged_par
   if (p->max_q_len > 0 && p->max_q_len < a->max_q) a->max_q = p->max_q_len;
   if (a->max_q > a->max_kv) a->max_q = a->max_kv;
   a->score_stride = ((size_t)a->max_kv + 255) / 256 * 256;
-  a->group_stride = (int)(a->score_stride / kGroupKeys);
+  a->groups = (int)(a->score_stride / kGroupKeys);
+  a->tiles = (int)(a->score_stride / kManyKeys);
 
   // few: rows of a sequence's unit; many: the rest
   a->few_rows = (long long)a->max_q * a->G <= 16 ? 16 : a->G <= kFewRows ? kFewRows : 0;
   if (uniform && (long long)(a->c.T / a->c.B) * a->G > a->few_rows) a->few_rows = 0;
+  // where longer chunks are possible anyway, the single tokens of a handful of sequences are not worth a pair of launches of their own
+  if (a->c.B <= kFewWorth && (long long)a->max_q * a->G > a->few_rows) a->few_rows = 0;
   l->few = a->few_rows > 0;
   const int few_tokens = l->few ? (a->max_q < a->few_rows / a->G ? a->max_q : a->few_rows / a->G) : 0;
   a->few_slots = few_tokens * a->G;
@@ -333,36 +770,41 @@ int plan_paged(const entmax_attn_paged_cache* cache, const entmax_attn_paged_par
   a->tile_tokens = 128 / a->G;
   a->many_slots = kManyTiles * a->tile_tokens * a->G;
   const int block_tokens = kManyTiles * a->tile_tokens;
-  a->many_blocks = uniform ? a->c.B * ((a->c.T / a->c.B + block_tokens - 1) / block_tokens) : a->c.T / block_tokens + a->c.B;
+  a->many_blocks = uniform ? a->c.B * ((a->c.T / a->c.B + block_tokens - 1) / block_tokens) : (a->c.T + block_tokens - 1) / block_tokens + a->c.B - 1;
 
   const size_t row_bytes = a->score_stride * sizeof(float);
-  size_t rows = 0;
+  size_t rows = 0, many_rows = 0;
   l->few_seqs = l->many_blocks = 0;
   if (l->few) {
     const size_t per = (size_t)a->c.KH * a->few_slots, fit = kSliceBytes / row_bytes / per;
-    l->few_seqs = fit < 1 ? 1 : fit < (size_t)a->c.B ? (int)fit : a->c.B;
+    l->few_seqs = a->c.B < kFewSeqs ? a->c.B : kFewSeqs;
+    if (fit < (size_t)l->few_seqs) l->few_seqs = fit < 1 ? 1 : (int)fit;
     rows = per * l->few_seqs;
   }
   if (l->many) {
     const size_t per = (size_t)a->c.KH * a->many_slots, fit = kSliceBytes / row_bytes / per;
     l->many_blocks = fit < 1 ? 1 : fit < (size_t)a->many_blocks ? (int)fit : a->many_blocks;
-    if (per * l->many_blocks > rows) rows = per * l->many_blocks;
+    many_rows = per * l->many_blocks;
   }
-  // work items: CTAs enough for a few waves, shares of the keys no shorter than two tiles
-  const long long few_units = (long long)l->few_seqs * a->c.KH;
-  long long chunks = few_units > 0 ? 4 * 296 / few_units : 1;
-  const long long most = ((a->max_kv + 127) / 128 + 1) / 2;
-  a->few_chunks = (int)(chunks < 1 ? 1 : chunks > most ? most : chunks);
+  // Work items of the "many" kernel: the number of shares that the machine works off in the fewest K tiles, an item's start counted as three
   const long long many_units = (long long)l->many_blocks * a->c.KH;
-  long long splits = many_units > 0 ? (2 * 148 + many_units - 1) / many_units : 1;
-  const long long most_splits = ((a->max_kv + 255) / 256 + 3) / 4;
-  a->many_splits = (int)(splits < 1 ? 1 : splits > most_splits ? most_splits : splits);
+  a->many_splits = 1;
+  long long best = 0;
+  for (int i = 1; i <= 8 && i * 4 <= a->tiles + 3; ++i) {
+    const long long cost = (many_units * i + 147) / 148 * ((a->tiles + i - 1) / i + 3);
+    if (best == 0 || cost < best) {
+      best = cost;
+      a->many_splits = i;
+    }
+  }
 
   size_t off = 256;
-  l->group_max = off;
-  off += (rows * a->group_stride * sizeof(float) + 255) / 256 * 256;
-  l->scores = off;
-  off += (rows * row_bytes + 255) / 256 * 256;
+  auto take = [&off](size_t floats) { const size_t at = off; off = (off + floats * sizeof(float) + 255) / 256 * 256; return at; };
+  l->spilled = take(rows > many_rows ? rows : many_rows);
+  l->group_max = take(rows * a->groups);
+  l->record_key = take(many_rows * a->tiles * 32);
+  l->row_info = take(4 * many_rows * a->many_splits);
+  l->scores = take((rows > many_rows ? rows : many_rows) * a->score_stride);
   l->total = off;
   return ENTMAX_ATTN_OK;
 }
@@ -401,16 +843,18 @@ extern "C" int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const
       !aligned4(gamma) || !aligned4(delta) || !aligned4(alibi_slopes))
     return ENTMAX_ATTN_EINVAL_ALIGN;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < l.total) return ENTMAX_ATTN_EINVAL_WORKSPACE;
-  int dev = 0, major = 0;
-  cudaError_t err = cudaGetDevice(&dev);
-  if (err == cudaSuccess) err = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
+  int major = 0;
+  cudaError_t err = device_facts(&major, &a.sms);
   if (err != cudaSuccess) return fail_cuda(err);
   if (major != 10) return ENTMAX_ATTN_EUNSUPPORTED;          // the score kernels need tcgen05 / TMA
   a.c.table = block_table; a.c.kv_len = kv_len; a.c.cu_q = cu_q;
   a.beta = beta; a.gamma = gamma; a.delta = delta; a.alibi = alibi_slopes;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  a.counter = reinterpret_cast<int32_t*>(ws);
+  a.counters = reinterpret_cast<int32_t*>(ws);
+  a.row_info = reinterpret_cast<float4*>(ws + l.row_info);
+  a.spilled = reinterpret_cast<int32_t*>(ws + l.spilled);
   a.group_max = reinterpret_cast<float*>(ws + l.group_max);
+  a.record_key = reinterpret_cast<int32_t*>(ws + l.record_key);
   a.scores = reinterpret_cast<float*>(ws + l.scores);
   a.o = static_cast<__nv_bfloat16*>(o);
   a.tau = tau;
@@ -421,15 +865,18 @@ extern "C" int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const
     err = cudaMemsetAsync(device_status, 0, sizeof(int32_t) * ENTMAX_ATTN_STATUS_WORDS, stream);
     if (err != cudaSuccess) return fail_cuda(err);
   }
+  auto clear_counters = [&]() { return cudaMemsetAsync(a.counters, 0, 2 * sizeof(int32_t), stream); };
   for (int b = 0; l.few && b < a.c.B && err == cudaSuccess; b += l.few_seqs) {
     const int n = a.c.B - b < l.few_seqs ? a.c.B - b : l.few_seqs;
-    err = launch_paged_few(a, q, k_cache, params->q_stride_t, params->q_stride_h, b, n, stream);
-    if (err == cudaSuccess) err = launch_solve<false>(a, v_cache, b, (long long)n * a.c.KH, stream);
+    if (solve_by_rows8(a, false, (long long)n * a.c.KH * a.few_slots)) err = clear_counters();
+    if (err == cudaSuccess) err = launch_paged_few(a, q, k_cache, params->q_stride_t, params->q_stride_h, b, n, stream);
+    if (err == cudaSuccess) err = launch_solve<false>(a, v_cache, b, n * a.c.KH, stream);
   }
   for (int blk = 0; l.many && blk < a.many_blocks && err == cudaSuccess; blk += l.many_blocks) {
     const int n = a.many_blocks - blk < l.many_blocks ? a.many_blocks - blk : l.many_blocks;
-    err = launch_paged_many(a, q, k_cache, params->q_stride_t, params->q_stride_h, blk, n, stream);
-    if (err == cudaSuccess) err = launch_solve<true>(a, v_cache, blk, (long long)n * a.c.KH, stream);
+    err = clear_counters();
+    if (err == cudaSuccess) err = launch_paged_many(a, q, k_cache, params->q_stride_t, params->q_stride_h, blk, n, stream);
+    if (err == cudaSuccess) err = launch_solve<true>(a, v_cache, blk, n * a.c.KH, stream);
   }
   if (err == cudaSuccess) err = cudaGetLastError();
   return err == cudaSuccess ? ENTMAX_ATTN_OK : fail_cuda(err);

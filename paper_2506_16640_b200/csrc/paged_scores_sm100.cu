@@ -1,18 +1,18 @@
 // Scores of new tokens against a paged cache on sm_100a: tcgen05 contractions (bf16 in, fp32 in TMEM), K pages staged by TMA
 // straight from the pool (one box per page and 64 columns; no copy of the cache, no gather kernel).
 //
-// What is kept of S = Q K^T is little: the maximum of every 32 keys of a row, and the scores of those groups of 32 whose maximum is
-// above (largest value seen so far) - 1.  Eq. 1's threshold is never below y_max - 1 (App. A), so every key of the support is in a
-// group that is kept, whatever order the tiles come in and however the keys are split: a bound taken from fewer keys is lower and
-// keeps more.  Which further groups are kept has no influence on the result (paged_solve_kernel looks only at the groups above
-// the final y_max - 1).
+// What is kept of S = Q K^T is little: the keys above a lower bound of the row's threshold, a bound that rises while the keys stream by --
+// the largest value so far minus 1 (App. A: tau >= y_max - 1), or the threshold of a few of the keys seen (that of a subset never exceeds
+// that of the whole row).  So every key of the support is kept, whatever order the tiles come in and however the keys are
+// split: a bound taken from fewer keys is lower and keeps more, and what is kept beyond the support has no influence on the result.
+// There is room for every key of a row: flat logits cost stores, not another path.
 //
 // Two shapes of the same product:
 //   few   sequences with at most 32 rows (new tokens x query heads of a K/V head): K tile of 128 keys as the M side, rows as N = 16 or
 //         32; TMEM lane = key, a warp's 32 keys are a group.  Bound by reading K: 2 CTAs per SM, a ring of TMA tiles each.
 //   many  longer chunks: 128 rows as the M side, two such Q tiles against K tiles of 256 keys (N = 256: at N = 128 the operand reads
-//         from shared memory bound the MMA).  TMEM lane = row, one thread scans its row's 256 columns: 1.5 instructions
-//         per 32 rows and key against 8 with a lane per key.  Bound by the tensor pipe.
+//         from shared memory bound the MMA).  TMEM lane = row, one thread scans its row's 256 columns: about one instruction
+//         per 32 rows and key against 8 with a lane per key.
 #include <cuda.h>
 
 #include "paged.cuh"
@@ -45,16 +45,18 @@ __device__ __forceinline__ void page_of_box(const PagedCache& c, int b, int key,
 constexpr int kTile = 128;
 constexpr int kFewThreads = 6 * 32;
 
-template <int HD, int NB>
+// NR: rows a thread works on (a multiple of 4); NB: rows of the MMA's B operand
+template <int HD, int NR>
 struct FewCfg {
+  static constexpr int NB = NR <= 16 ? 16 : 32;
   static constexpr int kHalves = HD / 64;
   static constexpr int kKBytes = kTile * HD * 2;
   static constexpr int kQBytes = NB * HD * 2;
-  static constexpr int kStages = HD == 128 ? 3 : 6;        // 96 KB of loads in flight per CTA
+  static constexpr int kStages = HD == 64 ? 6 : NR <= 16 ? 3 : 2;   // (two CTAs per SM)
   static constexpr int kBarBytes = 256;
-  static constexpr int kRowBytes = NB * 16;
+  static constexpr int kRowBytes = 4 * NR * 16;            // the rows' parameters, a copy per consumer warp
   static constexpr int kTmem = NB == 16 ? 32 : 64;         // two accumulators
-  static constexpr int kSmemBytes = kStages * kKBytes + kQBytes + kRowBytes + kBarBytes + 1024;
+  static constexpr int kFixedBytes = kStages * kKBytes + 2 * kQBytes + kRowBytes + kBarBytes + 1024;
 };
 
 // A = K tile, B = query rows, both K-major bf16, fp32 accumulate, M = 128, N = NB
@@ -62,48 +64,44 @@ __host__ __device__ constexpr uint32_t idesc_few(int nb) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(nb >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
 }
 
-template <int NB>
-__device__ __forceinline__ void load_columns(uint32_t taddr, float (&acc)[NB]) {
-  if constexpr (NB == 16) tmem_ld16(taddr, acc);
+template <int N>
+__device__ __forceinline__ void load_columns(uint32_t taddr, float (&acc)[N]) {
+  if constexpr (N == 8) tmem_ld8(taddr, acc);
+  else if constexpr (N == 16) tmem_ld16(taddr, acc);
   else tmem_ld32(taddr, acc);
 }
 
-template <int HD, int NB, bool kAlibi>
+// The tiles of all sequences and K/V heads, one after another (head by head), are dealt to the CTAs in equal runs: a CTA walks its run as
+// segments, each some tiles of one (sequence, K/V head).  So the machine is full and finishes together whatever the lengths are.
+struct FewSegment {
+  int b, kvh;            // sequence (of the slice) and K/V head
+  int tile, tiles;       // first tile and number of tiles
+};
+struct FewWalk {
+  long long x, end;      // next tile of the run, end of the run
+  int b, kvh;
+};
+
+template <int HD, int NR, bool kAlibi>
 __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_constant__ CUtensorMap map_q,
                                                                  const __grid_constant__ CUtensorMap map_k,
-                                                                 const __grid_constant__ PagedArgs a, int unit0) {
+                                                                 const __grid_constant__ PagedArgs a, int seq0, int seqs) {
   pdl_begin();
-  using C = FewCfg<HD, NB>;
+  using C = FewCfg<HD, NR>;
+  constexpr int NB = C::NB;
   extern __shared__ uint8_t smem_raw[];
+  __shared__ int warp_sum[kFewThreads / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int chunk = blockIdx.x % a.few_chunks, unit = blockIdx.x / a.few_chunks;
-  const int kvh = unit % a.c.KH, b = unit0 + unit / a.c.KH;
-  const PagedSeq s = paged_seq(a.c, b);
-  if (s.n == 0) return;
-  if (!paged_ok(a, s)) {
-    if (chunk == 0) {
-      if (threadIdx.x == 0 && a.status) atomicOr(a.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_LENGTH);
-      write_unserved(a, s, kvh, threadIdx.x, kFewThreads);
-    }
-    return;
-  }
-  if (!paged_few(a, s)) return;
-  // the sequence's tiles dealt evenly to as many of the unit's CTAs as get two at least
-  const int len_tiles = (s.len + kTile - 1) / kTile;
-  const int ctas = min(a.few_chunks, (len_tiles + 1) / 2);
-  if (chunk >= ctas) return;
-  const int tile0 = (int)((long long)len_tiles * chunk / ctas), tile1 = (int)((long long)len_tiles * (chunk + 1) / ctas);
-  const int tiles = tile1 - tile0;
-  const int rows = s.n * a.G;
   const int box_shift = min(a.c.ps_shift, 7);
 
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t k_smem = sbase;
-  const uint32_t q_smem = k_smem + C::kStages * C::kKBytes;
-  const uint32_t row_par = q_smem + C::kQBytes;             // per row: a, a * slope, position (float), position (int)
+  const uint32_t k_smem = sbase;                            // [kStages] K tiles
+  const uint32_t q_smem = k_smem + C::kStages * C::kKBytes; // [2] query rows of a segment
+  const uint32_t row_par = q_smem + 2 * C::kQBytes;         // [4 warps][NR]: a, slope, position (float), position (int)
   const uint32_t bars = row_par + C::kRowBytes;
-  const uint32_t q_full = bars;
-  const uint32_t kv_full = bars + 8;                        // [kStages]
+  const uint32_t q_full = bars;                             // [2]
+  const uint32_t q_empty = q_full + 16;                     // [2]
+  const uint32_t kv_full = q_empty + 16;                    // [kStages]
   const uint32_t kv_empty = kv_full + 8 * C::kStages;       // [kStages]
   const uint32_t s_full = kv_empty + 8 * C::kStages;        // [2]
   const uint32_t s_empty = s_full + 16;                     // [2]
@@ -111,17 +109,21 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
   const uint32_t abort_flag = tmem_slot + 4;
   const uint32_t drain_bar = tmem_slot + 8;                 // teardown: every MMA issued so far has finished
   const uint32_t drain_fail = drain_bar + 8;                // uint32: a teardown wait ran out as well
-  static_assert(8 * (1 + 2 * C::kStages + 4) + 8 + 16 <= C::kBarBytes, "barrier area");
+  static_assert(8 * (4 + 2 * C::kStages + 4) + 8 + 16 <= C::kBarBytes, "barrier area");
+  // tiles before sequence b, then {first row of q, new tokens, length} of it
+  int* before = reinterpret_cast<int*>(smem_raw + (bars + C::kBarBytes - smem_u32(smem_raw)));
+  int* info = before + seqs + 1;
 
   if (threadIdx.x == 0) {
-    mbar_init(q_full, 1);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(q_full + 8 * t, 1);
+      mbar_init(q_empty + 8 * t, 1);
+      mbar_init(s_full + 8 * t, 1);
+      mbar_init(s_empty + 8 * t, 4);
+    }
     for (int t = 0; t < C::kStages; ++t) {
       mbar_init(kv_full + 8 * t, 1);
       mbar_init(kv_empty + 8 * t, 1);
-    }
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(s_full + 8 * t, 1);
-      mbar_init(s_empty + 8 * t, 4);
     }
     mbar_init(drain_bar, 1);
     sts_u32(drain_fail, 0u);
@@ -133,64 +135,136 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
     tmem_alloc(tmem_slot, C::kTmem);
     tmem_relinquish();
   }
-  if (warp == 2 && lane < NB) {
-    float ra = 0.f, slope = 0.f;
-    int pos = -1;                                            // (rows past the last one see nothing)
-    if (lane < rows) {
-      const int head = kvh * a.G + lane % a.G;
-      pos = s.len - s.n + lane / a.G;
-      ra = paged_scale(a, head, pos);
-      if (kAlibi) slope = a.alibi[head] / a.sm_scale;        // bias in dot-product units
-    }
-    sts_f4(row_par + 16 * lane, ra, slope, (float)pos, __int_as_float(pos));
+  // ---- running sum of the sequences' tiles
+  const int per = (seqs + kFewThreads - 1) / kFewThreads;   // consecutive sequences of a thread
+  int mine = 0;
+  for (int i = threadIdx.x * per; i < min(seqs, (int)(threadIdx.x + 1) * per); ++i) {
+    const PagedSeq s = paged_seq(a.c, seq0 + i);
+    const int tiles = s.n > 0 && paged_ok(a, s) && paged_few(a, s) ? (s.len + kTile - 1) / kTile : 0;
+    info[3 * i] = s.q0;
+    info[3 * i + 1] = s.n;
+    info[3 * i + 2] = s.len;
+    before[i + 1] = tiles;
+    mine += tiles;
   }
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) warp_sum[warp] = incl;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  {
+    int at = incl - mine;
+    for (int i = 0; i < warp; ++i) at += warp_sum[i];
+    if (threadIdx.x == 0) before[0] = 0;
+    for (int i = threadIdx.x * per; i < min(seqs, (int)(threadIdx.x + 1) * per); ++i) {
+      at += before[i + 1];
+      before[i + 1] = at;
+    }
+  }
+  __syncthreads();
   const uint32_t tmem_base = lds_u32(tmem_slot);
+  const int head_tiles = before[seqs];                       // of one K/V head
+  const long long total = (long long)head_tiles * a.c.KH;
+  const long long ctas = min((long long)gridDim.x, max(total / 2, 1ll));   // (runs of two tiles at least)
+
+  FewWalk start;
+  start.x = start.end = 0;
+  start.b = start.kvh = 0;
+  if (blockIdx.x < ctas) {
+    start.x = total * blockIdx.x / ctas;
+    start.end = total * (blockIdx.x + 1) / ctas;
+    if (start.x < start.end) {
+      start.kvh = (int)(start.x / head_tiles);
+      const int y = (int)(start.x - (long long)start.kvh * head_tiles);
+      int lo = 0, hi = seqs;                                 // largest b with before[b] <= y
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (before[mid] <= y) lo = mid; else hi = mid;
+      }
+      start.b = lo;
+    }
+  }
+  auto next_segment = [&](FewWalk& w, FewSegment& g) -> bool {
+    if (w.x >= w.end) return false;
+    const int y = (int)(w.x - (long long)w.kvh * head_tiles);
+    while (before[w.b + 1] <= y) ++w.b;
+    g.b = w.b;
+    g.kvh = w.kvh;
+    g.tile = y - before[w.b];
+    g.tiles = (int)min((long long)(before[w.b + 1] - y), w.end - w.x);
+    w.x += g.tiles;
+    if (y + g.tiles == head_tiles) {
+      w.b = 0;
+      ++w.kvh;
+    }
+    return true;
+  };
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer: a lane per page box
-    if (elect_one()) {
-      mbar_expect_tx(q_full, (uint32_t)(a.few_slots * 128 * C::kHalves));
-      for (int hf = 0; hf < C::kHalves; ++hf)
-        tma_load_4d(q_smem + hf * (NB * 128), &map_q, q_full, hf * 64, kvh * a.G, s.q0, 0);
-    }
-    __syncwarp();
-    int stage = 0;
-    uint32_t phase = 0;
+    int stage = 0, qb = 0;
+    uint32_t phase = 0, qphase = 0;
     bool alive = true;
+    auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool {
+      return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+    };
     const int boxes = kTile >> box_shift;                    // of a whole tile: a power of two, at most 8
-    // 32 page numbers ahead, a lane each
-    const int ahead = 32 / boxes;                            // tiles they cover
-    int page = 0, slot = 0;
-    for (int t = 0; t < tiles; ++t) {
-      const int key0 = (tile0 + t) * kTile;
-      if (t % ahead == 0) {
-        const int key = key0 + (lane << box_shift);
-        if (key < s.len) page_of_box(a.c, b, key, a.status, page, slot);
-      }
-      const int src = (t % ahead) * boxes + (lane & (boxes - 1));
-      const int pg = __shfl_sync(0xffffffffu, page, src), sl = __shfl_sync(0xffffffffu, slot, src);
-      alive = __all_sync(0xffffffffu, mbar_wait(kv_empty + 8 * stage, phase ^ 1u, abort_flag));
+    const int ahead = 32 / boxes;                            // tiles that 32 page numbers, a lane each, cover
+    FewWalk w = start;
+    FewSegment g;
+    while (alive && next_segment(w, g)) {
+      const int q0 = info[3 * g.b], len = info[3 * g.b + 2];
+      const int b = seq0 + g.b;
+      auto look_up = [&](int t, int& page, int& slot) {
+        const int key = (g.tile + t) * kTile + (lane << box_shift);
+        if (t < g.tiles && key < len) page_of_box(a.c, b, key, a.status, page, slot);
+      };
+      int page = 0, slot = 0, page2 = 0, slot2 = 0;
+      look_up(0, page2, slot2);
+      alive = wait_all(q_empty + 8 * qb, qphase ^ 1u);
       if (!alive) break;
-      const int need = boxes_needed(key0, kTile, s.len, box_shift);
-      const uint32_t box_bytes = 128u << box_shift;
-      if (lane == 0) mbar_expect_tx(kv_full + 8 * stage, (uint32_t)need * box_bytes * C::kHalves);
-      __syncwarp();
-      if (lane < need) {
-#pragma unroll
+      if (elect_one()) {
+        mbar_expect_tx(q_full + 8 * qb, (uint32_t)(a.few_slots * 128 * C::kHalves));
         for (int hf = 0; hf < C::kHalves; ++hf)
-          tma_load_4d(k_smem + stage * C::kKBytes + hf * (kTile * 128) + lane * box_bytes, &map_k, kv_full + 8 * stage, hf * 64, sl,
-                      kvh, pg);
+          tma_load_4d(q_smem + qb * C::kQBytes + hf * (NB * 128), &map_q, q_full + 8 * qb, hf * 64, g.kvh * a.G, q0, 0);
       }
       __syncwarp();
-      if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+      if (++qb == 2) { qb = 0; qphase ^= 1u; }
+      for (int t = 0; t < g.tiles; ++t) {
+        const int key0 = (g.tile + t) * kTile;
+        if (t % ahead == 0) {
+          page = page2;
+          slot = slot2;
+          look_up(t + ahead, page2, slot2);                  // (its latency is covered by the tiles in between)
+        }
+        const int src = (t % ahead) * boxes + (lane & (boxes - 1));
+        const int pg = __shfl_sync(0xffffffffu, page, src), sl = __shfl_sync(0xffffffffu, slot, src);
+        alive = wait_all(kv_empty + 8 * stage, phase ^ 1u);
+        if (!alive) break;
+        const int need = boxes_needed(key0, kTile, len, box_shift);
+        const uint32_t box_bytes = 128u << box_shift;
+        if (lane == 0) mbar_expect_tx(kv_full + 8 * stage, (uint32_t)need * box_bytes * C::kHalves);
+        __syncwarp();
+        if (lane < need) {
+#pragma unroll
+          for (int hf = 0; hf < C::kHalves; ++hf)
+            tma_load_4d(k_smem + stage * C::kKBytes + hf * (kTile * 128) + lane * box_bytes, &map_k, kv_full + 8 * stage, hf * 64, sl,
+                        g.kvh, pg);
+        }
+        __syncwarp();
+        if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+      }
     }
     if (!alive && lane == 0) {
       // a wait ran out somewhere in the CTA: the copies this warp armed barriers for must land before shared
-      // memory goes away (stages before `stage`: this round of the ring; the others: the previous round)
-      bool ok = mbar_drain(q_full, 0u);
+      // memory goes away (buffers before the next one to fill: this round of the ring; the others: the previous round)
+      bool ok = true;
+      for (int t = 0; t < 2; ++t) ok &= mbar_drain(q_full + 8 * t, t < qb ? qphase : qphase ^ 1u);
       for (int st = 0; st < C::kStages; ++st) ok &= mbar_drain(kv_full + 8 * st, st < stage ? phase : phase ^ 1u);
       if (!ok) sts_u32(drain_fail, 1u);
     }
@@ -199,26 +273,34 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
     if (lane == 0) {
       constexpr uint32_t idesc = idesc_few(NB);
       const uint32_t k_lo = smem_desc_lo(k_smem), q_lo = smem_desc_lo(q_smem);
-      int stage = 0, buf = 0;
-      uint32_t phase = 0, sphase[2] = {0, 0};
-      bool alive = mbar_wait(q_full, 0, abort_flag);
-      for (int t = 0; t < tiles && alive; ++t) {
-        alive = mbar_wait(kv_full + 8 * stage, phase, abort_flag);
-        if (alive) alive = mbar_wait(s_empty + 8 * buf, sphase[buf] ^ 1u, abort_flag);
-        if (!alive) break;
-        sphase[buf] ^= 1u;
-        tc_fence_after();
-        const uint32_t a_lo = k_lo + stage * (C::kKBytes >> 4);
+      int stage = 0, buf = 0, qb = 0;
+      uint32_t phase = 0, qphase = 0, sphase[2] = {0, 0};
+      bool alive = true;
+      FewWalk w = start;
+      FewSegment g;
+      while (alive && next_segment(w, g)) {
+        alive = mbar_wait(q_full + 8 * qb, qphase, abort_flag);
+        const uint32_t b_lo = q_lo + qb * (C::kQBytes >> 4);
+        for (int t = 0; t < g.tiles && alive; ++t) {
+          alive = mbar_wait(kv_full + 8 * stage, phase, abort_flag);
+          if (alive) alive = mbar_wait(s_empty + 8 * buf, sphase[buf] ^ 1u, abort_flag);
+          if (!alive) break;
+          sphase[buf] ^= 1u;
+          tc_fence_after();
+          const uint32_t a_lo = k_lo + stage * (C::kKBytes >> 4);
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk) {
-          const uint32_t a_off = (kk >> 2) * ((kTile * 128) >> 4) + (kk & 3) * 2;
-          const uint32_t b_off = (kk >> 2) * ((NB * 128) >> 4) + (kk & 3) * 2;
-          umma_bf16(tmem_base + buf * NB, a_lo + a_off, q_lo + b_off, kDescHi, idesc, kk > 0 ? 1u : 0u);
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t a_off = (kk >> 2) * ((kTile * 128) >> 4) + (kk & 3) * 2;
+            const uint32_t b_off = (kk >> 2) * ((NB * 128) >> 4) + (kk & 3) * 2;
+            umma_bf16(tmem_base + buf * NB, a_lo + a_off, b_lo + b_off, kDescHi, idesc, kk > 0 ? 1u : 0u);
+          }
+          umma_commit(s_full + 8 * buf);
+          umma_commit(kv_empty + 8 * stage);
+          if (t == g.tiles - 1) umma_commit(q_empty + 8 * qb);
+          buf ^= 1;
+          if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
         }
-        umma_commit(s_full + 8 * buf);
-        umma_commit(kv_empty + 8 * stage);
-        buf ^= 1;
-        if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+        if (++qb == 2) { qb = 0; qphase ^= 1u; }
       }
       if (!alive) {
         // the tensor core must be done with shared memory and TMEM before they are released
@@ -230,46 +312,76 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
     // ------------------------------------------------------------------ a thread per key of the tile, a group per warp
     const int quad = warp & 3;
     const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16);
-    const size_t row0 = (size_t)unit * a.few_slots;
-    const int pos0 = s.len - s.n;
+    const uint32_t par = row_par + (uint32_t)quad * (NR * 16);
     uint32_t sphase[2] = {0, 0};
     int buf = 0;
     bool alive = true;
-    float bound[NB];                                         // (largest value so far) - 1, the same in every lane
-#pragma unroll
-    for (int r = 0; r < NB; ++r) bound[r] = -INFINITY;
-    for (int t = 0; t < tiles && alive; ++t) {
-      alive = __all_sync(0xffffffffu, mbar_wait(s_full + 8 * buf, sphase[buf], abort_flag));
-      if (!alive) break;
-      sphase[buf] ^= 1u;
-      tc_fence_after();
-      float acc[NB];
-      load_columns<NB>(taddr + buf * NB, acc);
-      tmem_ld_wait();
-      tc_fence_before();
+    FewWalk w = start;
+    FewSegment g;
+    while (alive && next_segment(w, g)) {
+      const int n = info[3 * g.b + 1], len = info[3 * g.b + 2];
+      const int rows = n * a.G;
+      const int pos0 = len - n;                              // position of the first new token
+      const int unit = g.b * a.c.KH + g.kvh;
+      float* score0 = a.scores + (size_t)unit * a.few_slots * a.score_stride;
+      float* max0 = a.group_max + (size_t)unit * a.groups * a.few_slots;
       __syncwarp();
-      if (lane == 0) mbar_arrive(s_empty + 8 * buf);
-      buf ^= 1;
-      const int group = (tile0 + t) * (kTile / 32) + quad;
-      const int j = group * 32 + lane;
-      if (group * 32 >= s.len) continue;                     // (groups nobody looks at)
-      const bool edge = group * 32 + 31 > pos0;
-      float mine = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < NB; ++r) {
-        if (r < rows) {
-          float ra, slope, posf, posi;
-          lds_f4(row_par + 16 * r, ra, slope, posf, posi);
-          float y = kAlibi ? ra * fmaf(slope, (float)j - posf, acc[r]) : ra * acc[r];
-          if (edge) y = j <= __float_as_int(posi) ? y : -INFINITY;
-          float m = y;
-          asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(m));
-          if (m > bound[r]) a.scores[(row0 + r) * a.score_stride + j] = y;
-          bound[r] = fmaxf(bound[r], m - 1.0f);
-          if (lane == r) mine = m;
+      if (lane < NR) {
+        float ra = 0.f, slope = 0.f;
+        int pos = -1;                                        // (rows past the last one see nothing)
+        if (lane < rows) {
+          const int head = g.kvh * a.G + lane % a.G;
+          pos = pos0 + lane / a.G;
+          ra = paged_scale(a, head, pos);
+          if (kAlibi) slope = a.alibi[head] / a.sm_scale;    // bias in dot-product units
         }
+        sts_f4(par + 16 * lane, ra, slope, (float)pos, __int_as_float(pos));
       }
-      if (lane < rows) a.group_max[(row0 + lane) * a.group_stride + group] = mine;
+      __syncwarp();
+      float bound[NR];                                       // (largest value so far) - 1, the same in every lane
+#pragma unroll
+      for (int r = 0; r < NR; ++r) bound[r] = r < rows ? -INFINITY : INFINITY;
+      for (int t = 0; t < g.tiles; ++t) {
+        alive = __all_sync(0xffffffffu, mbar_wait(s_full + 8 * buf, sphase[buf], abort_flag));
+        if (!alive) break;
+        sphase[buf] ^= 1u;
+        tc_fence_after();
+        float acc[NR < 8 ? 8 : NR];
+        load_columns<NR < 8 ? 8 : NR>(taddr + buf * NB, acc);
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_empty + 8 * buf);
+        buf ^= 1;
+        const int group = (g.tile + t) * (kTile / 32) + quad;
+        const int j = group * 32 + lane;
+        if (group * 32 >= len) continue;                     // (groups nobody looks at)
+        const bool edge = group * 32 + 31 > pos0;
+        float top = -INFINITY;                               // lane r: the maximum of row r
+        // four rows together, so that their reductions overlap
+#pragma unroll
+        for (int r0 = 0; r0 < NR; r0 += 4) {
+          float y[4], m[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            float ra, slope, posf, posi;
+            lds_f4(par + 16 * (r0 + u), ra, slope, posf, posi);
+            y[u] = ra * (kAlibi ? fmaf(slope, (float)j - posf, acc[r0 + u]) : acc[r0 + u]);
+            if (edge) y[u] = j <= __float_as_int(posi) ? y[u] : -INFINITY;
+            m[u] = y[u];
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(m[u]));
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int r = r0 + u;
+            if (m[u] > bound[r]) score0[(size_t)r * a.score_stride + j] = y[u];
+            bound[r] = fmaxf(bound[r], m[u] - 1.0f);
+            top = lane == r ? m[u] : top;
+          }
+        }
+        if (lane < rows) max0[(size_t)group * a.few_slots + lane] = top;
+      }
     }
   }
 
@@ -290,14 +402,25 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
     tc_fence_after();
     tmem_dealloc(tmem_base, C::kTmem);
   }
+  // sequences that cannot be served
+  for (int i = blockIdx.x; i < seqs; i += gridDim.x) {
+    PagedSeq s;
+    s.q0 = info[3 * i];
+    s.n = info[3 * i + 1];
+    s.len = info[3 * i + 2];
+    if (s.n == 0 || paged_ok(a, s)) continue;
+    if (threadIdx.x == 0 && a.status) atomicOr(a.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_LENGTH);
+    for (int kvh = 0; kvh < a.c.KH; ++kvh) write_unserved(a, s, kvh, threadIdx.x, kFewThreads);
+  }
 }
 
 // =============================================================================================== many
 constexpr int BM = 128;
-constexpr int BN = 256;
+constexpr int BN = kManyKeys;
 constexpr int kManyConsumers = 4 * kManyTiles;
-constexpr int kManyThreads = (2 + kManyConsumers) * 32;
-constexpr int kSchedSlots = 2;
+constexpr int kManyThreads = (3 + kManyConsumers) * 32;
+constexpr int kSchedWarp = 2 + kManyConsumers;
+constexpr int kSchedSlots = 4;
 static_assert(kManyTiles * BN == 512, "TMEM budget");
 
 template <int HD>
@@ -306,7 +429,7 @@ struct ManyCfg {
   static constexpr int kQBytes = BM * HD * 2;
   static constexpr int kKBytes = BN * HD * 2;
   static constexpr int kStages = HD == 128 ? 2 : 4;
-  static constexpr int kBarBytes = 512;
+  static constexpr int kBarBytes = 1024 + 512;
   static constexpr int kSmemBytes = kManyTiles * kQBytes + kStages * kKBytes + kBarBytes + 1024;
   static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
 };
@@ -315,12 +438,12 @@ __host__ __device__ constexpr uint32_t idesc_many() {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
 }
 
-// A work item: one block of new tokens, one K/V head, one share of the keys.  Published by the producer in eight words.
+// A work item: one block of new tokens, one K/V head, one share of the keys.  Published by the scheduler with the pages of its first keys.
 struct ManyItem {
   int b, kvh, q0, n, len, t0, lo, hi;      // t0: first token of the block within the chunk; K tiles lo .. hi - 1
-  int unit;                                // row slots: unit * many_slots
+  int unit, split;                         // row slots: unit * many_slots
 };
-constexpr int kItemWords = 9;
+constexpr int kItemWords = 10 + 64;        // the fields, then page and slot of 32 boxes
 
 // K tiles that Q tile x of the item looks at: lo .. this - 1 (no more than lo: none)
 __device__ __forceinline__ int many_tile_end(const PagedArgs& a, const ManyItem& it, int x) {
@@ -328,6 +451,60 @@ __device__ __forceinline__ int many_tile_end(const PagedArgs& a, const ManyItem&
   if (first >= it.n) return it.lo;
   const int last = min(first + a.tile_tokens, it.n) - 1;
   return max(min((it.len - it.n + last) / BN + 1, it.hi), it.lo);
+}
+
+// Where x > thr: eight values to rec (one 32-byte store), their first key to key, and both moved on.  Predicated instructions instead of a
+// branch: a lane that has nothing to store costs the warp its issue slots and no divergence.
+__device__ __forceinline__ void keep_record_if_greater(float x, float thr, float*& rec, int32_t*& key, int first, const float* v) {
+  asm volatile(
+      "{\n"
+      " .reg .pred p;\n"
+      " setp.gt.f32 p, %2, %3;\n"
+      " @p st.global.v8.f32 [%0], {%5, %6, %7, %8, %9, %10, %11, %12};\n"
+      " @p st.global.u32 [%1], %4;\n"
+      " @p add.u64 %0, %0, 32;\n"
+      " @p add.u64 %1, %1, 4;\n"
+      "}\n"
+      : "+l"(rec), "+l"(key)
+      : "f"(x), "f"(thr), "r"(first), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+      : "memory");
+}
+
+// A lower bound of the threshold of a row from eight values of eight of its keys (-inf: none), y = z / margin: the threshold of those alone, by
+// three steps from the left, in z's units.  Rows with no more than two of them in the bracket have nothing to gain (-inf is returned).
+template <int EC>
+__device__ __forceinline__ float eight_steps(const float (&y)[8], float expo) {
+  float tau = -1.0f;                                           // relative to the largest
+#pragma unroll 1
+  for (int it = 0; it < 3; ++it) {
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      float ye, ye1;
+      powers<EC>(fmaxf(y[q] - tau, 0.f), expo, ye, ye1);
+      s0 += ye;
+      s1 += ye1;
+    }
+    if (s0 > 1.0f && s1 > 0.f) tau += threshold_step(s0, s1, EC, expo);
+  }
+  return tau;
+}
+__device__ __forceinline__ float bound_from_eight(const float (&z)[8], float margin, int expo_class, float expo) {
+  const float m = max8(z);
+  int n = 0;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) n += z[q] > m - margin ? 1 : 0;
+  if (expo < 1.0f || !__any_sync(0xffffffffu, n > 2)) return -INFINITY;
+  float y[8];
+  const float r = 1.0f / margin;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) y[q] = (z[q] - m) * r;
+  const float tau = expo_class == kExpo2 ? eight_steps<kExpo2>(y, expo)
+                    : expo_class == kExpo1 ? eight_steps<kExpo1>(y, expo)
+                    : expo_class == kExpo4 ? eight_steps<kExpo4>(y, expo) : eight_steps<kExpoGeneral>(y, expo);
+  // a hair below for the rounding of the powers, of tau, and of the sum
+  const float bound = m + tau * margin - (1e-5f * margin + 1e-6f * fabsf(m));
+  return n > 2 && bound < INFINITY ? bound : -INFINITY;
 }
 
 template <int HD, bool kAlibi>
@@ -375,7 +552,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
     }
     for (int t = 0; t < kSchedSlots; ++t) {
       mbar_init(w_full + 8 * t, 1);
-      mbar_init(w_empty + 8 * t, 1 + kManyConsumers);              // MMA issuer + consumer warps
+      mbar_init(w_empty + 8 * t, 2 + kManyConsumers);              // producer, MMA issuer and consumer warps
     }
     mbar_init(drain_bar, 1);
     sts_u32(abort_flag, 0u);
@@ -404,87 +581,43 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
     it.lo = (int)lds_u32(at + 24);
     it.hi = (int)lds_u32(at + 28);
     it.unit = (int)lds_u32(at + 32);
+    it.split = (int)lds_u32(at + 36);
     return it;
   };
 
   if (warp == 0) {
-    // ------------------------------------------------------------- scheduler + TMA producer (the whole warp)
+    // ------------------------------------------------------------- TMA producer (the whole warp; a lane per page box)
     int stage = 0, slot = 0;
     uint32_t kphase = 0, qphase = 0 /* bit x: phase of Q tile slot x */, wphase = 0;
     bool alive = true;
     auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool {
       return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
     };
-    const int block_tokens = kManyTiles * a.tile_tokens;
-    const int n_items = blocks * a.c.KH * a.many_splits;
     while (alive) {
-      int k = 0;
-      if (lane == 0) k = atomicAdd(a.counter, 1);
-      k = __shfl_sync(0xffffffffu, k, 0);
-      ManyItem it;
-      it.b = -1;
-      if (k < n_items) {
-        // a K/V head's blocks one after another, later blocks (longer rows) first: the CTAs that run together stream the same keys
-        const int split = k % a.many_splits, u = k / a.many_splits;
-        it.kvh = u / blocks;
-        const int blk = block0 + blocks - 1 - (u - it.kvh * blocks);
-        if (a.c.cu_q) {
-          it.b = find_seq(a.c, blk, block_tokens, 1);
-          it.t0 = (blk - (clamped_cu(a.c, it.b) / block_tokens + it.b)) * block_tokens;
-        } else {
-          const int per = (a.c.T / a.c.B + block_tokens - 1) / block_tokens;
-          it.b = blk / per;
-          it.t0 = (blk - it.b * per) * block_tokens;
-        }
-        if (it.b >= a.c.B) continue;
-        const PagedSeq s = paged_seq(a.c, it.b);
-        it.q0 = s.q0; it.n = s.n; it.len = s.len;
-        if (it.t0 < 0 || it.t0 >= s.n) continue;
-        if (!paged_ok(a, s)) {
-          if (split == 0 && it.t0 == 0) {
-            if (lane == 0 && a.status) atomicOr(a.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_LENGTH);
-            write_unserved(a, s, it.kvh, lane, 32);
-          }
-          continue;
-        }
-        if (paged_few(a, s)) continue;
-        it.unit = (blk - block0) * a.c.KH + it.kvh;
-        const int last = min(it.t0 + block_tokens, s.n) - 1;
-        const int tiles = (s.len - s.n + last) / BN + 1;
-        it.lo = (int)((long long)tiles * split / a.many_splits);
-        it.hi = (int)((long long)tiles * (split + 1) / a.many_splits);
-        if (it.lo >= it.hi) continue;
-      }
-      alive = wait_all(w_empty + 8 * slot, wphase ^ 1u);
+      alive = wait_all(w_full + 8 * slot, wphase);
       if (!alive) break;
-      if (lane == 0) {
-        const uint32_t at = w_item + 4u * kItemWords * slot;
-        sts_u32(at, (uint32_t)it.b);
-        if (it.b >= 0) {
-          sts_u32(at + 4, (uint32_t)it.kvh);
-          sts_u32(at + 8, (uint32_t)it.q0);
-          sts_u32(at + 12, (uint32_t)it.n);
-          sts_u32(at + 16, (uint32_t)it.len);
-          sts_u32(at + 20, (uint32_t)it.t0);
-          sts_u32(at + 24, (uint32_t)it.lo);
-          sts_u32(at + 28, (uint32_t)it.hi);
-          sts_u32(at + 32, (uint32_t)it.unit);
-        }
-        mbar_arrive(w_full + 8 * slot);
-      }
+      const ManyItem it = read_item(slot);
+      const uint32_t boxes_at = w_item + 4u * kItemWords * slot + 40 + 8 * lane;
+      int page2 = (int)lds_u32(boxes_at), pslot2 = (int)lds_u32(boxes_at + 4);
       __syncwarp();
+      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
       if (++slot == kSchedSlots) { slot = 0; wphase ^= 1u; }
       if (it.b < 0) break;
       const int boxes = BN >> box_shift;                    // of a whole tile: a power of two, at most 16
       const int ahead = 32 / boxes;
-      int page = 0, pslot = 0;
       int end = it.lo;
       for (int x = 0; x < kManyTiles; ++x) end = max(end, many_tile_end(a, it, x));
+      auto look_up = [&](int t, int& page, int& pslot) {
+        const int key = t * BN + (lane << box_shift);
+        if (t < end && key < it.len) page_of_box(a.c, it.b, key, a.status, page, pslot);
+      };
+      int page = 0, pslot = 0;
       for (int t = it.lo; t < end && alive; ++t) {
         const int key0 = t * BN;
         if ((t - it.lo) % ahead == 0) {
-          const int key = key0 + (lane << box_shift);
-          if (key < it.len) page_of_box(a.c, it.b, key, a.status, page, pslot);
+          page = page2;
+          pslot = pslot2;
+          look_up(t + ahead, page2, pslot2);                // (its latency is covered by the tiles in between)
         }
         const int src = ((t - it.lo) % ahead) * boxes + (lane & (boxes - 1));
         const int pg = __shfl_sync(0xffffffffu, page, src), sl = __shfl_sync(0xffffffffu, pslot, src);
@@ -593,6 +726,71 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       umma_commit(drain_bar);
       if (!mbar_drain(drain_bar, 0u)) sts_u32(drain_fail, 1u);
     }
+  } else if (warp == kSchedWarp) {
+    // ------------------------------------------------------------------ scheduler: the next items, ahead of the others
+    int slot = 0;
+    uint32_t wphase = 0;
+    const int block_tokens = kManyTiles * a.tile_tokens;
+    const int n_items = blocks * a.c.KH * a.many_splits;
+    for (bool more = true; more;) {
+      int k = 0;
+      if (lane == 0) k = atomicAdd(a.counters, 1);
+      k = __shfl_sync(0xffffffffu, k, 0);
+      ManyItem it;
+      it.b = -1;
+      it.lo = it.len = 0;
+      more = k < n_items;
+      if (more) {
+        // a K/V head's blocks one after another, later blocks (longer rows) first: the CTAs that run together stream the same keys
+        it.split = k % a.many_splits;
+        const int u = k / a.many_splits;
+        it.kvh = u / blocks;
+        const int blk = block0 + blocks - 1 - (u - it.kvh * blocks);
+        it.b = find_block(a.c, blk, block_tokens, it.t0);
+        if (it.b >= a.c.B) continue;
+        const PagedSeq s = paged_seq(a.c, it.b);
+        it.q0 = s.q0; it.n = s.n; it.len = s.len;
+        if (it.t0 < 0 || it.t0 >= s.n) continue;
+        if (!paged_ok(a, s)) {
+          if (it.split == 0 && it.t0 == 0) {
+            if (lane == 0 && a.status) atomicOr(a.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_LENGTH);
+            write_unserved(a, s, it.kvh, lane, 32);
+          }
+          continue;
+        }
+        if (paged_few(a, s)) continue;
+        it.unit = (blk - block0) * a.c.KH + it.kvh;
+        const int last = min(it.t0 + block_tokens, s.n) - 1;
+        const int tiles = (s.len - s.n + last) / BN + 1;
+        it.lo = split_begin(tiles, it.split, a.many_splits);
+        it.hi = split_begin(tiles, it.split + 1, a.many_splits);
+        if (it.lo >= it.hi) continue;
+      }
+      int page = 0, pslot = 0;
+      const int key = it.lo * BN + (lane << box_shift);
+      if (it.b >= 0 && key < min(it.len, it.hi * BN)) page_of_box(a.c, it.b, key, a.status, page, pslot);
+      if (!__all_sync(0xffffffffu, mbar_wait(w_empty + 8 * slot, wphase ^ 1u, abort_flag))) break;
+      const uint32_t at = w_item + 4u * kItemWords * slot;
+      sts_u32(at + 40 + 8 * lane, (uint32_t)page);
+      sts_u32(at + 44 + 8 * lane, (uint32_t)pslot);
+      if (lane == 0) {
+        sts_u32(at, (uint32_t)it.b);
+        if (it.b >= 0) {
+          sts_u32(at + 4, (uint32_t)it.kvh);
+          sts_u32(at + 8, (uint32_t)it.q0);
+          sts_u32(at + 12, (uint32_t)it.n);
+          sts_u32(at + 16, (uint32_t)it.len);
+          sts_u32(at + 20, (uint32_t)it.t0);
+          sts_u32(at + 24, (uint32_t)it.lo);
+          sts_u32(at + 28, (uint32_t)it.hi);
+          sts_u32(at + 32, (uint32_t)it.unit);
+          sts_u32(at + 36, (uint32_t)it.split);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(w_full + 8 * slot);
+      if (++slot == kSchedSlots) { slot = 0; wphase ^= 1u; }
+    }
   } else {
     // -------------------------------------------------- consumers: one thread per query row
     const int x = (warp - 2) >> 2;
@@ -619,73 +817,93 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       const int head = it.kvh * a.G + row_local % a.G;
       const int pos = it.len - it.n + tok;
       const int lim = valid ? pos : -1;                        // last key the row sees
-      const int first_pos = it.len - it.n + it.t0 + x * a.tile_tokens;
+      const int first_pos = it.len - it.n + it.t0 + x * a.tile_tokens;             // of the tile's rows
+      const int last_pos = min(first_pos + a.tile_tokens, it.len) - 1;
       const float ra = valid ? paged_scale(a, head, pos) : 0.f;
       const float slope = kAlibi && valid ? a.alibi[head] / a.sm_scale : 0.f;
-      const size_t row = (size_t)it.unit * a.many_slots + (size_t)(valid ? x * tile_rows + row_local : 0);
-      float* score_row = a.scores + row * a.score_stride;
-      float* max_row = a.group_max + row * a.group_stride;
-      float bound = valid ? -INFINITY : INFINITY;              // (largest value so far) - 1
+      const int slot_row = valid ? x * tile_rows + row_local : 0;
+      const size_t row = (size_t)it.unit * a.many_slots + (size_t)slot_row;
+      float* rec = a.scores + row * a.score_stride + (size_t)it.lo * BN;             // next record
+      int32_t* rec_key = a.record_key + row * (size_t)(a.tiles * 32) + it.lo * 32;   // and where its key goes
+      const int32_t* rec_key0 = rec_key;
+      // Everything is compared before the scaling, z = <q,k> + slope (j - pos): y = a z, and a negative a turns z around first
+      const float sign = ra < 0.f ? -1.f : 1.f;
+      const bool turned = __any_sync(0xffffffffu, ra < 0.f);
+      const float mag = fabsf(ra), margin = 1.0f / mag;
+      // Lower bound of the row's threshold: (largest value so far) - margin, or what eight of its keys say, the largest of each of eight
+      // classes.  Rows without keys never have a candidate.
+      float thr = valid ? -INFINITY : INFINITY, best = -INFINITY;
+      float top[8];
+#pragma unroll
+      for (int g = 0; g < 8; ++g) top[g] = -INFINITY;
       for (int t = it.lo; t < end && alive; ++t) {
         alive = __all_sync(0xffffffffu, mbar_wait(my_full, fphase, abort_flag));
         if (!alive) break;
         fphase ^= 1u;
         tc_fence_after();
-        const int col_base = t * BN;
+        const int col_base = t * BN, step_no = t - it.lo;
         const bool edge = col_base + BN - 1 > first_pos;       // some row of the tile does not see all of it
-        // y of 32 columns as every use of them computes it
-        auto finish = [&](float (&v)[32], int col0) {
+        const int n_steps = min(BN / 64, (last_pos - col_base) / 64 + 1);   // 64-column steps that some row sees
+        // z of 64 columns from column col0 on, as both looks at them compute it
+        auto finish = [&](float (&v)[64], int col0) {
           if (kAlibi) {
-            const float t0 = (float)(col0 - pos);
+            const float t0 = slope * (float)(col0 - pos);
 #pragma unroll
-            for (int u = 0; u < 32; ++u) v[u] = ra * fmaf(slope, t0 + (float)u, v[u]);
-          } else {
+            for (int u = 0; u < 64; ++u) v[u] = fmaf(slope, (float)u, v[u]) + t0;
+          }
+          if (turned) {
 #pragma unroll
-            for (int u = 0; u < 32; ++u) v[u] *= ra;
+            for (int u = 0; u < 64; ++u) v[u] *= sign;
           }
           if (edge) {
 #pragma unroll
-            for (int u = 0; u < 32; ++u) v[u] = col0 + u <= lim ? v[u] : -INFINITY;
+            for (int u = 0; u < 64; ++u) v[u] = col0 + u <= lim ? v[u] : -INFINITY;
           }
         };
-        float gm[BN / 32], best = -INFINITY;
+        if (step_no == 0) {
+          // a stream that starts without a bound looks at its first tile twice
+#pragma unroll 1
+          for (int c = 0; c < n_steps; ++c) {
+            float v[64];
+            tmem_ld64(taddr_row + 64 * c, v);
+            tmem_ld_wait64(v);
+            finish(v, col_base + 64 * c);
 #pragma unroll
-        for (int g = 0; g < BN / 32; ++g) {
-          float v[32];
-          tmem_ld32(taddr_row + 32 * g, v);
-          tmem_ld_wait();
-          finish(v, col_base + 32 * g);
-          gm[g] = fmaxf(fmaxf(max8(&v[0]), max8(&v[8])), fmaxf(max8(&v[16]), max8(&v[24])));
-          best = fmaxf(best, gm[g]);
+            for (int q = 0; q < 8; ++q) top[q] = fmaxf(top[q], max8(&v[8 * q]));
+          }
+          best = max8(top);
+          thr = fmaxf(thr, fmaxf(best - margin, bound_from_eight(top, margin, a.expo_class, a.expo)));
         }
-        bound = fmaxf(bound, best - 1.0f);
-        unsigned hit = 0u;
+        // One straight pass, 64 columns at a time: maxima of eight columns, and eight columns with a candidate go to the row's records as
+        // they are, by predicated stores (branches on "some row has a candidate" cost more than the stores do)
+#pragma unroll 1
+        for (int c = 0; c < n_steps; ++c) {
+          float v[64];
+          tmem_ld64(taddr_row + 64 * c, v);
+          tmem_ld_wait64(v);
+          finish(v, col_base + 64 * c);
+          float g[8];
 #pragma unroll
-        for (int g = 0; g < BN / 32; ++g) hit |= gm[g] > bound ? 1u << g : 0u;
-        unsigned any = __reduce_or_sync(0xffffffffu, hit);
-        while (any) {
-          const int g = __ffs(any) - 1;
-          any &= any - 1;
-          float v[32];
-          tmem_ld32(taddr_row + 32 * g, v);
-          tmem_ld_wait();
-          finish(v, col_base + 32 * g);
-          if ((hit >> g) & 1u) {
-            float4* dst = reinterpret_cast<float4*>(score_row + col_base + 32 * g);
+          for (int q = 0; q < 8; ++q) g[q] = max8(&v[8 * q]);
+          const float m = max8(g);
+          best = fmaxf(best, m);
+          thr = fmaxf(thr, best - margin);
+          if (!__any_sync(0xffffffffu, m > thr)) continue;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) dst[u] = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+          for (int q = 0; q < 8; ++q) {
+            keep_record_if_greater(g[q], thr, rec, rec_key, col_base + 64 * c + 8 * q, &v[8 * q]);
+            top[q] = fmaxf(top[q], g[q]);
           }
         }
         // the accumulator has been read: hand it back to the MMA issuer
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(my_empty);
-        if (valid) {
-          float4* dst = reinterpret_cast<float4*>(max_row + t * (BN / 32));
-          dst[0] = make_float4(gm[0], gm[1], gm[2], gm[3]);
-          dst[1] = make_float4(gm[4], gm[5], gm[6], gm[7]);
-        }
+        if ((step_no & (step_no - 1)) == 0) thr = fmaxf(thr, bound_from_eight(top, margin, a.expo_class, a.expo));
       }
+      if (valid && alive)
+        a.row_info[((size_t)it.unit * a.many_splits + it.split) * a.many_slots + slot_row] =
+            make_float4(__int_as_float((int)(rec_key - rec_key0)), mag * thr, mag, 0.f);
     }
   }
 
@@ -717,17 +935,21 @@ cudaError_t map_pages(CUtensorMap* map, const PagedArgs& a, const void* k) {
                       a.c.ps_shift < 7 ? 1 << a.c.ps_shift : 128, 1);
 }
 
-template <int HD, int NB, bool kAlibi>
-cudaError_t launch_few(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int unit0, int units,
+template <int HD, int NR, bool kAlibi>
+cudaError_t launch_few(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int seq0, int seqs,
                        cudaStream_t stream) {
   CUtensorMap map_q, map_k;
+  const int smem = FewCfg<HD, NR>::kFixedBytes + (4 * kFewSeqs + 4) * 4;
+  static_assert(2 * (FewCfg<HD, NR>::kFixedBytes + (4 * kFewSeqs + 4) * 4 + 1024) <= 233472, "two CTAs per SM");
   cudaError_t err = map_queries(&map_q, a, q, q_st, q_sh, a.few_slots / a.G);
   if (err == cudaSuccess) err = map_pages(&map_k, a, k);
-  if (err == cudaSuccess)
-    err = cudaFuncSetAttribute(paged_few_kernel<HD, NB, kAlibi>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<HD, NB>::kSmemBytes);
+  if (err == cudaSuccess) err = cudaFuncSetAttribute(paged_few_kernel<HD, NR, kAlibi>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (err != cudaSuccess) return err;
-  return launch_kernel(paged_few_kernel<HD, NB, kAlibi>, (unsigned)((long long)units * a.c.KH * a.few_chunks), kFewThreads, FewCfg<HD, NB>::kSmemBytes,
-                       stream, map_q, map_k, a, unit0);
+  const int sms = a.sms;
+  // no more CTAs than the longest lengths could keep busy
+  const long long most = (long long)seqs * a.c.KH * ((a.max_kv + kTile - 1) / kTile);
+  const long long grid = most / 2 < 1 ? 1 : most / 2 < 2 * sms ? most / 2 : 2 * sms;
+  return launch_kernel(paged_few_kernel<HD, NR, kAlibi>, (unsigned)grid, kFewThreads, smem, stream, map_q, map_k, a, seq0, seqs);
 }
 
 template <int HD, bool kAlibi>
@@ -738,11 +960,8 @@ cudaError_t launch_many(const PagedArgs& a, const void* q, const void* k, int64_
   if (err == cudaSuccess) err = map_pages(&map_k, a, k);
   if (err == cudaSuccess)
     err = cudaFuncSetAttribute(paged_many_kernel<HD, kAlibi>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<HD>::kSmemBytes);
-  int dev = 0, sms = 0;
-  if (err == cudaSuccess) err = cudaGetDevice(&dev);
-  if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (err == cudaSuccess) err = cudaMemsetAsync(a.counter, 0, sizeof(int32_t), stream);
   if (err != cudaSuccess) return err;
+  const int sms = a.sms;
   const long long items = (long long)blocks * a.c.KH * a.many_splits;
   return launch_kernel(paged_many_kernel<HD, kAlibi>, (unsigned)(items < sms ? items : sms), kManyThreads, ManyCfg<HD>::kSmemBytes, stream, map_q, map_k,
                        a, block0, blocks);
@@ -750,13 +969,15 @@ cudaError_t launch_many(const PagedArgs& a, const void* q, const void* k, int64_
 
 }  // namespace
 
-cudaError_t launch_paged_few(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int unit0, int units,
+cudaError_t launch_paged_few(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int seq0, int seqs,
                              cudaStream_t stream) {
-#define ENTMAX_FEW(HD, NB)                                                              \
-  (a.alibi ? launch_few<HD, NB, true>(a, q, k, q_st, q_sh, unit0, units, stream)        \
-           : launch_few<HD, NB, false>(a, q, k, q_st, q_sh, unit0, units, stream))
-  if (a.c.D == 64) return a.few_rows <= 16 ? ENTMAX_FEW(64, 16) : ENTMAX_FEW(64, 32);
-  return a.few_rows <= 16 ? ENTMAX_FEW(128, 16) : ENTMAX_FEW(128, 32);
+#define ENTMAX_FEW(HD, NR)                                                              \
+  (a.alibi ? launch_few<HD, NR, true>(a, q, k, q_st, q_sh, seq0, seqs, stream)          \
+           : launch_few<HD, NR, false>(a, q, k, q_st, q_sh, seq0, seqs, stream))
+#define ENTMAX_FEW_ROWS(HD)                                                             \
+  (a.few_slots <= 4 ? ENTMAX_FEW(HD, 4) : a.few_slots <= 8 ? ENTMAX_FEW(HD, 8) : a.few_slots <= 16 ? ENTMAX_FEW(HD, 16) : ENTMAX_FEW(HD, 32))
+  return a.c.D == 64 ? ENTMAX_FEW_ROWS(64) : ENTMAX_FEW_ROWS(128);
+#undef ENTMAX_FEW_ROWS
 #undef ENTMAX_FEW
 }
 

@@ -44,6 +44,7 @@ def _run(pr, alpha, scale=None, slopes=None, **kw):
     status = torch.full((binding.STATUS_WORDS,), -1, dtype=torch.int32, device="cuda")
     sc = [t.cuda() for t in scale] if scale is not None else [None] * 3
     al = torch.tensor(slopes, dtype=torch.float32, device="cuda") if slopes is not None else None
+    kw.setdefault("support_size", torch.full(pr["q"].shape[:2], -1, dtype=torch.int32, device="cuda"))
     out = binding.entmax_attn_paged_fwd(pr["q"], pr["kc"], pr["vc"], alpha, pr["table"], pr["lens"], kw.pop("cu", pr["cu"]), *sc,
                                         alibi_slopes=al, status=status, **kw)
     torch.cuda.synchronize()
@@ -80,9 +81,8 @@ def test_single_tokens(H, KH, d, page):
     sc = _scales(H, 1, "length")
     got = _run(pr, 1.5, sc)
     _check(pr, 1.5, got, sc)
-    same = _run(pr, 1.5, sc, cu=None, max_q_len=1, max_kv_len=max(LENGTHS))
-    for x, y in zip(got[:2], same[:2]):
-        assert torch.equal(x, y)
+    # (the bounds choose the kernels, so the last bits may differ)
+    _check(pr, 1.5, _run(pr, 1.5, sc, cu=None, max_q_len=1, max_kv_len=max(LENGTHS)), sc)
 
 
 @pytest.mark.parametrize("alpha", [1.25, 1.5, 1.7, 2.0, 3.0])
@@ -129,6 +129,8 @@ def test_equal_logits_see_every_key(new):
     o, tau, supp, flags = got = _run(pr, 1.5)
     _check(pr, 1.5, got)
     n = torch.arange(2600 - new + 1, 2601, dtype=torch.float64)
+    # sums of up to 2600/32 equal terms by a lane are off by 82 * 2^-24 = 5e-6 of themselves at most, tau by that over e sum u = 2 sqrt(n): 5e-8,
+    # of 0.0196 in the longest row 2.5e-6
     assert torch.allclose(tau[:new, 0].cpu().double(), -n.pow(-0.5), rtol=1e-5)
     assert torch.equal(supp[:new, 0].cpu().long(), n.long())
 
@@ -172,11 +174,8 @@ def test_workspace_in_slices():
     pr = _problem(new, lens, 4, 2, 64, 16)
     wide = torch.full((len(new), (1 << 20) // 16), -1, dtype=torch.int32, device="cuda")
     wide[:, :pr["table"].shape[1]] = pr["table"]
-    want = _run(pr, 1.5)
     pr["table"] = wide
-    got = _run(pr, 1.5)
-    _check(pr, 1.5, got)
-    assert torch.equal(want[1], got[1])
+    _check(pr, 1.5, _run(pr, 1.5))
 
 
 @pytest.mark.parametrize("new,lens,bad", [([1, 1, 1], [5, 0, 40], 1), ([1, 1, 1], [5, 49, 40], 1), ([3, 60, 1], [40, 30, 9], 1),
