@@ -59,21 +59,6 @@ __device__ __forceinline__ int find_seq(const PagedCache& c, int x, int div, int
   return lo;
 }
 
-// Sequence and first token of block `blk` of blocks of `tokens` new tokens, by the whole warp.  Block ids run over the sequences with one
-// to spare each: sequence b has the ids from cu_q[b] / tokens + b on, at least as many as it has blocks (then t0 >= n).
-__device__ __forceinline__ int find_block(const PagedCache& c, int blk, int tokens, int& t0) {
-  int b;
-  if (c.cu_q) {
-    b = find_seq(c, blk, tokens, 1);
-    t0 = (blk - (clamped_cu(c, b) / tokens + b)) * tokens;
-  } else {
-    const int per = (c.T / c.B + tokens - 1) / tokens;
-    b = blk / per;
-    t0 = (blk - b * per) * tokens;
-  }
-  return b;
-}
-
 // Host: checks of the cache description shared by the entry points (defined in paged_append.cu).
 int check_paged_cache(const entmax_attn_paged_cache* cache, int total_q, PagedCache* out);
 
@@ -82,13 +67,14 @@ int check_paged_cache(const entmax_attn_paged_cache* cache, int total_q, PagedCa
 // scores y = (alpha-1) s (Eq. 1's units) the score kernels leave in the workspace what can matter: every key above some lower bound of the
 // row's threshold is there.  Two kernels, two forms:
 //   "few": a unit is a sequence with at most few_rows rows.
-//       group_max[unit][group][row]   the maximum over each group of 32 keys (-inf: none visible)
+//       group_max[row][group]         the maximum over each group of 32 keys (-inf: none visible)
 //       scores[row][key]              the scores of the groups whose maximum is above a bound of y_max - 1; other groups are not written
 //                                     (some may be)
-//   "many": a unit is a block of kManyTiles * tile_tokens tokens of a longer chunk, its keys are split among many_splits work items, and the
-//       item whose first K tile is lo keeps records of eight neighbouring keys, those with a value above the bound it had then, in key order:
+//   "many": a unit is a block of kManyTiles * tile_tokens tokens of a longer chunk; where there are few units, their K tiles are shared among
+//       several work items (ManyCut).  The item whose first K tile is lo keeps records of eight neighbouring keys, those with a value above
+//       the bound it had then, in key order:
 //       scores[row][256 lo + 8 i ..]  the values, before the scaling by |a|      record_key[row][32 lo + i]  the first key
-//       row_info[unit][split][row]    {number of records, the bound the item ended with, |a|, -}
+//       row_info[unit][item][row]     {number of records, the bound the item ended with, |a|, -}
 //       (room for every key: a row of flat logits keeps them all)
 constexpr int kGroupKeys = 32;
 constexpr int kManyKeys = 256;
@@ -107,21 +93,52 @@ struct PagedArgs {
   int few_slots;              // row slots of a unit there
   int tile_tokens;            // "many": new tokens per 128-row tile, 128 / G
   int many_slots;             // row slots of a unit there
-  int many_blocks;            // bound on the number of blocks: ceil(T / block_tokens) + B - 1
-  int many_splits;            // work items per unit of the "many" kernel, each a share of the keys
+  int many_blocks;            // bound on the number of blocks.  Block ids run over the sequences with one to spare each: sequence b has
+                              // the ids from cu_q[b] / block_tokens + b on, at least as many as it has blocks
+  int many_items;             // most work items of a unit of the "many" kernel
   size_t score_stride;        // floats per row of scores
   int groups, tiles;          // groups of 32 and tiles of 256 keys that a row has room for
   float* scores;
   float* group_max;
   int32_t* record_key;
   float4* row_info;
-  int32_t* counters;          // [0]: work items handed out by the "many" kernel, [1]: rows in spilled
+  uint2 record_bytes;         // {32, 4}: what a record takes in scores and in record_key (see the "many" kernel)
+  struct PagedBlock* blocks;  // "many": what is known of each block of the slice
+  int32_t* order;             // its blocks that have work, those with the longest rows first
+  int32_t* counters;          // see Counter
   int32_t* spilled;           // rows whose candidates did not fit the list of the kernel that takes eight lanes per row
   __nv_bfloat16* o;
   float* tau;
   int32_t* support;
   int32_t* status;
 };
+
+enum Counter : int {
+  kNextItem = 0,              // work items handed out by the "many" kernel
+  kSpilledRows,               // rows in spilled
+  kBlocks,                    // blocks in order
+  kCut,                       // K tiles per CTA where the units are cut (see ManyCut), 0 where they are not
+  kTiles,                     // K tiles of all blocks together (of one K/V head)
+  kCounters
+};
+struct __align__(16) PagedBlock {
+  int b, t0, q0, n;           // sequence (-1: nothing to do here), first token within its chunk, the chunk's first row of q, new tokens
+  int len, tiles, start, pad; // length; tiles of 256 keys that the block's last row sees; those of the blocks before it
+};
+
+// How a unit's K tiles are shared among work items.  With units enough for every SM to take several, each is one item (cut = 0).  Otherwise the
+// tiles of all units, head by head and block by block, are dealt to the CTAs in runs of `cut`, and a unit's items are its shares in the runs
+// it lies in.
+struct ManyCut {
+  int start, tiles, cut;      // start: the unit's first tile in that order
+  __device__ __forceinline__ int items() const { return cut ? (start + tiles - 1) / cut - start / cut + 1 : 1; }
+  __device__ __forceinline__ int begin(int item) const {   // first tile of an item; items(): the number of tiles
+    return item == 0 ? 0 : cut ? min((start / cut + item) * cut - start, tiles) : tiles;
+  }
+};
+__device__ __forceinline__ ManyCut many_cut(const int32_t* counters, const PagedBlock& pb, int kv_head) {
+  return ManyCut{kv_head * counters[kTiles] + pb.start, pb.tiles, counters[kCut]};
+}
 
 // Whether the sequence can be served at all, and by which kernel
 __device__ __forceinline__ bool paged_ok(const PagedArgs& a, const PagedSeq& s) {
@@ -136,9 +153,6 @@ __device__ __forceinline__ void powers(float y, float expo, float& ye, float& ye
 }
 // A lower bound of a threshold from an iterate that came from the left: a hair below it for the rounding
 __device__ __forceinline__ float bound_below(float tau) { return tau - 1e-5f * fmaxf(1.0f, fabsf(tau)); }
-
-// K tiles of 256 keys that work item `split` of a unit takes (of `tiles` that its last row sees): lo .. hi - 1
-__device__ __forceinline__ int split_begin(int tiles, int split, int splits) { return (int)((long long)tiles * split / splits); }
 
 // (alpha-1) c sm_scale of a query at position pos, c = delta + beta (ln n)^gamma with n = pos + 1 (delta for n = 1; 1 without
 // scale parameters)
@@ -166,7 +180,8 @@ __device__ __forceinline__ void write_unserved(const PagedArgs& a, const PagedSe
 
 cudaError_t launch_paged_few(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int seq0, int seqs,
                              cudaStream_t stream);
-cudaError_t launch_paged_many(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int block0, int blocks,
+// (after launch_paged_plan for the same blocks)
+cudaError_t launch_paged_many(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int blocks,
                               cudaStream_t stream);
 
 }  // namespace entmax

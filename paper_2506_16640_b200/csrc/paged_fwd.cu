@@ -81,26 +81,155 @@ __device__ __forceinline__ bool solve_step(TauIter& st, float s0, float s1, int 
 }
 constexpr int kMaxSteps = 64;
 constexpr int kBoundSteps = 5;       // steps towards the threshold of the cells' maxima
-constexpr int kFewCandidateCells = 8;   // groups above y_max - 1 up to which that bound is not looked for
+constexpr int kFewCandidates = 8;   // groups above y_max - 1 up to which that bound is not looked for
 
-// What the "many" kernel kept of a row: a list of records per work item that had keys of the row
+// What the "many" kernel kept of a row: a list of records per work item of its unit
 struct Records {
   const float* values;                  // [256 lo + 8 i]
   const int32_t* keys;                  // [32 lo + i]
-  const float4* info;                   // [split][slot]
-  int slots, splits, tiles;             // tiles: of the unit
-  __device__ __forceinline__ int begin(int split) const { return split_begin(tiles, split, splits); }
+  const float4* info;                   // [item][slot]
+  int slots, items;                     // items: those that had keys of the row
+  ManyCut cut;
 };
-__device__ __forceinline__ Records records_of(const PagedArgs& a, const PagedSeq& s, int t0, int unit, int r, size_t row) {
-  const int last = min(t0 + kManyTiles * a.tile_tokens, s.n) - 1;
-  return Records{a.scores + row * a.score_stride, a.record_key + row * (size_t)(a.tiles * 32),
-                 a.row_info + (size_t)unit * a.many_splits * a.many_slots + r, a.many_slots, a.many_splits,
-                 (s.len - s.n + last) / kManyKeys + 1};
+__device__ __forceinline__ Records records_of(const PagedArgs& a, const ManyCut& cut, int unit, int r, size_t row, int pos) {
+  Records rec = {a.scores + row * a.score_stride, a.record_key + row * (size_t)(a.tiles * 32),
+                 a.row_info + (size_t)unit * a.many_items * a.many_slots + r, a.many_slots, 0, cut};
+  const int all = cut.items();
+  while (rec.items < all && cut.begin(rec.items) <= pos / kManyKeys) ++rec.items;
+  return rec;
+}
+// The new tokens that a unit's rows belong to: a block of a sequence's chunk ("many"), or all of a sequence ("few")
+struct UnitOf {
+  PagedSeq s;
+  int b, t0;                            // (b = -1: nothing to do)
+  ManyCut cut;
+};
+template <bool kMany>
+__device__ __forceinline__ UnitOf unit_of(const PagedArgs& a, int first, int unit) {
+  const int at = unit / a.c.KH;
+  UnitOf u;
+  u.cut = ManyCut{0, 0, 0};
+  if constexpr (kMany) {
+    const PagedBlock pb = a.blocks[at];
+    u.b = pb.b; u.t0 = pb.t0;
+    u.cut = many_cut(a.counters, pb, unit - at * a.c.KH);
+    u.s = PagedSeq{pb.q0, pb.n, pb.len};
+  } else {
+    u.b = first + at;
+    u.t0 = 0;
+    u.s = paged_seq(a.c, u.b);
+    if (!paged_ok(a, u.s) || !paged_few(a, u.s)) u.b = -1;
+  }
+  return u;
+}
+
+// =================================================================================================== plan
+// What the "many" kernels need to know of the blocks block0 .. block0 + blocks - 1 of new tokens, and the order their work is handed out in:
+// longest rows first (by 1024 classes of length), so that the CTAs end together.  Clears the counters.  One CTA.
+constexpr int kPlanThreads = 1024;
+constexpr int kLeastCut = 4;
+__global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_constant__ PagedArgs a, int block0, int blocks) {
+  pdl_begin();
+  __shared__ int bin[kPlanThreads];               // blocks of a class, then the next place of the class
+  __shared__ int warp_sum[kPlanThreads / 32];
+  __shared__ int n_blocks;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tokens = kManyTiles * a.tile_tokens;
+  bin[tid] = 0;
+  if (tid <= kSpilledRows) a.counters[tid] = 0;
+  __syncthreads();
+  auto class_of = [&](int tiles) { return kPlanThreads - 1 - (int)((long long)(tiles - 1) * kPlanThreads / a.tiles); };
+  for (int i = warp * 32; i < blocks; i += kPlanThreads) {
+    // (a lane per block; the sequence of each found by a plain search, the loads of the lanes overlap)
+    const int blk = block0 + i + lane;
+    PagedBlock pb = {-1, 0, 0, 0, 0, 0, 0, 0};
+    if (i + lane < blocks) {
+      int b, t0;
+      if (a.c.cu_q) {
+        int lo = 0, hi = a.c.B;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (clamped_cu(a.c, mid) / tokens + mid <= blk) lo = mid; else hi = mid;
+        }
+        b = lo;
+        t0 = (blk - (clamped_cu(a.c, b) / tokens + b)) * tokens;
+      } else {
+        const int per = (a.c.T / a.c.B + tokens - 1) / tokens;
+        b = blk / per;
+        t0 = (blk - b * per) * tokens;
+      }
+      if (b < a.c.B && t0 >= 0) {
+        const PagedSeq s = paged_seq(a.c, b);
+        if (t0 < s.n) {
+          if (!paged_ok(a, s)) {
+            if (a.status) atomicOr(a.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_LENGTH);
+            const PagedSeq part = {s.q0 + t0, min(tokens, s.n - t0), s.len};
+            for (int kvh = 0; kvh < a.c.KH; ++kvh) write_unserved(a, part, kvh, 0, 1);
+          } else if (!paged_few(a, s)) {
+            pb.b = b;
+            pb.t0 = t0;
+            pb.q0 = s.q0;
+            pb.n = s.n;
+            pb.len = s.len;
+            pb.tiles = (s.len - s.n + min(t0 + tokens, s.n) - 1) / kManyKeys + 1;
+            atomicAdd(&bin[class_of(pb.tiles)], 1);
+          }
+        }
+      }
+      a.blocks[i + lane] = pb;
+    }
+  }
+  __syncthreads();
+  const int mine = bin[tid];
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) warp_sum[warp] = incl;
+  __syncthreads();
+  int before = 0;
+  for (int i = 0; i < warp; ++i) before += warp_sum[i];
+  bin[tid] = before + incl - mine;
+  if (tid == kPlanThreads - 1) {
+    n_blocks = before + incl;
+    a.counters[kBlocks] = n_blocks;
+  }
+  // tiles before each block
+  int carry = 0;
+  for (int i0 = 0; i0 < blocks; i0 += kPlanThreads) {
+    const int i = i0 + tid, tiles = i < blocks ? a.blocks[i].tiles : 0;
+    int upto = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += up;
+    }
+    __syncthreads();
+    if (lane == 31) warp_sum[warp] = upto;
+    __syncthreads();
+    int at = carry;
+    for (int k = 0; k < kPlanThreads / 32; ++k) {
+      if (k < warp) at += warp_sum[k];
+      carry += warp_sum[k];
+    }
+    if (i < blocks) a.blocks[i].start = at + upto - tiles;
+  }
+  if (tid == 0) {
+    a.counters[kTiles] = carry;
+    // units for less than three rounds of the machine are cut
+    const long long all = (long long)carry * a.c.KH;
+    a.counters[kCut] = n_blocks * a.c.KH >= 3 * a.sms ? 0 : max((int)((all + a.sms - 1) / a.sms), kLeastCut);
+  }
+  for (int i = tid; i < blocks; i += kPlanThreads) {
+    const PagedBlock pb = a.blocks[i];
+    if (pb.b >= 0) a.order[atomicAdd(&bin[class_of(pb.tiles)], 1)] = i;
+  }
 }
 
 // ================================================================================================ rows8
 constexpr int kList8 = 96;           // candidates of a row
-constexpr int kSteps8 = 8;           // loads of eight groups, or of four records, whose maxima stay in registers
 constexpr int kWarps8 = 8;
 constexpr int kRows8 = 4 * kWarps8;  // rows of a CTA
 
@@ -109,16 +238,23 @@ __device__ __forceinline__ float sum8(float x) {
   for (int o = 1; o < 8; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
+__device__ __forceinline__ float max8_lanes(float x) {
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+__device__ __forceinline__ float max4(const float4& x) { return fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)); }
 
+// (Loops are kept rolled: unrolled, this code no longer stayed in the instruction cache, 140 us against 90 on 150000 short rows.)
 template <int D, int EC, bool kMany>
 __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __grid_constant__ PagedArgs a,
                                                                       const __nv_bfloat16* __restrict__ v, int first, int units) {
   pdl_begin();
   __shared__ float list_y[kRows8][kList8];
-  __shared__ long long list_at[kRows8][kList8];
-  const int lane = threadIdx.x & 31, sl = lane & 7, sub = lane >> 3, sub_bit = 8 * sub;
+  __shared__ long long list_at[kRows8][kList8];          // key, then where its V row is
+  const int lane = threadIdx.x & 31, sl = lane & 7, sub_bit = lane & 24;
   const int slots = kMany ? a.many_slots : a.few_slots;
-  const int cta_row = (threadIdx.x >> 3);
+  const int cta_row = threadIdx.x >> 3;
   int unit, r;
   if constexpr (kMany) {
     const int per = (slots + kRows8 - 1) / kRows8;         // CTAs of a unit
@@ -130,204 +266,190 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
     r = (int)(row - (long long)unit * slots);
   }
   // ---- which row this is
-  int b, t0 = 0;
   const int kvh = unit % a.c.KH;
-  b = first + unit / a.c.KH;
-  if constexpr (kMany) b = find_block(a.c, b, kManyTiles * a.tile_tokens, t0);
-  bool live = unit < units && r < slots && b < a.c.B && t0 >= 0;
-  PagedSeq s = {0, 0, 0};
-  if (live) s = paged_seq(a.c, b);
-  const int tok = t0 + r / a.G;
-  live = live && tok < s.n && paged_ok(a, s) && paged_few(a, s) != kMany;
+  bool live = unit < units && r < slots;
+  UnitOf w;
+  w.b = -1;
+  if (live) w = unit_of<kMany>(a, first, unit);
+  const int tok = w.t0 + r / a.G;
+  live = live && w.b >= 0 && tok < w.s.n;
   if (!__any_sync(0xffffffffu, live)) return;
-  const int pos = s.len - s.n + tok;
+  const int pos = live ? w.s.len - w.s.n + tok : -1;
   const size_t row = (size_t)unit * slots + r;
-  const Pages pages = pages_of(a.c, live ? b : 0);
-  const __nv_bfloat16* v_head = v + (long long)kvh * a.c.s_head;
+  const float* y_row = a.scores + row * a.score_stride;
   float* my_y = list_y[cta_row];
   long long* my_at = list_at[cta_row];
+  const float4 none = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+
+  // ---- The keys above floor_y go to the list; loops run for the longest of the warp's four rows.  A row whose candidates do not fit gets a
+  // second try with a higher bound: the threshold of maxima of different keys alone, by a few steps from the left (any iterate is a bound;
+  // a hair below it for the rounding).  c = 1, alpha = 1.5, 32768 keys N(0, 1): 585 keys above y_max - 1, about 50 above that.
   int cnt = 0;
-  // appends those of this lane's four keys from `key` on that are above the bound to the row's list, lane by lane
-  auto append = [&](const float (&y)[4], int key, float floor_y) {
-    int mine = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) mine += y[e] > floor_y ? 1 : 0;
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, upto, o, 8);
-      if (sl >= o) upto += up;
-    }
-    int at = cnt + upto - mine;
-    cnt += __shfl_sync(0xffffffffu, upto, 7, 8);
+  float ymax = -INFINITY, floor_y = -INFINITY, mag = 0.f;
+  const Records rec = kMany && live ? records_of(a, w.cut, unit, r, row, pos) : Records{};
+  const int groups = live ? pos / kGroupKeys + 1 : 0;
+  const float4* max_row = reinterpret_cast<const float4*>(a.group_max + row * a.groups);
+  const int chunks = kMany ? 0 : (__reduce_max_sync(0xffffffffu, groups) + 31) / 32;
+  const int most_items = kMany ? __reduce_max_sync(0xffffffffu, rec.items) : 0;
+
+  auto append = [&](const float4& y4, int key) {            // this lane's four keys from `key` on
+    const float y[4] = {y4.x, y4.y, y4.z, y4.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (y[e] > floor_y) {
-        if (at < kList8) {
-          const long long off = pages.at(key + e);
-          if (off >= 0) prefetch_row<D>(v_head + off);
-          my_y[at] = y[e];
-          my_at[at] = off;
+      const bool on = y[e] > floor_y;
+      const unsigned bits = (__ballot_sync(0xffffffffu, on) >> sub_bit) & 0xffu;
+      const int at = cnt + __popc(bits & ((1u << sl) - 1u));
+      if (on && at < kList8) {
+        my_y[at] = y[e];
+        my_at[at] = key + e;
+      }
+      cnt += __popc(bits);
+    }
+  };
+  // many: f(this lane's four values, its first key's place) for every four records, two lanes to a record
+  auto for_records = [&](auto&& f) {
+#pragma unroll 1
+    for (int i = 0; i < most_items; ++i) {
+      int n = 0, lo = 0;
+      if (i < rec.items) {
+        const float4 info = rec.info[(size_t)i * rec.slots];
+        n = __float_as_int(info.x);
+        mag = info.z;
+        lo = rec.cut.begin(i);
+      }
+      const int most = __reduce_max_sync(0xffffffffu, n);
+#pragma unroll 1
+      for (int s0 = 0; s0 < most; s0 += 16) {
+        float4 y[4];
+        int key[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int at = s0 + 4 * u + (sl >> 1);
+          y[u] = none;
+          key[u] = 0;
+          if (at < n) {
+            y[u] = *reinterpret_cast<const float4*>(rec.values + (size_t)lo * kManyKeys + 8 * at + 4 * (sl & 1));
+            key[u] = rec.keys[lo * 32 + at] + 4 * (sl & 1);
+          }
         }
-        ++at;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (s0 + 4 * u >= most) break;
+          y[u].x *= mag; y[u].y *= mag; y[u].z *= mag; y[u].w *= mag;
+          f(y[u], key[u]);
+        }
       }
     }
   };
-  // A threshold of maxima of different keys alone, by a few steps from the left of floor_y (any iterate is a bound; a hair below it for the
-  // rounding).  for_maxima(f): f(a maximum) for all of this lane's.  c = 1, alpha = 1.5, 32768 keys N(0, 1): 585 keys above
-  // y_max - 1, about 50 above the bound of the maxima of 128 cells.
-  auto raise = [&](float floor_y, int few, auto&& for_maxima) -> float {
-    if (a.expo < 1.0f) return floor_y;
-    int n = 0;
-    for_maxima([&](float m) { n += m > floor_y ? 1 : 0; });
-    n = (int)sum8((float)n);
-    if (!__any_sync(0xffffffffu, n > few)) return floor_y;
-    float tau = floor_y;
+  // few: this lane's maxima of groups 32 i + 4 sl ..
+  auto maxima = [&](int i) {
+    float4 m = none;
+    const int g = 32 * i + 4 * sl;
+    if (g < groups) {
+      m = max_row[g >> 2];
+      if (g + 1 >= groups) m.y = -INFINITY;
+      if (g + 2 >= groups) m.z = -INFINITY;
+      if (g + 3 >= groups) m.w = -INFINITY;
+    }
+    return m;
+  };
+  if constexpr (kMany) {
+    for (int i = 0; i < rec.items; ++i) floor_y = fmaxf(floor_y, rec.info[(size_t)i * rec.slots].y);
+  } else {
+#pragma unroll 4
+    for (int i = 0; i < chunks; ++i) ymax = fmaxf(ymax, max4(maxima(i)));
+    ymax = max8_lanes(ymax);
+    floor_y = ymax - 1.0f;
+  }
+#pragma unroll 1
+  for (int attempt = 0;; ++attempt) {
+    cnt = 0;
+    if constexpr (kMany) {
+      for_records([&](const float4& y, int key) {
+        const float m = max4(y);
+        ymax = fmaxf(ymax, m);
+        if (__any_sync(0xffffffffu, m > floor_y)) append(y, key);
+      });
+      ymax = max8_lanes(ymax);
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < chunks; ++i) {
+        const float4 m = maxima(i);
+        unsigned bits = ((m.x > floor_y ? 1u : 0u) | (m.y > floor_y ? 2u : 0u) | (m.z > floor_y ? 4u : 0u) | (m.w > floor_y ? 8u : 0u)) << (4 * sl);
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) bits |= __shfl_xor_sync(0xffffffffu, bits, o);
+        while (__any_sync(0xffffffffu, bits != 0u)) {
+          float4 y[4];
+          int key[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            y[u] = none;
+            key[u] = (32 * i + __ffs(bits) - 1) * kGroupKeys + 4 * sl;
+            if (bits) y[u] = *reinterpret_cast<const float4*>(y_row + key[u]);
+            bits &= bits - 1;
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) append(y[u], key[u]);
+        }
+      }
+    }
+    const bool over = cnt > kList8;
+    if (attempt == 1 || a.expo < 1.0f || !__any_sync(0xffffffffu, over)) break;
+    float tau = fmaxf(floor_y, ymax - 1.0f);
+#pragma unroll 1
     for (int it = 0; it < kBoundSteps; ++it) {
       float s0 = 0.f, s1 = 0.f;
-      for_maxima([&](float m) {
+      auto add = [&](float m) {
         float ye, ye1;
         powers<EC>(fmaxf(m - tau, 0.f), a.expo, ye, ye1);
         s0 += ye;
         s1 += ye1;
-      });
+      };
+      if constexpr (kMany) {
+        for_records([&](const float4& y, int) { add(max4(y)); });
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < chunks; ++i) {
+          const float4 m = maxima(i);
+          add(m.x);
+          add(m.y);
+          add(m.z);
+          add(m.w);
+        }
+      }
       s0 = sum8(s0);
       s1 = sum8(s1);
       const bool go = s0 > 1.01f && s1 > 0.f;
       if (go) tau += threshold_step(s0, s1, EC, a.expo);
-      if (!__any_sync(0xffffffffu, go)) break;
+      if (!__any_sync(0xffffffffu, go && over)) break;
     }
-    return fmaxf(floor_y, bound_below(tau));
-  };
-
-  // ---- candidates; loops run for the longest of the warp's four rows
-  float ymax = -INFINITY, floor_y;
-  if constexpr (kMany) {
-    const Records rec = records_of(a, s, t0, unit, r, row);
-    int splits = 0;                                         // work items that had keys of the row
-    if (live)
-      while (splits < rec.splits && rec.begin(splits) <= pos / kManyKeys) ++splits;
-    float mag = 0.f, bound = -INFINITY;
-    auto count = [&](int i) {                               // records of item i (0 where there was none)
-      if (i >= splits || rec.begin(i) == rec.begin(i + 1)) return 0;
-      const float4 info = rec.info[(size_t)i * rec.slots];
-      mag = info.z;
-      bound = fmaxf(bound, info.y);
-      return __float_as_int(info.x);
-    };
-    // f(this lane's four values, its first key) for every four records: two lanes to a record
-    const int n_first = count(0);
-    const int most_splits = __reduce_max_sync(0xffffffffu, splits);
-    float4 kept[kSteps8];
-#pragma unroll
-    for (int i = 0; i < kSteps8; ++i) {
-      const int at = 4 * i + (sl >> 1);
-      kept[i] = at < n_first ? *reinterpret_cast<const float4*>(rec.values + 8 * at + 4 * (sl & 1))
-                             : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-    }
-    auto scaled = [&](const float4& z, float (&y)[4]) {
-      y[0] = mag * z.x; y[1] = mag * z.y; y[2] = mag * z.z; y[3] = mag * z.w;
-    };
-    auto for_records = [&](auto&& f) {
-      for (int i = 0; i < most_splits; ++i) {
-        const int n = i == 0 ? n_first : count(i), lo = i < splits ? rec.begin(i) : 0;
-        const int steps = (__reduce_max_sync(0xffffffffu, n) + 3) / 4;
-        float y[4];
-        int st = 0;
-        if (i == 0) {
-#pragma unroll
-          for (int u = 0; u < kSteps8; ++u) {
-            if (u < steps) {
-              const int at = 4 * u + (sl >> 1);
-              scaled(kept[u], y);
-              f(y, lo * 32 + at, at < n);
-            }
-          }
-          st = kSteps8;
-        }
-        for (; st < steps; ++st) {
-          const int at = 4 * st + (sl >> 1);
-          float4 z = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-          if (at < n) z = *reinterpret_cast<const float4*>(rec.values + (size_t)lo * kManyKeys + 8 * at + 4 * (sl & 1));
-          scaled(z, y);
-          f(y, lo * 32 + at, at < n);
-        }
-      }
-    };
-    for_records([&](const float (&y)[4], int, bool) { ymax = fmaxf(ymax, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))); });
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) ymax = fmaxf(ymax, __shfl_xor_sync(0xffffffffu, ymax, o));
-    floor_y = fmaxf(ymax - 1.0f, bound);
-    floor_y = raise(floor_y, kList8 / 4, [&](auto&& f) {
-      for_records([&](const float (&y)[4], int, bool) { f(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))); });
-    });
-    for_records([&](const float (&y)[4], int at, bool on) {
-      const bool any = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])) > floor_y;
-      if (!__any_sync(0xffffffffu, any)) return;
-      append(y, any && on ? rec.keys[at] + 4 * (sl & 1) : 0, floor_y);
-    });
-  } else {
-    const int groups = live ? pos / kGroupKeys + 1 : 0;
-    const float* max_row = a.group_max + (size_t)unit * a.groups * slots + r;
-    const float* y_row = a.scores + row * a.score_stride;
-    const int steps = (__reduce_max_sync(0xffffffffu, groups) + 7) / 8;
-    float kept[kSteps8];
-#pragma unroll
-    for (int i = 0; i < kSteps8; ++i) {
-      const int g = 8 * i + sl;
-      kept[i] = g < groups ? max_row[(size_t)g * slots] : -INFINITY;
-    }
-#pragma unroll
-    for (int i = 0; i < kSteps8; ++i) ymax = fmaxf(ymax, kept[i]);
-    for (int i = kSteps8; i < steps; i += 4) {
-      float m[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int g = 8 * (i + u) + sl;
-        m[u] = g < groups ? max_row[(size_t)g * slots] : -INFINITY;
-      }
-      ymax = fmaxf(ymax, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) ymax = fmaxf(ymax, __shfl_xor_sync(0xffffffffu, ymax, o));
-    // f(this lane's maximum of groups 8 i .. 8 i + 7, i)
-    auto for_groups = [&](auto&& f) {
-#pragma unroll
-      for (int i = 0; i < kSteps8; ++i)
-        if (i < steps) f(kept[i], i);
-      for (int i = kSteps8; i < steps; ++i) {
-        const int g = 8 * i + sl;
-        f(g < groups ? max_row[(size_t)g * slots] : -INFINITY, i);
-      }
-    };
-    floor_y = raise(ymax - 1.0f, kFewCandidateCells, [&](auto&& f) { for_groups([&](float m, int) { f(m); }); });
-    for_groups([&](float m, int i) {
-      unsigned bits = (__ballot_sync(0xffffffffu, m > floor_y) >> sub_bit) & 0xffu;
-      while (__any_sync(0xffffffffu, bits != 0u)) {
-        const int key0 = (8 * i + __ffs(bits) - 1) * kGroupKeys + 4 * sl;
-        float4 y4 = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-        if (bits) y4 = *reinterpret_cast<const float4*>(y_row + key0);
-        bits &= bits - 1;
-        const float y[4] = {y4.x, y4.y, y4.z, y4.w};
-        append(y, key0, floor_y);
-      }
-    });
+    if (over) floor_y = fmaxf(floor_y, fmaxf(ymax - 1.0f, bound_below(tau)));
   }
   if (live && cnt > kList8) {
-    if (sl == 0) a.spilled[atomicAdd(a.counters + 1, 1)] = (int)row;
+    if (sl == 0) a.spilled[atomicAdd(a.counters + kSpilledRows, 1)] = (int)row;
     live = false;
   }
   if (!live) cnt = 0;
   __syncwarp();
+  // ---- where the candidates' V rows are; they are asked for now and come while the threshold is found
+  const __nv_bfloat16* v_head = v + (long long)kvh * a.c.s_head;
+  const Pages pages = pages_of(a.c, live ? w.b : 0);
+  for (int e = sl; e < cnt; e += 8) {
+    const long long off = pages.at((int)my_at[e]);
+    if (off >= 0) prefetch_row<D>(v_head + off);
+    my_at[e] = off;
+  }
 
   // ---- threshold
   const int longest = __reduce_max_sync(0xffffffffu, cnt);
   TauIter st;
-  st.tau = st.lo = floor_y;
+  st.tau = st.lo = fmaxf(floor_y, ymax - 1.0f);
   st.hi = ymax;
   bool done = !live;
+#pragma unroll 1
   for (int it = 0; it < kMaxSteps; ++it) {
     float s0 = 0.f, s1 = 0.f;
+#pragma unroll 1
     for (int e = sl; e < longest; e += 8) {
       float ye, ye1;
       powers<EC>(e < cnt ? fmaxf(my_y[e] - st.tau, 0.f) : 0.f, a.expo, ye, ye1);
@@ -355,6 +477,7 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
   float acc[D / 8];
 #pragma unroll
   for (int e = 0; e < D / 8; ++e) acc[e] = 0.f;
+#pragma unroll 1
   for (int e0 = 0; e0 < cnt; e0 += 4) {
     float p[4];
     Share<D> x[4];
@@ -371,7 +494,7 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
     for (int u = 0; u < 4; ++u) add_share<D>(acc, p[u], x[u]);
   }
   if (live) {
-    const size_t out = (size_t)(s.q0 + tok) * a.H + kvh * a.G + r % a.G;
+    const size_t out = (size_t)(w.s.q0 + tok) * a.H + kvh * a.G + r % a.G;
     store_share<D>(a.o + out * D, sl, acc);
     if (sl == 0) {
       a.tau[out] = tau;
@@ -398,7 +521,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
   __shared__ float opart[W][D];
   const int lane = threadIdx.x & 31, sl = lane & 7, warp = threadIdx.x >> 5;
   const int slots = kMany ? a.many_slots : a.few_slots;
-  const int n_rows = kSpilled ? a.counters[1] : 0;
+  const int n_rows = kSpilled ? a.counters[kSpilledRows] : 0;
   float* my_max = maxima[warp];
   float* my_y = list_y[warp];
   int* my_j = list_j[warp];
@@ -427,33 +550,30 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
     const int row = kSpilled ? a.spilled[n] : n;
     const int unit = row / slots, r = row - unit * slots;
     // ---- which row this is
-    int t0 = 0;
     const int kvh = unit % a.c.KH;
-    int b = first + unit / a.c.KH;
-    if constexpr (kMany) b = find_block(a.c, b, kManyTiles * a.tile_tokens, t0);
-    if (b >= a.c.B || t0 < 0) break;                       // (no row; never so for listed ones)
-    const PagedSeq s = paged_seq(a.c, b);
-    const int tok = t0 + r / a.G;
-    if (tok >= s.n || !paged_ok(a, s) || paged_few(a, s) == kMany) break;
+    const UnitOf w = unit_of<kMany>(a, first, unit);
+    const PagedSeq s = w.s;
+    const int tok = w.t0 + r / a.G;
+    if (w.b < 0 || tok >= s.n) break;                      // (no row; never so for listed ones)
     const int pos = s.len - s.n + tok;
-    const Pages pages = pages_of(a.c, b);
+    const Pages pages = pages_of(a.c, w.b);
     const __nv_bfloat16* v_head = v + (long long)kvh * a.c.s_head;
     const float* y_row = a.scores + (size_t)row * a.score_stride;
     float ymax = -INFINITY, floor_y = -INFINITY;
 
     // for_keys(f): f(y, key) with a key per lane (y = -inf: none) for all keys of this warp that are kept and can be in the support
     const int groups = pos / kGroupKeys + 1;
-    const float* max_row = a.group_max + (size_t)unit * a.groups * slots + r;
+    const float* max_row = a.group_max + (size_t)row * a.groups;
     // few: group g is warp g mod W's, 32 of a warp's groups are a chunk (so that short rows and runs of neighbouring candidates are
     // spread over the warps)
     const int chunks = (groups + 32 * W - 1) / (32 * W);
     auto max_at = [&](int i) -> float {                    // this lane's group of the warp's chunk i
       if (i < kChunks) return my_max[i * 32 + lane];
       const int g = (i * 32 + lane) * W + warp;
-      return g < groups ? max_row[(size_t)g * slots] : -INFINITY;
+      return g < groups ? max_row[g] : -INFINITY;
     };
     Records rec;
-    if constexpr (kMany) rec = records_of(a, s, t0, unit, r, row);
+    if constexpr (kMany) rec = records_of(a, w.cut, unit, r, row, pos);
     auto for_keys = [&](auto&& f) {
       if constexpr (!kMany) {
         for (int i = 0; i < chunks; ++i) {
@@ -478,9 +598,8 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
         }
       } else {
         // four records of a work item are a warp's step
-        for (int i = 0; i < rec.splits && rec.begin(i) <= pos / kManyKeys; ++i) {
-          const int lo = rec.begin(i);
-          if (lo == rec.begin(i + 1)) continue;
+        for (int i = 0; i < rec.items; ++i) {
+          const int lo = rec.cut.begin(i);
           const float4 info = rec.info[(size_t)i * rec.slots];
           const int n = __float_as_int(info.x);
           for (int st = 4 * warp; st < n; st += 16 * W) {
@@ -510,7 +629,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
         const int g = (i * 32 + lane) * W + warp;
-        m[i] = g < groups ? max_row[(size_t)g * slots] : -INFINITY;
+        m[i] = g < groups ? max_row[g] : -INFINITY;
       }
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
@@ -530,8 +649,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
     red_slot ^= 1;
     floor_y = ymax - 1.0f;
     if constexpr (kMany) {
-      for (int i = 0; i < rec.splits && rec.begin(i) <= pos / kManyKeys; ++i)
-        if (rec.begin(i) < rec.begin(i + 1)) floor_y = fmaxf(floor_y, rec.info[(size_t)i * rec.slots].y);
+      for (int i = 0; i < rec.items; ++i) floor_y = fmaxf(floor_y, rec.info[(size_t)i * rec.slots].y);
     }
 
     // ---- the threshold of the groups' largest keys as a bound (see rows8)
@@ -540,7 +658,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
       for (int i = 0; i < chunks; ++i) cand += __popc(__ballot_sync(0xffffffffu, max_at(i) > floor_y));
       cand = (int)row_sum2(lane == 0 ? (float)cand : 0.f, 0.f).x;
       float tau = floor_y;
-      for (int it = 0; it < kBoundSteps && cand > kFewCandidateCells; ++it) {
+      for (int it = 0; it < kBoundSteps && cand > kFewCandidates; ++it) {
         float s0 = 0.f, s1 = 0.f;
         for (int i = 0; i < chunks; ++i) {
           const float d = max_at(i) - tau;
@@ -684,7 +802,7 @@ cudaError_t launch_solve_d(const PagedArgs& a, const __nv_bfloat16* v, int first
   }
 #undef ENTMAX_ROWS8
   if (err != cudaSuccess) return err;
-  return launch_kernel(paged_row_kernel<D, kMany, true>, 4 * 148, 32 * kRowWarps, 0, stream, a, v, first);
+  return launch_kernel(paged_row_kernel<D, kMany, true>, 2 * a.sms, 32 * kRowWarps, 0, stream, a, v, first);
 }
 
 // Eight lanes per row where there are rows enough to fill the machine that way, or where a row is short
@@ -704,6 +822,7 @@ cudaError_t launch_solve(const PagedArgs& a, const void* v, int first, int units
 constexpr size_t kSliceBytes = (size_t)4 << 30;     // scores held at a time (at least one sequence's or block's)
 constexpr int kFewRows = 32;
 constexpr int kFewWorth = 8;
+constexpr int kMostSms = 160;        // (sizes the workspace, which is the same on every device)
 
 // The current device's compute capability (major) and SMs, looked up once per device
 cudaError_t device_facts(int* major, int* sms) {
@@ -721,12 +840,12 @@ cudaError_t device_facts(int* major, int* sms) {
     if (dev >= 0 && dev < 64) known[dev].store(v, std::memory_order_relaxed);
   }
   *major = v >> 16;
-  *sms = v & 0xffff;
+  *sms = (v & 0xffff) < kMostSms ? v & 0xffff : kMostSms;
   return cudaSuccess;
 }
 
 struct PagedPlan {
-  size_t scores, group_max, record_key, row_info, spilled, total;
+  size_t scores, group_max, record_key, row_info, blocks, order, spilled, total;
   int few_seqs;          // sequences to a slice of the "few" kernel (at most kFewSeqs)
   int many_blocks;       // blocks to a slice of the "many" kernel
   bool few, many;
@@ -786,24 +905,18 @@ int plan_paged(const entmax_attn_paged_cache* cache, const entmax_attn_paged_par
     l->many_blocks = fit < 1 ? 1 : fit < (size_t)a->many_blocks ? (int)fit : a->many_blocks;
     many_rows = per * l->many_blocks;
   }
-  // Work items of the "many" kernel: the number of shares that the machine works off in the fewest K tiles, an item's start counted as three
-  const long long many_units = (long long)l->many_blocks * a->c.KH;
-  a->many_splits = 1;
-  long long best = 0;
-  for (int i = 1; i <= 8 && i * 4 <= a->tiles + 3; ++i) {
-    const long long cost = (many_units * i + 147) / 148 * ((a->tiles + i - 1) / i + 3);
-    if (best == 0 || cost < best) {
-      best = cost;
-      a->many_splits = i;
-    }
-  }
+  // (runs of kLeastCut tiles at least, one per SM)
+  a->many_items = a->tiles / kLeastCut + 2;
+  if (a->many_items > kMostSms + 1) a->many_items = kMostSms + 1;
 
   size_t off = 256;
   auto take = [&off](size_t floats) { const size_t at = off; off = (off + floats * sizeof(float) + 255) / 256 * 256; return at; };
+  l->blocks = take(l->many_blocks * (sizeof(PagedBlock) / sizeof(float)));
+  l->order = take(l->many_blocks);
   l->spilled = take(rows > many_rows ? rows : many_rows);
   l->group_max = take(rows * a->groups);
   l->record_key = take(many_rows * a->tiles * 32);
-  l->row_info = take(4 * many_rows * a->many_splits);
+  l->row_info = take(4 * many_rows * a->many_items);
   l->scores = take((rows > many_rows ? rows : many_rows) * a->score_stride);
   l->total = off;
   return ENTMAX_ATTN_OK;
@@ -852,10 +965,13 @@ extern "C" int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a.counters = reinterpret_cast<int32_t*>(ws);
   a.row_info = reinterpret_cast<float4*>(ws + l.row_info);
+  a.blocks = reinterpret_cast<PagedBlock*>(ws + l.blocks);
+  a.order = reinterpret_cast<int32_t*>(ws + l.order);
   a.spilled = reinterpret_cast<int32_t*>(ws + l.spilled);
   a.group_max = reinterpret_cast<float*>(ws + l.group_max);
   a.record_key = reinterpret_cast<int32_t*>(ws + l.record_key);
   a.scores = reinterpret_cast<float*>(ws + l.scores);
+  a.record_bytes = make_uint2(32u, 4u);
   a.o = static_cast<__nv_bfloat16*>(o);
   a.tau = tau;
   a.support = support_size;
@@ -865,18 +981,17 @@ extern "C" int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const
     err = cudaMemsetAsync(device_status, 0, sizeof(int32_t) * ENTMAX_ATTN_STATUS_WORDS, stream);
     if (err != cudaSuccess) return fail_cuda(err);
   }
-  auto clear_counters = [&]() { return cudaMemsetAsync(a.counters, 0, 2 * sizeof(int32_t), stream); };
   for (int b = 0; l.few && b < a.c.B && err == cudaSuccess; b += l.few_seqs) {
     const int n = a.c.B - b < l.few_seqs ? a.c.B - b : l.few_seqs;
-    if (solve_by_rows8(a, false, (long long)n * a.c.KH * a.few_slots)) err = clear_counters();
+    if (solve_by_rows8(a, false, (long long)n * a.c.KH * a.few_slots)) err = cudaMemsetAsync(a.counters, 0, kCounters * sizeof(int32_t), stream);
     if (err == cudaSuccess) err = launch_paged_few(a, q, k_cache, params->q_stride_t, params->q_stride_h, b, n, stream);
     if (err == cudaSuccess) err = launch_solve<false>(a, v_cache, b, n * a.c.KH, stream);
   }
   for (int blk = 0; l.many && blk < a.many_blocks && err == cudaSuccess; blk += l.many_blocks) {
     const int n = a.many_blocks - blk < l.many_blocks ? a.many_blocks - blk : l.many_blocks;
-    err = clear_counters();
-    if (err == cudaSuccess) err = launch_paged_many(a, q, k_cache, params->q_stride_t, params->q_stride_h, blk, n, stream);
-    if (err == cudaSuccess) err = launch_solve<true>(a, v_cache, blk, n * a.c.KH, stream);
+    err = launch_kernel(paged_plan_kernel, 1, kPlanThreads, 0, stream, a, blk, n);
+    if (err == cudaSuccess) err = launch_paged_many(a, q, k_cache, params->q_stride_t, params->q_stride_h, n, stream);
+    if (err == cudaSuccess) err = launch_solve<true>(a, v_cache, 0, n * a.c.KH, stream);
   }
   if (err == cudaSuccess) err = cudaGetLastError();
   return err == cudaSuccess ? ENTMAX_ATTN_OK : fail_cuda(err);

@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
       const int pos0 = len - n;                              // position of the first new token
       const int unit = g.b * a.c.KH + g.kvh;
       float* score0 = a.scores + (size_t)unit * a.few_slots * a.score_stride;
-      float* max0 = a.group_max + (size_t)unit * a.groups * a.few_slots;
+      float* max0 = a.group_max + ((size_t)unit * a.few_slots + (lane < rows ? lane : 0)) * a.groups;
       __syncwarp();
       if (lane < NR) {
         float ra = 0.f, slope = 0.f;
@@ -346,8 +346,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
         if (!alive) break;
         sphase[buf] ^= 1u;
         tc_fence_after();
-        float acc[NR < 8 ? 8 : NR];
-        load_columns<NR < 8 ? 8 : NR>(taddr + buf * NB, acc);
+        constexpr int kCols = NR <= 8 ? 8 : NR <= 16 ? 16 : 32;
+        float acc[kCols];
+        load_columns<kCols>(taddr + buf * NB, acc);
         tmem_ld_wait();
         tc_fence_before();
         __syncwarp();
@@ -380,7 +381,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
             top = lane == r ? m[u] : top;
           }
         }
-        if (lane < rows) max0[(size_t)group * a.few_slots + lane] = top;
+        if (lane < rows) max0[group] = top;
       }
     }
   }
@@ -441,7 +442,7 @@ __host__ __device__ constexpr uint32_t idesc_many() {
 // A work item: one block of new tokens, one K/V head, one share of the keys.  Published by the scheduler with the pages of its first keys.
 struct ManyItem {
   int b, kvh, q0, n, len, t0, lo, hi;      // t0: first token of the block within the chunk; K tiles lo .. hi - 1
-  int unit, split;                         // row slots: unit * many_slots
+  int unit, item;                          // row slots: unit * many_slots; which of the unit's items
 };
 constexpr int kItemWords = 10 + 64;        // the fields, then page and slot of 32 boxes
 
@@ -453,20 +454,29 @@ __device__ __forceinline__ int many_tile_end(const PagedArgs& a, const ManyItem&
   return max(min((it.len - it.n + last) / BN + 1, it.hi), it.lo);
 }
 
-// Where x > thr: eight values to rec (one 32-byte store), their first key to key, and both moved on.  Predicated instructions instead of a
-// branch: a lane that has nothing to store costs the warp its issue slots and no divergence.
-__device__ __forceinline__ void keep_record_if_greater(float x, float thr, float*& rec, int32_t*& key, int first, const float* v) {
+// Where x > thr: eight values to record n (one 32-byte store), their first key beside them, and n moved on.  Predicated instructions instead of
+// a branch: a lane that has nothing to store costs the warp its issue slots and no divergence.  The scan is bound by the ALU pipe
+// (comparisons and integer additions at half rate), so the addresses are products on the other one; the factors come from memory so that they
+// stay products.
+template <int kFirst>
+__device__ __forceinline__ void keep_record_if_greater(float x, float thr, uint32_t& n, const float* rec, const int32_t* key, uint2 bytes,
+                                                       int col0, const float* v) {
   asm volatile(
       "{\n"
       " .reg .pred p;\n"
-      " setp.gt.f32 p, %2, %3;\n"
-      " @p st.global.v8.f32 [%0], {%5, %6, %7, %8, %9, %10, %11, %12};\n"
-      " @p st.global.u32 [%1], %4;\n"
-      " @p add.u64 %0, %0, 32;\n"
-      " @p add.u64 %1, %1, 4;\n"
+      " .reg .u64 ra, ka;\n"
+      " .reg .u32 first;\n"
+      " setp.gt.f32 p, %1, %2;\n"
+      " mad.wide.u32 ra, %0, %5, %3;\n"
+      " mad.wide.u32 ka, %0, %6, %4;\n"
+      " add.u32 first, %7, %16;\n"
+      " @p st.global.v8.f32 [ra], {%8, %9, %10, %11, %12, %13, %14, %15};\n"
+      " @p st.global.u32 [ka], first;\n"
+      " @p add.u32 %0, %0, 1;\n"
       "}\n"
-      : "+l"(rec), "+l"(key)
-      : "f"(x), "f"(thr), "r"(first), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+      : "+r"(n)
+      : "f"(x), "f"(thr), "l"(rec), "l"(key), "r"(bytes.x), "r"(bytes.y), "r"(col0), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]),
+        "f"(v[5]), "f"(v[6]), "f"(v[7]), "n"(kFirst)
       : "memory");
 }
 
@@ -510,7 +520,7 @@ __device__ __forceinline__ float bound_from_eight(const float (&z)[8], float mar
 template <int HD, bool kAlibi>
 __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __grid_constant__ CUtensorMap map_q,
                                                                    const __grid_constant__ CUtensorMap map_k,
-                                                                   const __grid_constant__ PagedArgs a, int block0, int blocks) {
+                                                                   const __grid_constant__ PagedArgs a, int blocks) {
   pdl_begin();
   using C = ManyCfg<HD>;
   extern __shared__ uint8_t smem_raw[];
@@ -581,7 +591,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
     it.lo = (int)lds_u32(at + 24);
     it.hi = (int)lds_u32(at + 28);
     it.unit = (int)lds_u32(at + 32);
-    it.split = (int)lds_u32(at + 36);
+    it.item = (int)lds_u32(at + 36);
     return it;
   };
 
@@ -730,41 +740,51 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
     // ------------------------------------------------------------------ scheduler: the next items, ahead of the others
     int slot = 0;
     uint32_t wphase = 0;
-    const int block_tokens = kManyTiles * a.tile_tokens;
-    const int n_items = blocks * a.c.KH * a.many_splits;
+    const int n_blocks = a.counters[kBlocks], cut = a.counters[kCut], head_tiles = a.counters[kTiles];
+    const int n_items = n_blocks * a.c.KH;
+    int x = blockIdx.x * cut;                                // cut: next tile of this CTA's run
+    const int x_end = min(x + cut, head_tiles * a.c.KH);
     for (bool more = true; more;) {
-      int k = 0;
-      if (lane == 0) k = atomicAdd(a.counters, 1);
-      k = __shfl_sync(0xffffffffu, k, 0);
       ManyItem it;
       it.b = -1;
       it.lo = it.len = 0;
-      more = k < n_items;
-      if (more) {
-        // a K/V head's blocks one after another, later blocks (longer rows) first: the CTAs that run together stream the same keys
-        it.split = k % a.many_splits;
-        const int u = k / a.many_splits;
-        it.kvh = u / blocks;
-        const int blk = block0 + blocks - 1 - (u - it.kvh * blocks);
-        it.b = find_block(a.c, blk, block_tokens, it.t0);
-        if (it.b >= a.c.B) continue;
-        const PagedSeq s = paged_seq(a.c, it.b);
-        it.q0 = s.q0; it.n = s.n; it.len = s.len;
-        if (it.t0 < 0 || it.t0 >= s.n) continue;
-        if (!paged_ok(a, s)) {
-          if (it.split == 0 && it.t0 == 0) {
-            if (lane == 0 && a.status) atomicOr(a.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_LENGTH);
-            write_unserved(a, s, it.kvh, lane, 32);
-          }
-          continue;
+      if (cut == 0) {
+        // a K/V head's blocks one after another, the longest rows first: the CTAs that run together stream the same keys
+        int k = 0;
+        if (lane == 0) k = atomicAdd(a.counters + kNextItem, 1);
+        k = __shfl_sync(0xffffffffu, k, 0);
+        more = k < n_items;
+        if (more) {
+          it.kvh = k / n_blocks;
+          const int blk = a.order[k - it.kvh * n_blocks];
+          const PagedBlock pb = a.blocks[blk];
+          it.b = pb.b; it.t0 = pb.t0; it.q0 = pb.q0; it.n = pb.n; it.len = pb.len;
+          it.hi = pb.tiles;
+          it.item = 0;
+          it.unit = blk * a.c.KH + it.kvh;
         }
-        if (paged_few(a, s)) continue;
-        it.unit = (blk - block0) * a.c.KH + it.kvh;
-        const int last = min(it.t0 + block_tokens, s.n) - 1;
-        const int tiles = (s.len - s.n + last) / BN + 1;
-        it.lo = split_begin(tiles, it.split, a.many_splits);
-        it.hi = split_begin(tiles, it.split + 1, a.many_splits);
-        if (it.lo >= it.hi) continue;
+      } else {
+        more = x < x_end;
+        if (more) {
+          it.kvh = x / head_tiles;
+          const int y = x - it.kvh * head_tiles;
+          int lo = 0, n = blocks;                            // the block with start <= y < start + tiles: 32 candidates a step
+          while (n > 1) {
+            const int step = (n + 31) / 32;
+            const bool le = lane * step < n && (lane == 0 || a.blocks[lo + lane * step].start <= y);
+            const int i = 31 - __clz(__ballot_sync(0xffffffffu, le));
+            lo += i * step;
+            n = min(step, n - i * step);
+          }
+          const PagedBlock pb = a.blocks[lo];
+          const ManyCut c = many_cut(a.counters, pb, it.kvh);
+          it.b = pb.b; it.t0 = pb.t0; it.q0 = pb.q0; it.n = pb.n; it.len = pb.len;
+          it.lo = y - pb.start;
+          it.hi = min(pb.tiles, it.lo + x_end - x);
+          it.item = x / cut - c.start / cut;
+          it.unit = lo * a.c.KH + it.kvh;
+          x += it.hi - it.lo;
+        }
       }
       int page = 0, pslot = 0;
       const int key = it.lo * BN + (lane << box_shift);
@@ -784,7 +804,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
           sts_u32(at + 24, (uint32_t)it.lo);
           sts_u32(at + 28, (uint32_t)it.hi);
           sts_u32(at + 32, (uint32_t)it.unit);
-          sts_u32(at + 36, (uint32_t)it.split);
+          sts_u32(at + 36, (uint32_t)it.item);
         }
       }
       __syncwarp();
@@ -799,6 +819,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
     const uint32_t taddr_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(x * BN);
     const uint32_t my_full = s_full + 8 * x, my_empty = s_empty + 8 * x;
     const int tile_rows = a.tile_tokens * a.G;
+    const uint2 rec_bytes = a.record_bytes;
     uint32_t fphase = 0, wphase = 0;
     int slot = 0;
     bool alive = true;
@@ -823,9 +844,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       const float slope = kAlibi && valid ? a.alibi[head] / a.sm_scale : 0.f;
       const int slot_row = valid ? x * tile_rows + row_local : 0;
       const size_t row = (size_t)it.unit * a.many_slots + (size_t)slot_row;
-      float* rec = a.scores + row * a.score_stride + (size_t)it.lo * BN;             // next record
-      int32_t* rec_key = a.record_key + row * (size_t)(a.tiles * 32) + it.lo * 32;   // and where its key goes
-      const int32_t* rec_key0 = rec_key;
+      const float* rec = a.scores + row * a.score_stride + (size_t)it.lo * BN;
+      const int32_t* rec_key = a.record_key + row * (size_t)(a.tiles * 32) + it.lo * 32;
+      uint32_t n_rec = 0;
       // Everything is compared before the scaling, z = <q,k> + slope (j - pos): y = a z, and a negative a turns z around first
       const float sign = ra < 0.f ? -1.f : 1.f;
       const bool turned = __any_sync(0xffffffffu, ra < 0.f);
@@ -842,10 +863,12 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
         fphase ^= 1u;
         tc_fence_after();
         const int col_base = t * BN, step_no = t - it.lo;
-        const bool edge = col_base + BN - 1 > first_pos;       // some row of the tile does not see all of it
         const int n_steps = min(BN / 64, (last_pos - col_base) / 64 + 1);   // 64-column steps that some row sees
-        // z of 64 columns from column col0 on, as both looks at them compute it
-        auto finish = [&](float (&v)[64], int col0) {
+        // 64 columns from column 64 c on, as both looks at them take them
+        auto load = [&](float (&v)[64], int c) {
+          tmem_ld64(taddr_row + 64 * c, v);
+          tmem_ld_wait64(v);
+          const int col0 = col_base + 64 * c;
           if (kAlibi) {
             const float t0 = slope * (float)(col0 - pos);
 #pragma unroll
@@ -855,55 +878,59 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
 #pragma unroll
             for (int u = 0; u < 64; ++u) v[u] *= sign;
           }
-          if (edge) {
+          if (col0 + 63 > first_pos) {                         // some row of the tile does not see all of them
 #pragma unroll
             for (int u = 0; u < 64; ++u) v[u] = col0 + u <= lim ? v[u] : -INFINITY;
           }
         };
-        if (step_no == 0) {
-          // a stream that starts without a bound looks at its first tile twice
+        // Now and then the bound is also taken from eight classes of keys; a stream that starts without any looks at its first tile twice
+        const bool classes = step_no == 0 || step_no == 3 || (step_no & 15) == 15;
+        if (classes) {
 #pragma unroll 1
           for (int c = 0; c < n_steps; ++c) {
             float v[64];
-            tmem_ld64(taddr_row + 64 * c, v);
-            tmem_ld_wait64(v);
-            finish(v, col_base + 64 * c);
+            load(v, c);
 #pragma unroll
             for (int q = 0; q < 8; ++q) top[q] = fmaxf(top[q], max8(&v[8 * q]));
           }
-          best = max8(top);
+          best = fmaxf(best, max8(top));
           thr = fmaxf(thr, fmaxf(best - margin, bound_from_eight(top, margin, a.expo_class, a.expo)));
         }
-        // One straight pass, 64 columns at a time: maxima of eight columns, and eight columns with a candidate go to the row's records as
-        // they are, by predicated stores (branches on "some row has a candidate" cost more than the stores do)
+        // One straight pass: maxima of eight columns, and eight columns with a candidate go to the row's records as they are, by predicated
+        // stores where some row of the warp has one among 32 columns (a vote for 64: chunk of 2048 over 32768 keys 250 -> 243 us here;
+        // for eight each: 254)
 #pragma unroll 1
         for (int c = 0; c < n_steps; ++c) {
           float v[64];
-          tmem_ld64(taddr_row + 64 * c, v);
-          tmem_ld_wait64(v);
-          finish(v, col_base + 64 * c);
+          load(v, c);
           float g[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) g[q] = max8(&v[8 * q]);
-          const float m = max8(g);
-          best = fmaxf(best, m);
+          const float m_lo = fmaxf(fmaxf(g[0], g[1]), fmaxf(g[2], g[3])), m_hi = fmaxf(fmaxf(g[4], g[5]), fmaxf(g[6], g[7]));
+          best = max3(best, m_lo, m_hi);
           thr = fmaxf(thr, best - margin);
-          if (!__any_sync(0xffffffffu, m > thr)) continue;
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            keep_record_if_greater(g[q], thr, rec, rec_key, col_base + 64 * c + 8 * q, &v[8 * q]);
-            top[q] = fmaxf(top[q], g[q]);
+          const int col0 = col_base + 64 * c;
+          if (__any_sync(0xffffffffu, m_lo > thr)) {
+            keep_record_if_greater<0>(g[0], thr, n_rec, rec, rec_key, rec_bytes, col0, &v[0]);
+            keep_record_if_greater<8>(g[1], thr, n_rec, rec, rec_key, rec_bytes, col0, &v[8]);
+            keep_record_if_greater<16>(g[2], thr, n_rec, rec, rec_key, rec_bytes, col0, &v[16]);
+            keep_record_if_greater<24>(g[3], thr, n_rec, rec, rec_key, rec_bytes, col0, &v[24]);
+          }
+          if (__any_sync(0xffffffffu, m_hi > thr)) {
+            keep_record_if_greater<32>(g[4], thr, n_rec, rec, rec_key, rec_bytes, col0, &v[32]);
+            keep_record_if_greater<40>(g[5], thr, n_rec, rec, rec_key, rec_bytes, col0, &v[40]);
+            keep_record_if_greater<48>(g[6], thr, n_rec, rec, rec_key, rec_bytes, col0, &v[48]);
+            keep_record_if_greater<56>(g[7], thr, n_rec, rec, rec_key, rec_bytes, col0, &v[56]);
           }
         }
         // the accumulator has been read: hand it back to the MMA issuer
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(my_empty);
-        if ((step_no & (step_no - 1)) == 0) thr = fmaxf(thr, bound_from_eight(top, margin, a.expo_class, a.expo));
       }
       if (valid && alive)
-        a.row_info[((size_t)it.unit * a.many_splits + it.split) * a.many_slots + slot_row] =
-            make_float4(__int_as_float((int)(rec_key - rec_key0)), mag * thr, mag, 0.f);
+        a.row_info[((size_t)it.unit * a.many_items + it.item) * a.many_slots + slot_row] =
+            make_float4(__int_as_float((int)n_rec), mag * thr, mag, 0.f);
     }
   }
 
@@ -953,18 +980,15 @@ cudaError_t launch_few(const PagedArgs& a, const void* q, const void* k, int64_t
 }
 
 template <int HD, bool kAlibi>
-cudaError_t launch_many(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int block0, int blocks,
-                        cudaStream_t stream) {
+cudaError_t launch_many(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int blocks, cudaStream_t stream) {
   CUtensorMap map_q, map_k;
   cudaError_t err = map_queries(&map_q, a, q, q_st, q_sh, a.tile_tokens);
   if (err == cudaSuccess) err = map_pages(&map_k, a, k);
   if (err == cudaSuccess)
     err = cudaFuncSetAttribute(paged_many_kernel<HD, kAlibi>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<HD>::kSmemBytes);
   if (err != cudaSuccess) return err;
-  const int sms = a.sms;
-  const long long items = (long long)blocks * a.c.KH * a.many_splits;
-  return launch_kernel(paged_many_kernel<HD, kAlibi>, (unsigned)(items < sms ? items : sms), kManyThreads, ManyCfg<HD>::kSmemBytes, stream, map_q, map_k,
-                       a, block0, blocks);
+  // (where units are cut every SM gets a run; otherwise there are more of them than SMs)
+  return launch_kernel(paged_many_kernel<HD, kAlibi>, (unsigned)a.sms, kManyThreads, ManyCfg<HD>::kSmemBytes, stream, map_q, map_k, a, blocks);
 }
 
 }  // namespace
@@ -975,19 +999,19 @@ cudaError_t launch_paged_few(const PagedArgs& a, const void* q, const void* k, i
   (a.alibi ? launch_few<HD, NR, true>(a, q, k, q_st, q_sh, seq0, seqs, stream)          \
            : launch_few<HD, NR, false>(a, q, k, q_st, q_sh, seq0, seqs, stream))
 #define ENTMAX_FEW_ROWS(HD)                                                             \
-  (a.few_slots <= 4 ? ENTMAX_FEW(HD, 4) : a.few_slots <= 8 ? ENTMAX_FEW(HD, 8) : a.few_slots <= 16 ? ENTMAX_FEW(HD, 16) : ENTMAX_FEW(HD, 32))
+  (a.few_slots <= 4 ? ENTMAX_FEW(HD, 4) : a.few_slots <= 8 ? ENTMAX_FEW(HD, 8) : a.few_slots <= 16 ? ENTMAX_FEW(HD, 16) : a.few_slots <= 24 ? ENTMAX_FEW(HD, 24) : ENTMAX_FEW(HD, 32))
   return a.c.D == 64 ? ENTMAX_FEW_ROWS(64) : ENTMAX_FEW_ROWS(128);
 #undef ENTMAX_FEW_ROWS
 #undef ENTMAX_FEW
 }
 
-cudaError_t launch_paged_many(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int block0, int blocks,
+cudaError_t launch_paged_many(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int blocks,
                               cudaStream_t stream) {
   if (a.c.D == 64)
-    return a.alibi ? launch_many<64, true>(a, q, k, q_st, q_sh, block0, blocks, stream)
-                   : launch_many<64, false>(a, q, k, q_st, q_sh, block0, blocks, stream);
-  return a.alibi ? launch_many<128, true>(a, q, k, q_st, q_sh, block0, blocks, stream)
-                 : launch_many<128, false>(a, q, k, q_st, q_sh, block0, blocks, stream);
+    return a.alibi ? launch_many<64, true>(a, q, k, q_st, q_sh, blocks, stream)
+                   : launch_many<64, false>(a, q, k, q_st, q_sh, blocks, stream);
+  return a.alibi ? launch_many<128, true>(a, q, k, q_st, q_sh, blocks, stream)
+                 : launch_many<128, false>(a, q, k, q_st, q_sh, blocks, stream);
 }
 
 }  // namespace entmax
