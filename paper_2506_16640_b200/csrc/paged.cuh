@@ -102,6 +102,7 @@ struct PagedArgs {
   float* group_max;
   int32_t* record_key;
   float4* row_info;
+  float* row_scale;           // "many": [T][H] (alpha-1) c sm_scale
   uint2 record_bytes;         // {32, 4}: what a record takes in scores and in record_key (see the "many" kernel)
   struct PagedBlock* blocks;  // "many": what is known of each block of the slice
   int32_t* order;             // its blocks that have work, those with the longest rows first
@@ -114,8 +115,7 @@ struct PagedArgs {
 };
 
 enum Counter : int {
-  kNextItem = 0,              // work items handed out by the "many" kernel
-  kSpilledRows,               // rows in spilled
+  kSpilledRows = 0,           // rows in spilled
   kBlocks,                    // blocks in order
   kCut,                       // K tiles per CTA where the units are cut (see ManyCut), 0 where they are not
   kTiles,                     // K tiles of all blocks together (of one K/V head)

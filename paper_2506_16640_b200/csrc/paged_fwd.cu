@@ -125,7 +125,8 @@ __device__ __forceinline__ UnitOf unit_of(const PagedArgs& a, int first, int uni
 
 // =================================================================================================== plan
 // What the "many" kernels need to know of the blocks block0 .. block0 + blocks - 1 of new tokens, and the order their work is handed out in:
-// longest rows first (by 1024 classes of length), so that the CTAs end together.  Clears the counters.  One CTA.
+// longest rows first (by 1024 classes of length), so that the CTAs end together; clears the counters.  The first CTA does this, the others
+// fill in the scales of the rows.
 constexpr int kPlanThreads = 1024;
 constexpr int kLeastCut = 4;
 __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_constant__ PagedArgs a, int block0, int blocks) {
@@ -135,6 +136,16 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
   __shared__ int n_blocks;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int tokens = kManyTiles * a.tile_tokens;
+  if (blockIdx.x > 0) {
+    // warps take tokens in turn, lanes heads
+    for (int t = (blockIdx.x - 1) * (kPlanThreads / 32) + warp; t < a.c.T; t += (gridDim.x - 1) * (kPlanThreads / 32)) {
+      const int b = a.c.cu_q ? find_seq(a.c, t, 1, 0) : t / (a.c.T / a.c.B);
+      const PagedSeq s = paged_seq(a.c, b);
+      if (t < s.q0 || t >= s.q0 + s.n || !paged_ok(a, s) || paged_few(a, s)) continue;
+      for (int h = lane; h < a.H; h += 32) a.row_scale[(size_t)t * a.H + h] = paged_scale(a, h, s.len - s.n + t - s.q0);
+    }
+    return;
+  }
   bin[tid] = 0;
   if (tid <= kSpilledRows) a.counters[tid] = 0;
   __syncthreads();
@@ -845,7 +856,7 @@ cudaError_t device_facts(int* major, int* sms) {
 }
 
 struct PagedPlan {
-  size_t scores, group_max, record_key, row_info, blocks, order, spilled, total;
+  size_t scores, group_max, record_key, row_info, row_scale, blocks, order, spilled, total;
   int few_seqs;          // sequences to a slice of the "few" kernel (at most kFewSeqs)
   int many_blocks;       // blocks to a slice of the "many" kernel
   bool few, many;
@@ -917,6 +928,7 @@ int plan_paged(const entmax_attn_paged_cache* cache, const entmax_attn_paged_par
   l->group_max = take(rows * a->groups);
   l->record_key = take(many_rows * a->tiles * 32);
   l->row_info = take(4 * many_rows * a->many_items);
+  l->row_scale = take(l->many ? (size_t)a->c.T * a->H : 0);
   l->scores = take((rows > many_rows ? rows : many_rows) * a->score_stride);
   l->total = off;
   return ENTMAX_ATTN_OK;
@@ -965,6 +977,7 @@ extern "C" int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a.counters = reinterpret_cast<int32_t*>(ws);
   a.row_info = reinterpret_cast<float4*>(ws + l.row_info);
+  a.row_scale = reinterpret_cast<float*>(ws + l.row_scale);
   a.blocks = reinterpret_cast<PagedBlock*>(ws + l.blocks);
   a.order = reinterpret_cast<int32_t*>(ws + l.order);
   a.spilled = reinterpret_cast<int32_t*>(ws + l.spilled);
@@ -989,7 +1002,8 @@ extern "C" int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const
   }
   for (int blk = 0; l.many && blk < a.many_blocks && err == cudaSuccess; blk += l.many_blocks) {
     const int n = a.many_blocks - blk < l.many_blocks ? a.many_blocks - blk : l.many_blocks;
-    err = launch_kernel(paged_plan_kernel, 1, kPlanThreads, 0, stream, a, blk, n);
+    const int scale_ctas = (a.c.T + kPlanThreads / 32 - 1) / (kPlanThreads / 32);
+    err = launch_kernel(paged_plan_kernel, 1 + (scale_ctas < a.sms - 1 ? scale_ctas : a.sms - 1), kPlanThreads, 0, stream, a, blk, n);
     if (err == cudaSuccess) err = launch_paged_many(a, q, k_cache, params->q_stride_t, params->q_stride_h, n, stream);
     if (err == cudaSuccess) err = launch_solve<true>(a, v_cache, 0, n * a.c.KH, stream);
   }

@@ -423,6 +423,7 @@ constexpr int kManyThreads = (3 + kManyConsumers) * 32;
 constexpr int kSchedWarp = 2 + kManyConsumers;
 constexpr int kSchedSlots = 4;
 static_assert(kManyTiles * BN == 512, "TMEM budget");
+constexpr int kScaleBytes = kSchedSlots * kManyTiles * BM * 4;
 
 template <int HD>
 struct ManyCfg {
@@ -430,8 +431,9 @@ struct ManyCfg {
   static constexpr int kQBytes = BM * HD * 2;
   static constexpr int kKBytes = BN * HD * 2;
   static constexpr int kStages = HD == 128 ? 2 : 4;
+  static constexpr int kQBufs = HD == 128 ? kManyTiles : 2 * kManyTiles;   // Q tiles: the next item's too where they fit
   static constexpr int kBarBytes = 1024 + 512;
-  static constexpr int kSmemBytes = kManyTiles * kQBytes + kStages * kKBytes + kBarBytes + 1024;
+  static constexpr int kSmemBytes = kQBufs * kQBytes + kStages * kKBytes + kBarBytes + kScaleBytes + 1024;
   static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
 };
 
@@ -481,7 +483,8 @@ __device__ __forceinline__ void keep_record_if_greater(float x, float thr, uint3
 }
 
 // A lower bound of the threshold of a row from eight values of eight of its keys (-inf: none), y = z / margin: the threshold of those alone, by
-// three steps from the left, in z's units.  Rows with no more than two of them in the bracket have nothing to gain (-inf is returned).
+// three steps from the left, in z's units.  Rows with no more than two of them in the bracket have nothing to gain (-inf
+// is returned), nor is it worth the warp's time for less than eight rows.
 template <int EC>
 __device__ __forceinline__ float eight_steps(const float (&y)[8], float expo) {
   float tau = -1.0f;                                           // relative to the largest
@@ -504,7 +507,7 @@ __device__ __forceinline__ float bound_from_eight(const float (&z)[8], float mar
   int n = 0;
 #pragma unroll
   for (int q = 0; q < 8; ++q) n += z[q] > m - margin ? 1 : 0;
-  if (expo < 1.0f || !__any_sync(0xffffffffu, n > 2)) return -INFINITY;
+  if (expo < 1.0f || __popc(__ballot_sync(0xffffffffu, n > 2)) < 8) return -INFINITY;
   float y[8];
   const float r = 1.0f / margin;
 #pragma unroll
@@ -525,12 +528,13 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
   using C = ManyCfg<HD>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q_smem = sbase;                                   // [kManyTiles][kHalves][BM rows x 128 B]
-  const uint32_t k_smem = sbase + kManyTiles * C::kQBytes;         // [kStages][kHalves][BN rows x 128 B]
-  const uint32_t bars = k_smem + C::kStages * C::kKBytes;
-  const uint32_t q_full = bars;                                    // [kManyTiles]
-  const uint32_t q_empty = q_full + 8 * kManyTiles;                // [kManyTiles]
-  const uint32_t s_full = q_empty + 8 * kManyTiles;                // [kManyTiles]
+  const uint32_t q_smem = sbase;                                   // [kQBufs][kHalves][BM rows x 128 B]
+  const uint32_t k_smem = sbase + C::kQBufs * C::kQBytes;          // [kStages][kHalves][BN rows x 128 B]
+  const uint32_t scales = k_smem + C::kStages * C::kKBytes;        // float [kSchedSlots][kManyTiles * BM]: a of an item's rows
+  const uint32_t bars = scales + kScaleBytes;
+  const uint32_t q_full = bars;                                    // [kQBufs]
+  const uint32_t q_empty = q_full + 8 * C::kQBufs;                 // [kQBufs]
+  const uint32_t s_full = q_empty + 8 * C::kQBufs;                 // [kManyTiles]
   const uint32_t s_empty = s_full + 8 * kManyTiles;                // [kManyTiles]
   const uint32_t k_full = s_empty + 8 * kManyTiles;                // [kStages]
   const uint32_t k_empty = k_full + 8 * C::kStages;                // [kStages]
@@ -541,7 +545,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
   const uint32_t abort_flag = tmem_slot + 4;
   const uint32_t drain_bar = tmem_slot + 8;                        // teardown: every MMA issued so far has finished
   const uint32_t drain_fail = drain_bar + 8;                       // uint32: a teardown wait ran out as well
-  static_assert((4 * kManyTiles + 2 * C::kStages + 2 * kSchedSlots) * 8 + 4 * kSchedSlots * kItemWords + 8 + 16 <= C::kBarBytes,
+  static_assert((2 * kManyTiles + 2 * C::kQBufs + 2 * C::kStages + 2 * kSchedSlots) * 8 + 4 * kSchedSlots * kItemWords + 8 + 16 <= C::kBarBytes,
                 "barrier area");
   static_assert((4 * kSchedSlots * kItemWords) % 8 == 0, "drain_bar is 8-byte aligned");
 
@@ -550,9 +554,11 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
   const int box_shift = min(a.c.ps_shift, 7);
 
   if (threadIdx.x == 0) {
-    for (int t = 0; t < kManyTiles; ++t) {
+    for (int t = 0; t < C::kQBufs; ++t) {
       mbar_init(q_full + 8 * t, 1);
       mbar_init(q_empty + 8 * t, 1);
+    }
+    for (int t = 0; t < kManyTiles; ++t) {
       mbar_init(s_full + 8 * t, 1);
       mbar_init(s_empty + 8 * t, 4);
     }
@@ -598,7 +604,8 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
   if (warp == 0) {
     // ------------------------------------------------------------- TMA producer (the whole warp; a lane per page box)
     int stage = 0, slot = 0;
-    uint32_t kphase = 0, qphase = 0 /* bit x: phase of Q tile slot x */, wphase = 0;
+    int qb = 0;
+    uint32_t kphase = 0, qphase = 0, wphase = 0;
     bool alive = true;
     auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool {
       return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
@@ -622,6 +629,23 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
         if (t < end && key < it.len) page_of_box(a.c, it.b, key, a.status, page, pslot);
       };
       int page = 0, pslot = 0;
+      auto load_q = [&]() -> bool {
+        for (int x = 0; x < kManyTiles; ++x) {
+          if (many_tile_end(a, it, x) <= it.lo) continue;
+          if (!wait_all(q_empty + 8 * qb, qphase ^ 1u)) return false;
+          if (elect_one()) {
+            mbar_expect_tx(q_full + 8 * qb, (uint32_t)(a.tile_tokens * a.G * 128 * C::kHalves));
+            for (int hf = 0; hf < C::kHalves; ++hf)
+              tma_load_4d(q_smem + qb * C::kQBytes + hf * (BM * 128), &map_q, q_full + 8 * qb, hf * 64, it.kvh * a.G,
+                          it.q0 + it.t0 + x * a.tile_tokens, 0);
+          }
+          __syncwarp();
+          if (++qb == C::kQBufs) { qb = 0; qphase ^= 1u; }
+        }
+        return true;
+      };
+      // (with buffers of their own the next item's Q tiles come first, otherwise its K tile does while they wait for theirs)
+      if (C::kQBufs > kManyTiles) alive = load_q();
       for (int t = it.lo; t < end && alive; ++t) {
         const int key0 = t * BN;
         if ((t - it.lo) % ahead == 0) {
@@ -645,21 +669,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
         }
         __syncwarp();
         if (++stage == C::kStages) { stage = 0; kphase ^= 1u; }
-        if (t == it.lo) {
-          for (int x = 0; x < kManyTiles && alive; ++x) {
-            if (many_tile_end(a, it, x) <= it.lo) continue;
-            alive = wait_all(q_empty + 8 * x, ((qphase >> x) & 1u) ^ 1u);
-            if (!alive) break;
-            qphase ^= 1u << x;
-            if (elect_one()) {
-              mbar_expect_tx(q_full + 8 * x, (uint32_t)(a.tile_tokens * a.G * 128 * C::kHalves));
-              for (int hf = 0; hf < C::kHalves; ++hf)
-                tma_load_4d(q_smem + x * C::kQBytes + hf * (BM * 128), &map_q, q_full + 8 * x, hf * 64, it.kvh * a.G,
-                            it.q0 + it.t0 + x * a.tile_tokens, 0);
-            }
-            __syncwarp();
-          }
-        }
+        if (C::kQBufs == kManyTiles && t == it.lo && alive) alive = load_q();
       }
     }
     if (!alive && lane == 0) {
@@ -668,7 +678,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       // previous one (a barrier that was never armed reports its "previous" phase as complete at once).
       bool ok = true;
       for (int st = 0; st < C::kStages; ++st) ok &= mbar_drain(k_full + 8 * st, st < stage ? kphase : kphase ^ 1u);
-      for (int x = 0; x < kManyTiles; ++x) ok &= mbar_drain(q_full + 8 * x, ((qphase >> x) & 1u) ^ 1u);
+      for (int x = 0; x < C::kQBufs; ++x) ok &= mbar_drain(q_full + 8 * x, x < qb ? qphase : qphase ^ 1u);
       if (!ok) sts_u32(drain_fail, 1u);
     }
   } else if (warp == 1) {
@@ -676,7 +686,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
     constexpr uint32_t idesc = idesc_many();
     const uint64_t hi = (uint64_t)kDescHi << 32;
     const uint64_t q_desc = hi | smem_desc_lo(q_smem), k_desc = hi | smem_desc_lo(k_smem);
-    int stage = 0, slot = 0;
+    int stage = 0, slot = 0, qb = 0;
     uint32_t kphase = 0, qphase = 0, wphase = 0, sphase[kManyTiles] = {};
     bool alive = true;
     auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool {
@@ -692,10 +702,14 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       if (++slot == kSchedSlots) { slot = 0; wphase ^= 1u; }
       if (it.b < 0) break;
       const int lo = __shfl_sync(0xffffffffu, it.lo, 0);
-      int tx[kManyTiles], end = lo;
+      int tx[kManyTiles], buf[kManyTiles], end = lo;
+      uint32_t bphase[kManyTiles];
       for (int x = 0; x < kManyTiles; ++x) {
         tx[x] = __shfl_sync(0xffffffffu, many_tile_end(a, it, x), 0);
         end = max(end, tx[x]);
+        buf[x] = qb;
+        bphase[x] = qphase;
+        if (tx[x] > lo && ++qb == C::kQBufs) { qb = 0; qphase ^= 1u; }
       }
       for (int t = lo; t < end && alive; ++t) {
         alive = wait_all(k_full + 8 * stage, kphase);
@@ -704,15 +718,12 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
 #pragma unroll
         for (int x = 0; x < kManyTiles; ++x) {
           if (t >= tx[x] || !alive) continue;
-          if (t == lo) {
-            alive = wait_all(q_full + 8 * x, (qphase >> x) & 1u);
-            qphase ^= 1u << x;
-          }
+          if (t == lo) alive = wait_all(q_full + 8 * buf[x], bphase[x]);
           if (alive) alive = wait_all(s_empty + 8 * x, sphase[x] ^ 1u);
           if (!alive) continue;
           sphase[x] ^= 1u;
           tc_fence_after();
-          const uint64_t a_desc = q_desc + (uint64_t)(x * (C::kQBytes >> 4));
+          const uint64_t a_desc = q_desc + (uint64_t)(buf[x] * (C::kQBytes >> 4));
           if (elect_one()) {
 #pragma unroll
             for (int kk = 0; kk < HD / 16; ++kk) {
@@ -721,7 +732,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
               umma_bf16_desc(tmem_base + x * BN, a_desc + a_off, b_desc + b_off, idesc, kk > 0 ? 1u : 0u);
             }
             umma_commit(s_full + 8 * x);
-            if (t == tx[x] - 1) umma_commit(q_empty + 8 * x);
+            if (t == tx[x] - 1) umma_commit(q_empty + 8 * buf[x]);
           }
           __syncwarp();
         }
@@ -744,19 +755,21 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
     const int n_items = n_blocks * a.c.KH;
     int x = blockIdx.x * cut;                                // cut: next tile of this CTA's run
     const int x_end = min(x + cut, head_tiles * a.c.KH);
+    int round = 0;
     for (bool more = true; more;) {
       ManyItem it;
       it.b = -1;
       it.lo = it.len = 0;
       if (cut == 0) {
-        // a K/V head's blocks one after another, the longest rows first: the CTAs that run together stream the same keys
-        int k = 0;
-        if (lane == 0) k = atomicAdd(a.counters + kNextItem, 1);
-        k = __shfl_sync(0xffffffffu, k, 0);
-        more = k < n_items;
+        // The blocks with the longest rows first, one to a CTA and round, every other round backwards, so that the CTAs end together.  (Handed out by an atomic counter the next item came 2 us after it was
+        // asked for, half of what one of seven tiles takes.)
+        const int k = round * (int)gridDim.x + ((round & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
+        more = round * (int)gridDim.x < n_items;
+        ++round;
+        if (more && k >= n_items) continue;
         if (more) {
-          it.kvh = k / n_blocks;
-          const int blk = a.order[k - it.kvh * n_blocks];
+          it.kvh = k % a.c.KH;
+          const int blk = a.order[k / a.c.KH];
           const PagedBlock pb = a.blocks[blk];
           it.b = pb.b; it.t0 = pb.t0; it.q0 = pb.q0; it.n = pb.n; it.len = pb.len;
           it.hi = pb.tiles;
@@ -789,7 +802,20 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       int page = 0, pslot = 0;
       const int key = it.lo * BN + (lane << box_shift);
       if (it.b >= 0 && key < min(it.len, it.hi * BN)) page_of_box(a.c, it.b, key, a.status, page, pslot);
+      // a of the item's rows (the consumers would start each item with these loads)
+      float ra[kManyTiles * BM / 32];
+      const int tile_rows = a.tile_tokens * a.G;
+#pragma unroll
+      for (int i = 0; i < kManyTiles * BM / 32; ++i) {
+        const int in_tile = (32 * i) % BM + lane, tok = it.t0 + 32 * i / BM * a.tile_tokens + in_tile / a.G;
+        ra[i] = it.b >= 0 && in_tile < tile_rows && tok < it.n ? a.row_scale[(size_t)(it.q0 + tok) * a.H + it.kvh * a.G + in_tile % a.G] : 0.f;
+      }
       if (!__all_sync(0xffffffffu, mbar_wait(w_empty + 8 * slot, wphase ^ 1u, abort_flag))) break;
+      if (it.b >= 0) {
+        const uint32_t to = scales + 4u * (kManyTiles * BM) * slot;
+#pragma unroll
+        for (int i = 0; i < kManyTiles * BM / 32; ++i) sts_u32(to + 4 * (32 * i + lane), __float_as_uint(ra[i]));
+      }
       const uint32_t at = w_item + 4u * kItemWords * slot;
       sts_u32(at + 40 + 8 * lane, (uint32_t)page);
       sts_u32(at + 44 + 8 * lane, (uint32_t)pslot);
@@ -827,6 +853,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       alive = __all_sync(0xffffffffu, mbar_wait(w_full + 8 * slot, wphase, abort_flag));
       if (!alive) break;
       const ManyItem it = read_item(slot);
+      const float ra = __uint_as_float(lds_u32(scales + 4u * (uint32_t)((slot * kManyTiles + x) * BM + row_local)));
       __syncwarp();
       if (lane == 0) mbar_arrive(w_empty + 8 * slot);
       if (++slot == kSchedSlots) { slot = 0; wphase ^= 1u; }
@@ -840,7 +867,6 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       const int lim = valid ? pos : -1;                        // last key the row sees
       const int first_pos = it.len - it.n + it.t0 + x * a.tile_tokens;             // of the tile's rows
       const int last_pos = min(first_pos + a.tile_tokens, it.len) - 1;
-      const float ra = valid ? paged_scale(a, head, pos) : 0.f;
       const float slope = kAlibi && valid ? a.alibi[head] / a.sm_scale : 0.f;
       const int slot_row = valid ? x * tile_rows + row_local : 0;
       const size_t row = (size_t)it.unit * a.many_slots + (size_t)slot_row;
