@@ -84,6 +84,7 @@ constexpr int kFewSeqs = 256;   // sequences a launch of the "few" kernel takes
 struct PagedArgs {
   PagedCache c;
   int H, G;
+  unsigned inv_g;             // ceil(2^16 / G)
   int expo_class;
   float expo, alpha_m1, sm_scale;
   const float *beta, *gamma, *delta, *alibi;
@@ -112,6 +113,8 @@ struct PagedArgs {
   float* tau;
   int32_t* support;
   int32_t* status;
+  // r / G of a row slot: exact for r < 512, G <= 128 (r (G - 1) < 2^16)
+  __device__ __forceinline__ int by_g(int r) const { return (int)(((unsigned)r * inv_g) >> 16); }
 };
 
 enum Counter : int {

@@ -5,8 +5,9 @@
 // a bound too.  The keys above the bound are collected from what the score kernels left, into shared memory; Newton from the left on them;
 // p = [y - tau]_+^e; O = sum_j p_j v_j as a gather of V rows through the block table (asked for from memory as soon as a key is a
 // candidate).  All sums are taken in a fixed order.
-//   rows8   eight lanes per row: a record or a group's 32 scores and a V row are a coalesced access of eight lanes, sums take three
-//           shuffles, and a warp has four rows' chains of dependent loads under way.  Rows with more than kList8 candidates are listed for
+//   rows    eight lanes per row where there are many rows: a record or a group's 32 scores and a V row are a coalesced access of eight
+//           lanes, sums take three shuffles, and a warp has four rows' chains of dependent loads under way.  A warp per row where there are
+//           fewer.  Rows with more candidates than their list holds are listed for
 //   row     a CTA per row, for those and for calls of few or very long rows.
 #include <atomic>
 #include <cmath>
@@ -239,40 +240,51 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
   }
 }
 
-// ================================================================================================ rows8
-constexpr int kList8 = 96;           // candidates of a row
-constexpr int kWarps8 = 8;
-constexpr int kRows8 = 4 * kWarps8;  // rows of a CTA
+// ================================================================================================= rows
+// L lanes to a row, 8 or 32
+constexpr int kRowsWarps = 8;
+template <int L>
+struct RowsShape {
+  static constexpr int kRows = 32 * kRowsWarps / L;      // rows of a CTA
+  static constexpr int kList = L == 8 ? 96 : 256;        // candidates of a row
+  static constexpr unsigned kMask = L == 32 ? 0xffffffffu : (1u << (L & 31)) - 1u;
+};
 
-__device__ __forceinline__ float sum8(float x) {
+template <int L>
+__device__ __forceinline__ float sum_lanes(float x) {
 #pragma unroll
-  for (int o = 1; o < 8; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  for (int o = 1; o < L; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
-__device__ __forceinline__ float max8_lanes(float x) {
+template <int L>
+__device__ __forceinline__ float max_lanes(float x) {
 #pragma unroll
-  for (int o = 1; o < 8; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  for (int o = 1; o < L; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
   return x;
 }
 __device__ __forceinline__ float max4(const float4& x) { return fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)); }
 
-// (Loops are kept rolled: unrolled, this code no longer stayed in the instruction cache, 140 us against 90 on 150000 short rows.)
-template <int D, int EC, bool kMany>
-__global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __grid_constant__ PagedArgs a,
-                                                                      const __nv_bfloat16* __restrict__ v, int first, int units) {
+// (Loops are kept rolled: unrolled, this code no longer stayed in the instruction cache, 140 us against 86 on 11402 prompt tokens of 16 heads,
+// and 72 against 21 on 64 x 32 decode rows.)
+template <int D, int EC, bool kMany, int L>
+__global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_kernel(const __grid_constant__ PagedArgs a,
+                                                                                    const __nv_bfloat16* __restrict__ v, int first,
+                                                                                    int units) {
   pdl_begin();
-  __shared__ float list_y[kRows8][kList8];
-  __shared__ long long list_at[kRows8][kList8];          // key, then where its V row is
-  const int lane = threadIdx.x & 31, sl = lane & 7, sub_bit = lane & 24;
+  using S = RowsShape<L>;
+  constexpr int kOctets = L / 8;
+  __shared__ float list_y[S::kRows][S::kList];
+  __shared__ long long list_at[S::kRows][S::kList];      // key, then where its V row is
+  const int lane = threadIdx.x & 31, sl = lane & (L - 1), s8 = lane & 7, octet = sl >> 3, row_bit = lane & (32 - L);
   const int slots = kMany ? a.many_slots : a.few_slots;
-  const int cta_row = threadIdx.x >> 3;
+  const int cta_row = threadIdx.x / L;
   int unit, r;
   if constexpr (kMany) {
-    const int per = (slots + kRows8 - 1) / kRows8;         // CTAs of a unit
+    const int per = (slots + S::kRows - 1) / S::kRows;     // CTAs of a unit
     unit = blockIdx.x / per;
-    r = (blockIdx.x - unit * per) * kRows8 + cta_row;
+    r = (blockIdx.x - unit * per) * S::kRows + cta_row;
   } else {
-    const long long row = (long long)blockIdx.x * kRows8 + cta_row;
+    const long long row = (long long)blockIdx.x * S::kRows + cta_row;
     unit = (int)(row / slots);
     r = (int)(row - (long long)unit * slots);
   }
@@ -282,7 +294,8 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
   UnitOf w;
   w.b = -1;
   if (live) w = unit_of<kMany>(a, first, unit);
-  const int tok = w.t0 + r / a.G;
+  const int r_tok = a.by_g(r), g_head = r - r_tok * a.G;
+  const int tok = w.t0 + r_tok;
   live = live && w.b >= 0 && tok < w.s.n;
   if (!__any_sync(0xffffffffu, live)) return;
   const int pos = live ? w.s.len - w.s.n + tok : -1;
@@ -292,7 +305,7 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
   long long* my_at = list_at[cta_row];
   const float4 none = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
 
-  // ---- The keys above floor_y go to the list; loops run for the longest of the warp's four rows.  A row whose candidates do not fit gets a
+  // ---- The keys above floor_y go to the list; loops run for the longest of the warp's rows.  A row whose candidates do not fit gets a
   // second try with a higher bound: the threshold of maxima of different keys alone, by a few steps from the left (any iterate is a bound;
   // a hair below it for the rounding).  c = 1, alpha = 1.5, 32768 keys N(0, 1): 585 keys above y_max - 1, about 50 above that.
   int cnt = 0;
@@ -300,24 +313,28 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
   const Records rec = kMany && live ? records_of(a, w.cut, unit, r, row, pos) : Records{};
   const int groups = live ? pos / kGroupKeys + 1 : 0;
   const float4* max_row = reinterpret_cast<const float4*>(a.group_max + row * a.groups);
-  const int chunks = kMany ? 0 : (__reduce_max_sync(0xffffffffu, groups) + 31) / 32;
+  const int chunks = kMany ? 0 : (__reduce_max_sync(0xffffffffu, groups) + 4 * L - 1) / (4 * L);
   const int most_items = kMany ? __reduce_max_sync(0xffffffffu, rec.items) : 0;
 
+  auto row_bits = [&](bool x) { return (__ballot_sync(0xffffffffu, x) >> row_bit) & S::kMask; };
   auto append = [&](const float4& y4, int key) {            // this lane's four keys from `key` on
-    const float y[4] = {y4.x, y4.y, y4.z, y4.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool on = y[e] > floor_y;
-      const unsigned bits = (__ballot_sync(0xffffffffu, on) >> sub_bit) & 0xffu;
+    // (hardly ever more than one or two of them: a lane's first, then its second, ...)
+    unsigned left = (y4.x > floor_y ? 1u : 0u) | (y4.y > floor_y ? 2u : 0u) | (y4.z > floor_y ? 4u : 0u) | (y4.w > floor_y ? 8u : 0u);
+    for (;;) {
+      const unsigned all = __ballot_sync(0xffffffffu, left != 0u);
+      if (all == 0u) break;
+      const unsigned bits = (all >> row_bit) & S::kMask;
       const int at = cnt + __popc(bits & ((1u << sl) - 1u));
-      if (on && at < kList8) {
-        my_y[at] = y[e];
+      if (left && at < S::kList) {
+        const int e = __ffs(left) - 1;
+        my_y[at] = e < 2 ? (e == 0 ? y4.x : y4.y) : (e == 2 ? y4.z : y4.w);
         my_at[at] = key + e;
       }
+      left &= left - 1;
       cnt += __popc(bits);
     }
   };
-  // many: f(this lane's four values, its first key's place) for every four records, two lanes to a record
+  // many: f(this lane's four values, their first key) for every L / 2 records, two lanes to a record
   auto for_records = [&](auto&& f) {
 #pragma unroll 1
     for (int i = 0; i < most_items; ++i) {
@@ -330,12 +347,12 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
       }
       const int most = __reduce_max_sync(0xffffffffu, n);
 #pragma unroll 1
-      for (int s0 = 0; s0 < most; s0 += 16) {
+      for (int s0 = 0; s0 < most; s0 += 2 * L) {
         float4 y[4];
         int key[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const int at = s0 + 4 * u + (sl >> 1);
+          const int at = s0 + L / 2 * u + (sl >> 1);
           y[u] = none;
           key[u] = 0;
           if (at < n) {
@@ -345,17 +362,17 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          if (s0 + 4 * u >= most) break;
+          if (s0 + L / 2 * u >= most) break;
           y[u].x *= mag; y[u].y *= mag; y[u].z *= mag; y[u].w *= mag;
           f(y[u], key[u]);
         }
       }
     }
   };
-  // few: this lane's maxima of groups 32 i + 4 sl ..
+  // few: this lane's maxima of groups 4 L i + 4 sl ..
   auto maxima = [&](int i) {
     float4 m = none;
-    const int g = 32 * i + 4 * sl;
+    const int g = 4 * (L * i + sl);
     if (g < groups) {
       m = max_row[g >> 2];
       if (g + 1 >= groups) m.y = -INFINITY;
@@ -369,7 +386,7 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
   } else {
 #pragma unroll 4
     for (int i = 0; i < chunks; ++i) ymax = fmaxf(ymax, max4(maxima(i)));
-    ymax = max8_lanes(ymax);
+    ymax = max_lanes<L>(ymax);
     floor_y = ymax - 1.0f;
   }
 #pragma unroll 1
@@ -377,34 +394,42 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
     cnt = 0;
     if constexpr (kMany) {
       for_records([&](const float4& y, int key) {
-        const float m = max4(y);
-        ymax = fmaxf(ymax, m);
-        if (__any_sync(0xffffffffu, m > floor_y)) append(y, key);
+        ymax = fmaxf(ymax, max4(y));
+        append(y, key);
       });
-      ymax = max8_lanes(ymax);
+      ymax = max_lanes<L>(ymax);
     } else {
 #pragma unroll 1
       for (int i = 0; i < chunks; ++i) {
         const float4 m = maxima(i);
-        unsigned bits = ((m.x > floor_y ? 1u : 0u) | (m.y > floor_y ? 2u : 0u) | (m.z > floor_y ? 4u : 0u) | (m.w > floor_y ? 8u : 0u)) << (4 * sl);
+        const unsigned mine = (m.x > floor_y ? 1u : 0u) | (m.y > floor_y ? 2u : 0u) | (m.z > floor_y ? 4u : 0u) | (m.w > floor_y ? 8u : 0u);
+        if (!__any_sync(0xffffffffu, mine != 0u)) continue;
+#pragma unroll 1
+        for (int e = 0; e < 4; ++e) {
+          unsigned bits = row_bits((mine >> e) & 1u);        // groups 4 (L i + bit) + e
+          while (__any_sync(0xffffffffu, bits != 0u)) {
+            // four steps in flight, of as many groups as the row has octets of lanes, an octet the next bit each
+            float4 y[4];
+            int key[4];
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) bits |= __shfl_xor_sync(0xffffffffu, bits, o);
-        while (__any_sync(0xffffffffu, bits != 0u)) {
-          float4 y[4];
-          int key[4];
+            for (int u = 0; u < 4; ++u) {
+              unsigned my = bits;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            y[u] = none;
-            key[u] = (32 * i + __ffs(bits) - 1) * kGroupKeys + 4 * sl;
-            if (bits) y[u] = *reinterpret_cast<const float4*>(y_row + key[u]);
-            bits &= bits - 1;
+              for (int o = 0; o < kOctets; ++o) {
+                if (o < octet) my &= my - 1;
+                bits &= bits - 1;
+              }
+              y[u] = none;
+              key[u] = (4 * (L * i + __ffs(my) - 1) + e) * kGroupKeys + 4 * s8;
+              if (my) y[u] = *reinterpret_cast<const float4*>(y_row + key[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) append(y[u], key[u]);
           }
-#pragma unroll
-          for (int u = 0; u < 4; ++u) append(y[u], key[u]);
         }
       }
     }
-    const bool over = cnt > kList8;
+    const bool over = cnt > S::kList;
     if (attempt == 1 || a.expo < 1.0f || !__any_sync(0xffffffffu, over)) break;
     float tau = fmaxf(floor_y, ymax - 1.0f);
 #pragma unroll 1
@@ -428,15 +453,15 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
           add(m.w);
         }
       }
-      s0 = sum8(s0);
-      s1 = sum8(s1);
+      s0 = sum_lanes<L>(s0);
+      s1 = sum_lanes<L>(s1);
       const bool go = s0 > 1.01f && s1 > 0.f;
       if (go) tau += threshold_step(s0, s1, EC, a.expo);
       if (!__any_sync(0xffffffffu, go && over)) break;
     }
     if (over) floor_y = fmaxf(floor_y, fmaxf(ymax - 1.0f, bound_below(tau)));
   }
-  if (live && cnt > kList8) {
+  if (live && cnt > S::kList) {
     if (sl == 0) a.spilled[atomicAdd(a.counters + kSpilledRows, 1)] = (int)row;
     live = false;
   }
@@ -445,7 +470,7 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
   // ---- where the candidates' V rows are; they are asked for now and come while the threshold is found
   const __nv_bfloat16* v_head = v + (long long)kvh * a.c.s_head;
   const Pages pages = pages_of(a.c, live ? w.b : 0);
-  for (int e = sl; e < cnt; e += 8) {
+  for (int e = sl; e < cnt; e += L) {
     const long long off = pages.at((int)my_at[e]);
     if (off >= 0) prefetch_row<D>(v_head + off);
     my_at[e] = off;
@@ -461,52 +486,61 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
   for (int it = 0; it < kMaxSteps; ++it) {
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll 1
-    for (int e = sl; e < longest; e += 8) {
+    for (int e = sl; e < longest; e += L) {
       float ye, ye1;
       powers<EC>(e < cnt ? fmaxf(my_y[e] - st.tau, 0.f) : 0.f, a.expo, ye, ye1);
       s0 += ye;
       s1 += ye1;
     }
-    s0 = sum8(s0);
-    s1 = sum8(s1);
+    s0 = sum_lanes<L>(s0);
+    s1 = sum_lanes<L>(s1);
     if (!done) done = !solve_step(st, s0, s1, EC, a.expo);
     if (__all_sync(0xffffffffu, done)) break;
   }
   const float tau = st.tau;
   int support = 0;
-  for (int e = sl; e < cnt; e += 8) {
+  for (int e = sl; e < cnt; e += L) {
     const float d = fmaxf(my_y[e] - tau, 0.f);
     float p, p1;
     powers<EC>(d, a.expo, p, p1);
     support += d > 0.f ? 1 : 0;
     my_y[e] = my_at[e] >= 0 ? p : 0.f;                      // (a page that is not there counts as zeros)
   }
-  support = (int)sum8((float)support);
+  support = (int)sum_lanes<L>((float)support);
   __syncwarp();
 
-  // ---- O = sum_j p_j v_j, four V rows of each of the warp's rows in flight
+  // ---- O = sum_j p_j v_j: an octet of lanes to a V row, four of each octet in flight
   float acc[D / 8];
 #pragma unroll
   for (int e = 0; e < D / 8; ++e) acc[e] = 0.f;
 #pragma unroll 1
-  for (int e0 = 0; e0 < cnt; e0 += 4) {
+  for (int e0 = octet; e0 < cnt; e0 += 4 * kOctets) {
     float p[4];
     Share<D> x[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      p[u] = e0 + u < cnt ? my_y[e0 + u] : 0.f;
+      const int e = e0 + kOctets * u;
+      p[u] = e < cnt ? my_y[e] : 0.f;
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
         x[u].w[c] = make_uint4(0u, 0u, 0u, 0u);
-        if (p[u] > 0.f) x[u].w[c] = *reinterpret_cast<const uint4*>(v_head + my_at[e0 + u] + 64 * c + 8 * sl);
+        if (p[u] > 0.f) x[u].w[c] = *reinterpret_cast<const uint4*>(v_head + my_at[e] + 64 * c + 8 * s8);
       }
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) add_share<D>(acc, p[u], x[u]);
   }
-  if (live) {
-    const size_t out = (size_t)(w.s.q0 + tok) * a.H + kvh * a.G + r % a.G;
-    store_share<D>(a.o + out * D, sl, acc);
+  if constexpr (L == 32) {
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < D / 8; ++e) {
+      acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 8);
+      acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 16);
+    }
+  }
+  if (live && octet == 0) {
+    const size_t out = (size_t)(w.s.q0 + tok) * a.H + kvh * a.G + g_head;
+    store_share<D>(a.o + out * D, s8, acc);
     if (sl == 0) {
       a.tau[out] = tau;
       if (a.support) a.support[out] = support;
@@ -515,27 +549,28 @@ __global__ void __launch_bounds__(32 * kWarps8, 4) paged_rows8_kernel(const __gr
 }
 
 // ================================================================================================== row
-constexpr int kRowWarps = 8;
+constexpr int kCtaWarps = 8;
 constexpr int kSeg = 256;            // list entries of a warp
+constexpr int kRowsWorth = 1184, kRows8Worth = 9472;   // rows from which on a warp to a row, and eight lanes, fill the machine
 constexpr int kChunks = 8;           // chunks of 32 groups of a warp whose maxima stay in shared memory
 
-// kSpilled: the rows listed by rows8, by CTAs that stay; otherwise a CTA for every row slot
+// kSpilled: the rows listed by the rows kernel, by CTAs that stay; otherwise a CTA for each of the n_slots row slots
 template <int D, bool kMany, bool kSpilled>
-__global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_kernel(const __grid_constant__ PagedArgs a,
-                                                                     const __nv_bfloat16* __restrict__ v, int first) {
+__global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __grid_constant__ PagedArgs a,
+                                                                     const __nv_bfloat16* __restrict__ v, int first, int n_slots) {
   pdl_begin();
-  constexpr int W = kRowWarps;
-  __shared__ float list_y[W][kSeg];
-  __shared__ int list_j[W][kSeg];
-  __shared__ float maxima[W][kChunks * 32];
+  constexpr int W = kCtaWarps;
+  __shared__ float list_y[kCtaWarps][kSeg];
+  __shared__ long long list_at[kCtaWarps][kSeg];          // where the V row is
+  __shared__ float maxima[kCtaWarps][kChunks * 32];
   __shared__ float2 red[2][W];
   __shared__ float opart[W][D];
   const int lane = threadIdx.x & 31, sl = lane & 7, warp = threadIdx.x >> 5;
   const int slots = kMany ? a.many_slots : a.few_slots;
-  const int n_rows = kSpilled ? a.counters[kSpilledRows] : 0;
+  const int n_rows = kSpilled ? a.counters[kSpilledRows] : n_slots;
   float* my_max = maxima[warp];
   float* my_y = list_y[warp];
-  int* my_j = list_j[warp];
+  long long* my_at = list_at[warp];
   int red_slot = 0;
   // sums over the row's warps in a fixed order; every thread gets them
   auto row_sum2 = [&](float x, float y) {
@@ -556,8 +591,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
     return make_float2(x, y);
   };
 
-  for (int n = blockIdx.x;; n += gridDim.x) {
-    if (kSpilled && n >= n_rows) break;
+  for (int n = blockIdx.x; n < n_rows; n += gridDim.x) {
     const int row = kSpilled ? a.spilled[n] : n;
     const int unit = row / slots, r = row - unit * slots;
     // ---- which row this is
@@ -565,14 +599,15 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
     const UnitOf w = unit_of<kMany>(a, first, unit);
     const PagedSeq s = w.s;
     const int tok = w.t0 + r / a.G;
-    if (w.b < 0 || tok >= s.n) break;                      // (no row; never so for listed ones)
+    if (w.b < 0 || tok >= s.n) continue;                   // (no row)
     const int pos = s.len - s.n + tok;
     const Pages pages = pages_of(a.c, w.b);
     const __nv_bfloat16* v_head = v + (long long)kvh * a.c.s_head;
     const float* y_row = a.scores + (size_t)row * a.score_stride;
     float ymax = -INFINITY, floor_y = -INFINITY;
 
-    // for_keys(f): f(y, key) with a key per lane (y = -inf: none) for all keys of this warp that are kept and can be in the support
+    // for_keys(f): f(y, key) with a key per lane (y = -inf: none) for all keys of this warp that are kept and can be in the support,
+    // eight (four records) in flight
     const int groups = pos / kGroupKeys + 1;
     const float* max_row = a.group_max + (size_t)row * a.groups;
     // few: group g is warp g mod W's, 32 of a warp's groups are a chunk (so that short rows and runs of neighbouring candidates are
@@ -590,10 +625,10 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
         for (int i = 0; i < chunks; ++i) {
           unsigned todo = __ballot_sync(0xffffffffu, max_at(i) > floor_y);
           while (todo) {
-            int at[4];
-            float y[4];
+            int at[8];
+            float y[8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < 8; ++u) {
               at[u] = -1;
               y[u] = -INFINITY;
               if (todo) {
@@ -603,7 +638,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
               }
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < 8; ++u)
               if (at[u] >= 0) f(y[u], at[u]);
           }
         }
@@ -663,7 +698,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
       for (int i = 0; i < rec.items; ++i) floor_y = fmaxf(floor_y, rec.info[(size_t)i * rec.slots].y);
     }
 
-    // ---- the threshold of the groups' largest keys as a bound (see rows8)
+    // ---- the threshold of the groups' largest keys as a bound (see the rows kernel)
     if (!kMany && a.expo >= 1.0f) {
       int cand = 0;
       for (int i = 0; i < chunks; ++i) cand += __popc(__ballot_sync(0xffffffffu, max_at(i) > floor_y));
@@ -693,10 +728,10 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
       const unsigned m = __ballot_sync(0xffffffffu, y > floor_y);
       const int at = cnt + __popc(m & ((1u << lane) - 1u));
       if (y > floor_y && at < kSeg) {
-        my_y[at] = y;
-        my_j[at] = key;
         const long long off = pages.at(key);
         if (off >= 0) prefetch_row<D>(v_head + off);
+        my_y[at] = y;
+        my_at[at] = off;
       }
       cnt += __popc(m);
     });
@@ -727,29 +762,27 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
     }
     const float tau = st.tau;
 
-    // ---- O = sum_j p_j v_j: a key per eight lanes, sixteen V rows of a warp in flight
+    // ---- O = sum_j p_j v_j: a key per eight lanes, 32 (head_dim 128: 16) V rows of a warp in flight
+    constexpr int kFlight = D == 64 ? 8 : 4;
     float acc[D / 8];
 #pragma unroll
     for (int e = 0; e < D / 8; ++e) acc[e] = 0.f;
     int support = 0;
-    auto gather = [&](float y, int j) {                     // a key per lane (y = -inf: none)
+    auto gather = [&](float y, long long off) {             // a key per lane (y = -inf: none)
       const float d = y - tau;
       float p = 0.f, p1;
-      long long off = -1;
-      if (d > 0.f) {
-        pow_pair(d, a.expo_class, a.expo, p, p1);
-        off = pages.at(j);
-      }
+      if (d > 0.f) pow_pair(d, a.expo_class, a.expo, p, p1);
+      else off = -1;
       const unsigned m = __ballot_sync(0xffffffffu, d > 0.f);
       support += __popc(m);
-      // (the eight lanes of a key take the set bits of their own octet of the mask, so no bit is looked for twice)
+      // (eight lanes take the keys of their own octet of lanes)
 #pragma unroll
-      for (int e0 = 0; e0 < 8; e0 += 4) {
-        if (((m >> e0) & 0x0f0f0f0fu) == 0u) continue;
-        float px[4];
-        Share<D> x[4];
+      for (int e0 = 0; e0 < 8; e0 += kFlight) {
+        if (kFlight < 8 && ((m >> e0) & 0x0f0f0f0fu) == 0u) continue;
+        float px[kFlight];
+        Share<D> x[kFlight];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < kFlight; ++u) {
           const int src = (lane & 24) + e0 + u;
           px[u] = __shfl_sync(0xffffffffu, p, src);
           const long long at = __shfl_sync(0xffffffffu, off, src);
@@ -760,28 +793,28 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
           }
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) add_share<D>(acc, px[u], x[u]);
+        for (int u = 0; u < kFlight; ++u) add_share<D>(acc, px[u], x[u]);
       }
     };
     if (!walk) {
       for (int e0 = 0; e0 < cnt; e0 += 32) {
         const int e = e0 + lane;
-        gather(e < cnt ? my_y[e] : -INFINITY, e < cnt ? my_j[e] : 0);
+        gather(e < cnt ? my_y[e] : -INFINITY, e < cnt ? my_at[e] : -1);
       }
     } else {
-      for_keys([&](float y, int key) { gather(y, key); });
+      for_keys([&](float y, int key) { gather(y, y > tau ? pages.at(key) : -1); });
     }
 #pragma unroll
     for (int e = 0; e < D / 8; ++e) {
       acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 8);
       acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 16);
     }
+    const size_t out = (size_t)(s.q0 + tok) * a.H + kvh * a.G + r % a.G;
     if (lane < 8) {
 #pragma unroll
       for (int e = 0; e < D / 8; ++e) opart[warp][(e >> 3) * 64 + 8 * sl + (e & 7)] = acc[e];
     }
     const float2 total = row_sum2(lane == 0 ? (float)support : 0.f, 0.f);   // (a barrier; counts stay below 2^24)
-    const size_t out = (size_t)(s.q0 + tok) * a.H + kvh * a.G + r % a.G;
     if ((int)threadIdx.x < D) {
       float o = 0.f;
 #pragma unroll
@@ -792,41 +825,45 @@ __global__ void __launch_bounds__(32 * kRowWarps, D == 64 ? 3 : 2) paged_row_ker
       a.tau[out] = tau;
       if (a.support) a.support[out] = (int)total.x;
     }
-    if (!kSpilled) break;
     __syncthreads();                                        // (opart is read before the next row writes it)
   }
 }
 
-template <int D, bool kMany>
-cudaError_t launch_solve_d(const PagedArgs& a, const __nv_bfloat16* v, int first, int units, bool rows8, cudaStream_t stream) {
-  const int slots = kMany ? a.many_slots : a.few_slots;
-  const long long rows = (long long)units * slots;
-  if (!rows8) return launch_kernel(paged_row_kernel<D, kMany, false>, (unsigned)rows, 32 * kRowWarps, 0, stream, a, v, first);
-  const unsigned ctas = (unsigned)(kMany ? (long long)units * ((slots + kRows8 - 1) / kRows8) : (rows + kRows8 - 1) / kRows8);
-  cudaError_t err;
-#define ENTMAX_ROWS8(EC) launch_kernel(paged_rows8_kernel<D, EC, kMany>, ctas, 32 * kWarps8, 0, stream, a, v, first, units)
-  switch (a.expo_class) {
-    case kExpo2: err = ENTMAX_ROWS8(kExpo2); break;
-    case kExpo1: err = ENTMAX_ROWS8(kExpo1); break;
-    case kExpo4: err = ENTMAX_ROWS8(kExpo4); break;
-    default: err = ENTMAX_ROWS8(kExpoGeneral); break;
-  }
-#undef ENTMAX_ROWS8
-  if (err != cudaSuccess) return err;
-  return launch_kernel(paged_row_kernel<D, kMany, true>, 2 * a.sms, 32 * kRowWarps, 0, stream, a, v, first);
+// Lanes of a row in the solve of a launch; 0: a CTA
+int solve_lanes(const PagedArgs& a, bool many, long long rows) {
+  if (rows < kRowsWorth || a.max_kv > (many ? 1 << 20 : 32768)) return 0;
+  return rows < kRows8Worth ? 32 : 8;
 }
 
-// Eight lanes per row where there are rows enough to fill the machine that way, or where a row is short
-bool solve_by_rows8(const PagedArgs& a, bool many, long long rows) {
-  return a.max_kv <= (many ? 65536 : 8192) && (rows >= 8 * 148 || a.max_kv <= 2048);
+template <int D, bool kMany, int L>
+cudaError_t launch_rows(const PagedArgs& a, const __nv_bfloat16* v, int first, int units, cudaStream_t stream) {
+  constexpr int kRows = RowsShape<L>::kRows;
+  const int slots = kMany ? a.many_slots : a.few_slots;
+  const unsigned ctas = (unsigned)(kMany ? (long long)units * ((slots + kRows - 1) / kRows) : ((long long)units * slots + kRows - 1) / kRows);
+  cudaError_t err;
+#define ENTMAX_ROWS(EC) launch_kernel(paged_rows_kernel<D, EC, kMany, L>, ctas, 32 * kRowsWarps, 0, stream, a, v, first, units)
+  switch (a.expo_class) {
+    case kExpo2: err = ENTMAX_ROWS(kExpo2); break;
+    case kExpo1: err = ENTMAX_ROWS(kExpo1); break;
+    case kExpo4: err = ENTMAX_ROWS(kExpo4); break;
+    default: err = ENTMAX_ROWS(kExpoGeneral); break;
+  }
+#undef ENTMAX_ROWS
+  if (err != cudaSuccess) return err;
+  return launch_kernel(paged_row_kernel<D, kMany, true>, 2 * a.sms, 32 * kCtaWarps, 0, stream, a, v, first, 0);
 }
+
+template <int D, bool kMany>
+cudaError_t launch_solve_d(const PagedArgs& a, const __nv_bfloat16* v, int first, int units, cudaStream_t stream) {
+  const int rows = units * (kMany ? a.many_slots : a.few_slots), lanes = solve_lanes(a, kMany, rows);
+  if (lanes == 0) return launch_kernel(paged_row_kernel<D, kMany, false>, (unsigned)rows, 32 * kCtaWarps, 0, stream, a, v, first, rows);
+  return lanes == 8 ? launch_rows<D, kMany, 8>(a, v, first, units, stream) : launch_rows<D, kMany, 32>(a, v, first, units, stream);
+}
+
 template <bool kMany>
 cudaError_t launch_solve(const PagedArgs& a, const void* v, int first, int units, cudaStream_t stream) {
   const __nv_bfloat16* vb = static_cast<const __nv_bfloat16*>(v);
-  const long long rows = (long long)units * (kMany ? a.many_slots : a.few_slots);
-  const bool rows8 = solve_by_rows8(a, kMany, rows);
-  return a.c.D == 64 ? launch_solve_d<64, kMany>(a, vb, first, units, rows8, stream)
-                     : launch_solve_d<128, kMany>(a, vb, first, units, rows8, stream);
+  return a.c.D == 64 ? launch_solve_d<64, kMany>(a, vb, first, units, stream) : launch_solve_d<128, kMany>(a, vb, first, units, stream);
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -869,6 +906,7 @@ int plan_paged(const entmax_attn_paged_cache* cache, const entmax_attn_paged_par
   if (p->q_heads < 1 || p->q_heads % a->c.KH) return ENTMAX_ATTN_EINVAL_SHAPE;
   a->H = p->q_heads;
   a->G = a->H / a->c.KH;
+  a->inv_g = (65536u + a->G - 1) / a->G;
   if (a->G > 128) return ENTMAX_ATTN_EINVAL_SHAPE;
   if ((long long)a->c.T * a->H > 0x7fffffffLL / 2 || (long long)a->c.B * a->H > 0x7fffffffLL / 2048) return ENTMAX_ATTN_EINVAL_SHAPE;
   if (p->max_q_len < 0 || p->max_kv_len < 0) return ENTMAX_ATTN_EINVAL_SHAPE;
@@ -996,7 +1034,7 @@ extern "C" int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const
   }
   for (int b = 0; l.few && b < a.c.B && err == cudaSuccess; b += l.few_seqs) {
     const int n = a.c.B - b < l.few_seqs ? a.c.B - b : l.few_seqs;
-    if (solve_by_rows8(a, false, (long long)n * a.c.KH * a.few_slots)) err = cudaMemsetAsync(a.counters, 0, kCounters * sizeof(int32_t), stream);
+    if (solve_lanes(a, false, (long long)n * a.c.KH * a.few_slots) != 0) err = cudaMemsetAsync(a.counters, 0, kCounters * sizeof(int32_t), stream);
     if (err == cudaSuccess) err = launch_paged_few(a, q, k_cache, params->q_stride_t, params->q_stride_h, b, n, stream);
     if (err == cudaSuccess) err = launch_solve<false>(a, v_cache, b, n * a.c.KH, stream);
   }

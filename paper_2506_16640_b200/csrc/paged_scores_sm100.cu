@@ -362,6 +362,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
         // four rows together, so that their reductions overlap
 #pragma unroll
         for (int r0 = 0; r0 < NR; r0 += 4) {
+          if (r0 > 0 && r0 >= rows) continue;                // (sequences with fewer rows than the longest)
           float y[4], m[4];
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
@@ -883,6 +884,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       float top[8];
 #pragma unroll
       for (int g = 0; g < 8; ++g) top[g] = -INFINITY;
+      bool flat = false;
       for (int t = it.lo; t < end && alive; ++t) {
         alive = __all_sync(0xffffffffu, mbar_wait(my_full, fphase, abort_flag));
         if (!alive) break;
@@ -909,9 +911,8 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
             for (int u = 0; u < 64; ++u) v[u] = col0 + u <= lim ? v[u] : -INFINITY;
           }
         };
-        // Now and then the bound is also taken from eight classes of keys; a stream that starts without any looks at its first tile twice
-        const bool classes = step_no == 0 || step_no == 3 || (step_no & 15) == 15;
-        if (classes) {
+        // a stream that starts without a bound looks at its first tile twice
+        if (step_no == 0) {
 #pragma unroll 1
           for (int c = 0; c < n_steps; ++c) {
             float v[64];
@@ -919,8 +920,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
 #pragma unroll
             for (int q = 0; q < 8; ++q) top[q] = fmaxf(top[q], max8(&v[8 * q]));
           }
-          best = fmaxf(best, max8(top));
-          thr = fmaxf(thr, fmaxf(best - margin, bound_from_eight(top, margin, a.expo_class, a.expo)));
+          best = max8(top);
+          const float bound = bound_from_eight(top, margin, a.expo_class, a.expo);
+          flat = __any_sync(0xffffffffu, bound > -INFINITY);
+          thr = fmaxf(thr, fmaxf(best - margin, bound));
         }
         // One straight pass: maxima of eight columns, and eight columns with a candidate go to the row's records as they are, by predicated
         // stores where some row of the warp has one among 32 columns (a vote for 64: chunk of 2048 over 32768 keys 250 -> 243 us here;
@@ -935,6 +938,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
           const float m_lo = fmaxf(fmaxf(g[0], g[1]), fmaxf(g[2], g[3])), m_hi = fmaxf(fmaxf(g[4], g[5]), fmaxf(g[6], g[7]));
           best = max3(best, m_lo, m_hi);
           thr = fmaxf(thr, best - margin);
+          if (flat) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) top[q] = fmaxf(top[q], g[q]);
+          }
           const int col0 = col_base + 64 * c;
           if (__any_sync(0xffffffffu, m_lo > thr)) {
             keep_record_if_greater<0>(g[0], thr, n_rec, rec, rec_key, rec_bytes, col0, &v[0]);
@@ -953,6 +960,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(my_empty);
+        // Where supports are long the bound is taken from the classes again after 2, 4, 8, ... tiles (keys that are a record among all before
+        // them come ever more rarely)
+        if (flat && step_no > 0 && (step_no & (step_no + 1)) == 0)
+          thr = fmaxf(thr, bound_from_eight(top, margin, a.expo_class, a.expo));
       }
       if (valid && alive)
         a.row_info[((size_t)it.unit * a.many_items + it.item) * a.many_slots + slot_row] =
