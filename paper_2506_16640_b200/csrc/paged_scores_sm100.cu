@@ -592,6 +592,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
   tc_fence_after();
   const uint32_t tmem_base = lds_u32(tmem_slot);
 
+  // Slopes: an item's tiles from the last one backwards (see paged_few_kernel).  (hi: of the item's Q tile or the item, whose ends meet in the
+  // item's last tile.)
+  auto tile_of = [&](int lo, int hi, int step) { return kAlibi ? hi - 1 - step : lo + step; };
   auto read_item = [&](int slot) {
     ManyItem it;
     const uint32_t at = w_item + 4u * kItemWords * slot;
@@ -631,9 +634,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       const int ahead = 32 / boxes;
       int end = it.lo;
       for (int x = 0; x < kManyTiles; ++x) end = max(end, many_tile_end(a, it, x));
-      auto look_up = [&](int t, int& page, int& pslot) {
-        const int key = t * BN + (lane << box_shift);
-        if (t < end && key < it.len) page_of_box(a.c, it.b, key, a.status, page, pslot);
+      auto look_up = [&](int step, int& page, int& pslot) {
+        const int at = step + lane / boxes, key = tile_of(it.lo, end, at) * BN + ((lane & (boxes - 1)) << box_shift);
+        if (at < end - it.lo && key < it.len) page_of_box(a.c, it.b, key, a.status, page, pslot);
       };
       int page = 0, pslot = 0;
       auto load_q = [&]() -> bool {
@@ -653,14 +656,14 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       };
       // (with buffers of their own the next item's Q tiles come first, otherwise its K tile does while they wait for theirs)
       if (C::kQBufs > kManyTiles) alive = load_q();
-      for (int t = it.lo; t < end && alive; ++t) {
-        const int key0 = t * BN;
-        if ((t - it.lo) % ahead == 0) {
+      for (int step = 0; step < end - it.lo && alive; ++step) {
+        const int key0 = tile_of(it.lo, end, step) * BN;
+        if (step % ahead == 0) {
           page = page2;
           pslot = pslot2;
-          look_up(t + ahead, page2, pslot2);                // (its latency is covered by the tiles in between)
+          look_up(step + ahead, page2, pslot2);             // (its latency is covered by the tiles in between)
         }
-        const int src = ((t - it.lo) % ahead) * boxes + (lane & (boxes - 1));
+        const int src = (step % ahead) * boxes + (lane & (boxes - 1));
         const int pg = __shfl_sync(0xffffffffu, page, src), sl = __shfl_sync(0xffffffffu, pslot, src);
         alive = wait_all(k_empty + 8 * stage, kphase ^ 1u);
         if (!alive) break;
@@ -676,7 +679,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
         }
         __syncwarp();
         if (++stage == C::kStages) { stage = 0; kphase ^= 1u; }
-        if (C::kQBufs == kManyTiles && t == it.lo && alive) alive = load_q();
+        if (C::kQBufs == kManyTiles && step == 0 && alive) alive = load_q();
       }
     }
     if (!alive && lane == 0) {
@@ -718,14 +721,15 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
         bphase[x] = qphase;
         if (tx[x] > lo && ++qb == C::kQBufs) { qb = 0; qphase ^= 1u; }
       }
-      for (int t = lo; t < end && alive; ++t) {
+      for (int step = 0; step < end - lo && alive; ++step) {
+        const int t = tile_of(lo, end, step);
         alive = wait_all(k_full + 8 * stage, kphase);
         if (!alive) break;
         const uint64_t b_desc = k_desc + (uint64_t)(stage * (C::kKBytes >> 4));
 #pragma unroll
         for (int x = 0; x < kManyTiles; ++x) {
           if (t >= tx[x] || !alive) continue;
-          if (t == lo) alive = wait_all(q_full + 8 * buf[x], bphase[x]);
+          if (t == (kAlibi ? tx[x] - 1 : lo)) alive = wait_all(q_full + 8 * buf[x], bphase[x]);
           if (alive) alive = wait_all(s_empty + 8 * x, sphase[x] ^ 1u);
           if (!alive) continue;
           sphase[x] ^= 1u;
@@ -739,7 +743,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
               umma_bf16_desc(tmem_base + x * BN, a_desc + a_off, b_desc + b_off, idesc, kk > 0 ? 1u : 0u);
             }
             umma_commit(s_full + 8 * x);
-            if (t == tx[x] - 1) umma_commit(q_empty + 8 * buf[x]);
+            if (t == (kAlibi ? lo : tx[x] - 1)) umma_commit(q_empty + 8 * buf[x]);
           }
           __syncwarp();
         }
@@ -766,7 +770,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
     for (bool more = true; more;) {
       ManyItem it;
       it.b = -1;
-      it.lo = it.len = 0;
+      it.lo = it.hi = it.len = 0;
       if (cut == 0) {
         // The blocks with the longest rows first, one to a CTA and round, every other round backwards, so that the CTAs end together.  (Handed out by an atomic counter the next item came 2 us after it was
         // asked for, half of what one of seven tiles takes.)
@@ -807,8 +811,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
         }
       }
       int page = 0, pslot = 0;
-      const int key = it.lo * BN + (lane << box_shift);
-      if (it.b >= 0 && key < min(it.len, it.hi * BN)) page_of_box(a.c, it.b, key, a.status, page, pslot);
+      const int boxes = BN >> box_shift, step = lane / boxes;
+      const int key = tile_of(it.lo, it.hi, step) * BN + ((lane & (boxes - 1)) << box_shift);
+      if (it.b >= 0 && step < it.hi - it.lo && key < it.len) page_of_box(a.c, it.b, key, a.status, page, pslot);
       // a of the item's rows (the consumers would start each item with these loads)
       float ra[kManyTiles * BM / 32];
       const int tile_rows = a.tile_tokens * a.G;
@@ -891,12 +896,12 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
 #pragma unroll
       for (int g = 0; g < 8; ++g) top[g] = -INFINITY;
       bool flat = false;
-      for (int t = it.lo; t < end && alive; ++t) {
+      for (int step_no = 0; step_no < end - it.lo && alive; ++step_no) {
         alive = __all_sync(0xffffffffu, mbar_wait(my_full, fphase, abort_flag));
         if (!alive) break;
         fphase ^= 1u;
         tc_fence_after();
-        const int col_base = t * BN, step_no = t - it.lo;
+        const int col_base = tile_of(it.lo, end, step_no) * BN;
         const int n_steps = min(BN / 64, (last_pos - col_base) / 64 + 1);   // 64-column steps that some row sees
         // 64 columns from column 64 c on, as both looks at them take them
         auto load = [&](float (&v)[64], int c) {
