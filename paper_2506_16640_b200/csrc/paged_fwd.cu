@@ -129,7 +129,6 @@ __device__ __forceinline__ UnitOf unit_of(const PagedArgs& a, int first, int uni
 // longest rows first (by 1024 classes of length), so that the CTAs end together; clears the counters.  The first CTA does this, the others
 // fill in the scales of the rows.
 constexpr int kPlanThreads = 1024;
-constexpr int kLeastCut = 4;
 __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_constant__ PagedArgs a, int block0, int blocks) {
   pdl_begin();
   __shared__ int bin[kPlanThreads];               // blocks of a class, then the next place of the class
@@ -232,7 +231,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
     a.counters[kTiles] = carry;
     // units for less than three rounds of the machine are cut
     const long long all = (long long)carry * a.c.KH;
-    a.counters[kCut] = n_blocks * a.c.KH >= 3 * a.sms ? 0 : max((int)((all + a.sms - 1) / a.sms), kLeastCut);
+    a.counters[kCut] = n_blocks * a.c.KH >= 3 * a.sms ? 0 : (int)((all + a.sms - 1) / a.sms);
   }
   for (int i = tid; i < blocks; i += kPlanThreads) {
     const PagedBlock pb = a.blocks[i];
@@ -316,6 +315,9 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_ke
   const int chunks = kMany ? 0 : (__reduce_max_sync(0xffffffffu, groups) + 4 * L - 1) / (4 * L);
   const int most_items = kMany ? __reduce_max_sync(0xffffffffu, rec.items) : 0;
 
+  // what the row's items left, a lane each (those past L are read when their turn comes)
+  float4 info = make_float4(0.f, -INFINITY, 0.f, 0.f);
+  if (kMany && sl < rec.items) info = rec.info[(size_t)sl * rec.slots];
   auto row_bits = [&](bool x) { return (__ballot_sync(0xffffffffu, x) >> row_bit) & S::kMask; };
   auto append = [&](const float4& y4, int key) {            // this lane's four keys from `key` on
     // (hardly ever more than one or two of them: a lane's first, then its second, ...)
@@ -338,12 +340,12 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_ke
   auto for_records = [&](auto&& f) {
 #pragma unroll 1
     for (int i = 0; i < most_items; ++i) {
-      int n = 0, lo = 0;
+      int n = __float_as_int(__shfl_sync(0xffffffffu, info.x, i & (L - 1), L)), lo = 0;
       if (i < rec.items) {
-        const float4 info = rec.info[(size_t)i * rec.slots];
-        n = __float_as_int(info.x);
-        mag = info.z;
+        if (i >= L) n = __float_as_int(rec.info[(size_t)i * rec.slots].x);
         lo = rec.cut.begin(i);
+      } else {
+        n = 0;
       }
       const int most = __reduce_max_sync(0xffffffffu, n);
 #pragma unroll 1
@@ -382,7 +384,10 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_ke
     return m;
   };
   if constexpr (kMany) {
-    for (int i = 0; i < rec.items; ++i) floor_y = fmaxf(floor_y, rec.info[(size_t)i * rec.slots].y);
+    mag = __shfl_sync(0xffffffffu, info.z, 0, L);
+    floor_y = info.y;
+    for (int i = sl + L; i < rec.items; i += L) floor_y = fmaxf(floor_y, rec.info[(size_t)i * rec.slots].y);
+    floor_y = max_lanes<L>(floor_y);
   } else {
 #pragma unroll 4
     for (int i = 0; i < chunks; ++i) ymax = fmaxf(ymax, max4(maxima(i)));
@@ -954,8 +959,8 @@ int plan_paged(const entmax_attn_paged_cache* cache, const entmax_attn_paged_par
     l->many_blocks = fit < 1 ? 1 : fit < (size_t)a->many_blocks ? (int)fit : a->many_blocks;
     many_rows = per * l->many_blocks;
   }
-  // (runs of kLeastCut tiles at least, one per SM)
-  a->many_items = a->tiles / kLeastCut + 2;
+  // (one run per SM, of a tile at least)
+  a->many_items = a->tiles + 2;
   if (a->many_items > kMostSms + 1) a->many_items = kMostSms + 1;
 
   size_t off = 256;

@@ -15,6 +15,8 @@
 //         per 32 rows and key against 8 with a lane per key.
 #include <cuda.h>
 
+#include <atomic>
+
 #include "paged.cuh"
 #include "sm100_ptx.cuh"
 
@@ -492,6 +494,7 @@ __device__ __forceinline__ void keep_record_if_greater(float x, float thr, uint3
 // A lower bound of the threshold of a row from eight values of eight of its keys (-inf: none), y = z / margin: the threshold of those alone, by
 // three steps from the left, in z's units.  Rows with no more than two of them in the bracket have nothing to gain (-inf
 // is returned), nor is it worth the warp's time for less than eight rows.
+__device__ __forceinline__ float sqrt_fast(float x) { return x * rsqrtf(x); }
 template <int EC>
 __device__ __forceinline__ float eight_steps(const float (&y)[8], float expo) {
   float tau = -1.0f;                                           // relative to the largest
@@ -505,7 +508,9 @@ __device__ __forceinline__ float eight_steps(const float (&y)[8], float expo) {
       s0 += ye;
       s1 += ye1;
     }
-    if (s0 > 1.0f && s1 > 0.f) tau += threshold_step(s0, s1, EC, expo);
+    // threshold_step with the fast square root and quotients: a few ulp, well within the hair below
+    const float root = EC == kExpo1 ? s0 : EC == kExpo2 ? s0 * rsqrtf(s0) : EC == kExpo4 ? sqrt_fast(sqrt_fast(s0)) : __powf(s0, __fdividef(1.0f, expo));
+    if (s0 > 1.0f && s1 > 0.f) tau += __fdividef(s0 - __fdividef(s0, root), s1);
   }
   return tau;
 }
@@ -516,7 +521,7 @@ __device__ __forceinline__ float bound_from_eight(const float (&z)[8], float mar
   for (int q = 0; q < 8; ++q) n += z[q] > m - margin ? 1 : 0;
   if (expo < 1.0f || __popc(__ballot_sync(0xffffffffu, n > 2)) < 8) return -INFINITY;
   float y[8];
-  const float r = 1.0f / margin;
+  const float r = __fdividef(1.0f, margin);
 #pragma unroll
   for (int q = 0; q < 8; ++q) y[q] = (z[q] - m) * r;
   const float tau = expo_class == kExpo2 ? eight_steps<kExpo2>(y, expo)
@@ -918,8 +923,15 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
             for (int u = 0; u < 64; ++u) v[u] *= sign;
           }
           if (col0 + 63 > first_pos) {                         // some row of the tile does not see all of them
+            // (as bits: tested several at a time, where a comparison each is one more of the ALU's instructions per column)
+            const int seen = lim + 1 - col0;                   // columns that the row sees
+            const uint32_t lo = seen >= 32 ? 0xffffffffu : seen > 0 ? (1u << seen) - 1u : 0u;
+            const uint32_t hi = seen >= 64 ? 0xffffffffu : seen > 32 ? (1u << (seen - 32)) - 1u : 0u;
 #pragma unroll
-            for (int u = 0; u < 64; ++u) v[u] = col0 + u <= lim ? v[u] : -INFINITY;
+            for (int u = 0; u < 32; ++u) {
+              v[u] = (lo >> u) & 1u ? v[u] : -INFINITY;
+              v[32 + u] = (hi >> u) & 1u ? v[32 + u] : -INFINITY;
+            }
           }
         };
         // a stream that starts without a bound looks at its first tile twice
@@ -1010,6 +1022,19 @@ cudaError_t map_pages(CUtensorMap* map, const PagedArgs& a, const void* k) {
                       a.c.ps_shift < 7 ? 1 << a.c.ps_shift : 128, 1);
 }
 
+// Lets a kernel have its shared memory; once per device
+template <auto* kKernel>
+cudaError_t allow_smem(int bytes) {
+  static std::atomic<unsigned long long> allowed{0};
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0ull;
+  if (err != cudaSuccess || (allowed.load(std::memory_order_relaxed) & bit)) return err;
+  err = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (err == cudaSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+  return err;
+}
+
 template <int HD, int NR, bool kAlibi>
 cudaError_t launch_few(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int seq0, int seqs,
                        cudaStream_t stream) {
@@ -1018,7 +1043,7 @@ cudaError_t launch_few(const PagedArgs& a, const void* q, const void* k, int64_t
   static_assert(2 * (FewCfg<HD, NR>::kFixedBytes + (4 * kFewSeqs + 4) * 4 + 1024) <= 233472, "two CTAs per SM");
   cudaError_t err = map_queries(&map_q, a, q, q_st, q_sh, a.few_slots / a.G);
   if (err == cudaSuccess) err = map_pages(&map_k, a, k);
-  if (err == cudaSuccess) err = cudaFuncSetAttribute(paged_few_kernel<HD, NR, kAlibi>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (err == cudaSuccess) err = allow_smem<&paged_few_kernel<HD, NR, kAlibi>>(smem);
   if (err != cudaSuccess) return err;
   const int sms = a.sms;
   // no more CTAs than the longest lengths could keep busy
@@ -1032,8 +1057,7 @@ cudaError_t launch_many(const PagedArgs& a, const void* q, const void* k, int64_
   CUtensorMap map_q, map_k;
   cudaError_t err = map_queries(&map_q, a, q, q_st, q_sh, a.tile_tokens);
   if (err == cudaSuccess) err = map_pages(&map_k, a, k);
-  if (err == cudaSuccess)
-    err = cudaFuncSetAttribute(paged_many_kernel<HD, kAlibi>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<HD>::kSmemBytes);
+  if (err == cudaSuccess) err = allow_smem<&paged_many_kernel<HD, kAlibi>>(ManyCfg<HD>::kSmemBytes);
   if (err != cudaSuccess) return err;
   // (where units are cut every SM gets a run; otherwise there are more of them than SMs)
   return launch_kernel(paged_many_kernel<HD, kAlibi>, (unsigned)a.sms, kManyThreads, ManyCfg<HD>::kSmemBytes, stream, map_q, map_k, a, blocks);

@@ -51,7 +51,7 @@ def _run(pr, alpha, scale=None, slopes=None, **kw):
     return (*out, int(status[0]))
 
 
-def _check(pr, alpha, got, scale=None, slopes=None, skip=(), sm_scale=None):
+def _check(pr, alpha, got, scale=None, slopes=None, skip=(), sm_scale=None, heads=None, rows=None):
     o, tau, supp, flags = got
     assert flags == 0
     o, tau, supp = o.cpu().double(), tau.cpu().double(), supp.cpu()
@@ -59,16 +59,18 @@ def _check(pr, alpha, got, scale=None, slopes=None, skip=(), sm_scale=None):
     q = pr["q"].cpu()
     t = 0
     for b, (n, L) in enumerate(zip(pr["new"], pr["kv"])):
-        for h in range(pr["H"]) if n and b not in skip else ():
+        for h in (heads or range(pr["H"])) if n and b not in skip else ():
             sc = None if scale is None else [s[h] for s in scale]
             m = 0.0 if slopes is None else slopes[h]
-            ro, rt, to, tt, lo, hi = paged.attend(q[t:t + n, h], pr["keys"][b][:, h // R], pr["values"][b][:, h // R], L - n, alpha, sc, m,
-                                                  sm_scale)
-            et, eo = (tau[t:t + n, h] - rt).abs() / tt, (o[t:t + n, h] - ro).abs() / to
-            assert float(et.max()) <= 1.0, ("tau", b, h, int(et.argmax()), float(et.max()))
-            assert float(eo.max()) <= 1.0, ("o", b, h, int(eo.max(1)[0].argmax()), float(eo.max()))
-            s = supp[t:t + n, h]
-            assert bool(((s >= lo) & (s <= hi)).all()), ("support", b, h)
+            for i in ([slice(0, n)] if rows is None else [slice(r, r + 1) for r in rows if r < n]):
+                at = slice(t + i.start, t + i.stop)
+                ro, rt, to, tt, lo, hi = paged.attend(q[at, h], pr["keys"][b][:, h // R], pr["values"][b][:, h // R], L - n + i.start, alpha, sc,
+                                                      m, sm_scale)
+                et, eo = (tau[at, h] - rt).abs() / tt, (o[at, h] - ro).abs() / to
+                assert float(et.max()) <= 1.0, ("tau", b, h, i, int(et.argmax()), float(et.max()))
+                assert float(eo.max()) <= 1.0, ("o", b, h, i, int(eo.max(1)[0].argmax()), float(eo.max()))
+                s = supp[at, h]
+                assert bool(((s >= lo) & (s <= hi)).all()), ("support", b, h, i)
         t += n
 
 
@@ -208,6 +210,87 @@ def test_pages_outside_the_pool(new):
         assert torch.equal(o[new[0]:], good[0][new[0]:]) and torch.equal(tau[new[0]:], good[1][new[0]:])
 
 
+@pytest.mark.parametrize("new,max_q,max_kv,bad", [([2, 7, 1], 4, 0, 1), ([1, 1, 1], 0, 60, 0), ([70, 20, 90], 80, 0, 2)])
+def test_bounds_that_are_too_small(new, max_q, max_kv, bad):
+    lens = [100, 50, 95]
+    pr = _problem(new, lens, 4, 2, 64, 16)
+    o, tau, supp, flags = _run(pr, 1.5, max_q_len=max_q, max_kv_len=max_kv)
+    assert flags == binding.FLAG_BAD_LENGTH
+    left_out = [bad] if max_q else [b for b in range(3) if lens[b] > max_kv]
+    for b in left_out:
+        a, e = sum(new[:b]), sum(new[:b + 1])
+        assert bool((o[a:e] == 0).all() and torch.isneginf(tau[a:e]).all() and (supp[a:e] == 0).all())
+    _check(pr, 1.5, (o, tau, supp, 0), skip=left_out)
+
+
+def test_large_batches():
+    # more sequences than a launch for few rows takes, some idle, some with a few tokens; then enough blocks that none is cut
+    g = np.random.default_rng(0)
+    lens = [int(n) for n in g.integers(1, 90, 600)]
+    new = [min(n, int(m)) for n, m in zip(lens, g.integers(0, 4, 600))]
+    pr = _problem(new, lens, 4, 2, 64, 16)
+    sc = _scales(4, 2, "length")
+    _check(pr, 1.5, _run(pr, 1.5, sc, max_q_len=3, max_kv_len=90), sc, skip=range(0, 600, 3))
+    _check(pr, 1.5, _run(pr, 1.5, sc), sc, skip=[b for b in range(600) if b % 7])
+    lens = [int(n) for n in g.integers(40, 700, 60)]
+    new = [min(n, int(m)) for n, m in zip(lens, g.integers(33, 60, 60))]
+    pr = _problem(new, lens, 8, 8, 64, 16)
+    sc = _scales(8, 2, "length")
+    _check(pr, 1.5, _run(pr, 1.5, sc), sc, heads=[0, 3, 7], skip=range(1, 60, 4))
+
+
+@pytest.mark.parametrize("n", [1, 5, 40])
+def test_uniform_chunks_without_offsets(n):
+    lens = [41, 300, 64]
+    pr = _problem([n] * 3, lens, 4, 2, 64, 16)
+    _check(pr, 1.5, _run(pr, 1.5, cu=None))
+
+
+@pytest.mark.parametrize("new,H,KH,sigma", [(1, 16, 2, 1.0), (40, 1, 1, 1.0), (1, 4, 1, 0.05), (20, 2, 1, 0.05)])
+def test_long_contexts(new, H, KH, sigma):
+    # rows of 2200 groups; a unit cut into more work items than a row's lanes
+    pr = _problem([new], [70001], H, KH, 64, 64, sigma=sigma, plant=sigma == 1.0)
+    sc = _scales(H, 5, "length") if sigma == 1.0 else None
+    _check(pr, 1.5, _run(pr, 1.5, sc), sc, heads=[0, H - 1], rows=[0, new // 2, new - 1])
+
+
+@pytest.mark.parametrize("new,lens,H,KH,alpha", [([400, 390], [2600, 400], 8, 2, 1.5), ([1] * 50, [2000 - 7 * b for b in range(50)], 32, 4, 1.25)])
+def test_more_rows_with_long_supports_than_lists_hold(new, lens, H, KH, alpha):
+    # enough rows for the kernels with many rows to a CTA, each with hundreds of keys or all of them in its support
+    pr = _problem(new, lens, H, KH, 64, 32, sigma=0.3, plant=False)
+    pr["q"][::2] = 0
+    _check(pr, alpha, _run(pr, alpha), heads=[0, H - 1], skip=range(3, len(new), 5), rows=[0, 1, 170, 389])
+
+
+def test_two_calls_at_once():
+    a = _problem([1] * 40, [600 + b for b in range(40)], 8, 2, 64, 16, seed=1)
+    b = _problem([300, 1], [900, 77], 8, 2, 64, 16, seed=2)
+    want = [binding.entmax_attn_paged_fwd(p["q"], p["kc"], p["vc"], 1.5, p["table"], p["lens"], p["cu"])[:2] for p in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = []
+        for p, st in zip((a, b), streams):
+            with torch.cuda.stream(st):
+                got.append(binding.entmax_attn_paged_fwd(p["q"], p["kc"], p["vc"], 1.5, p["table"], p["lens"], p["cu"])[:2])
+        torch.cuda.synchronize()
+        for w, x in zip(want, got):
+            assert torch.equal(w[0], x[0]) and torch.equal(w[1], x[1])
+
+
+@pytest.mark.parametrize("kind", ["zero", "negative", "nan"])
+def test_scales_without_an_order(kind):
+    # c = 0: every key alike; c < 0: the smallest products win; c not finite: reported, rows finite or not but the call ends
+    for new, lens in (([1, 3], [200, 50]), ([90, 1], [200, 50])):
+        pr = _problem(new, lens, 4, 2, 64, 16)
+        sc = [torch.full((4,), x) for x in {"zero": (0.0, 1.0, 0.0), "negative": (-0.5, 1.0, -1.0), "nan": (1.0, 1.0, float("nan"))}[kind]]
+        got = _run(pr, 1.5, sc)
+        if kind == "nan":
+            assert got[3] == binding.FLAG_BAD_SCALE
+        else:
+            _check(pr, 1.5, got, sc)
+
+
 def test_offsets_beyond_32_bits():
     # a pool of more than 2^32 bytes, the sequence's pages at its end
     d, KH, page = 128, 2, 256
@@ -304,6 +387,7 @@ def _check_append(qkv, H, KH, new, lens, page, rotation, interleaved, before, af
     ([1, 0, 37, 5], [17, 40, 37, 129], 6, 2, 128, 32, "heads"),
     ([130, 1], [200, 256], 32, 8, 128, 64, "fused"),
     ([3], [3], 1, 1, 64, 16, "tokens"),
+    ([b % 3 for b in range(700)], [b % 3 + 5 * (b % 50) + 1 for b in range(700)], 2, 1, 64, 16, "tokens"),
 ])
 def test_append(rot, interleaved, new, lens, H, KH, d, page, layout):
     qkv, kc, vc, table, cu, kv_len = _append_problem(new, lens, H, KH, d, page, layout=layout)
