@@ -394,8 +394,50 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_ke
     ymax = max_lanes<L>(ymax);
     floor_y = ymax - 1.0f;
   }
+  // over: rows to raise the bound of.  Where groups are looked at, their number tells before anything is collected.
+  bool over = false;
+  if constexpr (!kMany) {
+    int n = 0;
 #pragma unroll 1
-  for (int attempt = 0;; ++attempt) {
+    for (int i = 0; i < chunks; ++i) {
+      const float4 m = maxima(i);
+      n += (m.x > floor_y ? 1 : 0) + (m.y > floor_y ? 1 : 0) + (m.z > floor_y ? 1 : 0) + (m.w > floor_y ? 1 : 0);
+    }
+    over = sum_lanes<L>((float)n) > (float)(S::kList / 4);
+  }
+#pragma unroll 1
+  for (int attempt = 0; attempt < 3; ++attempt) {
+    if (a.expo >= 1.0f && __any_sync(0xffffffffu, over)) {
+      float tau = fmaxf(floor_y, ymax - 1.0f);
+#pragma unroll 1
+      for (int it = 0; it < kBoundSteps; ++it) {
+        float s0 = 0.f, s1 = 0.f;
+        auto add = [&](float m) {
+          float ye, ye1;
+          powers<EC>(fmaxf(m - tau, 0.f), a.expo, ye, ye1);
+          s0 += ye;
+          s1 += ye1;
+        };
+        if constexpr (kMany) {
+          for_records([&](const float4& y, int) { add(max4(y)); });
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < chunks; ++i) {
+            const float4 m = maxima(i);
+            add(m.x);
+            add(m.y);
+            add(m.z);
+            add(m.w);
+          }
+        }
+        s0 = sum_lanes<L>(s0);
+        s1 = sum_lanes<L>(s1);
+        const bool go = s0 > 1.01f && s1 > 0.f;
+        if (go) tau += threshold_step(s0, s1, EC, a.expo);
+        if (!__any_sync(0xffffffffu, go && over)) break;
+      }
+      if (over) floor_y = fmaxf(floor_y, fmaxf(ymax - 1.0f, bound_below(tau)));
+    }
     cnt = 0;
     if constexpr (kMany) {
       for_records([&](const float4& y, int key) {
@@ -434,37 +476,10 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_ke
         }
       }
     }
-    const bool over = cnt > S::kList;
-    if (attempt == 1 || a.expo < 1.0f || !__any_sync(0xffffffffu, over)) break;
-    float tau = fmaxf(floor_y, ymax - 1.0f);
-#pragma unroll 1
-    for (int it = 0; it < kBoundSteps; ++it) {
-      float s0 = 0.f, s1 = 0.f;
-      auto add = [&](float m) {
-        float ye, ye1;
-        powers<EC>(fmaxf(m - tau, 0.f), a.expo, ye, ye1);
-        s0 += ye;
-        s1 += ye1;
-      };
-      if constexpr (kMany) {
-        for_records([&](const float4& y, int) { add(max4(y)); });
-      } else {
-#pragma unroll 1
-        for (int i = 0; i < chunks; ++i) {
-          const float4 m = maxima(i);
-          add(m.x);
-          add(m.y);
-          add(m.z);
-          add(m.w);
-        }
-      }
-      s0 = sum_lanes<L>(s0);
-      s1 = sum_lanes<L>(s1);
-      const bool go = s0 > 1.01f && s1 > 0.f;
-      if (go) tau += threshold_step(s0, s1, EC, a.expo);
-      if (!__any_sync(0xffffffffu, go && over)) break;
-    }
-    if (over) floor_y = fmaxf(floor_y, fmaxf(ymax - 1.0f, bound_below(tau)));
+    // (once more, if that was without a raised bound)
+    const bool tried = over;
+    over = cnt > S::kList;
+    if (a.expo < 1.0f || !__any_sync(0xffffffffu, over && !tried)) break;
   }
   if (live && cnt > S::kList) {
     if (sl == 0) a.spilled[atomicAdd(a.counters + kSpilledRows, 1)] = (int)row;
@@ -556,7 +571,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_ke
 // ================================================================================================== row
 constexpr int kCtaWarps = 8;
 constexpr int kSeg = 256;            // list entries of a warp
-constexpr int kRowsWorth = 1184, kRows8Worth = 9472;   // rows from which on a warp to a row, and eight lanes, fill the machine
+constexpr int kCtaRows = 2 * 148, kLongRow = 16384, kRows8Worth = 9472;   // (see solve_lanes)
 constexpr int kChunks = 8;           // chunks of 32 groups of a warp whose maxima stay in shared memory
 
 // kSpilled: the rows listed by the rows kernel, by CTAs that stay; otherwise a CTA for each of the n_slots row slots
@@ -834,9 +849,11 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
   }
 }
 
-// Lanes of a row in the solve of a launch; 0: a CTA
+// Lanes of a row in the solve of a launch; 0: a CTA.  A CTA per row where all fit the machine at once (two to an SM), and for up to three rounds of
+// long rows: 256 rows of 65536 keys 17 us against 25 with a warp each, 320 of 48222 26 against 51, 1120 of 45231 69 against 52, 640 of
+// 4096 23 against 13.  Eight lanes where there are more rows than warps to keep (37000 rows of chunks 18 us against 39 with a warp each).
 int solve_lanes(const PagedArgs& a, bool many, long long rows) {
-  if (rows < kRowsWorth || a.max_kv > (many ? 1 << 20 : 32768)) return 0;
+  if (rows <= kCtaRows || (rows <= 3 * kCtaRows && a.max_kv > kLongRow) || a.max_kv > 1 << 20) return 0;
   return rows < kRows8Worth ? 32 : 8;
 }
 
