@@ -24,7 +24,8 @@
  *     memory, never synchronises the device or a stream, and enqueues all work in the order of
  *     `cuda_stream` (a cudaStream_t passed as void*; NULL = the legacy default stream).  The backward
  *     calls clear their accumulators on a stream of the library's own that is forked from and joined
- *     back to `cuda_stream` with events inside the call: the caller sees plain stream order.
+ *     back to `cuda_stream` with events inside the call, and entmax_attn_paged_fwd runs short and long
+ *     chunks side by side that way: the caller sees plain stream order.
  *   - Q, K, V, O, dO, dQ, dK, dV share one layout: [batch, heads, seq, head_dim] with head_dim
  *     innermost and contiguous; the other three strides come from the params struct (in elements).
  *     tau is [batch, heads, seq] float32, contiguous.  beta, gamma, delta are [heads] float32.
@@ -357,7 +358,9 @@ int entmax_attn_paged_append(const entmax_attn_paged_cache* cache, const entmax_
  *   tau           out, device float32 [total_q, q_heads]
  *   support_size  out, device int32 [total_q, q_heads] or NULL: number of keys with p > 0
  *   max_q_len, max_kv_len   the most new tokens and the longest kv_len of any sequence of the call (0: not known).  They size the workspace and
- *                 the launches; a sequence beyond them is left out (ENTMAX_ATTN_FLAG_BAD_LENGTH)
+ *                 the launches; a sequence beyond them is left out (ENTMAX_ATTN_FLAG_BAD_LENGTH).  The workspace has room for the scores
+ *                 of the rows worked on at a time, max_kv_len floats each: up to about 5 GiB, or, where those are more, one sequence's
+ *                 or one block's (128 to 256 rows of each K/V head)
  *   workspace     device scratch, 256-byte aligned, >= entmax_attn_paged_workspace_bytes(cache, params, cu_q == NULL) bytes
  * The rows of a sequence that is left out get O = 0, tau = -inf, support size 0.  K is read once per K/V head (chunks: once
  * per 256 rows of a head's group), V only on the support.  Results are bitwise reproducible, and slots past a sequence's length may hold anything.

@@ -62,6 +62,13 @@ WsLayout make_layout(const Problem& p, bool is_bwd);
 int make_problem(const entmax_attn_params* params, Problem* out);
 int check_scale_ptrs(const float* beta, const float* gamma, const float* delta, Problem* p);
 int fail_cuda(cudaError_t err);
+// A second stream of the calling thread on the current device, with the events it is forked from and joined back to a caller's stream by
+struct SideStream {
+  cudaStream_t stream = nullptr;
+  cudaEvent_t fork = nullptr, join = nullptr;
+};
+cudaError_t side_stream(SideStream** out);
+bool side_stream_made();   // whether the thread has it already on this device
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // y^e and y^(e-1) of a clamped y >= 0 (0 where the entry is outside the support: ok == false), with the

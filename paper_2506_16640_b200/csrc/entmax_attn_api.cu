@@ -15,38 +15,6 @@ thread_local cudaEvent_t g_prof_stop[2] = {nullptr, nullptr};
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-// A second stream per (host thread, device) on which the backward call clears its fp32 accumulators while the
-// score sweep, which does not touch them, runs on the caller's stream: forked from and joined back to the
-// caller's stream with events, so the caller sees ordinary stream order (and a stream capture stays one graph).
-struct SideStream {
-  cudaStream_t stream = nullptr;
-  cudaEvent_t fork = nullptr, join = nullptr;
-};
-thread_local SideStream g_side[64];
-
-cudaError_t side_stream(SideStream** out) {
-  int dev = 0;
-  cudaError_t err = cudaGetDevice(&dev);
-  if (err != cudaSuccess) return err;
-  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  SideStream& s = g_side[dev];
-  if (!s.stream) {
-    cudaStream_t st = nullptr;
-    cudaEvent_t e0 = nullptr, e1 = nullptr;
-    err = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
-    if (err == cudaSuccess) err = cudaEventCreateWithFlags(&e0, cudaEventDisableTiming);
-    if (err == cudaSuccess) err = cudaEventCreateWithFlags(&e1, cudaEventDisableTiming);
-    if (err != cudaSuccess) {
-      if (e0) cudaEventDestroy(e0);
-      if (st) cudaStreamDestroy(st);
-      return err;
-    }
-    s.stream = st; s.fork = e0; s.join = e1;
-  }
-  *out = &s;
-  return cudaSuccess;
-}
-
 struct SavedLayout {
   size_t counts, entries, total;
 };
@@ -75,6 +43,42 @@ int check_device_for_bf16() {
 }
 
 }  // namespace
+
+// A second stream per (host thread, device) on which the backward call clears its fp32 accumulators while the
+// score sweep, which does not touch them, runs on the caller's stream: forked from and joined back to the
+// caller's stream with events, so the caller sees ordinary stream order (and a stream capture stays one graph).  The paged
+// attention call runs its two kinds of sequences side by side the same way.
+namespace {
+thread_local SideStream g_side[64];
+}  // namespace
+
+cudaError_t side_stream(SideStream** out) {
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  SideStream& s = g_side[dev];
+  if (!s.stream) {
+    cudaStream_t st = nullptr;
+    cudaEvent_t e0 = nullptr, e1 = nullptr;
+    err = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
+    if (err == cudaSuccess) err = cudaEventCreateWithFlags(&e0, cudaEventDisableTiming);
+    if (err == cudaSuccess) err = cudaEventCreateWithFlags(&e1, cudaEventDisableTiming);
+    if (err != cudaSuccess) {
+      if (e0) cudaEventDestroy(e0);
+      if (st) cudaStreamDestroy(st);
+      return err;
+    }
+    s.stream = st; s.fork = e0; s.join = e1;
+  }
+  *out = &s;
+  return cudaSuccess;
+}
+
+bool side_stream_made() {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64 && g_side[dev].stream != nullptr;
+}
 
 int fail_cuda(cudaError_t err) {
   g_last_cuda_error = (int)err;

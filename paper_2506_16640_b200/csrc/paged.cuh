@@ -70,7 +70,7 @@ int check_paged_cache(const entmax_attn_paged_cache* cache, int total_q, PagedCa
 //       group_max[row][group]         the maximum over each group of 32 keys (-inf: none visible)
 //       scores[row][key]              the scores of the groups whose maximum is above a bound of y_max - 1; other groups are not written
 //                                     (some may be)
-//   "many": a unit is a block of kManyTiles * tile_tokens tokens of a longer chunk; where there are few units, their K tiles are shared among
+//   "many": a unit is a block of kManyTiles * tile_tokens tokens of a longer chunk; where units are few or uneven, their K tiles are shared among
 //       several work items (ManyCut).  The item whose first K tile is lo keeps records of eight neighbouring keys, those with a value above
 //       the bound it had then, in key order:
 //       scores[row][256 lo + 8 i ..]  the values, before the scaling by |a|      record_key[row][32 lo + i]  the first key
@@ -79,6 +79,7 @@ int check_paged_cache(const entmax_attn_paged_cache* cache, int total_q, PagedCa
 constexpr int kGroupKeys = 32;
 constexpr int kManyKeys = 256;
 constexpr int kManyTiles = 2;
+constexpr int kMostSms = 160;       // (sizes the workspace, which is the same on every device)
 constexpr int kFewSeqs = 256;   // sequences a launch of the "few" kernel takes
 
 struct PagedArgs {
@@ -129,9 +130,9 @@ struct __align__(16) PagedBlock {
   int len, tiles, start, pad; // length; tiles of 256 keys that the block's last row sees; those of the blocks before it
 };
 
-// How a unit's K tiles are shared among work items.  With units enough for every SM to take several, each is one item (cut = 0).  Otherwise the
+// How a unit's K tiles are shared among work items.  Where the units can be dealt to the CTAs evenly, each is one item (cut = 0).  Otherwise the
 // tiles of all units, head by head and block by block, are dealt to the CTAs in runs of `cut`, and a unit's items are its shares in the runs
-// it lies in.
+// it lies in (each starts without a bound).  The rule is the plan kernel's.
 struct ManyCut {
   int start, tiles, cut;      // start: the unit's first tile in that order
   __device__ __forceinline__ int items() const { return cut ? (start + tiles - 1) / cut - start / cut + 1 : 1; }
@@ -139,6 +140,8 @@ struct ManyCut {
     return item == 0 ? 0 : cut ? min((start / cut + item) * cut - start, tiles) : tiles;
   }
 };
+// Uncut units: the item, in the order of length, that a CTA takes in a round (every other round backwards)
+__device__ __forceinline__ int many_dealt(int round, int cta, int ctas) { return round * ctas + ((round & 1) ? ctas - 1 - cta : cta); }
 __device__ __forceinline__ ManyCut many_cut(const int32_t* counters, const PagedBlock& pb, int kv_head) {
   return ManyCut{kv_head * counters[kTiles] + pb.start, pb.tiles, counters[kCut]};
 }
@@ -183,7 +186,7 @@ __device__ __forceinline__ void write_unserved(const PagedArgs& a, const PagedSe
 
 cudaError_t launch_paged_few(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int seq0, int seqs,
                              cudaStream_t stream);
-// (after launch_paged_plan for the same blocks)
+// (behind the plan kernel for the same blocks)
 cudaError_t launch_paged_many(const PagedArgs& a, const void* q, const void* k, int64_t q_st, int64_t q_sh, int blocks,
                               cudaStream_t stream);
 

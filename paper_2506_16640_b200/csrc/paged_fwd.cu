@@ -133,7 +133,8 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
   pdl_begin();
   __shared__ int bin[kPlanThreads];               // blocks of a class, then the next place of the class
   __shared__ int warp_sum[kPlanThreads / 32];
-  __shared__ int n_blocks;
+  __shared__ int n_blocks, longest;
+  __shared__ int load[256];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int tokens = kManyTiles * a.tile_tokens;
   if (blockIdx.x > 0) {
@@ -147,6 +148,8 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
     return;
   }
   bin[tid] = 0;
+  if (tid < 256) load[tid] = 0;
+  if (tid == 0) longest = 0;
   if (tid <= kSpilledRows) a.counters[tid] = 0;
   __syncthreads();
   auto class_of = [&](int tiles) { return kPlanThreads - 1 - (int)((long long)(tiles - 1) * kPlanThreads / a.tiles); };
@@ -203,6 +206,9 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
   int before = 0;
   for (int i = 0; i < warp; ++i) before += warp_sum[i];
   bin[tid] = before + incl - mine;
+  // (a class of several lengths counts as its longest)
+  auto class_tiles = [&](int cls) { return (int)(((long long)(kPlanThreads - cls) * a.tiles + kPlanThreads - 1) / kPlanThreads); };
+  if (mine > 0 && bin[tid] == 0) longest = class_tiles(tid);
   if (tid == kPlanThreads - 1) {
     n_blocks = before + incl;
     a.counters[kBlocks] = n_blocks;
@@ -227,11 +233,35 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
     }
     if (i < blocks) a.blocks[i].start = at + upto - tiles;
   }
+  // Units are cut where the longest walk of a CTA that deals them whole passes the mean by 12 tiles: that is about what the new starts cost.
+  // (scores and solves, uncut against cut: two prompts of up to 4096 tokens, 3 tiles: 103 against 118 us; 16 sequences, four with chunks of
+  // up to 1000 tokens, 9: 118 against 134; a chunk of 1024 over 30000 keys, 32 heads, 16: 279 against 268; of 2048 over 32768, 16 heads, 20:
+  // 266 against 246; three sequences, one with a chunk of 500 over 9001 keys, 27: 104 against 75)
+  const int all = carry * a.c.KH;                           // (scores are held for all of them at once, so it fits)
+  auto even = [&]() { return (longest - 12) * a.sms <= all; };
+  if (even()) {
+    // nor does the longest unit by itself: each CTA's walk, in the order that the many kernel deals units (item k's class is the last one with
+    // no more than k / KH blocks before it)
+    // (few instructions and no divisions: they come from memory each time.  The first version of this loop cost 4 us.)
+    const int items = n_blocks * a.c.KH, cta = tid & 255;
+    int sum = 0;
+#pragma unroll 1
+    for (int round = tid >> 8; round * a.sms < items; round += kPlanThreads / 256) {
+      const int k = many_dealt(round, cta, a.sms);
+      if (cta >= a.sms || k >= items) continue;
+      int cls = 0;
+#pragma unroll 1
+      for (int half = kPlanThreads / 2; half > 0; half /= 2)
+        if (bin[cls + half] * a.c.KH <= k) cls += half;
+      sum += class_tiles(cls);
+    }
+    sum = atomicAdd(&load[cta], sum) + sum;                 // (the last of a CTA's threads sees the whole)
+    atomicMax(&longest, sum);
+    __syncthreads();
+  }
   if (tid == 0) {
     a.counters[kTiles] = carry;
-    // units for less than three rounds of the machine are cut
-    const long long all = (long long)carry * a.c.KH;
-    a.counters[kCut] = n_blocks * a.c.KH >= 3 * a.sms ? 0 : (int)((all + a.sms - 1) / a.sms);
+    a.counters[kCut] = even() ? 0 : (all + a.sms - 1) / a.sms;
   }
   for (int i = tid; i < blocks; i += kPlanThreads) {
     const PagedBlock pb = a.blocks[i];
@@ -852,7 +882,7 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
 // Lanes of a row in the solve of a launch; 0: a CTA.  A CTA per row where all fit the machine at once (two to an SM), and for up to three rounds of
 // long rows: 256 rows of 65536 keys 17 us against 25 with a warp each, 320 of 48222 26 against 51, 1120 of 45231 69 against 52, 640 of
 // 4096 23 against 13.  Eight lanes where there are more rows than warps to keep (37000 rows of chunks 18 us against 39 with a warp each).
-int solve_lanes(const PagedArgs& a, bool many, long long rows) {
+int solve_lanes(const PagedArgs& a, long long rows) {
   if (rows <= kCtaRows || (rows <= 3 * kCtaRows && a.max_kv > kLongRow) || a.max_kv > 1 << 20) return 0;
   return rows < kRows8Worth ? 32 : 8;
 }
@@ -877,7 +907,7 @@ cudaError_t launch_rows(const PagedArgs& a, const __nv_bfloat16* v, int first, i
 
 template <int D, bool kMany>
 cudaError_t launch_solve_d(const PagedArgs& a, const __nv_bfloat16* v, int first, int units, cudaStream_t stream) {
-  const int rows = units * (kMany ? a.many_slots : a.few_slots), lanes = solve_lanes(a, kMany, rows);
+  const int rows = units * (kMany ? a.many_slots : a.few_slots), lanes = solve_lanes(a, rows);
   if (lanes == 0) return launch_kernel(paged_row_kernel<D, kMany, false>, (unsigned)rows, 32 * kCtaWarps, 0, stream, a, v, first, rows);
   return lanes == 8 ? launch_rows<D, kMany, 8>(a, v, first, units, stream) : launch_rows<D, kMany, 32>(a, v, first, units, stream);
 }
@@ -889,10 +919,11 @@ cudaError_t launch_solve(const PagedArgs& a, const void* v, int first, int units
 }
 
 // ------------------------------------------------------------------------------------------------ host
-constexpr size_t kSliceBytes = (size_t)4 << 30;     // scores held at a time (at least one sequence's or block's)
-constexpr int kFewRows = 32;
-constexpr int kFewWorth = 8;
-constexpr int kMostSms = 160;        // (sizes the workspace, which is the same on every device)
+// Scores held at a time (at least one sequence's or block's): launches are milliseconds long there, so that slices cost nothing and a workspace
+// stays what a server can spare.
+constexpr size_t kSliceBytes = (size_t)4 << 30;
+constexpr int kFewRows = 32;         // most rows of the few kernel's MMA
+constexpr int kFewWorth = 8;         // (see plan_paged)
 
 // The current device's compute capability (major) and SMs, looked up once per device
 cudaError_t device_facts(int* major, int* sms) {
@@ -919,6 +950,8 @@ struct PagedPlan {
   int few_seqs;          // sequences to a slice of the "few" kernel (at most kFewSeqs)
   int many_blocks;       // blocks to a slice of the "many" kernel
   bool few, many;
+  bool both;             // the two side by side, each with buffers of its own
+  size_t few_scores, few_spilled;
 };
 
 int plan_paged(const entmax_attn_paged_cache* cache, const entmax_attn_paged_params* p, bool uniform, PagedArgs* a, PagedPlan* l) {
@@ -951,7 +984,9 @@ int plan_paged(const entmax_attn_paged_cache* cache, const entmax_attn_paged_par
   // few: rows of a sequence's unit; many: the rest
   a->few_rows = (long long)a->max_q * a->G <= 16 ? 16 : a->G <= kFewRows ? kFewRows : 0;
   if (uniform && (long long)(a->c.T / a->c.B) * a->G > a->few_rows) a->few_rows = 0;
-  // where longer chunks are possible anyway, the single tokens of a handful of sequences are not worth a pair of launches of their own
+  // Where longer chunks are possible anyway, the single tokens of a handful of sequences are not worth launches of their own.  (taken along by
+  // the many kernel against a few kernel beside it, contexts up to 9001: 4 sequences, one of them a chunk of 100, 73 us and 73; 8, two
+  // chunks of 500, 79 and 78; 8 with contexts of 30001 124 and 131; 16, four chunks of 1000, 137 and 134; 24, two chunks of 500, 93 and 81)
   if (a->c.B <= kFewWorth && (long long)a->max_q * a->G > a->few_rows) a->few_rows = 0;
   l->few = a->few_rows > 0;
   const int few_tokens = l->few ? (a->max_q < a->few_rows / a->G ? a->max_q : a->few_rows / a->G) : 0;
@@ -989,7 +1024,16 @@ int plan_paged(const entmax_attn_paged_cache* cache, const entmax_attn_paged_par
   l->record_key = take(many_rows * a->tiles * 32);
   l->row_info = take(4 * many_rows * a->many_items);
   l->row_scale = take(l->many ? (size_t)a->c.T * a->H : 0);
-  l->scores = take((rows > many_rows ? rows : many_rows) * a->score_stride);
+  // A call with both kinds of sequences and room for all of each runs them side by side (24 sequences, two of them with chunks: 92 us one
+  // after the other, 76 now); otherwise they take turns with the same buffers
+  l->both = l->few && l->many && l->few_seqs == a->c.B && l->many_blocks == a->many_blocks &&
+            (rows + many_rows) * row_bytes <= kSliceBytes;
+  l->few_scores = l->scores = take((l->both || rows < many_rows ? many_rows : rows) * a->score_stride);
+  l->few_spilled = l->spilled;
+  if (l->both) {
+    l->few_scores = take(rows * a->score_stride);
+    l->few_spilled = take(rows);
+  }
   l->total = off;
   return ENTMAX_ATTN_OK;
 }
@@ -1054,18 +1098,42 @@ extern "C" int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const
     err = cudaMemsetAsync(device_status, 0, sizeof(int32_t) * ENTMAX_ATTN_STATUS_WORDS, stream);
     if (err != cudaSuccess) return fail_cuda(err);
   }
-  for (int b = 0; l.few && b < a.c.B && err == cudaSuccess; b += l.few_seqs) {
-    const int n = a.c.B - b < l.few_seqs ? a.c.B - b : l.few_seqs;
-    if (solve_lanes(a, false, (long long)n * a.c.KH * a.few_slots) != 0) err = cudaMemsetAsync(a.counters, 0, kCounters * sizeof(int32_t), stream);
-    if (err == cudaSuccess) err = launch_paged_few(a, q, k_cache, params->q_stride_t, params->q_stride_h, b, n, stream);
-    if (err == cudaSuccess) err = launch_solve<false>(a, v_cache, b, n * a.c.KH, stream);
-  }
-  for (int blk = 0; l.many && blk < a.many_blocks && err == cudaSuccess; blk += l.many_blocks) {
-    const int n = a.many_blocks - blk < l.many_blocks ? a.many_blocks - blk : l.many_blocks;
+  auto run_few = [&](PagedArgs f, int b, int n, cudaStream_t st) {
+    f.scores = reinterpret_cast<float*>(ws + l.few_scores);
+    f.spilled = reinterpret_cast<int32_t*>(ws + l.few_spilled);
+    f.counters = a.counters + kCounters;
+    cudaError_t e = cudaSuccess;
+    if (solve_lanes(f, (long long)n * f.c.KH * f.few_slots) != 0) e = cudaMemsetAsync(f.counters, 0, kCounters * sizeof(int32_t), st);
+    if (e == cudaSuccess) e = launch_paged_few(f, q, k_cache, params->q_stride_t, params->q_stride_h, b, n, st);
+    return e == cudaSuccess ? launch_solve<false>(f, v_cache, b, n * f.c.KH, st) : e;
+  };
+  auto run_many = [&](int blk, int n) {
     const int scale_ctas = (a.c.T + kPlanThreads / 32 - 1) / (kPlanThreads / 32);
-    err = launch_kernel(paged_plan_kernel, 1 + (scale_ctas < a.sms - 1 ? scale_ctas : a.sms - 1), kPlanThreads, 0, stream, a, blk, n);
-    if (err == cudaSuccess) err = launch_paged_many(a, q, k_cache, params->q_stride_t, params->q_stride_h, n, stream);
-    if (err == cudaSuccess) err = launch_solve<true>(a, v_cache, 0, n * a.c.KH, stream);
+    cudaError_t e = launch_kernel(paged_plan_kernel, 1 + (scale_ctas < a.sms - 1 ? scale_ctas : a.sms - 1), kPlanThreads, 0, stream, a, blk, n);
+    if (e == cudaSuccess) e = launch_paged_many(a, q, k_cache, params->q_stride_t, params->q_stride_h, n, stream);
+    return e == cudaSuccess ? launch_solve<true>(a, v_cache, 0, n * a.c.KH, stream) : e;
+  };
+  // (no stream is made while one is being captured: such a first call goes one after the other)
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  const bool fork = l.both && (side_stream_made() || (cudaStreamIsCapturing(stream, &capture) == cudaSuccess &&
+                                                      capture == cudaStreamCaptureStatusNone));
+  if (fork) {
+    SideStream* side = nullptr;
+    err = side_stream(&side);
+    if (err == cudaSuccess) err = cudaEventRecord(side->fork, stream);
+    if (err == cudaSuccess) err = cudaStreamWaitEvent(side->stream, side->fork, 0);
+    if (err != cudaSuccess) return fail_cuda(err);
+    err = run_few(a, 0, a.c.B, side->stream);
+    if (err == cudaSuccess) err = run_many(0, a.many_blocks);
+    // (joined whatever happened: a capture must not end with the other stream still forked)
+    cudaError_t join = cudaEventRecord(side->join, side->stream);
+    if (join == cudaSuccess) join = cudaStreamWaitEvent(stream, side->join, 0);
+    if (err == cudaSuccess) err = join;
+  } else {
+    for (int b = 0; l.few && b < a.c.B && err == cudaSuccess; b += l.few_seqs)
+      err = run_few(a, b, a.c.B - b < l.few_seqs ? a.c.B - b : l.few_seqs, stream);
+    for (int blk = 0; l.many && blk < a.many_blocks && err == cudaSuccess; blk += l.many_blocks)
+      err = run_many(blk, a.many_blocks - blk < l.many_blocks ? a.many_blocks - blk : l.many_blocks);
   }
   if (err == cudaSuccess) err = cudaGetLastError();
   return err == cudaSuccess ? ENTMAX_ATTN_OK : fail_cuda(err);

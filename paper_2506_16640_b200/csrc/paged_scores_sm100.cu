@@ -777,9 +777,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       it.b = -1;
       it.lo = it.hi = it.len = 0;
       if (cut == 0) {
-        // The blocks with the longest rows first, one to a CTA and round, every other round backwards, so that the CTAs end together.  (Handed out by an atomic counter the next item came 2 us after it was
-        // asked for, half of what one of seven tiles takes.)
-        const int k = round * (int)gridDim.x + ((round & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
+        // The blocks with the longest rows first, one to a CTA and round, every other round backwards, so that the CTAs end together.
+        // (Handed out by an atomic counter the next item came 2 us after it was asked for, half of what one of seven tiles takes.)
+        const int k = many_dealt(round, (int)blockIdx.x, (int)gridDim.x);
         more = round * (int)gridDim.x < n_items;
         ++round;
         if (more && k >= n_items) continue;
@@ -1059,7 +1059,6 @@ cudaError_t launch_many(const PagedArgs& a, const void* q, const void* k, int64_
   if (err == cudaSuccess) err = map_pages(&map_k, a, k);
   if (err == cudaSuccess) err = allow_smem<&paged_many_kernel<HD, kAlibi>>(ManyCfg<HD>::kSmemBytes);
   if (err != cudaSuccess) return err;
-  // (where units are cut every SM gets a run; otherwise there are more of them than SMs)
   return launch_kernel(paged_many_kernel<HD, kAlibi>, (unsigned)a.sms, kManyThreads, ManyCfg<HD>::kSmemBytes, stream, map_q, map_k, a, blocks);
 }
 

@@ -346,6 +346,50 @@ def test_graph_replay_and_second_stream():
     assert torch.equal(again, o) and not torch.equal(o[:2], eager[0][:2])
 
 
+def test_short_and_long_chunks_side_by_side():
+    # both kinds of sequences in one call: against the definition, captured in a thread that never made such a call, and replayed among eager ones
+    import threading
+    new, lens = [1] * 9 + [100, 2, 60], [300, 20, 1, 77, 256, 40, 129, 9, 500, 700, 64, 60]
+    pr = _problem(new, lens, 4, 2, 64, 16)
+    sc = _scales(4, 1, "length")
+    cuda = [t.cuda() for t in sc]
+    out = dict(o=torch.zeros((sum(new), 4, 64), dtype=torch.bfloat16, device="cuda"), tau=torch.zeros((sum(new), 4), device="cuda"),
+               support_size=torch.zeros((sum(new), 4), dtype=torch.int32, device="cuda"))
+    call = lambda **kw: binding.entmax_attn_paged_fwd(pr["q"], pr["kc"], pr["vc"], 1.5, pr["table"], pr["lens"], pr["cu"], *cuda, **kw)  # noqa: E731
+    graph = torch.cuda.CUDAGraph()
+    failed = []
+
+    def capture():
+        try:
+            with torch.cuda.graph(graph):
+                call(**out)
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    torch.cuda.synchronize()
+    t = threading.Thread(target=capture)
+    t.start()
+    t.join()
+    assert not failed, failed
+    got = _run(pr, 1.5, sc)
+    _check(pr, 1.5, got, sc)
+    for _ in range(3):
+        for x in out.values():
+            x.zero_()
+        graph.replay()
+        eager = call()
+        torch.cuda.synchronize()
+        assert torch.equal(out["o"], got[0]) and torch.equal(out["tau"], got[1]) and torch.equal(out["support_size"], got[2])
+        assert torch.equal(eager[0], got[0]) and torch.equal(eager[1], got[1])
+    again = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(again):
+        call(**out)
+    out["o"].zero_()
+    again.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out["o"], got[0])
+
+
 # ------------------------------------------------------------------------------------------------ append
 def _append_problem(new, lens, H, KH, d, page, seed=0, layout="tokens"):
     g = torch.Generator().manual_seed(seed)
