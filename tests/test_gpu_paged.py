@@ -239,6 +239,27 @@ def test_large_batches():
     _check(pr, 1.5, _run(pr, 1.5, sc), sc, heads=[0, 3, 7], skip=range(1, 60, 4))
 
 
+@pytest.mark.parametrize("new,lens,H,KH,d,page,slopes,columns", [
+    ([70, 33, 40], [9000, 300, 5000], 4, 2, 64, 16, None, 0),
+    ([70, 33, 40], [9000, 300, 5000], 4, 2, 128, 64, [0.0, 0.01, 0.3, 2.0], 0),
+    ([70, 33, 40], [9000, 300, 5000], 2, 1, 64, 256, None, 1100),           # a table for 281600 keys: rows of several lengths share a class
+    ([35] * 80 + [300], list(range(35, 115)) + [9000], 4, 4, 64, 16, None, 0),      # one long chunk among short prompts
+    ([257] * 24, [257] * 12 + [900] * 12, 16, 8, 64, 32, [0.1] * 16, 0),
+])
+def test_uneven_and_even_units(new, lens, H, KH, d, page, slopes, columns):
+    # chunks whose keys are shared among work items, and such that whole units are dealt evenly
+    pr = _problem(new, lens, H, KH, d, page)
+    if columns:
+        wide = torch.full((len(new), columns), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+        wide[:, :pr["table"].shape[1]] = pr["table"]
+        pr["table"] = wide
+    sc = _scales(H, 3, "length")
+    got = _run(pr, 1.5, sc, slopes)
+    again = _run(pr, 1.5, sc, slopes)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+    _check(pr, 1.5, got, sc, slopes, heads=[0, H - 1], skip=[b for b in range(len(new)) if len(new) > 3 and b % 9 not in (0, 8)])
+
+
 @pytest.mark.parametrize("n", [1, 5, 40])
 def test_uniform_chunks_without_offsets(n):
     lens = [41, 300, 64]
