@@ -611,7 +611,7 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
   pdl_begin();
   constexpr int W = kCtaWarps;
   __shared__ float list_y[kCtaWarps][kSeg];
-  __shared__ long long list_at[kCtaWarps][kSeg];          // where the V row is
+  __shared__ long long list_at[kCtaWarps][kSeg];          // key, then where its V row is
   __shared__ float maxima[kCtaWarps][kChunks * 32];
   __shared__ float2 red[2][W];
   __shared__ float opart[W][D];
@@ -778,13 +778,19 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
       const unsigned m = __ballot_sync(0xffffffffu, y > floor_y);
       const int at = cnt + __popc(m & ((1u << lane) - 1u));
       if (y > floor_y && at < kSeg) {
-        const long long off = pages.at(key);
-        if (off >= 0) prefetch_row<D>(v_head + off);
         my_y[at] = y;
-        my_at[at] = off;
+        my_at[at] = key;
       }
       cnt += __popc(m);
     });
+    // (not while they are collected, where each would wait for the block table by itself)
+    __syncwarp();
+#pragma unroll 4
+    for (int e = lane; e < min(cnt, kSeg); e += 32) {
+      const long long off = pages.at((int)my_at[e]);
+      if (off >= 0) prefetch_row<D>(v_head + off);
+      my_at[e] = off;
+    }
     const bool walk = __syncthreads_or(cnt > kSeg);         // more than the lists hold: the kept keys are walked every time
 
     // ---- threshold
