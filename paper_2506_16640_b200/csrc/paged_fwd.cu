@@ -601,7 +601,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_ke
 // ================================================================================================== row
 constexpr int kCtaWarps = 8;
 constexpr int kSeg = 256;            // list entries of a warp
-constexpr int kCtaRows = 2 * 148, kLongRow = 16384, kRows8Worth = 9472;   // (see solve_lanes)
+constexpr int kCtaRows = 2 * 148, kLongRow = 4096, kRows8Worth = 9472;   // (see solve_lanes)
 constexpr int kChunks = 8;           // chunks of 32 groups of a warp whose maxima stay in shared memory
 
 // kSpilled: the rows listed by the rows kernel, by CTAs that stay; otherwise a CTA for each of the n_slots row slots
@@ -885,12 +885,14 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
   }
 }
 
-// Lanes of a row in the solve of a launch; 0: a CTA.  A CTA per row where all fit the machine at once (two to an SM), and for up to three rounds of
-// long rows: 256 rows of 65536 keys 17 us against 25 with a warp each, 320 of 48222 26 against 51, 1120 of 45231 69 against 52, 640 of
-// 4096 23 against 13.  Eight lanes where there are more rows than warps to keep (37000 rows of chunks 18 us against 39 with a warp each).
+// Lanes of a row in the solve of a launch; 0: a CTA.  A CTA per row where all fit the machine at once (two to an SM), which takes 8 us for the
+// shortest rows, and for two or three rounds of longer ones: 256 rows of 65536 keys 16 us against 27 with a warp each, 320 of 48222 24 against
+// 54, 512 of 16384 18 against 23, 384 of 6000 at c = 1 21 against 26; but 576 of 4096 18 against 18, 448 of 2048 16 against 14, 640 of 4096
+// 22 against 15, 1120 of 45231 64 against 55.  Eight lanes where there are more rows than warps to keep (37000 rows of chunks 18 us against
+// 39 with a warp each).
 int solve_lanes(const PagedArgs& a, long long rows) {
-  if (rows <= kCtaRows || (rows <= 3 * kCtaRows && a.max_kv > kLongRow) || a.max_kv > 1 << 20) return 0;
-  return rows < kRows8Worth ? 32 : 8;
+  const int rounds = a.max_kv <= kLongRow ? 1 : a.max_kv <= 4 * kLongRow ? 2 : 3;
+  return rows <= rounds * kCtaRows ? 0 : rows < kRows8Worth ? 32 : 8;
 }
 
 template <int D, bool kMany, int L>
