@@ -355,6 +355,14 @@ def _call_on(device, fn, *args):
         return fn(*args)
 
 
+def _new_on(stream, like, shape, dtype):
+    """A tensor that the allocator gives away again in the order of the stream the call runs on."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
 def _append_layout(what, q, k, v, k_cache, v_cache, block_table, kv_len, cu_q, rotation, interleaved, q_out, status):
     T, KH, D = k.shape if k.dim() == 3 else (0, 0, 0)
     ks, vs = _row_strides("k", k, KH, D), _row_strides("v", v, KH, D)
@@ -396,7 +404,7 @@ def entmax_attn_paged_append(q, k, v, k_cache, v_cache, block_table, kv_len, cu_
         what, q, k, v, k_cache, v_cache, block_table, kv_len, cu_q, rotation, interleaved, q_out, status))
     device = k.get_device()
     if q is not None and q_out is None:
-        q_out = q.new_empty((T, H, D))
+        q_out = _new_on(stream, q, (T, H, D), torch.bfloat16)
     if T == 0:
         return q_out
     rc = _call_on(device, lambda: load().entmax_attn_paged_append(
@@ -447,13 +455,15 @@ def entmax_attn_paged_fwd(q, k_cache, v_cache, alpha, block_table, kv_len, cu_q=
         tau, support_size, status))
     device = q.get_device()
     if o is None:
-        o = q.new_empty((T, H, D))
+        o = _new_on(stream, q, (T, H, D), torch.bfloat16)
     if tau is None:
-        tau = q.new_empty((T, H), dtype=torch.float32)
+        tau = _new_on(stream, q, (T, H), torch.float32)
     if T == 0:
         return o, tau, support_size
     if workspace is None:
-        workspace = q.new_empty(nbytes, dtype=torch.uint8)
+        workspace = _new_on(stream, q, (nbytes,), torch.uint8)
+    elif workspace.dtype != torch.uint8 or workspace.get_device() != device or not workspace.is_contiguous():
+        raise EntmaxAttnError("%s: workspace must be a contiguous uint8 tensor on the device of q" % what)
     rc = _call_on(device, lambda: load().entmax_attn_paged_fwd(
         cache, params, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(cu_q), kv_len.data_ptr(), block_table.data_ptr(), _ptr(beta),
         _ptr(gamma), _ptr(delta), _ptr(alibi_slopes), o.data_ptr(), tau.data_ptr(), _ptr(support_size), workspace.data_ptr(),

@@ -367,6 +367,26 @@ def test_graph_replay_and_second_stream():
     assert torch.equal(again, o) and not torch.equal(o[:2], eager[0][:2])
 
 
+def test_memory_of_a_call_on_another_stream():
+    # what the call allocates is given away in the order of its own stream, not of the current one that never waits for it
+    pr = _problem([1] * 9 + [100], [300] * 9 + [400], 4, 2, 64, 16)
+    want = _run(pr, 1.5, max_q_len=100, max_kv_len=400)
+    side = torch.cuda.Stream()
+    args = (pr["q"], pr["kc"], pr["vc"], 1.5, pr["table"], pr["lens"], pr["cu"])
+    for _ in range(2):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)                   # some ms: the call's work starts after what follows here
+        o, tau, _ = binding.entmax_attn_paged_fwd(*args, max_q_len=100, max_kv_len=400, stream=side)
+        mine = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for n in (1 << 12, 1 << 16, 1 << 20, 1 << 21, 1 << 22, 1 << 23, 1 << 24)]
+        torch.cuda.synchronize()
+        assert all(bool((m == 7).all()) for m in mine)
+        assert torch.equal(o, want[0]) and torch.equal(tau, want[1])
+        del mine
+    with pytest.raises(binding.EntmaxAttnError, match="workspace"):
+        binding.entmax_attn_paged_fwd(*args, workspace=torch.empty(1 << 26, dtype=torch.uint8))
+
+
 def test_short_and_long_chunks_side_by_side():
     # both kinds of sequences in one call: against the definition, captured in a thread that never made such a call, and replayed among eager ones
     import threading
