@@ -8,7 +8,10 @@
 //   rows    eight lanes per row where there are many rows: a record or a group's 32 scores and a V row are a coalesced access of eight
 //           lanes, sums take three shuffles, and a warp has four rows' chains of dependent loads under way.  A warp per row where there are
 //           fewer.  Rows with more candidates than their list holds are listed for
-//   row     a CTA per row, for those and for calls of few or very long rows.
+//   row     a CTA per row, for those and for calls of few or long rows.
+// Bound by instructions where the machine is full (182000 rows of prompts 73 us, 68 % of the issue slots), else by the chain maxima - candidates -
+// pages - threshold - V rows: 2048 decode rows 13 us with a warp each, 256 rows of 65536 keys 16 us and 256 flat ones of 8192 (supports of
+// hundreds) 20 us with a CTA each.
 #include <atomic>
 #include <cmath>
 
@@ -127,7 +130,7 @@ __device__ __forceinline__ UnitOf unit_of(const PagedArgs& a, int first, int uni
 // =================================================================================================== plan
 // What the "many" kernels need to know of the blocks block0 .. block0 + blocks - 1 of new tokens, and the order their work is handed out in:
 // longest rows first (by 1024 classes of length), so that the CTAs end together; clears the counters.  The first CTA does this, the others
-// fill in the scales of the rows.
+// fill in the scales of the rows.  Latency: 5.5 us for one chunk of 2048, 7.5 for 357 blocks of prompts.
 constexpr int kPlanThreads = 1024;
 __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_constant__ PagedArgs a, int block0, int blocks) {
   pdl_begin();
