@@ -551,15 +551,29 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_ke
     if (__all_sync(0xffffffffu, done)) break;
   }
   const float tau = st.tau;
-  int support = 0;
-  for (int e = sl; e < cnt; e += L) {
-    const float d = fmaxf(my_y[e] - tau, 0.f);
-    float p, p1;
+  // (the list closes up to the support: half and more of the candidates have p = 0.  A page that is not there counts as zeros.)
+  int support = 0, kept = 0;
+#pragma unroll 1
+  for (int e0 = 0; e0 < longest; e0 += L) {
+    const int e = e0 + sl;
+    float d = 0.f, p, p1;
+    long long at = -1;
+    if (e < cnt) {
+      d = fmaxf(my_y[e] - tau, 0.f);
+      at = my_at[e];
+    }
     powers<EC>(d, a.expo, p, p1);
-    support += d > 0.f ? 1 : 0;
-    my_y[e] = my_at[e] >= 0 ? p : 0.f;                      // (a page that is not there counts as zeros)
+    support += __popc(row_bits(d > 0.f));
+    const unsigned bits = row_bits(p > 0.f && at >= 0);
+    __syncwarp();
+    if ((bits >> sl) & 1u) {
+      const int to = kept + __popc(bits & ((1u << sl) - 1u));
+      my_y[to] = p;
+      my_at[to] = at;
+    }
+    kept += __popc(bits);
   }
-  support = (int)sum_lanes<L>((float)support);
+  cnt = kept;
   __syncwarp();
 
   // ---- O = sum_j p_j v_j: an octet of lanes to a V row, four of each octet in flight
