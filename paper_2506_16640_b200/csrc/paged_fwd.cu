@@ -9,7 +9,7 @@
 //           lanes, sums take three shuffles, and a warp has four rows' chains of dependent loads under way.  A warp per row where there are
 //           fewer.  Rows with more candidates than their list holds are listed for
 //   row     a CTA per row, for those and for calls of few or long rows.
-// Bound by instructions where the machine is full (182000 rows of prompts 73 us, 68 % of the issue slots), else by the chain maxima - candidates -
+// Bound by instructions where the machine is full (182000 rows of prompts 70 us, 68 % of the issue slots), else by the chain maxima - candidates -
 // pages - threshold - V rows: 2048 decode rows 13 us with a warp each, 256 rows of 65536 keys 16 us and 256 flat ones of 8192 (supports of
 // hundreds) 20 us with a CTA each.
 #include <atomic>
@@ -273,8 +273,8 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
 }
 
 // ================================================================================================= rows
-// L lanes to a row, 8 or 32
-constexpr int kRowsWarps = 8;
+// L lanes to a row, 8 or 32.  (CTAs of eight warps: 72 us against 70 on 182000 rows of prompts, 16.8 against 15.6 on 3600 of two chunks)
+constexpr int kRowsWarps = 4;
 template <int L>
 struct RowsShape {
   static constexpr int kRows = 32 * kRowsWarps / L;      // rows of a CTA
@@ -299,7 +299,7 @@ __device__ __forceinline__ float max4(const float4& x) { return fmaxf(fmaxf(x.x,
 // (Loops are kept rolled: unrolled, this code no longer stayed in the instruction cache, 140 us against 86 on 11402 prompt tokens of 16 heads,
 // and 72 against 21 on 64 x 32 decode rows.)
 template <int D, int EC, bool kMany, int L>
-__global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 4 : 3) paged_rows_kernel(const __grid_constant__ PagedArgs a,
+__global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_kernel(const __grid_constant__ PagedArgs a,
                                                                                     const __nv_bfloat16* __restrict__ v, int first,
                                                                                     int units) {
   pdl_begin();
