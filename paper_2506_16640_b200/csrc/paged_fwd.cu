@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
   pdl_begin();
   __shared__ int bin[kPlanThreads];               // blocks of a class, then the next place of the class
   __shared__ int warp_sum[kPlanThreads / 32];
-  __shared__ int n_blocks, longest;
+  __shared__ int n_blocks, longest, walk;         // longest block; longest walk of a CTA that takes whole units (both in tiles)
   __shared__ int load[256];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int tokens = kManyTiles * a.tile_tokens;
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
   }
   bin[tid] = 0;
   if (tid < 256) load[tid] = 0;
-  if (tid == 0) longest = 0;
+  if (tid == 0) longest = walk = 0;
   if (tid <= kSpilledRows) a.counters[tid] = 0;
   __syncthreads();
   auto class_of = [&](int tiles) { return kPlanThreads - 1 - (int)((long long)(tiles - 1) * kPlanThreads / a.tiles); };
@@ -241,8 +241,9 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
   // up to 1000 tokens, 9: 118 against 134; a chunk of 1024 over 30000 keys, 32 heads, 16: 279 against 268; of 2048 over 32768, 16 heads, 20:
   // 266 against 246; three sequences, one with a chunk of 500 over 9001 keys, 27: 104 against 75)
   const int all = carry * a.c.KH;                           // (scores are held for all of them at once, so it fits)
-  auto even = [&]() { return (longest - 12) * a.sms <= all; };
-  if (even()) {
+  auto even = [&](int tiles) { return (tiles - 12) * a.sms <= all; };
+  // (longest stays as it is from the barriers above on, so that all threads take the same way here)
+  if (even(longest)) {
     // nor does the longest unit by itself: each CTA's walk, in the order that the many kernel deals units (item k's class is the last one with
     // no more than k / KH blocks before it)
     // (few instructions and no divisions: they come from memory each time.  The first version of this loop cost 4 us.)
@@ -259,12 +260,12 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
       sum += class_tiles(cls);
     }
     sum = atomicAdd(&load[cta], sum) + sum;                 // (the last of a CTA's threads sees the whole)
-    atomicMax(&longest, sum);
-    __syncthreads();
+    atomicMax(&walk, sum);
   }
+  __syncthreads();
   if (tid == 0) {
     a.counters[kTiles] = carry;
-    a.counters[kCut] = even() ? 0 : (all + a.sms - 1) / a.sms;
+    a.counters[kCut] = even(max(longest, walk)) ? 0 : (all + a.sms - 1) / a.sms;
   }
   for (int i = tid; i < blocks; i += kPlanThreads) {
     const PagedBlock pb = a.blocks[i];

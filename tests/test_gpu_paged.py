@@ -260,6 +260,18 @@ def test_uneven_and_even_units(new, lens, H, KH, d, page, slopes, columns):
     _check(pr, 1.5, got, sc, slopes, heads=[0, H - 1], skip=[b for b in range(len(new)) if len(new) > 3 and b % 9 not in (0, 8)])
 
 
+def test_units_that_are_cut_only_after_they_were_dealt():
+    # 152 equal units of 13 tiles for 148 SMs: no unit is too long by itself, but four CTAs would take two of them; the plan kernel's warps have
+    # to agree on that way, call for call
+    pr = _problem([256] * 19, [3328] * 19, 8, 8, 64, 16)
+    sc = _scales(8, 3, "length")
+    got = _run(pr, 1.5, sc, max_q_len=256, max_kv_len=3328)
+    _check(pr, 1.5, got, sc, heads=[0, 7], skip=range(1, 18), rows=[0, 100, 255])
+    for _ in range(30):
+        again = _run(pr, 1.5, sc, max_q_len=256, max_kv_len=3328)
+        assert all(torch.equal(x, y) for x, y in zip(got[:3], again[:3]))
+
+
 @pytest.mark.parametrize("n", [1, 5, 40])
 def test_uniform_chunks_without_offsets(n):
     lens = [41, 300, 64]
