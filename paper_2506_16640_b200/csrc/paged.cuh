@@ -140,10 +140,23 @@ struct ManyCut {
     return item == 0 ? 0 : cut ? min((start / cut + item) * cut - start, tiles) : tiles;
   }
 };
+// A kernel whose bounded wait has run out returns before it has written all it should.  Such a call's results are invalid (and flagged), but its
+// solve must not read outside the row's room.  "many": the CTA that gives up clears every row's record counts (clear_records).  "few": a group's unwritten
+// scores may name a key of the last group that the row does not see, and so a page behind its last one; the look-up stays among the table's entries.
+// (Counts and keys held to their room where the solve reads them cost it 2 %.)
+__host__ __device__ __forceinline__ int page_entry(int key, int ps_shift, int max_pages) {
+  return (int)min((unsigned)key >> ps_shift, (unsigned)max_pages - 1u);
+}
 // Uncut units: the item, in the order of length, that a CTA takes in a round (every other round backwards)
 __device__ __forceinline__ int many_dealt(int round, int cta, int ctas) { return round * ctas + ((round & 1) ? ctas - 1 - cta : cta); }
 __device__ __forceinline__ ManyCut many_cut(const int32_t* counters, const PagedBlock& pb, int kv_head) {
   return ManyCut{kv_head * counters[kTiles] + pb.start, pb.tiles, counters[kCut]};
+}
+
+// No records for any row of the units of `blocks` blocks, whatever has been written by whom
+__device__ __forceinline__ void clear_records(const PagedArgs& a, int blocks, int t, int threads) {
+  const size_t n = (size_t)blocks * a.c.KH * a.many_items * a.many_slots;
+  for (size_t i = t; i < n; i += threads) a.row_info[i] = make_float4(0.f, -INFINITY, 0.f, 0.f);
 }
 
 // Whether the sequence can be served at all, and by which kernel

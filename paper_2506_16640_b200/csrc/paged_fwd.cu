@@ -56,16 +56,16 @@ __device__ __forceinline__ void store_share(__nv_bfloat16* row, int sl, const fl
 // Where V row j of a sequence is, in elements from the K/V head's first (-1: its page is not in the pool)
 struct Pages {
   const int32_t* table;
-  int shift, n_pages;
+  int shift, n_pages, max_pages;
   long long s_page, s_tok;
   __device__ __forceinline__ long long at(int j) const {
-    const int page = table[j >> shift];
+    const int page = table[page_entry(j, shift, max_pages)];
     if ((unsigned)page >= (unsigned)n_pages) return -1;
     return (long long)page * s_page + (long long)(j & ((1 << shift) - 1)) * s_tok;
   }
 };
 __device__ __forceinline__ Pages pages_of(const PagedCache& c, int b) {
-  return Pages{c.table + (long long)b * c.table_stride, c.ps_shift, c.n_pages, c.s_page, c.s_tok};
+  return Pages{c.table + (long long)b * c.table_stride, c.ps_shift, c.n_pages, c.max_pages, c.s_page, c.s_tok};
 }
 // (a V row is one or two 128-byte lines)
 template <int D>

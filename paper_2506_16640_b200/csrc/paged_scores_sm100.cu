@@ -1010,6 +1010,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
       const uint64_t t0 = global_ns();
       while (global_ns() - t0 < 200000ull) { }
     }
+    clear_records(a, blocks, threadIdx.x, kManyThreads);
     __syncthreads();
   }
   if (warp == 1) {

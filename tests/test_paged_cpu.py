@@ -169,3 +169,36 @@ def test_reference_pins():
     turn = torch.tensor([[0.0, 0.0, 1.0, 1.0]])
     assert paged.rotate(x, turn, torch.tensor([0]), False).tolist() == [[[-3.0, -4.0, 1.0, 2.0]]]
     assert paged.rotate(x, turn, torch.tensor([0]), True).tolist() == [[[-2.0, 1.0, -4.0, 3.0]]]
+
+
+_BOUNDS = r"""
+#include <cstdio>
+#include <random>
+#include "paged.cuh"
+using namespace entmax;
+// Keys as a solve finds them whose score kernel has not ended: any of the row's groups.  The table's entry is the key's own where the row sees it,
+// and one of the sequence's entries in any case.
+int main() {
+  std::mt19937 g(7);
+  auto upto = [&](int n) { return (int)(g() % (unsigned)n); };
+  int behind = 0;
+  for (int trial = 0; trial < 200000; ++trial) {
+    const int shift = 4 + upto(13), pages = 1 + upto(trial % 3 ? 5 : (1 << 24) >> shift), pos = upto(pages << shift);
+    const int key = pos / kGroupKeys * kGroupKeys + upto(kGroupKeys), entry = page_entry(key, shift, pages), seen = upto(pos + 1);
+    if (entry < 0 || entry >= pages) return printf("key %d in entry %d of %d\n", key, entry, pages), 1;
+    if (page_entry(seen, shift, pages) != seen >> shift) return printf("entry of key %d changed\n", seen), 1;
+    behind += key >> shift >= pages;
+  }
+  return behind > 0 ? 0 : 2;
+}
+"""
+
+
+def test_keys_of_unwritten_scores_stay_in_the_block_table(tmp_path):
+    import subprocess
+    src, exe = tmp_path / "bounds.cu", tmp_path / "bounds"
+    src.write_text(_BOUNDS)
+    subprocess.run([lib_build._nvcc(), "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", lib_build.CSRC, "-I", lib_build.INCLUDE,
+                    "-o", str(exe), str(src)], check=True, capture_output=True, text=True)
+    run = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert run.returncode == 0, run.stdout
