@@ -994,9 +994,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
         if (flat && step_no > 0 && (step_no & (step_no + 1)) == 0)
           thr = fmaxf(thr, bound_from_eight(top, margin, a.expo_class, a.expo));
       }
+      // (a = 0: every key is kept and y = 0 for all of them; a that is not a number: there is no bound either)
       if (valid && alive)
         a.row_info[((size_t)it.unit * a.many_items + it.item) * a.many_slots + slot_row] =
-            make_float4(__int_as_float((int)n_rec), mag * thr, mag, 0.f);
+            make_float4(__int_as_float((int)n_rec), mag > 0.f ? mag * thr : -INFINITY, mag, 0.f);
     }
   }
 

@@ -324,6 +324,21 @@ def test_scales_without_an_order(kind):
             _check(pr, 1.5, got, sc)
 
 
+@pytest.mark.parametrize("new,lens,H,KH", [([64], [32768], 16, 4), ([64] + [200] * 11, [20000] + [200] * 11, 4, 2)])
+def test_heads_of_scale_zero_in_units_of_many_work_items(new, lens, H, KH):
+    # delta = beta = 0: the mean of V; more items to a unit than a row has lanes, 32 of them and eight
+    pr = _problem(new, lens, H, KH, 64, 16)
+    sc = _scales(H, 6, "length")
+    for t in (sc[0], sc[2]):
+        t[::3] = 0.0
+    got = _run(pr, 1.5, sc, max_q_len=max(new), max_kv_len=max(lens))
+    _check(pr, 1.5, got, sc, heads=[0, 1, 3, H - 1], skip=range(2, len(new)), rows=[0, 1, 40, 63])
+    # (every key; sums of up to 1024 equal terms by a lane are off by 6e-5 of themselves at most, tau by half of that, and by 1e-7 of 0.0055 for the step
+    # it ends at)
+    n = torch.arange(lens[0] - 63, lens[0] + 1)
+    assert torch.equal(got[2][:64, 0].cpu().long(), n) and torch.allclose(got[1][:64, 0].cpu().double(), -n.double().pow(-0.5), rtol=1e-4)
+
+
 def test_offsets_beyond_32_bits():
     # a pool of more than 2^32 bytes, the sequence's pages at its end
     d, KH, page = 128, 2, 256
