@@ -74,7 +74,7 @@ int check_paged_cache(const entmax_attn_paged_cache* cache, int total_q, PagedCa
 //       several work items (ManyCut).  The item whose first K tile is lo keeps records of eight neighbouring keys, those with a value above
 //       the bound it had then, in key order:
 //       scores[row][256 lo + 8 i ..]  the values, before the scaling by |a|      record_key[row][32 lo + i]  the first key
-//       row_info[unit][item][row]     {number of records, the bound the item ended with, |a|, -}
+//       row_info[unit][item][row]     {number of records, the bound the item ended with, |a|, the largest value} (bound and value before the scaling, too)
 //       (room for every key: a row of flat logits keeps them all)
 constexpr int kGroupKeys = 32;
 constexpr int kManyKeys = 256;
@@ -156,7 +156,7 @@ __device__ __forceinline__ ManyCut many_cut(const int32_t* counters, const Paged
 // No records for any row of the units of `blocks` blocks, whatever has been written by whom
 __device__ __forceinline__ void clear_records(const PagedArgs& a, int blocks, int t, int threads) {
   const size_t n = (size_t)blocks * a.c.KH * a.many_items * a.many_slots;
-  for (size_t i = t; i < n; i += threads) a.row_info[i] = make_float4(0.f, -INFINITY, 0.f, 0.f);
+  for (size_t i = t; i < n; i += threads) a.row_info[i] = make_float4(0.f, -INFINITY, 0.f, -INFINITY);
 }
 
 // Whether the sequence can be served at all, and by which kernel
@@ -172,6 +172,14 @@ __device__ __forceinline__ void powers(float y, float expo, float& ye, float& ye
 }
 // A lower bound of a threshold from an iterate that came from the left: a hair below it for the rounding
 __device__ __forceinline__ float bound_below(float tau) { return tau - 1e-5f * fmaxf(1.0f, fabsf(tau)); }
+
+// The bound y_max - 1 of a threshold, below y_max in any case: from |y_max| = 2^24 on, where 1 is less than a float's distance from the next, the float
+// before it, so that the largest keys are above the bound
+__device__ __forceinline__ float one_below(float ymax) {
+  const float y = ymax - 1.0f;
+  if (y < ymax || !(ymax > -INFINITY)) return y;
+  return __int_as_float(__float_as_int(ymax) + (ymax > 0.f ? -1 : 1));
+}
 
 // (alpha-1) c sm_scale of a query at position pos, c = delta + beta (ln n)^gamma with n = pos + 1 (delta for n = 1; 1 without
 // scale parameters)

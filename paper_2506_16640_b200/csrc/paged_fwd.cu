@@ -76,13 +76,15 @@ __device__ __forceinline__ void prefetch_row(const __nv_bfloat16* p) {
 
 // One step of the threshold iteration on the candidates from their sums.  Returns false when st.tau is final.  e >= 1: Newton on the e-norm,
 // from the left; the rounding of a long step over many keys can pass the root, and a step back from there lands at or before it.
-__device__ __forceinline__ bool solve_step(TauIter& st, float s0, float s1, int expo_class, float expo) {
+__device__ __forceinline__ bool solve_step(TauIter& st, float s0, float s1, int expo_class, float expo, float tolerance) {
   if (expo < 1.0f) return tau_iter_update(st, s0, s1, expo_class, expo, 1e-7f);
   if (!(s1 > 0.f)) return false;
   const float step = threshold_step(s0, s1, expo_class, expo);
   st.tau += step;
-  return fabsf(step) > 1e-7f * fmaxf(1.0f, fabsf(st.tau));
+  return fabsf(step) > tolerance;
 }
+// (the largest value's size sets how far tau, a float of that size, need be known; where scores are large differences among them are what counts)
+__device__ __forceinline__ float step_tolerance(float ymax) { return 1e-7f * fminf(fmaxf(1.0f, fabsf(ymax)), 16.0f); }
 constexpr int kMaxSteps = 64;
 constexpr int kBoundSteps = 5;       // steps towards the threshold of the cells' maxima
 constexpr int kFewCandidates = 8;   // groups above y_max - 1 up to which that bound is not looked for
@@ -342,7 +344,9 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
   // second try with a higher bound: the threshold of maxima of different keys alone, by a few steps from the left (any iterate is a bound;
   // a hair below it for the rounding).  c = 1, alpha = 1.5, 32768 keys N(0, 1): 585 keys above y_max - 1, about 50 above that.
   int cnt = 0;
-  float ymax = -INFINITY, floor_y = -INFINITY, mag = 0.f;
+  // Candidates are told by the values as they were kept (many: before the scaling by mag), floor_y among them.  What goes to the list, and the
+  // threshold, is relative to the largest value: in [-1, 0] whatever the size of the scores.
+  float top = -INFINITY, floor_y = -INFINITY, mag = 0.f;
   const Records rec = kMany && live ? records_of(a, w.cut, unit, r, row, pos) : Records{};
   const int groups = live ? pos / kGroupKeys + 1 : 0;
   const float4* max_row = reinterpret_cast<const float4*>(a.group_max + row * a.groups);
@@ -350,7 +354,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
   const int most_items = kMany ? __reduce_max_sync(0xffffffffu, rec.items) : 0;
 
   // what the row's items left, a lane each (those past L are read when their turn comes)
-  float4 info = make_float4(0.f, -INFINITY, 0.f, 0.f);
+  float4 info = make_float4(0.f, -INFINITY, 0.f, -INFINITY);
   if (kMany && sl < rec.items) info = rec.info[(size_t)sl * rec.slots];
   auto row_bits = [&](bool x) { return (__ballot_sync(0xffffffffu, x) >> row_bit) & S::kMask; };
   auto append = [&](const float4& y4, int key) {            // this lane's four keys from `key` on
@@ -363,7 +367,8 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
       const int at = cnt + __popc(bits & ((1u << sl) - 1u));
       if (left && at < S::kList) {
         const int e = __ffs(left) - 1;
-        my_y[at] = e < 2 ? (e == 0 ? y4.x : y4.y) : (e == 2 ? y4.z : y4.w);
+        const float y = e < 2 ? (e == 0 ? y4.x : y4.y) : (e == 2 ? y4.z : y4.w);
+        my_y[at] = kMany ? mag * (y - top) : y - top;
         my_at[at] = key + e;
       }
       left &= left - 1;
@@ -399,7 +404,6 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           if (s0 + L / 2 * u >= most) break;
-          y[u].x *= mag; y[u].y *= mag; y[u].z *= mag; y[u].w *= mag;
           f(y[u], key[u]);
         }
       }
@@ -420,14 +424,22 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
   if constexpr (kMany) {
     mag = __shfl_sync(0xffffffffu, info.z, 0, L);
     floor_y = info.y;
-    for (int i = sl + L; i < rec.items; i += L) floor_y = fmaxf(floor_y, rec.info[(size_t)i * rec.slots].y);
+    top = info.w;
+    for (int i = sl + L; i < rec.items; i += L) {
+      const float4 other = rec.info[(size_t)i * rec.slots];
+      floor_y = fmaxf(floor_y, other.y);
+      top = fmaxf(top, other.w);
+    }
     floor_y = max_lanes<L>(floor_y);
+    top = max_lanes<L>(top);
   } else {
 #pragma unroll 4
-    for (int i = 0; i < chunks; ++i) ymax = fmaxf(ymax, max4(maxima(i)));
-    ymax = max_lanes<L>(ymax);
-    floor_y = ymax - 1.0f;
+    for (int i = 0; i < chunks; ++i) top = fmaxf(top, max4(maxima(i)));
+    top = max_lanes<L>(top);
+    floor_y = one_below(top);
   }
+  // (-1 too where a = 0 and nothing bounds the row)
+  auto floor_of_list = [&]() { return fmaxf(kMany ? mag * (floor_y - top) : floor_y - top, -1.0f); };
   // over: rows to raise the bound of.  Where groups are looked at, their number tells before anything is collected.
   bool over = false;
   if constexpr (!kMany) {
@@ -442,13 +454,13 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
 #pragma unroll 1
   for (int attempt = 0; attempt < 3; ++attempt) {
     if (a.expo >= 1.0f && __any_sync(0xffffffffu, over)) {
-      float tau = fmaxf(floor_y, ymax - 1.0f);
+      float tau = floor_of_list();
 #pragma unroll 1
       for (int it = 0; it < kBoundSteps; ++it) {
         float s0 = 0.f, s1 = 0.f;
         auto add = [&](float m) {
           float ye, ye1;
-          powers<EC>(fmaxf(m - tau, 0.f), a.expo, ye, ye1);
+          powers<EC>(fmaxf((kMany ? mag * (m - top) : m - top) - tau, 0.f), a.expo, ye, ye1);
           s0 += ye;
           s1 += ye1;
         };
@@ -470,15 +482,12 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
         if (go) tau += threshold_step(s0, s1, EC, a.expo);
         if (!__any_sync(0xffffffffu, go && over)) break;
       }
-      if (over) floor_y = fmaxf(floor_y, fmaxf(ymax - 1.0f, bound_below(tau)));
+      // (back among the values as they were kept: a hair more for the rounding there)
+      if (over) floor_y = fmaxf(floor_y, top + (kMany ? bound_below(tau) / mag : bound_below(tau)) - 0x1p-21f * fabsf(top));
     }
     cnt = 0;
     if constexpr (kMany) {
-      for_records([&](const float4& y, int key) {
-        ymax = fmaxf(ymax, max4(y));
-        append(y, key);
-      });
-      ymax = max_lanes<L>(ymax);
+      for_records(append);
     } else {
 #pragma unroll 1
       for (int i = 0; i < chunks; ++i) {
@@ -533,9 +542,10 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
   // ---- threshold
   const int longest = __reduce_max_sync(0xffffffffu, cnt);
   TauIter st;
-  st.tau = st.lo = fmaxf(floor_y, ymax - 1.0f);
-  st.hi = ymax;
+  st.tau = st.lo = floor_of_list();
+  st.hi = 0.f;
   bool done = !live;
+  const float tolerance = step_tolerance(kMany ? mag * top : top);
 #pragma unroll 1
   for (int it = 0; it < kMaxSteps; ++it) {
     float s0 = 0.f, s1 = 0.f;
@@ -548,7 +558,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
     }
     s0 = sum_lanes<L>(s0);
     s1 = sum_lanes<L>(s1);
-    if (!done) done = !solve_step(st, s0, s1, EC, a.expo);
+    if (!done) done = !solve_step(st, s0, s1, EC, a.expo, tolerance);
     if (__all_sync(0xffffffffu, done)) break;
   }
   const float tau = st.tau;
@@ -610,7 +620,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
     const size_t out = (size_t)(w.s.q0 + tok) * a.H + kvh * a.G + g_head;
     store_share<D>(a.o + out * D, s8, acc);
     if (sl == 0) {
-      a.tau[out] = tau;
+      a.tau[out] = (kMany ? mag * top : top) + tau;
       if (a.support) a.support[out] = support;
     }
   }
@@ -672,10 +682,10 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
     const Pages pages = pages_of(a.c, w.b);
     const __nv_bfloat16* v_head = v + (long long)kvh * a.c.s_head;
     const float* y_row = a.scores + (size_t)row * a.score_stride;
-    float ymax = -INFINITY, floor_y = -INFINITY;
+    float ymax = -INFINITY, floor_y = -INFINITY, zmax = -INFINITY;
 
-    // for_keys(f): f(y, key) with a key per lane (y = -inf: none) for all keys of this warp that are kept and can be in the support,
-    // eight (four records) in flight
+    // for_keys(f): f(value relative to the largest, key) with a key per lane (-inf: none) for all keys of this warp that are kept and can be in the
+    // support, eight (four records) in flight
     const int groups = pos / kGroupKeys + 1;
     const float* max_row = a.group_max + (size_t)row * a.groups;
     // few: group g is warp g mod W's, 32 of a warp's groups are a chunk (so that short rows and runs of neighbouring candidates are
@@ -707,7 +717,7 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
             }
 #pragma unroll
             for (int u = 0; u < 8; ++u)
-              if (at[u] >= 0) f(y[u], at[u]);
+              if (at[u] >= 0) f(y[u] - ymax, at[u]);
           }
         }
       } else {
@@ -725,7 +735,7 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
               y[u] = -INFINITY;
               key[u] = 0;
               if (at < n) {
-                y[u] = info.z * y_row[(size_t)lo * kManyKeys + 8 * at + sl];
+                y[u] = info.z * (y_row[(size_t)lo * kManyKeys + 8 * at + sl] - zmax);
                 key[u] = rec.keys[lo * 32 + at] + sl;
               }
             }
@@ -751,19 +761,24 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
         ymax = fmaxf(ymax, m[i]);
       }
       for (int i = kChunks; i < chunks; ++i) ymax = fmaxf(ymax, max_at(i));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) ymax = fmaxf(ymax, __shfl_xor_sync(0xffffffffu, ymax, o));
+      if (lane == 0) red[red_slot][warp].x = ymax;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < W; ++i) ymax = fmaxf(ymax, red[red_slot][i].x);
+      red_slot ^= 1;
+      floor_y = one_below(ymax);
     } else {
-      for_keys([&](float y, int) { ymax = fmaxf(ymax, y); });
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ymax = fmaxf(ymax, __shfl_xor_sync(0xffffffffu, ymax, o));
-    if (lane == 0) red[red_slot][warp].x = ymax;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < W; ++i) ymax = fmaxf(ymax, red[red_slot][i].x);
-    red_slot ^= 1;
-    floor_y = ymax - 1.0f;
-    if constexpr (kMany) {
-      for (int i = 0; i < rec.items; ++i) floor_y = fmaxf(floor_y, rec.info[(size_t)i * rec.slots].y);
+      float mag = 0.f, thr = -INFINITY;
+      for (int i = 0; i < rec.items; ++i) {
+        const float4 info = rec.info[(size_t)i * rec.slots];
+        mag = info.z;
+        thr = fmaxf(thr, info.y);
+        zmax = fmaxf(zmax, info.w);
+      }
+      ymax = mag * zmax;
+      floor_y = fmaxf(mag * (thr - zmax), -1.0f);
     }
 
     // ---- the threshold of the groups' largest keys as a bound (see the rows kernel)
@@ -792,10 +807,11 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
 
     // ---- candidates
     int cnt = 0;
+    const float floor_rel = kMany ? floor_y : fmaxf(floor_y - ymax, -1.0f);
     for_keys([&](float y, int key) {
-      const unsigned m = __ballot_sync(0xffffffffu, y > floor_y);
+      const unsigned m = __ballot_sync(0xffffffffu, y > floor_rel);
       const int at = cnt + __popc(m & ((1u << lane) - 1u));
-      if (y > floor_y && at < kSeg) {
+      if (y > floor_rel && at < kSeg) {
         my_y[at] = y;
         my_at[at] = key;
       }
@@ -813,8 +829,9 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
 
     // ---- threshold
     TauIter st;
-    st.tau = st.lo = floor_y;
-    st.hi = ymax;
+    st.tau = st.lo = floor_rel;
+    const float tolerance = step_tolerance(ymax);
+    st.hi = 0.f;
     for (int it = 0; it < kMaxSteps; ++it) {
       float s0 = 0.f, s1 = 0.f;
       auto add = [&](float y) {
@@ -832,7 +849,7 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
         for_keys([&](float y, int) { add(y); });
       }
       const float2 sum = row_sum2(s0, s1);
-      if (!solve_step(st, sum.x, sum.y, a.expo_class, a.expo)) break;
+      if (!solve_step(st, sum.x, sum.y, a.expo_class, a.expo, tolerance)) break;
     }
     const float tau = st.tau;
 
@@ -896,7 +913,7 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
       a.o[out * D + threadIdx.x] = __float2bfloat16(o);
     }
     if (threadIdx.x == 0) {
-      a.tau[out] = tau;
+      a.tau[out] = ymax + tau;
       if (a.support) a.support[out] = (int)total.x;
     }
     __syncthreads();                                        // (opart is read before the next row writes it)

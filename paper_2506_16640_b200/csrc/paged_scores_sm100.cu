@@ -348,7 +348,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
         sts_f4(par + 16 * lane, ra, slope, (float)pos, __int_as_float(pos));
       }
       __syncwarp();
-      float bound[NR];                                       // (largest value so far) - 1, the same in every lane
+      // (largest value so far) - 1, the same in every lane.  A group at the bound is written too: where the 1 is lost in rounding (see one_below) it
+      // holds a value as large as any.
+      float bound[NR];
 #pragma unroll
       for (int r = 0; r < NR; ++r) bound[r] = r < rows ? -INFINITY : INFINITY;
       for (int t = 0; t < g.tiles; ++t) {
@@ -387,7 +389,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int r = r0 + u;
-            if (m[u] > bound[r]) score0[(size_t)r * a.score_stride + j] = y[u];
+            if (m[u] >= bound[r]) score0[(size_t)r * a.score_stride + j] = y[u];
             bound[r] = fmaxf(bound[r], m[u] - 1.0f);
             top = lane == r ? m[u] : top;
           }
@@ -537,6 +539,9 @@ __device__ __forceinline__ float bound_from_eight(const float (&z)[8], float mar
   const float bound = m + tau * margin - (1e-5f * margin + 1e-6f * fabsf(m));
   return n > 2 && bound < INFINITY ? bound : -INFINITY;
 }
+
+// best - margin (y_max - 1 in z's units), and below the best where the margin is lost in its rounding
+__device__ __forceinline__ float margin_below(float best, float margin) { return (best - margin) - fabsf(best) * 0x1p-21f; }
 
 template <int HD, bool kAlibi>
 __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __grid_constant__ CUtensorMap map_q,
@@ -952,7 +957,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
           best = max8(top);
           const float bound = bound_from_eight(top, margin, a.expo_class, a.expo);
           flat = __any_sync(0xffffffffu, bound > -INFINITY);
-          thr = fmaxf(thr, fmaxf(best - margin, bound));
+          thr = fmaxf(thr, fmaxf(margin_below(best, margin), bound));
         }
         // One straight pass: maxima of eight columns, and eight columns with a candidate go to the row's records as they are, by predicated
         // stores where some row of the warp has one among 32 columns (a vote for 64: chunk of 2048 over 32768 keys 250 -> 243 us here;
@@ -966,7 +971,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
           for (int q = 0; q < 8; ++q) g[q] = max8(&v[8 * q]);
           const float m_lo = fmaxf(fmaxf(g[0], g[1]), fmaxf(g[2], g[3])), m_hi = fmaxf(fmaxf(g[4], g[5]), fmaxf(g[6], g[7]));
           best = max3(best, m_lo, m_hi);
-          thr = fmaxf(thr, best - margin);
+          thr = fmaxf(thr, margin_below(best, margin));
           if (flat) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) top[q] = fmaxf(top[q], g[q]);
@@ -994,10 +999,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) paged_many_kernel(const __gri
         if (flat && step_no > 0 && (step_no & (step_no + 1)) == 0)
           thr = fmaxf(thr, bound_from_eight(top, margin, a.expo_class, a.expo));
       }
-      // (a = 0: every key is kept and y = 0 for all of them; a that is not a number: there is no bound either)
+      // (bound and best unscaled: a = 0 leaves no bound, and every key is kept)
       if (valid && alive)
-        a.row_info[((size_t)it.unit * a.many_items + it.item) * a.many_slots + slot_row] =
-            make_float4(__int_as_float((int)n_rec), mag > 0.f ? mag * thr : -INFINITY, mag, 0.f);
+        a.row_info[((size_t)it.unit * a.many_items + it.item) * a.many_slots + slot_row] = make_float4(__int_as_float((int)n_rec), thr, mag, best);
     }
   }
 

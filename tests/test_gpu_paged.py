@@ -339,6 +339,57 @@ def test_heads_of_scale_zero_in_units_of_many_work_items(new, lens, H, KH):
     assert torch.equal(got[2][:64, 0].cpu().long(), n) and torch.allclose(got[1][:64, 0].cpu().double(), -n.double().pow(-0.5), rtol=1e-4)
 
 
+@pytest.mark.parametrize("alpha", [1.5, 2.0, 3.0])
+@pytest.mark.parametrize("new,lens,H,KH", [
+    ([1, 3, 1], [257, 300, 1], 4, 2), ([1] * 80, [40 + b for b in range(80)], 8, 4),     # rows of few tokens: a CTA each, 32 lanes,
+    ([1] * 256, [5 + b % 40 for b in range(256)], 40, 8),                                # and eight
+    ([100], [600], 2, 1), ([300, 100], [300, 900], 4, 2), ([256] * 40, [256 + b for b in range(40)], 1, 1),       # the same of longer chunks
+])
+def test_scores_without_room_for_a_bracket(new, lens, H, KH, alpha):
+    # scores beyond 2^24, where y_max - 1 is no float of its own: exact products of powers of two, so the result is the mean of V over the keys
+    # that share the largest score; queries of either sign, so that largest scores are negative too
+    d, page = 64, 16
+    g = torch.Generator().manual_seed(H + len(new))
+    T = sum(new)
+    unit = 2.0 ** 25                                          # of the scores y = (alpha - 1) <q,k>
+    q = torch.zeros((T, H, d))
+    q[..., 0] = 2.0 ** 13 / (alpha - 1.0) * torch.where(torch.rand((T, H), generator=g) < 0.5, -1.0, 1.0)
+    keys, marks, values = [], [], []
+    for n in lens:
+        k = torch.zeros((n, KH, d))
+        m = 128 + torch.randint(0, 128, (n, KH), generator=g)
+        m[torch.rand((n, KH), generator=g) < 4.0 / n] = 254
+        m[torch.rand((n, KH), generator=g) < 4.0 / n] = 129
+        k[..., 0] = m * 2.0 ** 12
+        keys.append(k.to(torch.bfloat16))
+        marks.append(m.double())
+        values.append(torch.randn((n, KH, d), generator=g).to(torch.bfloat16))
+    kc, vc, table = paged.pool(keys, values, page, d, KH, 3, "cuda")
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+    pr = dict(q=q.to(torch.bfloat16).cuda(), kc=kc, vc=vc, table=table, cu=cu, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    o, tau, supp, flags = _run(pr, alpha, sm_scale=1.0, max_q_len=max(new), max_kv_len=max(lens))
+    assert flags == 0
+    o, tau, supp, t, several = o.cpu().double(), tau.cpu().double(), supp.cpu(), 0, 0
+    sign = q[..., 0].sign().double()
+    for b, (n, L) in enumerate(zip(new, lens)):
+        j, i = torch.arange(L), torch.arange(L - n, L)[:, None]
+        for h in range(H) if b % 16 == 0 or len(new) < 60 else (b % H,):
+            y = sign[t:t + n, h, None] * unit * marks[b][:, h // (H // KH)]
+            y = torch.where(j <= i, y, -torch.inf)
+            top = y.amax(1, keepdim=True)
+            ties = (y == top).double()
+            count, v = ties.sum(1, keepdim=True), values[b][:, h // (H // KH)].double()
+            several += int((count > 1).sum())
+            # p = 1 / count within e / |t| times the 1e-7 at which the iteration stops (t = -count^(1 - alpha), count <= 40: 1e-5 of p for alpha = 3),
+            # or a mass within 1.6e-6 of 1; one rounding of O
+            assert bool(((o[t:t + n, h] - ties @ v / count).abs() <= 2.0 ** -8 * (ties @ v / count).abs() + 2e-5 * (ties @ v.abs()) / count).all()), (b, h)
+            assert torch.equal(supp[t:t + n, h].long(), count[:, 0].long()), (b, h)
+            want = top - count.pow(1.0 - alpha)
+            assert bool(((tau[t:t + n, h, None] - want).abs() <= 2.0 ** -23 * want.abs()).all()), (b, h)
+        t += n
+    assert several > 0
+
+
 def test_offsets_beyond_32_bits():
     # a pool of more than 2^32 bytes, the sequence's pages at its end
     d, KH, page = 128, 2, 256
