@@ -67,8 +67,8 @@ struct SideStream {
   cudaStream_t stream = nullptr;
   cudaEvent_t fork = nullptr, join = nullptr;
 };
-cudaError_t side_stream(SideStream** out);
-bool side_stream_made();   // whether the thread has it already on this device
+// nullptr: work of `stream` cannot be forked to it now (see the definition) and runs one after the other
+cudaError_t side_stream(cudaStream_t stream, SideStream** out);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // y^e and y^(e-1) of a clamped y >= 0 (0 where the entry is outside the support: ok == false), with the

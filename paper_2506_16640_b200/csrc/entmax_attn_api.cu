@@ -52,12 +52,23 @@ namespace {
 thread_local SideStream g_side[64];
 }  // namespace
 
-cudaError_t side_stream(SideStream** out) {
+// A stream that has been forked from one under capture is part of that capture until it ends, not only until the join: another call of the thread
+// in between, eager or under another capture, cannot use it.  None is made during a capture either.
+cudaError_t side_stream(cudaStream_t stream, SideStream** out) {
+  *out = nullptr;
   int dev = 0;
   cudaError_t err = cudaGetDevice(&dev);
   if (err != cudaSuccess) return err;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   SideStream& s = g_side[dev];
+  cudaStreamCaptureStatus mine = cudaStreamCaptureStatusNone, its = cudaStreamCaptureStatusNone;
+  unsigned long long my_id = 0, its_id = 0;
+  err = cudaStreamGetCaptureInfo(stream, &mine, &my_id);
+  if (err == cudaSuccess && s.stream) err = cudaStreamGetCaptureInfo(s.stream, &its, &its_id);
+  if (err != cudaSuccess) return err;
+  const bool captured = mine != cudaStreamCaptureStatusNone;
+  if (!s.stream && captured) return cudaSuccess;
+  if (its != cudaStreamCaptureStatusNone && !(captured && my_id == its_id)) return cudaSuccess;
   if (!s.stream) {
     cudaStream_t st = nullptr;
     cudaEvent_t e0 = nullptr, e1 = nullptr;
@@ -73,11 +84,6 @@ cudaError_t side_stream(SideStream** out) {
   }
   *out = &s;
   return cudaSuccess;
-}
-
-bool side_stream_made() {
-  int dev = 0;
-  return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64 && g_side[dev].stream != nullptr;
 }
 
 int fail_cuda(cudaError_t err) {
@@ -366,11 +372,12 @@ int bwd_impl(const entmax_attn_params* params, const void* q, const void* k, con
     if (err != cudaSuccess) return fail_cuda(err);
   }
   // with a score sweep ahead (bf16, no saved supports) the accumulators are cleared beside it, otherwise in line
-  const bool clear_aside = p.dtype == ENTMAX_ATTN_DTYPE_BF16 && !fwd_workspace && !saved_supports;
   SideStream* side = nullptr;
-  if (clear_aside) {
-    err = side_stream(&side);
+  if (p.dtype == ENTMAX_ATTN_DTYPE_BF16 && !fwd_workspace && !saved_supports) {
+    err = side_stream(stream, &side);
     if (err != cudaSuccess) return fail_cuda(err);
+  }
+  if (side) {
     err = cudaEventRecord(side->fork, stream);
     if (err == cudaSuccess) err = cudaStreamWaitEvent(side->stream, side->fork, 0);
     if (err == cudaSuccess) err = cudaMemsetAsync(acc_dk, 0, acc_bytes, side->stream);
@@ -426,7 +433,7 @@ int bwd_impl(const entmax_attn_params* params, const void* q, const void* k, con
                          device_status, stream);
       if (err != cudaSuccess) return fail_cuda(err);
       if (g_prof_stop[1]) cudaEventRecord(g_prof_stop[1], stream);
-      err = cudaStreamWaitEvent(stream, side->join, 0);     // the accumulators are clear from here on
+      if (side) err = cudaStreamWaitEvent(stream, side->join, 0);     // the accumulators are clear from here on
       if (err != cudaSuccess) return fail_cuda(err);
       err = launch_row_bwd(p, q, k, v, d_o, scale, tau, list_cnt, entries, dq, acc_dk, acc_dv, dc_rows, fb_count,
                            fb_list, tile_mask, tile_flag, tile_list, tile_count, device_status, 0, kListCap, stream);

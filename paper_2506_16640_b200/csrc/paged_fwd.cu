@@ -1156,14 +1156,13 @@ extern "C" int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const
     if (e == cudaSuccess) e = launch_paged_many(a, q, k_cache, params->q_stride_t, params->q_stride_h, n, stream);
     return e == cudaSuccess ? launch_solve<true>(a, v_cache, 0, n * a.c.KH, stream) : e;
   };
-  // (no stream is made while one is being captured: such a first call goes one after the other)
-  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-  const bool fork = l.both && (side_stream_made() || (cudaStreamIsCapturing(stream, &capture) == cudaSuccess &&
-                                                      capture == cudaStreamCaptureStatusNone));
-  if (fork) {
-    SideStream* side = nullptr;
-    err = side_stream(&side);
-    if (err == cudaSuccess) err = cudaEventRecord(side->fork, stream);
+  SideStream* side = nullptr;
+  if (l.both) {
+    err = side_stream(stream, &side);
+    if (err != cudaSuccess) return fail_cuda(err);
+  }
+  if (side) {
+    err = cudaEventRecord(side->fork, stream);
     if (err == cudaSuccess) err = cudaStreamWaitEvent(side->stream, side->fork, 0);
     if (err != cudaSuccess) return fail_cuda(err);
     err = run_few(a, 0, a.c.B, side->stream);

@@ -509,6 +509,35 @@ def test_short_and_long_chunks_side_by_side():
     assert torch.equal(out["o"], got[0])
 
 
+def test_eager_call_while_another_stream_of_the_thread_is_captured():
+    # the library's second stream is part of the first graph's capture until that ends: the other call does without it
+    new, lens = [1] * 9 + [100, 2, 60], [300, 20, 1, 77, 256, 40, 129, 9, 500, 700, 64, 60]
+    pr = _problem(new, lens, 4, 2, 64, 16)
+    args = (pr["q"], pr["kc"], pr["vc"], 1.5, pr["table"], pr["lens"], pr["cu"])
+
+    def buffers():
+        return dict(o=torch.zeros((sum(new), 4, 64), dtype=torch.bfloat16, device="cuda"), tau=torch.zeros((sum(new), 4), device="cuda"),
+                    workspace=torch.empty(1 << 26, dtype=torch.uint8, device="cuda"))
+
+    want, captured, eager = buffers(), buffers(), buffers()
+    binding.entmax_attn_paged_fwd(*args, **want)             # (the second stream is there from now on)
+    torch.cuda.synchronize()
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, capture_error_mode="relaxed"):
+        binding.entmax_attn_paged_fwd(*args, **captured)
+        binding.entmax_attn_paged_fwd(*args, stream=other, **eager)
+        binding.entmax_attn_paged_fwd(*args, **captured)
+    other.synchronize()
+    assert torch.equal(eager["o"], want["o"]) and torch.equal(eager["tau"], want["tau"])
+    assert bool((captured["o"] == 0).all())
+    for _ in range(2):
+        captured["o"].zero_()
+        graph.replay()
+        binding.entmax_attn_paged_fwd(*args, **eager)
+        torch.cuda.synchronize()
+        assert torch.equal(captured["o"], want["o"]) and torch.equal(captured["tau"], want["tau"]) and torch.equal(eager["o"], want["o"])
+
+
 # ------------------------------------------------------------------------------------------------ append
 def _append_problem(new, lens, H, KH, d, page, seed=0, layout="tokens"):
     g = torch.Generator().manual_seed(seed)
