@@ -363,6 +363,17 @@ def _new_on(stream, like, shape, dtype):
         return like.new_empty(shape, dtype=dtype)
 
 
+def _clear_status(status, stream):
+    """What the library does at the start of a call, for a call that has nothing to launch."""
+    if status is None:
+        return
+    if stream is None:
+        status.zero_()
+    else:
+        with torch.cuda.stream(stream):
+            status.zero_()
+
+
 def _append_layout(what, q, k, v, k_cache, v_cache, block_table, kv_len, cu_q, rotation, interleaved, q_out, status):
     T, KH, D = k.shape if k.dim() == 3 else (0, 0, 0)
     ks, vs = _row_strides("k", k, KH, D), _row_strides("v", v, KH, D)
@@ -406,6 +417,7 @@ def entmax_attn_paged_append(q, k, v, k_cache, v_cache, block_table, kv_len, cu_
     if q is not None and q_out is None:
         q_out = _new_on(stream, q, (T, H, D), torch.bfloat16)
     if T == 0:
+        _clear_status(status, stream)
         return q_out
     rc = _call_on(device, lambda: load().entmax_attn_paged_append(
         cache, params, _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(rotation), _ptr(cu_q), kv_len.data_ptr(), block_table.data_ptr(), _ptr(q_out),
@@ -459,6 +471,7 @@ def entmax_attn_paged_fwd(q, k_cache, v_cache, alpha, block_table, kv_len, cu_q=
     if tau is None:
         tau = _new_on(stream, q, (T, H), torch.float32)
     if T == 0:
+        _clear_status(status, stream)
         return o, tau, support_size
     if workspace is None:
         workspace = _new_on(stream, q, (nbytes,), torch.uint8)

@@ -171,6 +171,20 @@ def test_reference_pins():
     assert paged.rotate(x, turn, torch.tensor([0]), True).tolist() == [[[-2.0, 1.0, -4.0, 3.0]]]
 
 
+def test_calls_without_new_tokens_clear_the_status():
+    # nothing is launched, and what an earlier call reported does not stay behind
+    from paper_2506_16640_b200 import binding
+    kc = torch.zeros((10, 16, 2, 64), dtype=torch.bfloat16)
+    table, lens, cu = torch.zeros((3, 4), dtype=torch.int32), torch.ones(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    q, k = torch.zeros((0, 4, 64), dtype=torch.bfloat16), torch.zeros((0, 2, 64), dtype=torch.bfloat16)
+    status = torch.full((binding.STATUS_WORDS,), 5, dtype=torch.int32)
+    assert binding.entmax_attn_paged_append(q, k, k, kc, kc, table, lens, cu, status=status).shape == q.shape
+    assert int(status.abs().sum()) == 0
+    status.fill_(5)
+    o, tau, _ = binding.entmax_attn_paged_fwd(q, kc, kc, 1.5, table, lens, cu, status=status)
+    assert o.shape == q.shape and tau.shape == (0, 4) and int(status.abs().sum()) == 0
+
+
 _BOUNDS = r"""
 #include <cstdio>
 #include <random>
