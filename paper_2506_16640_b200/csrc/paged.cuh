@@ -43,14 +43,14 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedCache& c, int b) {
   return s;
 }
 
-// Largest b with cu_q[b] / div + b * add <= x, by the whole warp (every lane returns it): 32 candidates a step.
-__device__ __forceinline__ int find_seq(const PagedCache& c, int x, int div, int add) {
+// Largest b with cu_q[b] <= x, the sequence of row x, by the whole warp (every lane returns it): 32 candidates a step.
+__device__ __forceinline__ int find_seq(const PagedCache& c, int x) {
   const int lane = threadIdx.x & 31;
   int lo = 0, n = c.B;                    // the answer is in [lo, lo + n)
   while (n > 1) {
     const int step = (n + 31) / 32;
     const int b = lo + lane * step;
-    const bool le = lane * step < n && (lane == 0 || clamped_cu(c, b) / div + b * add <= x);
+    const bool le = lane * step < n && (lane == 0 || clamped_cu(c, b) <= x);
     const unsigned m = __ballot_sync(0xffffffffu, le);
     const int k = 31 - __clz(m);          // (a prefix of the lanes; lane 0 is always in it)
     lo += k * step;
@@ -109,7 +109,7 @@ struct PagedArgs {
   struct PagedBlock* blocks;  // "many": what is known of each block of the slice
   int32_t* order;             // its blocks that have work, those with the longest rows first
   int32_t* counters;          // see Counter
-  int32_t* spilled;           // rows whose candidates did not fit the list of the kernel that takes eight lanes per row
+  int32_t* spilled;           // rows whose candidates did not fit their list in the kernel that takes eight or 32 lanes per row
   __nv_bfloat16* o;
   float* tau;
   int32_t* support;

@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32) paged_append_kernel(const _
   const long long t_long = w / a.parts;
   if (t_long >= a.c.T) return;
   const int t = (int)t_long, part = (int)(w - t_long * a.parts);
-  const int b = a.c.cu_q ? find_seq(a.c, t, 1, 0) : t / (a.c.T / a.c.B);
+  const int b = a.c.cu_q ? find_seq(a.c, t) : t / (a.c.T / a.c.B);
   const PagedSeq s = paged_seq(a.c, b);
   if (t < s.q0 || t >= s.q0 + s.n) return;       // a row behind the last sequence
   const int pos = s.len - s.n + (t - s.q0);

@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const __grid_c
   if (blockIdx.x > 0) {
     // warps take tokens in turn, lanes heads
     for (int t = (blockIdx.x - 1) * (kPlanThreads / 32) + warp; t < a.c.T; t += (gridDim.x - 1) * (kPlanThreads / 32)) {
-      const int b = a.c.cu_q ? find_seq(a.c, t, 1, 0) : t / (a.c.T / a.c.B);
+      const int b = a.c.cu_q ? find_seq(a.c, t) : t / (a.c.T / a.c.B);
       const PagedSeq s = paged_seq(a.c, b);
       if (t < s.q0 || t >= s.q0 + s.n || !paged_ok(a, s) || paged_few(a, s)) continue;
       for (int h = lane; h < a.H; h += 32) a.row_scale[(size_t)t * a.H + h] = paged_scale(a, h, s.len - s.n + t - s.q0);
@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, L == 8 ? 8 : 6) paged_rows_ke
 // ================================================================================================== row
 constexpr int kCtaWarps = 8;
 constexpr int kSeg = 256;            // list entries of a warp
-constexpr int kCtaRows = 2 * 148, kLongRow = 4096, kRows8Worth = 9472;   // (see solve_lanes)
+constexpr int kLongRow = 4096, kRows8Warps = 64;     // (see solve_lanes)
 constexpr int kChunks = 8;           // chunks of 32 groups of a warp whose maxima stay in shared memory
 
 // kSpilled: the rows listed by the rows kernel, by CTAs that stay; otherwise a CTA for each of the n_slots row slots
@@ -923,11 +923,11 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) paged_row_kernel(const __gr
 // Lanes of a row in the solve of a launch; 0: a CTA.  A CTA per row where all fit the machine at once (two to an SM), which takes 8 us for the
 // shortest rows, and for two or three rounds of longer ones: 256 rows of 65536 keys 16 us against 27 with a warp each, 320 of 48222 24 against
 // 54, 512 of 16384 18 against 23, 384 of 6000 at c = 1 21 against 26; but 576 of 4096 18 against 18, 448 of 2048 16 against 14, 640 of 4096
-// 22 against 15, 1120 of 45231 64 against 55.  Eight lanes where there are more rows than warps to keep (37000 rows of chunks 18 us against
-// 39 with a warp each).
+// 22 against 15, 1120 of 45231 64 against 55.  Eight lanes where there are more rows than the machine holds warps, 64 to an SM (37000 rows of
+// chunks 18 us against 39 with a warp each).
 int solve_lanes(const PagedArgs& a, long long rows) {
   const int rounds = a.max_kv <= kLongRow ? 1 : a.max_kv <= 4 * kLongRow ? 2 : 3;
-  return rows <= rounds * kCtaRows ? 0 : rows < kRows8Worth ? 32 : 8;
+  return rows <= rounds * 2 * a.sms ? 0 : rows < kRows8Warps * a.sms ? 32 : 8;
 }
 
 template <int D, bool kMany, int L>
