@@ -538,6 +538,125 @@ def test_eager_call_while_another_stream_of_the_thread_is_captured():
         assert torch.equal(captured["o"], want["o"]) and torch.equal(captured["tau"], want["tau"]) and torch.equal(eager["o"], want["o"])
 
 
+@pytest.mark.parametrize("new", [1, 150])
+def test_equal_logits_of_128(new):
+    # every visible key in the support, and every one of its V rows gathered, four rows of 128 in flight
+    pr = _problem([new, 1], [2600, 700], 2, 1, 128, 16, plant=False)
+    pr["q"].zero_()
+    got = _run(pr, 1.5)
+    _check(pr, 1.5, got)
+    assert torch.equal(got[2][:new, 0].cpu().long(), torch.arange(2600 - new + 1, 2601))
+
+
+@pytest.mark.parametrize("sigma", [0.02, 0.3])
+@pytest.mark.parametrize("alpha", [1.25, 1.5, 1.9, 2.0])
+def test_flat_rows_of_128(sigma, alpha):
+    pr = _problem([1, 90], [2000, 1300], 4, 2, 128, 32, sigma=sigma, plant=False)
+    _check(pr, alpha, _run(pr, alpha))
+
+
+@pytest.mark.parametrize("new,lens,H,KH,alpha", [([400, 390], [2600, 400], 8, 2, 1.5), ([1] * 50, [2000 - 7 * b for b in range(50)], 32, 4, 1.25),
+                                                 ([1] * 3 + [700], [9001, 30, 5000, 700], 4, 4, 2.0)])
+def test_more_rows_of_128_with_long_supports_than_lists_hold(new, lens, H, KH, alpha):
+    # as for head_dim 64; rows whose lists overflow are walked by a CTA
+    pr = _problem(new, lens, H, KH, 128, 32, sigma=0.3, plant=False)
+    pr["q"][::2] = 0
+    _check(pr, alpha, _run(pr, alpha), heads=[0, H - 1], skip=range(3, len(new), 5) if len(new) > 4 else (), rows=[0, 1, 170, 389, 699])
+
+
+@pytest.mark.parametrize("new,H,KH,sigma", [(1, 16, 2, 1.0), (40, 1, 1, 1.0), (1, 4, 1, 0.05), (20, 2, 1, 0.05)])
+def test_long_contexts_of_128(new, H, KH, sigma):
+    pr = _problem([new], [40001], H, KH, 128, 64, sigma=sigma, plant=sigma == 1.0)
+    sc = _scales(H, 5, "length") if sigma == 1.0 else None
+    _check(pr, 1.5, _run(pr, 1.5, sc), sc, heads=[0, H - 1], rows=[0, new // 2, new - 1])
+
+
+@pytest.mark.parametrize("alpha", [1.1, 2.5, 3.0, 8.0])
+@pytest.mark.parametrize("new,lens", [([1, 1], [9000, 4097]), ([80, 3], [6000, 2500]), ([1] * 90, [1500 + b for b in range(90)])])
+def test_far_alphas_over_long_contexts(alpha, new, lens):
+    pr = _problem(new, lens, 4, 2, 64, 16, seed=9)
+    sc = _scales(4, 7, "length")
+    _check(pr, alpha, _run(pr, alpha, sc), sc, skip=range(2, len(new), 3), rows=[0, 40, 79])
+
+
+MIXES = [([1] * 7, [1, 16, 17, 300, 33, 64, 129], 4, 2, 64, 16), ([5, 1, 0, 3, 8], [700, 1, 90, 3, 8], 8, 2, 128, 32),
+         ([1] * 9 + [100, 2, 60], [300, 20, 1, 77, 256, 40, 129, 9, 500, 700, 64, 60], 4, 2, 64, 16), ([130, 259], [1000, 259], 6, 2, 128, 16),
+         ([300], [300], 8, 1, 64, 128), ([64], [9000], 4, 2, 64, 16), ([2, 5], [300, 6], 128, 1, 64, 32), ([1] * 300, [5] * 300, 40, 8, 64, 16)]
+
+
+def _paged_workspace(pr, hints):
+    T = sum(pr["new"])
+    cache = binding._paged_cache("workspace", pr["kc"], pr["vc"], pr["table"], pr["lens"], pr["cu"], None, T, pr["kc"].device)
+    params = binding.PagedParams(T, pr["H"], *hints, 1.5, 0.0, pr["H"] * pr["d"], pr["d"])
+    return binding.entmax_attn_paged_workspace_bytes(cache, params, False)
+
+
+@pytest.mark.parametrize("hinted", [False, True])
+@pytest.mark.parametrize("new,lens,H,KH,d,page", MIXES)
+def test_attention_writes_nothing_outside_its_outputs(new, lens, H, KH, d, page, hinted):
+    from test_gpu_robustness import Guarded
+    pr = _problem(new, lens, H, KH, d, page, seed=H)
+    hints = (max(new), max(lens)) if hinted else (0, 0)
+    T = sum(new)
+    sc = [t.cuda() for t in _scales(H, 4, "length")]
+    slopes = torch.linspace(0.0, 0.5, H, device="cuda")
+    inputs = {}
+    for n in ("q", "kc", "vc", "table", "cu", "lens"):
+        inputs[n] = Guarded(tuple(pr[n].shape), pr[n].dtype)
+        inputs[n].t.copy_(pr[n])
+    o, tau, supp = Guarded((T, H, d), torch.bfloat16), Guarded((T, H), torch.float32), Guarded((T, H), torch.int32)
+    status, ws = Guarded((binding.STATUS_WORDS,), torch.int32), Guarded((_paged_workspace(pr, hints),), torch.uint8)
+    i = {n: g.t for n, g in inputs.items()}
+    for al in (None, slopes):
+        binding.entmax_attn_paged_fwd(i["q"], i["kc"], i["vc"], 1.5, i["table"], i["lens"], i["cu"], *sc, alibi_slopes=al, max_q_len=hints[0],
+                                      max_kv_len=hints[1], o=o.t, tau=tau.t, support_size=supp.t, workspace=ws.t, status=status.t)
+        torch.cuda.synchronize()
+        for name, g in [*inputs.items(), ("O", o), ("tau", tau), ("support", supp), ("status", status), ("workspace", ws)]:
+            g.check(name)
+        for n, g in inputs.items():
+            assert torch.equal(g.t.contiguous().view(torch.uint8), pr[n].contiguous().view(torch.uint8)), n
+        _check(pr, 1.5, (o.t, tau.t, supp.t, int(status.t[0])), _scales(H, 4, "length"), None if al is None else slopes.tolist(),
+               heads=[0, H - 1], skip=range(5, len(new), 7), rows=[0, 1, 100, 299])
+
+
+@pytest.mark.parametrize("new,lens,H,KH,d,page", MIXES)
+def test_results_do_not_depend_on_what_the_workspace_held(new, lens, H, KH, d, page):
+    pr = _problem(new, lens, H, KH, d, page, seed=H)
+    sc = _scales(H, 4, "length")
+    hints = dict(max_q_len=max(new), max_kv_len=max(lens))
+    ws = torch.empty(_paged_workspace(pr, tuple(hints.values())), dtype=torch.uint8, device="cuda")
+    want = None
+    for fill in (0, 0xFF, 0x7F, 0x5A, 0x80):             # zeros, NaN, large numbers of either sign
+        ws.fill_(fill)
+        got = _run(pr, 1.5, sc, workspace=ws, **hints)
+        want = want or got
+        assert all(torch.equal(x, y) for x, y in zip(want[:3], got[:3])) and got[3] == 0
+
+
+@pytest.mark.parametrize("rot,interleaved", [(0, False), (64, False), (32, True)])
+@pytest.mark.parametrize("new,lens,H,KH,d,page", [m for m in MIXES if m[2] < 100])
+def test_append_writes_nothing_outside_its_slots(new, lens, H, KH, d, page, rot, interleaved):
+    from test_gpu_robustness import Guarded
+    qkv, kc, vc, table, cu, kv_len = _append_problem(new, lens, H, KH, d, page)
+    rotation = binding.rotation_table(max(lens), rot) if rot else None
+    guarded = {}
+    for n, t in dict(qkv=qkv, kc=kc, vc=vc, table=table, cu=cu, kv_len=kv_len, rotation=rotation).items():
+        if t is not None:
+            guarded[n] = Guarded(tuple(t.shape), t.dtype)
+            guarded[n].t.copy_(t)
+    guarded["q_out"], guarded["status"] = Guarded((sum(new), H, d), torch.bfloat16), Guarded((binding.STATUS_WORDS,), torch.int32)
+    i = {n: g.t for n, g in guarded.items()}
+    binding.entmax_attn_paged_append(i["qkv"][:, :H], i["qkv"][:, H:H + KH], i["qkv"][:, H + KH:], i["kc"], i["vc"], i["table"], i["kv_len"],
+                                     i["cu"], rotation=i.get("rotation"), interleaved=interleaved, q_out=i["q_out"], status=i["status"])
+    torch.cuda.synchronize()
+    assert int(i["status"][0]) == 0
+    for n, g in guarded.items():
+        g.check(n)
+    _check_append(qkv, H, KH, new, lens, page, rotation, interleaved, (kc, vc), (i["kc"], i["vc"]), table, i["q_out"])
+    for n, t in (("qkv", qkv), ("table", table), ("cu", cu), ("kv_len", kv_len)):
+        assert torch.equal(i[n].view(torch.uint8), t.contiguous().view(torch.uint8)), n
+
+
 # ------------------------------------------------------------------------------------------------ append
 def _append_problem(new, lens, H, KH, d, page, seed=0, layout="tokens"):
     g = torch.Generator().manual_seed(seed)
