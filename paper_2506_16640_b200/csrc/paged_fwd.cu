@@ -9,9 +9,9 @@
 //           lanes, sums take three shuffles, and a warp has four rows' chains of dependent loads under way.  A warp per row where there are
 //           fewer.  Rows with more candidates than their list holds are listed for
 //   row     a CTA per row, for those and for calls of few or long rows.
-// Bound by instructions where the machine is full (182000 rows of prompts 70 us, 68 % of the issue slots), else by the chain maxima - candidates -
-// pages - threshold - V rows: 2048 decode rows 13 us with a warp each, 256 rows of 65536 keys 16 us and 256 flat ones of 8192 (supports of
-// hundreds) 20 us with a CTA each.
+// Bound by instructions where the machine is full (182000 rows of prompts 70 us, 71 % of the issue slots), else by the chain maxima - candidates -
+// pages - threshold - V rows: 2048 decode rows 13 us with a warp each, 256 rows of 65536 keys 15 us and 256 flat ones of 8192 (supports of
+// hundreds) 25 us with a CTA each.
 #include <atomic>
 #include <cmath>
 

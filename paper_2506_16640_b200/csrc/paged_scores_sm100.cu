@@ -78,8 +78,8 @@ __device__ __forceinline__ void load_columns(uint32_t taddr, float (&acc)[N]) {
 
 // The tiles of all sequences and K/V heads, one after another (head by head), are dealt to the CTAs in equal runs: a CTA walks its run as
 // segments, each some tiles of one (sequence, K/V head).  So the machine is full and finishes together whatever the lengths are.
-// Bound by reading K once: 64 single tokens, contexts up to 4096, 8 K/V heads of 128: 318 MB in 57 us (5.6 TB/s, start-up included); five tokens
-// each of 32 sequences over 8192 keys with slopes 94 us (5.7 TB/s).
+// Bound by reading K once: 64 single tokens, contexts up to 4096, 8 K/V heads of 128: 318 MB in 57 us (5.6 TB/s, start-up included; 60 behind a
+// flushed L2); five tokens each of 32 sequences over 8192 keys with slopes 94 us (5.7 TB/s).
 struct FewSegment {
   int b, kvh;            // sequence (of the slice) and K/V head
   int tile, tiles;       // first tile and number of tiles
@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(const __grid_
 
 // =============================================================================================== many
 // Two Q tiles share each K tile; a scheduler warp hands out work items, so that producer, MMA issuer and consumers run ahead of one another across
-// items.  Bound by the MMA at head_dim 128 (2048 tokens over 32768 keys, 16 heads: 266 GFLOP in 211 us, 1.26 PFLOP/s, tensor pipe 71 % busy) and
+// items.  Bound by the MMA at head_dim 128 (2048 tokens over 32768 keys, 16 heads: 266 GFLOP in 210 us, 1.27 PFLOP/s, tensor pipe 70 % busy) and
 // by the consumers' scan at 64, where an accumulator is made in half the time and short rows look at their first tile twice (11402 prompt tokens,
 // 16 heads: 86 us; with the scan left out 38).
 constexpr int BM = 128;
