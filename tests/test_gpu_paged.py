@@ -412,6 +412,34 @@ def test_repeats_are_bit_equal():
         assert all(torch.equal(x, y) for x, y in zip(a[:3], b[:3]))
 
 
+@pytest.mark.parametrize("new,lens,H,KH,d,alpha,sigma", [
+    ([188, 7, 106], [3962, 228, 444], 33, 1, 64, 1.1, 0.02), ([300, 250, 90], [300, 250, 90], 40, 2, 128, 1.5, 1.0),
+    ([482, 334], [482, 334], 33, 1, 128, 1.7, 1.0), ([41] * 20, [125 + 9 * b for b in range(20)], 20, 1, 64, 1.5, 0.3),
+    ([130, 259, 401], [1000, 259, 401], 6, 2, 128, 2.0, 0.3), ([3, 1, 8, 7], [96, 191, 196, 1219], 33, 1, 128, 1.5, 1.0),
+])
+def test_repeats_are_bit_equal_whatever_ran_before(new, lens, H, KH, d, alpha, sigma):
+    # groups that leave rows of a 128-row tile empty: nothing of an earlier kernel's shared memory may show
+    pr = _problem(new, lens, H, KH, d, 16, sigma=sigma)
+    others = [_problem([200, 60], [700, 60], 8, 2, x, 16, sigma=s) for x, s in ((64, 1.0), (128, 0.02), (128, 30.0))]
+    want = _run(pr, alpha)
+    _check(pr, alpha, want, heads=[0, H - 1], rows=[0, 1, 40, 187], skip=range(3, len(new)))
+    for i in range(12):
+        _run(others[i % 3], 1.5)
+        got = _run(pr, alpha)
+        assert all(torch.equal(x, y) for x, y in zip(want[:3], got[:3])), i
+
+
+@pytest.mark.parametrize("H,KH,n", [(6, 2, 150), (33, 1, 100), (4, 2, 190), (20, 1, 61)])
+def test_a_sequence_does_not_depend_on_the_queries_packed_behind_it(H, KH, n):
+    # the last tile of its chunk holds rows of the next sequence (or rows behind the last one)
+    pr = _problem([n, 150], [900, 400], H, KH, 64, 16, rows_behind=70)
+    want = _run(pr, 1.5)
+    for fill in (0.0, 0.01, -3.0, 1e4, float("inf"), float("nan")):
+        pr["q"][n:] = fill
+        got = _run(pr, 1.5)
+        assert all(torch.equal(x[:n], y[:n]) for x, y in zip(want[:3], got[:3])), fill
+
+
 def test_graph_replay_and_second_stream():
     pr = _problem([1, 1, 90], [64, 200, 300], 4, 2, 64, 16)
     sc = [t.cuda() for t in _scales(4, 1, "length")]
