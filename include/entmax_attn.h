@@ -100,6 +100,7 @@ typedef struct {
 #define ENTMAX_ATTN_FLAG_BAD_LENGTH 4      /* entmax_attn_decode_fwd: some kv_len[b] outside [q_len, kv_capacity];
                                               entmax_attn_paged_*: a sequence's lengths do not fit (see there)     */
 #define ENTMAX_ATTN_FLAG_BAD_PAGE 8        /* entmax_attn_paged_*: a page number outside the pool                  */
+#define ENTMAX_ATTN_FLAG_NO_PAGES 16       /* entmax_attn_paged_tables: not enough free pages for some sequence     */
 
 /* Bytes of scratch the caller must pass to entmax_attn_fwd (is_bwd = 0) or entmax_attn_bwd
  * (is_bwd = 1) for these params.  Returns 0 if the params are invalid.  No paper counterpart: the
@@ -379,6 +380,124 @@ int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const entmax_att
                           const int32_t* block_table, const float* beta, const float* gamma, const float* delta,
                           const float* alibi_slopes, void* o, float* tau, int32_t* support_size, void* workspace,
                           size_t workspace_bytes, int32_t* device_status, void* cuda_stream);
+
+/* Tables of a serving step, from the requests' lengths: where each sequence's new tokens go, and what entmax_attn_paged_append,
+ * entmax_attn_paged_fwd and entmax_attn_softmax_paged_fwd take.  (The paper has no counterpart: it does not describe serving.)
+ *   kv_len        in,  device int32 [batch]: tokens each sequence has in the cache.  -1 - n: a sequence of n tokens that the call before left out
+ *   new_len       in,  device int32 [batch]: tokens it gets now (0: none); -1: it has ended, its pages are given back
+ *   block_table   in/out, device int32 [batch][table_stride]: the entries of the pages that the new tokens begin are written, no others
+ *   free_pages    in/out, device int32 [free_capacity]: a stack of the pages nobody holds, taken from its end.  The pages of ended sequences are put on
+ *                 it after the call's own have been taken; a page must belong to one sequence alone to be given back
+ *   free_count    in,  device int32 [1]: pages on the stack;  free_count_out: pages left on it (may be free_count itself)
+ *   kv_len_out    out, device int32 [batch]: kv_len + new_len (may be kv_len itself); 0 for an ended sequence
+ *   cu_q          out, device int32 [batch + 1]: sums of new_len (an ended sequence counts as 0)
+ *   positions     out, device int32 [total_q] or NULL: position of each new token within its sequence
+ *   slots         out, device int64 [total_q] or NULL: page * page_size + place in the page
+ * Sequences get their pages in order.  One whose pages no longer suffice (ENTMAX_ATTN_FLAG_NO_PAGES; those behind it that need a page fare the same), and one that
+ * would be longer than max_pages * page_size or whose kv_len or new_len is out of range (ENTMAX_ATTN_FLAG_BAD_LENGTH), is left out: its kv_len_out is
+ * -1 - n, n its tokens in the cache, which the attention calls leave out as well and a later call takes up again; its new tokens keep
+ * their rows, with positions and slots -1, and it gets no page.  Rows behind cu_q[batch] are left alone; when the new tokens are more than total_q, those behind it are
+ * not written (ENTMAX_ATTN_FLAG_BAD_LENGTH).  A page number outside the pool on the stack or in the table sets ENTMAX_ATTN_FLAG_BAD_PAGE and gives its tokens slot -1
+ * (in the table and on the stack it is passed on, for the attention calls to report); pages that the stack has no room for are flagged the same way and lost.
+ * One launch; results do not depend on its order.  Errors as for entmax_attn_fwd. */
+typedef struct {
+  int32_t batch, total_q;              /* total_q: rows of positions and slots (0 with none)                       */
+  int32_t page_size, num_pages;        /* as in entmax_attn_paged_cache                                            */
+  int32_t max_pages, free_capacity;    /* entries in a row of the table; room on the stack                         */
+  int64_t table_stride;
+} entmax_attn_paged_tables_params;
+int entmax_attn_paged_tables(const entmax_attn_paged_tables_params* params, const int32_t* kv_len, const int32_t* new_len, int32_t* block_table,
+                             int32_t* free_pages, const int32_t* free_count, int32_t* kv_len_out, int32_t* cu_q, int32_t* positions,
+                             int64_t* slots, int32_t* free_count_out, int32_t* device_status, void* cuda_stream);
+
+/* Softmax attention: the limit alpha -> 1 of the family (App. A), with the same scale, slopes and layouts, for models that have such layers next to
+ * alpha-entmax ones or are compared with them (with the scale the paper's SSMax / ASSMax variants).  Row i of query head h:
+ *   z_ij = sm_scale <q_i, k_j>,   x_ij = softcap tanh(z_ij / softcap) - m_h |i - j|,   s_ij = c_i x_ij,
+ *   p_ij = exp(s_ij - lse_i) over the keys the row sees,   O_i = sum_j p_ij v_j;   a row that sees none: O = 0, lse = -inf, no gradient.
+ * Query heads g * kv_head .. g * kv_head + g - 1, g = heads / kv_heads, share a K/V head.
+ *   seq           any length; row i sees the keys j <= i (causal = 1) or all, of those the ones in its range where ranges are given
+ *   softcap       0: scores are not capped
+ *   q, k, v, o    strides in elements, head_dim innermost (all 0: contiguous [batch, heads or kv_heads, seq, head_dim]); at least head_dim, multiples
+ *                 of 8, where their dimension has more than one entry
+ *   row_ranges    in, device int32 [batch, seq, 2], 8-byte aligned: the first key a row sees and one behind the last, or NULL (entmax_attn_row_ranges
+ *                 makes them for documents, prefixes and windows; any ranges will do, empty ones too)
+ *   beta, gamma, delta   in, device float32 [heads], all three or none: c_i = delta + beta (ln n_i)^gamma, n_i the number of keys row i sees
+ *                 (delta for n_i <= 1);  c_rows: in, device float32 [batch, heads, seq] instead of them;  neither: c_i = 1
+ *   alibi_slopes  in, device float32 [heads] or NULL
+ *   o             out, dtype of q;  lse: out, device float32 [batch, heads, seq] contiguous, natural logarithm
+ * Backward:
+ *   o, lse        what the forward call returned;  d_o in
+ *   dq, dk, dv    out (overwritten), dk and dv summed over the query heads that share them
+ *   d_scale_rows  out, device float32 [batch, heads, seq] or NULL: dL/dc_i = sum_j dS_ij x_ij
+ *   dbeta, dgamma, ddelta  out, device float32 [heads], all three or none; they need beta, gamma, delta
+ *   workspace     256-byte aligned, >= entmax_attn_softmax_workspace_bytes(params) bytes; the forward call needs none
+ * Nothing is added up by atomics: results are bitwise reproducible.  Errors as for entmax_attn_fwd (softcap negative or not finite: EINVAL_ALPHA). */
+typedef struct {
+  int64_t b, h, n;                     /* elements between batch rows, heads, tokens                                */
+} entmax_attn_strides;
+typedef struct {
+  int32_t batch, heads, kv_heads, seq, head_dim; /* head_dim in {64, 128}; heads a multiple of kv_heads             */
+  int32_t dtype;                       /* ENTMAX_ATTN_DTYPE_*                                                       */
+  int32_t causal;
+  float sm_scale;                      /* 0 means 1/sqrt(head_dim)                                                  */
+  float softcap;
+  entmax_attn_strides q, k, v, o;
+} entmax_attn_softmax_params;
+typedef struct {
+  const int32_t* row_ranges;
+  const float *beta, *gamma, *delta;
+  const float* c_rows;
+  const float* alibi_slopes;
+} entmax_attn_softmax_terms;           /* any member may be NULL, and the struct itself                             */
+typedef struct {
+  entmax_attn_strides d_o, dq, dk, dv; /* strides, as in the params                                                 */
+  float* d_scale_rows;
+  float *dbeta, *dgamma, *ddelta;
+} entmax_attn_softmax_grads;
+int entmax_attn_softmax_fwd(const entmax_attn_softmax_params* params, const void* q, const void* k, const void* v,
+                            const entmax_attn_softmax_terms* terms, void* o, float* lse, int32_t* device_status, void* cuda_stream);
+size_t entmax_attn_softmax_workspace_bytes(const entmax_attn_softmax_params* params);
+int entmax_attn_softmax_bwd(const entmax_attn_softmax_params* params, const void* q, const void* k, const void* v,
+                            const entmax_attn_softmax_terms* terms, const void* o, const float* lse, const void* d_o,
+                            const entmax_attn_softmax_grads* grads, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes,
+                            int32_t* device_status, void* cuda_stream);
+
+/* The keys each row sees when documents are packed into a batch row: document e of batch row b holds the tokens cu_docs[b][e] ..
+ * cu_docs[b][e+1] - 1, and its tokens see keys of their own document alone.  causal: key j <= i, or j in the document's first
+ * prefix_len[b][e] tokens where those are given; window > 0: of those only j > i - window (not causal: |i - j| < window).  Tokens in no
+ * document (padding) see nothing.
+ *   cu_docs       in,  device int32 [batch, docs + 1], ascending in each row, held to 0 .. seq (the last ones may be empty)
+ *   prefix_len    in,  device int32 [batch, docs] or NULL (only with causal)
+ *   row_ranges    out, device int32 [batch, seq, 2] as entmax_attn_softmax_fwd takes them (its causal is then 0: what is visible is all here) */
+int entmax_attn_row_ranges(int32_t batch, int32_t seq, int32_t docs, int32_t causal, int32_t window, const int32_t* cu_docs,
+                           const int32_t* prefix_len, int32_t* row_ranges, void* cuda_stream);
+
+/* Softmax attention of new tokens over a paged cache, with the cache, packing, scale and slopes of entmax_attn_paged_fwd: the token at position pos sees the
+ * keys j <= pos, with window > 0 only j > pos - window, and n = the number of keys it sees; s_j = c (softcap tanh(z_j / softcap) - m_h (pos - j)).
+ *   q             in,  device bf16 [total_q, q_heads, head_dim] with strides (multiples of 8, at least head_dim)
+ *   beta, gamma, delta   in, device float32 [q_heads]; all three or none (c = 1)
+ *   alibi_slopes  in,  device float32 [q_heads] or NULL
+ *   o             out, device bf16 [total_q, q_heads, head_dim] contiguous;  lse: out, device float32 [total_q, q_heads]
+ *   max_q_len, max_kv_len   the most new tokens and the longest kv_len of any sequence of the call (0: not known): they size the workspace and the
+ *                 launches; a sequence beyond them is left out (ENTMAX_ATTN_FLAG_BAD_LENGTH)
+ *   workspace     device scratch, 256-byte aligned, >= entmax_attn_softmax_paged_workspace_bytes(cache, params, cu_q == NULL) bytes
+ * The rows of a sequence that is left out get O = 0, lse = -inf.  Slots past a sequence's length may hold anything.  K and V are read once per K/V
+ * head (chunks: once per 256 rows of a query head).  Results are bitwise reproducible.  Errors as for entmax_attn_fwd; bf16 only. */
+typedef struct {
+  int32_t total_q, q_heads;
+  int32_t max_q_len, max_kv_len;
+  int32_t window;                      /* 0: none                                                                   */
+  float softcap;                       /* 0: scores are not capped                                                  */
+  float sm_scale;                      /* 0 means 1/sqrt(head_dim)                                                  */
+  int64_t q_stride_t, q_stride_h;
+} entmax_attn_softmax_paged_params;
+size_t entmax_attn_softmax_paged_workspace_bytes(const entmax_attn_paged_cache* cache, const entmax_attn_softmax_paged_params* params,
+                                                 int uniform);
+int entmax_attn_softmax_paged_fwd(const entmax_attn_paged_cache* cache, const entmax_attn_softmax_paged_params* params, const void* q,
+                                  const void* k_cache, const void* v_cache, const int32_t* cu_q, const int32_t* kv_len,
+                                  const int32_t* block_table, const float* beta, const float* gamma, const float* delta,
+                                  const float* alibi_slopes, void* o, float* lse, void* workspace, size_t workspace_bytes,
+                                  int32_t* device_status, void* cuda_stream);
 
 /* Forward pass for callers that cannot provide a workspace.  (The paper has no counterpart: it does
  * not discuss memory management.)

@@ -60,3 +60,52 @@ def entmax_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, beta: Op
     o, tau = _EntmaxAttention.apply(q, k, v, beta, gamma, delta, c_rows, alibi_slopes, float(alpha), bool(causal),
                                     float(sm_scale), bool(keep_supports))
     return (o, tau) if return_tau else o
+
+
+class _SoftmaxAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, causal, softcap, sm_scale):
+        o, lse = binding.entmax_attn_softmax_fwd(q, k, v, causal, beta, gamma, delta, c_rows=c_rows, alibi_slopes=alibi_slopes,
+                                                 row_ranges=row_ranges, softcap=softcap, sm_scale=sm_scale)
+        ctx.save_for_backward(q, k, v, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, o, lse)
+        ctx.causal, ctx.softcap, ctx.sm_scale = causal, softcap, sm_scale
+        ctx.mark_non_differentiable(lse)
+        return o, lse
+
+    @staticmethod
+    def backward(ctx, d_o, _d_lse):
+        q, k, v, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, o, lse = ctx.saved_tensors
+        want_params = beta is not None and any(ctx.needs_input_grad[3:6])
+        want_rows = c_rows is not None and ctx.needs_input_grad[6]
+        if not _kernel_layout(d_o):
+            d_o = d_o.contiguous()
+        dq, dk, dv, dc, grads = binding.entmax_attn_softmax_bwd(
+            q, k, v, o, lse, d_o, ctx.causal, beta, gamma, delta, c_rows=c_rows, alibi_slopes=alibi_slopes, row_ranges=row_ranges,
+            softcap=ctx.softcap, sm_scale=ctx.sm_scale, want_scale_rows=want_rows, want_param_grads=want_params)
+        db, dg, dd = grads if grads is not None else (None, None, None)
+        return dq, dk, dv, db, dg, dd, dc, None, None, None, None, None
+
+
+def _kernel_layout(x):
+    """Whether the kernels can read x [B,H,N,d] as it lies (what autograd hands over may be broadcast: strides of 0)."""
+    D = x.shape[3]
+    return x.stride(3) == 1 and x.data_ptr() % 16 == 0 and all(n == 1 or s >= D and s % 8 == 0 for n, s in zip(x.shape[:3], x.stride()[:3]))
+
+
+def softmax_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, beta: Optional[torch.Tensor] = None,
+                      gamma: Optional[torch.Tensor] = None, delta: Optional[torch.Tensor] = None, *,
+                      c_rows: Optional[torch.Tensor] = None, alibi_slopes: Optional[torch.Tensor] = None,
+                      row_ranges: Optional[torch.Tensor] = None, causal: bool = True, softcap: float = 0.0, sm_scale: float = 0.0,
+                      return_lse: bool = False):
+    """Softmax attention (the alpha -> 1 member of the family) of q [B,H,N,d], k, v [B,G,N,d], H a multiple of G (CUDA tensors, bf16 or fp32, each with
+    strides of its own, d contiguous); differentiable with respect to q, k, v and the scale's parameters beta, gamma, delta (float32 [H]) or
+    table c_rows (float32 [B,H,N]).
+
+    alibi_slopes: float32 [H]; softcap > 0 caps the scores by a tanh; row_ranges: int32 [B,N,2] from binding.entmax_attn_row_ranges (documents,
+    prefixes, windows), with causal=False.  Returns O, or (O, lse).
+
+    To capture a training step into a CUDA graph, let no eager graph of the same leaves live (PyTorch would add up their gradients on that
+    graph's stream)."""
+    o, lse = _SoftmaxAttention.apply(q, k, v, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, bool(causal), float(softcap),
+                                     float(sm_scale))
+    return (o, lse) if return_lse else o

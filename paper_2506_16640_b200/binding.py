@@ -19,7 +19,7 @@ DTYPE_BF16, DTYPE_FP32 = 0, 1
 STATUS_WORDS = 8
 STATUS_FLAGS, STATUS_DENSE_ROWS, STATUS_TILE_SWEEPS, STATUS_TILES = 0, 1, 2, 3
 STATUS_SKIPPED_STEPS, STATUS_SCORED_STEPS = 4, 5
-FLAG_WAIT_EXPIRED, FLAG_BAD_SCALE, FLAG_BAD_LENGTH, FLAG_BAD_PAGE = 1, 2, 4, 8
+FLAG_WAIT_EXPIRED, FLAG_BAD_SCALE, FLAG_BAD_LENGTH, FLAG_BAD_PAGE, FLAG_NO_PAGES = 1, 2, 4, 8, 16
 PAGED_MAX_KV = 1 << 24
 
 
@@ -62,6 +62,37 @@ class PagedParams(ctypes.Structure):
     _fields_ = [("total_q", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("max_q_len", ctypes.c_int32),
                 ("max_kv_len", ctypes.c_int32), ("alpha", ctypes.c_float), ("sm_scale", ctypes.c_float),
                 ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64)]
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("n", ctypes.c_int64)]
+
+
+class SoftmaxParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("seq", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32), ("sm_scale", ctypes.c_float),
+                ("softcap", ctypes.c_float), ("q", Strides), ("k", Strides), ("v", Strides), ("o", Strides)]
+
+
+class SoftmaxTerms(ctypes.Structure):
+    _fields_ = [("row_ranges", ctypes.c_void_p), ("beta", ctypes.c_void_p), ("gamma", ctypes.c_void_p), ("delta", ctypes.c_void_p),
+                ("c_rows", ctypes.c_void_p), ("alibi_slopes", ctypes.c_void_p)]
+
+
+class SoftmaxGrads(ctypes.Structure):
+    _fields_ = [("d_o", Strides), ("dq", Strides), ("dk", Strides), ("dv", Strides), ("d_scale_rows", ctypes.c_void_p),
+                ("dbeta", ctypes.c_void_p), ("dgamma", ctypes.c_void_p), ("ddelta", ctypes.c_void_p)]
+
+
+class SoftmaxPagedParams(ctypes.Structure):
+    _fields_ = [("total_q", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("max_q_len", ctypes.c_int32), ("max_kv_len", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("softcap", ctypes.c_float), ("sm_scale", ctypes.c_float), ("q_stride_t", ctypes.c_int64),
+                ("q_stride_h", ctypes.c_int64)]
+
+
+class PagedTablesParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("total_q", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("free_capacity", ctypes.c_int32), ("table_stride", ctypes.c_int64)]
 
 
 class WsLayout(ctypes.Structure):
@@ -129,6 +160,21 @@ def load():
         lib.entmax_attn_paged_fwd.restype = ctypes.c_int
         lib.entmax_attn_paged_fwd.argtypes = [cp, gp, vp, vp, vp, ip, ip, ip, fp, fp, fp, fp, vp, fp, ip, vp, ctypes.c_size_t,
                                               ip, vp]
+        sp, tp, sg, kp = (ctypes.POINTER(t) for t in (SoftmaxParams, SoftmaxTerms, SoftmaxGrads, SoftmaxPagedParams))
+        lib.entmax_attn_softmax_fwd.restype = ctypes.c_int
+        lib.entmax_attn_softmax_fwd.argtypes = [sp, vp, vp, vp, tp, vp, fp, ip, vp]
+        lib.entmax_attn_softmax_workspace_bytes.restype = ctypes.c_size_t
+        lib.entmax_attn_softmax_workspace_bytes.argtypes = [sp]
+        lib.entmax_attn_softmax_bwd.restype = ctypes.c_int
+        lib.entmax_attn_softmax_bwd.argtypes = [sp, vp, vp, vp, tp, vp, fp, vp, sg, vp, vp, vp, vp, ctypes.c_size_t, ip, vp]
+        lib.entmax_attn_row_ranges.restype = ctypes.c_int
+        lib.entmax_attn_row_ranges.argtypes = [ctypes.c_int32] * 5 + [ip, ip, ip, vp]
+        lib.entmax_attn_softmax_paged_workspace_bytes.restype = ctypes.c_size_t
+        lib.entmax_attn_softmax_paged_workspace_bytes.argtypes = [cp, kp, ctypes.c_int]
+        lib.entmax_attn_softmax_paged_fwd.restype = ctypes.c_int
+        lib.entmax_attn_softmax_paged_fwd.argtypes = [cp, kp, vp, vp, vp, ip, ip, ip, fp, fp, fp, fp, vp, fp, vp, ctypes.c_size_t, ip, vp]
+        lib.entmax_attn_paged_tables.restype = ctypes.c_int
+        lib.entmax_attn_paged_tables.argtypes = [ctypes.POINTER(PagedTablesParams)] + [ip] * 11 + [vp]
         lib.entmax_attn_saved_bytes.restype = ctypes.c_size_t
         lib.entmax_attn_saved_bytes.argtypes = [pp]
         lib.entmax_attn_save_supports.restype = ctypes.c_int
@@ -483,6 +529,210 @@ def entmax_attn_paged_fwd(q, k_cache, v_cache, alpha, block_table, kv_len, cu_q=
         workspace.numel(), _ptr(status), _stream_ptr(stream)))
     _check(rc, what)
     return o, tau, support_size
+
+
+def _softmax_paged_layout(what, q, k_cache, v_cache, block_table, kv_len, cu_q, beta, gamma, delta, alibi_slopes, softcap, window, sm_scale,
+                          max_q_len, max_kv_len, o, lse, status):
+    T, H, D = q.shape if q.dim() == 3 else (0, 0, 0)
+    params = SoftmaxPagedParams(T, H, int(max_q_len), int(max_kv_len), int(window), float(softcap), float(sm_scale), *_row_strides("q", q, H, D))
+    device = q.device
+    cache = _paged_cache(what, k_cache, v_cache, block_table, kv_len, cu_q, status, T, device)
+    if cache.head_dim != D:
+        raise EntmaxAttnError("%s: q and the cache disagree on head_dim" % what)
+    _check_tensors(what, device, ("beta", beta, (H,), torch.float32), ("gamma", gamma, (H,), torch.float32), ("delta", delta, (H,), torch.float32),
+                   ("alibi_slopes", alibi_slopes, (H,), torch.float32), ("o", o, (T, H, D), torch.bfloat16), ("lse", lse, (T, H), torch.float32))
+    # (0 bytes: parameters that the call itself refuses, with the reason)
+    nbytes = int(load().entmax_attn_softmax_paged_workspace_bytes(ctypes.byref(cache), ctypes.byref(params), int(cu_q is None))) if T else 0
+    return ctypes.byref(cache), ctypes.byref(params), T, H, D, nbytes
+
+
+def entmax_attn_softmax_paged_fwd(q, k_cache, v_cache, block_table, kv_len, cu_q=None, beta=None, gamma=None, delta=None, *,
+                                  alibi_slopes=None, softcap=0.0, window=0, sm_scale=0.0, max_q_len=0, max_kv_len=0, o=None, lse=None,
+                                  workspace=None, status=None, stream=None):
+    """Softmax attention of new tokens over a paged cache that already holds their keys and values: tensors, packing and lengths as for
+    entmax_attn_paged_fwd; softcap caps the scores by a tanh, window > 0 leaves a token its last `window` keys.
+    Returns (o [T, H, d], lse [T, H])."""
+    what = "entmax_attn_softmax_paged_fwd"
+    where = (what, q.numel(), k_cache.numel(), block_table.numel(), max_q_len, max_kv_len)
+    key = (softcap, window, sm_scale, _layout_of(q, k_cache, v_cache, block_table, kv_len, cu_q, beta, gamma, delta, alibi_slopes, o, lse, status))
+    known = _layouts.get(where)
+    cache, params, T, H, D, nbytes = known[1] if known is not None and known[0] == key else _keep(where, key, _softmax_paged_layout(
+        what, q, k_cache, v_cache, block_table, kv_len, cu_q, beta, gamma, delta, alibi_slopes, softcap, window, sm_scale, max_q_len, max_kv_len,
+        o, lse, status))
+    device = q.get_device()
+    if o is None:
+        o = _new_on(stream, q, (T, H, D), torch.bfloat16)
+    if lse is None:
+        lse = _new_on(stream, q, (T, H), torch.float32)
+    if T == 0:
+        _clear_status(status, stream)
+        return o, lse
+    if workspace is None:
+        workspace = _new_on(stream, q, (nbytes,), torch.uint8)
+    elif workspace.dtype != torch.uint8 or workspace.get_device() != device or not workspace.is_contiguous():
+        raise EntmaxAttnError("%s: workspace must be a contiguous uint8 tensor on the device of q" % what)
+    rc = _call_on(device, lambda: load().entmax_attn_softmax_paged_fwd(
+        cache, params, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(cu_q), kv_len.data_ptr(), block_table.data_ptr(), _ptr(beta),
+        _ptr(gamma), _ptr(delta), _ptr(alibi_slopes), o.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.numel(), _ptr(status),
+        _stream_ptr(stream)))
+    _check(rc, what)
+    return o, lse
+
+
+def _check_tensors(what, device, *named):
+    for name, t, shape, dtype in named:
+        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.device != device):
+            raise EntmaxAttnError("%s: %s must be a contiguous %s %s tensor on %s" % (what, name, dtype, list(shape), device))
+
+
+def _tables_layout(what, kv_len, new_len, block_table, free_pages, free_count, page_size, num_pages, total_q, kv_len_out, cu_q, positions, slots,
+                   free_count_out, status):
+    i32, device = torch.int32, kv_len.device
+    if block_table.dim() != 2 or block_table.dtype != i32 or block_table.device != device or block_table.shape[1] > 1 and block_table.stride(1) != 1:
+        raise EntmaxAttnError("%s: block_table must be an int32 [batch, max_pages] tensor with contiguous rows, on the device of kv_len" % what)
+    B, max_pages = block_table.shape
+    _check_tensors(what, device, ("kv_len", kv_len, (B,), i32), ("new_len", new_len, (B,), i32), ("free_pages", free_pages, (free_pages.numel(),), i32),
+                   ("free_count", free_count, (1,), i32), ("kv_len_out", kv_len_out, (B,), i32), ("cu_q", cu_q, (B + 1,), i32),
+                   ("positions", positions, (total_q,), i32), ("slots", slots, (total_q,), torch.int64), ("free_count_out", free_count_out, (1,), i32))
+    if status is not None and (status.dtype != i32 or status.numel() < STATUS_WORDS or not status.is_contiguous() or status.device != device):
+        raise EntmaxAttnError("%s: status must be a contiguous int32 tensor of %d words on the device of kv_len" % (what, STATUS_WORDS))
+    return ctypes.byref(PagedTablesParams(B, int(total_q), int(page_size), int(num_pages), max_pages, free_pages.numel(),
+                                          block_table.stride(0) if B > 1 else max_pages)), B
+
+
+def entmax_attn_paged_tables(kv_len, new_len, block_table, free_pages, free_count, page_size, num_pages, total_q, *, kv_len_out=None, cu_q=None,
+                             positions=None, slots=None, free_count_out=None, status=None, stream=None):
+    """Tables of a serving step from the requests' lengths, on the GPU: kv_len int32 [B] tokens in the cache, new_len int32 [B] tokens to
+    come (-1: the sequence has ended and gives its pages back), block_table int32 [B, max_pages] (completed in place), free_pages int32 [capacity]
+    and free_count int32 [1], a stack of free pages, total_q the sum of the new tokens.  kv_len_out and free_count_out may be kv_len and free_count.
+    Returns (kv_len_out [B], cu_q [B + 1], positions [total_q] int32, slots [total_q] int64, free_count_out [1])."""
+    what = "entmax_attn_paged_tables"
+    where = (what, kv_len.numel(), block_table.numel(), free_pages.numel(), total_q)
+    key = (page_size, num_pages, _layout_of(kv_len, new_len, block_table, free_pages, free_count, kv_len_out, cu_q, positions, slots, free_count_out,
+                                            status))
+    known = _layouts.get(where)
+    params, B = known[1] if known is not None and known[0] == key else _keep(where, key, _tables_layout(
+        what, kv_len, new_len, block_table, free_pages, free_count, page_size, num_pages, total_q, kv_len_out, cu_q, positions, slots,
+        free_count_out, status))
+    kv_len_out = _new_on(stream, kv_len, (B,), torch.int32) if kv_len_out is None else kv_len_out
+    cu_q = _new_on(stream, kv_len, (B + 1,), torch.int32) if cu_q is None else cu_q
+    positions = _new_on(stream, kv_len, (total_q,), torch.int32) if positions is None else positions
+    slots = _new_on(stream, kv_len, (total_q,), torch.int64) if slots is None else slots
+    free_count_out = _new_on(stream, kv_len, (1,), torch.int32) if free_count_out is None else free_count_out
+    rc = _call_on(kv_len.get_device(), lambda: load().entmax_attn_paged_tables(
+        params, kv_len.data_ptr(), new_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), kv_len_out.data_ptr(),
+        cu_q.data_ptr(), positions.data_ptr(), slots.data_ptr(), free_count_out.data_ptr(), _ptr(status), _stream_ptr(stream)))
+    _check(rc, what)
+    return kv_len_out, cu_q, positions, slots, free_count_out
+
+
+def entmax_attn_row_ranges(cu_docs, seq, causal, *, prefix_len=None, window=0, row_ranges=None, stream=None):
+    """The keys each row sees when documents are packed into a batch row: cu_docs int32 [B, docs + 1] boundaries, prefix_len int32 [B, docs] or
+    None (tokens every row of the document sees; causal only), window > 0: the last `window` keys.  Tokens in no document see nothing.
+    Returns int32 [B, seq, 2] for entmax_attn_softmax_fwd and softmax_attention, which are then called with causal=False."""
+    what = "entmax_attn_row_ranges"
+    if cu_docs.dim() != 2 or cu_docs.shape[1] < 2 or cu_docs.dtype != torch.int32 or not cu_docs.is_contiguous():
+        raise EntmaxAttnError("%s: cu_docs must be a contiguous int32 [batch, docs + 1] tensor" % what)
+    B, docs = cu_docs.shape[0], cu_docs.shape[1] - 1
+    _check_tensors(what, cu_docs.device, ("prefix_len", prefix_len, (B, docs), torch.int32), ("row_ranges", row_ranges, (B, seq, 2), torch.int32))
+    if row_ranges is None:
+        row_ranges = _new_on(stream, cu_docs, (B, seq, 2), torch.int32)
+    rc = _call_on(cu_docs.get_device(), lambda: load().entmax_attn_row_ranges(
+        B, int(seq), docs, int(bool(causal)), int(window), cu_docs.data_ptr(), _ptr(prefix_len), row_ranges.data_ptr(), _stream_ptr(stream)))
+    _check(rc, what)
+    return row_ranges
+
+
+def _strides4(what, name, x, shape, dtype, device):
+    if x.shape != shape or x.dtype != dtype or x.device != device or x.stride(3) != 1:
+        raise EntmaxAttnError("%s: %s must be a %s %s tensor on %s with the last dimension contiguous" % (what, name, dtype, list(shape), device))
+    # (a dimension of one entry may have any stride; 0 throughout would mean "contiguous")
+    return Strides(x.stride(0), x.stride(1), max(x.stride(2), 1))
+
+
+def _softmax_layout(what, q, k, v, causal, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, softcap, sm_scale, o, lse, status, d_o, dq, dk,
+                    dv, d_scale_rows, bwd):
+    if q.dim() != 4 or k.dim() != 4:
+        raise EntmaxAttnError("%s: expected [batch, heads, seq, head_dim] tensors" % what)
+    if q.dtype not in (torch.bfloat16, torch.float32):
+        raise EntmaxAttnError("%s: dtype must be bfloat16 or float32" % what)
+    (B, H, N, D), G, dev, dt = q.shape, k.shape[1], q.device, q.dtype
+    shape, kv = (B, H, N, D), (B, G, N, D)
+    strides = lambda name, x, sh: _strides4(what, name, x, sh, dt, dev)  # noqa: E731
+    none = Strides(0, 0, 0)
+    params = SoftmaxParams(B, H, G, N, D, DTYPE_BF16 if dt == torch.bfloat16 else DTYPE_FP32, int(bool(causal)), float(sm_scale), float(softcap),
+                           strides("q", q, shape), strides("k", k, kv), strides("v", v, kv), none if o is None else strides("o", o, shape))
+    f32 = torch.float32
+    _check_tensors(what, dev, ("beta", beta, (H,), f32), ("gamma", gamma, (H,), f32), ("delta", delta, (H,), f32), ("c_rows", c_rows, (B, H, N), f32),
+                   ("alibi_slopes", alibi_slopes, (H,), f32), ("row_ranges", row_ranges, (B, N, 2), torch.int32), ("lse", lse, (B, H, N), f32),
+                   ("d_scale_rows", d_scale_rows, (B, H, N), f32))
+    if status is not None and (status.dtype != torch.int32 or status.numel() < STATUS_WORDS or not status.is_contiguous() or status.device != dev):
+        raise EntmaxAttnError("%s: status must be a contiguous int32 tensor of %d words on the device of q" % (what, STATUS_WORDS))
+    if not bwd:
+        return params, None, 0
+    grads = SoftmaxGrads(strides("d_o", d_o, shape), *(none if x is None else strides(name, x, sh) for name, x, sh in
+                                                      (("dq", dq, shape), ("dk", dk, kv), ("dv", dv, kv))), None, None, None, None)
+    return params, grads, int(load().entmax_attn_softmax_workspace_bytes(ctypes.byref(params)))
+
+
+def entmax_attn_softmax_fwd(q, k, v, causal, beta=None, gamma=None, delta=None, *, c_rows=None, alibi_slopes=None, row_ranges=None, softcap=0.0,
+                            sm_scale=0.0, o=None, lse=None, status=None, stream=None):
+    """Softmax attention (alpha -> 1) of q [B,H,N,d], k, v [B,G,N,d] (H a multiple of G; bf16 or fp32, each with strides of its own, d contiguous):
+    scores c (softcap tanh(z / softcap) - slope |i - j|), c from beta, gamma, delta [H] or c_rows [B,H,N]; row_ranges int32 [B,N,2]: the keys a row
+    sees (entmax_attn_row_ranges).  Returns (o, lse)."""
+    what = "entmax_attn_softmax_fwd"
+    where = (what, q.numel(), k.numel())
+    key = (causal, softcap, sm_scale, _layout_of(q, k, v, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, o, lse, status))
+    known = _layouts.get(where)
+    params, _, _ = known[1] if known is not None and known[0] == key else _keep(where, key, _softmax_layout(
+        what, q, k, v, causal, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, softcap, sm_scale, o, lse, status, None, None, None, None, None,
+        False))
+    B, H, N, _ = shape = q.shape
+    if o is None:
+        o = _new_on(stream, q, shape, q.dtype)
+    if lse is None:
+        lse = _new_on(stream, q, (B, H, N), torch.float32)
+    terms = SoftmaxTerms(_ptr(row_ranges), _ptr(beta), _ptr(gamma), _ptr(delta), _ptr(c_rows), _ptr(alibi_slopes))
+    rc = _call_on(q.get_device(), lambda: load().entmax_attn_softmax_fwd(
+        ctypes.byref(params), q.data_ptr(), k.data_ptr(), v.data_ptr(), ctypes.byref(terms), o.data_ptr(), lse.data_ptr(), _ptr(status),
+        _stream_ptr(stream)))
+    _check(rc, what)
+    return o, lse
+
+
+def entmax_attn_softmax_bwd(q, k, v, o, lse, d_o, causal, beta=None, gamma=None, delta=None, *, c_rows=None, alibi_slopes=None, row_ranges=None,
+                            softcap=0.0, sm_scale=0.0, want_scale_rows=False, want_param_grads=False, dq=None, dk=None, dv=None,
+                            d_scale_rows=None, workspace=None, status=None, stream=None):
+    """Backward pass of entmax_attn_softmax_fwd, whose o and lse it takes.
+    Returns (dq, dk, dv, d_scale_rows or None, (dbeta, dgamma, ddelta) or None)."""
+    what = "entmax_attn_softmax_bwd"
+    where = (what, q.numel(), k.numel())
+    key = (causal, softcap, sm_scale, _layout_of(q, k, v, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, o, lse, status, d_o, dq, dk, dv,
+                                                 d_scale_rows))
+    known = _layouts.get(where)
+    params, strides, nbytes = known[1] if known is not None and known[0] == key else _keep(where, key, _softmax_layout(
+        what, q, k, v, causal, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, softcap, sm_scale, o, lse, status, d_o, dq, dk, dv, d_scale_rows,
+        True))
+    B, H, N, _ = q.shape
+    dq = _new_on(stream, q, q.shape, q.dtype) if dq is None else dq
+    dk = _new_on(stream, k, k.shape, k.dtype) if dk is None else dk
+    dv = _new_on(stream, v, v.shape, v.dtype) if dv is None else dv
+    if d_scale_rows is None and want_scale_rows:
+        d_scale_rows = _new_on(stream, q, (B, H, N), torch.float32)
+    params_grads = tuple(_new_on(stream, q, (H,), torch.float32) for _ in range(3)) if want_param_grads else None
+    if workspace is None:
+        workspace = _new_on(stream, q, (nbytes,), torch.uint8)
+    elif workspace.dtype != torch.uint8 or workspace.get_device() != q.get_device() or not workspace.is_contiguous():
+        raise EntmaxAttnError("%s: workspace must be a contiguous uint8 tensor on the device of q" % what)
+    g = params_grads or (None, None, None)
+    terms = SoftmaxTerms(_ptr(row_ranges), _ptr(beta), _ptr(gamma), _ptr(delta), _ptr(c_rows), _ptr(alibi_slopes))
+    grads = SoftmaxGrads(strides.d_o, strides.dq, strides.dk, strides.dv, _ptr(d_scale_rows), _ptr(g[0]), _ptr(g[1]), _ptr(g[2]))
+    rc = _call_on(q.get_device(), lambda: load().entmax_attn_softmax_bwd(
+        ctypes.byref(params), q.data_ptr(), k.data_ptr(), v.data_ptr(), ctypes.byref(terms), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(),
+        ctypes.byref(grads), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(), workspace.numel(), _ptr(status),
+        _stream_ptr(stream)))
+    _check(rc, what)
+    return dq, dk, dv, d_scale_rows, params_grads
 
 
 def _param_grads(H: int, device):

@@ -1,0 +1,85 @@
+// Declarations shared by the kernels of softmax attention, the alpha = 1 member of the family (softmax_*.cu).
+//
+//   z_ij = sm_scale <q_i, k_j>,  x_ij = cap tanh(z_ij / cap) - m_h |i - j|,  s_ij = c_i x_ij,
+//   p_ij = exp(s_ij - lse_i) over the keys j the row sees,  O_i = sum_j p_ij v_j;  a row that sees none: O = 0, lse = -inf.
+// Everything is kept in units of the accumulator <q_i, k_j>: x / sm_scale = cap_acc tanh(acc * cap_inv) - slope_acc |i - j|, and
+// s log2(e) = a_i (x / sm_scale) with a_i = c_i sm_scale log2(e), so that a probability is one FMA and one exp2.
+#pragma once
+
+#include "common.cuh"
+
+namespace entmax {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct SoftmaxArgs {
+  int B, H, KH, G, N, D;              // G = H / KH query heads share a K/V head
+  int causal;
+  float sm_scale;
+  float cap_acc, cap_inv;             // cap / sm_scale and sm_scale / cap (0, 0: not capped)
+  const int2* ranges;                 // [B][N] {first key, one behind the last} or nullptr
+  const float *beta, *gamma, *delta;  // [H] or nullptr
+  const float* c_rows;                // [B][H][N] or nullptr
+  const float* alibi;                 // [H] or nullptr
+  entmax_attn_strides q, k, v, o;
+};
+
+// The keys [x, y) that row i of batch row b sees; y = x where there are none.
+__device__ __forceinline__ int2 visible_keys(const SoftmaxArgs& a, int b, int i) {
+  int2 r = make_int2(0, a.causal ? i + 1 : a.N);
+  if (a.ranges) {
+    const int2 given = a.ranges[(size_t)b * a.N + i];
+    r.x = max(given.x, 0);
+    r.y = min(given.y, r.y);
+  }
+  if (r.y <= r.x) r = make_int2(0, 0);
+  return r;
+}
+
+// (ln n)^gamma grown by beta on top of delta; n = 1 (and 0): delta alone
+__device__ __forceinline__ float length_scale(float beta, float gamma, float delta, int n) {
+  return n > 1 ? delta + beta * powf(logf((float)n), gamma) : delta;
+}
+// c of row i, which sees n keys
+__device__ __forceinline__ float row_scale(const SoftmaxArgs& a, int b, int h, int i, int n) {
+  if (a.c_rows) return a.c_rows[((size_t)b * a.H + h) * a.N + i];
+  if (a.beta) return length_scale(a.beta[h], a.gamma[h], a.delta[h], n);
+  return 1.0f;
+}
+
+// tanh from one exp2 and one reciprocal, the absolute error a few 1e-7 (what is needed here: a score's error is cap times it).  Large arguments
+// end at +-1: exp2 overflows to infinity or vanishes.
+__device__ __forceinline__ float tanh_full(float u) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * (2.0f * kLog2e)));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.0f));
+  return fmaf(-2.0f, r, 1.0f);
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Host: checks of the parameters and the terms (defined in softmax_api.cu)
+int check_softmax(const entmax_attn_softmax_params* params, const entmax_attn_softmax_terms* terms, SoftmaxArgs* out);
+
+// Gradient outputs and what the backward pass works with
+struct SoftmaxGrads {
+  const float* lse;
+  entmax_attn_strides d_o, dq, dk, dv;
+  float* dc_rows;                     // [B][H][N] or nullptr
+  float* row_dot;                     // [B][H][N] scratch: sum_j p_ij dP_ij
+};
+
+// CUDA-core kernels, any dtype of the library's (float32 problems)
+template <typename T>
+cudaError_t launch_softmax_rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, cudaStream_t stream);
+template <typename T>
+cudaError_t launch_softmax_rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* d_o,
+                                    void* dq, void* dk, void* dv, cudaStream_t stream);
+// dbeta, dgamma, ddelta [H] from dL/dc of every row
+cudaError_t launch_softmax_scale_grad(const SoftmaxArgs& a, const float* dc_rows, float* dbeta, float* dgamma, float* ddelta, cudaStream_t stream);
+
+}  // namespace entmax
