@@ -13,7 +13,7 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(_ROOT, "include")
 LIB = os.path.join(_HERE, "libentmax_attn.so")
-SOURCES = ["entmax_attn_api.cu", "dense_rows.cu", "fp32_rows.cu", "row_lists.cu", "sweep_sm100.cu", "tile_fwd_sm100.cu", "tile_bwd_sm100.cu", "decode.cu", "decode_scores_sm100.cu", "no_alloc.cu", "selftest.cu", "scale_proj.cu", "paged_append.cu", "paged_scores_sm100.cu", "paged_fwd.cu", "paged_tables.cu", "softmax_api.cu", "softmax_rows.cu", "softmax_paged.cu"]
+SOURCES = ["entmax_attn_api.cu", "dense_rows.cu", "fp32_rows.cu", "row_lists.cu", "sweep_sm100.cu", "tile_fwd_sm100.cu", "tile_bwd_sm100.cu", "decode.cu", "decode_scores_sm100.cu", "no_alloc.cu", "selftest.cu", "scale_proj.cu", "paged_append.cu", "paged_scores_sm100.cu", "paged_fwd.cu", "paged_tables.cu", "softmax_api.cu", "softmax_rows.cu", "softmax_paged.cu", "softmax_fwd_sm100.cu"]
 
 
 def _nvcc() -> str:
@@ -31,7 +31,7 @@ def needs_build() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = _sources() + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "sm100_ptx.cuh"), os.path.join(CSRC, "decode.cuh"), os.path.join(CSRC, "paged.cuh"), os.path.join(CSRC, "softmax.cuh"), os.path.join(INCLUDE, "entmax_attn.h")]
+    deps = _sources() + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "sm100_ptx.cuh"), os.path.join(CSRC, "decode.cuh"), os.path.join(CSRC, "paged.cuh"), os.path.join(CSRC, "softmax.cuh"), os.path.join(CSRC, "softmax_tile.cuh"), os.path.join(INCLUDE, "entmax_attn.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -79,6 +79,9 @@ cudaError_t launch_softmax_rows_fwd(const SoftmaxArgs& a, const void* q, const v
 template <typename T>
 cudaError_t launch_softmax_rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* d_o,
                                     void* dq, void* dk, void* dv, cudaStream_t stream);
+// Tensor-core kernels (bf16)
+cudaError_t launch_softmax_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, int32_t* status,
+                               cudaStream_t stream);
 // dbeta, dgamma, ddelta [H] from dL/dc of every row
 cudaError_t launch_softmax_scale_grad(const SoftmaxArgs& a, const float* dc_rows, float* dbeta, float* dgamma, float* ddelta, cudaStream_t stream);
 

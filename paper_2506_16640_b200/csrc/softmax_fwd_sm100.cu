@@ -1,0 +1,622 @@
+// Softmax attention on sm_100a, forward: whole sequences ([B, H, N, D] tensors) and chunks of new tokens over a paged cache, one kernel.
+//
+// A work item is two Q tiles of 128 rows that share a K/V head -- two query heads of a group at the same rows where the group is even, two neighbouring
+// tiles of one head otherwise -- so that every K/V tile in shared memory is used twice.  K/V tiles come last to first (with slopes the largest
+// scores first).  Per Q tile and K/V tile of 128 keys
+//   S = Q K^T        both operands in shared memory, S in TMEM;
+//   P = exp2(a x - a m)   a thread per row: its 128 scores in registers, running maximum m, running sum l of the float32 probabilities;
+//                         P as bf16 over S's own columns (2^-9 of a probability at most: what the product's input type holds);
+//   O += P V         P from TMEM, V with the head dim contiguous, O in TMEM.
+// O is not rescaled for every rise of the maximum: P may grow up to 2^8 above the m it is measured from before O and l are brought to a new one, exactly, so
+// that nothing is lost and the correction is rare.  While one tile's softmax runs the tensor core works on the other's O and next S.
+// Next to the MMAs (per pair of steps 4 x 128 x 128 x D, 2048 cycles at D = 128) the 2 x 16384 exponentials take 2048 cycles of the special-function
+// unit: a part of them is computed on the FMA pipe instead (exp2_pair_fma).
+//
+// CTA: warps 0..3 and 4..7 the rows of the two tiles, warp 8 MMA issuer, warp 9 TMA producer and scheduler.  Items are handed out by the hardware: a
+// running CTA takes over one that has not started (longest rows of a head first).  Every wait is bounded (see sm100_ptx.cuh).
+#include <cuda.h>
+
+#include "paged.cuh"
+#include "sm100_ptx.cuh"
+#include "softmax.cuh"
+#include "softmax_tile.cuh"
+
+namespace entmax {
+
+namespace {
+
+using namespace sm100;
+
+constexpr int kRows = 128, kKeys = 128;
+constexpr int kFwdThreads = 320;
+constexpr int kBarArea = 512;
+
+template <int HD>
+struct FwdCfg {
+  static constexpr int kHalves = HD / 64;
+  static constexpr int kTileBytes = kKeys * HD * 2;
+  static constexpr int kStages = HD == 128 ? 4 : 8;                  // K and V tiles in turn
+  static constexpr int kSmemBytes = 2 * kTileBytes + kStages * kTileBytes + kBarArea + 1024;
+  static_assert(kSmemBytes <= 232448, "shared memory of one CTA");
+  static constexpr int kTmemO = 256;
+};
+
+// What the scheduler says about an item, in shared memory
+struct Work {
+  int valid;            // 0: nothing left
+  int b, kh;
+  int h[2], row0[2];    // head and first row (paged: new token of the sequence) of the two tiles
+  int lo[2], hi[2];     // their K/V tiles, lo >= hi: none
+  int q0, n, len;       // paged: first row of q, new tokens, length
+  int part;             // paged, shared out: where its results go (tile t: part + t), -1: it has all keys
+  int first_key;        // paged: no row sees a key before it
+};
+static_assert(sizeof(Work) == 64, "two of them behind the barriers");
+
+struct FwdArgs {
+  SoftmaxArgs a;
+  int tiles;            // Q tiles (or pairs of tiles) per head
+  int pairs;            // pairs of heads in a group (pair_heads), 1 otherwise
+  int pair_heads;
+  __nv_bfloat16* o;
+  float* lse;
+  int32_t* status;
+  // paged
+  PagedCache c;
+  int window, max_q, max_kv, few_rows, shares, box_shift;
+  float* part_o;        // [part][128][HD]
+  float2* part_ml;      // [part][128] {maximum in base-2 units, sum}
+};
+
+__host__ __device__ constexpr uint32_t fwd_idesc_s() {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+}
+// A from TMEM, B with N contiguous
+template <int HD>
+__host__ __device__ constexpr uint32_t fwd_idesc_o() {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+}
+
+// The K/V tiles that the 128 rows from row0 on see, by the whole warp
+__device__ __forceinline__ int2 tile_span(const SoftmaxArgs& a, int b, int row0) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0x7fffffff, hi = 0;
+  if (row0 < a.N) {
+    if (!a.ranges) {
+      lo = 0;
+      hi = a.causal ? min(row0 + kRows, a.N) : a.N;
+    } else {
+      for (int r = lane; r < kRows && row0 + r < a.N; r += 32) {
+        const int2 s = visible_keys(a, b, row0 + r);
+        if (s.y > s.x) { lo = min(lo, s.x); hi = max(hi, s.y); }
+      }
+      lo = __reduce_min_sync(0xffffffffu, lo);
+      hi = __reduce_max_sync(0xffffffffu, hi);
+    }
+  }
+  return hi > lo ? make_int2(lo / kKeys, (hi + kKeys - 1) / kKeys) : make_int2(0, 0);
+}
+
+// Paged: block id -> sequence and first new token, by the whole warp.  Sequence b has the ids from cu[b] / block + b on, at least as many as it has blocks.
+__device__ __forceinline__ int block_start(const PagedCache& c, int b, int block) {
+  const int cu = c.cu_q ? clamped_cu(c, b) : b * (c.T / c.B);
+  return cu / block + b;
+}
+__device__ __forceinline__ int find_block(const PagedCache& c, int id, int block) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = c.B;
+  while (n > 1) {
+    const int step = (n + 31) / 32;
+    const bool le = lane * step < n && (lane == 0 || block_start(c, lo + lane * step, block) <= id);
+    const int k = 31 - __clz(__ballot_sync(0xffffffffu, le));
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo;
+}
+
+template <int HD, bool PAGED>
+__global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ FwdArgs f) {
+  pdl_begin();
+  using C = FwdCfg<HD>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_smem = sbase, kv_smem = sbase + 2 * C::kTileBytes;
+  const uint32_t bars = kv_smem + C::kStages * C::kTileBytes;
+  const uint32_t work_at = bars;                                     // Work [2]
+  const uint32_t answer = bars + 128;                                // 16 bytes
+  const uint32_t q_full = bars + 144, q_empty = bars + 160;          // [2] each
+  const uint32_t s_full = bars + 176, p_full = bars + 192;
+  const uint32_t o_full = bars + 208, o_empty = bars + 224;
+  const uint32_t w_full = bars + 240, w_empty = bars + 256;
+  const uint32_t next_bar = bars + 272, drain_bar = bars + 280;
+  const uint32_t tmem_slot = bars + 288, abort_flag = bars + 292, drain_fail = bars + 296;
+  const uint32_t kv_full = bars + 304, kv_empty = bars + 304 + 8 * C::kStages;
+  static_assert(304 + 16 * C::kStages <= kBarArea, "barriers");
+  const Work* work = reinterpret_cast<const Work*>(smem_raw + (work_at - smem_u32(smem_raw)));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(q_full + 8 * t, 1);
+      mbar_init(q_empty + 8 * t, 1);
+      mbar_init(s_full + 8 * t, 1);
+      mbar_init(p_full + 8 * t, 4);
+      mbar_init(o_full + 8 * t, 1);
+      mbar_init(o_empty + 8 * t, 4);
+      mbar_init(w_full + 8 * t, 1);
+      mbar_init(w_empty + 8 * t, 9);
+    }
+    for (int st = 0; st < C::kStages; ++st) {
+      mbar_init(kv_full + 8 * st, 1);
+      mbar_init(kv_empty + 8 * st, 1);
+    }
+    mbar_init(next_bar, 1);
+    mbar_init(drain_bar, 1);
+    sts_u32(abort_flag, 0u);
+    sts_u32(drain_fail, 0u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 8) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = lds_u32(tmem_slot);
+  const SoftmaxArgs& a = f.a;
+  auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
+
+  if (warp == 9) {
+    // ------------------------------------------------------------------ scheduler and TMA producer (the whole warp runs the control flow)
+    uint32_t next_phase = 0, wphase = 0, qphase[2] = {0, 0}, idx = 0;   // idx: K and V tiles loaded so far
+    int slot = 0;
+    bool alive = true, asked = false;
+    int item = (int)blockIdx.x;
+    while (alive) {
+      Work w;
+      w.valid = item >= 0;
+      w.part = -1;
+      if (item >= 0) {
+        asked = true;
+        if (elect_one()) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the last answer has been read
+          mbar_expect_tx(next_bar, 16);
+          next_cta_request(answer, next_bar);
+        }
+        __syncwarp();
+        int rest = item;
+        if constexpr (!PAGED) {
+          const int pair = rest % f.pairs;
+          rest /= f.pairs;
+          const int tile = f.tiles - 1 - rest % f.tiles;
+          rest /= f.tiles;
+          w.b = rest / a.KH;
+          w.kh = rest - w.b * a.KH;
+          w.h[0] = w.kh * a.G + (f.pair_heads ? 2 * pair : pair);
+          w.h[1] = f.pair_heads ? w.h[0] + 1 : w.h[0];
+          w.row0[0] = f.pair_heads ? tile * kRows : tile * 2 * kRows;
+          w.row0[1] = f.pair_heads ? w.row0[0] : w.row0[0] + kRows;
+          const int2 s0 = tile_span(a, w.b, w.row0[0]);
+          const int2 s1 = f.pair_heads ? s0 : tile_span(a, w.b, w.row0[1]);
+          w.lo[0] = s0.x; w.hi[0] = s0.y; w.lo[1] = s1.x; w.hi[1] = s1.y;
+          w.q0 = 0; w.n = a.N; w.len = a.N; w.first_key = 0;
+        } else {
+          const int share = rest % f.shares;
+          rest /= f.shares;
+          const int unit = rest;                                      // (block, K/V head, pair of heads)
+          const int pair = rest % f.pairs;
+          rest /= f.pairs;
+          w.kh = rest % a.KH;
+          const int id = rest / a.KH;
+          const int block = f.pair_heads ? kRows : 2 * kRows;
+          w.b = find_block(f.c, id, block);
+          const PagedSeq s = paged_seq(f.c, w.b);
+          w.q0 = s.q0; w.n = s.n; w.len = s.len;
+          w.h[0] = w.kh * a.G + (f.pair_heads ? 2 * pair : pair);
+          w.h[1] = f.pair_heads ? w.h[0] + 1 : w.h[0];
+          w.row0[0] = (id - block_start(f.c, w.b, block)) * block;
+          w.row0[1] = f.pair_heads ? w.row0[0] : w.row0[0] + kRows;
+          w.part = f.shares > 1 ? 2 * (unit * f.shares + share) : -1;
+          const bool ok = s.len >= s.n && s.len <= f.max_kv && s.n <= f.max_q && (long long)s.n * a.G > f.few_rows && w.row0[0] < s.n && w.row0[0] >= 0;
+          int most = 0, least = 0x7fffffff;
+          w.first_key = 0;
+          for (int t = 0; t < 2; ++t) {
+            w.lo[t] = w.hi[t] = 0;
+            if (!ok || w.row0[t] >= s.n) continue;
+            const int pos0 = s.len - s.n + w.row0[t];
+            const int first = f.window > 0 ? max(0, pos0 - f.window + 1) : 0;
+            if (t == 0) w.first_key = first;
+            w.lo[t] = first / kKeys;
+            w.hi[t] = (min(pos0 + kRows, s.len) + kKeys - 1) / kKeys;
+            least = min(least, w.lo[t]);
+            most = max(most, w.hi[t]);
+          }
+          if (f.shares > 1 && most > least) {
+            const int all = most - least;
+            const int from = least + (int)((long long)all * share / f.shares), to = least + (int)((long long)all * (share + 1) / f.shares);
+            for (int t = 0; t < 2; ++t) {
+              const bool rows = w.hi[t] > w.lo[t];
+              w.lo[t] = max(w.lo[t], from);
+              w.hi[t] = rows ? min(w.hi[t], to) : 0;
+            }
+          }
+          if (!ok) w.valid = 2;                                       // nothing of it is this kernel's
+        }
+      }
+      if (w.valid != 2) {
+        alive = wait_all(w_empty + 8 * slot, wphase ^ 1u);
+        if (!alive) break;
+        if (lane == 0) {
+          *const_cast<Work*>(work + slot) = w;
+          mbar_arrive(w_full + 8 * slot);
+        }
+        __syncwarp();
+        if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      }
+      if (item < 0) break;
+      int lo = 0x7fffffff, hi = 0;
+      if (w.valid == 1) {
+        for (int t = 0; t < 2; ++t)
+          if (w.hi[t] > w.lo[t]) { lo = min(lo, w.lo[t]); hi = max(hi, w.hi[t]); }
+      }
+      if (hi > lo) {
+        for (int t = 0; t < 2 && alive; ++t) {
+          if (w.hi[t] <= w.lo[t]) continue;
+          alive = wait_all(q_empty + 8 * t, qphase[t] ^ 1u);
+          if (!alive) break;
+          qphase[t] ^= 1u;
+          if (elect_one()) {
+            mbar_expect_tx(q_full + 8 * t, C::kTileBytes);
+            for (int hf = 0; hf < C::kHalves; ++hf)
+              tma_load_4d(q_smem + t * C::kTileBytes + hf * (kRows * 128), &map_q, q_full + 8 * t, hf * 64, PAGED ? w.q0 + w.row0[t] : w.row0[t],
+                          w.h[t], PAGED ? 0 : w.b);
+          }
+          __syncwarp();
+        }
+        // paged: lane x looks after box x of a tile, one tile ahead
+        int page = 0, page_next = 0;
+        auto look_up = [&](int j) -> int {
+          const int key = j * kKeys + (lane << f.box_shift);
+          if (j < lo || lane >= (kKeys >> f.box_shift) || key >= w.len || key + (1 << f.box_shift) <= w.first_key) return -2;
+          int p = f.c.table[(long long)w.b * f.c.table_stride + (key >> f.c.ps_shift)];
+          if ((unsigned)p >= (unsigned)f.c.n_pages) {                 // (read as zeros)
+            if (f.status) atomicOr(f.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_PAGE);
+            p = f.c.n_pages;
+          }
+          return p;
+        };
+        if constexpr (PAGED) page_next = look_up(hi - 1);
+        for (int j = hi - 1; j >= lo && alive; --j) {
+          if constexpr (PAGED) {
+            page = page_next;
+            page_next = look_up(j - 1);
+          }
+          for (int which = 0; which < 2; ++which, ++idx) {
+            const int st = idx % C::kStages;
+            const uint32_t round = idx / C::kStages;
+            alive = wait_all(kv_empty + 8 * st, (round & 1u) ^ 1u);
+            if (!alive) break;
+            const uint32_t dst = kv_smem + st * C::kTileBytes;
+            const CUtensorMap* map = which ? &map_v : &map_k;
+            if constexpr (!PAGED) {
+              if (elect_one()) {
+                mbar_expect_tx(kv_full + 8 * st, C::kTileBytes);
+                for (int hf = 0; hf < C::kHalves; ++hf)
+                  tma_load_4d(dst + hf * (kKeys * 128), map, kv_full + 8 * st, hf * 64, j * kKeys, w.kh, w.b);
+              }
+            } else {
+              const int boxes = __popc(__ballot_sync(0xffffffffu, page >= 0));
+              if (lane == 0) mbar_expect_tx(kv_full + 8 * st, boxes * (C::kHalves * 128) << f.box_shift);
+              __syncwarp();
+              if (page >= 0) {
+                const int slot0 = (j * kKeys + (lane << f.box_shift)) & ((1 << f.c.ps_shift) - 1);
+                for (int hf = 0; hf < C::kHalves; ++hf)
+                  tma_load_4d(dst + hf * (kKeys * 128) + (lane << (f.box_shift + 7)), map, kv_full + 8 * st, hf * 64, slot0, w.kh, page);
+              }
+            }
+            __syncwarp();
+          }
+        }
+        if (!alive) break;
+      }
+      // the next item
+      alive = wait_all(next_bar, next_phase);
+      if (!alive) break;
+      next_phase ^= 1u;
+      asked = false;
+      item = next_cta_answer(answer);
+      __syncwarp();
+    }
+    if (!alive && lane == 0) {
+      bool ok = true;
+      for (int t = 0; t < 2; ++t) ok &= mbar_drain(q_full + 8 * t, qphase[t] ^ 1u);
+      for (int st = 0; st < C::kStages; ++st) {
+        const uint32_t armed = idx / C::kStages + ((uint32_t)st < idx % C::kStages ? 1u : 0u);   // times its barrier has been armed
+        ok &= mbar_drain(kv_full + 8 * st, (armed & 1u) ^ 1u);
+      }
+      if (asked) ok &= mbar_drain(next_bar, next_phase);
+      if (!ok) sts_u32(drain_fail, 1u);
+    }
+  } else if (warp == 8) {
+    // ------------------------------------------------------------------ MMA issuer
+    constexpr uint32_t id_s = fwd_idesc_s();
+    constexpr uint32_t id_o = fwd_idesc_o<HD>();
+    const uint64_t dhi = (uint64_t)kDescHi << 32;
+    const uint64_t q_d = dhi | smem_desc_lo(q_smem), k_d = dhi | smem_desc_lo(kv_smem), v_d = dhi | mn_desc_lo(kv_smem);
+    constexpr uint32_t kStageD = C::kTileBytes >> 4;
+    uint32_t wphase = 0, qphase[2] = {0, 0}, pphase[2] = {0, 0}, ophase[2] = {0, 0}, idx = 0;
+    int slot = 0;
+    bool alive = true;
+    while (alive) {
+      alive = wait_all(w_full + 8 * slot, wphase);
+      if (!alive) break;
+      const Work w = work[slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (!w.valid) break;
+      int lo = 0x7fffffff, hi = 0;
+      for (int t = 0; t < 2; ++t)
+        if (w.hi[t] > w.lo[t]) { lo = min(lo, w.lo[t]); hi = max(hi, w.hi[t]); }
+      if (hi <= lo) continue;
+      auto active = [&](int t, int j) { return j >= w.lo[t] && j < w.hi[t]; };
+      auto wait_kv = [&](uint32_t i) { return wait_all(kv_full + 8 * (i % C::kStages), (i / C::kStages) & 1u); };
+      auto issue_s = [&](int t, int j, uint32_t i) -> bool {
+        if (j == w.hi[t] - 1) {
+          if (!wait_all(q_full + 8 * t, qphase[t])) return false;
+          qphase[t] ^= 1u;
+        }
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t qt = q_d + t * kStageD, ks = k_d + (i % C::kStages) * kStageD;
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * ((kRows * 128) >> 4) + (kk & 3) * 2;
+            umma_bf16_desc(tmem + t * kKeys, qt + off, ks + off, id_s, kk > 0 ? 1u : 0u);
+          }
+          umma_commit(s_full + 8 * t);
+          if (j == w.lo[t]) umma_commit(q_empty + 8 * t);
+        }
+        __syncwarp();
+        return true;
+      };
+      alive = wait_kv(idx);
+      for (int t = 0; t < 2 && alive; ++t)
+        if (active(t, hi - 1)) alive = issue_s(t, hi - 1, idx);
+      if (!alive) break;
+      if (elect_one()) umma_commit(kv_empty + 8 * (idx % C::kStages));
+      __syncwarp();
+      for (int j = hi - 1; j >= lo && alive; --j, idx += 2) {
+        const uint32_t iv = idx + 1, ik = idx + 2;                    // V of this step, K of the next
+        alive = wait_kv(iv);
+        if (!alive) break;
+        if constexpr (PAGED) {
+          // rows of V that no query sees may hold anything (NaN times a probability of 0 is NaN): zeros instead
+          const int k0 = j * kKeys;
+          if (k0 + kKeys > w.len || k0 < w.first_key) {
+            const uint32_t dst = kv_smem + (iv % C::kStages) * C::kTileBytes;
+            for (int r = lane; r < kKeys * C::kHalves; r += 32) {
+              const int key = k0 + (r & (kKeys - 1));
+              if (key >= w.len || key < w.first_key)
+                for (int e = 0; e < 8; ++e) sts_f4(dst + r * 128 + e * 16, 0.f, 0.f, 0.f, 0.f);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
+        }
+        if (j > lo) {
+          alive = wait_kv(ik);
+          if (!alive) break;
+        }
+        for (int t = 0; t < 2 && alive; ++t) {
+          if (active(t, j)) {
+            alive = wait_all(p_full + 8 * t, pphase[t]);
+            if (!alive) break;
+            pphase[t] ^= 1u;
+            if (j == w.hi[t] - 1) {
+              // the previous item's O has been read
+              alive = wait_all(o_empty + 8 * t, ophase[t] ^ 1u);
+              if (!alive) break;
+              ophase[t] ^= 1u;
+            }
+            tc_fence_after();
+            if (elect_one()) {
+              const uint64_t vs = v_d + (iv % C::kStages) * kStageD;
+#pragma unroll
+              for (int kk = 0; kk < kKeys / 16; ++kk)
+                umma_bf16_ts(tmem + C::kTmemO + t * HD, tmem + t * kKeys + kk * 8, vs + kk * ((16 * 128) >> 4), id_o,
+                             (j < w.hi[t] - 1 || kk > 0) ? 1u : 0u);
+              if (j == w.lo[t]) umma_commit(o_full + 8 * t);
+            }
+            __syncwarp();
+          }
+          if (j > lo && active(t, j - 1)) alive = issue_s(t, j - 1, ik);
+        }
+        if (!alive) break;
+        if (elect_one()) {
+          umma_commit(kv_empty + 8 * (iv % C::kStages));
+          if (j > lo) umma_commit(kv_empty + 8 * (ik % C::kStages));
+        }
+        __syncwarp();
+      }
+    }
+    if (!alive && lane == 0) {
+      umma_commit(drain_bar);
+      if (!mbar_drain(drain_bar, 0u)) sts_u32(drain_fail, 1u);
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax: a thread per row
+    const int t = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
+    const uint32_t s_at = lane_base + t * kKeys, o_at = lane_base + C::kTmemO + t * HD;
+    uint32_t wphase = 0, sphase = 0, ophase = 0;
+    int slot = 0;
+    bool alive = true;
+    while (alive) {
+      alive = wait_all(w_full + 8 * slot, wphase);
+      if (!alive) break;
+      const int valid = work[slot].valid, b = work[slot].b, h = work[slot].h[t], i = work[slot].row0[t] + row, lo = work[slot].lo[t],
+                hi = work[slot].hi[t], q0 = work[slot].q0, n = work[slot].n, len = work[slot].len, part = work[slot].part;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (!valid) break;
+      const bool mine = i < n;
+      const int pos = PAGED ? len - n + i : i;                        // among the keys
+      int2 sees = make_int2(0, 0x7fffffff);                           // (rows behind the last: whatever comes, nothing is stored)
+      float scale = 0.f;
+      if (mine) {
+        if constexpr (PAGED) {
+          sees = make_int2(f.window > 0 ? max(0, pos - f.window + 1) : 0, pos + 1);
+          scale = a.beta ? length_scale(a.beta[h], a.gamma[h], a.delta[h], sees.y - sees.x) : 1.0f;
+          if (a.beta && f.status && !isfinite(scale)) atomicOr(f.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_SCALE);
+        } else {
+          sees = visible_keys(a, b, i);
+          scale = row_scale(a, b, h, i, sees.y - sees.x);
+          if ((a.beta || a.c_rows) && f.status && !isfinite(scale)) atomicOr(f.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_SCALE);
+        }
+      }
+      RowSoftmax sm;
+      sm.start(scale * a.sm_scale * kLog2e, a.alibi ? a.alibi[h] / a.sm_scale : 0.f, pos);
+      for (int j = hi - 1; j >= lo && alive; --j) {
+        alive = wait_all(s_full + 8 * t, sphase);
+        if (!alive) break;
+        sphase ^= 1u;
+        tc_fence_after();
+        float s[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(s_at + c * 32, s[c]);
+        tmem_ld_wait();
+        const int k0 = j * kKeys;
+        const bool edge = __any_sync(0xffffffffu, sees.x > k0 || sees.y < k0 + kKeys);
+        const float grown = sm.take(a, s, k0, sees, edge);
+        if (j < hi - 1 && __any_sync(0xffffffffu, grown != 1.0f)) {
+#pragma unroll
+          for (int c = 0; c < HD / 16; ++c) {
+            float v[16];
+            uint32_t u[16];
+            tmem_ld16(o_at + c * 16, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(v[e] * grown);
+            tmem_st16(o_at + c * 16, u);
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t p[16];
+          sm.probabilities(s[c], p, edge);
+          tmem_st16(s_at + c * 16, p);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + 8 * t);
+      }
+      if (!alive) break;
+      float inv = 0.f;
+      const float mass = sm.sum();
+      if (!PAGED || part < 0) {
+        inv = mass > 0.f ? 1.0f / mass : 0.f;
+        if (mine) {
+          const float lse = mass > 0.f ? (sm.base() + log2f(mass)) * kLn2 : -INFINITY;
+          if constexpr (PAGED) f.lse[(size_t)(q0 + i) * a.H + h] = lse;
+          else f.lse[((size_t)b * a.H + h) * a.N + i] = lse;
+        }
+      } else if (mine) {
+        f.part_ml[(size_t)(part + t) * kRows + row] = make_float2(sm.base(), mass);
+      }
+      __nv_bfloat16* out = nullptr;
+      if (mine)
+        out = PAGED ? f.o + ((size_t)(q0 + i) * a.H + h) * HD : f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n;
+      const bool some = hi > lo;
+      if (some) {
+        alive = wait_all(o_full + 8 * t, ophase);
+        if (!alive) break;
+        ophase ^= 1u;
+        tc_fence_after();
+      }
+#pragma unroll
+      for (int c = 0; c < HD / 32; ++c) {
+        float v[32];
+        if (some) {
+          tmem_ld32(o_at + c * 32, v);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = 0.f;
+        }
+        if (mine) {
+          if (PAGED && part >= 0) {
+            float4* to = reinterpret_cast<float4*>(f.part_o + ((size_t)(part + t) * kRows + row) * HD + c * 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              // (a row that sees nothing: its O is 0 times what the tile's other rows left it with, which is 0)
+              const float* x = v + 8 * e;
+              *reinterpret_cast<uint4*>(out + c * 32 + 8 * e) = make_uint4(bf16x2(x[0] * inv, x[1] * inv), bf16x2(x[2] * inv, x[3] * inv),
+                                                                           bf16x2(x[4] * inv, x[5] * inv), bf16x2(x[6] * inv, x[7] * inv));
+            }
+          }
+        }
+      }
+      if (some) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(o_empty + 8 * t);
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------------- teardown
+  tc_fence_before();
+  __syncthreads();
+  if (lds_u32(abort_flag)) {
+    if (threadIdx.x == 0 && f.status) atomicOr(f.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_WAIT_EXPIRED);
+    if (lds_u32(drain_fail)) {
+      const uint64_t t0 = global_ns();
+      while (global_ns() - t0 < 200000ull) { }
+    }
+    __syncthreads();
+  }
+  if (warp == 8) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int HD>
+cudaError_t fwd_launch(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, int32_t* status, cudaStream_t stream) {
+  CUtensorMap map_q, map_k, map_v;
+  cudaError_t err = make_tile_map(&map_q, q, a.D, a.N, a.H, a.B, a.q.n, a.q.h, a.q.b);
+  if (err == cudaSuccess) err = make_tile_map(&map_k, k, a.D, a.N, a.KH, a.B, a.k.n, a.k.h, a.k.b);
+  if (err == cudaSuccess) err = make_tile_map(&map_v, v, a.D, a.N, a.KH, a.B, a.v.n, a.v.h, a.v.b);
+  if (err == cudaSuccess)
+    err = cudaFuncSetAttribute(softmax_fwd_kernel<HD, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdCfg<HD>::kSmemBytes);
+  if (err != cudaSuccess) return err;
+  FwdArgs f = {};
+  f.a = a;
+  f.pair_heads = a.G % 2 == 0;
+  f.pairs = f.pair_heads ? a.G / 2 : a.G;
+  f.tiles = f.pair_heads ? (a.N + kRows - 1) / kRows : (a.N + 2 * kRows - 1) / (2 * kRows);
+  f.o = static_cast<__nv_bfloat16*>(o);
+  f.lse = lse;
+  f.status = status;
+  const unsigned grid = (unsigned)((long long)a.B * a.KH * f.pairs * f.tiles);
+  return launch_kernel(softmax_fwd_kernel<HD, false>, grid, kFwdThreads, FwdCfg<HD>::kSmemBytes, stream, map_q, map_k, map_v, f);
+}
+
+}  // namespace
+
+cudaError_t launch_softmax_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, int32_t* status,
+                               cudaStream_t stream) {
+  return a.D == 64 ? fwd_launch<64>(a, q, k, v, o, lse, status, stream) : fwd_launch<128>(a, q, k, v, o, lse, status, stream);
+}
+
+}  // namespace entmax
