@@ -70,7 +70,7 @@ struct SoftmaxGrads {
   const float* lse;
   entmax_attn_strides d_o, dq, dk, dv;
   float* dc_rows;                     // [B][H][N] or nullptr
-  float* row_dot;                     // [B][H][N] scratch: sum_j p_ij dP_ij
+  float* row_dot;                     // float32 problems: [B][H][N] scratch, sum_j p_ij dP_ij
 };
 
 // CUDA-core kernels, any dtype of the library's (float32 problems)
@@ -82,6 +82,11 @@ cudaError_t launch_softmax_rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g,
 // Tensor-core kernels (bf16)
 cudaError_t launch_softmax_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, int32_t* status,
                                cudaStream_t stream);
+// rows, spans: scratch of so many bytes
+size_t softmax_bwd_rows_bytes(const SoftmaxArgs& a);
+size_t softmax_bwd_spans_bytes(const SoftmaxArgs& a);
+cudaError_t launch_softmax_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* o, const void* d_o,
+                               void* dq, void* dk, void* dv, float* rows, void* spans, int32_t* status, cudaStream_t stream);
 // dbeta, dgamma, ddelta [H] from dL/dc of every row
 cudaError_t launch_softmax_scale_grad(const SoftmaxArgs& a, const float* dc_rows, float* dbeta, float* dgamma, float* ddelta, cudaStream_t stream);
 

@@ -106,15 +106,16 @@ bool take_strides(const entmax_attn_strides& given, int B, int H, int N, int D, 
 }
 
 struct BwdWorkspace {
-  size_t row_dot, dc_rows, bytes;
+  size_t dc_rows, rows, spans, bytes;   // rows: of the tensor-core kernels, or sum_j p_ij dP_ij of the float32 ones
 };
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-BwdWorkspace bwd_workspace(const SoftmaxArgs& a) {
+BwdWorkspace bwd_workspace(const SoftmaxArgs& a, bool bf16) {
   BwdWorkspace w;
-  const size_t rows = (size_t)a.B * a.H * a.N * 4;
-  w.row_dot = 0;
-  w.dc_rows = up256(rows);
-  w.bytes = w.dc_rows + up256(rows);
+  const size_t per_row = up256((size_t)a.B * a.H * a.N * 4);
+  w.dc_rows = 0;
+  w.rows = per_row;
+  w.spans = w.rows + (bf16 ? up256(softmax_bwd_rows_bytes(a)) : per_row);
+  w.bytes = w.spans + (bf16 ? up256(softmax_bwd_spans_bytes(a)) : 0);
   return w;
 }
 
@@ -187,7 +188,7 @@ extern "C" int entmax_attn_softmax_fwd(const entmax_attn_softmax_params* params,
 
 extern "C" size_t entmax_attn_softmax_workspace_bytes(const entmax_attn_softmax_params* params) {
   SoftmaxArgs a;
-  return check_softmax(params, nullptr, &a) == ENTMAX_ATTN_OK ? bwd_workspace(a).bytes : 0;
+  return check_softmax(params, nullptr, &a) == ENTMAX_ATTN_OK ? bwd_workspace(a, params->dtype == ENTMAX_ATTN_DTYPE_BF16).bytes : 0;
 }
 
 extern "C" int entmax_attn_softmax_bwd(const entmax_attn_softmax_params* params, const void* q, const void* k, const void* v,
@@ -207,17 +208,18 @@ extern "C" int entmax_attn_softmax_bwd(const entmax_attn_softmax_params* params,
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(d_o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) ||
       (reinterpret_cast<uintptr_t>(lse) & 3u))
     return ENTMAX_ATTN_EINVAL_ALIGN;
-  const BwdWorkspace w = bwd_workspace(a);
+  const bool bf16 = params->dtype == ENTMAX_ATTN_DTYPE_BF16;
+  const BwdWorkspace w = bwd_workspace(a, bf16);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < w.bytes) return ENTMAX_ATTN_EINVAL_WORKSPACE;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   g.lse = lse;
-  g.row_dot = reinterpret_cast<float*>(ws + w.row_dot);
+  g.row_dot = reinterpret_cast<float*>(ws + w.rows);
   g.dc_rows = grads->d_scale_rows ? grads->d_scale_rows : given ? reinterpret_cast<float*>(ws + w.dc_rows) : nullptr;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   rc = clear_status(device_status, stream);
   if (rc != ENTMAX_ATTN_OK) return rc;
-  cudaError_t err = params->dtype == ENTMAX_ATTN_DTYPE_FP32 ? launch_softmax_rows_bwd<float>(a, g, q, k, v, d_o, dq, dk, dv, stream)
-                                                            : launch_softmax_rows_bwd<__nv_bfloat16>(a, g, q, k, v, d_o, dq, dk, dv, stream);
+  cudaError_t err = bf16 ? launch_softmax_bwd(a, g, q, k, v, o, d_o, dq, dk, dv, reinterpret_cast<float*>(ws + w.rows), ws + w.spans, device_status, stream)
+                         : launch_softmax_rows_bwd<float>(a, g, q, k, v, d_o, dq, dk, dv, stream);
   if (err == cudaSuccess && given) err = launch_softmax_scale_grad(a, g.dc_rows, grads->dbeta, grads->dgamma, grads->ddelta, stream);
   return err == cudaSuccess ? ENTMAX_ATTN_OK : fail_cuda(err);
 }

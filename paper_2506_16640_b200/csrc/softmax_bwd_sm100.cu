@@ -1,0 +1,1039 @@
+// Softmax attention on sm_100a, backward: dQ (and dL/dc) query-major, dK and dV key-major.
+//
+//   P = exp2(a x - lse log2 e),  dP = dO V^T,  D_i = <dO_i, O_i>,  dS = P (dP - D),  dx = dS (1 - tanh^2)
+//   dQ_i = c_i sm sum_j dx_ij k_j,   dK_j = sum_i c_i sm dx_ij q_i,   dV_j = sum_i P_ij dO_i
+// Two kernels, so that nothing is added up by atomics: the scores and dP are formed twice (seven products instead of five), but no gradient goes
+// through memory as a float32 sum and results are the same every time.
+//   softmax_dq_kernel   an item is a Q tile of 128 rows: S and dP in TMEM, a row's 128 columns by four threads, dS as bf16 over S's own columns
+//                       and from there into dQ += dS K.  Leaves {lse log2 e, a, D} of every row, and which keys every tile sees, to the other kernel.
+//                       dL/dc_i = sum dS x is formed as sum p dP x - (sum p dP)(sum p x) / sum p, all of float32 probabilities: the D above comes
+//                       from the O that was rounded to bf16, which is good enough for dS (an error of 2^-9 of D times p) but not for a float32 result.
+//   softmax_dkv_kernel  an item is a K/V tile; over all query heads that share it and all Q tiles that see it: S^T = K Q^T and dP^T = V dO^T with the keys
+//                       along the lanes, so that P^T and dS^T are, over their own columns, the A operands of dV += P^T dO and dK += dS^T Q; what
+//                       depends on the query comes from shared memory, four columns a load.
+//
+// CTA of both: warp 0 scheduler and TMA producer, warp 1 MMA issuer, warps 2..17 four threads per TMEM lane (32 columns each).  Every wait is bounded.
+#include <cuda.h>
+
+#include "sm100_ptx.cuh"
+#include "softmax.cuh"
+#include "softmax_tile.cuh"
+
+namespace entmax {
+
+namespace {
+
+using namespace sm100;
+
+constexpr int kT = 128;
+constexpr int kWarps = 16;                       // element code
+constexpr int kBwdThreads = (2 + kWarps) * 32;
+constexpr int kBwdBars = 1536;
+
+template <int HD>
+struct BwdCfg {
+  static constexpr int kHalves = HD / 64;
+  static constexpr int kTile = kT * HD * 2;
+  static constexpr int kKStages = 3, kVStages = 2;
+  static constexpr int kSmemQ = (2 + kKStages + kVStages) * kTile + kBwdBars + 1024;
+  static constexpr int kRowBytes = 3 * kT * 4;                      // what a step needs to know of its 128 queries
+  static constexpr int kSmemKV = 6 * kTile + 2 * kRowBytes + kBwdBars + 1024;
+  static_assert(kSmemQ <= 232448 && kSmemKV <= 232448, "shared memory of one CTA");
+};
+
+struct BwdWork {
+  int valid, b, h, tile, lo, hi, pad[2];
+};
+
+struct BwdArgs {
+  SoftmaxArgs a;
+  SoftmaxGrads g;
+  int tiles;                    // of 128 rows, per head
+  const __nv_bfloat16 *o, *d_o;
+  __nv_bfloat16 *dq, *dk, *dv;
+  float* rows;                  // [B H tiles][3][128]: lse log2 e (+inf: a row that sees nothing), a, D
+  int4* spans;                  // [B tiles] {first key any row sees, one behind the last, largest first, smallest last}, with ranges
+  int32_t* status;
+};
+
+__host__ __device__ constexpr uint32_t bwd_idesc_kk() {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kT >> 3) << 17) | ((uint32_t)(kT >> 4) << 24);
+}
+// A from TMEM, B with N contiguous
+template <int HD>
+__host__ __device__ constexpr uint32_t bwd_idesc_kn() {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(kT >> 4) << 24);
+}
+// A bf16 operand written over the columns it came from: the 32 columns of thread group q hold 32 entries in their first 16, so K step kk (16
+// entries) starts here
+__device__ __forceinline__ uint32_t a_column(int kk) { return (uint32_t)((kk >> 1) * 32 + (kk & 1) * 8); }
+
+// {first key, one behind the last, largest first, smallest last} over the rows of a tile that see something, by the whole warp
+__device__ __forceinline__ int4 span_of(const SoftmaxArgs& a, int b, int row0) {
+  const int lane = threadIdx.x & 31;
+  int4 s = make_int4(0x7fffffff, 0, 0, 0x7fffffff);
+  for (int r = lane; r < kT && row0 + r < a.N; r += 32) {
+    const int2 v = visible_keys(a, b, row0 + r);
+    if (v.y <= v.x) continue;
+    s.x = min(s.x, v.x); s.y = max(s.y, v.y); s.z = max(s.z, v.x); s.w = min(s.w, v.y);
+  }
+  s.x = __reduce_min_sync(0xffffffffu, s.x);
+  s.y = __reduce_max_sync(0xffffffffu, s.y);
+  s.z = __reduce_max_sync(0xffffffffu, s.z);
+  s.w = __reduce_min_sync(0xffffffffu, s.w);
+  return s;
+}
+
+// x of 32 accumulators and, where they are capped, their tanh in t (x and t / grow share what they can)
+template <bool CAP, bool SLOPE>
+__device__ __forceinline__ float score_of(const SoftmaxArgs& a, float s, float slope, float dist) {
+  float x = CAP ? a.cap_acc * s : s;             // (CAP: s is the tanh)
+  if (SLOPE) x = fmaf(-slope, fabsf(dist), x);
+  return x;
+}
+__device__ __forceinline__ void to_tanh(float cap_inv, float (&s)[32]) {
+  float most = 0.f;
+#pragma unroll
+  for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(s[e]));
+  if (__all_sync(0xffffffffu, most * cap_inv <= 1.0f)) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = tanh_small(s[e] * cap_inv);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = tanh_full(s[e] * cap_inv);
+  }
+}
+
+__device__ __forceinline__ void bwd_teardown(uint32_t tmem, uint32_t abort_flag, uint32_t drain_fail, int32_t* status) {
+  tc_fence_before();
+  __syncthreads();
+  if (lds_u32(abort_flag)) {
+    if (threadIdx.x == 0 && status) atomicOr(status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_WAIT_EXPIRED);
+    if (lds_u32(drain_fail)) {
+      const uint64_t t0 = global_ns();
+      while (global_ns() - t0 < 200000ull) { }
+    }
+    __syncthreads();
+  }
+  if ((threadIdx.x >> 5) == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ dQ
+struct RowTerms {
+  float lse2, a, dot, slope;
+  int2 sees;
+  int i;
+};
+
+// 32 columns from key j0 on: dS as bf16 pairs; dc: {sum p dP x, sum p dP, sum p x, sum p} where wanted
+template <bool CAP, bool SLOPE>
+__device__ __forceinline__ void dq_elements(const SoftmaxArgs& args, const RowTerms& r, int j0, bool edge, bool want_dc, float (&s)[32],
+                                            const float (&dp)[32], uint32_t (&ds)[16], float (&dc)[4]) {
+#pragma unroll
+  for (int e = 0; e < 32; e += 2) {
+    float d[2];
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const int j = j0 + e + z;
+      const float x = score_of<CAP, SLOPE>(args, s[e + z], r.slope, (float)(j - r.i));
+      float p = exp2_fast(fmaf(x, r.a, -r.lse2));
+      if (edge) p = j >= r.sees.x && j < r.sees.y ? p : 0.f;
+      d[z] = p * (dp[e + z] - r.dot);
+      if (CAP) d[z] *= fmaf(-s[e + z], s[e + z], 1.0f);
+      if (want_dc) {
+        const float u = p * dp[e + z];
+        dc[0] = fmaf(u, x, dc[0]);
+        dc[1] += u;
+        dc[2] = fmaf(p, x, dc[2]);
+        dc[3] += p;
+      }
+    }
+    ds[e >> 1] = bf16x2(d[0], d[1]);
+  }
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
+                                                                    const __grid_constant__ BwdArgs f) {
+  pdl_begin();
+  using C = BwdCfg<HD>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_smem = sbase, do_smem = q_smem + C::kTile, k_smem = do_smem + C::kTile, v_smem = k_smem + C::kKStages * C::kTile;
+  const uint32_t bars = v_smem + C::kVStages * C::kTile;
+  const uint32_t work_at = bars, answer = bars + 64;
+  const uint32_t q_full = bars + 80, q_empty = bars + 88;
+  const uint32_t k_full = bars + 96, k_empty = bars + 120;           // [3]
+  const uint32_t v_full = bars + 144, v_empty = bars + 160;          // [2]
+  const uint32_t s_full = bars + 176, s_empty = bars + 184;          // S and dP of a tile
+  const uint32_t ds_full = bars + 192, ds_empty = bars + 200;
+  const uint32_t dq_full = bars + 208, dq_empty = bars + 216;
+  const uint32_t w_full = bars + 224, w_empty = bars + 240;          // [2]
+  const uint32_t next_bar = bars + 256, drain_bar = bars + 264, x_bar = bars + 272;
+  const uint32_t tmem_slot = bars + 280, abort_flag = bars + 284, drain_fail = bars + 288;
+  const uint32_t dot_at = bars + 320;                                // float [2][128]: of this item and the one before
+  const BwdWork* work = reinterpret_cast<const BwdWork*>(smem_raw + (work_at - smem_u32(smem_raw)));
+  constexpr int kS = 0, kDP = kT, kDQ = 2 * kT, kDS = 2 * kT + 128;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
+    for (int st = 0; st < C::kKStages; ++st) { mbar_init(k_full + 8 * st, 1); mbar_init(k_empty + 8 * st, 1); }
+    for (int st = 0; st < C::kVStages; ++st) { mbar_init(v_full + 8 * st, 1); mbar_init(v_empty + 8 * st, 1); }
+    mbar_init(s_full, 1);
+    mbar_init(s_empty, kWarps);
+    mbar_init(ds_full, kWarps);
+    mbar_init(ds_empty, 1);
+    mbar_init(dq_full, 1);
+    mbar_init(dq_empty, kWarps);
+    for (int t = 0; t < 2; ++t) { mbar_init(w_full + 8 * t, 1); mbar_init(w_empty + 8 * t, 1 + kWarps); }
+    mbar_init(next_bar, 1);
+    mbar_init(drain_bar, 1);
+    mbar_init(x_bar, kWarps);
+    sts_u32(abort_flag, 0u);
+    sts_u32(drain_fail, 0u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = lds_u32(tmem_slot);
+  const SoftmaxArgs& a = f.a;
+  auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
+
+  if (warp == 0) {
+    uint32_t next_phase = 0, wphase = 0, qphase = 0, kidx = 0, vidx = 0;
+    int slot = 0;
+    bool alive = true, asked = false;
+    int item = (int)blockIdx.x;
+    while (alive) {
+      BwdWork w = {};
+      w.valid = item >= 0;
+      if (item >= 0) {
+        asked = true;
+        if (elect_one()) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          mbar_expect_tx(next_bar, 16);
+          next_cta_request(answer, next_bar);
+        }
+        __syncwarp();
+        const int bh = item / f.tiles;
+        w.tile = f.tiles - 1 - (item - bh * f.tiles);
+        w.b = bh / a.H;
+        w.h = bh - w.b * a.H;
+        const int row0 = w.tile * kT;
+        if (a.ranges) {
+          const int4 s = span_of(a, w.b, row0);
+          if (w.h == 0 && lane == 0) f.spans[w.b * f.tiles + w.tile] = s;
+          if (s.y > s.x) { w.lo = s.x / kT; w.hi = (s.y + kT - 1) / kT; }
+        } else {
+          w.hi = ((a.causal ? min(row0 + kT, a.N) : a.N) + kT - 1) / kT;
+        }
+      }
+      alive = wait_all(w_empty + 8 * slot, wphase ^ 1u);
+      if (!alive) break;
+      if (lane == 0) {
+        *const_cast<BwdWork*>(work + slot) = w;
+        mbar_arrive(w_full + 8 * slot);
+      }
+      __syncwarp();
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (item < 0) break;
+      if (w.hi > w.lo) {
+        alive = wait_all(q_empty, qphase ^ 1u);
+        if (!alive) break;
+        qphase ^= 1u;
+        if (elect_one()) {
+          mbar_expect_tx(q_full, 2 * C::kTile);
+          for (int hf = 0; hf < C::kHalves; ++hf) {
+            tma_load_4d(q_smem + hf * (kT * 128), &map_q, q_full, hf * 64, w.tile * kT, w.h, w.b);
+            tma_load_4d(do_smem + hf * (kT * 128), &map_do, q_full, hf * 64, w.tile * kT, w.h, w.b);
+          }
+        }
+        __syncwarp();
+        const int kh = w.h / a.G;
+        for (int j = w.hi - 1; j >= w.lo && alive; --j) {
+          const int ks = kidx % C::kKStages, vs = vidx % C::kVStages;
+          alive = wait_all(k_empty + 8 * ks, ((kidx / C::kKStages) & 1u) ^ 1u);
+          if (!alive) break;
+          ++kidx;
+          if (elect_one()) {
+            mbar_expect_tx(k_full + 8 * ks, C::kTile);
+            for (int hf = 0; hf < C::kHalves; ++hf)
+              tma_load_4d(k_smem + ks * C::kTile + hf * (kT * 128), &map_k, k_full + 8 * ks, hf * 64, j * kT, kh, w.b);
+          }
+          __syncwarp();
+          alive = wait_all(v_empty + 8 * vs, ((vidx / C::kVStages) & 1u) ^ 1u);
+          if (!alive) break;
+          ++vidx;
+          if (elect_one()) {
+            mbar_expect_tx(v_full + 8 * vs, C::kTile);
+            for (int hf = 0; hf < C::kHalves; ++hf)
+              tma_load_4d(v_smem + vs * C::kTile + hf * (kT * 128), &map_v, v_full + 8 * vs, hf * 64, j * kT, kh, w.b);
+          }
+          __syncwarp();
+        }
+        if (!alive) break;
+      }
+      alive = wait_all(next_bar, next_phase);
+      if (!alive) break;
+      next_phase ^= 1u;
+      asked = false;
+      item = next_cta_answer(answer);
+      __syncwarp();
+    }
+    if (!alive && lane == 0) {
+      bool ok = mbar_drain(q_full, qphase ^ 1u);
+      for (uint32_t st = 0; st < C::kKStages; ++st) ok &= mbar_drain(k_full + 8 * st, ((kidx / C::kKStages + (st < kidx % C::kKStages ? 1u : 0u)) & 1u) ^ 1u);
+      for (uint32_t st = 0; st < C::kVStages; ++st) ok &= mbar_drain(v_full + 8 * st, ((vidx / C::kVStages + (st < vidx % C::kVStages ? 1u : 0u)) & 1u) ^ 1u);
+      if (asked) ok &= mbar_drain(next_bar, next_phase);
+      if (!ok) sts_u32(drain_fail, 1u);
+    }
+  } else if (warp == 1) {
+    constexpr uint32_t id_kk = bwd_idesc_kk(), id_kn = bwd_idesc_kn<HD>();
+    const uint64_t dhi = (uint64_t)kDescHi << 32;
+    const uint64_t q_d = dhi | smem_desc_lo(q_smem), do_d = dhi | smem_desc_lo(do_smem), k_d = dhi | smem_desc_lo(k_smem),
+                   v_d = dhi | smem_desc_lo(v_smem), kn_d = dhi | mn_desc_lo(k_smem);
+    constexpr uint32_t kStageD = C::kTile >> 4;
+    uint32_t wphase = 0, qphase = 0, sphase = 0, dsphase = 0, dqphase = 0, kidx = 0, vidx = 0;
+    int slot = 0;
+    bool alive = true;
+    while (alive) {
+      alive = wait_all(w_full + 8 * slot, wphase);
+      if (!alive) break;
+      const int valid = work[slot].valid, lo = work[slot].lo, hi = work[slot].hi;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (!valid) break;
+      if (hi <= lo) continue;
+      alive = wait_all(q_full, qphase);
+      if (!alive) break;
+      qphase ^= 1u;
+      auto issue_s = [&](bool last) -> bool {
+        const uint32_t ks = kidx % C::kKStages, vs = vidx % C::kVStages;
+        bool ok = wait_all(k_full + 8 * ks, (kidx / C::kKStages) & 1u);
+        if (ok) ok = wait_all(v_full + 8 * vs, (vidx / C::kVStages) & 1u);
+        if (ok) ok = wait_all(s_empty, sphase ^ 1u);
+        if (!ok) return false;
+        ++kidx;
+        ++vidx;
+        sphase ^= 1u;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * ((kT * 128) >> 4) + (kk & 3) * 2;
+            umma_bf16_desc(tmem + kS, q_d + off, k_d + ks * kStageD + off, id_kk, kk > 0 ? 1u : 0u);
+          }
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * ((kT * 128) >> 4) + (kk & 3) * 2;
+            umma_bf16_desc(tmem + kDP, do_d + off, v_d + vs * kStageD + off, id_kk, kk > 0 ? 1u : 0u);
+          }
+          umma_commit(s_full);
+          umma_commit(v_empty + 8 * vs);
+          if (last) umma_commit(q_empty);
+        }
+        __syncwarp();
+        return true;
+      };
+      uint32_t kq = kidx;                        // the K tile the next dQ reads
+      alive = issue_s(hi - lo == 1);
+      for (int j = hi - 1; j >= lo && alive; --j, ++kq) {
+        if (j > lo) {
+          alive = issue_s(j == lo + 1);
+          if (!alive) break;
+        }
+        alive = wait_all(ds_full, dsphase);
+        if (!alive) break;
+        dsphase ^= 1u;
+        if (j == hi - 1) {
+          alive = wait_all(dq_empty, dqphase ^ 1u);
+          if (!alive) break;
+          dqphase ^= 1u;
+        }
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t kn = kn_d + (kq % C::kKStages) * kStageD;
+#pragma unroll
+          for (int kk = 0; kk < kT / 16; ++kk)
+            umma_bf16_ts(tmem + kDQ, tmem + kDS + kk * 8, kn + kk * ((16 * 128) >> 4), id_kn, (j < hi - 1 || kk > 0) ? 1u : 0u);
+          umma_commit(k_empty + 8 * (kq % C::kKStages));
+          umma_commit(ds_empty);
+          if (j == lo) umma_commit(dq_full);
+        }
+        __syncwarp();
+      }
+    }
+    if (!alive && lane == 0) {
+      umma_commit(drain_bar);
+      if (!mbar_drain(drain_bar, 0u)) sts_u32(drain_fail, 1u);
+    }
+  } else {
+    const int quad = warp & 3, quarter = (warp - 2) >> 2, row = quad * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
+    uint32_t wphase = 0, sphase = 0, dsphase = 0, dqphase = 0, xphase = 0, dot_buf = 0;
+    int slot = 0;
+    bool alive = true;
+    const bool want_dc = f.g.dc_rows != nullptr;
+    while (alive) {
+      alive = wait_all(w_full + 8 * slot, wphase);
+      if (!alive) break;
+      const int valid = work[slot].valid, b = work[slot].b, h = work[slot].h, tile = work[slot].tile, lo = work[slot].lo, hi = work[slot].hi;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (!valid) break;
+      // D of the tile's rows, eight rows a warp: a row's 32 lanes read D / 32 elements each of O and dO
+      {
+        constexpr int E = HD / 32;
+        const int first = (warp - 2) * 8;
+        float part[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const int i = tile * kT + first + r;
+          part[r] = 0.f;
+          if (i < a.N) {
+            float x[E], y[E];
+            load_slice<E>(f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n + lane * E, x);
+            load_slice<E>(f.d_o + (long long)b * f.g.d_o.b + (long long)h * f.g.d_o.h + (long long)i * f.g.d_o.n + lane * E, y);
+#pragma unroll
+            for (int e = 0; e < E; ++e) part[r] = fmaf(x[e], y[e], part[r]);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) part[r] = warp_sum(part[r]);
+        if (lane == 0)
+          for (int r = 0; r < 8; ++r) sts_u32(dot_at + dot_buf + 4 * (first + r), __float_as_uint(part[r]));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(x_bar);
+        alive = wait_all(x_bar, xphase);
+        if (!alive) break;
+        xphase ^= 1u;
+      }
+      RowTerms r;
+      r.i = tile * kT + row;
+      r.dot = __uint_as_float(lds_u32(dot_at + dot_buf + 4 * row));
+      dot_buf ^= 512u;
+      const bool mine = r.i < a.N;
+      r.sees = mine ? visible_keys(a, b, r.i) : make_int2(0, 0);
+      const size_t at = ((size_t)b * a.H + h) * a.N + (mine ? r.i : 0);
+      const bool some = r.sees.y > r.sees.x;
+      const float g = mine ? row_scale(a, b, h, r.i, r.sees.y - r.sees.x) * a.sm_scale : 0.f;
+      r.a = g * kLog2e;
+      r.lse2 = some ? f.g.lse[at] * kLog2e : INFINITY;
+      r.slope = a.alibi ? a.alibi[h] / a.sm_scale : 0.f;
+      if (!some) { r.sees = make_int2(0, 0x7fffffff); r.a = 0.f; }   // (probability exp2(-inf) everywhere, without a mask)
+      if (quarter == 0) {
+        float* out = f.rows + ((size_t)(b * a.H + h) * f.tiles + tile) * (3 * kT) + row;
+        out[0] = r.lse2;
+        out[kT] = r.a;
+        out[2 * kT] = r.dot;
+      }
+      float dc[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int j = hi - 1; j >= lo && alive; --j) {
+        alive = wait_all(s_full, sphase);
+        if (!alive) break;
+        sphase ^= 1u;
+        tc_fence_after();
+        float s[32], dp[32];
+        tmem_ld32(lane_base + kS + quarter * 32, s);
+        tmem_ld32(lane_base + kDP + quarter * 32, dp);
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_empty);
+        const int j0 = j * kT + quarter * 32;
+        const bool edge = __any_sync(0xffffffffu, r.sees.x > j0 || r.sees.y < j0 + 32);
+        uint32_t ds[16];
+        if (a.cap_acc > 0.f) {
+          to_tanh(a.cap_inv, s);
+          if (r.slope != 0.f) dq_elements<true, true>(a, r, j0, edge, want_dc, s, dp, ds, dc);
+          else dq_elements<true, false>(a, r, j0, edge, want_dc, s, dp, ds, dc);
+        } else {
+          if (r.slope != 0.f) dq_elements<false, true>(a, r, j0, edge, want_dc, s, dp, ds, dc);
+          else dq_elements<false, false>(a, r, j0, edge, want_dc, s, dp, ds, dc);
+        }
+        // the dS before has been taken
+        alive = wait_all(ds_empty, dsphase ^ 1u);
+        if (!alive) break;
+        dsphase ^= 1u;
+        tc_fence_after();
+        tmem_st16(lane_base + kDS + quarter * 16, ds);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ds_full);
+      }
+      if (!alive) break;
+      const bool any = hi > lo;
+      if (any) {
+        alive = wait_all(dq_full, dqphase);
+        if (!alive) break;
+        dqphase ^= 1u;
+        tc_fence_after();
+      }
+      if (quarter < HD / 32) {
+        float v[32];
+        if (any) {
+          tmem_ld32(lane_base + kDQ + quarter * 32, v);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = 0.f;
+        }
+        if (mine) {
+          __nv_bfloat16* out = f.dq + (long long)b * f.g.dq.b + (long long)h * f.g.dq.h + (long long)r.i * f.g.dq.n + quarter * 32;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float* x = v + 8 * e;
+            *reinterpret_cast<uint4*>(out + 8 * e) = make_uint4(bf16x2(x[0] * g, x[1] * g), bf16x2(x[2] * g, x[3] * g), bf16x2(x[4] * g, x[5] * g),
+                                                                bf16x2(x[6] * g, x[7] * g));
+          }
+        }
+      }
+      if (want_dc) {
+        // the four threads of a row meet through the dS columns, which nobody needs until the next item's first dS is written: behind dq_empty of all
+        const uint32_t mine_at = lane_base + kDS + quarter * 16;
+        uint32_t u[8] = {__float_as_uint(dc[0]), __float_as_uint(dc[1]), __float_as_uint(dc[2]), __float_as_uint(dc[3]), 0u, 0u, 0u, 0u};
+        tmem_st8(mine_at, u);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(x_bar);
+        alive = wait_all(x_bar, xphase);
+        if (!alive) break;
+        xphase ^= 1u;
+        tc_fence_after();
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int qq = 0; qq < 4; ++qq) {
+          float v[8];
+          tmem_ld8(lane_base + kDS + qq * 16, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] += v[e];
+        }
+        if (quarter == 0 && mine) f.g.dc_rows[at] = some ? (sum[0] - sum[1] * (sum[2] / sum[3])) * a.sm_scale : 0.f;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(x_bar);       // (all have read before anyone writes the next item's dS there)
+        alive = wait_all(x_bar, xphase);
+        if (!alive) break;
+        xphase ^= 1u;
+        tc_fence_after();
+      }
+      if (any) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(dq_empty);
+      }
+    }
+  }
+  bwd_teardown(tmem, abort_flag, drain_fail, f.status);
+}
+
+// ------------------------------------------------------------------------------------------------ dK, dV
+// The Q tiles that see a K/V tile, in order; all roles walk them alike.  Ranges: 32 tiles' spans are looked at together.
+struct QTiles {
+  int tiles, first, b, k0;
+  const int4* spans;
+  int base;              // mask: those of the tiles base .. base + 31 that see the keys
+  uint32_t mask;
+  __device__ __forceinline__ void start(const BwdArgs& f, int batch, int kt) {
+    tiles = f.tiles;
+    b = batch;
+    k0 = kt * kT;
+    spans = f.a.ranges ? f.spans + (size_t)batch * f.tiles : nullptr;
+    first = f.a.causal && !spans ? kt : 0;
+    rewind();
+  }
+  __device__ __forceinline__ void rewind() {
+    base = -32;
+    mask = 0u;
+    if (!spans) base = first - 1;
+  }
+  // the next tile, or -1 (the whole warp)
+  __device__ __forceinline__ int next() {
+    if (!spans) return ++base < tiles ? base : -1;
+    while (mask == 0u) {
+      base += 32;
+      if (base >= tiles) return -1;
+      const int t = base + (threadIdx.x & 31);
+      bool sees = false;
+      if (t < tiles) {
+        const int4 s = spans[t];
+        sees = s.x < k0 + kT && s.y > k0;
+      }
+      mask = __ballot_sync(0xffffffffu, sees);
+    }
+    const int bit = __ffs(mask) - 1;
+    mask &= mask - 1u;
+    return base + bit;
+  }
+};
+
+// 32 queries (columns) of one key (lane): P^T as bf16 pairs, the scores' tanh (CAP) or nothing left in s, p kept in place of s otherwise
+template <bool CAP, bool SLOPE>
+__device__ __forceinline__ void dkv_probabilities(const SoftmaxArgs& args, float slope, int key, int i0, uint32_t rows_at, float (&s)[32], float (&p)[32]) {
+#pragma unroll
+  for (int e = 0; e < 32; e += 4) {
+    float l[4], m[4];
+    lds_f4(rows_at + 4 * e, l[0], l[1], l[2], l[3]);
+    lds_f4(rows_at + 4 * (kT + e), m[0], m[1], m[2], m[3]);
+#pragma unroll
+    for (int z = 0; z < 4; ++z)
+      p[e + z] = exp2_fast(fmaf(score_of<CAP, SLOPE>(args, s[e + z], slope, (float)(i0 + e + z - key)), m[z], -l[z]));
+  }
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
+                                                                     const __grid_constant__ BwdArgs f) {
+  pdl_begin();
+  using C = BwdCfg<HD>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t k_smem = sbase, v_smem = k_smem + C::kTile, q_smem = v_smem + C::kTile, do_smem = q_smem + 2 * C::kTile;
+  const uint32_t rows_smem = do_smem + 2 * C::kTile;                 // [2][3][128] floats
+  const uint32_t bars = rows_smem + 2 * C::kRowBytes;
+  const uint32_t work_at = bars, answer = bars + 64;
+  const uint32_t kv_full = bars + 80, kv_empty = bars + 88;
+  const uint32_t q_full = bars + 96, q_empty = bars + 112;           // [2], with the rows' terms
+  const uint32_t do_full = bars + 128, do_empty = bars + 144;        // [2]
+  const uint32_t s_full = bars + 160, p_full = bars + 168, dp_full = bars + 176, ds_full = bars + 184;
+  const uint32_t acc_full = bars + 192, acc_empty = bars + 200;
+  const uint32_t w_full = bars + 208, w_empty = bars + 224;          // [2]
+  const uint32_t r_empty = bars + 240;                               // [2] the rows' terms have been read
+  const uint32_t next_bar = bars + 256, drain_bar = bars + 264;
+  const uint32_t tmem_slot = bars + 272, abort_flag = bars + 276, drain_fail = bars + 280;
+  const BwdWork* work = reinterpret_cast<const BwdWork*>(smem_raw + (work_at - smem_u32(smem_raw)));
+  constexpr int kS = 0, kDP = kT, kDK = 2 * kT, kDV = 2 * kT + HD;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    mbar_init(kv_full, 1);
+    mbar_init(kv_empty, 1);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(q_full + 8 * t, 1);
+      mbar_init(q_empty + 8 * t, 1);
+      mbar_init(do_full + 8 * t, 1);
+      mbar_init(do_empty + 8 * t, 1);
+      mbar_init(w_full + 8 * t, 1);
+      mbar_init(w_empty + 8 * t, 1 + kWarps);
+      mbar_init(r_empty + 8 * t, kWarps);
+    }
+    mbar_init(s_full, 1);
+    mbar_init(p_full, kWarps);
+    mbar_init(dp_full, 1);
+    mbar_init(ds_full, kWarps);
+    mbar_init(acc_full, 1);
+    mbar_init(acc_empty, kWarps);
+    mbar_init(next_bar, 1);
+    mbar_init(drain_bar, 1);
+    sts_u32(abort_flag, 0u);
+    sts_u32(drain_fail, 0u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = lds_u32(tmem_slot);
+  const SoftmaxArgs& a = f.a;
+  auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
+
+  if (warp == 0) {
+    uint32_t next_phase = 0, wphase = 0, kvphase = 0, idx = 0;       // idx: steps loaded so far
+    int slot = 0;
+    bool alive = true, asked = false;
+    int item = (int)blockIdx.x;
+    while (alive) {
+      BwdWork w = {};
+      w.valid = item >= 0;
+      if (item >= 0) {
+        asked = true;
+        if (elect_one()) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          mbar_expect_tx(next_bar, 16);
+          next_cta_request(answer, next_bar);
+        }
+        __syncwarp();
+        const int bk = item / f.tiles;
+        w.tile = item - bk * f.tiles;
+        w.b = bk / a.KH;
+        w.h = bk - w.b * a.KH;
+      }
+      alive = wait_all(w_empty + 8 * slot, wphase ^ 1u);
+      if (!alive) break;
+      if (lane == 0) {
+        *const_cast<BwdWork*>(work + slot) = w;
+        mbar_arrive(w_full + 8 * slot);
+      }
+      __syncwarp();
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (item < 0) break;
+      QTiles qt;
+      qt.start(f, w.b, w.tile);
+      bool first = true;
+      for (int g = 0; g < a.G && alive; ++g) {
+        const int h = w.h * a.G + g;
+        qt.rewind();
+        for (int t = qt.next(); t >= 0 && alive; t = qt.next(), ++idx) {
+          const int st = idx & 1;
+          const uint32_t parity = ((idx >> 1) & 1u) ^ 1u;
+          if (first) {
+            first = false;
+            alive = wait_all(kv_empty, kvphase ^ 1u);
+            if (!alive) break;
+            kvphase ^= 1u;
+            if (elect_one()) {
+              mbar_expect_tx(kv_full, 2 * C::kTile);
+              for (int hf = 0; hf < C::kHalves; ++hf) {
+                tma_load_4d(k_smem + hf * (kT * 128), &map_k, kv_full, hf * 64, w.tile * kT, w.h, w.b);
+                tma_load_4d(v_smem + hf * (kT * 128), &map_v, kv_full, hf * 64, w.tile * kT, w.h, w.b);
+              }
+            }
+            __syncwarp();
+          }
+          alive = wait_all(q_empty + 8 * st, parity);
+          if (alive) alive = wait_all(r_empty + 8 * st, parity);
+          if (!alive) break;
+          if (elect_one()) {
+            mbar_expect_tx(q_full + 8 * st, C::kTile + C::kRowBytes);
+            for (int hf = 0; hf < C::kHalves; ++hf)
+              tma_load_4d(q_smem + st * C::kTile + hf * (kT * 128), &map_q, q_full + 8 * st, hf * 64, t * kT, h, w.b);
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                             rows_smem + st * C::kRowBytes),
+                         "l"(reinterpret_cast<uint64_t>(f.rows + ((size_t)(w.b * a.H + h) * f.tiles + t) * (3 * kT))), "r"(C::kRowBytes),
+                         "r"(q_full + 8 * st)
+                         : "memory");
+          }
+          __syncwarp();
+          alive = wait_all(do_empty + 8 * st, parity);
+          if (!alive) {
+            ++idx;                               // (Q of this step is on its way)
+            break;
+          }
+          if (elect_one()) {
+            mbar_expect_tx(do_full + 8 * st, C::kTile);
+            for (int hf = 0; hf < C::kHalves; ++hf)
+              tma_load_4d(do_smem + st * C::kTile + hf * (kT * 128), &map_do, do_full + 8 * st, hf * 64, t * kT, h, w.b);
+          }
+          __syncwarp();
+        }
+      }
+      if (!alive) break;
+      alive = wait_all(next_bar, next_phase);
+      if (!alive) break;
+      next_phase ^= 1u;
+      asked = false;
+      item = next_cta_answer(answer);
+      __syncwarp();
+    }
+    if (!alive && lane == 0) {
+      bool ok = mbar_drain(kv_full, kvphase ^ 1u);
+      for (uint32_t st = 0; st < 2; ++st) {
+        const uint32_t armed = (idx >> 1) + (st < (idx & 1u) ? 1u : 0u);
+        ok &= mbar_drain(q_full + 8 * st, (armed & 1u) ^ 1u);
+        ok &= mbar_drain(do_full + 8 * st, (armed & 1u) ^ 1u);       // (one armed less at most: its phase has passed, or this wait ends by its bound)
+      }
+      if (asked) ok &= mbar_drain(next_bar, next_phase);
+      if (!ok) sts_u32(drain_fail, 1u);
+    }
+  } else if (warp == 1) {
+    constexpr uint32_t id_kk = bwd_idesc_kk(), id_kn = bwd_idesc_kn<HD>();
+    const uint64_t dhi = (uint64_t)kDescHi << 32;
+    const uint64_t q_d = dhi | smem_desc_lo(q_smem), do_d = dhi | smem_desc_lo(do_smem), k_d = dhi | smem_desc_lo(k_smem),
+                   v_d = dhi | smem_desc_lo(v_smem), qn_d = dhi | mn_desc_lo(q_smem), don_d = dhi | mn_desc_lo(do_smem);
+    constexpr uint32_t kStageD = C::kTile >> 4;
+    uint32_t wphase = 0, kvphase = 0, pphase = 0, dsphase = 0, accphase = 0, idx = 0;
+    int slot = 0;
+    bool alive = true;
+    while (alive) {
+      alive = wait_all(w_full + 8 * slot, wphase);
+      if (!alive) break;
+      const BwdWork w = work[slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (!w.valid) break;
+      QTiles qt;
+      qt.start(f, w.b, w.tile);
+      int count = 0;
+      for (int t = qt.next(); t >= 0; t = qt.next()) ++count;
+      const int steps = count * a.G;
+      if (steps == 0) continue;
+      alive = wait_all(kv_full, kvphase);
+      if (!alive) break;
+      kvphase ^= 1u;
+      // S^T of step i: over the P^T before, which dV has taken by then (the tensor core works in order)
+      auto issue_s = [&](uint32_t i) -> bool {
+        const uint32_t st = i & 1u;
+        if (!wait_all(q_full + 8 * st, (i >> 1) & 1u)) return false;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * ((kT * 128) >> 4) + (kk & 3) * 2;
+            umma_bf16_desc(tmem + kS, k_d + off, q_d + st * kStageD + off, id_kk, kk > 0 ? 1u : 0u);
+          }
+          umma_commit(s_full);
+        }
+        __syncwarp();
+        return true;
+      };
+      auto issue_dp = [&](uint32_t i) -> bool {
+        const uint32_t st = i & 1u;
+        if (!wait_all(do_full + 8 * st, (i >> 1) & 1u)) return false;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * ((kT * 128) >> 4) + (kk & 3) * 2;
+            umma_bf16_desc(tmem + kDP, v_d + off, do_d + st * kStageD + off, id_kk, kk > 0 ? 1u : 0u);
+          }
+          umma_commit(dp_full);
+        }
+        __syncwarp();
+        return true;
+      };
+      alive = issue_s(idx);
+      if (alive) alive = issue_dp(idx);
+      for (int n = 0; n < steps && alive; ++n, ++idx) {
+        const uint32_t st = idx & 1u;
+        alive = wait_all(p_full, pphase);
+        if (!alive) break;
+        pphase ^= 1u;
+        if (n == 0) {
+          alive = wait_all(acc_empty, accphase ^ 1u);
+          if (!alive) break;
+          accphase ^= 1u;
+        }
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < kT / 16; ++kk)
+            umma_bf16_ts(tmem + kDV, tmem + kS + a_column(kk), don_d + st * kStageD + kk * ((16 * 128) >> 4), id_kn, (n > 0 || kk > 0) ? 1u : 0u);
+          umma_commit(do_empty + 8 * st);        // (dP of this step came before)
+        }
+        __syncwarp();
+        if (n + 1 < steps) {
+          alive = issue_s(idx + 1);
+          if (!alive) break;
+        }
+        alive = wait_all(ds_full, dsphase);
+        if (!alive) break;
+        dsphase ^= 1u;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < kT / 16; ++kk)
+            umma_bf16_ts(tmem + kDK, tmem + kDP + a_column(kk), qn_d + st * kStageD + kk * ((16 * 128) >> 4), id_kn, (n > 0 || kk > 0) ? 1u : 0u);
+          umma_commit(q_empty + 8 * st);
+          if (n + 1 == steps) {
+            umma_commit(kv_empty);
+            umma_commit(acc_full);
+          }
+        }
+        __syncwarp();
+        if (n + 1 < steps) alive = issue_dp(idx + 1);
+      }
+    }
+    if (!alive && lane == 0) {
+      umma_commit(drain_bar);
+      if (!mbar_drain(drain_bar, 0u)) sts_u32(drain_fail, 1u);
+    }
+  } else {
+    const int quad = warp & 3, quarter = (warp - 2) >> 2, row = quad * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
+    uint32_t wphase = 0, sphase = 0, dpphase = 0, accphase = 0, idx = 0;
+    int slot = 0;
+    bool alive = true;
+    while (alive) {
+      alive = wait_all(w_full + 8 * slot, wphase);
+      if (!alive) break;
+      const int valid = work[slot].valid, b = work[slot].b, kh = work[slot].h, kt = work[slot].tile;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (!valid) break;
+      QTiles qt;
+      qt.start(f, b, kt);
+      const int key = kt * kT + row;
+      const bool mine = key < a.N;
+      bool any = false;
+      for (int g = 0; g < a.G && alive; ++g) {
+        const float slope = a.alibi ? a.alibi[kh * a.G + g] / a.sm_scale : 0.f;
+        qt.rewind();
+        for (int t = qt.next(); t >= 0 && alive; t = qt.next(), ++idx) {
+          any = true;
+          const uint32_t st = idx & 1u;
+          const int i0 = t * kT + quarter * 32;
+          const uint32_t rows_at = rows_smem + st * C::kRowBytes + quarter * 128;
+          bool edge;
+          if (a.ranges) {
+            const int4 s = qt.spans[t];
+            edge = s.z > kt * kT || s.w < (kt + 1) * kT;
+          } else {
+            edge = a.causal && t == kt;
+          }
+          alive = wait_all(s_full, sphase);
+          if (alive) alive = wait_all(q_full + 8 * st, (idx >> 1) & 1u);   // (the rows' terms; long there)
+          if (!alive) break;
+          sphase ^= 1u;
+          tc_fence_after();
+          float s[32], p[32];
+          tmem_ld32(lane_base + kS + quarter * 32, s);
+          tmem_ld_wait();
+          if (a.cap_acc > 0.f) {
+            to_tanh(a.cap_inv, s);
+            if (slope != 0.f) dkv_probabilities<true, true>(a, slope, key, i0, rows_at, s, p);
+            else dkv_probabilities<true, false>(a, slope, key, i0, rows_at, s, p);
+          } else {
+            if (slope != 0.f) dkv_probabilities<false, true>(a, slope, key, i0, rows_at, s, p);
+            else dkv_probabilities<false, false>(a, slope, key, i0, rows_at, s, p);
+          }
+          if (edge) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const int i = min(i0 + e, a.N - 1);
+              const int2 sees = visible_keys(a, b, i);
+              p[e] = key >= sees.x && key < sees.y ? p[e] : 0.f;
+            }
+          }
+          uint32_t u[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) u[e] = bf16x2(p[2 * e], p[2 * e + 1]);
+          tmem_st16(lane_base + kS + quarter * 32, u);
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full);
+          alive = wait_all(dp_full, dpphase);
+          if (!alive) break;
+          dpphase ^= 1u;
+          tc_fence_after();
+          float dp[32];
+          tmem_ld32(lane_base + kDP + quarter * 32, dp);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            float m[4], d[4];
+            lds_f4(rows_at + 4 * (kT + e), m[0], m[1], m[2], m[3]);
+            lds_f4(rows_at + 4 * (2 * kT + e), d[0], d[1], d[2], d[3]);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+              dp[e + z] = p[e + z] * m[z] * (dp[e + z] - d[z]);
+              if (a.cap_acc > 0.f) dp[e + z] *= fmaf(-s[e + z], s[e + z], 1.0f);
+            }
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(r_empty + 8 * st);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) u[e] = bf16x2(dp[2 * e], dp[2 * e + 1]);
+          tmem_st16(lane_base + kDP + quarter * 32, u);
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(ds_full);
+        }
+      }
+      if (!alive) break;
+      if (any) {
+        alive = wait_all(acc_full, accphase);
+        if (!alive) break;
+        accphase ^= 1u;
+        tc_fence_after();
+      }
+      if (quarter < HD / 32) {
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+          float v[32];
+          if (any) {
+            tmem_ld32(lane_base + (which ? kDV : kDK) + quarter * 32, v);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = 0.f;
+          }
+          if (mine) {
+            const entmax_attn_strides& s = which ? f.g.dv : f.g.dk;
+            __nv_bfloat16* out = (which ? f.dv : f.dk) + (long long)b * s.b + (long long)kh * s.h + (long long)key * s.n + quarter * 32;
+            const float mul = which ? 1.0f : kLn2;               // (the rows' a has log2 e in it)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float* x = v + 8 * e;
+              *reinterpret_cast<uint4*>(out + 8 * e) = make_uint4(bf16x2(x[0] * mul, x[1] * mul), bf16x2(x[2] * mul, x[3] * mul),
+                                                                  bf16x2(x[4] * mul, x[5] * mul), bf16x2(x[6] * mul, x[7] * mul));
+            }
+          }
+        }
+      }
+      if (any) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acc_empty);
+      }
+    }
+  }
+  bwd_teardown(tmem, abort_flag, drain_fail, f.status);
+}
+
+template <int HD>
+cudaError_t bwd_launch(const BwdArgs& f, const void* q, const void* k, const void* v, const void* d_o, cudaStream_t stream) {
+  const SoftmaxArgs& a = f.a;
+  CUtensorMap map_q, map_k, map_v, map_do;
+  cudaError_t err = make_tile_map(&map_q, q, a.D, a.N, a.H, a.B, a.q.n, a.q.h, a.q.b);
+  if (err == cudaSuccess) err = make_tile_map(&map_k, k, a.D, a.N, a.KH, a.B, a.k.n, a.k.h, a.k.b);
+  if (err == cudaSuccess) err = make_tile_map(&map_v, v, a.D, a.N, a.KH, a.B, a.v.n, a.v.h, a.v.b);
+  if (err == cudaSuccess) err = make_tile_map(&map_do, d_o, a.D, a.N, a.H, a.B, f.g.d_o.n, f.g.d_o.h, f.g.d_o.b);
+  if (err == cudaSuccess) err = cudaFuncSetAttribute(softmax_dq_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdCfg<HD>::kSmemQ);
+  if (err == cudaSuccess) err = cudaFuncSetAttribute(softmax_dkv_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdCfg<HD>::kSmemKV);
+  if (err != cudaSuccess) return err;
+  err = launch_kernel(softmax_dq_kernel<HD>, (unsigned)((long long)a.B * a.H * f.tiles), kBwdThreads, BwdCfg<HD>::kSmemQ, stream, map_q, map_k, map_v,
+                      map_do, f);
+  if (err != cudaSuccess) return err;
+  return launch_kernel(softmax_dkv_kernel<HD>, (unsigned)((long long)a.B * a.KH * f.tiles), kBwdThreads, BwdCfg<HD>::kSmemKV, stream, map_q, map_k, map_v,
+                       map_do, f);
+}
+
+}  // namespace
+
+size_t softmax_bwd_rows_bytes(const SoftmaxArgs& a) { return (size_t)a.B * a.H * ((a.N + kT - 1) / kT) * (3 * kT) * 4; }
+size_t softmax_bwd_spans_bytes(const SoftmaxArgs& a) { return (size_t)a.B * ((a.N + kT - 1) / kT) * 16; }
+
+cudaError_t launch_softmax_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* o, const void* d_o,
+                               void* dq, void* dk, void* dv, float* rows, void* spans, int32_t* status, cudaStream_t stream) {
+  BwdArgs f = {};
+  f.a = a;
+  f.g = g;
+  f.tiles = (a.N + kT - 1) / kT;
+  f.o = static_cast<const __nv_bfloat16*>(o);
+  f.d_o = static_cast<const __nv_bfloat16*>(d_o);
+  f.dq = static_cast<__nv_bfloat16*>(dq);
+  f.dk = static_cast<__nv_bfloat16*>(dk);
+  f.dv = static_cast<__nv_bfloat16*>(dv);
+  f.rows = rows;
+  f.spans = static_cast<int4*>(spans);
+  f.status = status;
+  return a.D == 64 ? bwd_launch<64>(f, q, k, v, d_o, stream) : bwd_launch<128>(f, q, k, v, d_o, stream);
+}
+
+}  // namespace entmax

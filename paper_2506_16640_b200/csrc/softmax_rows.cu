@@ -372,10 +372,7 @@ cudaError_t launch_softmax_rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g,
   return a.D == 64 ? rows_bwd<64, T>(a, g, q, k, v, d_o, dq, dk, dv, stream) : rows_bwd<128, T>(a, g, q, k, v, d_o, dq, dk, dv, stream);
 }
 template cudaError_t launch_softmax_rows_fwd<float>(const SoftmaxArgs&, const void*, const void*, const void*, void*, float*, cudaStream_t);
-template cudaError_t launch_softmax_rows_fwd<__nv_bfloat16>(const SoftmaxArgs&, const void*, const void*, const void*, void*, float*, cudaStream_t);
 template cudaError_t launch_softmax_rows_bwd<float>(const SoftmaxArgs&, const SoftmaxGrads&, const void*, const void*, const void*, const void*, void*,
                                                     void*, void*, cudaStream_t);
-template cudaError_t launch_softmax_rows_bwd<__nv_bfloat16>(const SoftmaxArgs&, const SoftmaxGrads&, const void*, const void*, const void*,
-                                                            const void*, void*, void*, void*, cudaStream_t);
 
 }  // namespace entmax
