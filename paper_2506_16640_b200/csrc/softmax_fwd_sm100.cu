@@ -16,9 +16,8 @@
 // running CTA takes over one that has not started (longest rows of a head first).  Every wait is bounded (see sm100_ptx.cuh).
 #include <cuda.h>
 
-#include "paged.cuh"
 #include "sm100_ptx.cuh"
-#include "softmax.cuh"
+#include "softmax_paged.cuh"
 #include "softmax_tile.cuh"
 
 namespace entmax {
@@ -97,11 +96,7 @@ __device__ __forceinline__ int2 tile_span(const SoftmaxArgs& a, int b, int row0)
   return hi > lo ? make_int2(lo / kKeys, (hi + kKeys - 1) / kKeys) : make_int2(0, 0);
 }
 
-// Paged: block id -> sequence and first new token, by the whole warp.  Sequence b has the ids from cu[b] / block + b on, at least as many as it has blocks.
-__device__ __forceinline__ int block_start(const PagedCache& c, int b, int block) {
-  const int cu = c.cu_q ? clamped_cu(c, b) : b * (c.T / c.B);
-  return cu / block + b;
-}
+// Paged: the sequence of a block id, by the whole warp (see block_start)
 __device__ __forceinline__ int find_block(const PagedCache& c, int id, int block) {
   const int lane = threadIdx.x & 31;
   int lo = 0, n = c.B;
@@ -612,7 +607,35 @@ cudaError_t fwd_launch(const SoftmaxArgs& a, const void* q, const void* k, const
   return launch_kernel(softmax_fwd_kernel<HD, false>, grid, kFwdThreads, FwdCfg<HD>::kSmemBytes, stream, map_q, map_k, map_v, f);
 }
 
+template <int HD>
+cudaError_t chunks_launch(const SoftmaxPagedArgs& p, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t stream) {
+  CUtensorMap map_q;
+  cudaError_t err = make_tile_map(&map_q, p.q, p.c.D, p.c.T, p.H, 1, p.q_st, p.q_sh, p.c.T * p.q_st);
+  if (err == cudaSuccess)
+    err = cudaFuncSetAttribute(softmax_fwd_kernel<HD, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdCfg<HD>::kSmemBytes);
+  if (err != cudaSuccess) return err;
+  FwdArgs f = {};
+  f.a.B = p.c.B; f.a.H = p.H; f.a.KH = p.c.KH; f.a.G = p.G; f.a.D = p.c.D;
+  f.a.sm_scale = p.sm_scale; f.a.cap_acc = p.cap_acc; f.a.cap_inv = p.cap_inv;
+  f.a.beta = p.beta; f.a.gamma = p.gamma; f.a.delta = p.delta; f.a.alibi = p.alibi;
+  f.pair_heads = p.G % 2 == 0;
+  f.pairs = chunk_pairs(p.G);
+  f.o = p.o;
+  f.lse = p.lse;
+  f.status = p.status;
+  f.c = p.c;
+  f.window = p.window; f.max_q = p.max_q; f.max_kv = p.max_kv; f.few_rows = p.few_rows;
+  f.shares = p.shares; f.box_shift = p.box_shift;
+  f.part_o = p.chunk_o; f.part_ml = p.chunk_ml;
+  const long long units = ((long long)p.c.T / chunk_block(p.G) + p.c.B) * p.c.KH * f.pairs;
+  return launch_kernel(softmax_fwd_kernel<HD, true>, (unsigned)(units * p.shares), kFwdThreads, FwdCfg<HD>::kSmemBytes, stream, map_q, map_k, map_v, f);
+}
+
 }  // namespace
+
+cudaError_t launch_softmax_chunks(const SoftmaxPagedArgs& a, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t stream) {
+  return a.c.D == 64 ? chunks_launch<64>(a, map_k, map_v, stream) : chunks_launch<128>(a, map_k, map_v, stream);
+}
 
 cudaError_t launch_softmax_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, int32_t* status,
                                cudaStream_t stream) {
