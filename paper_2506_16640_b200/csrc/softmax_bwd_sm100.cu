@@ -84,6 +84,18 @@ __device__ __forceinline__ int4 span_of(const SoftmaxArgs& a, int b, int row0) {
   return s;
 }
 
+// Item -> (batch row, head) and tile: causal calls hand out the longest tiles of all heads first, the others a head after the other, whose
+// K/V tiles (Q tiles) then stay in L2
+__device__ __forceinline__ void item_of(const SoftmaxArgs& a, int item, int tiles, int heads, int& head, int& tile) {
+  if (a.causal && !a.ranges) {
+    tile = item / heads;
+    head = item - tile * heads;
+  } else {
+    head = item / tiles;
+    tile = item - head * tiles;
+  }
+}
+
 // x of 32 accumulators and, where they are capped, their tanh in t (x and t / grow share what they can)
 template <bool CAP, bool SLOPE>
 __device__ __forceinline__ float score_of(const SoftmaxArgs& a, float s, float slope, float dist) {
@@ -220,15 +232,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
       BwdWork w = {};
       w.valid = item >= 0;
       if (item >= 0) {
-        asked = true;
-        if (elect_one()) {
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          mbar_expect_tx(next_bar, 16);
-          next_cta_request(answer, next_bar);
-        }
-        __syncwarp();
-        const int bh = item / f.tiles;
-        w.tile = f.tiles - 1 - (item - bh * f.tiles);
+        int bh;
+        item_of(a, item, f.tiles, a.B * a.H, bh, w.tile);
+        w.tile = f.tiles - 1 - w.tile;
         w.b = bh / a.H;
         w.h = bh - w.b * a.H;
         const int row0 = w.tile * kT;
@@ -285,6 +291,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
         }
         if (!alive) break;
       }
+      // (asked for behind the item's last copy: asked for earlier, an item would wait for a CTA that is busy while others have run out)
+      asked = true;
+      if (elect_one()) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the last answer has been read
+        mbar_expect_tx(next_bar, 16);
+        next_cta_request(answer, next_bar);
+      }
+      __syncwarp();
       alive = wait_all(next_bar, next_phase);
       if (!alive) break;
       next_phase ^= 1u;
@@ -584,17 +598,23 @@ struct QTiles {
   }
 };
 
-// 32 queries (columns) of one key (lane): P^T as bf16 pairs, the scores' tanh (CAP) or nothing left in s, p kept in place of s otherwise
+// 32 queries (columns) of one key (lane): P^T as bf16 pairs, and in place of s what dP - D is multiplied by: P a (1 - tanh^2)
 template <bool CAP, bool SLOPE>
-__device__ __forceinline__ void dkv_probabilities(const SoftmaxArgs& args, float slope, int key, int i0, uint32_t rows_at, float (&s)[32], float (&p)[32]) {
+__device__ __forceinline__ void dkv_probabilities(const SoftmaxArgs& args, float slope, int dist, uint32_t rows_at, float (&s)[32], uint32_t (&u)[16]) {
 #pragma unroll
   for (int e = 0; e < 32; e += 4) {
-    float l[4], m[4];
+    float l[4], m[4], p[4];
     lds_f4(rows_at + 4 * e, l[0], l[1], l[2], l[3]);
     lds_f4(rows_at + 4 * (kT + e), m[0], m[1], m[2], m[3]);
 #pragma unroll
-    for (int z = 0; z < 4; ++z)
-      p[e + z] = exp2_fast(fmaf(score_of<CAP, SLOPE>(args, s[e + z], slope, (float)(i0 + e + z - key)), m[z], -l[z]));
+    for (int z = 0; z < 4; ++z) {
+      const float t = s[e + z];
+      p[z] = exp2_fast(fmaf(score_of<CAP, SLOPE>(args, t, slope, (float)(dist + e + z)), m[z], -l[z]));
+      s[e + z] = p[z] * m[z];
+      if (CAP) s[e + z] *= fmaf(-t, t, 1.0f);
+    }
+    u[e >> 1] = bf16x2(p[0], p[1]);
+    u[(e >> 1) + 1] = bf16x2(p[2], p[3]);
   }
 }
 
@@ -668,15 +688,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
       BwdWork w = {};
       w.valid = item >= 0;
       if (item >= 0) {
-        asked = true;
-        if (elect_one()) {
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          mbar_expect_tx(next_bar, 16);
-          next_cta_request(answer, next_bar);
-        }
-        __syncwarp();
-        const int bk = item / f.tiles;
-        w.tile = item - bk * f.tiles;
+        int bk;
+        item_of(a, item, f.tiles, a.B * a.KH, bk, w.tile);
         w.b = bk / a.KH;
         w.h = bk - w.b * a.KH;
       }
@@ -740,6 +753,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
         }
       }
       if (!alive) break;
+      // (asked for behind the item's last copy: asked for earlier, an item would wait for a CTA that is busy while others have run out)
+      asked = true;
+      if (elect_one()) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the last answer has been read
+        mbar_expect_tx(next_bar, 16);
+        next_cta_request(answer, next_bar);
+      }
+      __syncwarp();
       alive = wait_all(next_bar, next_phase);
       if (!alive) break;
       next_phase ^= 1u;
@@ -899,28 +920,34 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           if (!alive) break;
           sphase ^= 1u;
           tc_fence_after();
-          float s[32], p[32];
+          float s[32];
+          uint32_t u[16];
           tmem_ld32(lane_base + kS + quarter * 32, s);
           tmem_ld_wait();
           if (a.cap_acc > 0.f) {
             to_tanh(a.cap_inv, s);
-            if (slope != 0.f) dkv_probabilities<true, true>(a, slope, key, i0, rows_at, s, p);
-            else dkv_probabilities<true, false>(a, slope, key, i0, rows_at, s, p);
+            if (slope != 0.f) dkv_probabilities<true, true>(a, slope, i0 - key, rows_at, s, u);
+            else dkv_probabilities<true, false>(a, slope, i0 - key, rows_at, s, u);
           } else {
-            if (slope != 0.f) dkv_probabilities<false, true>(a, slope, key, i0, rows_at, s, p);
-            else dkv_probabilities<false, false>(a, slope, key, i0, rows_at, s, p);
+            if (slope != 0.f) dkv_probabilities<false, true>(a, slope, i0 - key, rows_at, s, u);
+            else dkv_probabilities<false, false>(a, slope, i0 - key, rows_at, s, u);
           }
           if (edge) {
+            // lane e knows the range of query i0 + e; bit e: it sees this lane's key
+            const int2 sees = i0 + lane < a.N ? visible_keys(a, b, i0 + lane) : make_int2(0, 0);
+            uint32_t seen = 0u;
+#pragma unroll 4
+            for (int e = 0; e < 32; ++e) {
+              const int from = __shfl_sync(0xffffffffu, sees.x, e), to = __shfl_sync(0xffffffffu, sees.y, e);
+              seen |= (key >= from && key < to ? 1u : 0u) << e;
+            }
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              const int i = min(i0 + e, a.N - 1);
-              const int2 sees = visible_keys(a, b, i);
-              p[e] = key >= sees.x && key < sees.y ? p[e] : 0.f;
+              const bool on = (seen >> e) & 1u;
+              s[e] = on ? s[e] : 0.f;
+              u[e >> 1] &= on ? 0xffffffffu : (e & 1) ? 0x0000ffffu : 0xffff0000u;
             }
           }
-          uint32_t u[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) u[e] = bf16x2(p[2 * e], p[2 * e + 1]);
           tmem_st16(lane_base + kS + quarter * 32, u);
           tmem_st_wait();
           tc_fence_before();
@@ -930,24 +957,23 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           if (!alive) break;
           dpphase ^= 1u;
           tc_fence_after();
-          float dp[32];
-          tmem_ld32(lane_base + kDP + quarter * 32, dp);
-          tmem_ld_wait();
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            float m[4], d[4];
-            lds_f4(rows_at + 4 * (kT + e), m[0], m[1], m[2], m[3]);
-            lds_f4(rows_at + 4 * (2 * kT + e), d[0], d[1], d[2], d[3]);
+          for (int c = 0; c < 2; ++c) {
+            float dp[16];
+            tmem_ld16(lane_base + kDP + quarter * 32 + c * 16, dp);
+            tmem_ld_wait();
 #pragma unroll
-            for (int z = 0; z < 4; ++z) {
-              dp[e + z] = p[e + z] * m[z] * (dp[e + z] - d[z]);
-              if (a.cap_acc > 0.f) dp[e + z] *= fmaf(-s[e + z], s[e + z], 1.0f);
+            for (int e = 0; e < 16; e += 4) {
+              float d[4];
+              lds_f4(rows_at + 4 * (2 * kT + c * 16 + e), d[0], d[1], d[2], d[3]);
+#pragma unroll
+              for (int z = 0; z < 4; ++z) dp[e + z] = s[c * 16 + e + z] * (dp[e + z] - d[z]);
+              u[c * 8 + (e >> 1)] = bf16x2(dp[e], dp[e + 1]);
+              u[c * 8 + (e >> 1) + 1] = bf16x2(dp[e + 2], dp[e + 3]);
             }
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(r_empty + 8 * st);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) u[e] = bf16x2(dp[2 * e], dp[2 * e + 1]);
           tmem_st16(lane_base + kDP + quarter * 32, u);
           tmem_st_wait();
           tc_fence_before();

@@ -176,19 +176,21 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
       w.valid = item >= 0;
       w.part = -1;
       if (item >= 0) {
-        asked = true;
-        if (elect_one()) {
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the last answer has been read
-          mbar_expect_tx(next_bar, 16);
-          next_cta_request(answer, next_bar);
-        }
-        __syncwarp();
         int rest = item;
         if constexpr (!PAGED) {
+          // causal: the longest rows of all heads first; otherwise a head after the other, whose K/V tiles then stay in L2
+          int tile;
+          if (a.causal && !a.ranges) {
+            const int heads = a.B * a.KH * f.pairs;
+            tile = f.tiles - 1 - rest / heads;
+            rest %= heads;
+          }
           const int pair = rest % f.pairs;
           rest /= f.pairs;
-          const int tile = f.tiles - 1 - rest % f.tiles;
-          rest /= f.tiles;
+          if (!(a.causal && !a.ranges)) {
+            tile = f.tiles - 1 - rest % f.tiles;
+            rest /= f.tiles;
+          }
           w.b = rest / a.KH;
           w.kh = rest - w.b * a.KH;
           w.h[0] = w.kh * a.G + (f.pair_heads ? 2 * pair : pair);
@@ -318,7 +320,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
         }
         if (!alive) break;
       }
-      // the next item
+      // (asked for behind the item's last copy: asked for earlier, an item would wait for a CTA that is busy while others have run out)
+      asked = true;
+      if (elect_one()) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the last answer has been read
+        mbar_expect_tx(next_bar, 16);
+        next_cta_request(answer, next_bar);
+      }
+      __syncwarp();
       alive = wait_all(next_bar, next_phase);
       if (!alive) break;
       next_phase ^= 1u;
