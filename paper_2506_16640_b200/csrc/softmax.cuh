@@ -2,8 +2,9 @@
 //
 //   z_ij = sm_scale <q_i, k_j>,  x_ij = cap tanh(z_ij / cap) - m_h |i - j|,  s_ij = c_i x_ij,
 //   p_ij = exp(s_ij - lse_i) over the keys j the row sees,  O_i = sum_j p_ij v_j;  a row that sees none: O = 0, lse = -inf.
-// Everything is kept in units of the accumulator <q_i, k_j>: x / sm_scale = cap_acc tanh(acc * cap_inv) - slope_acc |i - j|, and
-// s log2(e) = a_i (x / sm_scale) with a_i = c_i sm_scale log2(e), so that a probability is one FMA and one exp2.
+// Scores are kept in a unit of their own: that of the accumulator <q_i, k_j>, x / unit = acc - (m_h / sm_scale) |i - j| with unit = sm_scale, or of the cap,
+// x / unit = tanh(acc * cap_inv) - (m_h / cap) |i - j| with unit = cap; s log2(e) = a_i (x / unit) with a_i = c_i unit log2(e), so that a probability is one
+// FMA and one exp2.
 #pragma once
 
 #include "common.cuh"
@@ -17,7 +18,8 @@ struct SoftmaxArgs {
   int B, H, KH, G, N, D;              // G = H / KH query heads share a K/V head
   int causal;
   float sm_scale;
-  float cap_acc, cap_inv;             // cap / sm_scale and sm_scale / cap (0, 0: not capped)
+  float cap_inv;                      // sm_scale / cap (0: not capped)
+  float unit;                         // of the scores: sm_scale, or the cap
   const int2* ranges;                 // [B][N] {first key, one behind the last} or nullptr
   const float *beta, *gamma, *delta;  // [H] or nullptr
   const float* c_rows;                // [B][H][N] or nullptr

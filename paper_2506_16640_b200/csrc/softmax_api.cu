@@ -138,10 +138,11 @@ int check_softmax(const entmax_attn_softmax_params* p, const entmax_attn_softmax
   if (p->dtype != ENTMAX_ATTN_DTYPE_BF16 && p->dtype != ENTMAX_ATTN_DTYPE_FP32) return ENTMAX_ATTN_EINVAL_DTYPE;
   if (!std::isfinite(p->sm_scale) || p->sm_scale < 0.f || !std::isfinite(p->softcap) || p->softcap < 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
   a.sm_scale = p->sm_scale > 0.f ? p->sm_scale : 1.0f / std::sqrt((float)a.D);
+  a.unit = a.sm_scale;
   if (p->softcap > 0.f) {
-    a.cap_acc = p->softcap / a.sm_scale;
+    a.unit = p->softcap;
     a.cap_inv = a.sm_scale / p->softcap;
-    if (!std::isfinite(a.cap_acc) || !std::isfinite(a.cap_inv) || a.cap_acc == 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
+    if (!std::isfinite(a.cap_inv) || a.cap_inv == 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
   }
   a.causal = p->causal ? 1 : 0;
   if (!take_strides(p->q, a.B, a.H, a.N, a.D, 8, &a.q) || !take_strides(p->k, a.B, a.KH, a.N, a.D, 8, &a.k) ||

@@ -5,7 +5,7 @@
 // Two kernels, so that nothing is added up by atomics: the scores and dP are formed twice (seven products instead of five), but no gradient goes
 // through memory as a float32 sum and results are the same every time.
 //   softmax_dq_kernel   an item is a Q tile of 128 rows: S and dP in TMEM, a row's 128 columns by four threads, dS as bf16 over S's own columns
-//                       and from there into dQ += dS K.  Leaves {lse log2 e, a, D} of every row, and which keys every tile sees, to the other kernel.
+//                       and from there into dQ += dS K.  Leaves -lse log2 e, a and -D of every row, and which keys every tile sees, to the other kernel.
 //                       dL/dc_i = sum dS x is formed as sum p dP x - (sum p dP)(sum p x) / sum p, all of float32 probabilities: the D above comes
 //                       from the O that was rounded to bf16, which is good enough for dS (an error of 2^-9 of D times p) but not for a float32 result.
 //   softmax_dkv_kernel  an item is a K/V tile; over all query heads that share it and all Q tiles that see it: S^T = K Q^T and dP^T = V dO^T with the keys
@@ -51,7 +51,7 @@ struct BwdArgs {
   int tiles;                    // of 128 rows, per head
   const __nv_bfloat16 *o, *d_o;
   __nv_bfloat16 *dq, *dk, *dv;
-  float* rows;                  // [B H tiles][3][128]: lse log2 e (+inf: a row that sees nothing), a, D
+  float* rows;                  // [B H tiles][3][128]: -lse log2 e (-inf: a row that sees nothing), a, -D
   int4* spans;                  // [B tiles] {first key any row sees, one behind the last, largest first, smallest last}, with ranges
   int32_t* status;
 };
@@ -96,26 +96,6 @@ __device__ __forceinline__ void item_of(const SoftmaxArgs& a, int item, int tile
   }
 }
 
-// x of 32 accumulators and, where they are capped, their tanh in t (x and t / grow share what they can)
-template <bool CAP, bool SLOPE>
-__device__ __forceinline__ float score_of(const SoftmaxArgs& a, float s, float slope, float dist) {
-  float x = CAP ? a.cap_acc * s : s;             // (CAP: s is the tanh)
-  if (SLOPE) x = fmaf(-slope, fabsf(dist), x);
-  return x;
-}
-__device__ __forceinline__ void to_tanh(float cap_inv, float (&s)[32]) {
-  float most = 0.f;
-#pragma unroll
-  for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(s[e]));
-  if (__all_sync(0xffffffffu, most * cap_inv <= 1.0f)) {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) s[e] = tanh_small(s[e] * cap_inv);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) s[e] = tanh_full(s[e] * cap_inv);
-  }
-}
-
 __device__ __forceinline__ void bwd_teardown(uint32_t tmem, uint32_t abort_flag, uint32_t drain_fail, int32_t* status) {
   tc_fence_before();
   __syncthreads();
@@ -140,30 +120,48 @@ struct RowTerms {
   int i;
 };
 
-// 32 columns from key j0 on: dS as bf16 pairs; dc: {sum p dP x, sum p dP, sum p x, sum p} where wanted
-template <bool CAP, bool SLOPE>
-__device__ __forceinline__ void dq_elements(const SoftmaxArgs& args, const RowTerms& r, int j0, bool edge, bool want_dc, float (&s)[32],
-                                            const float (&dp)[32], uint32_t (&ds)[16], float (&dc)[4]) {
+// 32 columns from key j0 on (s: their accumulators, or the tanh of capped ones): dS as bf16 pairs; dc: {sum p dP x, sum p dP, sum p x, sum p} where wanted, the even
+// and the odd columns' apart
+template <bool CAP, bool SLOPE, bool DC, bool EDGE>
+__device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const float (&s)[32], const float (&dp)[32], uint32_t (&ds)[16], uint64_t (&dc)[4]) {
+  const uint64_t a2 = pack2(r.a, r.a), l2 = pack2(-r.lse2, -r.lse2), d2 = pack2(-r.dot, -r.dot);
 #pragma unroll
   for (int e = 0; e < 32; e += 2) {
-    float d[2];
-#pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const int j = j0 + e + z;
-      const float x = score_of<CAP, SLOPE>(args, s[e + z], r.slope, (float)(j - r.i));
-      float p = exp2_fast(fmaf(x, r.a, -r.lse2));
-      if (edge) p = j >= r.sees.x && j < r.sees.y ? p : 0.f;
-      d[z] = p * (dp[e + z] - r.dot);
-      if (CAP) d[z] *= fmaf(-s[e + z], s[e + z], 1.0f);
-      if (want_dc) {
-        const float u = p * dp[e + z];
-        dc[0] = fmaf(u, x, dc[0]);
-        dc[1] += u;
-        dc[2] = fmaf(p, x, dc[2]);
-        dc[3] += p;
-      }
+    const uint64_t t = pack2(s[e], s[e + 1]);
+    uint64_t x = t;
+    if (SLOPE) x = pack2(fmaf(-r.slope, fabsf((float)(j0 + e - r.i)), s[e]), fmaf(-r.slope, fabsf((float)(j0 + e + 1 - r.i)), s[e + 1]));
+    float p0, p1;
+    unpack2(fma2(x, a2, l2), p0, p1);
+    p0 = exp2_fast(p0);
+    p1 = exp2_fast(p1);
+    if (EDGE) {
+      p0 = j0 + e >= r.sees.x && j0 + e < r.sees.y ? p0 : 0.f;
+      p1 = j0 + e + 1 >= r.sees.x && j0 + e + 1 < r.sees.y ? p1 : 0.f;
     }
-    ds[e >> 1] = bf16x2(d[0], d[1]);
+    const uint64_t p = pack2(p0, p1), v = pack2(dp[e], dp[e + 1]);
+    uint64_t d = mul2(p, add2(v, d2));
+    if (CAP) d = mul2(d, fma2(t, pack2(-s[e], -s[e + 1]), pack2(1.0f, 1.0f)));
+    if (DC) {
+      const uint64_t u = mul2(p, v);
+      dc[0] = fma2(u, x, dc[0]);
+      dc[1] = add2(u, dc[1]);
+      dc[2] = fma2(p, x, dc[2]);
+      dc[3] = add2(p, dc[3]);
+    }
+    float d0, d1;
+    unpack2(d, d0, d1);
+    ds[e >> 1] = bf16x2(d0, d1);
+  }
+}
+template <bool CAP, bool SLOPE>
+__device__ __forceinline__ void dq_elements_of(const RowTerms& r, int j0, bool edge, bool want_dc, const float (&s)[32], const float (&dp)[32],
+                                               uint32_t (&ds)[16], uint64_t (&dc)[4]) {
+  if (want_dc) {
+    if (edge) dq_elements<CAP, SLOPE, true, true>(r, j0, s, dp, ds, dc);
+    else dq_elements<CAP, SLOPE, true, false>(r, j0, s, dp, ds, dc);
+  } else {
+    if (edge) dq_elements<CAP, SLOPE, false, true>(r, j0, s, dp, ds, dc);
+    else dq_elements<CAP, SLOPE, false, false>(r, j0, s, dp, ds, dc);
   }
 }
 
@@ -444,18 +442,18 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
       r.sees = mine ? visible_keys(a, b, r.i) : make_int2(0, 0);
       const size_t at = ((size_t)b * a.H + h) * a.N + (mine ? r.i : 0);
       const bool some = r.sees.y > r.sees.x;
-      const float g = mine ? row_scale(a, b, h, r.i, r.sees.y - r.sees.x) * a.sm_scale : 0.f;
-      r.a = g * kLog2e;
+      const float c = mine ? row_scale(a, b, h, r.i, r.sees.y - r.sees.x) : 0.f, g = c * a.sm_scale;
+      r.a = c * a.unit * kLog2e;
       r.lse2 = some ? f.g.lse[at] * kLog2e : INFINITY;
-      r.slope = a.alibi ? a.alibi[h] / a.sm_scale : 0.f;
+      r.slope = a.alibi ? a.alibi[h] / a.unit : 0.f;
       if (!some) { r.sees = make_int2(0, 0x7fffffff); r.a = 0.f; }   // (probability exp2(-inf) everywhere, without a mask)
       if (quarter == 0) {
         float* out = f.rows + ((size_t)(b * a.H + h) * f.tiles + tile) * (3 * kT) + row;
-        out[0] = r.lse2;
+        out[0] = -r.lse2;
         out[kT] = r.a;
-        out[2 * kT] = r.dot;
+        out[2 * kT] = -r.dot;
       }
-      float dc[4] = {0.f, 0.f, 0.f, 0.f};
+      uint64_t dc[4] = {0u, 0u, 0u, 0u};         // (pairs of float32 zeros)
       for (int j = hi - 1; j >= lo && alive; --j) {
         alive = wait_all(s_full, sphase);
         if (!alive) break;
@@ -471,13 +469,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
         const int j0 = j * kT + quarter * 32;
         const bool edge = __any_sync(0xffffffffu, r.sees.x > j0 || r.sees.y < j0 + 32);
         uint32_t ds[16];
-        if (a.cap_acc > 0.f) {
-          to_tanh(a.cap_inv, s);
-          if (r.slope != 0.f) dq_elements<true, true>(a, r, j0, edge, want_dc, s, dp, ds, dc);
-          else dq_elements<true, false>(a, r, j0, edge, want_dc, s, dp, ds, dc);
+        if (a.cap_inv > 0.f) {
+          tanh_scores(a.cap_inv, s);
+          if (r.slope != 0.f) dq_elements_of<true, true>(r, j0, edge, want_dc, s, dp, ds, dc);
+          else dq_elements_of<true, false>(r, j0, edge, want_dc, s, dp, ds, dc);
         } else {
-          if (r.slope != 0.f) dq_elements<false, true>(a, r, j0, edge, want_dc, s, dp, ds, dc);
-          else dq_elements<false, false>(a, r, j0, edge, want_dc, s, dp, ds, dc);
+          if (r.slope != 0.f) dq_elements_of<false, true>(r, j0, edge, want_dc, s, dp, ds, dc);
+          else dq_elements_of<false, false>(r, j0, edge, want_dc, s, dp, ds, dc);
         }
         // the dS before has been taken
         alive = wait_all(ds_empty, dsphase ^ 1u);
@@ -520,7 +518,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
       if (want_dc) {
         // the four threads of a row meet through the dS columns, which nobody needs until the next item's first dS is written: behind dq_empty of all
         const uint32_t mine_at = lane_base + kDS + quarter * 16;
-        uint32_t u[8] = {__float_as_uint(dc[0]), __float_as_uint(dc[1]), __float_as_uint(dc[2]), __float_as_uint(dc[3]), 0u, 0u, 0u, 0u};
+        uint32_t u[8] = {};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x, y;
+          unpack2(dc[e], x, y);
+          u[e] = __float_as_uint(x + y);
+        }
         tmem_st8(mine_at, u);
         tmem_st_wait();
         tc_fence_before();
@@ -539,7 +543,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[e] += v[e];
         }
-        if (quarter == 0 && mine) f.g.dc_rows[at] = some ? (sum[0] - sum[1] * (sum[2] / sum[3])) * a.sm_scale : 0.f;
+        if (quarter == 0 && mine) f.g.dc_rows[at] = some ? (sum[0] - sum[1] * (sum[2] / sum[3])) * a.unit : 0.f;
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(x_bar);       // (all have read before anyone writes the next item's dS there)
@@ -600,21 +604,27 @@ struct QTiles {
 
 // 32 queries (columns) of one key (lane): P^T as bf16 pairs, and in place of s what dP - D is multiplied by: P a (1 - tanh^2)
 template <bool CAP, bool SLOPE>
-__device__ __forceinline__ void dkv_probabilities(const SoftmaxArgs& args, float slope, int dist, uint32_t rows_at, float (&s)[32], uint32_t (&u)[16]) {
+__device__ __forceinline__ void dkv_probabilities(float slope, int dist, uint32_t rows_at, float (&s)[32], uint32_t (&u)[16]) {
 #pragma unroll
   for (int e = 0; e < 32; e += 4) {
-    float l[4], m[4], p[4];
+    float l[4], m[4];
     lds_f4(rows_at + 4 * e, l[0], l[1], l[2], l[3]);
     lds_f4(rows_at + 4 * (kT + e), m[0], m[1], m[2], m[3]);
 #pragma unroll
-    for (int z = 0; z < 4; ++z) {
-      const float t = s[e + z];
-      p[z] = exp2_fast(fmaf(score_of<CAP, SLOPE>(args, t, slope, (float)(dist + e + z)), m[z], -l[z]));
-      s[e + z] = p[z] * m[z];
-      if (CAP) s[e + z] *= fmaf(-t, t, 1.0f);
+    for (int z = 0; z < 4; z += 2) {
+      const uint64_t t = pack2(s[e + z], s[e + z + 1]), m2 = pack2(m[z], m[z + 1]);
+      uint64_t x = t;
+      if (SLOPE)
+        x = pack2(fmaf(-slope, fabsf((float)(dist + e + z)), s[e + z]), fmaf(-slope, fabsf((float)(dist + e + z + 1)), s[e + z + 1]));
+      float p0, p1;
+      unpack2(fma2(x, m2, pack2(l[z], l[z + 1])), p0, p1);
+      p0 = exp2_fast(p0);
+      p1 = exp2_fast(p1);
+      u[(e + z) >> 1] = bf16x2(p0, p1);
+      uint64_t w = mul2(pack2(p0, p1), m2);
+      if (CAP) w = mul2(w, fma2(t, pack2(-s[e + z], -s[e + z + 1]), pack2(1.0f, 1.0f)));
+      unpack2(w, s[e + z], s[e + z + 1]);
     }
-    u[e >> 1] = bf16x2(p[0], p[1]);
-    u[(e >> 1) + 1] = bf16x2(p[2], p[3]);
   }
 }
 
@@ -901,7 +911,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
       const bool mine = key < a.N;
       bool any = false;
       for (int g = 0; g < a.G && alive; ++g) {
-        const float slope = a.alibi ? a.alibi[kh * a.G + g] / a.sm_scale : 0.f;
+        const float slope = a.alibi ? a.alibi[kh * a.G + g] / a.unit : 0.f;
         qt.rewind();
         for (int t = qt.next(); t >= 0 && alive; t = qt.next(), ++idx) {
           any = true;
@@ -924,13 +934,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           uint32_t u[16];
           tmem_ld32(lane_base + kS + quarter * 32, s);
           tmem_ld_wait();
-          if (a.cap_acc > 0.f) {
-            to_tanh(a.cap_inv, s);
-            if (slope != 0.f) dkv_probabilities<true, true>(a, slope, i0 - key, rows_at, s, u);
-            else dkv_probabilities<true, false>(a, slope, i0 - key, rows_at, s, u);
+          if (a.cap_inv > 0.f) {
+            tanh_scores(a.cap_inv, s);
+            if (slope != 0.f) dkv_probabilities<true, true>(slope, i0 - key, rows_at, s, u);
+            else dkv_probabilities<true, false>(slope, i0 - key, rows_at, s, u);
           } else {
-            if (slope != 0.f) dkv_probabilities<false, true>(a, slope, i0 - key, rows_at, s, u);
-            else dkv_probabilities<false, false>(a, slope, i0 - key, rows_at, s, u);
+            if (slope != 0.f) dkv_probabilities<false, true>(slope, i0 - key, rows_at, s, u);
+            else dkv_probabilities<false, false>(slope, i0 - key, rows_at, s, u);
           }
           if (edge) {
             // lane e knows the range of query i0 + e; bit e: it sees this lane's key
@@ -967,9 +977,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
               float d[4];
               lds_f4(rows_at + 4 * (2 * kT + c * 16 + e), d[0], d[1], d[2], d[3]);
 #pragma unroll
-              for (int z = 0; z < 4; ++z) dp[e + z] = s[c * 16 + e + z] * (dp[e + z] - d[z]);
-              u[c * 8 + (e >> 1)] = bf16x2(dp[e], dp[e + 1]);
-              u[c * 8 + (e >> 1) + 1] = bf16x2(dp[e + 2], dp[e + 3]);
+              for (int z = 0; z < 4; z += 2) {
+                float x, y;
+                unpack2(mul2(pack2(s[c * 16 + e + z], s[c * 16 + e + z + 1]), add2(pack2(dp[e + z], dp[e + z + 1]), pack2(d[z], d[z + 1]))), x, y);
+                u[c * 8 + ((e + z) >> 1)] = bf16x2(x, y);
+              }
             }
           }
           __syncwarp();
@@ -1002,7 +1014,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           if (mine) {
             const entmax_attn_strides& s = which ? f.g.dv : f.g.dk;
             __nv_bfloat16* out = (which ? f.dv : f.dk) + (long long)b * s.b + (long long)kh * s.h + (long long)key * s.n + quarter * 32;
-            const float mul = which ? 1.0f : kLn2;               // (the rows' a has log2 e in it)
+            const float mul = which ? 1.0f : kLn2 * a.sm_scale / a.unit;   // (the rows' a is c unit log2 e)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float* x = v + 8 * e;

@@ -9,10 +9,9 @@
 //   O += P V         P from TMEM, V with the head dim contiguous, O in TMEM.
 // O is not rescaled for every rise of the maximum: P may grow up to 2^8 above the m it is measured from before O and l are brought to a new one, exactly, so
 // that nothing is lost and the correction is rare.  While one tile's softmax runs the tensor core works on the other's O and next S.
-// Next to the MMAs (per pair of steps 4 x 128 x 128 x D, 2048 cycles at D = 128) the 2 x 16384 exponentials take 2048 cycles of the special-function
-// unit: a part of them is computed on the FMA pipe instead (exp2_pair_fma).
-//
-// CTA: warps 0..3 and 4..7 the rows of the two tiles, warp 8 MMA issuer, warp 9 TMA producer and scheduler.  Items are handed out by the hardware: a
+// Bound by the chain of one tile -- S from TMEM, maximum, 128 exponentials a thread (16384 a tile, 1024 cycles of the special-function unit), P to TMEM, then O and
+// the next S behind the other tile's -- of which two are under way.  Computing a part of the exponentials on the FMA pipe made it longer.
+// CTA: warps 0..3 and 4..7 the rows of the two tiles, warp 8 MMA issuer, warp 9 TMA producer and scheduler (10, 11: idle, registers go by warpgroups).  Items are handed out by the hardware: a
 // running CTA takes over one that has not started (longest rows of a head first).  Every wait is bounded (see sm100_ptx.cuh).
 #include <cuda.h>
 
@@ -27,7 +26,9 @@ namespace {
 using namespace sm100;
 
 constexpr int kRows = 128, kKeys = 128;
-constexpr int kFwdThreads = 320;
+constexpr int kFwdThreads = 384;
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
+static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * 168, "no more than the launch's, 168 a thread");
 constexpr int kBarArea = 512;
 
 template <int HD>
@@ -63,6 +64,7 @@ struct FwdArgs {
   // paged
   PagedCache c;
   int window, max_q, max_kv, few_rows, shares, box_shift;
+  const __nv_bfloat16* v;
   float* part_o;        // [part][128][HD]
   float2* part_ml;      // [part][128] {maximum in base-2 units, sum}
 };
@@ -110,7 +112,7 @@ __device__ __forceinline__ int find_block(const PagedCache& c, int id, int block
   return lo;
 }
 
-template <int HD, bool PAGED>
+template <int HD, bool PAGED, bool CAP, bool TERMS>
 __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                                                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ FwdArgs f) {
   pdl_begin();
@@ -127,8 +129,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
   const uint32_t w_full = bars + 240, w_empty = bars + 256;
   const uint32_t next_bar = bars + 272, drain_bar = bars + 280;
   const uint32_t tmem_slot = bars + 288, abort_flag = bars + 292, drain_fail = bars + 296;
-  const uint32_t kv_full = bars + 304, kv_empty = bars + 304 + 8 * C::kStages;
-  static_assert(304 + 16 * C::kStages <= kBarArea, "barriers");
+  const uint32_t p_half = bars + 304;                                // [2]
+  const uint32_t kv_full = bars + 320, kv_empty = bars + 320 + 8 * C::kStages;
+  static_assert(320 + 16 * C::kStages <= kBarArea, "barriers");
   const Work* work = reinterpret_cast<const Work*>(smem_raw + (work_at - smem_u32(smem_raw)));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -137,6 +140,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
       mbar_init(q_full + 8 * t, 1);
       mbar_init(q_empty + 8 * t, 1);
       mbar_init(s_full + 8 * t, 1);
+      mbar_init(p_half + 8 * t, 4);
       mbar_init(p_full + 8 * t, 4);
       mbar_init(o_full + 8 * t, 1);
       mbar_init(o_empty + 8 * t, 4);
@@ -165,6 +169,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
   const SoftmaxArgs& a = f.a;
   auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
 
+  if (warp >= 8) {
+  registers_down<kOtherRegs>();
   if (warp == 9) {
     // ------------------------------------------------------------------ scheduler and TMA producer (the whole warp runs the control flow)
     uint32_t next_phase = 0, wphase = 0, qphase[2] = {0, 0}, idx = 0;   // idx: K and V tiles loaded so far
@@ -305,6 +311,28 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
                 for (int hf = 0; hf < C::kHalves; ++hf)
                   tma_load_4d(dst + hf * (kKeys * 128), map, kv_full + 8 * st, hf * 64, j * kKeys, w.kh, w.b);
               }
+            } else if (which == 1 && (j * kKeys + kKeys > w.len || j * kKeys < w.first_key)) {
+              // Slots that no row sees may hold anything, and a NaN times a probability of 0 is one too.  A V tile that has some is put together by this
+              // warp, with zeros for them (and not by clearing rows behind a TMA copy: such stores were seen to lose against the copy's own).
+              for (int r = lane; r < kKeys; r += 32) {
+                const int key = j * kKeys + r;
+                const int p = __shfl_sync(0xffffffffu, page, r >> f.box_shift);
+                const bool some = p >= 0 && p < f.c.n_pages && key < w.len && key >= w.first_key;
+                const uint4* src = reinterpret_cast<const uint4*>(f.v + (some ? (long long)p * f.c.s_page + (long long)(key & ((1 << f.c.ps_shift) - 1)) * f.c.s_tok +
+                                                                                      (long long)w.kh * f.c.s_head
+                                                                              : 0));
+                uint4 x[HD / 8];
+#pragma unroll
+                for (int e = 0; e < HD / 8; ++e) x[e] = some ? src[e] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int e = 0; e < HD / 8; ++e)
+                  asm volatile("st.shared::cta.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (e >> 3) * (kKeys * 128) + r * 128 + (((e & 7) ^ (r & 7)) << 4)),
+                               "r"(x[e].x), "r"(x[e].y), "r"(x[e].z), "r"(x[e].w)
+                               : "memory");
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) mbar_arrive(kv_full + 8 * st);
             } else {
               const int boxes = __popc(__ballot_sync(0xffffffffu, page >= 0));
               if (lane == 0) mbar_expect_tx(kv_full + 8 * st, boxes * (C::kHalves * 128) << f.box_shift);
@@ -398,45 +426,37 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
         const uint32_t iv = idx + 1, ik = idx + 2;                    // V of this step, K of the next
         alive = wait_kv(iv);
         if (!alive) break;
-        if constexpr (PAGED) {
-          // rows of V that no query sees may hold anything (NaN times a probability of 0 is NaN): zeros instead
-          const int k0 = j * kKeys;
-          if (k0 + kKeys > w.len || k0 < w.first_key) {
-            const uint32_t dst = kv_smem + (iv % C::kStages) * C::kTileBytes;
-            for (int r = lane; r < kKeys * C::kHalves; r += 32) {
-              const int key = k0 + (r & (kKeys - 1));
-              if (key >= w.len || key < w.first_key)
-                for (int e = 0; e < 8; ++e) sts_f4(dst + r * 128 + e * 16, 0.f, 0.f, 0.f, 0.f);
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-          }
-        }
         if (j > lo) {
           alive = wait_kv(ik);
           if (!alive) break;
         }
         for (int t = 0; t < 2 && alive; ++t) {
           if (active(t, j)) {
-            alive = wait_all(p_full + 8 * t, pphase[t]);
+            alive = wait_all(p_half + 8 * t, pphase[t]);
             if (!alive) break;
-            pphase[t] ^= 1u;
             if (j == w.hi[t] - 1) {
               // the previous item's O has been read
               alive = wait_all(o_empty + 8 * t, ophase[t] ^ 1u);
               if (!alive) break;
               ophase[t] ^= 1u;
             }
-            tc_fence_after();
-            if (elect_one()) {
-              const uint64_t vs = v_d + (iv % C::kStages) * kStageD;
+            auto add_half = [&](int half) {
+              tc_fence_after();
+              if (elect_one()) {
+                const uint64_t vs = v_d + (iv % C::kStages) * kStageD;
 #pragma unroll
-              for (int kk = 0; kk < kKeys / 16; ++kk)
-                umma_bf16_ts(tmem + C::kTmemO + t * HD, tmem + t * kKeys + kk * 8, vs + kk * ((16 * 128) >> 4), id_o,
-                             (j < w.hi[t] - 1 || kk > 0) ? 1u : 0u);
-              if (j == w.lo[t]) umma_commit(o_full + 8 * t);
-            }
-            __syncwarp();
+                for (int kk = half * (kKeys / 32); kk < (half + 1) * (kKeys / 32); ++kk)
+                  umma_bf16_ts(tmem + C::kTmemO + t * HD, tmem + t * kKeys + kk * 8, vs + kk * ((16 * 128) >> 4), id_o,
+                               (j < w.hi[t] - 1 || kk > 0) ? 1u : 0u);
+                if (half == 1 && j == w.lo[t]) umma_commit(o_full + 8 * t);
+              }
+              __syncwarp();
+            };
+            add_half(0);
+            alive = wait_all(p_full + 8 * t, pphase[t]);
+            if (!alive) break;
+            pphase[t] ^= 1u;
+            add_half(1);
           }
           if (j > lo && active(t, j - 1)) alive = issue_s(t, j - 1, ik);
         }
@@ -452,8 +472,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
       umma_commit(drain_bar);
       if (!mbar_drain(drain_bar, 0u)) sts_u32(drain_fail, 1u);
     }
+  }
   } else {
     // ------------------------------------------------------------------ softmax: a thread per row
+    registers_up<kSoftmaxRegs>();
     const int t = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
     const uint32_t s_at = lane_base + t * kKeys, o_at = lane_base + C::kTmemO + t * HD;
@@ -484,8 +506,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
           if ((a.beta || a.c_rows) && f.status && !isfinite(scale)) atomicOr(f.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_SCALE);
         }
       }
-      RowSoftmax sm;
-      sm.start(scale * a.sm_scale * kLog2e, a.alibi ? a.alibi[h] / a.sm_scale : 0.f, pos);
+      RowSoftmax<CAP, TERMS> sm;
+      sm.start(scale * a.unit * kLog2e, a.alibi ? a.alibi[h] / a.unit : 0.f, pos);
       for (int j = hi - 1; j >= lo && alive; --j) {
         alive = wait_all(s_full + 8 * t, sphase);
         if (!alive) break;
@@ -494,10 +516,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
         float s[4][32];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(s_at + c * 32, s[c]);
-        tmem_ld_wait();
         const int k0 = j * kKeys;
         const bool edge = __any_sync(0xffffffffu, sees.x > k0 || sees.y < k0 + kKeys);
-        const float grown = sm.take(a, s, k0, sees, edge);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld_wait32(s[c]);
+        const float grown = sm.take(a.cap_inv, s, k0, sees, edge);
         if (j < hi - 1 && __any_sync(0xffffffffu, grown != 1.0f)) {
 #pragma unroll
           for (int c = 0; c < HD / 16; ++c) {
@@ -513,13 +536,16 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint32_t p[16];
-          sm.probabilities(s[c], p, edge);
+          sm.probabilities(s[c], p);
           tmem_st16(s_at + c * 16, p);
+          if (c == 1 || c == 3) {
+            // (the first half of P goes ahead)
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive((c == 1 ? p_half : p_full) + 8 * t);
+          }
         }
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + 8 * t);
       }
       if (!alive) break;
       float inv = 0.f;
@@ -595,14 +621,29 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
   }
 }
 
+template <int HD, bool PAGED, bool CAP, bool TERMS>
+cudaError_t launch_variant(unsigned grid, const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const FwdArgs& f,
+                           cudaStream_t stream) {
+  const cudaError_t err =
+      cudaFuncSetAttribute(softmax_fwd_kernel<HD, PAGED, CAP, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdCfg<HD>::kSmemBytes);
+  if (err != cudaSuccess) return err;
+  return launch_kernel(softmax_fwd_kernel<HD, PAGED, CAP, TERMS>, grid, kFwdThreads, FwdCfg<HD>::kSmemBytes, stream, map_q, map_k, map_v, f);
+}
+template <int HD, bool PAGED>
+cudaError_t launch_any(unsigned grid, const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const FwdArgs& f, cudaStream_t stream) {
+  const bool cap = f.a.cap_inv > 0.f, terms = f.a.beta || f.a.c_rows || f.a.alibi;
+  if (cap) return terms ? launch_variant<HD, PAGED, true, true>(grid, map_q, map_k, map_v, f, stream)
+                        : launch_variant<HD, PAGED, true, false>(grid, map_q, map_k, map_v, f, stream);
+  return terms ? launch_variant<HD, PAGED, false, true>(grid, map_q, map_k, map_v, f, stream)
+               : launch_variant<HD, PAGED, false, false>(grid, map_q, map_k, map_v, f, stream);
+}
+
 template <int HD>
 cudaError_t fwd_launch(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, int32_t* status, cudaStream_t stream) {
   CUtensorMap map_q, map_k, map_v;
   cudaError_t err = make_tile_map(&map_q, q, a.D, a.N, a.H, a.B, a.q.n, a.q.h, a.q.b);
   if (err == cudaSuccess) err = make_tile_map(&map_k, k, a.D, a.N, a.KH, a.B, a.k.n, a.k.h, a.k.b);
   if (err == cudaSuccess) err = make_tile_map(&map_v, v, a.D, a.N, a.KH, a.B, a.v.n, a.v.h, a.v.b);
-  if (err == cudaSuccess)
-    err = cudaFuncSetAttribute(softmax_fwd_kernel<HD, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdCfg<HD>::kSmemBytes);
   if (err != cudaSuccess) return err;
   FwdArgs f = {};
   f.a = a;
@@ -612,20 +653,17 @@ cudaError_t fwd_launch(const SoftmaxArgs& a, const void* q, const void* k, const
   f.o = static_cast<__nv_bfloat16*>(o);
   f.lse = lse;
   f.status = status;
-  const unsigned grid = (unsigned)((long long)a.B * a.KH * f.pairs * f.tiles);
-  return launch_kernel(softmax_fwd_kernel<HD, false>, grid, kFwdThreads, FwdCfg<HD>::kSmemBytes, stream, map_q, map_k, map_v, f);
+  return launch_any<HD, false>((unsigned)((long long)a.B * a.KH * f.pairs * f.tiles), map_q, map_k, map_v, f, stream);
 }
 
 template <int HD>
 cudaError_t chunks_launch(const SoftmaxPagedArgs& p, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t stream) {
   CUtensorMap map_q;
-  cudaError_t err = make_tile_map(&map_q, p.q, p.c.D, p.c.T, p.H, 1, p.q_st, p.q_sh, p.c.T * p.q_st);
-  if (err == cudaSuccess)
-    err = cudaFuncSetAttribute(softmax_fwd_kernel<HD, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdCfg<HD>::kSmemBytes);
+  const cudaError_t err = make_tile_map(&map_q, p.q, p.c.D, p.c.T, p.H, 1, p.q_st, p.q_sh, p.c.T * p.q_st);
   if (err != cudaSuccess) return err;
   FwdArgs f = {};
   f.a.B = p.c.B; f.a.H = p.H; f.a.KH = p.c.KH; f.a.G = p.G; f.a.D = p.c.D;
-  f.a.sm_scale = p.sm_scale; f.a.cap_acc = p.cap_acc; f.a.cap_inv = p.cap_inv;
+  f.a.sm_scale = p.sm_scale; f.a.cap_inv = p.cap_inv; f.a.unit = p.unit;
   f.a.beta = p.beta; f.a.gamma = p.gamma; f.a.delta = p.delta; f.a.alibi = p.alibi;
   f.pair_heads = p.G % 2 == 0;
   f.pairs = chunk_pairs(p.G);
@@ -636,8 +674,9 @@ cudaError_t chunks_launch(const SoftmaxPagedArgs& p, const CUtensorMap& map_k, c
   f.window = p.window; f.max_q = p.max_q; f.max_kv = p.max_kv; f.few_rows = p.few_rows;
   f.shares = p.shares; f.box_shift = p.box_shift;
   f.part_o = p.chunk_o; f.part_ml = p.chunk_ml;
+  f.v = p.v;
   const long long units = ((long long)p.c.T / chunk_block(p.G) + p.c.B) * p.c.KH * f.pairs;
-  return launch_kernel(softmax_fwd_kernel<HD, true>, (unsigned)(units * p.shares), kFwdThreads, FwdCfg<HD>::kSmemBytes, stream, map_q, map_k, map_v, f);
+  return launch_any<HD, true>((unsigned)(units * p.shares), map_q, map_k, map_v, f, stream);
 }
 
 }  // namespace

@@ -10,6 +10,7 @@
 #include <cuda.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "sm100_ptx.cuh"
 #include "softmax_paged.cuh"
@@ -254,8 +255,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
         const float c = a.beta ? length_scale(a.beta[h], a.gamma[h], a.delta[h], pos[y] + 1 - begin[y]) : 1.0f;
         if (a.beta && a.status && mine && !isfinite(c)) atomicOr(a.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_SCALE);
         flip[y] = c < 0.f;
-        scale[y] = fmaxf(fabsf(c * a.sm_scale * kLog2e), 1e-30f);    // (see RowSoftmax)
-        slope[y] = a.alibi ? a.alibi[h] / a.sm_scale : 0.f;
+        scale[y] = fmaxf(fabsf(c * a.unit * kLog2e), 1e-30f);    // (see RowSoftmax)
+        slope[y] = a.alibi ? a.alibi[h] / a.unit : 0.f;
       }
 #pragma unroll
       for (int e = 0; e < HD / 8; ++e)
@@ -271,16 +272,6 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
         const int key0 = kg * (8 * NT);          // this warp's keys of the tile
         const int k0 = j * kTileKeys + key0;
         const bool edge = k0 < all_from || k0 + 8 * NT > all_to;
-        if (edge && (k0 < first_key || k0 + 8 * NT > w.len)) {
-          // rows of V nobody sees may hold anything: zeros instead (each warp its own keys; the warps of other rows write the same)
-          for (int r = lane; r < 8 * NT * C::kHalves; r += 32) {
-            const int key = r % (8 * NT), hf = r / (8 * NT);
-            if (k0 + key < first_key || k0 + key >= w.len)
-              for (int e = 0; e < 8; ++e) sts_f4(v_at + hf * (kTileKeys * 128) + (key0 + key) * 128 + e * 16, 0.f, 0.f, 0.f, 0.f);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the next copy into this stage comes behind them)
-          __syncwarp();
-        }
         float s[NT][4];
 #pragma unroll
         for (int e = 0; e < NT; ++e)
@@ -298,10 +289,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
             mma16816(s[e + 1], q[kk], b2, b3);
           }
         }
-        if (a.cap_acc > 0.f) {
-#pragma unroll
-          for (int e = 0; e < NT; ++e) cap_scores(a.cap_acc, a.cap_inv, s[e]);
-        }
+        if (a.cap_inv > 0.f) tanh_scores(a.cap_inv, reinterpret_cast<float (&)[4 * NT]>(s));
         float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int e = 0; e < NT; ++e) {
@@ -348,18 +336,32 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
             p[e >> 1][(e & 1) * 2 + y] = bf16x2(p0, p1);
           }
         }
+        // O += P V.  Slots no row sees may hold anything, and a NaN times a probability of 0 is one too: their entries are taken for 0 in the registers.
+        auto add_values = [&](auto some_unseen) {
 #pragma unroll
-        for (int kk = 0; kk < NT / 2; ++kk) {
-          const int row = key0 + 16 * kk + (lane & 7) + (((lane >> 3) & 1) << 3);
+          for (int kk = 0; kk < NT / 2; ++kk) {
+            const int row = key0 + 16 * kk + (lane & 7) + (((lane >> 3) & 1) << 3);
+            uint32_t m0 = 0xffffffffu, m1 = 0xffffffffu;
+            if (decltype(some_unseen)::value) {
+              auto seen = [&](int key) -> uint32_t {
+                return (key >= first_key && key < w.len ? 0x0000ffffu : 0u) | (key + 1 >= first_key && key + 1 < w.len ? 0xffff0000u : 0u);
+              };
+              m0 = seen(k0 + 16 * kk + 2 * (lane & 3));
+              m1 = seen(k0 + 16 * kk + 2 * (lane & 3) + 8);
+            }
 #pragma unroll
-          for (int e = 0; e < HD / 8; e += 2) {
-            const int unit = (e & 7) + (lane >> 4);
-            uint32_t b0, b1, b2, b3;
-            ldsm4_t(v_at + (e >> 3) * (kTileKeys * 128) + row * 128 + ((unit ^ (row & 7)) << 4), b0, b1, b2, b3);
-            mma16816(out[e], p[kk], b0, b1);
-            mma16816(out[e + 1], p[kk], b2, b3);
+            for (int e = 0; e < HD / 8; e += 2) {
+              const int unit = (e & 7) + (lane >> 4);
+              uint32_t b0, b1, b2, b3;
+              ldsm4_t(v_at + (e >> 3) * (kTileKeys * 128) + row * 128 + ((unit ^ (row & 7)) << 4), b0, b1, b2, b3);
+              if (decltype(some_unseen)::value) { b0 &= m0; b1 &= m1; b2 &= m0; b3 &= m1; }
+              mma16816(out[e], p[kk], b0, b1);
+              mma16816(out[e + 1], p[kk], b2, b3);
+            }
           }
-        }
+        };
+        if (k0 < first_key || k0 + 8 * NT > w.len) add_values(std::true_type{});
+        else add_values(std::false_type{});
         __syncwarp();
         if (lane == 0) mbar_arrive(empty + 8 * st);
       }
@@ -539,10 +541,11 @@ int softmax_paged_args(const entmax_attn_paged_cache* cache, const entmax_attn_s
   a.G = a.H / a.c.KH;
   a.window = p->window;
   a.sm_scale = p->sm_scale > 0.f ? p->sm_scale : 1.0f / std::sqrt((float)a.c.D);
+  a.unit = a.sm_scale;
   if (p->softcap > 0.f) {
-    a.cap_acc = p->softcap / a.sm_scale;
+    a.unit = p->softcap;
     a.cap_inv = a.sm_scale / p->softcap;
-    if (!std::isfinite(a.cap_acc) || !std::isfinite(a.cap_inv) || a.cap_acc == 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
+    if (!std::isfinite(a.cap_inv) || a.cap_inv == 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
   }
   const int most_kv = a.c.max_pages << a.c.ps_shift;
   a.max_kv = p->max_kv_len > 0 && p->max_kv_len < most_kv ? p->max_kv_len : most_kv;
@@ -658,6 +661,7 @@ extern "C" int entmax_attn_softmax_paged_fwd(const entmax_attn_paged_cache* cach
   a.c.table = block_table; a.c.kv_len = kv_len; a.c.cu_q = cu_q;
   a.beta = beta; a.gamma = gamma; a.delta = delta; a.alibi = alibi_slopes;
   a.q = static_cast<const __nv_bfloat16*>(q);
+  a.v = static_cast<const __nv_bfloat16*>(v_cache);
   a.o = static_cast<__nv_bfloat16*>(o);
   a.lse = lse;
   a.status = device_status;

@@ -14,10 +14,10 @@ struct SoftmaxPagedArgs {
   int max_q, max_kv;                  // longest chunk and sequence that are served
   int few_rows;                       // sequences with n * G <= few_rows rows are the "few" kernel's
   int box_shift;                      // a page's boxes have 1 << box_shift keys
-  float sm_scale, cap_acc, cap_inv;
+  float sm_scale, cap_inv, unit;
   const float *beta, *gamma, *delta, *alibi;
   long long q_st, q_sh;
-  const __nv_bfloat16* q;
+  const __nv_bfloat16 *q, *v;
   __nv_bfloat16* o;
   float* lse;
   int32_t* status;

@@ -104,13 +104,13 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// x_ij / sm_scale of an accumulator and what d x / d acc is at it
+// The capped score of an accumulator, in the scores' unit, and d z / d (sm_scale acc) at it
 __device__ __forceinline__ float capped(const SoftmaxArgs& a, float acc, float& slope) {
   slope = 1.0f;
-  if (a.cap_acc == 0.f) return acc;
+  if (a.cap_inv == 0.f) return acc;
   const float t = tanh_full(acc * a.cap_inv);
   slope = 1.0f - t * t;
-  return a.cap_acc * t;
+  return t;
 }
 
 // Keys that any row of the tile sees; lo, hi: two words of shared memory
@@ -146,11 +146,11 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_fwd_kernel(const Sof
   for (int y = 0; y < 4; ++y) {
     const int i = row0 + ty * 4 + y;
     sees[y] = i < a.N ? visible_keys(a, b, i) : make_int2(0, 0);
-    scale[y] = i < a.N ? row_scale(a, b, h, i, sees[y].y - sees[y].x) * a.sm_scale * kLog2e : 0.f;
+    scale[y] = i < a.N ? row_scale(a, b, h, i, sees[y].y - sees[y].x) * a.unit * kLog2e : 0.f;
     top[y] = -INFINITY;
     mass[y] = 0.f;
   }
-  const float slope = a.alibi ? a.alibi[h] / a.sm_scale : 0.f;
+  const float slope = a.alibi ? a.alibi[h] / a.unit : 0.f;
   load_rows<D>(Q, q + b * a.q.b + h * a.q.h, a.q.n, row0, a.N);
   const int2 range = tile_range(sees, lo_hi);
   for (int j0 = range.x / kT * kT; j0 < range.y; j0 += kT) {
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_dq_kernel(const Soft
     c[y] = i < a.N ? row_scale(a, b, h, i, sees[y].y - sees[y].x) : 0.f;
     lse2[y] = sees[y].y > sees[y].x ? g.lse[(size_t)bh * a.N + i] * kLog2e : 0.f;
   }
-  const float slope = a.alibi ? a.alibi[h] / a.sm_scale : 0.f;
+  const float slope = a.alibi ? a.alibi[h] / a.unit : 0.f;
   load_rows<D>(Q, q + b * a.q.b + h * a.q.h, a.q.n, row0, a.N);
   load_rows<D>(DO, d_o + b * g.d_o.b + h * g.d_o.h, g.d_o.n, row0, a.N);
   const int2 range = tile_range(sees, lo_hi);
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_dq_kernel(const Soft
           const int j = j0 + tx + 16 * x;
           float grow;
           const float xa = capped(a, s[y][x], grow) - slope * fabsf((float)(i - j));
-          const float p = j >= sees[y].x && j < sees[y].y ? exp2f(c[y] * a.sm_scale * kLog2e * xa - lse2[y]) : 0.f;
+          const float p = j >= sees[y].x && j < sees[y].y ? exp2f(c[y] * a.unit * kLog2e * xa - lse2[y]) : 0.f;
           if (pass == 0) {
             dot[y] = fmaf(p, dp[y][x], dot[y]);
           } else {
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_dq_kernel(const Soft
     const float total = row_sum(dc[y]);
     if (tx == 0 && i < a.N) {
       g.row_dot[(size_t)bh * a.N + i] = dot[y];
-      if (g.dc_rows) g.dc_rows[(size_t)bh * a.N + i] = total * a.sm_scale;
+      if (g.dc_rows) g.dc_rows[(size_t)bh * a.N + i] = total * a.unit;
     }
   }
   store_rows<D>(dq + b * g.dq.b + h * g.dq.h, g.dq.n, row0, a.N, out, mul);
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_dkv_kernel(const Sof
   load_rows<D>(K, k + b * a.k.b + kh * a.k.h, a.k.n, j0, a.N);
   load_rows<D>(V, v + b * a.v.b + kh * a.v.h, a.v.n, j0, a.N);
   for (int h = kh * a.G; h < (kh + 1) * a.G; ++h) {
-    const float slope = a.alibi ? a.alibi[h] / a.sm_scale : 0.f;
+    const float slope = a.alibi ? a.alibi[h] / a.unit : 0.f;
     for (int row0 = 0; row0 < a.N; row0 += kT) {
       int2 sees[4];
 #pragma unroll
@@ -311,16 +311,16 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_dkv_kernel(const Sof
         const int i = row0 + ty * 4 + y;
         const bool any = sees[y].y > sees[y].x;
         const size_t at = ((size_t)b * a.H + h) * a.N + (any ? i : 0);
-        const float c = any ? row_scale(a, b, h, i, sees[y].y - sees[y].x) * a.sm_scale : 0.f;
+        const float c = any ? row_scale(a, b, h, i, sees[y].y - sees[y].x) : 0.f;
         const float lse2 = any ? g.lse[at] * kLog2e : 0.f, dot = any ? g.row_dot[at] : 0.f;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int j = j0 + tx + 16 * x;
           float grow;
           const float xa = capped(a, s[y][x], grow) - slope * fabsf((float)(i - j));
-          const float p = j >= sees[y].x && j < sees[y].y ? exp2f(c * kLog2e * xa - lse2) : 0.f;
+          const float p = j >= sees[y].x && j < sees[y].y ? exp2f(c * a.unit * kLog2e * xa - lse2) : 0.f;
           P[(ty * 4 + y) * C::kLdS + tx + 16 * x] = p;
-          S[(ty * 4 + y) * C::kLdS + tx + 16 * x] = p * (dp[y][x] - dot) * grow * c;
+          S[(ty * 4 + y) * C::kLdS + tx + 16 * x] = p * (dp[y][x] - dot) * grow * (c * a.sm_scale);
         }
       }
       __syncthreads();

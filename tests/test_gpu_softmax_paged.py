@@ -213,6 +213,20 @@ def test_repeats_are_bit_equal_whatever_the_workspace_held(new, lens, H, KH, d):
         assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
 
 
+@pytest.mark.parametrize("new,lens,H,KH,d,page,kind", [
+    ([3, 2, 5], [600, 2, 70], 8, 4, 128, 32, "window100"), ([1] * 5, [700, 33, 64, 1000, 17], 8, 2, 128, 16, "window300"),
+    ([300, 1, 140], [700, 90, 400], 8, 4, 64, 16, "window90+cap"), ([300, 260], [333, 1400], 4, 2, 128, 256, "cap")])
+def test_many_repeats_over_slots_that_hold_anything(new, lens, H, KH, d, page, kind):
+    # tiles with slots that no row sees (NaN here), cleared in time in every one of many runs
+    pr = _problem(new, lens, H, KH, d, page, seed=27)
+    t = _terms(kind, H)
+    ref = _run(pr, t)
+    _check(pr, ref, t)
+    for _ in range(500):
+        got = _run(pr, t)
+        assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+
+
 def test_writes_nothing_outside_its_outputs():
     for new, lens in (([1, 1], [700, 64]), ([140, 3], [400, 50])):
         pr = _problem(new, lens, 6, 2, 64, 16, seed=8)
