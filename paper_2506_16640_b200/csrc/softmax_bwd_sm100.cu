@@ -4,15 +4,18 @@
 //   dQ_i = c_i sm sum_j dx_ij k_j,   dK_j = sum_i c_i sm dx_ij q_i,   dV_j = sum_i P_ij dO_i
 // Two kernels, so that nothing is added up by atomics: the scores and dP are formed twice (seven products instead of five), but no gradient goes
 // through memory as a float32 sum and results are the same every time.
-//   softmax_dq_kernel   an item is a Q tile of 128 rows: S and dP in TMEM, a row's 128 columns by four threads, dS as bf16 over S's own columns
-//                       and from there into dQ += dS K.  Leaves -lse log2 e, a and -D of every row, and which keys every tile sees, to the other kernel.
+//   softmax_dq_kernel   an item is a Q tile of 128 rows: S and dP in TMEM, a row's 128 columns by four threads, dS as bf16 to TMEM and
+//                       from there into dQ += dS K.  Leaves -lse log2 e, a and -D of every row, and which keys every tile sees, to the other kernel.
 //                       dL/dc_i = sum dS x is formed as sum p dP x - (sum p dP)(sum p x) / sum p, all of float32 probabilities: the D above comes
 //                       from the O that was rounded to bf16, which is good enough for dS (an error of 2^-9 of D times p) but not for a float32 result.
 //   softmax_dkv_kernel  an item is a K/V tile; over all query heads that share it and all Q tiles that see it: S^T = K Q^T and dP^T = V dO^T with the keys
 //                       along the lanes, so that P^T and dS^T are, over their own columns, the A operands of dV += P^T dO and dK += dS^T Q; what
 //                       depends on the query comes from shared memory, four columns a load.
 //
-// CTA of both: warp 0 scheduler and TMA producer, warp 1 MMA issuer, warps 2..17 four threads per TMEM lane (32 columns each).  Every wait is bounded.
+// CTA of both: warp 0 scheduler and TMA producer, warp 1 MMA issuer, warps 2..17 four threads per TMEM lane (32 columns each).  The dQ kernel has a second
+// issuer, warp 18, for dQ alone: an issuer is held up by the products it issues, and a wait that is over at once still takes 100 cycles, of which a step has
+// five (16 heads x 8192 x 128, no mask: 667 us with one, 580 with two; forward and dK / dV, whose issuers' products depend on one another, lost by a
+// second one).  Every wait is bounded.
 #include <cuda.h>
 
 #include "sm100_ptx.cuh"
@@ -27,7 +30,10 @@ using namespace sm100;
 
 constexpr int kT = 128;
 constexpr int kWarps = 16;                       // element code
+constexpr int kGroups = kWarps / 4;              // threads per TMEM lane
+constexpr int kChunks = 4 / kGroups;             // times 32 columns each
 constexpr int kBwdThreads = (2 + kWarps) * 32;
+constexpr int kDqThreads = (3 + kWarps) * 32, kSecond = 2 + kWarps;   // dQ: with a second MMA issuer, that warp
 constexpr int kBwdBars = 1536;
 
 template <int HD>
@@ -64,8 +70,7 @@ template <int HD>
 __host__ __device__ constexpr uint32_t bwd_idesc_kn() {
   return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(kT >> 4) << 24);
 }
-// A bf16 operand written over the columns it came from: the 32 columns of thread group q hold 32 entries in their first 16, so K step kk (16
-// entries) starts here
+// A bf16 operand written over the columns it came from: every 32 columns hold their 32 entries in the first 16, so K step kk (16 entries) starts here
 __device__ __forceinline__ uint32_t a_column(int kk) { return (uint32_t)((kk >> 1) * 32 + (kk & 1) * 8); }
 
 // {first key, one behind the last, largest first, smallest last} over the rows of a tile that see something, by the whole warp
@@ -120,53 +125,47 @@ struct RowTerms {
   int i;
 };
 
-// 32 columns from key j0 on (s: their accumulators, or the tanh of capped ones): dS as bf16 pairs; dc: {sum p dP x, sum p dP, sum p x, sum p} where wanted, the even
+// 64 columns from key j0 on (s: their accumulators, or the tanh of capped ones): dS as bf16 pairs; dc: {sum p dP x, sum p dP, sum p x, sum p} where wanted, the even
 // and the odd columns' apart
 template <bool CAP, bool SLOPE, bool DC, bool EDGE>
-__device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const float (&s)[32], const float (&dp)[32], uint32_t (&ds)[16], uint64_t (&dc)[4]) {
+__device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const float (&s)[kChunks][32], const float (&dp)[kChunks][32], uint32_t (&ds)[kChunks][16],
+                                            uint64_t (&dc)[4]) {
   const uint64_t a2 = pack2(r.a, r.a), l2 = pack2(-r.lse2, -r.lse2), d2 = pack2(-r.dot, -r.dot);
 #pragma unroll
-  for (int e = 0; e < 32; e += 2) {
-    const uint64_t t = pack2(s[e], s[e + 1]);
-    uint64_t x = t;
-    if (SLOPE) x = pack2(fmaf(-r.slope, fabsf((float)(j0 + e - r.i)), s[e]), fmaf(-r.slope, fabsf((float)(j0 + e + 1 - r.i)), s[e + 1]));
-    float p0, p1;
-    unpack2(fma2(x, a2, l2), p0, p1);
-    p0 = exp2_fast(p0);
-    p1 = exp2_fast(p1);
-    if (EDGE) {
-      p0 = j0 + e >= r.sees.x && j0 + e < r.sees.y ? p0 : 0.f;
-      p1 = j0 + e + 1 >= r.sees.x && j0 + e + 1 < r.sees.y ? p1 : 0.f;
+  for (int c = 0; c < kChunks; ++c) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      const int j = j0 + c * 32 + e;
+      const uint64_t t = pack2(s[c][e], s[c][e + 1]);
+      uint64_t x = t;
+      if (SLOPE) x = pack2(fmaf(-r.slope, fabsf((float)(j - r.i)), s[c][e]), fmaf(-r.slope, fabsf((float)(j + 1 - r.i)), s[c][e + 1]));
+      float p0, p1;
+      unpack2(fma2(x, a2, l2), p0, p1);
+      p0 = exp2_fast(p0);
+      p1 = exp2_fast(p1);
+      if (EDGE) {
+        p0 = j >= r.sees.x && j < r.sees.y ? p0 : 0.f;
+        p1 = j + 1 >= r.sees.x && j + 1 < r.sees.y ? p1 : 0.f;
+      }
+      const uint64_t p = pack2(p0, p1), v = pack2(dp[c][e], dp[c][e + 1]);
+      uint64_t d = mul2(p, add2(v, d2));
+      if (CAP) d = mul2(d, fma2(t, pack2(-s[c][e], -s[c][e + 1]), pack2(1.0f, 1.0f)));
+      if (DC) {
+        const uint64_t u = mul2(p, v);
+        dc[0] = fma2(u, x, dc[0]);
+        dc[1] = add2(u, dc[1]);
+        dc[2] = fma2(p, x, dc[2]);
+        dc[3] = add2(p, dc[3]);
+      }
+      float d0, d1;
+      unpack2(d, d0, d1);
+      ds[c][e >> 1] = bf16x2(d0, d1);
     }
-    const uint64_t p = pack2(p0, p1), v = pack2(dp[e], dp[e + 1]);
-    uint64_t d = mul2(p, add2(v, d2));
-    if (CAP) d = mul2(d, fma2(t, pack2(-s[e], -s[e + 1]), pack2(1.0f, 1.0f)));
-    if (DC) {
-      const uint64_t u = mul2(p, v);
-      dc[0] = fma2(u, x, dc[0]);
-      dc[1] = add2(u, dc[1]);
-      dc[2] = fma2(p, x, dc[2]);
-      dc[3] = add2(p, dc[3]);
-    }
-    float d0, d1;
-    unpack2(d, d0, d1);
-    ds[e >> 1] = bf16x2(d0, d1);
   }
 }
-template <bool CAP, bool SLOPE>
-__device__ __forceinline__ void dq_elements_of(const RowTerms& r, int j0, bool edge, bool want_dc, const float (&s)[32], const float (&dp)[32],
-                                               uint32_t (&ds)[16], uint64_t (&dc)[4]) {
-  if (want_dc) {
-    if (edge) dq_elements<CAP, SLOPE, true, true>(r, j0, s, dp, ds, dc);
-    else dq_elements<CAP, SLOPE, true, false>(r, j0, s, dp, ds, dc);
-  } else {
-    if (edge) dq_elements<CAP, SLOPE, false, true>(r, j0, s, dp, ds, dc);
-    else dq_elements<CAP, SLOPE, false, false>(r, j0, s, dp, ds, dc);
-  }
-}
-
-template <int HD>
-__global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+// CAP, SLOPE, DC known at compile time: see RowSoftmax
+template <int HD, bool CAP, bool SLOPE, bool DC>
+__global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                                                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
                                                                     const __grid_constant__ BwdArgs f) {
   pdl_begin();
@@ -179,13 +178,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
   const uint32_t q_full = bars + 80, q_empty = bars + 88;
   const uint32_t k_full = bars + 96, k_empty = bars + 120;           // [3]
   const uint32_t v_full = bars + 144, v_empty = bars + 160;          // [2]
-  const uint32_t s_full = bars + 176, s_empty = bars + 184;          // S and dP of a tile
+  const uint32_t s_full = bars + 176, s_empty = bars + 184;
+  const uint32_t dp_full = bars + 296, dp_empty = bars + 304;
   const uint32_t ds_full = bars + 192, ds_empty = bars + 200;
   const uint32_t dq_full = bars + 208, dq_empty = bars + 216;
   const uint32_t w_full = bars + 224, w_empty = bars + 240;          // [2]
-  const uint32_t next_bar = bars + 256, drain_bar = bars + 264, x_bar = bars + 272;
+  const uint32_t next_bar = bars + 256, x_bar = bars + 264, drain_bar = bars + 312;   // drain_bar [2]
   const uint32_t tmem_slot = bars + 280, abort_flag = bars + 284, drain_fail = bars + 288;
-  const uint32_t dot_at = bars + 320;                                // float [2][128]: of this item and the one before
+  const uint32_t dot_at = bars + 336;                                // float [2][128]: of this item and the one before
   const BwdWork* work = reinterpret_cast<const BwdWork*>(smem_raw + (work_at - smem_u32(smem_raw)));
   constexpr int kS = 0, kDP = kT, kDQ = 2 * kT, kDS = 2 * kT + 128;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -197,13 +197,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
     for (int st = 0; st < C::kVStages; ++st) { mbar_init(v_full + 8 * st, 1); mbar_init(v_empty + 8 * st, 1); }
     mbar_init(s_full, 1);
     mbar_init(s_empty, kWarps);
+    mbar_init(dp_full, 1);
+    mbar_init(dp_empty, kWarps);
     mbar_init(ds_full, kWarps);
     mbar_init(ds_empty, 1);
     mbar_init(dq_full, 1);
     mbar_init(dq_empty, kWarps);
-    for (int t = 0; t < 2; ++t) { mbar_init(w_full + 8 * t, 1); mbar_init(w_empty + 8 * t, 1 + kWarps); }
+    for (int t = 0; t < 2; ++t) { mbar_init(w_full + 8 * t, 1); mbar_init(w_empty + 8 * t, 2 + kWarps); mbar_init(drain_bar + 8 * t, 1); }
     mbar_init(next_bar, 1);
-    mbar_init(drain_bar, 1);
     mbar_init(x_bar, kWarps);
     sts_u32(abort_flag, 0u);
     sts_u32(drain_fail, 0u);
@@ -217,9 +218,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = lds_u32(tmem_slot);
+  const uint32_t tmem = uniform(lds_u32(tmem_slot));
   const SoftmaxArgs& a = f.a;
   auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
+  // two barriers at once: the second one's answer comes with the first's
+  auto wait_both = [&](uint32_t bar, uint32_t parity, uint32_t bar2, uint32_t parity2) -> bool {
+    const bool a1 = mbar_try_wait(bar, parity), a2 = mbar_try_wait(bar2, parity2);
+    if (__all_sync(0xffffffffu, a1 && a2)) return true;
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag) && mbar_wait(bar2, parity2, abort_flag));
+  };
 
   if (warp == 0) {
     uint32_t next_phase = 0, wphase = 0, qphase = 0, kidx = 0, vidx = 0;
@@ -312,18 +319,20 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
       if (!ok) sts_u32(drain_fail, 1u);
     }
   } else if (warp == 1) {
-    constexpr uint32_t id_kk = bwd_idesc_kk(), id_kn = bwd_idesc_kn<HD>();
+    // ------------------------------------------------------------------ S and dP.  Each is issued again as soon as the element warps have the last one in
+    // registers: while one is on its way between the two sides the tensor core has the other.
+    constexpr uint32_t id_kk = bwd_idesc_kk();
     const uint64_t dhi = (uint64_t)kDescHi << 32;
     const uint64_t q_d = dhi | smem_desc_lo(q_smem), do_d = dhi | smem_desc_lo(do_smem), k_d = dhi | smem_desc_lo(k_smem),
-                   v_d = dhi | smem_desc_lo(v_smem), kn_d = dhi | mn_desc_lo(k_smem);
+                   v_d = dhi | smem_desc_lo(v_smem);
     constexpr uint32_t kStageD = C::kTile >> 4;
-    uint32_t wphase = 0, qphase = 0, sphase = 0, dsphase = 0, dqphase = 0, kidx = 0, vidx = 0;
+    uint32_t wphase = 0, qphase = 0, sphase = 0, dpphase = 0, kidx = 0, vidx = 0;
     int slot = 0;
     bool alive = true;
     while (alive) {
       alive = wait_all(w_full + 8 * slot, wphase);
       if (!alive) break;
-      const int valid = work[slot].valid, lo = work[slot].lo, hi = work[slot].hi;
+      const int valid = uniform(work[slot].valid), lo = uniform(work[slot].lo), hi = uniform(work[slot].hi);
       __syncwarp();
       if (lane == 0) mbar_arrive(w_empty + 8 * slot);
       if (++slot == 2) { slot = 0; wphase ^= 1u; }
@@ -332,14 +341,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
       alive = wait_all(q_full, qphase);
       if (!alive) break;
       qphase ^= 1u;
-      auto issue_s = [&](bool last) -> bool {
+      for (int j = hi - 1; j >= lo && alive; --j) {
         const uint32_t ks = kidx % C::kKStages, vs = vidx % C::kVStages;
-        bool ok = wait_all(k_full + 8 * ks, (kidx / C::kKStages) & 1u);
-        if (ok) ok = wait_all(v_full + 8 * vs, (vidx / C::kVStages) & 1u);
-        if (ok) ok = wait_all(s_empty, sphase ^ 1u);
-        if (!ok) return false;
+        alive = wait_both(k_full + 8 * ks, (kidx / C::kKStages) & 1u, s_empty, sphase ^ 1u);
+        if (!alive) break;
         ++kidx;
-        ++vidx;
         sphase ^= 1u;
         tc_fence_after();
         if (elect_one()) {
@@ -348,42 +354,23 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
             const uint32_t off = (kk >> 2) * ((kT * 128) >> 4) + (kk & 3) * 2;
             umma_bf16_desc(tmem + kS, q_d + off, k_d + ks * kStageD + off, id_kk, kk > 0 ? 1u : 0u);
           }
+          umma_commit(s_full);
+        }
+        __syncwarp();
+        alive = wait_both(v_full + 8 * vs, (vidx / C::kVStages) & 1u, dp_empty, dpphase ^ 1u);
+        if (!alive) break;
+        ++vidx;
+        dpphase ^= 1u;
+        tc_fence_after();
+        if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < HD / 16; ++kk) {
             const uint32_t off = (kk >> 2) * ((kT * 128) >> 4) + (kk & 3) * 2;
             umma_bf16_desc(tmem + kDP, do_d + off, v_d + vs * kStageD + off, id_kk, kk > 0 ? 1u : 0u);
           }
-          umma_commit(s_full);
+          umma_commit(dp_full);
           umma_commit(v_empty + 8 * vs);
-          if (last) umma_commit(q_empty);
-        }
-        __syncwarp();
-        return true;
-      };
-      uint32_t kq = kidx;                        // the K tile the next dQ reads
-      alive = issue_s(hi - lo == 1);
-      for (int j = hi - 1; j >= lo && alive; --j, ++kq) {
-        if (j > lo) {
-          alive = issue_s(j == lo + 1);
-          if (!alive) break;
-        }
-        alive = wait_all(ds_full, dsphase);
-        if (!alive) break;
-        dsphase ^= 1u;
-        if (j == hi - 1) {
-          alive = wait_all(dq_empty, dqphase ^ 1u);
-          if (!alive) break;
-          dqphase ^= 1u;
-        }
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t kn = kn_d + (kq % C::kKStages) * kStageD;
-#pragma unroll
-          for (int kk = 0; kk < kT / 16; ++kk)
-            umma_bf16_ts(tmem + kDQ, tmem + kDS + kk * 8, kn + kk * ((16 * 128) >> 4), id_kn, (j < hi - 1 || kk > 0) ? 1u : 0u);
-          umma_commit(k_empty + 8 * (kq % C::kKStages));
-          umma_commit(ds_empty);
-          if (j == lo) umma_commit(dq_full);
+          if (j == lo) umma_commit(q_empty);
         }
         __syncwarp();
       }
@@ -392,13 +379,54 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
       umma_commit(drain_bar);
       if (!mbar_drain(drain_bar, 0u)) sts_u32(drain_fail, 1u);
     }
-  } else {
-    const int quad = warp & 3, quarter = (warp - 2) >> 2, row = quad * 32 + lane;
-    const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
-    uint32_t wphase = 0, sphase = 0, dsphase = 0, dqphase = 0, xphase = 0, dot_buf = 0;
+  } else if (warp == kSecond) {
+    // ------------------------------------------------------------------ dQ
+    constexpr uint32_t id_kn = bwd_idesc_kn<HD>();
+    const uint64_t kn_d = ((uint64_t)kDescHi << 32) | mn_desc_lo(k_smem);
+    constexpr uint32_t kStageD = C::kTile >> 4;
+    uint32_t wphase = 0, dsphase = 0, dqphase = 0, kidx = 0;
     int slot = 0;
     bool alive = true;
-    const bool want_dc = f.g.dc_rows != nullptr;
+    while (alive) {
+      alive = wait_all(w_full + 8 * slot, wphase);
+      if (!alive) break;
+      const int valid = uniform(work[slot].valid), lo = uniform(work[slot].lo), hi = uniform(work[slot].hi);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (!valid) break;
+      if (hi <= lo) continue;
+      alive = wait_all(dq_empty, dqphase ^ 1u);              // the previous item's dQ has been read
+      if (!alive) break;
+      dqphase ^= 1u;
+      for (int j = hi - 1; j >= lo && alive; --j, ++kidx) {
+        const uint32_t ks = kidx % C::kKStages;
+        alive = wait_both(k_full + 8 * ks, (kidx / C::kKStages) & 1u, ds_full, dsphase);
+        if (!alive) break;
+        dsphase ^= 1u;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t kn = kn_d + ks * kStageD;
+#pragma unroll
+          for (int kk = 0; kk < kT / 16; ++kk)
+            umma_bf16_ts(tmem + kDQ, tmem + kDS + kk * 8, kn + kk * ((16 * 128) >> 4), id_kn, (j < hi - 1 || kk > 0) ? 1u : 0u);
+          umma_commit(k_empty + 8 * ks);                     // (S of this tile came long before)
+          umma_commit(ds_empty);
+          if (j == lo) umma_commit(dq_full);
+        }
+        __syncwarp();
+      }
+    }
+    if (!alive && lane == 0) {
+      umma_commit(drain_bar + 8);
+      if (!mbar_drain(drain_bar + 8, 0u)) sts_u32(drain_fail, 1u);
+    }
+  } else {
+    const int quad = warp & 3, group = (warp - 2) >> 2, row = quad * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
+    uint32_t wphase = 0, sphase = 0, dpphase = 0, dsphase = 0, dqphase = 0, xphase = 0, dot_buf = 0;
+    int slot = 0;
+    bool alive = true;
     while (alive) {
       alive = wait_all(w_full + 8 * slot, wphase);
       if (!alive) break;
@@ -407,27 +435,30 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
       if (lane == 0) mbar_arrive(w_empty + 8 * slot);
       if (++slot == 2) { slot = 0; wphase ^= 1u; }
       if (!valid) break;
-      // D of the tile's rows, eight rows a warp: a row's 32 lanes read D / 32 elements each of O and dO
+      // D of the tile's rows, 16 rows a warp: a row's 32 lanes read D / 32 elements each of O and dO
       {
         constexpr int E = HD / 32;
-        const int first = (warp - 2) * 8;
-        float part[8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          const int i = tile * kT + first + r;
-          part[r] = 0.f;
-          if (i < a.N) {
-            float x[E], y[E];
-            load_slice<E>(f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n + lane * E, x);
-            load_slice<E>(f.d_o + (long long)b * f.g.d_o.b + (long long)h * f.g.d_o.h + (long long)i * f.g.d_o.n + lane * E, y);
+        for (int batch = 0; batch < kT / kWarps / 8; ++batch) {
+          const int first = (warp - 2) * (kT / kWarps) + batch * 8;
+          float part[8];
 #pragma unroll
-            for (int e = 0; e < E; ++e) part[r] = fmaf(x[e], y[e], part[r]);
+          for (int r = 0; r < 8; ++r) {
+            const int i = tile * kT + first + r;
+            part[r] = 0.f;
+            if (i < a.N) {
+              float x[E], y[E];
+              load_slice<E>(f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n + lane * E, x);
+              load_slice<E>(f.d_o + (long long)b * f.g.d_o.b + (long long)h * f.g.d_o.h + (long long)i * f.g.d_o.n + lane * E, y);
+#pragma unroll
+              for (int e = 0; e < E; ++e) part[r] = fmaf(x[e], y[e], part[r]);
+            }
           }
-        }
 #pragma unroll
-        for (int r = 0; r < 8; ++r) part[r] = warp_sum(part[r]);
-        if (lane == 0)
-          for (int r = 0; r < 8; ++r) sts_u32(dot_at + dot_buf + 4 * (first + r), __float_as_uint(part[r]));
+          for (int r = 0; r < 8; ++r) part[r] = warp_sum(part[r]);
+          if (lane == 0)
+            for (int r = 0; r < 8; ++r) sts_u32(dot_at + dot_buf + 4 * (first + r), __float_as_uint(part[r]));
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(x_bar);
         alive = wait_all(x_bar, xphase);
@@ -447,7 +478,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
       r.lse2 = some ? f.g.lse[at] * kLog2e : INFINITY;
       r.slope = a.alibi ? a.alibi[h] / a.unit : 0.f;
       if (!some) { r.sees = make_int2(0, 0x7fffffff); r.a = 0.f; }   // (probability exp2(-inf) everywhere, without a mask)
-      if (quarter == 0) {
+      if (group == 0) {
         float* out = f.rows + ((size_t)(b * a.H + h) * f.tiles + tile) * (3 * kT) + row;
         out[0] = -r.lse2;
         out[kT] = r.a;
@@ -459,30 +490,41 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
         if (!alive) break;
         sphase ^= 1u;
         tc_fence_after();
-        float s[32], dp[32];
-        tmem_ld32(lane_base + kS + quarter * 32, s);
-        tmem_ld32(lane_base + kDP + quarter * 32, dp);
-        tmem_ld_wait();
+        const int j0 = j * kT + group * (32 * kChunks);
+        const bool edge = __any_sync(0xffffffffu, r.sees.x > j0 || r.sees.y < j0 + 32 * kChunks);
+        float s[kChunks][32], dp[kChunks][32];
+        uint32_t ds[kChunks][16];
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) tmem_ld32(lane_base + kS + group * (32 * kChunks) + c * 32, s[c]);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) tmem_ld_wait32(s[c]);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(s_empty);
-        const int j0 = j * kT + quarter * 32;
-        const bool edge = __any_sync(0xffffffffu, r.sees.x > j0 || r.sees.y < j0 + 32);
-        uint32_t ds[16];
-        if (a.cap_inv > 0.f) {
-          tanh_scores(a.cap_inv, s);
-          if (r.slope != 0.f) dq_elements_of<true, true>(r, j0, edge, want_dc, s, dp, ds, dc);
-          else dq_elements_of<true, false>(r, j0, edge, want_dc, s, dp, ds, dc);
-        } else {
-          if (r.slope != 0.f) dq_elements_of<false, true>(r, j0, edge, want_dc, s, dp, ds, dc);
-          else dq_elements_of<false, false>(r, j0, edge, want_dc, s, dp, ds, dc);
+        alive = wait_all(dp_full, dpphase);
+        if (!alive) break;
+        dpphase ^= 1u;
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) tmem_ld32(lane_base + kDP + group * (32 * kChunks) + c * 32, dp[c]);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) tmem_ld_wait32(dp[c]);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(dp_empty);
+        if (CAP) {
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) tanh_scores(a.cap_inv, s[c]);
         }
+        if (edge) dq_elements<CAP, SLOPE, DC, true>(r, j0, s, dp, ds, dc);
+        else dq_elements<CAP, SLOPE, DC, false>(r, j0, s, dp, ds, dc);
         // the dS before has been taken
         alive = wait_all(ds_empty, dsphase ^ 1u);
         if (!alive) break;
         dsphase ^= 1u;
         tc_fence_after();
-        tmem_st16(lane_base + kDS + quarter * 16, ds);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) tmem_st16(lane_base + kDS + (group * kChunks + c) * 16, ds[c]);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -496,17 +538,18 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
         dqphase ^= 1u;
         tc_fence_after();
       }
-      if (quarter < HD / 32) {
+      for (int c = group; c < HD / 32; c += kGroups) {
+        const int col = c * 32;
         float v[32];
         if (any) {
-          tmem_ld32(lane_base + kDQ + quarter * 32, v);
+          tmem_ld32(lane_base + kDQ + col, v);
           tmem_ld_wait();
         } else {
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = 0.f;
         }
         if (mine) {
-          __nv_bfloat16* out = f.dq + (long long)b * f.g.dq.b + (long long)h * f.g.dq.h + (long long)r.i * f.g.dq.n + quarter * 32;
+          __nv_bfloat16* out = f.dq + (long long)b * f.g.dq.b + (long long)h * f.g.dq.h + (long long)r.i * f.g.dq.n + col;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float* x = v + 8 * e;
@@ -515,9 +558,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
           }
         }
       }
-      if (want_dc) {
+      if (DC) {
         // the four threads of a row meet through the dS columns, which nobody needs until the next item's first dS is written: behind dq_empty of all
-        const uint32_t mine_at = lane_base + kDS + quarter * 16;
+        const uint32_t mine_at = lane_base + kDS + group * 16;
         uint32_t u[8] = {};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -536,14 +579,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dq_kernel(const __grid
         tc_fence_after();
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int qq = 0; qq < 4; ++qq) {
+        for (int other = 0; other < kGroups; ++other) {
           float v[8];
-          tmem_ld8(lane_base + kDS + qq * 16, v);
+          tmem_ld8(lane_base + kDS + other * 16, v);
           tmem_ld_wait();
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[e] += v[e];
         }
-        if (quarter == 0 && mine) f.g.dc_rows[at] = some ? (sum[0] - sum[1] * (sum[2] / sum[3])) * a.unit : 0.f;
+        if (group == 0 && mine) f.g.dc_rows[at] = some ? (sum[0] - sum[1] * (sum[2] / sum[3])) * a.unit : 0.f;
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(x_bar);       // (all have read before anyone writes the next item's dS there)
@@ -602,33 +645,38 @@ struct QTiles {
   }
 };
 
-// 32 queries (columns) of one key (lane): P^T as bf16 pairs, and in place of s what dP - D is multiplied by: P a (1 - tanh^2)
+// 64 queries (columns) of one key (lane): P^T as bf16 pairs, and in place of s what dP - D is multiplied by: P a (1 - tanh^2)
 template <bool CAP, bool SLOPE>
-__device__ __forceinline__ void dkv_probabilities(float slope, int dist, uint32_t rows_at, float (&s)[32], uint32_t (&u)[16]) {
+__device__ __forceinline__ void dkv_probabilities(float slope, int dist, uint32_t rows_at, float (&s)[kChunks][32], uint32_t (&u)[kChunks][16]) {
 #pragma unroll
-  for (int e = 0; e < 32; e += 4) {
-    float l[4], m[4];
-    lds_f4(rows_at + 4 * e, l[0], l[1], l[2], l[3]);
-    lds_f4(rows_at + 4 * (kT + e), m[0], m[1], m[2], m[3]);
+  for (int c = 0; c < kChunks; ++c) {
 #pragma unroll
-    for (int z = 0; z < 4; z += 2) {
-      const uint64_t t = pack2(s[e + z], s[e + z + 1]), m2 = pack2(m[z], m[z + 1]);
-      uint64_t x = t;
-      if (SLOPE)
-        x = pack2(fmaf(-slope, fabsf((float)(dist + e + z)), s[e + z]), fmaf(-slope, fabsf((float)(dist + e + z + 1)), s[e + z + 1]));
-      float p0, p1;
-      unpack2(fma2(x, m2, pack2(l[z], l[z + 1])), p0, p1);
-      p0 = exp2_fast(p0);
-      p1 = exp2_fast(p1);
-      u[(e + z) >> 1] = bf16x2(p0, p1);
-      uint64_t w = mul2(pack2(p0, p1), m2);
-      if (CAP) w = mul2(w, fma2(t, pack2(-s[e + z], -s[e + z + 1]), pack2(1.0f, 1.0f)));
-      unpack2(w, s[e + z], s[e + z + 1]);
+    for (int e = 0; e < 32; e += 4) {
+      float l[4], m[4];
+      lds_f4(rows_at + 4 * (c * 32 + e), l[0], l[1], l[2], l[3]);
+      lds_f4(rows_at + 4 * (kT + c * 32 + e), m[0], m[1], m[2], m[3]);
+#pragma unroll
+      for (int z = 0; z < 4; z += 2) {
+        float& s0 = s[c][e + z];
+        float& s1 = s[c][e + z + 1];
+        const uint64_t t = pack2(s0, s1), m2 = pack2(m[z], m[z + 1]);
+        uint64_t x = t;
+        if (SLOPE)
+          x = pack2(fmaf(-slope, fabsf((float)(dist + c * 32 + e + z)), s0), fmaf(-slope, fabsf((float)(dist + c * 32 + e + z + 1)), s1));
+        float p0, p1;
+        unpack2(fma2(x, m2, pack2(l[z], l[z + 1])), p0, p1);
+        p0 = exp2_fast(p0);
+        p1 = exp2_fast(p1);
+        u[c][(e + z) >> 1] = bf16x2(p0, p1);
+        uint64_t w = mul2(pack2(p0, p1), m2);
+        if (CAP) w = mul2(w, fma2(t, pack2(-s0, -s1), pack2(1.0f, 1.0f)));
+        unpack2(w, s0, s1);
+      }
     }
   }
 }
 
-template <int HD>
+template <int HD, bool CAP, bool SLOPE>
 __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                                                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
                                                                      const __grid_constant__ BwdArgs f) {
@@ -648,7 +696,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
   const uint32_t w_full = bars + 208, w_empty = bars + 224;          // [2]
   const uint32_t r_empty = bars + 240;                               // [2] the rows' terms have been read
   const uint32_t next_bar = bars + 256, drain_bar = bars + 264;
-  const uint32_t tmem_slot = bars + 272, abort_flag = bars + 276, drain_fail = bars + 280;
+  const uint32_t tmem_slot = bars + 280, abort_flag = bars + 284, drain_fail = bars + 288;
   const BwdWork* work = reinterpret_cast<const BwdWork*>(smem_raw + (work_at - smem_u32(smem_raw)));
   constexpr int kS = 0, kDP = kT, kDK = 2 * kT, kDV = 2 * kT + HD;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -656,6 +704,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
   if (threadIdx.x == 0) {
     mbar_init(kv_full, 1);
     mbar_init(kv_empty, 1);
+    mbar_init(drain_bar, 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(q_full + 8 * t, 1);
       mbar_init(q_empty + 8 * t, 1);
@@ -672,7 +721,6 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
     mbar_init(acc_full, 1);
     mbar_init(acc_empty, kWarps);
     mbar_init(next_bar, 1);
-    mbar_init(drain_bar, 1);
     sts_u32(abort_flag, 0u);
     sts_u32(drain_fail, 0u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -685,7 +733,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = lds_u32(tmem_slot);
+  const uint32_t tmem = uniform(lds_u32(tmem_slot));
   const SoftmaxArgs& a = f.a;
   auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
 
@@ -804,12 +852,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
       __syncwarp();
       if (lane == 0) mbar_arrive(w_empty + 8 * slot);
       if (++slot == 2) { slot = 0; wphase ^= 1u; }
-      if (!w.valid) break;
+      if (uniform(w.valid) == 0) break;
       QTiles qt;
       qt.start(f, w.b, w.tile);
       int count = 0;
       for (int t = qt.next(); t >= 0; t = qt.next()) ++count;
-      const int steps = count * a.G;
+      const int steps = uniform(count * a.G);
       if (steps == 0) continue;
       alive = wait_all(kv_full, kvphase);
       if (!alive) break;
@@ -892,7 +940,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
       if (!mbar_drain(drain_bar, 0u)) sts_u32(drain_fail, 1u);
     }
   } else {
-    const int quad = warp & 3, quarter = (warp - 2) >> 2, row = quad * 32 + lane;
+    const int quad = warp & 3, group = (warp - 2) >> 2, row = quad * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
     uint32_t wphase = 0, sphase = 0, dpphase = 0, accphase = 0, idx = 0;
     int slot = 0;
@@ -916,8 +964,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
         for (int t = qt.next(); t >= 0 && alive; t = qt.next(), ++idx) {
           any = true;
           const uint32_t st = idx & 1u;
-          const int i0 = t * kT + quarter * 32;
-          const uint32_t rows_at = rows_smem + st * C::kRowBytes + quarter * 128;
+          const int i0 = t * kT + group * (32 * kChunks);
+          const uint32_t rows_at = rows_smem + st * C::kRowBytes + group * (128 * kChunks);
           bool edge;
           if (a.ranges) {
             const int4 s = qt.spans[t];
@@ -930,35 +978,39 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           if (!alive) break;
           sphase ^= 1u;
           tc_fence_after();
-          float s[32];
-          uint32_t u[16];
-          tmem_ld32(lane_base + kS + quarter * 32, s);
-          tmem_ld_wait();
-          if (a.cap_inv > 0.f) {
-            tanh_scores(a.cap_inv, s);
-            if (slope != 0.f) dkv_probabilities<true, true>(slope, i0 - key, rows_at, s, u);
-            else dkv_probabilities<true, false>(slope, i0 - key, rows_at, s, u);
-          } else {
-            if (slope != 0.f) dkv_probabilities<false, true>(slope, i0 - key, rows_at, s, u);
-            else dkv_probabilities<false, false>(slope, i0 - key, rows_at, s, u);
-          }
-          if (edge) {
-            // lane e knows the range of query i0 + e; bit e: it sees this lane's key
-            const int2 sees = i0 + lane < a.N ? visible_keys(a, b, i0 + lane) : make_int2(0, 0);
-            uint32_t seen = 0u;
-#pragma unroll 4
-            for (int e = 0; e < 32; ++e) {
-              const int from = __shfl_sync(0xffffffffu, sees.x, e), to = __shfl_sync(0xffffffffu, sees.y, e);
-              seen |= (key >= from && key < to ? 1u : 0u) << e;
-            }
+          float s[kChunks][32];
+          uint32_t u[kChunks][16];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const bool on = (seen >> e) & 1u;
-              s[e] = on ? s[e] : 0.f;
-              u[e >> 1] &= on ? 0xffffffffu : (e & 1) ? 0x0000ffffu : 0xffff0000u;
+          for (int c = 0; c < kChunks; ++c) tmem_ld32(lane_base + kS + group * (32 * kChunks) + c * 32, s[c]);
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) tmem_ld_wait32(s[c]);
+          if (CAP) {
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) tanh_scores(a.cap_inv, s[c]);
+          }
+          dkv_probabilities<CAP, SLOPE>(slope, i0 - key, rows_at, s, u);
+          if (edge) {
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+              // lane e knows the range of query i0 + 32 c + e; bit e: it sees this lane's key
+              const int i = i0 + c * 32 + lane;
+              const int2 sees = i < a.N ? visible_keys(a, b, i) : make_int2(0, 0);
+              uint32_t seen = 0u;
+#pragma unroll 4
+              for (int e = 0; e < 32; ++e) {
+                const int from = __shfl_sync(0xffffffffu, sees.x, e), to = __shfl_sync(0xffffffffu, sees.y, e);
+                seen |= (key >= from && key < to ? 1u : 0u) << e;
+              }
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                const bool on = (seen >> e) & 1u;
+                s[c][e] = on ? s[c][e] : 0.f;
+                u[c][e >> 1] &= on ? 0xffffffffu : (e & 1) ? 0x0000ffffu : 0xffff0000u;
+              }
             }
           }
-          tmem_st16(lane_base + kS + quarter * 32, u);
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) tmem_st16(lane_base + kS + group * (32 * kChunks) + c * 32, u[c]);
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
@@ -967,26 +1019,28 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           if (!alive) break;
           dpphase ^= 1u;
           tc_fence_after();
+          float dp[kChunks][32];
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float dp[16];
-            tmem_ld16(lane_base + kDP + quarter * 32 + c * 16, dp);
-            tmem_ld_wait();
+          for (int c = 0; c < kChunks; ++c) tmem_ld32(lane_base + kDP + group * (32 * kChunks) + c * 32, dp[c]);
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
+          for (int c = 0; c < kChunks; ++c) tmem_ld_wait32(dp[c]);
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
               float d[4];
-              lds_f4(rows_at + 4 * (2 * kT + c * 16 + e), d[0], d[1], d[2], d[3]);
+              lds_f4(rows_at + 4 * (2 * kT + c * 32 + e), d[0], d[1], d[2], d[3]);
 #pragma unroll
               for (int z = 0; z < 4; z += 2) {
                 float x, y;
-                unpack2(mul2(pack2(s[c * 16 + e + z], s[c * 16 + e + z + 1]), add2(pack2(dp[e + z], dp[e + z + 1]), pack2(d[z], d[z + 1]))), x, y);
-                u[c * 8 + ((e + z) >> 1)] = bf16x2(x, y);
+                unpack2(mul2(pack2(s[c][e + z], s[c][e + z + 1]), add2(pack2(dp[c][e + z], dp[c][e + z + 1]), pack2(d[z], d[z + 1]))), x, y);
+                u[c][(e + z) >> 1] = bf16x2(x, y);
               }
             }
+            tmem_st16(lane_base + kDP + group * (32 * kChunks) + c * 32, u[c]);
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(r_empty + 8 * st);
-          tmem_st16(lane_base + kDP + quarter * 32, u);
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
@@ -1000,12 +1054,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
         accphase ^= 1u;
         tc_fence_after();
       }
-      if (quarter < HD / 32) {
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
+      for (int which = 0; which < 2; ++which) {
+        for (int c = group; c < HD / 32; c += kGroups) {
+          const int col = c * 32;
           float v[32];
           if (any) {
-            tmem_ld32(lane_base + (which ? kDV : kDK) + quarter * 32, v);
+            tmem_ld32(lane_base + (which ? kDV : kDK) + col, v);
             tmem_ld_wait();
           } else {
 #pragma unroll
@@ -1013,7 +1068,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           }
           if (mine) {
             const entmax_attn_strides& s = which ? f.g.dv : f.g.dk;
-            __nv_bfloat16* out = (which ? f.dv : f.dk) + (long long)b * s.b + (long long)kh * s.h + (long long)key * s.n + quarter * 32;
+            __nv_bfloat16* out = (which ? f.dv : f.dk) + (long long)b * s.b + (long long)kh * s.h + (long long)key * s.n + col;
             const float mul = which ? 1.0f : kLn2 * a.sm_scale / a.unit;   // (the rows' a is c unit log2 e)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -1042,14 +1097,32 @@ cudaError_t bwd_launch(const BwdArgs& f, const void* q, const void* k, const voi
   if (err == cudaSuccess) err = make_tile_map(&map_k, k, a.D, a.N, a.KH, a.B, a.k.n, a.k.h, a.k.b);
   if (err == cudaSuccess) err = make_tile_map(&map_v, v, a.D, a.N, a.KH, a.B, a.v.n, a.v.h, a.v.b);
   if (err == cudaSuccess) err = make_tile_map(&map_do, d_o, a.D, a.N, a.H, a.B, f.g.d_o.n, f.g.d_o.h, f.g.d_o.b);
-  if (err == cudaSuccess) err = cudaFuncSetAttribute(softmax_dq_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdCfg<HD>::kSmemQ);
-  if (err == cudaSuccess) err = cudaFuncSetAttribute(softmax_dkv_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdCfg<HD>::kSmemKV);
   if (err != cudaSuccess) return err;
-  err = launch_kernel(softmax_dq_kernel<HD>, (unsigned)((long long)a.B * a.H * f.tiles), kBwdThreads, BwdCfg<HD>::kSmemQ, stream, map_q, map_k, map_v,
-                      map_do, f);
-  if (err != cudaSuccess) return err;
-  return launch_kernel(softmax_dkv_kernel<HD>, (unsigned)((long long)a.B * a.KH * f.tiles), kBwdThreads, BwdCfg<HD>::kSmemKV, stream, map_q, map_k, map_v,
-                       map_do, f);
+  auto dq = [&](auto kernel) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdCfg<HD>::kSmemQ);
+    return e != cudaSuccess ? e : launch_kernel(kernel, (unsigned)((long long)a.B * a.H * f.tiles), kDqThreads, BwdCfg<HD>::kSmemQ, stream, map_q, map_k, map_v,
+                                                map_do, f);
+  };
+  auto dkv = [&](auto kernel) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdCfg<HD>::kSmemKV);
+    return e != cudaSuccess ? e : launch_kernel(kernel, (unsigned)((long long)a.B * a.KH * f.tiles), kBwdThreads, BwdCfg<HD>::kSmemKV, stream, map_q, map_k, map_v,
+                                                map_do, f);
+  };
+  const bool dc = f.g.dc_rows != nullptr;
+  if (a.cap_inv > 0.f) {
+    if (a.alibi) {
+      err = dc ? dq(softmax_dq_kernel<HD, true, true, true>) : dq(softmax_dq_kernel<HD, true, true, false>);
+      return err != cudaSuccess ? err : dkv(softmax_dkv_kernel<HD, true, true>);
+    }
+    err = dc ? dq(softmax_dq_kernel<HD, true, false, true>) : dq(softmax_dq_kernel<HD, true, false, false>);
+    return err != cudaSuccess ? err : dkv(softmax_dkv_kernel<HD, true, false>);
+  }
+  if (a.alibi) {
+    err = dc ? dq(softmax_dq_kernel<HD, false, true, true>) : dq(softmax_dq_kernel<HD, false, true, false>);
+    return err != cudaSuccess ? err : dkv(softmax_dkv_kernel<HD, false, true>);
+  }
+  err = dc ? dq(softmax_dq_kernel<HD, false, false, true>) : dq(softmax_dq_kernel<HD, false, false, false>);
+  return err != cudaSuccess ? err : dkv(softmax_dkv_kernel<HD, false, false>);
 }
 
 }  // namespace

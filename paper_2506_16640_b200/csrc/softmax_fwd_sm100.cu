@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = lds_u32(tmem_slot);
+  const uint32_t tmem = uniform(lds_u32(tmem_slot));
   const SoftmaxArgs& a = f.a;
   auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
 
@@ -386,7 +386,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
     while (alive) {
       alive = wait_all(w_full + 8 * slot, wphase);
       if (!alive) break;
-      const Work w = work[slot];
+      Work w;
+      w.valid = uniform(work[slot].valid);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        w.lo[t] = uniform(work[slot].lo[t]);
+        w.hi[t] = uniform(work[slot].hi[t]);
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(w_empty + 8 * slot);
       if (++slot == 2) { slot = 0; wphase ^= 1u; }
@@ -507,7 +513,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
         }
       }
       RowSoftmax<CAP, TERMS> sm;
-      sm.start(scale * a.unit * kLog2e, a.alibi ? a.alibi[h] / a.unit : 0.f, pos);
+      sm.start(mine, scale * a.unit * kLog2e, a.alibi ? a.alibi[h] / a.unit : 0.f, pos);
       for (int j = hi - 1; j >= lo && alive; --j) {
         alive = wait_all(s_full + 8 * t, sphase);
         if (!alive) break;

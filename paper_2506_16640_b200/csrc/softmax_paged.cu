@@ -289,7 +289,18 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
             mma16816(s[e + 1], q[kk], b2, b3);
           }
         }
-        if (a.cap_inv > 0.f) tanh_scores(a.cap_inv, reinterpret_cast<float (&)[4 * NT]>(s));
+        if (a.cap_inv > 0.f) {
+          if (edge) {                            // (what lies in an unseen slot has no say in how the tanh is computed)
+#pragma unroll
+            for (int e = 0; e < NT; ++e)
+#pragma unroll
+              for (int z = 0; z < 4; ++z) {
+                const int key = k0 + 8 * e + 2 * (lane & 3) + (z & 1);
+                s[e][z] = key >= begin[z >> 1] && key <= pos[z >> 1] ? s[e][z] : 0.f;
+              }
+          }
+          tanh_scores(a.cap_inv, reinterpret_cast<float (&)[4 * NT]>(s));
+        }
         float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int e = 0; e < NT; ++e) {

@@ -10,15 +10,20 @@ namespace entmax {
 // swizzle: atoms of eight rows repeat every 1024 bytes, 64-element blocks every 128 * 128 bytes.
 __device__ __forceinline__ uint32_t mn_desc_lo(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | ((uint32_t)((128 * 128) >> 4) << 16); }
 
+// A value that all lanes have, as one the compiler knows to be the same in all of them: descriptors and loop bounds then stay in uniform registers
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 // tanh of N values times inv, in place (the whole warp).  Scores are mostly far below the cap: where the warp has none beyond half of it, an odd polynomial of
 // degree 9 (least maximum error on [-1/2, 1/2], 3.5e-8, fitted by iterated weighted least squares), two values an instruction; otherwise exp2 and a reciprocal.
+// counts: whether this thread's values are anyone's (others have no say in which it is).
 template <int N>
-__device__ __forceinline__ void tanh_scores(float inv, float (&s)[N]) {
+__device__ __forceinline__ void tanh_scores(float inv, float (&s)[N], bool counts = true) {
   using namespace sm100;
   float most = fabsf(s[0]);
 #pragma unroll
   for (int e = 1; e < N; ++e) most = fmaxf(most, fabsf(s[e]));
-  if (__all_sync(0xffffffffu, most * inv <= 0.5f)) {
+  if (__all_sync(0xffffffffu, !counts || most * inv <= 0.5f)) {
     const uint64_t inv2 = pack2(inv, inv);
 #pragma unroll
     for (int e = 0; e < N; e += 2) {
@@ -51,7 +56,9 @@ struct RowSoftmax {
   float a, m, slope, sign, minus_am;
   float l0, l1;             // the sum, in two halves
   int pos;
-  __device__ __forceinline__ void start(float a_signed, float slope_unit, int position) {
+  bool mine;                // a row of the problem
+  __device__ __forceinline__ void start(bool is_row, float a_signed, float slope_unit, int position) {
+    mine = is_row;
     sign = a_signed < 0.f ? -1.0f : 1.0f;
     a = fmaxf(fabsf(a_signed), 1e-30f);      // c = 0: every visible key weighs the same, while 0 * -inf would be NaN
     slope = slope_unit;
@@ -63,9 +70,16 @@ struct RowSoftmax {
   // Accumulators to scores (in place), masked ones to -inf; returns the factor that O has to be multiplied by (1 mostly)
   __device__ __forceinline__ float take(float cap_inv, float (&s)[4][32], int k0, int2 sees, bool edge) {
     using namespace sm100;
+    const int from = sees.x - k0, to = sees.y - k0;
     if (CAP) {
+      if (edge) {                            // (what a masked score happens to be has no say in how the tanh is computed)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) tanh_scores(cap_inv, s[c]);
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s[c][e] = c * 32 + e >= from && c * 32 + e < to ? s[c][e] : 0.f;
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tanh_scores(cap_inv, s[c], mine);
     }
     if (TERMS) {
       if (slope != 0.f) {
@@ -79,7 +93,6 @@ struct RowSoftmax {
         for (int e = 0; e < 32; e += 2) unpack2(mul2(pack2(s[c][e], s[c][e + 1]), g), s[c][e], s[c][e + 1]);
     }
     if (edge) {
-      const int from = sees.x - k0, to = sees.y - k0;
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll

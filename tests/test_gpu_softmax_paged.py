@@ -227,6 +227,25 @@ def test_many_repeats_over_slots_that_hold_anything(new, lens, H, KH, d, page, k
         assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
 
 
+@pytest.mark.parametrize("n", [1, 4, 140])
+def test_a_sequence_does_not_depend_on_what_is_packed_around_it(n):
+    # the same sequence alone, and with a neighbour of huge queries: bit for bit
+    t = _terms("cap+slopes", 4)
+    pr = _problem([n, 130], [n + 300, 200], 4, 2, 128, 16, seed=41)
+    pr["q"][n:] *= 100.0
+    both = _run(pr, t)
+    alone = dict(pr, q=pr["q"][:n].contiguous(), cu=pr["cu"][:2].contiguous(), lens=pr["lens"][:1].contiguous(), table=pr["table"][:1].contiguous())
+    # (the bounds of the larger call, which the launches go by)
+    one = _run(alone, t, max_q_len=n, max_kv_len=0)
+    two = _run(pr, t, max_q_len=max(n, 130), max_kv_len=0)
+    assert torch.equal(both[0], two[0])
+    assert (one[0].float() - two[0][:n].float()).abs().max() <= 2.0 ** -7 * two[0][:n].float().abs().max()
+    small = dict(pr, q=pr["q"].clone())
+    small["q"][n:] *= 0.001
+    three = _run(small, t)
+    assert torch.equal(three[0][:n], both[0][:n]) and torch.equal(three[1][:n], both[1][:n])
+
+
 def test_writes_nothing_outside_its_outputs():
     for new, lens in (([1, 1], [700, 64]), ([140, 3], [400, 50])):
         pr = _problem(new, lens, 6, 2, 64, 16, seed=8)
