@@ -18,6 +18,8 @@
 // second one).  Every wait is bounded.
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "sm100_ptx.cuh"
 #include "softmax.cuh"
 #include "softmax_tile.cuh"
@@ -646,15 +648,15 @@ struct QTiles {
 };
 
 // 64 queries (columns) of one key (lane): P^T as bf16 pairs, and in place of s what dP - D is multiplied by: P a (1 - tanh^2)
-template <bool CAP, bool SLOPE>
-__device__ __forceinline__ void dkv_probabilities(float slope, int dist, uint32_t rows_at, float (&s)[kChunks][32], uint32_t (&u)[kChunks][16]) {
+template <bool CAP, bool SLOPE, bool SCALED>
+__device__ __forceinline__ void dkv_probabilities(float scale, float slope, int dist, uint32_t rows_at, float (&s)[kChunks][32], uint32_t (&u)[kChunks][16]) {
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
 #pragma unroll
     for (int e = 0; e < 32; e += 4) {
-      float l[4], m[4];
+      float l[4], m[4] = {scale, scale, scale, scale};
       lds_f4(rows_at + 4 * (c * 32 + e), l[0], l[1], l[2], l[3]);
-      lds_f4(rows_at + 4 * (kT + c * 32 + e), m[0], m[1], m[2], m[3]);
+      if (SCALED) lds_f4(rows_at + 4 * (kT + c * 32 + e), m[0], m[1], m[2], m[3]);   // (four wavefronts, though all lanes want the same)
 #pragma unroll
       for (int z = 0; z < 4; z += 2) {
         float& s0 = s[c][e + z];
@@ -676,7 +678,7 @@ __device__ __forceinline__ void dkv_probabilities(float slope, int dist, uint32_
   }
 }
 
-template <int HD, bool CAP, bool SLOPE>
+template <int HD, bool CAP, bool SLOPE, bool SCALED>
 __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                                                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
                                                                      const __grid_constant__ BwdArgs f) {
@@ -988,7 +990,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) tanh_scores(a.cap_inv, s[c]);
           }
-          dkv_probabilities<CAP, SLOPE>(slope, i0 - key, rows_at, s, u);
+          dkv_probabilities<CAP, SLOPE, SCALED>(a.unit * kLog2e, slope, i0 - key, rows_at, s, u);
           if (edge) {
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
@@ -1108,21 +1110,16 @@ cudaError_t bwd_launch(const BwdArgs& f, const void* q, const void* k, const voi
     return e != cudaSuccess ? e : launch_kernel(kernel, (unsigned)((long long)a.B * a.KH * f.tiles), kBwdThreads, BwdCfg<HD>::kSmemKV, stream, map_q, map_k, map_v,
                                                 map_do, f);
   };
-  const bool dc = f.g.dc_rows != nullptr;
-  if (a.cap_inv > 0.f) {
-    if (a.alibi) {
-      err = dc ? dq(softmax_dq_kernel<HD, true, true, true>) : dq(softmax_dq_kernel<HD, true, true, false>);
-      return err != cudaSuccess ? err : dkv(softmax_dkv_kernel<HD, true, true>);
-    }
-    err = dc ? dq(softmax_dq_kernel<HD, true, false, true>) : dq(softmax_dq_kernel<HD, true, false, false>);
-    return err != cudaSuccess ? err : dkv(softmax_dkv_kernel<HD, true, false>);
-  }
-  if (a.alibi) {
-    err = dc ? dq(softmax_dq_kernel<HD, false, true, true>) : dq(softmax_dq_kernel<HD, false, true, false>);
-    return err != cudaSuccess ? err : dkv(softmax_dkv_kernel<HD, false, true>);
-  }
-  err = dc ? dq(softmax_dq_kernel<HD, false, false, true>) : dq(softmax_dq_kernel<HD, false, false, false>);
-  return err != cudaSuccess ? err : dkv(softmax_dkv_kernel<HD, false, false>);
+  auto both = [&](auto cap, auto slope) {
+    constexpr bool kCap = decltype(cap)::value, kSlope = decltype(slope)::value;
+    cudaError_t e = f.g.dc_rows ? dq(softmax_dq_kernel<HD, kCap, kSlope, true>) : dq(softmax_dq_kernel<HD, kCap, kSlope, false>);
+    if (e != cudaSuccess) return e;
+    return a.beta || a.c_rows ? dkv(softmax_dkv_kernel<HD, kCap, kSlope, true>) : dkv(softmax_dkv_kernel<HD, kCap, kSlope, false>);
+  };
+  using T = std::true_type;
+  using F = std::false_type;
+  if (a.cap_inv > 0.f) return a.alibi ? both(T{}, T{}) : both(T{}, F{});
+  return a.alibi ? both(F{}, T{}) : both(F{}, F{});
 }
 
 }  // namespace

@@ -512,7 +512,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
           if ((a.beta || a.c_rows) && f.status && !isfinite(scale)) atomicOr(f.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_SCALE);
         }
       }
-      RowSoftmax<CAP, TERMS> sm;
+      RowSoftmax<CAP, TERMS, PAGED> sm;
       sm.start(mine, scale * a.unit * kLog2e, a.alibi ? a.alibi[h] / a.unit : 0.f, pos);
       for (int j = hi - 1; j >= lo && alive; --j) {
         alive = wait_all(s_full + 8 * t, sphase);

@@ -50,8 +50,8 @@ __device__ __forceinline__ void slope_scores(float slope, int pos, int j0, float
 // Running softmax of one row, a tile of 128 scores at a time.  The scores are x = x_ij in units of the accumulator, or of the cap where there is one (CAP: then the
 // accumulator's tanh is x), with the sign of c folded in (TERMS: calls with scales or slopes); |a| x are the base-2 exponents.  m is what the probabilities are
 // measured from: the maximum, or up to 8 / |a| below it.  CAP and TERMS are known at compile time: branches over code that a call does not need
-// would cut the loop's schedule into pieces (plain calls lost a fifth).
-template <bool CAP, bool TERMS>
+// would cut the loop's schedule into pieces (plain calls lost a fifth).  UNSEEN: masked keys may be anything, not only data of the call.
+template <bool CAP, bool TERMS, bool UNSEEN>
 struct RowSoftmax {
   float a, m, slope, sign, minus_am;
   float l0, l1;             // the sum, in two halves
@@ -72,7 +72,7 @@ struct RowSoftmax {
     using namespace sm100;
     const int from = sees.x - k0, to = sees.y - k0;
     if (CAP) {
-      if (edge) {                            // (what a masked score happens to be has no say in how the tanh is computed)
+      if (UNSEEN && edge) {                  // (what a masked score happens to be has no say in how the tanh is computed)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
