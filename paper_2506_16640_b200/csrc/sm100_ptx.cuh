@@ -267,6 +267,27 @@ __device__ __forceinline__ void tmem_ld_wait64(float (&r)[64]) {
                :
                : "memory");
 }
+// 16 lanes x 32 fp32 columns in the layout of an m16n8 product's accumulators: of the columns 8 k .. 8 k + 7, thread t gets in r[4 k] and r[4 k + 1] the
+// columns 2 (t % 4) and the next of lane t / 4, in r[4 k + 2] and r[4 k + 3] those of lane t / 4 + 8
+__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
+        "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(taddr)
+      : "memory");
+}
+// 16 lanes x 16 columns of 32 bits, what such a fragment leaves as bf16 pairs: of the columns 4 k .. 4 k + 3, thread t has column t % 4 of lane t / 4 in u[2 k] and of
+// lane t / 4 + 8 in u[2 k + 1]
+__device__ __forceinline__ void tmem_st_frag(uint32_t taddr, const uint32_t* u) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(u[0]), "r"(u[1]), "r"(u[2]),
+               "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+               : "memory");
+}
+__device__ __forceinline__ void lds_f2(uint32_t addr, float& x, float& y) {
+  asm volatile("ld.shared::cta.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(addr) : "memory");
+}
 __device__ __forceinline__ void tmem_ld_wait32(float (&r)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
                : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),

@@ -10,7 +10,7 @@
 //                       from the O that was rounded to bf16, which is good enough for dS (an error of 2^-9 of D times p) but not for a float32 result.
 //   softmax_dkv_kernel  an item is a K/V tile; over all query heads that share it and all Q tiles that see it: S^T = K Q^T and dP^T = V dO^T with the keys
 //                       along the lanes, so that P^T and dS^T are, over their own columns, the A operands of dV += P^T dO and dK += dS^T Q; what
-//                       depends on the query comes from shared memory, four columns a load.
+//                       depends on the query comes from shared memory.
 //
 // CTA of both: warp 0 scheduler and TMA producer, warp 1 MMA issuer, warps 2..17 four threads per TMEM lane (32 columns each).  The dQ kernel has a second
 // issuer, warp 18, for dQ alone: an issuer is held up by the products it issues, and a wait that is over at once still takes 100 cycles, of which a step has
@@ -647,33 +647,34 @@ struct QTiles {
   }
 };
 
-// 64 queries (columns) of one key (lane): P^T as bf16 pairs, and in place of s what dP - D is multiplied by: P a (1 - tanh^2)
+// The transposed scores of 32 queries (columns) and 32 keys (lanes) in the layout of tmem_ld_frag, lanes 0 .. 15 in s[0 .. 15], 16 .. 31 behind them: a thread has four keys
+// and eight queries, for which it reads shared memory once (a thread of the plain layout has one key and 32 queries; with four wavefronts to a load that all
+// lanes share, those loads took as much of the shared memory's time as the products' operands).
+// s: P^T as bf16 pairs goes to u, and in place of s what dP - D is multiplied by, P a (1 - tanh^2).  dist: first query - first key of the thread
 template <bool CAP, bool SLOPE, bool SCALED>
-__device__ __forceinline__ void dkv_probabilities(float scale, float slope, int dist, uint32_t rows_at, float (&s)[kChunks][32], uint32_t (&u)[kChunks][16]) {
+__device__ __forceinline__ void dkv_probabilities(float scale, float slope, int dist, uint32_t rows_at, float (&s)[32], uint32_t (&u)[16]) {
 #pragma unroll
-  for (int c = 0; c < kChunks; ++c) {
+  for (int k = 0; k < 4; ++k) {
+    float l0, l1, m0 = scale, m1 = scale;
+    lds_f2(rows_at + 32 * k, l0, l1);
+    if (SCALED) lds_f2(rows_at + 4 * kT + 32 * k, m0, m1);
+    const uint64_t l2 = pack2(l0, l1), m2 = pack2(m0, m1);
 #pragma unroll
-    for (int e = 0; e < 32; e += 4) {
-      float l[4], m[4] = {scale, scale, scale, scale};
-      lds_f4(rows_at + 4 * (c * 32 + e), l[0], l[1], l[2], l[3]);
-      if (SCALED) lds_f4(rows_at + 4 * (kT + c * 32 + e), m[0], m[1], m[2], m[3]);   // (four wavefronts, though all lanes want the same)
-#pragma unroll
-      for (int z = 0; z < 4; z += 2) {
-        float& s0 = s[c][e + z];
-        float& s1 = s[c][e + z + 1];
-        const uint64_t t = pack2(s0, s1), m2 = pack2(m[z], m[z + 1]);
-        uint64_t x = t;
-        if (SLOPE)
-          x = pack2(fmaf(-slope, fabsf((float)(dist + c * 32 + e + z)), s0), fmaf(-slope, fabsf((float)(dist + c * 32 + e + z + 1)), s1));
-        float p0, p1;
-        unpack2(fma2(x, m2, pack2(l[z], l[z + 1])), p0, p1);
-        p0 = exp2_fast(p0);
-        p1 = exp2_fast(p1);
-        u[c][(e + z) >> 1] = bf16x2(p0, p1);
-        uint64_t w = mul2(pack2(p0, p1), m2);
-        if (CAP) w = mul2(w, fma2(t, pack2(-s0, -s1), pack2(1.0f, 1.0f)));
-        unpack2(w, s0, s1);
-      }
+    for (int y = 0; y < 4; ++y) {                // keys 0, 8, 16, 24 behind the thread's first
+      const int at = (y >> 1) * 16 + 4 * k + (y & 1) * 2;
+      float& s0 = s[at];
+      float& s1 = s[at + 1];
+      const uint64_t t = pack2(s0, s1);
+      uint64_t x = t;
+      if (SLOPE) x = pack2(fmaf(-slope, fabsf((float)(dist + 8 * k - 8 * y)), s0), fmaf(-slope, fabsf((float)(dist + 8 * k - 8 * y + 1)), s1));
+      float p0, p1;
+      unpack2(fma2(x, m2, l2), p0, p1);
+      p0 = exp2_fast(p0);
+      p1 = exp2_fast(p1);
+      u[(y >> 1) * 8 + 2 * k + (y & 1)] = bf16x2(p0, p1);
+      uint64_t w = mul2(pack2(p0, p1), m2);
+      if (CAP) w = mul2(w, fma2(t, pack2(-s0, -s1), pack2(1.0f, 1.0f)));
+      unpack2(w, s0, s1);
     }
   }
 }
@@ -966,8 +967,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
         for (int t = qt.next(); t >= 0 && alive; t = qt.next(), ++idx) {
           any = true;
           const uint32_t st = idx & 1u;
-          const int i0 = t * kT + group * (32 * kChunks);
-          const uint32_t rows_at = rows_smem + st * C::kRowBytes + group * (128 * kChunks);
+          const int i0 = t * kT + group * 32 + 2 * (lane & 3);        // this thread's first query and first key
+          const int key0 = kt * kT + quad * 32 + (lane >> 2);
+          const uint32_t rows_at = rows_smem + st * C::kRowBytes + 4 * (group * 32 + 2 * (lane & 3));
           bool edge;
           if (a.ranges) {
             const int4 s = qt.spans[t];
@@ -980,39 +982,32 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           if (!alive) break;
           sphase ^= 1u;
           tc_fence_after();
-          float s[kChunks][32];
-          uint32_t u[kChunks][16];
-#pragma unroll
-          for (int c = 0; c < kChunks; ++c) tmem_ld32(lane_base + kS + group * (32 * kChunks) + c * 32, s[c]);
-#pragma unroll
-          for (int c = 0; c < kChunks; ++c) tmem_ld_wait32(s[c]);
-          if (CAP) {
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c) tanh_scores(a.cap_inv, s[c]);
-          }
-          dkv_probabilities<CAP, SLOPE, SCALED>(a.unit * kLog2e, slope, i0 - key, rows_at, s, u);
+          const uint32_t s_at = lane_base + kS + group * 32, dp_at = lane_base + kDP + group * 32;
+          constexpr uint32_t kLanes16 = 16u << 16;
+          float s[32];
+          uint32_t u[16];
+          tmem_ld_frag(s_at, s);
+          tmem_ld_frag(s_at + kLanes16, s + 16);
+          tmem_ld_wait32(s);
+          if (CAP) tanh_scores(a.cap_inv, s);
+          dkv_probabilities<CAP, SLOPE, SCALED>(a.unit * kLog2e, slope, i0 - key0, rows_at, s, u);
           if (edge) {
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-              // lane e knows the range of query i0 + 32 c + e; bit e: it sees this lane's key
-              const int i = i0 + c * 32 + lane;
+            for (int e = 0; e < 8; ++e) {
+              const int i = i0 + 8 * (e >> 1) + (e & 1);
               const int2 sees = i < a.N ? visible_keys(a, b, i) : make_int2(0, 0);
-              uint32_t seen = 0u;
-#pragma unroll 4
-              for (int e = 0; e < 32; ++e) {
-                const int from = __shfl_sync(0xffffffffu, sees.x, e), to = __shfl_sync(0xffffffffu, sees.y, e);
-                seen |= (key >= from && key < to ? 1u : 0u) << e;
-              }
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                const bool on = (seen >> e) & 1u;
-                s[c][e] = on ? s[c][e] : 0.f;
-                u[c][e >> 1] &= on ? 0xffffffffu : (e & 1) ? 0x0000ffffu : 0xffff0000u;
+              for (int y = 0; y < 4; ++y) {
+                const bool on = key0 + 8 * y >= sees.x && key0 + 8 * y < sees.y;
+                float& w = s[(y >> 1) * 16 + 4 * (e >> 1) + (y & 1) * 2 + (e & 1)];
+                w = on ? w : 0.f;
+                u[(y >> 1) * 8 + 2 * (e >> 1) + (y & 1)] &= on ? 0xffffffffu : (e & 1) ? 0x0000ffffu : 0xffff0000u;
               }
             }
           }
-#pragma unroll
-          for (int c = 0; c < kChunks; ++c) tmem_st16(lane_base + kS + group * (32 * kChunks) + c * 32, u[c]);
+          // (both halves' scores have been read by the warp: the operands go over them, the lanes' 16 columns at the front of their 32)
+          tmem_st_frag(s_at, u);
+          tmem_st_frag(s_at + kLanes16, u + 8);
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
@@ -1021,26 +1016,26 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           if (!alive) break;
           dpphase ^= 1u;
           tc_fence_after();
-          float dp[kChunks][32];
+          float dp[32];
+          tmem_ld_frag(dp_at, dp);
+          tmem_ld_frag(dp_at + kLanes16, dp + 16);
+          float d[8];
 #pragma unroll
-          for (int c = 0; c < kChunks; ++c) tmem_ld32(lane_base + kDP + group * (32 * kChunks) + c * 32, dp[c]);
+          for (int k = 0; k < 4; ++k) lds_f2(rows_at + 4 * (2 * kT) + 32 * k, d[2 * k], d[2 * k + 1]);
+          tmem_ld_wait32(dp);
 #pragma unroll
-          for (int c = 0; c < kChunks; ++c) tmem_ld_wait32(dp[c]);
+          for (int k = 0; k < 4; ++k) {
+            const uint64_t d2 = pack2(d[2 * k], d[2 * k + 1]);
 #pragma unroll
-          for (int c = 0; c < kChunks; ++c) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              float d[4];
-              lds_f4(rows_at + 4 * (2 * kT + c * 32 + e), d[0], d[1], d[2], d[3]);
-#pragma unroll
-              for (int z = 0; z < 4; z += 2) {
-                float x, y;
-                unpack2(mul2(pack2(s[c][e + z], s[c][e + z + 1]), add2(pack2(dp[c][e + z], dp[c][e + z + 1]), pack2(d[z], d[z + 1]))), x, y);
-                u[c][(e + z) >> 1] = bf16x2(x, y);
-              }
+            for (int y = 0; y < 4; ++y) {
+              const int at = (y >> 1) * 16 + 4 * k + (y & 1) * 2;
+              float x0, x1;
+              unpack2(mul2(pack2(s[at], s[at + 1]), add2(pack2(dp[at], dp[at + 1]), d2)), x0, x1);
+              u[(y >> 1) * 8 + 2 * k + (y & 1)] = bf16x2(x0, x1);
             }
-            tmem_st16(lane_base + kDP + group * (32 * kChunks) + c * 32, u[c]);
           }
+          tmem_st_frag(dp_at, u);
+          tmem_st_frag(dp_at + kLanes16, u + 8);
           __syncwarp();
           if (lane == 0) mbar_arrive(r_empty + 8 * st);
           tmem_st_wait();
