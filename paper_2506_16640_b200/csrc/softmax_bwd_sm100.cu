@@ -32,8 +32,7 @@ using namespace sm100;
 
 constexpr int kT = 128;
 constexpr int kWarps = 16;                       // element code
-constexpr int kGroups = kWarps / 4;              // threads per TMEM lane
-constexpr int kChunks = 4 / kGroups;             // times 32 columns each
+constexpr int kGroups = kWarps / 4;              // threads per TMEM lane, 32 columns each
 constexpr int kBwdThreads = (2 + kWarps) * 32;
 constexpr int kDqThreads = (3 + kWarps) * 32, kSecond = 2 + kWarps;   // dQ: with a second MMA issuer, that warp
 constexpr int kBwdBars = 1536;
@@ -50,7 +49,9 @@ struct BwdCfg {
 };
 
 struct BwdWork {
-  int valid, b, h, tile, lo, hi, pad[2];
+  int valid, b, h, tile, lo, hi;
+  int some_short;               // dQ: some row sees keys of the last K/V tile alone
+  int pad;
 };
 
 struct BwdArgs {
@@ -127,42 +128,39 @@ struct RowTerms {
   int i;
 };
 
-// 64 columns from key j0 on (s: their accumulators, or the tanh of capped ones): dS as bf16 pairs; dc: {sum p dP x, sum p dP, sum p x, sum p} where wanted, the even
+// 32 columns from key j0 on (s: their accumulators, or the tanh of capped ones): dS as bf16 pairs; dc: {sum p dP x, sum p dP, sum p x, sum p} where wanted, the even
 // and the odd columns' apart
 template <bool CAP, bool SLOPE, bool DC, bool EDGE>
-__device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const float (&s)[kChunks][32], const float (&dp)[kChunks][32], uint32_t (&ds)[kChunks][16],
+__device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const float (&s)[32], const float (&dp)[32], uint32_t (&ds)[16],
                                             uint64_t (&dc)[4]) {
   const uint64_t a2 = pack2(r.a, r.a), l2 = pack2(-r.lse2, -r.lse2), d2 = pack2(-r.dot, -r.dot);
 #pragma unroll
-  for (int c = 0; c < kChunks; ++c) {
-#pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-      const int j = j0 + c * 32 + e;
-      const uint64_t t = pack2(s[c][e], s[c][e + 1]);
-      uint64_t x = t;
-      if (SLOPE) x = pack2(fmaf(-r.slope, fabsf((float)(j - r.i)), s[c][e]), fmaf(-r.slope, fabsf((float)(j + 1 - r.i)), s[c][e + 1]));
-      float p0, p1;
-      unpack2(fma2(x, a2, l2), p0, p1);
-      p0 = exp2_fast(p0);
-      p1 = exp2_fast(p1);
-      if (EDGE) {
-        p0 = j >= r.sees.x && j < r.sees.y ? p0 : 0.f;
-        p1 = j + 1 >= r.sees.x && j + 1 < r.sees.y ? p1 : 0.f;
-      }
-      const uint64_t p = pack2(p0, p1), v = pack2(dp[c][e], dp[c][e + 1]);
-      uint64_t d = mul2(p, add2(v, d2));
-      if (CAP) d = mul2(d, fma2(t, pack2(-s[c][e], -s[c][e + 1]), pack2(1.0f, 1.0f)));
-      if (DC) {
-        const uint64_t u = mul2(p, v);
-        dc[0] = fma2(u, x, dc[0]);
-        dc[1] = add2(u, dc[1]);
-        dc[2] = fma2(p, x, dc[2]);
-        dc[3] = add2(p, dc[3]);
-      }
-      float d0, d1;
-      unpack2(d, d0, d1);
-      ds[c][e >> 1] = bf16x2(d0, d1);
+  for (int e = 0; e < 32; e += 2) {
+    const int j = j0 + e;
+    const uint64_t t = pack2(s[e], s[e + 1]);
+    uint64_t x = t;
+    if (SLOPE) x = pack2(fmaf(-r.slope, fabsf((float)(j - r.i)), s[e]), fmaf(-r.slope, fabsf((float)(j + 1 - r.i)), s[e + 1]));
+    float p0, p1;
+    unpack2(fma2(x, a2, l2), p0, p1);
+    p0 = exp2_fast(p0);
+    p1 = exp2_fast(p1);
+    if (EDGE) {
+      p0 = j >= r.sees.x && j < r.sees.y ? p0 : 0.f;
+      p1 = j + 1 >= r.sees.x && j + 1 < r.sees.y ? p1 : 0.f;
     }
+    const uint64_t p = pack2(p0, p1), v = pack2(dp[e], dp[e + 1]);
+    uint64_t d = mul2(p, add2(v, d2));
+    if (CAP) d = mul2(d, fma2(t, pack2(-s[e], -s[e + 1]), pack2(1.0f, 1.0f)));
+    if (DC) {
+      const uint64_t u = mul2(p, v);
+      dc[0] = fma2(u, x, dc[0]);
+      dc[1] = add2(u, dc[1]);
+      dc[2] = fma2(p, x, dc[2]);
+      dc[3] = add2(p, dc[3]);
+    }
+    float d0, d1;
+    unpack2(d, d0, d1);
+    ds[e >> 1] = bf16x2(d0, d1);
   }
 }
 // CAP, SLOPE, DC known at compile time: see RowSoftmax
@@ -248,9 +246,14 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         if (a.ranges) {
           const int4 s = span_of(a, w.b, row0);
           if (w.h == 0 && lane == 0) f.spans[w.b * f.tiles + w.tile] = s;
-          if (s.y > s.x) { w.lo = s.x / kT; w.hi = (s.y + kT - 1) / kT; }
+          if (s.y > s.x) {
+            w.lo = s.x / kT;
+            w.hi = (s.y + kT - 1) / kT;
+            w.some_short = s.z >= (w.hi - 1) * kT;
+          }
         } else {
           w.hi = ((a.causal ? min(row0 + kT, a.N) : a.N) + kT - 1) / kT;
+          w.some_short = w.hi == 1;
         }
       }
       alive = wait_all(w_empty + 8 * slot, wphase ^ 1u);
@@ -429,10 +432,19 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
     uint32_t wphase = 0, sphase = 0, dpphase = 0, dsphase = 0, dqphase = 0, xphase = 0, dot_buf = 0;
     int slot = 0;
     bool alive = true;
+    // all element warps
+    auto meet_all = [&]() -> bool {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(x_bar);
+      const bool ok = wait_all(x_bar, xphase);
+      xphase ^= 1u;
+      return ok;
+    };
     while (alive) {
       alive = wait_all(w_full + 8 * slot, wphase);
       if (!alive) break;
       const int valid = work[slot].valid, b = work[slot].b, h = work[slot].h, tile = work[slot].tile, lo = work[slot].lo, hi = work[slot].hi;
+      const bool some_short = work[slot].some_short != 0;
       __syncwarp();
       if (lane == 0) mbar_arrive(w_empty + 8 * slot);
       if (++slot == 2) { slot = 0; wphase ^= 1u; }
@@ -461,11 +473,8 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
           if (lane == 0)
             for (int r = 0; r < 8; ++r) sts_u32(dot_at + dot_buf + 4 * (first + r), __float_as_uint(part[r]));
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(x_bar);
-        alive = wait_all(x_bar, xphase);
+        alive = meet_all();
         if (!alive) break;
-        xphase ^= 1u;
       }
       RowTerms r;
       r.i = tile * kT + row;
@@ -486,20 +495,68 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         out[kT] = r.a;
         out[2 * kT] = -r.dot;
       }
+      if (some_short) {
+        // D of the rows that see keys of the last tile alone, from their float32 probabilities: with few keys the O it came from, rounded to bf16, is what dQ and
+        // dK would be least exact by.  (A look at the first step's S and dP, which the loop then takes.)  The four threads of a row meet through the dS
+        // columns, which the dQ before has read.
+        alive = wait_all(s_full, sphase);
+        if (alive) alive = wait_all(dp_full, dpphase);
+        if (alive) alive = wait_all(ds_empty, dsphase ^ 1u);
+        if (!alive) break;
+        tc_fence_after();
+        float sum0 = 0.f, sum1 = 0.f;
+        const int j0 = (hi - 1) * kT + group * 32;
+        float s[32], dp[32];
+        tmem_ld32(lane_base + kS + group * 32, s);
+        tmem_ld32(lane_base + kDP + group * 32, dp);
+        tmem_ld_wait32(s);
+        tmem_ld_wait32(dp);
+        if (CAP) tanh_scores(a.cap_inv, s);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          float x = s[e];
+          if (SLOPE) x = fmaf(-r.slope, fabsf((float)(j0 + e - r.i)), x);
+          float p = exp2_fast(fmaf(x, r.a, -r.lse2));
+          p = j0 + e >= r.sees.x && j0 + e < r.sees.y ? p : 0.f;
+          sum0 = fmaf(p, dp[e], sum0);
+          sum1 += p;
+        }
+        tmem_st2(lane_base + kDS + group * 16, __float_as_uint(sum0), __float_as_uint(sum1));
+        tmem_st_wait();
+        tc_fence_before();
+        alive = meet_all();
+        if (!alive) break;
+        tc_fence_after();
+        float dot = 0.f, mass = 0.f;
+#pragma unroll
+        for (int other = 0; other < kGroups; ++other) {
+          uint32_t x, y;
+          tmem_ld2(lane_base + kDS + other * 16, x, y);
+          tmem_ld_wait();
+          dot += __uint_as_float(x);
+          mass += __uint_as_float(y);
+        }
+        if (some && r.sees.x >= (hi - 1) * kT && mass > 0.f) {
+          r.dot = dot / mass;
+          if (group == 0) f.rows[((size_t)(b * a.H + h) * f.tiles + tile) * (3 * kT) + 2 * kT + row] = -r.dot;
+        }
+        tc_fence_before();
+        alive = meet_all();                      // (all have read before anyone writes dS there)
+        if (!alive) break;
+        tc_fence_after();
+      }
       uint64_t dc[4] = {0u, 0u, 0u, 0u};         // (pairs of float32 zeros)
       for (int j = hi - 1; j >= lo && alive; --j) {
         alive = wait_all(s_full, sphase);
         if (!alive) break;
         sphase ^= 1u;
         tc_fence_after();
-        const int j0 = j * kT + group * (32 * kChunks);
-        const bool edge = __any_sync(0xffffffffu, r.sees.x > j0 || r.sees.y < j0 + 32 * kChunks);
-        float s[kChunks][32], dp[kChunks][32];
-        uint32_t ds[kChunks][16];
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) tmem_ld32(lane_base + kS + group * (32 * kChunks) + c * 32, s[c]);
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) tmem_ld_wait32(s[c]);
+        const int j0 = j * kT + group * 32;
+        const bool edge = __any_sync(0xffffffffu, r.sees.x > j0 || r.sees.y < j0 + 32);
+        float s[32], dp[32];
+        uint32_t ds[16];
+        tmem_ld32(lane_base + kS + group * 32, s);
+        tmem_ld_wait32(s);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(s_empty);
@@ -507,17 +564,12 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         if (!alive) break;
         dpphase ^= 1u;
         tc_fence_after();
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) tmem_ld32(lane_base + kDP + group * (32 * kChunks) + c * 32, dp[c]);
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) tmem_ld_wait32(dp[c]);
+        tmem_ld32(lane_base + kDP + group * 32, dp);
+        tmem_ld_wait32(dp);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(dp_empty);
-        if (CAP) {
-#pragma unroll
-          for (int c = 0; c < kChunks; ++c) tanh_scores(a.cap_inv, s[c]);
-        }
+        if (CAP) tanh_scores(a.cap_inv, s);
         if (edge) dq_elements<CAP, SLOPE, DC, true>(r, j0, s, dp, ds, dc);
         else dq_elements<CAP, SLOPE, DC, false>(r, j0, s, dp, ds, dc);
         // the dS before has been taken
@@ -525,8 +577,7 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         if (!alive) break;
         dsphase ^= 1u;
         tc_fence_after();
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) tmem_st16(lane_base + kDS + (group * kChunks + c) * 16, ds[c]);
+        tmem_st16(lane_base + kDS + group * 16, ds);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -573,11 +624,8 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         tmem_st8(mine_at, u);
         tmem_st_wait();
         tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(x_bar);
-        alive = wait_all(x_bar, xphase);
+        alive = meet_all();
         if (!alive) break;
-        xphase ^= 1u;
         tc_fence_after();
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -590,11 +638,8 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         }
         if (group == 0 && mine) f.g.dc_rows[at] = some ? (sum[0] - sum[1] * (sum[2] / sum[3])) * a.unit : 0.f;
         tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(x_bar);       // (all have read before anyone writes the next item's dS there)
-        alive = wait_all(x_bar, xphase);
+        alive = meet_all();                      // (all have read before anyone writes the next item's dS there)
         if (!alive) break;
-        xphase ^= 1u;
         tc_fence_after();
       }
       if (any) {
@@ -610,39 +655,46 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
 // ------------------------------------------------------------------------------------------------ dK, dV
 // The Q tiles that see a K/V tile, in order; all roles walk them alike.  Ranges: 32 tiles' spans are looked at together.
 struct QTiles {
-  int tiles, first, b, k0;
+  int tiles, first, k0, diagonal;
   const int4* spans;
-  int base;              // mask: those of the tiles base .. base + 31 that see the keys
-  uint32_t mask;
+  int base;              // masks: those of the tiles base .. base + 31 that see the keys, and of them those with a row that does not see all
+  uint32_t mask, partly;
+  bool edge;             // the last tile: whether it has such a row
   __device__ __forceinline__ void start(const BwdArgs& f, int batch, int kt) {
     tiles = f.tiles;
-    b = batch;
     k0 = kt * kT;
     spans = f.a.ranges ? f.spans + (size_t)batch * f.tiles : nullptr;
-    first = f.a.causal && !spans ? kt : 0;
+    diagonal = f.a.causal && !spans ? kt : -1;
+    first = max(diagonal, 0);
+    edge = false;
     rewind();
   }
   __device__ __forceinline__ void rewind() {
-    base = -32;
-    mask = 0u;
-    if (!spans) base = first - 1;
+    base = spans ? -32 : first - 1;
+    mask = partly = 0u;
   }
   // the next tile, or -1 (the whole warp)
   __device__ __forceinline__ int next() {
-    if (!spans) return ++base < tiles ? base : -1;
+    if (!spans) {
+      edge = ++base == diagonal;
+      return base < tiles ? base : -1;
+    }
     while (mask == 0u) {
       base += 32;
       if (base >= tiles) return -1;
       const int t = base + (threadIdx.x & 31);
-      bool sees = false;
+      bool sees = false, some = false;
       if (t < tiles) {
         const int4 s = spans[t];
         sees = s.x < k0 + kT && s.y > k0;
+        some = s.z > k0 || s.w < k0 + kT;
       }
       mask = __ballot_sync(0xffffffffu, sees);
+      partly = __ballot_sync(0xffffffffu, some);
     }
     const int bit = __ffs(mask) - 1;
     mask &= mask - 1u;
+    edge = (partly >> bit) & 1u;
     return base + bit;
   }
 };
@@ -970,13 +1022,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           const int i0 = t * kT + group * 32 + 2 * (lane & 3);        // this thread's first query and first key
           const int key0 = kt * kT + quad * 32 + (lane >> 2);
           const uint32_t rows_at = rows_smem + st * C::kRowBytes + 4 * (group * 32 + 2 * (lane & 3));
-          bool edge;
-          if (a.ranges) {
-            const int4 s = qt.spans[t];
-            edge = s.z > kt * kT || s.w < (kt + 1) * kT;
-          } else {
-            edge = a.causal && t == kt;
-          }
+          const bool edge = qt.edge;
           alive = wait_all(s_full, sphase);
           if (alive) alive = wait_all(q_full + 8 * st, (idx >> 1) & 1u);   // (the rows' terms; long there)
           if (!alive) break;
