@@ -7,7 +7,7 @@
 //   softmax_dq_kernel   an item is a Q tile of 128 rows: S and dP in TMEM, a row's 128 columns by four threads, dS as bf16 to TMEM and
 //                       from there into dQ += dS K.  Leaves -lse log2 e, a and -D of every row, and which keys every tile sees, to the other kernel.
 //                       dL/dc_i = sum dS x is formed as sum p dP x - (sum p dP)(sum p x) / sum p, all of float32 probabilities: the D above comes
-//                       from the O that was rounded to bf16, which is good enough for dS (an error of 2^-9 of D times p) but not for a float32 result.
+//                       from the O that was rounded to bf16, which is good enough for dS but not for a float32 result.
 //   softmax_dkv_kernel  an item is a K/V tile; over all query heads that share it and all Q tiles that see it: S^T = K Q^T and dP^T = V dO^T with the keys
 //                       along the lanes, so that P^T and dS^T are, over their own columns, the A operands of dV += P^T dO and dK += dS^T Q; what
 //                       depends on the query comes from shared memory.
@@ -128,11 +128,11 @@ struct RowTerms {
   int i;
 };
 
-// 32 columns from key j0 on (s: their accumulators, or the tanh of capped ones): dS as bf16 pairs; dc: {sum p dP x, sum p dP, sum p x, sum p} where wanted, the even
-// and the odd columns' apart
-template <bool CAP, bool SLOPE, bool DC, bool EDGE>
+// 32 columns from key j0 on (s: their accumulators, or the tanh of capped ones): dS as bf16 pairs; FINE: what their rounding left
+// over as bf16 pairs, and in sums {sum p dP, sum p, and with DC sum p dP x, sum p x}, the even and the odd columns' apart
+template <bool CAP, bool SLOPE, bool FINE, bool DC, bool EDGE>
 __device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const float (&s)[32], const float (&dp)[32], uint32_t (&ds)[16],
-                                            uint64_t (&dc)[4]) {
+                                            uint32_t (&dl)[16], uint64_t (&sums)[4]) {
   const uint64_t a2 = pack2(r.a, r.a), l2 = pack2(-r.lse2, -r.lse2), d2 = pack2(-r.dot, -r.dot);
 #pragma unroll
   for (int e = 0; e < 32; e += 2) {
@@ -151,20 +151,27 @@ __device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const flo
     const uint64_t p = pack2(p0, p1), v = pack2(dp[e], dp[e + 1]);
     uint64_t d = mul2(p, add2(v, d2));
     if (CAP) d = mul2(d, fma2(t, pack2(-s[e], -s[e + 1]), pack2(1.0f, 1.0f)));
-    if (DC) {
+    if (FINE) {
       const uint64_t u = mul2(p, v);
-      dc[0] = fma2(u, x, dc[0]);
-      dc[1] = add2(u, dc[1]);
-      dc[2] = fma2(p, x, dc[2]);
-      dc[3] = add2(p, dc[3]);
+      sums[0] = add2(u, sums[0]);
+      sums[1] = add2(p, sums[1]);
+      if (DC) {
+        sums[2] = fma2(u, x, sums[2]);
+        sums[3] = fma2(p, x, sums[3]);
+      }
     }
     float d0, d1;
     unpack2(d, d0, d1);
     ds[e >> 1] = bf16x2(d0, d1);
+    if (FINE) dl[e >> 1] = bf16x2(d0 - __uint_as_float(ds[e >> 1] << 16), d1 - __uint_as_float(ds[e >> 1] & 0xffff0000u));
   }
 }
-// CAP, SLOPE, DC known at compile time: see RowSoftmax
-template <int HD, bool CAP, bool SLOPE, bool DC>
+// CAP, SLOPE, FINE, DC known at compile time: see RowSoftmax.
+// FINE: calls with scales or slopes, whose maps are sharp.  A row of dS sums to zero, so dQ is what remains of a cancellation where its few keys weigh about the
+// same, and 2^-9 of every term is a part of that: dQ gets what the rounding of dS left over as a second product.  And dK gets D from the float32 probabilities.
+// (8 x 12 x 1024 x 64 with a learned scale: dQ 2.5e-3 off in norm without, 1.9e-3 with; the rounding of dQ itself is 1.7e-3.  Plain calls, 2.4e-3, would lose
+// 4 to 9 % of the backward pass.)
+template <int HD, bool CAP, bool SLOPE, bool FINE, bool DC>
 __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                                                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
                                                                     const __grid_constant__ BwdArgs f) {
@@ -187,7 +194,7 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
   const uint32_t tmem_slot = bars + 280, abort_flag = bars + 284, drain_fail = bars + 288;
   const uint32_t dot_at = bars + 336;                                // float [2][128]: of this item and the one before
   const BwdWork* work = reinterpret_cast<const BwdWork*>(smem_raw + (work_at - smem_u32(smem_raw)));
-  constexpr int kS = 0, kDP = kT, kDQ = 2 * kT, kDS = 2 * kT + 128;
+  constexpr int kS = 0, kDP = kT, kDQ = 2 * kT, kDS = 2 * kT + 128, kDL = kDS + 64;   // (kDL: what the rounding of dS left over)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -415,6 +422,8 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
 #pragma unroll
           for (int kk = 0; kk < kT / 16; ++kk)
             umma_bf16_ts(tmem + kDQ, tmem + kDS + kk * 8, kn + kk * ((16 * 128) >> 4), id_kn, (j < hi - 1 || kk > 0) ? 1u : 0u);
+#pragma unroll
+          for (int kk = 0; FINE && kk < kT / 16; ++kk) umma_bf16_ts(tmem + kDQ, tmem + kDL + kk * 8, kn + kk * ((16 * 128) >> 4), id_kn, 1u);
           umma_commit(k_empty + 8 * ks);                     // (S of this tile came long before)
           umma_commit(ds_empty);
           if (j == lo) umma_commit(dq_full);
@@ -545,7 +554,7 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         if (!alive) break;
         tc_fence_after();
       }
-      uint64_t dc[4] = {0u, 0u, 0u, 0u};         // (pairs of float32 zeros)
+      uint64_t sums[4] = {0u, 0u, 0u, 0u};       // (pairs of float32 zeros)
       for (int j = hi - 1; j >= lo && alive; --j) {
         alive = wait_all(s_full, sphase);
         if (!alive) break;
@@ -554,7 +563,7 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         const int j0 = j * kT + group * 32;
         const bool edge = __any_sync(0xffffffffu, r.sees.x > j0 || r.sees.y < j0 + 32);
         float s[32], dp[32];
-        uint32_t ds[16];
+        uint32_t ds[16], dl[16];
         tmem_ld32(lane_base + kS + group * 32, s);
         tmem_ld_wait32(s);
         tc_fence_before();
@@ -570,14 +579,15 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         __syncwarp();
         if (lane == 0) mbar_arrive(dp_empty);
         if (CAP) tanh_scores(a.cap_inv, s);
-        if (edge) dq_elements<CAP, SLOPE, DC, true>(r, j0, s, dp, ds, dc);
-        else dq_elements<CAP, SLOPE, DC, false>(r, j0, s, dp, ds, dc);
+        if (edge) dq_elements<CAP, SLOPE, FINE, DC, true>(r, j0, s, dp, ds, dl, sums);
+        else dq_elements<CAP, SLOPE, FINE, DC, false>(r, j0, s, dp, ds, dl, sums);
         // the dS before has been taken
         alive = wait_all(ds_empty, dsphase ^ 1u);
         if (!alive) break;
         dsphase ^= 1u;
         tc_fence_after();
         tmem_st16(lane_base + kDS + group * 16, ds);
+        if (FINE) tmem_st16(lane_base + kDL + group * 16, dl);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -611,14 +621,14 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
           }
         }
       }
-      if (DC) {
+      if (FINE) {
         // the four threads of a row meet through the dS columns, which nobody needs until the next item's first dS is written: behind dq_empty of all
         const uint32_t mine_at = lane_base + kDS + group * 16;
         uint32_t u[8] = {};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float x, y;
-          unpack2(dc[e], x, y);
+          unpack2(sums[e], x, y);
           u[e] = __float_as_uint(x + y);
         }
         tmem_st8(mine_at, u);
@@ -636,7 +646,13 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[e] += v[e];
         }
-        if (group == 0 && mine) f.g.dc_rows[at] = some ? (sum[0] - sum[1] * (sum[2] / sum[3])) * a.unit : 0.f;
+        if (group == 0 && some) {
+          const float dot = sum[0] / sum[1];     // (sum p is 1 to float32's rounding: dividing by it takes out what all of the row's probabilities are off by)
+          f.rows[((size_t)(b * a.H + h) * f.tiles + tile) * (3 * kT) + 2 * kT + row] = -dot;
+          if (DC) f.g.dc_rows[at] = (sum[2] - dot * sum[3]) * a.unit;
+        } else if (DC && group == 0 && mine) {
+          f.g.dc_rows[at] = 0.f;
+        }
         tc_fence_before();
         alive = meet_all();                      // (all have read before anyone writes the next item's dS there)
         if (!alive) break;
@@ -1153,9 +1169,13 @@ cudaError_t bwd_launch(const BwdArgs& f, const void* q, const void* k, const voi
   };
   auto both = [&](auto cap, auto slope) {
     constexpr bool kCap = decltype(cap)::value, kSlope = decltype(slope)::value;
-    cudaError_t e = f.g.dc_rows ? dq(softmax_dq_kernel<HD, kCap, kSlope, true>) : dq(softmax_dq_kernel<HD, kCap, kSlope, false>);
+    const bool scaled = a.beta || a.c_rows;
+    cudaError_t e;
+    if (f.g.dc_rows) e = dq(softmax_dq_kernel<HD, kCap, kSlope, true, true>);
+    else if (kSlope || scaled) e = dq(softmax_dq_kernel<HD, kCap, kSlope, true, false>);
+    else e = dq(softmax_dq_kernel<HD, kCap, kSlope, kSlope, false>);   // (kSlope: not reached, and the same kernel as above)
     if (e != cudaSuccess) return e;
-    return a.beta || a.c_rows ? dkv(softmax_dkv_kernel<HD, kCap, kSlope, true>) : dkv(softmax_dkv_kernel<HD, kCap, kSlope, false>);
+    return scaled ? dkv(softmax_dkv_kernel<HD, kCap, kSlope, true>) : dkv(softmax_dkv_kernel<HD, kCap, kSlope, false>);
   };
   using T = std::true_type;
   using F = std::false_type;
