@@ -458,37 +458,8 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
       if (lane == 0) mbar_arrive(w_empty + 8 * slot);
       if (++slot == 2) { slot = 0; wphase ^= 1u; }
       if (!valid) break;
-      // D of the tile's rows, 16 rows a warp: a row's 32 lanes read D / 32 elements each of O and dO
-      {
-        constexpr int E = HD / 32;
-#pragma unroll
-        for (int batch = 0; batch < kT / kWarps / 8; ++batch) {
-          const int first = (warp - 2) * (kT / kWarps) + batch * 8;
-          float part[8];
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            const int i = tile * kT + first + r;
-            part[r] = 0.f;
-            if (i < a.N) {
-              float x[E], y[E];
-              load_slice<E>(f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n + lane * E, x);
-              load_slice<E>(f.d_o + (long long)b * f.g.d_o.b + (long long)h * f.g.d_o.h + (long long)i * f.g.d_o.n + lane * E, y);
-#pragma unroll
-              for (int e = 0; e < E; ++e) part[r] = fmaf(x[e], y[e], part[r]);
-            }
-          }
-#pragma unroll
-          for (int r = 0; r < 8; ++r) part[r] = warp_sum(part[r]);
-          if (lane == 0)
-            for (int r = 0; r < 8; ++r) sts_u32(dot_at + dot_buf + 4 * (first + r), __float_as_uint(part[r]));
-        }
-        alive = meet_all();
-        if (!alive) break;
-      }
       RowTerms r;
       r.i = tile * kT + row;
-      r.dot = __uint_as_float(lds_u32(dot_at + dot_buf + 4 * row));
-      dot_buf ^= 512u;
       const bool mine = r.i < a.N;
       r.sees = mine ? visible_keys(a, b, r.i) : make_int2(0, 0);
       const size_t at = ((size_t)b * a.H + h) * a.N + (mine ? r.i : 0);
@@ -498,6 +469,33 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
       r.lse2 = some ? f.g.lse[at] * kLog2e : INFINITY;
       r.slope = a.alibi ? a.alibi[h] / a.unit : 0.f;
       if (!some) { r.sees = make_int2(0, 0x7fffffff); r.a = 0.f; }   // (probability exp2(-inf) everywhere, without a mask)
+      // D of the tile's rows, eight rows a warp: the 32 lanes read D / 32 elements each of O and dO (the loads above are on their way meanwhile)
+      {
+        constexpr int E = HD / 32;
+        static_assert(kT == 8 * kWarps, "eight rows a warp");
+        const int first = (warp - 2) * 8;
+        float part[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const int i = tile * kT + first + y;
+          part[y] = 0.f;
+          if (i < a.N) {
+            float u[E], v[E];
+            load_slice<E>(f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n + lane * E, u);
+            load_slice<E>(f.d_o + (long long)b * f.g.d_o.b + (long long)h * f.g.d_o.h + (long long)i * f.g.d_o.n + lane * E, v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) part[y] = fmaf(u[e], v[e], part[y]);
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < 8; ++y) part[y] = warp_sum(part[y]);
+        if (lane == 0)
+          for (int y = 0; y < 8; ++y) sts_u32(dot_at + dot_buf + 4 * (first + y), __float_as_uint(part[y]));
+        alive = meet_all();
+        if (!alive) break;
+        r.dot = __uint_as_float(lds_u32(dot_at + dot_buf + 4 * row));
+        dot_buf ^= 512u;
+      }
       if (group == 0) {
         float* out = f.rows + ((size_t)(b * a.H + h) * f.tiles + tile) * (3 * kT) + row;
         out[0] = -r.lse2;
