@@ -75,10 +75,8 @@ struct SoftmaxGrads {
   float* row_dot;                     // float32 problems: [B][H][N] scratch, sum_j p_ij dP_ij
 };
 
-// CUDA-core kernels, any dtype of the library's (float32 problems)
-template <typename T>
+// CUDA-core kernels (float32 problems)
 cudaError_t launch_softmax_rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, cudaStream_t stream);
-template <typename T>
 cudaError_t launch_softmax_rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* d_o,
                                     void* dq, void* dk, void* dv, cudaStream_t stream);
 // Tensor-core kernels (bf16)

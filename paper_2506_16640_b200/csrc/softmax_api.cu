@@ -133,7 +133,7 @@ int check_softmax(const entmax_attn_softmax_params* p, const entmax_attn_softmax
   a.B = p->batch; a.H = p->heads; a.KH = p->kv_heads; a.N = p->seq; a.D = p->head_dim;
   if (a.B < 1 || a.H < 1 || a.KH < 1 || a.N < 1 || a.H % a.KH) return ENTMAX_ATTN_EINVAL_SHAPE;
   if (a.D != 64 && a.D != 128) return ENTMAX_ATTN_EINVAL_SHAPE;
-  if ((long long)a.B * a.H > 0x7fffffffLL / 2 || (long long)a.B * a.H * a.N > 0x7fffffffLL / 2) return ENTMAX_ATTN_EINVAL_SHAPE;
+  if (a.H >= 1 << 28 || (long long)a.B * a.H > 0x7fffffffLL / 2 || (long long)a.B * a.H * a.N > 0x7fffffffLL / 2) return ENTMAX_ATTN_EINVAL_SHAPE;
   a.G = a.H / a.KH;
   if (p->dtype != ENTMAX_ATTN_DTYPE_BF16 && p->dtype != ENTMAX_ATTN_DTYPE_FP32) return ENTMAX_ATTN_EINVAL_DTYPE;
   if (!std::isfinite(p->sm_scale) || p->sm_scale < 0.f || !std::isfinite(p->softcap) || p->softcap < 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
@@ -182,7 +182,7 @@ extern "C" int entmax_attn_softmax_fwd(const entmax_attn_softmax_params* params,
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   rc = clear_status(device_status, stream);
   if (rc != ENTMAX_ATTN_OK) return rc;
-  const cudaError_t err = params->dtype == ENTMAX_ATTN_DTYPE_FP32 ? launch_softmax_rows_fwd<float>(a, q, k, v, o, lse, stream)
+  const cudaError_t err = params->dtype == ENTMAX_ATTN_DTYPE_FP32 ? launch_softmax_rows_fwd(a, q, k, v, o, lse, stream)
                                                                   : launch_softmax_fwd(a, q, k, v, o, lse, device_status, stream);
   return err == cudaSuccess ? ENTMAX_ATTN_OK : fail_cuda(err);
 }
@@ -220,7 +220,7 @@ extern "C" int entmax_attn_softmax_bwd(const entmax_attn_softmax_params* params,
   rc = clear_status(device_status, stream);
   if (rc != ENTMAX_ATTN_OK) return rc;
   cudaError_t err = bf16 ? launch_softmax_bwd(a, g, q, k, v, o, d_o, dq, dk, dv, reinterpret_cast<float*>(ws + w.rows), ws + w.spans, device_status, stream)
-                         : launch_softmax_rows_bwd<float>(a, g, q, k, v, d_o, dq, dk, dv, stream);
+                         : launch_softmax_rows_bwd(a, g, q, k, v, d_o, dq, dk, dv, stream);
   if (err == cudaSuccess && given) err = launch_softmax_scale_grad(a, g.dc_rows, grads->dbeta, grads->dgamma, grads->ddelta, stream);
   return err == cudaSuccess ? ENTMAX_ATTN_OK : fail_cuda(err);
 }

@@ -24,8 +24,8 @@ struct RowCfg {
 };
 
 // rows row0 .. of one head into a tile, zeros behind the last
-template <int D, typename T>
-__device__ __forceinline__ void load_rows(float* dst, const T* base, long long stride, int row0, int N) {
+template <int D>
+__device__ __forceinline__ void load_rows(float* dst, const float* base, long long stride, int row0, int N) {
   constexpr int kPieces = D / 4;
   for (int t = threadIdx.x; t < kT * kPieces; t += kRowThreads) {
     const int r = t / kPieces, c = (t - r * kPieces) * 4;
@@ -78,8 +78,8 @@ __device__ __forceinline__ void add_product(const float* S, const float* R, floa
     }
   }
 }
-template <int D, typename T>
-__device__ __forceinline__ void store_rows(T* base, long long stride, int row0, int N, const float (&out)[4][D / 16], const float (&mul)[4]) {
+template <int D>
+__device__ __forceinline__ void store_rows(float* base, long long stride, int row0, int N, const float (&out)[4][D / 16], const float (&mul)[4]) {
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll
   for (int y = 0; y < 4; ++y) {
@@ -129,8 +129,8 @@ __device__ __forceinline__ int2 tile_range(const int2 (&sees)[4], int* lo_hi) {
   return make_int2(lo_hi[0], lo_hi[1]);
 }
 
-template <int D, typename T>
-__global__ void __launch_bounds__(kRowThreads) softmax_rows_fwd_kernel(const SoftmaxArgs a, const T* q, const T* k, const T* v, T* o, float* lse) {
+template <int D>
+__global__ void __launch_bounds__(kRowThreads) softmax_rows_fwd_kernel(const SoftmaxArgs a, const float* q, const float* k, const float* v, float* o, float* lse) {
   pdl_begin();
   using C = RowCfg<D>;
   extern __shared__ float smem[];
@@ -199,9 +199,9 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_fwd_kernel(const Sof
   store_rows<D>(o + b * a.o.b + h * a.o.h, a.o.n, row0, a.N, out, inv);
 }
 
-template <int D, typename T>
-__global__ void __launch_bounds__(kRowThreads) softmax_rows_dq_kernel(const SoftmaxArgs a, const SoftmaxGrads g, const T* q, const T* k, const T* v,
-                                                                      const T* d_o, T* dq) {
+template <int D>
+__global__ void __launch_bounds__(kRowThreads) softmax_rows_dq_kernel(const SoftmaxArgs a, const SoftmaxGrads g, const float* q, const float* k, const float* v,
+                                                                      const float* d_o, float* dq) {
   pdl_begin();
   using C = RowCfg<D>;
   extern __shared__ float smem[];
@@ -273,9 +273,9 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_dq_kernel(const Soft
   store_rows<D>(dq + b * g.dq.b + h * g.dq.h, g.dq.n, row0, a.N, out, mul);
 }
 
-template <int D, typename T>
-__global__ void __launch_bounds__(kRowThreads) softmax_rows_dkv_kernel(const SoftmaxArgs a, const SoftmaxGrads g, const T* q, const T* k, const T* v,
-                                                                       const T* d_o, T* dk, T* dv) {
+template <int D>
+__global__ void __launch_bounds__(kRowThreads) softmax_rows_dkv_kernel(const SoftmaxArgs a, const SoftmaxGrads g, const float* q, const float* k, const float* v,
+                                                                       const float* d_o, float* dk, float* dv) {
   pdl_begin();
   using C = RowCfg<D>;
   extern __shared__ float smem[];
@@ -334,45 +334,40 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_dkv_kernel(const Sof
   store_rows<D>(dv + b * g.dv.b + kh * g.dv.h, g.dv.n, j0, a.N, out_v, one);
 }
 
-template <int D, typename T>
+template <int D>
 cudaError_t rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, cudaStream_t stream) {
   using C = RowCfg<D>;
   const int smem = (3 * C::kTile + C::kScores) * 4;
-  cudaError_t err = cudaFuncSetAttribute(softmax_rows_fwd_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t err = cudaFuncSetAttribute(softmax_rows_fwd_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (err != cudaSuccess) return err;
   const unsigned grid = (unsigned)((long long)a.B * a.H * ((a.N + kT - 1) / kT));
-  return launch_kernel(softmax_rows_fwd_kernel<D, T>, grid, kRowThreads, smem, stream, a, static_cast<const T*>(q), static_cast<const T*>(k),
-                       static_cast<const T*>(v), static_cast<T*>(o), lse);
+  return launch_kernel(softmax_rows_fwd_kernel<D>, grid, kRowThreads, smem, stream, a, static_cast<const float*>(q), static_cast<const float*>(k),
+                       static_cast<const float*>(v), static_cast<float*>(o), lse);
 }
-template <int D, typename T>
+template <int D>
 cudaError_t rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* d_o, void* dq, void* dk,
                      void* dv, cudaStream_t stream) {
   using C = RowCfg<D>;
   const int smem_q = (4 * C::kTile + C::kScores) * 4, smem_kv = (4 * C::kTile + 2 * C::kScores) * 4;
-  cudaError_t err = cudaFuncSetAttribute(softmax_rows_dq_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_q);
-  if (err == cudaSuccess) err = cudaFuncSetAttribute(softmax_rows_dkv_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_kv);
+  cudaError_t err = cudaFuncSetAttribute(softmax_rows_dq_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_q);
+  if (err == cudaSuccess) err = cudaFuncSetAttribute(softmax_rows_dkv_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_kv);
   if (err != cudaSuccess) return err;
   const long long tiles = (a.N + kT - 1) / kT;
-  err = launch_kernel(softmax_rows_dq_kernel<D, T>, (unsigned)(a.B * a.H * tiles), kRowThreads, smem_q, stream, a, g, static_cast<const T*>(q),
-                      static_cast<const T*>(k), static_cast<const T*>(v), static_cast<const T*>(d_o), static_cast<T*>(dq));
+  err = launch_kernel(softmax_rows_dq_kernel<D>, (unsigned)(a.B * a.H * tiles), kRowThreads, smem_q, stream, a, g, static_cast<const float*>(q),
+                      static_cast<const float*>(k), static_cast<const float*>(v), static_cast<const float*>(d_o), static_cast<float*>(dq));
   if (err != cudaSuccess) return err;
-  return launch_kernel(softmax_rows_dkv_kernel<D, T>, (unsigned)(a.B * a.KH * tiles), kRowThreads, smem_kv, stream, a, g, static_cast<const T*>(q),
-                       static_cast<const T*>(k), static_cast<const T*>(v), static_cast<const T*>(d_o), static_cast<T*>(dk), static_cast<T*>(dv));
+  return launch_kernel(softmax_rows_dkv_kernel<D>, (unsigned)(a.B * a.KH * tiles), kRowThreads, smem_kv, stream, a, g, static_cast<const float*>(q),
+                       static_cast<const float*>(k), static_cast<const float*>(v), static_cast<const float*>(d_o), static_cast<float*>(dk), static_cast<float*>(dv));
 }
 
 }  // namespace
 
-template <typename T>
 cudaError_t launch_softmax_rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, cudaStream_t stream) {
-  return a.D == 64 ? rows_fwd<64, T>(a, q, k, v, o, lse, stream) : rows_fwd<128, T>(a, q, k, v, o, lse, stream);
+  return a.D == 64 ? rows_fwd<64>(a, q, k, v, o, lse, stream) : rows_fwd<128>(a, q, k, v, o, lse, stream);
 }
-template <typename T>
 cudaError_t launch_softmax_rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* d_o,
                                     void* dq, void* dk, void* dv, cudaStream_t stream) {
-  return a.D == 64 ? rows_bwd<64, T>(a, g, q, k, v, d_o, dq, dk, dv, stream) : rows_bwd<128, T>(a, g, q, k, v, d_o, dq, dk, dv, stream);
+  return a.D == 64 ? rows_bwd<64>(a, g, q, k, v, d_o, dq, dk, dv, stream) : rows_bwd<128>(a, g, q, k, v, d_o, dq, dk, dv, stream);
 }
-template cudaError_t launch_softmax_rows_fwd<float>(const SoftmaxArgs&, const void*, const void*, const void*, void*, float*, cudaStream_t);
-template cudaError_t launch_softmax_rows_bwd<float>(const SoftmaxArgs&, const SoftmaxGrads&, const void*, const void*, const void*, const void*, void*,
-                                                    void*, void*, cudaStream_t);
 
 }  // namespace entmax
