@@ -431,7 +431,9 @@ int entmax_attn_paged_tables(const entmax_attn_paged_tables_params* params, cons
  *   d_scale_rows  out, device float32 [batch, heads, seq] or NULL: dL/dc_i = sum_j dS_ij x_ij
  *   dbeta, dgamma, ddelta  out, device float32 [heads], all three or none; they need beta, gamma, delta
  *   workspace     256-byte aligned, >= entmax_attn_softmax_workspace_bytes(params) bytes; the forward call needs none
- * Nothing is added up by atomics: results are bitwise reproducible.  Errors as for entmax_attn_fwd (softcap negative or not finite: EINVAL_ALPHA). */
+ * q, k, v, o and d_o have to be finite, in rows that see nothing and keys that nobody sees as well (a probability of 0 times a NaN is one).
+ * Nothing is added up by atomics: results are bitwise reproducible.  Errors as for entmax_attn_fwd (softcap negative or not finite: EINVAL_ALPHA;
+ * heads from 2^28, batch * heads * seq from 2^30 on: EINVAL_SHAPE). */
 typedef struct {
   int64_t b, h, n;                     /* elements between batch rows, heads, tokens                                */
 } entmax_attn_strides;
@@ -481,8 +483,9 @@ int entmax_attn_row_ranges(int32_t batch, int32_t seq, int32_t docs, int32_t cau
  *   max_q_len, max_kv_len   the most new tokens and the longest kv_len of any sequence of the call (0: not known): they size the workspace and the
  *                 launches; a sequence beyond them is left out (ENTMAX_ATTN_FLAG_BAD_LENGTH)
  *   workspace     device scratch, 256-byte aligned, >= entmax_attn_softmax_paged_workspace_bytes(cache, params, cu_q == NULL) bytes
- * The rows of a sequence that is left out get O = 0, lse = -inf.  Slots past a sequence's length may hold anything.  K and V are read once per K/V
- * head (chunks: once per 256 rows of a query head).  Results are bitwise reproducible.  Errors as for entmax_attn_fwd; bf16 only. */
+ * The rows of a sequence that is left out get O = 0, lse = -inf.  Slots past a sequence's length may hold anything.  A sequence with 64 rows at most
+ * (a row: a new token and one of the g = q_heads / kv_heads query heads of a K/V head, g <= 128) reads K and V once per K/V head, a longer chunk once for every
+ * 128 new tokens and two of the query heads (g odd: 256 tokens and one).  Results are bitwise reproducible.  Errors as for entmax_attn_fwd; bf16 only. */
 typedef struct {
   int32_t total_q, q_heads;
   int32_t max_q_len, max_kv_len;

@@ -15,6 +15,7 @@ from __future__ import annotations
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -73,6 +74,7 @@ class _SoftmaxAttention(torch.autograd.Function):
         return o, lse
 
     @staticmethod
+    @once_differentiable                    # (second derivatives are refused instead of being taken for zero)
     def backward(ctx, d_o, _d_lse):
         q, k, v, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, o, lse = ctx.saved_tensors
         want_params = beta is not None and any(ctx.needs_input_grad[3:6])
@@ -102,7 +104,7 @@ def softmax_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, beta: O
     table c_rows (float32 [B,H,N]).
 
     alibi_slopes: float32 [H]; softcap > 0 caps the scores by a tanh; row_ranges: int32 [B,N,2] from binding.entmax_attn_row_ranges (documents,
-    prefixes, windows), with causal=False.  Returns O, or (O, lse).
+    prefixes, windows), with causal=False.  Returns O, or (O, lse); lse has no gradient, and there are no second derivatives.
 
     To capture a training step into a CUDA graph, let no eager graph of the same leaves live (PyTorch would add up their gradients on that
     graph's stream)."""

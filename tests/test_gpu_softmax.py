@@ -97,6 +97,12 @@ def test_sizes(B, H, G, N, d, causal, dtype):
     _both_ways(q, k, v, d_o, causal, {})
 
 
+@pytest.mark.parametrize("B,H,G,N,d", [(500, 4, 2, 1, 64), (260, 3, 3, 3, 128)])
+def test_many_short_sequences(B, H, G, N, d):
+    q, k, v, d_o = _inputs(B, H, G, N, d, bf16, seed=B)
+    _both_ways(q, k, v, d_o, True, {})
+
+
 KINDS = ["cap", "lowcap", "slopes", "length", "rows", "ranges", "cap+slopes+length", "ranges+rows+cap", "ranges+slopes+length", "rows+slopes"]
 
 
@@ -247,6 +253,16 @@ def test_autograd():
     want = _want(q, k, v, True, {"c_rows": c}, torch.ones_like(o))
     for name, x in zip(("dq", "dk", "dv", "dc"), got):
         softmax.check(name, x, want)
+
+
+def test_no_second_derivatives_and_no_broadcast_inputs():
+    q, k, v, _ = _inputs(1, 2, 2, 40, 64, seed=14)
+    leaves = [x.detach().requires_grad_(True) for x in (q, k, v)]
+    (dq,) = torch.autograd.grad(autograd.softmax_attention(*leaves).float().square().sum(), leaves[:1], create_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(dq.float().sum(), leaves)
+    with pytest.raises(binding.EntmaxAttnError):
+        autograd.softmax_attention(q, k[:, :1].expand(1, 2, 40, 64), v)
 
 
 def test_autograd_against_differences():

@@ -91,6 +91,12 @@ def test_chunks(new, lens, H, KH, d, page):
     _check(pr, _run(pr))
 
 
+@pytest.mark.parametrize("H,d,page", [(71, 64, 16), (128, 128, 32), (64, 64, 4096), (65, 128, 64)])
+def test_one_kv_head_for_many_query_heads(H, d, page):
+    pr = _problem([1, 1, 2, 1], [1, 700, 90, 129], H, 1, d, page, seed=H)
+    _check(pr, _run(pr))
+
+
 @pytest.mark.parametrize("kind", ["cap", "slopes", "length", "negative", "window1", "window40", "cap+slopes+length+window100", "slopes+negative"])
 @pytest.mark.parametrize("new,lens", [([1, 1, 1], [1, 200, 1030]), ([3, 2, 5], [600, 2, 70]), ([150, 1, 40], [700, 90, 40])])
 def test_terms(kind, new, lens):

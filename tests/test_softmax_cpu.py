@@ -53,6 +53,11 @@ def test_forward_refusals(lib):
     assert lib.entmax_attn_softmax_fwd(None, X, X, X, None, X, X, None, None) == NULL
 
 
+def test_sizes_beyond_the_launches_are_refused(lib):
+    assert _fwd(lib, _params(heads=1 << 28, kv_heads=1, batch=1, seq=1)) == SHAPE
+    assert _fwd(lib, _params(heads=1 << 10, kv_heads=1, batch=1 << 10, seq=1 << 10)) == SHAPE
+
+
 def test_backward_refusals(lib):
     from paper_2506_16640_b200.binding import SoftmaxGrads, SoftmaxTerms, Strides
     p = _params()
