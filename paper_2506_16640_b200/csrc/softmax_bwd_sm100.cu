@@ -6,8 +6,9 @@
 // through memory as a float32 sum and results are the same every time.
 //   softmax_dq_kernel   an item is a Q tile of 128 rows: S and dP in TMEM, a row's 128 columns by four threads, dS as bf16 to TMEM and
 //                       from there into dQ += dS K.  Leaves -lse log2 e, a and -D of every row, and which keys every tile sees, to the other kernel.
-//                       dL/dc_i = sum dS x is formed as sum p dP x - (sum p dP)(sum p x) / sum p, all of float32 probabilities: the D above comes
-//                       from the O that was rounded to bf16, which is good enough for dS but not for a float32 result.
+//                       dL/dc_i = sum dS x is formed as (sum p y x - (sum p y)(sum p x) / sum p) / sum p with y = dP - D, all of float32
+//                       probabilities and with x measured from the middle of the row's scores: the D above comes from the O that was rounded to bf16,
+//                       which is good enough for dS but not for a float32 result.
 //   softmax_dkv_kernel  an item is a K/V tile; over all query heads that share it and all Q tiles that see it: S^T = K Q^T and dP^T = V dO^T with the keys
 //                       along the lanes, so that P^T and dS^T are, over their own columns, the A operands of dV += P^T dO and dK += dS^T Q; what
 //                       depends on the query comes from shared memory.
@@ -123,13 +124,13 @@ __device__ __forceinline__ void bwd_teardown(uint32_t tmem, uint32_t abort_flag,
 
 // ------------------------------------------------------------------------------------------------ dQ
 struct RowTerms {
-  float lse2, a, dot, slope;
+  float lse2, a, dot, slope, mid;   // mid: about where the row's scores lie (any value will do)
   int2 sees;
   int i;
 };
 
 // 32 columns from key j0 on (s: their accumulators, or the tanh of capped ones): dS as bf16 pairs; FINE: what their rounding left
-// over as bf16 pairs, and in sums {sum p dP, sum p, and with DC sum p dP x, sum p x}, the even and the odd columns' apart
+// over as bf16 pairs, and in sums {sum p (dP - D), sum p, and with DC sum p (dP - D) (x - mid), sum p (x - mid)}, the even and the odd columns' apart
 template <bool CAP, bool SLOPE, bool FINE, bool DC, bool EDGE>
 __device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const float (&s)[32], const float (&dp)[32], uint32_t (&ds)[16],
                                             uint32_t (&dl)[16], uint64_t (&sums)[4]) {
@@ -150,16 +151,16 @@ __device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const flo
     }
     const uint64_t p = pack2(p0, p1), v = pack2(dp[e], dp[e + 1]);
     uint64_t d = mul2(p, add2(v, d2));
-    if (CAP) d = mul2(d, fma2(t, pack2(-s[e], -s[e + 1]), pack2(1.0f, 1.0f)));
     if (FINE) {
-      const uint64_t u = mul2(p, v);
-      sums[0] = add2(u, sums[0]);
+      sums[0] = add2(d, sums[0]);
       sums[1] = add2(p, sums[1]);
       if (DC) {
-        sums[2] = fma2(u, x, sums[2]);
-        sums[3] = fma2(p, x, sums[3]);
+        const uint64_t y = add2(x, pack2(-r.mid, -r.mid));
+        sums[2] = fma2(d, y, sums[2]);
+        sums[3] = fma2(p, y, sums[3]);
       }
     }
+    if (CAP) d = mul2(d, fma2(t, pack2(-s[e], -s[e + 1]), pack2(1.0f, 1.0f)));
     float d0, d1;
     unpack2(d, d0, d1);
     ds[e >> 1] = bf16x2(d0, d1);
@@ -468,6 +469,8 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
       r.a = c * a.unit * kLog2e;
       r.lse2 = some ? f.g.lse[at] * kLog2e : INFINITY;
       r.slope = a.alibi ? a.alibi[h] / a.unit : 0.f;
+      // (the logarithm of the scores' mean exponential, which lies between the least and the largest)
+      r.mid = DC && fabsf(r.a) > 1e-3f && some ? (r.lse2 - log2f((float)(r.sees.y - r.sees.x))) / r.a : 0.f;
       if (!some) { r.sees = make_int2(0, 0x7fffffff); r.a = 0.f; }   // (probability exp2(-inf) everywhere, without a mask)
       // D of the tile's rows, eight rows a warp: the 32 lanes read D / 32 elements each of O and dO (the loads above are on their way meanwhile)
       {
@@ -645,9 +648,9 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
           for (int e = 0; e < 4; ++e) sum[e] += v[e];
         }
         if (group == 0 && some) {
-          const float dot = sum[0] / sum[1];     // (sum p is 1 to float32's rounding: dividing by it takes out what all of the row's probabilities are off by)
-          f.rows[((size_t)(b * a.H + h) * f.tiles + tile) * (3 * kT) + 2 * kT + row] = -dot;
-          if (DC) f.g.dc_rows[at] = (sum[2] - dot * sum[3]) * a.unit;
+          const float more = sum[0] / sum[1];    // (sum p is 1 to float32's rounding: dividing by it, in dc as well, takes out what all of the row's probabilities are off by)
+          f.rows[((size_t)(b * a.H + h) * f.tiles + tile) * (3 * kT) + 2 * kT + row] = -(r.dot + more);
+          if (DC) f.g.dc_rows[at] = (sum[2] - more * sum[3]) / sum[1] * a.unit;
         } else if (DC && group == 0 && mine) {
           f.g.dc_rows[at] = 0.f;
         }
