@@ -27,16 +27,15 @@ struct SoftmaxArgs {
   entmax_attn_strides q, k, v, o;
 };
 
-// The keys [x, y) that row i of batch row b sees; y = x where there are none.
-__device__ __forceinline__ int2 visible_keys(const SoftmaxArgs& a, int b, int i) {
-  int2 r = make_int2(0, a.causal ? i + 1 : a.N);
-  if (a.ranges) {
-    const int2 given = a.ranges[(size_t)b * a.N + i];
-    r.x = max(given.x, 0);
-    r.y = min(given.y, r.y);
-  }
+// The keys [x, y) that row i sees of the ones its range says; y = x where there are none.
+__device__ __forceinline__ int2 seen_of(const SoftmaxArgs& a, int2 range, int i) {
+  int2 r = make_int2(max(range.x, 0), min(range.y, a.causal ? i + 1 : a.N));
   if (r.y <= r.x) r = make_int2(0, 0);
   return r;
+}
+// The same from the row's range in memory, or without one
+__device__ __forceinline__ int2 visible_keys(const SoftmaxArgs& a, int b, int i) {
+  return a.ranges ? seen_of(a, a.ranges[(size_t)b * a.N + i], i) : make_int2(0, a.causal ? i + 1 : a.N);
 }
 
 // (ln n)^gamma grown by beta on top of delta; n = 1 (and 0): delta alone

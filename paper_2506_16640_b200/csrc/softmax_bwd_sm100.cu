@@ -81,8 +81,12 @@ __device__ __forceinline__ uint32_t a_column(int kk) { return (uint32_t)((kk >> 
 __device__ __forceinline__ int4 span_of(const SoftmaxArgs& a, int b, int row0) {
   const int lane = threadIdx.x & 31;
   int4 s = make_int4(0x7fffffff, 0, 0, 0x7fffffff);
-  for (int r = lane; r < kT && row0 + r < a.N; r += 32) {
-    const int2 v = visible_keys(a, b, row0 + r);
+  int2 range[kT / 32];                           // (rows behind the last: the last once more)
+#pragma unroll
+  for (int t = 0; t < kT / 32; ++t) range[t] = a.ranges[(size_t)b * a.N + min(row0 + t * 32 + lane, a.N - 1)];
+#pragma unroll
+  for (int t = 0; t < kT / 32; ++t) {
+    const int2 v = seen_of(a, range[t], min(row0 + t * 32 + lane, a.N - 1));
     if (v.y <= v.x) continue;
     s.x = min(s.x, v.x); s.y = max(s.y, v.y); s.z = max(s.z, v.x); s.w = min(s.w, v.y);
   }
@@ -477,18 +481,19 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
         constexpr int E = HD / 32;
         static_assert(kT == 8 * kWarps, "eight rows a warp");
         const int first = (warp - 2) * 8;
-        float part[8];
+        float part[8], u[8][E], v[8][E];
+        // (all loads first, those of rows behind the last from the last: a condition around each made the eight rows' latencies add up, 5 us of an item)
 #pragma unroll
         for (int y = 0; y < 8; ++y) {
-          const int i = tile * kT + first + y;
-          part[y] = 0.f;
-          if (i < a.N) {
-            float u[E], v[E];
-            load_slice<E>(f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n + lane * E, u);
-            load_slice<E>(f.d_o + (long long)b * f.g.d_o.b + (long long)h * f.g.d_o.h + (long long)i * f.g.d_o.n + lane * E, v);
+          const int i = min(tile * kT + first + y, a.N - 1);
+          load_slice<E>(f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n + lane * E, u[y]);
+          load_slice<E>(f.d_o + (long long)b * f.g.d_o.b + (long long)h * f.g.d_o.h + (long long)i * f.g.d_o.n + lane * E, v[y]);
+        }
 #pragma unroll
-            for (int e = 0; e < E; ++e) part[y] = fmaf(u[e], v[e], part[y]);
-          }
+        for (int y = 0; y < 8; ++y) {
+          part[y] = 0.f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) part[y] = fmaf(u[y][e], v[y][e], part[y]);
         }
 #pragma unroll
         for (int y = 0; y < 8; ++y) part[y] = warp_sum(part[y]);
@@ -612,15 +617,7 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = 0.f;
         }
-        if (mine) {
-          __nv_bfloat16* out = f.dq + (long long)b * f.g.dq.b + (long long)h * f.g.dq.h + (long long)r.i * f.g.dq.n + col;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float* x = v + 8 * e;
-            *reinterpret_cast<uint4*>(out + 8 * e) = make_uint4(bf16x2(x[0] * g, x[1] * g), bf16x2(x[2] * g, x[3] * g), bf16x2(x[4] * g, x[5] * g),
-                                                                bf16x2(x[6] * g, x[7] * g));
-          }
-        }
+        store_quad_rows(v, g, f.dq + (long long)b * f.g.dq.b + (long long)h * f.g.dq.h + (long long)r.i * f.g.dq.n + col, f.g.dq.n, a.N - r.i);
       }
       if (FINE) {
         // the four threads of a row meet through the dS columns, which nobody needs until the next item's first dS is written: behind dq_empty of all
@@ -1028,7 +1025,6 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
       QTiles qt;
       qt.start(f, b, kt);
       const int key = kt * kT + row;
-      const bool mine = key < a.N;
       bool any = false;
       for (int g = 0; g < a.G && alive; ++g) {
         const float slope = a.alibi ? a.alibi[kh * a.G + g] / a.unit : 0.f;
@@ -1040,6 +1036,20 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           const int key0 = kt * kT + quad * 32 + (lane >> 2);
           const uint32_t rows_at = rows_smem + st * C::kRowBytes + 4 * (group * 32 + 2 * (lane & 3));
           const bool edge = qt.edge;
+          int2 sees[8];                          // the eight queries' keys (asked for ahead of the wait; rows behind the last have probabilities of 0 anyway)
+          if (edge) {
+            if (a.ranges) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) sees[e] = a.ranges[(size_t)b * a.N + min(i0 + 8 * (e >> 1) + (e & 1), a.N - 1)];
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) sees[e] = make_int2(0, a.N);
+            }
+            if (a.causal) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) sees[e].y = min(sees[e].y, i0 + 8 * (e >> 1) + (e & 1) + 1);
+            }
+          }
           alive = wait_all(s_full, sphase);
           if (alive) alive = wait_all(q_full + 8 * st, (idx >> 1) & 1u);   // (the rows' terms; long there)
           if (!alive) break;
@@ -1057,11 +1067,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           if (edge) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const int i = i0 + 8 * (e >> 1) + (e & 1);
-              const int2 sees = i < a.N ? visible_keys(a, b, i) : make_int2(0, 0);
 #pragma unroll
               for (int y = 0; y < 4; ++y) {
-                const bool on = key0 + 8 * y >= sees.x && key0 + 8 * y < sees.y;
+                const bool on = key0 + 8 * y >= sees[e].x && key0 + 8 * y < sees[e].y;
                 float& w = s[(y >> 1) * 16 + 4 * (e >> 1) + (y & 1) * 2 + (e & 1)];
                 w = on ? w : 0.f;
                 u[(y >> 1) * 8 + 2 * (e >> 1) + (y & 1)] &= on ? 0xffffffffu : (e & 1) ? 0x0000ffffu : 0xffff0000u;
@@ -1126,17 +1134,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[e] = 0.f;
           }
-          if (mine) {
-            const entmax_attn_strides& s = which ? f.g.dv : f.g.dk;
-            __nv_bfloat16* out = (which ? f.dv : f.dk) + (long long)b * s.b + (long long)kh * s.h + (long long)key * s.n + col;
-            const float mul = which ? 1.0f : kLn2 * a.sm_scale / a.unit;   // (the rows' a is c unit log2 e)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float* x = v + 8 * e;
-              *reinterpret_cast<uint4*>(out + 8 * e) = make_uint4(bf16x2(x[0] * mul, x[1] * mul), bf16x2(x[2] * mul, x[3] * mul),
-                                                                  bf16x2(x[4] * mul, x[5] * mul), bf16x2(x[6] * mul, x[7] * mul));
-            }
-          }
+          const entmax_attn_strides& s = which ? f.g.dv : f.g.dk;
+          store_quad_rows(v, which ? 1.0f : kLn2 * a.sm_scale / a.unit,   // (the rows' a is c unit log2 e)
+                          (which ? f.dv : f.dk) + (long long)b * s.b + (long long)kh * s.h + (long long)key * s.n + col, s.n, a.N - key);
         }
       }
       if (any) {

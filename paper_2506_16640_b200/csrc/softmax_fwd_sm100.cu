@@ -87,8 +87,12 @@ __device__ __forceinline__ int2 tile_span(const SoftmaxArgs& a, int b, int row0)
       lo = 0;
       hi = a.causal ? min(row0 + kRows, a.N) : a.N;
     } else {
-      for (int r = lane; r < kRows && row0 + r < a.N; r += 32) {
-        const int2 s = visible_keys(a, b, row0 + r);
+      int2 range[kRows / 32];                    // (rows behind the last: the last once more)
+#pragma unroll
+      for (int t = 0; t < kRows / 32; ++t) range[t] = a.ranges[(size_t)b * a.N + min(row0 + t * 32 + lane, a.N - 1)];
+#pragma unroll
+      for (int t = 0; t < kRows / 32; ++t) {
+        const int2 s = seen_of(a, range[t], min(row0 + t * 32 + lane, a.N - 1));
         if (s.y > s.x) { lo = min(lo, s.x); hi = max(hi, s.y); }
       }
       lo = __reduce_min_sync(0xffffffffu, lo);
@@ -566,9 +570,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
       } else if (mine) {
         f.part_ml[(size_t)(part + t) * kRows + row] = make_float2(sm.base(), mass);
       }
-      __nv_bfloat16* out = nullptr;
-      if (mine)
-        out = PAGED ? f.o + ((size_t)(q0 + i) * a.H + h) * HD : f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n;
+      __nv_bfloat16* out = PAGED ? f.o + ((long long)(q0 + i) * a.H + h) * HD : f.o + (long long)b * a.o.b + (long long)h * a.o.h + (long long)i * a.o.n;
+      const long long stride = PAGED ? (long long)a.H * HD : a.o.n;
       const bool some = hi > lo;
       if (some) {
         alive = wait_all(o_full + 8 * t, ophase);
@@ -586,20 +589,18 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = 0.f;
         }
-        if (mine) {
-          if (PAGED && part >= 0) {
-            float4* to = reinterpret_cast<float4*>(f.part_o + ((size_t)(part + t) * kRows + row) * HD + c * 32);
+        if (PAGED && part >= 0) {
+          float* to = f.part_o + ((size_t)(part + t) * kRows + row) * HD + c * 32;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) to[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-          } else {
+          for (int half = 0; half < 2; ++half) {
+            uint32_t w[16];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              // (a row that sees nothing: its O is 0 times what the tile's other rows left it with, which is 0)
-              const float* x = v + 8 * e;
-              *reinterpret_cast<uint4*>(out + c * 32 + 8 * e) = make_uint4(bf16x2(x[0] * inv, x[1] * inv), bf16x2(x[2] * inv, x[3] * inv),
-                                                                           bf16x2(x[4] * inv, x[5] * inv), bf16x2(x[6] * inv, x[7] * inv));
-            }
+            for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(v[half * 16 + e]);
+            store_quad_rows(w, to + half * 16, HD * 4, n - i);
           }
+        } else {
+          // (a row that sees nothing: its O is 0 times what the tile's other rows left it with, which is 0)
+          store_quad_rows(v, inv, out + c * 32, stride, n - i);
         }
       }
       if (some) {

@@ -10,6 +10,40 @@ namespace entmax {
 // swizzle: atoms of eight rows repeat every 1024 bytes, 64-element blocks every 128 * 128 bytes.
 __device__ __forceinline__ uint32_t mn_desc_lo(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | ((uint32_t)((128 * 128) >> 4) << 16); }
 
+// Rows of a tile that lie one to a lane, 16 32-bit words (64 bytes) of each, to memory: the four lanes of a quad swap 16-byte pieces, so that a store fills
+// 64 bytes of eight rows and not 16 of 32, each in a line of its own (32 passes of the load/store unit to an instruction: 2 us of every 128 x 64 tile of two
+// gradients).  By the whole warp.  own: where this lane's row has them; pitch: bytes to the next row; left: rows that exist from this lane's on.
+__device__ __forceinline__ void store_quad_rows(uint32_t (&w)[16], void* own, long long pitch, int left) {
+  const int l = threadIdx.x & 3;
+  // a 4 x 4 transpose of pieces: row l's piece k goes to lane k as its row l's
+#pragma unroll
+  for (int bit = 1; bit < 4; bit *= 2) {
+    const bool upper = (l & bit) != 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k & bit) continue;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        uint32_t& lo = w[4 * k + x];
+        uint32_t& hi = w[4 * (k + bit) + x];
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, bit);
+        if (upper) lo = got; else hi = got;
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (k - l < left)
+      *reinterpret_cast<uint4*>(static_cast<char*>(own) + (k - l) * pitch + l * 16) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+}
+// 32 columns as bf16, times mul
+__device__ __forceinline__ void store_quad_rows(const float (&v)[32], float mul, __nv_bfloat16* own, long long stride, int left) {
+  uint32_t w[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) w[e] = sm100::bf16x2(v[2 * e] * mul, v[2 * e + 1] * mul);
+  store_quad_rows(w, own, stride * 2, left);
+}
+
 // A value that all lanes have, as one the compiler knows to be the same in all of them: descriptors and loop bounds then stay in uniform registers
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
