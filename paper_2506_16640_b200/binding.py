@@ -409,6 +409,14 @@ def _new_on(stream, like, shape, dtype):
         return like.new_empty(shape, dtype=dtype)
 
 
+def _like_on(stream, like):
+    """The same, contiguous with the shape and dtype of `like` (1 us less than by shape)."""
+    if stream is None:
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
+
+
 def _clear_status(status, stream):
     """What the library does at the start of a call, for a call that has nothing to launch."""
     if status is None:
@@ -561,7 +569,7 @@ def entmax_attn_softmax_paged_fwd(q, k_cache, v_cache, block_table, kv_len, cu_q
         o, lse, status))
     device = q.get_device()
     if o is None:
-        o = _new_on(stream, q, (T, H, D), torch.bfloat16)
+        o = _like_on(stream, q)
     if lse is None:
         lse = _new_on(stream, q, (T, H), torch.float32)
     if T == 0:
@@ -614,11 +622,11 @@ def entmax_attn_paged_tables(kv_len, new_len, block_table, free_pages, free_coun
     params, B = known[1] if known is not None and known[0] == key else _keep(where, key, _tables_layout(
         what, kv_len, new_len, block_table, free_pages, free_count, page_size, num_pages, total_q, kv_len_out, cu_q, positions, slots,
         free_count_out, status))
-    kv_len_out = _new_on(stream, kv_len, (B,), torch.int32) if kv_len_out is None else kv_len_out
+    kv_len_out = _like_on(stream, kv_len) if kv_len_out is None else kv_len_out
     cu_q = _new_on(stream, kv_len, (B + 1,), torch.int32) if cu_q is None else cu_q
     positions = _new_on(stream, kv_len, (total_q,), torch.int32) if positions is None else positions
     slots = _new_on(stream, kv_len, (total_q,), torch.int64) if slots is None else slots
-    free_count_out = _new_on(stream, kv_len, (1,), torch.int32) if free_count_out is None else free_count_out
+    free_count_out = _like_on(stream, free_count) if free_count_out is None else free_count_out
     rc = _call_on(kv_len.get_device(), lambda: load().entmax_attn_paged_tables(
         params, kv_len.data_ptr(), new_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), kv_len_out.data_ptr(),
         cu_q.data_ptr(), positions.data_ptr(), slots.data_ptr(), free_count_out.data_ptr(), _ptr(status), _stream_ptr(stream)))
@@ -689,7 +697,7 @@ def entmax_attn_softmax_fwd(q, k, v, causal, beta=None, gamma=None, delta=None, 
         False))
     B, H, N, _ = shape = q.shape
     if o is None:
-        o = _new_on(stream, q, shape, q.dtype)
+        o = _like_on(stream, q)
     if lse is None:
         lse = _new_on(stream, q, (B, H, N), torch.float32)
     terms = SoftmaxTerms(_ptr(row_ranges), _ptr(beta), _ptr(gamma), _ptr(delta), _ptr(c_rows), _ptr(alibi_slopes))
@@ -714,12 +722,14 @@ def entmax_attn_softmax_bwd(q, k, v, o, lse, d_o, causal, beta=None, gamma=None,
         what, q, k, v, causal, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, softcap, sm_scale, o, lse, status, d_o, dq, dk, dv, d_scale_rows,
         True))
     B, H, N, _ = q.shape
-    dq = _new_on(stream, q, q.shape, q.dtype) if dq is None else dq
-    dk = _new_on(stream, k, k.shape, k.dtype) if dk is None else dk
-    dv = _new_on(stream, v, v.shape, v.dtype) if dv is None else dv
+    dq = _like_on(stream, q) if dq is None else dq
+    dk = _like_on(stream, k) if dk is None else dk
+    dv = _like_on(stream, v) if dv is None else dv
     if d_scale_rows is None and want_scale_rows:
         d_scale_rows = _new_on(stream, q, (B, H, N), torch.float32)
-    params_grads = tuple(_new_on(stream, q, (H,), torch.float32) for _ in range(3)) if want_param_grads else None
+    if want_param_grads and beta is None:
+        raise EntmaxAttnError("%s: there are no scale parameters to take gradients of" % what)
+    params_grads = tuple([_like_on(stream, x) for x in (beta, gamma, delta)]) if want_param_grads else None
     if workspace is None:
         workspace = _new_on(stream, q, (nbytes,), torch.uint8)
     elif workspace.dtype != torch.uint8 or workspace.get_device() != q.get_device() or not workspace.is_contiguous():
