@@ -1,7 +1,8 @@
 // Softmax attention of new tokens over a paged cache (entmax_attn_softmax_paged_fwd): the few rows of a sequence that generates, and the joins.
 //
 // Few rows (n new tokens x G query heads of a K/V head, 16, 32 or 64 at most): bound by reading K and V once from HBM, so the kernel is built around that
-// stream.  The work is tiles of 64 keys of all sequences and K/V heads in a row; every CTA takes an equal run of them, whatever sequences it cuts.  A producer warp
+// stream.  The work is tiles of 64 keys of all sequences and K/V heads in a row; every CTA takes an equal run of them, whatever sequences it cuts (short
+// sequences that fill the GPU anyway: a CTA for each K/V head of each).  A producer warp
 // brings the tiles' pages by TMA (a box per page and 64 columns) three tiles ahead; four warps share the rows (16 each) or the keys of a tile, each with a
 // running maximum and sum of its own: S = Q K^T and O += P V by m16n8k16 products with Q, P, O in registers (16 rows do not fill a tcgen05 tile, and
 // at 8 flops a byte the stream is six times slower than these products).  The warps meet at the end of a run's sequence.  A sequence that lies in
@@ -100,25 +101,32 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
 
   if (warp == 4) {
     // ------------------------------------------------------------------ which tiles are this CTA's, and their way into shared memory
-    long long total = 0;
-    for (int b = lane; b < a.c.B; b += 32) {
-      const int2 t = few_tiles(a, paged_seq(a.c, b));
-      total += t.y - t.x;
-    }
+    long long total = 0, ctas = 1, begin = 0, end = 0;
+    if (a.whole) {
+      const int2 t = few_tiles(a, paged_seq(a.c, blockIdx.x / a.c.KH));
+      begin = (long long)(blockIdx.x % a.c.KH) * (t.y - t.x);
+      end = begin + (t.y - t.x);
+    } else {
+      for (int b = lane; b < a.c.B; b += 32) {
+        const int2 t = few_tiles(a, paged_seq(a.c, b));
+        total += t.y - t.x;
+      }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    total *= a.c.KH;
-    const long long ctas = min((long long)gridDim.x, total);         // (each of them gets a tile: no gaps between a sequence's pieces)
-    const long long begin = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0, end = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
-    if (lane == 0) a.pieces[blockIdx.x] = FewPiece{-1, 0, 0, 0};
+      for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      total *= a.c.KH;
+      ctas = min((long long)gridDim.x, total);                       // (each of them gets a tile: no gaps between a sequence's pieces)
+      begin = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
+      end = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
+      if (lane == 0) a.pieces[blockIdx.x] = FewPiece{-1, 0, 0, 0};
+    }
     uint32_t wphase = 0, idx = 0;
     int slot = 0;
     bool alive = true;
     if (begin < end) {
       // the sequence of the first tile: 32 sequences at a time
       long long before = 0;                      // tiles (of all K/V heads) in front of sequence b
-      int b = 0;
-      for (int b0 = 0; b0 < a.c.B; b0 += 32) {
+      int b = a.whole ? blockIdx.x / a.c.KH : 0;
+      for (int b0 = 0; !a.whole && b0 < a.c.B; b0 += 32) {
         const int2 t = b0 + lane < a.c.B ? few_tiles(a, paged_seq(a.c, b0 + lane)) : make_int2(0, 0);
         const long long mine = (long long)(t.y - t.x) * a.c.KH;
         long long incl = mine;
@@ -578,7 +586,14 @@ int softmax_paged_args(const entmax_attn_paged_cache* cache, const entmax_attn_s
   const long long tiles = (long long)a.c.B * a.c.KH * ((keys + kTileKeys - 1) / kTileKeys);
   const long long ctas = (tiles + 3) / 4;
   w.few_ctas = (int)(ctas < 2 * kSms ? (ctas > 0 ? ctas : 1) : 2 * kSms);
-  const size_t few_slots = (size_t)w.few_ctas * 2 * a.few_rows;
+  // A CTA per sequence and K/V head, nothing cut and nothing to join, where it has at most nine tiles more than its equal share: cutting costs a launch, a second
+  // meeting of the warps and the join, about as much as they do.  12 heads x 64 over 400 keys (3 more) 9.3 us against 12.2 cut, 777 (9) 13.2 against 12.4 and
+  // 2 us less on the host, 1024 (12) 14.9 against 10.6; 256 units x 128 over 1024 keys (2) 26.5 against 33.1, lengths of 1 to 1024 21.7 against 30.3,
+  // 64 units (13) 20.2 against 13.9.  32 tiles at most: with one long sequence among short ones the others would wait for it.
+  const long long units = (long long)a.c.B * a.c.KH, unit_tiles = (keys + kTileKeys - 1) / kTileKeys, share = units * unit_tiles / (2 * kSms);
+  a.whole = units <= 2 * kSms && unit_tiles <= 32 && unit_tiles - (share > 4 ? share : 4) <= 9;
+  if (a.whole) w.few_ctas = (int)units;
+  const size_t few_slots = a.whole ? 0 : (size_t)w.few_ctas * 2 * a.few_rows;
   w.pieces = 0;
   w.part_ml = w.pieces + up256((size_t)w.few_ctas * sizeof(FewPiece));
   w.part_o = w.part_ml + up256(few_slots * sizeof(float2));
@@ -618,7 +633,7 @@ cudaError_t few_launch(const SoftmaxPagedArgs& a, const PagedPlan& w, const CUte
   cudaError_t err = cudaFuncSetAttribute(softmax_few_kernel<HD, RG>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<HD>::kSmem);
   if (err != cudaSuccess) return err;
   err = launch_kernel(softmax_few_kernel<HD, RG>, (unsigned)w.few_ctas, kFewThreads, FewCfg<HD>::kSmem, stream, map_k, map_v, a);
-  if (err != cudaSuccess) return err;
+  if (err != cudaSuccess || a.whole) return err;
   return launch_kernel(softmax_few_join_kernel<HD, RG>, dim3((unsigned)w.few_ctas, 4 * RG), 128, 0, stream, a);
 }
 template <int HD>

@@ -13,6 +13,7 @@ struct SoftmaxPagedArgs {
   int H, G, window;
   int max_q, max_kv;                  // longest chunk and sequence that are served
   int few_rows;                       // sequences with n * G <= few_rows rows are the "few" kernel's
+  int whole;                          // "few": a CTA per sequence and K/V head, nothing is cut
   int box_shift;                      // a page's boxes have 1 << box_shift keys
   float sm_scale, cap_inv, unit;
   const float *beta, *gamma, *delta, *alibi;
