@@ -69,14 +69,13 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// RG: groups of 16 rows (1, 2, 4); the 4 / RG warps of a group share a tile's keys
+// RG: groups of 16 rows (1, 2, 4) that sequences have at most; the warps share the rows of one in as few groups as it fills, and the 4 / groups warps of a
+// group a tile's keys
 template <int HD, int RG>
 __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                                      const __grid_constant__ SoftmaxPagedArgs a) {
   pdl_begin();
   using C = FewCfg<HD>;
-  constexpr int KG = 4 / RG;                     // warps that share the keys
-  constexpr int NT = kTileKeys / KG / 8;         // eight-key columns of a warp
   extern __shared__ uint8_t smem_raw[];
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t meet = sbase + kFewStages * C::kStage;
@@ -229,19 +228,15 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
       uint4* o = reinterpret_cast<uint4*>(a.o + (long long)s.q0 * a.H * HD);
       for (long long e = threadIdx.x; e < rows * (HD / 8); e += 128) o[e] = make_uint4(0u, 0u, 0u, 0u);
     }
-    const int rg = warp % RG, kg = warp / RG;
-    const int r0 = rg * 16 + (lane >> 2);        // this thread's rows: r0, r0 + 8
     uint32_t wphase = 0, xphase = 0, idx = 0;
     int slot = 0;
-    bool alive = true;
-    while (alive) {
-      alive = wait_all(w_full + 8 * slot, wphase);
-      if (!alive) break;
-      const FewWork w = work[slot];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
-      if (++slot == 2) { slot = 0; wphase ^= 1u; }
-      if (!w.valid) break;
+    auto serve = [&](const FewWork& w, auto groups) -> bool {
+      constexpr int RGS = decltype(groups)::value;
+      constexpr int KG = 4 / RGS;                // warps that share the keys
+      constexpr int NT = kTileKeys / KG / 8;     // eight-key columns of a warp
+      const int rg = warp % RGS, kg = warp / RGS;
+      const int r0 = rg * 16 + (lane >> 2);      // this thread's rows: r0, r0 + 8
+      bool alive = true;
       const int rows = w.n * a.G;
       uint32_t q[HD / 16][4];
       float scale[2], slope[2], top[2] = {-INFINITY, -INFINITY}, mass[2] = {0.f, 0.f}, out[HD / 8][4];
@@ -384,7 +379,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
         __syncwarp();
         if (lane == 0) mbar_arrive(empty + 8 * st);
       }
-      if (!alive) break;
+      if (!alive) return false;
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         mass[y] += __shfl_xor_sync(0xffffffffu, mass[y], 1);
@@ -400,9 +395,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
       };
 #pragma unroll 1
       for (int other = 1; other < KG && alive; ++other) {
-        // (RG > 1: the groups' first warps take turns at the room for one O)
+        // (RGS > 1: the groups' first warps take turns at the room for one O)
 #pragma unroll 1
-        for (int turn = 0; turn < RG && alive; ++turn) {
+        for (int turn = 0; turn < RGS && alive; ++turn) {
           if (rg == turn && kg == other) {
 #pragma unroll
             for (int e = 0; e < HD / 8; ++e) {
@@ -436,7 +431,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
           alive = meet_all();
         }
       }
-      if (!alive) break;
+      if (!alive) return false;
       if (kg == 0) {
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
@@ -460,6 +455,21 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
           }
         }
       }
+      return true;
+    };
+    bool alive = true;
+    while (alive) {
+      alive = wait_all(w_full + 8 * slot, wphase);
+      if (!alive) break;
+      const FewWork w = work[slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(w_empty + 8 * slot);
+      if (++slot == 2) { slot = 0; wphase ^= 1u; }
+      if (!w.valid) break;
+      const int rows = w.n * a.G;
+      if (rows <= 16) alive = serve(w, std::integral_constant<int, 1>{});
+      else if (rows <= 32 || RG < 4) alive = serve(w, std::integral_constant<int, RG < 2 ? RG : 2>{});
+      else alive = serve(w, std::integral_constant<int, RG>{});
     }
   }
   __syncthreads();
