@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(256) row_ranges_kernel(int B, int N, int docs,
 
 // dbeta = sum dc (ln n)^gamma, dgamma = sum dc beta (ln n)^gamma ln ln n, ddelta = sum dc over the rows of a head (the first two over n > 1).
 // A cluster of CTAs per head; partial sums meet in the shared memory of its first CTA and are added in rank order.  Bound by the latency of its loads: 12 heads x 8192
-// rows 3 us behind the kernel before.
+// rows 8 us, a call with 2 x 16 heads x 4096 rows 8 us longer for it.
 constexpr int kScaleCtas = 8, kScaleThreads = 256;
 __global__ void __cluster_dims__(kScaleCtas, 1, 1) __launch_bounds__(kScaleThreads)
     softmax_scale_grad_kernel(const SoftmaxArgs a, const float* __restrict__ dc_rows, float* dbeta, float* dgamma, float* ddelta) {
