@@ -104,11 +104,12 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// The capped score of an accumulator, in the scores' unit, and d z / d (sm_scale acc) at it
+// The capped score of an accumulator, in the scores' unit, and d z / d (sm_scale acc) at it.  The tanh is exact to a part of itself: an error that does not shrink
+// with the score is multiplied by the cap, which may be far above every score.
 __device__ __forceinline__ float capped(const SoftmaxArgs& a, float acc, float& slope) {
   slope = 1.0f;
   if (a.cap_inv == 0.f) return acc;
-  const float t = tanh_full(acc * a.cap_inv);
+  const float t = tanhf(acc * a.cap_inv);
   slope = 1.0f - t * t;
   return t;
 }
