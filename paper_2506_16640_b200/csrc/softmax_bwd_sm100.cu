@@ -1066,7 +1066,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) softmax_dkv_kernel(const __gri
           tmem_ld_frag(s_at, s);
           tmem_ld_frag(s_at + kLanes16, s + 16);
           tmem_ld_wait32(s);
-          if (CAP) tanh_scores(a.cap_inv, s);
+          if (CAP) tanh_scores_of_rows(a.cap_inv, s);
           dkv_probabilities<CAP, SLOPE, SCALED>(a.unit * kLog2e, slope, i0 - key0, rows_at, s, u);
           if (edge) {
 #pragma unroll

@@ -304,7 +304,15 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
                 s[e][z] = key >= begin[z >> 1] && key <= pos[z >> 1] ? s[e][z] : 0.f;
               }
           }
-          tanh_scores(a.cap_inv, reinterpret_cast<float (&)[4 * NT]>(s));
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {          // a row at a time
+            float x[2 * NT];
+#pragma unroll
+            for (int e = 0; e < NT; ++e) { x[2 * e] = s[e][2 * y]; x[2 * e + 1] = s[e][2 * y + 1]; }
+            tanh_scores(a.cap_inv, x);
+#pragma unroll
+            for (int e = 0; e < NT; ++e) { s[e][2 * y] = x[2 * e]; s[e][2 * y + 1] = x[2 * e + 1]; }
+          }
         }
         float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll

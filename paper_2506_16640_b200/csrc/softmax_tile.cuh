@@ -48,26 +48,40 @@ __device__ __forceinline__ void store_quad_rows(const float (&v)[32], float mul,
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 
-// tanh of N values times inv, in place (the whole warp).  Scores are mostly far below the cap: where the warp has none beyond half of it, an odd polynomial of
-// degree 9 (least maximum error on [-1/2, 1/2], 3.5e-8, fitted by iterated weighted least squares), two values an instruction; otherwise exp2 and a reciprocal.
-// counts: whether this thread's values are anyone's (others have no say in which it is).
+// tanh of N values times inv, in place.  Scores are mostly far below the cap: where a thread has none beyond half of it, the polynomial, two values an instruction; otherwise
+// exp2 and a reciprocal, whose absolute error (1.2e-7, times the cap) is a part of the largest of the thread's values.  So the values have to be of one row: what another row's scores are
+// must not matter to it.  counts: whether they are anyone's.
 template <int N>
 __device__ __forceinline__ void tanh_scores(float inv, float (&s)[N], bool counts = true) {
   using namespace sm100;
   float most = fabsf(s[0]);
 #pragma unroll
   for (int e = 1; e < N; ++e) most = fmaxf(most, fabsf(s[e]));
-  if (__all_sync(0xffffffffu, !counts || most * inv <= 0.5f)) {
+  if (!counts || most * inv <= 0.5f) {
     const uint64_t inv2 = pack2(inv, inv);
 #pragma unroll
     for (int e = 0; e < N; e += 2) {
       const uint64_t u = mul2(pack2(s[e], s[e + 1]), inv2), w = mul2(u, u);
-      uint64_t p = fma2(w, pack2(0.016737575f, 0.016737575f), pack2(-0.052762136f, -0.052762136f));
-      p = fma2(w, p, pack2(0.13320571f, 0.13320571f));
-      p = fma2(w, p, pack2(-0.33332777f, -0.33332777f));
-      p = fma2(w, p, pack2(0.99999994f, 0.99999994f));
+      uint64_t p = fma2(w, pack2(kTanh8, kTanh8), pack2(kTanh6, kTanh6));
+      p = fma2(w, p, pack2(kTanh4, kTanh4));
+      p = fma2(w, p, pack2(kTanh2, kTanh2));
+      p = fma2(w, p, pack2(kTanh0, kTanh0));
       unpack2(mul2(u, p), s[e], s[e + 1]);
     }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) s[e] = tanh_large(s[e] * inv);
+  }
+}
+// The same for values of several rows (the whole warp): where the warp has one beyond half of the cap, each takes its own way.
+template <int N>
+__device__ __forceinline__ void tanh_scores_of_rows(float inv, float (&s)[N]) {
+  using namespace sm100;
+  float most = fabsf(s[0]);
+#pragma unroll
+  for (int e = 1; e < N; ++e) most = fmaxf(most, fabsf(s[e]));
+  if (__all_sync(0xffffffffu, most * inv <= 0.5f)) {
+    tanh_scores(inv, s, false);
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e) s[e] = tanh_full(s[e] * inv);

@@ -5,6 +5,7 @@ tests/softmax.py grants every score anyway, so the bounds are those of the call 
 import pytest
 import torch
 
+import paged
 import softmax
 from paper_2506_16640_b200 import binding
 
@@ -47,3 +48,44 @@ def test_scores_far_below_the_cap(cap, kind, dtype):
     want = _problem(q, k, v, d_o, cap, t.get("alibi_slopes"), t.get("c_rows"))
     for name, x in _run(q, k, v, d_o, cap, **t).items():
         softmax.check(name, x, want, "cap %g" % cap)
+
+
+@pytest.mark.parametrize("dtype", [f32, bf16])
+@pytest.mark.parametrize("cap", [1e3, 1e5])
+def test_scores_far_below_the_cap_next_to_rows_beyond_it(cap, dtype):
+    # every sixteenth row has scores far beyond the cap, the others have theirs as without them (those rows' d_o is 0: no gradient of theirs
+    # in dk and dv, and D = 0)
+    B, H, G, N, d = 1, 2, 1, 200, 64
+    q, k, v, d_o = _inputs(B, H, G, N, d, dtype, seed=4)
+    far = torch.arange(N, device="cuda") % 16 == 5
+    q[:, :, far] *= 4 * cap
+    d_o[:, :, far] = 0.0
+    near = ~far.cpu()
+    got, want = _run(q, k, v, d_o, cap), _problem(q, k, v, d_o, cap)
+    for name in ("o", "lse", "dq", "dc"):
+        softmax.check(name, got[name][:, :, near], {n: want[n][:, :, near] for n in (name, name + "_tol")}, "cap %g" % cap)
+    for name in ("dk", "dv"):
+        softmax.check(name, got[name], want, "cap %g" % cap)
+
+
+@pytest.mark.parametrize("cap", [1e3, 1e5])
+@pytest.mark.parametrize("n", [1, 4, 130])
+def test_paged_scores_far_below_the_cap_next_to_rows_beyond_it(n, cap):
+    # rows of a warp: two query heads of the same tokens, one of them with scores far beyond the cap
+    H, KH, d, page = 4, 2, 64, 16
+    g = torch.Generator().manual_seed(5)
+    lens = [n + 70, n + 400]
+    keys, values = ([torch.randn((m, KH, d), generator=g).to(bf16) for m in lens] for _ in range(2))
+    q = torch.randn((2 * n, H, d), generator=g).to(bf16)
+    q[:, 0::2] *= 4 * cap
+    kc, vc, table = paged.pool(keys, values, page, d, KH, 5, "cuda")
+    o, lse = binding.entmax_attn_softmax_paged_fwd(q.cuda(), kc, vc, table, torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                                                   torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda"), softcap=cap)
+    for b in range(2):
+        pos = torch.arange(lens[b] - n, lens[b])
+        rows = slice(b * n, (b + 1) * n)
+        for h in range(1, H, 2):
+            args = (q[rows, h], keys[b][:, h // 2], values[b][:, h // 2], torch.zeros_like(pos), pos + 1, None, None)
+            want = _bounds_without_a_cap(softmax.head(*args, cap, pos=pos), softmax.head(*args, 0.0, pos=pos))
+            softmax.check("o", o[rows, h], want)
+            softmax.check("lse", lse[rows, h], want)
