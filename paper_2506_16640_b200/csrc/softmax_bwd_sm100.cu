@@ -473,7 +473,8 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
       r.sees = mine ? visible_keys(a, b, r.i) : make_int2(0, 0);
       const size_t at = ((size_t)b * a.H + h) * a.N + (mine ? r.i : 0);
       const bool some = r.sees.y > r.sees.x;
-      const float c = mine ? row_scale(a, b, h, r.i, r.sees.y - r.sees.x) : 0.f, g = c * a.sm_scale;
+      // (a row that sees nothing has no scale: what the table holds for it, of padding, may be anything)
+      const float held = mine ? row_scale(a, b, h, r.i, r.sees.y - r.sees.x) : 0.f, c = some ? held : 0.f, g = c * a.sm_scale;
       r.a = c * a.unit * kLog2e;
       r.lse2 = some ? f.g.lse[at] * kLog2e : INFINITY;
       r.slope = a.alibi ? a.alibi[h] / a.unit : 0.f;

@@ -218,8 +218,9 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_dq_kernel(const Soft
   for (int y = 0; y < 4; ++y) {
     const int i = row0 + ty * 4 + y;
     sees[y] = i < a.N ? visible_keys(a, b, i) : make_int2(0, 0);
-    c[y] = i < a.N ? row_scale(a, b, h, i, sees[y].y - sees[y].x) : 0.f;
-    lse2[y] = sees[y].y > sees[y].x ? g.lse[(size_t)bh * a.N + i] * kLog2e : 0.f;
+    const bool some = sees[y].y > sees[y].x;       // (a row that sees nothing has no scale: what the table holds for it, of padding, may be anything)
+    c[y] = some ? row_scale(a, b, h, i, sees[y].y - sees[y].x) : 0.f;
+    lse2[y] = some ? g.lse[(size_t)bh * a.N + i] * kLog2e : 0.f;
   }
   const float slope = a.alibi ? a.alibi[h] / a.unit : 0.f;
   load_rows<D>(Q, q + b * a.q.b + h * a.q.h, a.q.n, row0, a.N);

@@ -1,0 +1,37 @@
+"""Softmax attention with scales that are not finite."""
+import pytest
+import torch
+
+import softmax
+from paper_2506_16640_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+bf16, f32 = torch.bfloat16, torch.float32
+INF, NAN = float("inf"), float("nan")
+
+
+def _inputs(B, H, G, N, d, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randn((B, n, N, d), generator=g).to(dtype).cuda() for n in (H, G, G, H)]
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+@pytest.mark.parametrize("rows_grad", [True, False])
+def test_scales_of_rows_that_see_nothing(dtype, bad, rows_grad):
+    # padding behind the documents and a hole between them, with whatever a model projects from it as its scale
+    B, H, G, N, d = 1, 2, 1, 200, 64
+    q, k, v, d_o = _inputs(B, H, G, N, d, dtype)
+    cu = torch.tensor([[3, 90, 150]], dtype=torch.int32, device="cuda")
+    ranges = binding.entmax_attn_row_ranges(cu, N, True)
+    empty = (ranges[..., 0] >= ranges[..., 1])[:, None].expand(B, H, N)
+    assert int(empty.sum()) == H * 53
+    c = 0.5 + torch.rand((B, H, N), generator=torch.Generator().manual_seed(1)).cuda()
+    want = softmax.problem(*(x.cpu() for x in (q, k, v)), False, ranges.cpu(), None, None, None, c.cpu(), None, 0.0, None, d_o.cpu())
+    c[empty] = bad
+    o, lse = binding.entmax_attn_softmax_fwd(q, k, v, False, c_rows=c, row_ranges=ranges)
+    dq, dk, dv, dc, _ = binding.entmax_attn_softmax_bwd(q, k, v, o, lse, d_o, False, c_rows=c, row_ranges=ranges, want_scale_rows=rows_grad)
+    for name, x in (("o", o), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)) + ((("dc", dc),) if rows_grad else ()):
+        softmax.check(name, x, want)
+    assert (o[empty] == 0).all() and (dq[empty] == 0).all() and (lse[empty] == -INF).all()
