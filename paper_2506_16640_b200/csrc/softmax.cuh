@@ -83,7 +83,8 @@ struct SoftmaxGrads {
 };
 
 // CUDA-core kernels (float32 problems)
-cudaError_t launch_softmax_rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, cudaStream_t stream);
+cudaError_t launch_softmax_rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, int32_t* status,
+                                    cudaStream_t stream);
 cudaError_t launch_softmax_rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* d_o,
                                     void* dq, void* dk, void* dv, cudaStream_t stream);
 // Tensor-core kernels (bf16)

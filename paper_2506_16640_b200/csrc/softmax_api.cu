@@ -193,7 +193,7 @@ extern "C" int entmax_attn_softmax_fwd(const entmax_attn_softmax_params* params,
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   rc = clear_status(device_status, stream);
   if (rc != ENTMAX_ATTN_OK) return rc;
-  const cudaError_t err = params->dtype == ENTMAX_ATTN_DTYPE_FP32 ? launch_softmax_rows_fwd(a, q, k, v, o, lse, stream)
+  const cudaError_t err = params->dtype == ENTMAX_ATTN_DTYPE_FP32 ? launch_softmax_rows_fwd(a, q, k, v, o, lse, device_status, stream)
                                                                   : launch_softmax_fwd(a, q, k, v, o, lse, device_status, stream);
   return err == cudaSuccess ? ENTMAX_ATTN_OK : fail_cuda(err);
 }

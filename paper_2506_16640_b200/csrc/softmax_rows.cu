@@ -131,7 +131,8 @@ __device__ __forceinline__ int2 tile_range(const int2 (&sees)[4], int* lo_hi) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(kRowThreads) softmax_rows_fwd_kernel(const SoftmaxArgs a, const float* q, const float* k, const float* v, float* o, float* lse) {
+__global__ void __launch_bounds__(kRowThreads) softmax_rows_fwd_kernel(const SoftmaxArgs a, const float* q, const float* k, const float* v, float* o, float* lse,
+                                                                       int32_t* status) {
   pdl_begin();
   using C = RowCfg<D>;
   extern __shared__ float smem[];
@@ -147,7 +148,9 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_fwd_kernel(const Sof
   for (int y = 0; y < 4; ++y) {
     const int i = row0 + ty * 4 + y;
     sees[y] = i < a.N ? visible_keys(a, b, i) : make_int2(0, 0);
-    scale[y] = i < a.N ? row_scale(a, b, h, i, sees[y].y - sees[y].x) * a.unit * kLog2e : 0.f;
+    const float c = i < a.N ? row_scale(a, b, h, i, sees[y].y - sees[y].x) : 0.f;
+    if (tx == 0 && status && !isfinite(c)) atomicOr(status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_SCALE);
+    scale[y] = c * a.unit * kLog2e;
     top[y] = -INFINITY;
     mass[y] = 0.f;
   }
@@ -337,14 +340,14 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_dkv_kernel(const Sof
 }
 
 template <int D>
-cudaError_t rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, cudaStream_t stream) {
+cudaError_t rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, int32_t* status, cudaStream_t stream) {
   using C = RowCfg<D>;
   const int smem = (3 * C::kTile + C::kScores) * 4;
   cudaError_t err = cudaFuncSetAttribute(softmax_rows_fwd_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (err != cudaSuccess) return err;
   const unsigned grid = (unsigned)((long long)a.B * a.H * ((a.N + kT - 1) / kT));
   return launch_kernel(softmax_rows_fwd_kernel<D>, grid, kRowThreads, smem, stream, a, static_cast<const float*>(q), static_cast<const float*>(k),
-                       static_cast<const float*>(v), static_cast<float*>(o), lse);
+                       static_cast<const float*>(v), static_cast<float*>(o), lse, status);
 }
 template <int D>
 cudaError_t rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* d_o, void* dq, void* dk,
@@ -364,8 +367,9 @@ cudaError_t rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q,
 
 }  // namespace
 
-cudaError_t launch_softmax_rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, cudaStream_t stream) {
-  return a.D == 64 ? rows_fwd<64>(a, q, k, v, o, lse, stream) : rows_fwd<128>(a, q, k, v, o, lse, stream);
+cudaError_t launch_softmax_rows_fwd(const SoftmaxArgs& a, const void* q, const void* k, const void* v, void* o, float* lse, int32_t* status,
+                                    cudaStream_t stream) {
+  return a.D == 64 ? rows_fwd<64>(a, q, k, v, o, lse, status, stream) : rows_fwd<128>(a, q, k, v, o, lse, status, stream);
 }
 cudaError_t launch_softmax_rows_bwd(const SoftmaxArgs& a, const SoftmaxGrads& g, const void* q, const void* k, const void* v, const void* d_o,
                                     void* dq, void* dk, void* dv, cudaStream_t stream) {

@@ -16,6 +16,10 @@ def _inputs(B, H, G, N, d, dtype, seed=0):
     return [torch.randn((B, n, N, d), generator=g).to(dtype).cuda() for n in (H, G, G, H)]
 
 
+def _status():
+    return torch.full((binding.STATUS_WORDS,), -1, dtype=torch.int32, device="cuda")
+
+
 @pytest.mark.parametrize("dtype", [bf16, f32])
 @pytest.mark.parametrize("bad", [NAN, INF, -INF])
 @pytest.mark.parametrize("rows_grad", [True, False])
@@ -35,3 +39,21 @@ def test_scales_of_rows_that_see_nothing(dtype, bad, rows_grad):
     for name, x in (("o", o), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)) + ((("dc", dc),) if rows_grad else ()):
         softmax.check(name, x, want)
     assert (o[empty] == 0).all() and (dq[empty] == 0).all() and (lse[empty] == -INF).all()
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("bad", [NAN, INF])
+@pytest.mark.parametrize("kind", ["rows", "length"])
+def test_a_scale_that_is_not_finite_is_reported(dtype, bad, kind):
+    B, H, G, N, d = 1, 2, 1, 150, 64
+    q, k, v, _ = _inputs(B, H, G, N, d, dtype, seed=1)
+    t = {"c_rows": torch.ones((B, H, N), device="cuda")}
+    if kind == "rows":
+        t["c_rows"][0, 1, 77] = bad
+    else:
+        t = dict(beta=torch.tensor([1.0, bad], device="cuda"), gamma=torch.ones(2, device="cuda"), delta=torch.ones(2, device="cuda"))
+    status = _status()
+    binding.entmax_attn_softmax_fwd(q, k, v, True, **t, status=status)
+    assert int(status[0]) == binding.FLAG_BAD_SCALE
+    binding.entmax_attn_softmax_fwd(q, k, v, True, status=status)
+    assert int(status[0]) == 0
