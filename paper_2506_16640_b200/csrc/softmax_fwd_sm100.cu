@@ -518,6 +518,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
           if ((a.beta || a.c_rows) && f.status && !isfinite(scale)) atomicOr(f.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_SCALE);
         }
       }
+      if (!PAGED && sees.y <= sees.x) scale = 0.f;                    // (it has none, whatever the table holds for it)
       RowSoftmax<CAP, TERMS, PAGED> sm;
       sm.start(mine, scale * a.unit * kLog2e, a.alibi ? a.alibi[h] / a.unit : 0.f, pos);
       for (int j = hi - 1; j >= lo && alive; --j) {
@@ -563,9 +564,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
       float inv = 0.f;
       const float mass = sm.sum();
       if (!PAGED || part < 0) {
-        inv = mass > 0.f ? 1.0f / mass : 0.f;
+        inv = mass != 0.f ? 1.0f / mass : 0.f;                        // (0: it sees nothing; a NaN is none of that)
         if (mine) {
-          const float lse = mass > 0.f ? (sm.base() + log2f(mass)) * kLn2 : -INFINITY;
+          const float lse = mass != 0.f ? (sm.base() + log2f(mass)) * kLn2 : -INFINITY;
           if constexpr (PAGED) f.lse[(size_t)(q0 + i) * a.H + h] = lse;
           else f.lse[((size_t)b * a.H + h) * a.N + i] = lse;
         }

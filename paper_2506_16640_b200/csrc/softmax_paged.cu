@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
         const float c = a.beta ? length_scale(a.beta[h], a.gamma[h], a.delta[h], pos[y] + 1 - begin[y]) : 1.0f;
         if (a.beta && a.status && mine && !isfinite(c)) atomicOr(a.status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_SCALE);
         flip[y] = c < 0.f;
-        scale[y] = fmaxf(fabsf(c * a.unit * kLog2e), 1e-30f);    // (see RowSoftmax)
+        scale[y] = at_least_tiny(fabsf(c * a.unit * kLog2e));    // (see RowSoftmax)
         slope[y] = a.alibi ? a.alibi[h] / a.unit : 0.f;
       }
 #pragma unroll
@@ -492,14 +492,15 @@ __global__ void __launch_bounds__(kFewThreads, 2) softmax_few_kernel(const __gri
   }
 }
 
-// One row from `count` pieces: sum_p 2^(m_p - M) O_p over the sum of 2^(m_p - M) l_p, by a warp.  at(p): the row's place among the pieces
+// One row from `count` pieces: sum_p 2^(m_p - M) O_p over the sum of 2^(m_p - M) l_p, by a warp.  at(p): the row's place among the pieces.  Pieces without a key that the row
+// sees have l = 0; one whose l is NaN makes the row NaN, as it does where nothing is cut.
 template <int HD, typename At>
 __device__ __forceinline__ void join_row(const float* part_o, const float2* part_ml, int count, At at, __nv_bfloat16* o, float* lse) {
   const int lane = threadIdx.x & 31;
   float most = -INFINITY;
   for (int p = lane; p < count; p += 32) {
     const float2 ml = part_ml[at(p)];
-    if (ml.y > 0.f) most = fmaxf(most, ml.x);
+    if (ml.y != 0.f) most = fmaxf(most, ml.x);
   }
 #pragma unroll
   for (int s = 16; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
@@ -508,18 +509,18 @@ __device__ __forceinline__ void join_row(const float* part_o, const float2* part
   for (int p = 0; p < count; ++p) {
     const size_t x = at(p);
     const float2 ml = part_ml[x];
-    const float f = ml.y > 0.f ? exp2_fast(ml.x - most) : 0.f;
+    const float f = ml.y != 0.f ? exp2_fast(ml.x - most) : 0.f;
     sum = fmaf(ml.y, f, sum);
     float v[E];
     load_slice<E>(part_o + x * HD + lane * E, v);
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[e] = ml.y > 0.f ? fmaf(v[e], f, out[e]) : out[e];
+    for (int e = 0; e < E; ++e) out[e] = ml.y != 0.f ? fmaf(v[e], f, out[e]) : out[e];
   }
-  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+  const float inv = sum != 0.f ? 1.0f / sum : 0.f;
 #pragma unroll
   for (int e = 0; e < E; ++e) out[e] *= inv;
   store_slice<E>(o + lane * E, out);
-  if (lane == 0) *lse = sum > 0.f ? (most + log2f(sum)) * kLn2 : -INFINITY;
+  if (lane == 0) *lse = sum != 0.f ? (most + log2f(sum)) * kLn2 : -INFINITY;
 }
 
 // The sequences that were cut: CTA x joins the one that begins in CTA x's run without ending there, a warp per row

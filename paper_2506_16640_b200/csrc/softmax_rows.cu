@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_fwd_kernel(const Sof
     sees[y] = i < a.N ? visible_keys(a, b, i) : make_int2(0, 0);
     const float c = i < a.N ? row_scale(a, b, h, i, sees[y].y - sees[y].x) : 0.f;
     if (tx == 0 && status && !isfinite(c)) atomicOr(status + ENTMAX_ATTN_STATUS_FLAGS, ENTMAX_ATTN_FLAG_BAD_SCALE);
-    scale[y] = c * a.unit * kLog2e;
+    scale[y] = isfinite(c) ? c * a.unit * kLog2e : NAN;      // (infinity times negative scores alone would leave a row as if it saw nothing)
     top[y] = -INFINITY;
     mass[y] = 0.f;
   }
@@ -196,9 +196,9 @@ __global__ void __launch_bounds__(kRowThreads) softmax_rows_fwd_kernel(const Sof
   float inv[4];
 #pragma unroll
   for (int y = 0; y < 4; ++y) {
-    inv[y] = mass[y] > 0.f ? 1.0f / mass[y] : 0.f;
+    inv[y] = mass[y] != 0.f ? 1.0f / mass[y] : 0.f;
     const int i = row0 + ty * 4 + y;
-    if (tx == 0 && i < a.N) lse[(size_t)bh * a.N + i] = mass[y] > 0.f ? top[y] * kLn2 + logf(mass[y]) : -INFINITY;
+    if (tx == 0 && i < a.N) lse[(size_t)bh * a.N + i] = mass[y] != 0.f ? top[y] * kLn2 + logf(mass[y]) : -INFINITY;
   }
   store_rows<D>(o + b * a.o.b + h * a.o.h, a.o.n, row0, a.N, out, inv);
 }

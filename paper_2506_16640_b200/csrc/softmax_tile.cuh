@@ -88,6 +88,9 @@ __device__ __forceinline__ void tanh_scores_of_rows(float inv, float (&s)[N]) {
   }
 }
 
+// What scores are multiplied by, never 0; a NaN stays one
+__device__ __forceinline__ float at_least_tiny(float x) { return x < 1e-30f ? 1e-30f : x; }
+
 // the slope's term of N scores from column j0 on
 template <int N>
 __device__ __forceinline__ void slope_scores(float slope, int pos, int j0, float (&s)[N]) {
@@ -108,7 +111,7 @@ struct RowSoftmax {
   __device__ __forceinline__ void start(bool is_row, float a_signed, float slope_unit, int position) {
     mine = is_row;
     sign = a_signed < 0.f ? -1.0f : 1.0f;
-    a = fmaxf(fabsf(a_signed), 1e-30f);      // c = 0: every visible key weighs the same, while 0 * -inf would be NaN
+    a = at_least_tiny(fabsf(a_signed));      // c = 0: every visible key weighs the same, while 0 * -inf would be NaN
     slope = slope_unit;
     pos = position;
     m = -INFINITY;

@@ -1,7 +1,9 @@
-"""Softmax attention with scales that are not finite."""
+"""Softmax attention with scales that are not finite: in rows that see nothing they have no say, elsewhere they are reported and what they make of the
+row is not taken for an empty one."""
 import pytest
 import torch
 
+import paged
 import softmax
 from paper_2506_16640_b200 import binding
 
@@ -57,3 +59,41 @@ def test_a_scale_that_is_not_finite_is_reported(dtype, bad, kind):
     assert int(status[0]) == binding.FLAG_BAD_SCALE
     binding.entmax_attn_softmax_fwd(q, k, v, True, status=status)
     assert int(status[0]) == 0
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("bad", [NAN, INF])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_rows_of_a_scale_that_is_not_finite_are_no_empty_rows(dtype, bad, cap):
+    B, H, G, N, d = 1, 2, 1, 300, 64
+    q, k, v, _ = _inputs(B, H, G, N, d, dtype, seed=2)
+    c = torch.ones((B, H, N), device="cuda")
+    ref, ref_lse = binding.entmax_attn_softmax_fwd(q, k, v, True, c_rows=c, softcap=cap)
+    c[0, 1, 277] = bad
+    o, lse = binding.entmax_attn_softmax_fwd(q, k, v, True, c_rows=c, softcap=cap)
+    assert torch.isnan(lse[0, 1, 277]) and torch.isnan(o[0, 1, 277]).all()
+    # the other rows have what they had
+    o[0, 1, 277], lse[0, 1, 277] = ref[0, 1, 277], ref_lse[0, 1, 277]
+    assert torch.equal(o, ref) and torch.equal(lse, ref_lse)
+
+
+@pytest.mark.parametrize("bad", [NAN, INF])
+@pytest.mark.parametrize("new,lens", [([1, 1], [20, 40]), ([1, 1], [6000, 30000]), ([4], [9000]), ([140, 1], [200, 30]), ([140], [30000])])
+def test_paged_rows_of_a_scale_that_is_not_finite_whether_cut_or_not(new, lens, bad):
+    # sequences of one CTA, sequences cut over many and joined, chunks whose keys are shared out and joined
+    H, KH, d, page = 4, 2, 64, 64
+    g = torch.Generator().manual_seed(3)
+    keys, values = ([torch.randn((m, KH, d), generator=g).to(bf16) for m in lens] for _ in range(2))
+    q = torch.randn((sum(new), H, d), generator=g).to(bf16).cuda()
+    kc, vc, table = paged.pool(keys, values, page, d, KH, 3, "cuda")
+    cu = torch.tensor([0] + [sum(new[:i + 1]) for i in range(len(new))], dtype=torch.int32, device="cuda")
+    kv = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    one = torch.ones(H, device="cuda")
+    delta = torch.tensor([1.0, 1.0, bad, 1.0], device="cuda")
+    ref, ref_lse = binding.entmax_attn_softmax_paged_fwd(q, kc, vc, table, kv, cu, 0 * one, one, one)
+    status = _status()
+    o, lse = binding.entmax_attn_softmax_paged_fwd(q, kc, vc, table, kv, cu, 0 * one, one, delta, status=status)
+    assert int(status[0]) == binding.FLAG_BAD_SCALE
+    assert torch.isnan(o[:, 2]).all() and torch.isnan(lse[:, 2]).all()
+    for h in (0, 1, 3):                          # (the other heads have what they had)
+        assert torch.equal(o[:, h], ref[:, h]) and torch.equal(lse[:, h], ref_lse[:, h])
