@@ -62,6 +62,8 @@ WsLayout make_layout(const Problem& p, bool is_bwd);
 int make_problem(const entmax_attn_params* params, Problem* out);
 int check_scale_ptrs(const float* beta, const float* gamma, const float* delta, Problem* p);
 int fail_cuda(cudaError_t err);
+// ENTMAX_ATTN_OK where the current device has what the bf16 kernels need
+int check_device_for_bf16();
 // A second stream of the calling thread on the current device, with the events it is forked from and joined back to a caller's stream by
 struct SideStream {
   cudaStream_t stream = nullptr;

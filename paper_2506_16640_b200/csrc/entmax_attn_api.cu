@@ -33,6 +33,8 @@ int check_workspace(const Problem& p, bool is_bwd, void* ws, size_t ws_bytes, Ws
   return ENTMAX_ATTN_OK;
 }
 
+}  // namespace
+
 int check_device_for_bf16() {
   int dev = 0, major = 0;
   cudaError_t err = cudaGetDevice(&dev);
@@ -41,8 +43,6 @@ int check_device_for_bf16() {
   if (err != cudaSuccess) return fail_cuda(err);
   return major == 10 ? ENTMAX_ATTN_OK : ENTMAX_ATTN_EUNSUPPORTED;
 }
-
-}  // namespace
 
 // A second stream per (host thread, device) on which the backward call clears its fp32 accumulators while the
 // score sweep, which does not touch them, runs on the caller's stream: forked from and joined back to the

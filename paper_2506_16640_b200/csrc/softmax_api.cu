@@ -190,6 +190,7 @@ extern "C" int entmax_attn_softmax_fwd(const entmax_attn_softmax_params* params,
   if (rc != ENTMAX_ATTN_OK) return rc;
   if (!q || !k || !v || !o || !lse) return ENTMAX_ATTN_EINVAL_NULL;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return ENTMAX_ATTN_EINVAL_ALIGN;
+  if (params->dtype == ENTMAX_ATTN_DTYPE_BF16 && (rc = check_device_for_bf16()) != ENTMAX_ATTN_OK) return rc;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   rc = clear_status(device_status, stream);
   if (rc != ENTMAX_ATTN_OK) return rc;
@@ -227,6 +228,7 @@ extern "C" int entmax_attn_softmax_bwd(const entmax_attn_softmax_params* params,
   g.lse = lse;
   g.row_dot = reinterpret_cast<float*>(ws + w.rows);
   g.dc_rows = grads->d_scale_rows ? grads->d_scale_rows : given ? reinterpret_cast<float*>(ws + w.dc_rows) : nullptr;
+  if (bf16 && (rc = check_device_for_bf16()) != ENTMAX_ATTN_OK) return rc;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   rc = clear_status(device_status, stream);
   if (rc != ENTMAX_ATTN_OK) return rc;

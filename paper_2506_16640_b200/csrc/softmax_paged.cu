@@ -694,7 +694,7 @@ extern "C" int entmax_attn_softmax_paged_fwd(const entmax_attn_paged_cache* cach
                                              int32_t* device_status, void* cuda_stream) {
   SoftmaxPagedArgs a;
   PagedPlan w;
-  const int rc = softmax_paged_args(cache, params, cu_q == nullptr, &a, &w);
+  int rc = softmax_paged_args(cache, params, cu_q == nullptr, &a, &w);
   if (rc != ENTMAX_ATTN_OK) return rc;
   if (!q || !k_cache || !v_cache || !kv_len || !block_table || !o || !lse) return ENTMAX_ATTN_EINVAL_NULL;
   const int given = (beta != nullptr) + (gamma != nullptr) + (delta != nullptr);
@@ -705,6 +705,7 @@ extern "C" int entmax_attn_softmax_paged_fwd(const entmax_attn_paged_cache* cach
                           reinterpret_cast<uintptr_t>(alibi_slopes) | reinterpret_cast<uintptr_t>(lse);
   if (words & 3u) return ENTMAX_ATTN_EINVAL_ALIGN;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < w.bytes) return ENTMAX_ATTN_EINVAL_WORKSPACE;
+  if ((rc = check_device_for_bf16()) != ENTMAX_ATTN_OK) return rc;
   a.c.table = block_table; a.c.kv_len = kv_len; a.c.cu_q = cu_q;
   a.beta = beta; a.gamma = gamma; a.delta = delta; a.alibi = alibi_slopes;
   a.q = static_cast<const __nv_bfloat16*>(q);
