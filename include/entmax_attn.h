@@ -397,7 +397,7 @@ int entmax_attn_paged_fwd(const entmax_attn_paged_cache* cache, const entmax_att
  * would be longer than max_pages * page_size or whose kv_len or new_len is out of range (ENTMAX_ATTN_FLAG_BAD_LENGTH), is left out: its kv_len_out is
  * -1 - n, n its tokens in the cache, which the attention calls leave out as well and a later call takes up again; its new tokens keep
  * their rows, with positions and slots -1, and it gets no page.  Rows behind cu_q[batch] are left alone; when the new tokens are more than total_q, those behind it are
- * not written (ENTMAX_ATTN_FLAG_BAD_LENGTH).  A page number outside the pool on the stack or in the table sets ENTMAX_ATTN_FLAG_BAD_PAGE and gives its tokens slot -1
+ * not written (ENTMAX_ATTN_FLAG_BAD_LENGTH; without positions and slots their number is nobody's concern).  A page number outside the pool on the stack or in the table sets ENTMAX_ATTN_FLAG_BAD_PAGE and gives its tokens slot -1
  * (in the table and on the stack it is passed on, for the attention calls to report); pages that the stack has no room for are flagged the same way and lost.
  * One launch; results do not depend on its order.  Errors as for entmax_attn_fwd. */
 typedef struct {

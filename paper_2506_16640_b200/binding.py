@@ -627,9 +627,11 @@ def entmax_attn_paged_tables(kv_len, new_len, block_table, free_pages, free_coun
     positions = _new_on(stream, kv_len, (total_q,), torch.int32) if positions is None else positions
     slots = _new_on(stream, kv_len, (total_q,), torch.int64) if slots is None else slots
     free_count_out = _like_on(stream, free_count) if free_count_out is None else free_count_out
+    # (an empty tensor has no address, and without positions and slots the library does not hold the new tokens to total_q: any address stands
+    # for no rows)
     rc = _call_on(kv_len.get_device(), lambda: load().entmax_attn_paged_tables(
         params, kv_len.data_ptr(), new_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), kv_len_out.data_ptr(),
-        cu_q.data_ptr(), positions.data_ptr(), slots.data_ptr(), free_count_out.data_ptr(), _ptr(status), _stream_ptr(stream)))
+        cu_q.data_ptr(), positions.data_ptr() or cu_q.data_ptr(), slots.data_ptr(), free_count_out.data_ptr(), _ptr(status), _stream_ptr(stream)))
     _check(rc, what)
     return kv_len_out, cu_q, positions, slots, free_count_out
 
