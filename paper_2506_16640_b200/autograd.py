@@ -97,17 +97,20 @@ def _kernel_layout(x):
 def softmax_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, beta: Optional[torch.Tensor] = None,
                       gamma: Optional[torch.Tensor] = None, delta: Optional[torch.Tensor] = None, *,
                       c_rows: Optional[torch.Tensor] = None, alibi_slopes: Optional[torch.Tensor] = None,
-                      row_ranges: Optional[torch.Tensor] = None, causal: bool = True, softcap: float = 0.0, sm_scale: float = 0.0,
+                      row_ranges: Optional[torch.Tensor] = None, causal: Optional[bool] = None, softcap: float = 0.0, sm_scale: float = 0.0,
                       return_lse: bool = False):
     """Softmax attention (the alpha -> 1 member of the family) of q [B,H,N,d], k, v [B,G,N,d], H a multiple of G (CUDA tensors, bf16 or fp32, each with
     strides of its own, d contiguous); differentiable with respect to q, k, v and the scale's parameters beta, gamma, delta (float32 [H]) or
     table c_rows (float32 [B,H,N]).
 
-    alibi_slopes: float32 [H]; softcap > 0 caps the scores by a tanh; row_ranges: int32 [B,N,2] from binding.entmax_attn_row_ranges (documents,
-    prefixes, windows), with causal=False.  Returns O, or (O, lse); lse has no gradient, and there are no second derivatives.
+    alibi_slopes: float32 [H]; softcap > 0 caps the scores by a tanh.  row_ranges: int32 [B,N,2] from binding.entmax_attn_row_ranges (documents,
+    prefixes, windows), which then say all that a row sees; without them a row sees itself and what is before it (causal).  causal=False without
+    ranges: everything; causal=True with them: of a row's range what is not behind the row (a prefix is cut off there).  Returns O, or (O, lse); lse has no gradient, and there are no second derivatives.
 
     To capture a training step into a CUDA graph, let no eager graph of the same leaves live (PyTorch would add up their gradients on that
     graph's stream)."""
+    if causal is None:
+        causal = row_ranges is None
     o, lse = _SoftmaxAttention.apply(q, k, v, beta, gamma, delta, c_rows, alibi_slopes, row_ranges, bool(causal), float(softcap),
                                      float(sm_scale))
     return (o, lse) if return_lse else o
