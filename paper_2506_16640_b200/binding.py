@@ -729,7 +729,7 @@ def entmax_attn_softmax_bwd(q, k, v, o, lse, d_o, causal, beta=None, gamma=None,
     dv = _like_on(stream, v) if dv is None else dv
     if d_scale_rows is None and want_scale_rows:
         d_scale_rows = _new_on(stream, q, (B, H, N), torch.float32)
-    if want_param_grads and beta is None:
+    if want_param_grads and (beta is None or gamma is None or delta is None):
         raise EntmaxAttnError("%s: there are no scale parameters to take gradients of" % what)
     params_grads = tuple([_like_on(stream, x) for x in (beta, gamma, delta)]) if want_param_grads else None
     if workspace is None:
