@@ -416,7 +416,7 @@ int entmax_attn_paged_tables(const entmax_attn_paged_tables_params* params, cons
  *   p_ij = exp(s_ij - lse_i) over the keys the row sees,   O_i = sum_j p_ij v_j;   a row that sees none: O = 0, lse = -inf, no gradient.
  * Query heads g * kv_head .. g * kv_head + g - 1, g = heads / kv_heads, share a K/V head.
  *   seq           any length; row i sees the keys j <= i (causal = 1) or all, of those the ones in its range where ranges are given
- *   softcap       0: scores are not capped
+ *   softcap       0: scores are not capped; otherwise, like an sm_scale that is not 0, between 2^-100 and 2^100
  *   q, k, v, o    strides in elements, head_dim innermost (all 0: contiguous [batch, heads or kv_heads, seq, head_dim]); at least head_dim, multiples
  *                 of 8, where their dimension has more than one entry
  *   row_ranges    in, device int32 [batch, seq, 2], 8-byte aligned: the first key a row sees and one behind the last, or NULL (entmax_attn_row_ranges
@@ -432,7 +432,7 @@ int entmax_attn_paged_tables(const entmax_attn_paged_tables_params* params, cons
  *   dbeta, dgamma, ddelta  out, device float32 [heads], all three or none; they need beta, gamma, delta
  *   workspace     256-byte aligned, >= entmax_attn_softmax_workspace_bytes(params) bytes; the forward call needs none
  * q, k, v, o and d_o have to be finite, in rows that see nothing and keys that nobody sees as well (a probability of 0 times a NaN is one).
- * Nothing is added up by atomics: results are bitwise reproducible.  Errors as for entmax_attn_fwd (softcap negative or not finite: EINVAL_ALPHA;
+ * Nothing is added up by atomics: results are bitwise reproducible.  Errors as for entmax_attn_fwd (softcap or sm_scale out of range: EINVAL_ALPHA;
  * heads from 2^28, batch * heads * seq from 2^30 on: EINVAL_SHAPE). */
 typedef struct {
   int64_t b, h, n;                     /* elements between batch rows, heads, tokens                                */

@@ -71,6 +71,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
+// Host: the unit of the scores and what goes with it (defined in softmax_api.cu).  Fails for scales and caps beyond 2^+-100: c times the unit, the slope over it and its
+// reciprocal have to stay float32 numbers.
+int softmax_unit(float given_scale, float softcap, int D, float* sm_scale, float* cap_inv, float* unit);
 // Host: checks of the parameters and the terms (defined in softmax_api.cu)
 int check_softmax(const entmax_attn_softmax_params* params, const entmax_attn_softmax_terms* terms, SoftmaxArgs* out);
 

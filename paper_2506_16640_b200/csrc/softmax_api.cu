@@ -138,6 +138,20 @@ int clear_status(int32_t* status, cudaStream_t stream) {
 
 }  // namespace
 
+int softmax_unit(float given_scale, float softcap, int D, float* sm_scale, float* cap_inv, float* unit) {
+  const float least = std::ldexp(1.0f, -100), most = std::ldexp(1.0f, 100);
+  for (const float x : {given_scale, softcap})
+    if (x != 0.f && !(x >= least && x <= most)) return ENTMAX_ATTN_EINVAL_ALPHA;      // (a NaN too)
+  *sm_scale = *unit = given_scale > 0.f ? given_scale : 1.0f / std::sqrt((float)D);
+  *cap_inv = 0.f;
+  if (softcap > 0.f) {
+    *unit = softcap;
+    *cap_inv = *sm_scale / softcap;
+    if (!std::isnormal(*cap_inv)) return ENTMAX_ATTN_EINVAL_ALPHA;
+  }
+  return ENTMAX_ATTN_OK;
+}
+
 int check_softmax(const entmax_attn_softmax_params* p, const entmax_attn_softmax_terms* terms, SoftmaxArgs* out) {
   if (!p) return ENTMAX_ATTN_EINVAL_NULL;
   SoftmaxArgs a = {};
@@ -147,14 +161,8 @@ int check_softmax(const entmax_attn_softmax_params* p, const entmax_attn_softmax
   if (a.H >= 1 << 28 || (long long)a.B * a.H > 0x7fffffffLL / 2 || (long long)a.B * a.H * a.N > 0x7fffffffLL / 2) return ENTMAX_ATTN_EINVAL_SHAPE;
   a.G = a.H / a.KH;
   if (p->dtype != ENTMAX_ATTN_DTYPE_BF16 && p->dtype != ENTMAX_ATTN_DTYPE_FP32) return ENTMAX_ATTN_EINVAL_DTYPE;
-  if (!std::isfinite(p->sm_scale) || p->sm_scale < 0.f || !std::isfinite(p->softcap) || p->softcap < 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
-  a.sm_scale = p->sm_scale > 0.f ? p->sm_scale : 1.0f / std::sqrt((float)a.D);
-  a.unit = a.sm_scale;
-  if (p->softcap > 0.f) {
-    a.unit = p->softcap;
-    a.cap_inv = a.sm_scale / p->softcap;
-    if (!std::isfinite(a.cap_inv) || a.cap_inv == 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
-  }
+  const int rc = softmax_unit(p->sm_scale, p->softcap, a.D, &a.sm_scale, &a.cap_inv, &a.unit);
+  if (rc != ENTMAX_ATTN_OK) return rc;
   a.causal = p->causal ? 1 : 0;
   if (!take_strides(p->q, a.B, a.H, a.N, a.D, 8, &a.q) || !take_strides(p->k, a.B, a.KH, a.N, a.D, 8, &a.k) ||
       !take_strides(p->v, a.B, a.KH, a.N, a.D, 8, &a.v) || !take_strides(p->o, a.B, a.H, a.N, a.D, 8, &a.o))

@@ -569,24 +569,18 @@ int softmax_paged_args(const entmax_attn_paged_cache* cache, const entmax_attn_s
                        PagedPlan* plan) {
   if (!p) return ENTMAX_ATTN_EINVAL_NULL;
   SoftmaxPagedArgs a = {};
-  const int rc = check_paged_cache(cache, p->total_q, &a.c);
+  int rc = check_paged_cache(cache, p->total_q, &a.c);
   if (rc != ENTMAX_ATTN_OK) return rc;
   if (p->q_heads < 1 || p->q_heads % a.c.KH || p->q_heads / a.c.KH > 128 || (long long)p->total_q * p->q_heads > 0x7fffffffLL / 2)
     return ENTMAX_ATTN_EINVAL_SHAPE;
   if (p->max_q_len < 0 || p->max_kv_len < 0 || p->window < 0) return ENTMAX_ATTN_EINVAL_SHAPE;
   if (uniform && p->total_q % a.c.B) return ENTMAX_ATTN_EINVAL_SHAPE;
-  if (!std::isfinite(p->sm_scale) || p->sm_scale < 0.f || !std::isfinite(p->softcap) || p->softcap < 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
   if (p->q_stride_t < a.c.D || p->q_stride_h < a.c.D || p->q_stride_t % 8 || p->q_stride_h % 8) return ENTMAX_ATTN_EINVAL_SHAPE;
   a.H = p->q_heads;
   a.G = a.H / a.c.KH;
   a.window = p->window;
-  a.sm_scale = p->sm_scale > 0.f ? p->sm_scale : 1.0f / std::sqrt((float)a.c.D);
-  a.unit = a.sm_scale;
-  if (p->softcap > 0.f) {
-    a.unit = p->softcap;
-    a.cap_inv = a.sm_scale / p->softcap;
-    if (!std::isfinite(a.cap_inv) || a.cap_inv == 0.f) return ENTMAX_ATTN_EINVAL_ALPHA;
-  }
+  rc = softmax_unit(p->sm_scale, p->softcap, a.c.D, &a.sm_scale, &a.cap_inv, &a.unit);
+  if (rc != ENTMAX_ATTN_OK) return rc;
   const int most_kv = a.c.max_pages << a.c.ps_shift;
   a.max_kv = p->max_kv_len > 0 && p->max_kv_len < most_kv ? p->max_kv_len : most_kv;
   const int most_q = uniform ? p->total_q / a.c.B : p->total_q;

@@ -88,8 +88,9 @@ __device__ __forceinline__ void tanh_scores_of_rows(float inv, float (&s)[N]) {
   }
 }
 
-// What scores are multiplied by, never 0; a NaN stays one
-__device__ __forceinline__ float at_least_tiny(float x) { return x < 1e-30f ? 1e-30f : x; }
+// What scores are multiplied by, never 0: the least normal number instead, which leaves a score that a slope has made 1e34 units (2^-100 is the least unit) without weight.  A NaN
+// stays one.
+__device__ __forceinline__ float at_least_tiny(float x) { return x < 1.17549435e-38f ? 1.17549435e-38f : x; }
 
 // the slope's term of N scores from column j0 on
 template <int N>

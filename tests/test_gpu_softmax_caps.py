@@ -89,3 +89,26 @@ def test_paged_scores_far_below_the_cap_next_to_rows_beyond_it(n, cap):
             want = _bounds_without_a_cap(softmax.head(*args, cap, pos=pos), softmax.head(*args, 0.0, pos=pos))
             softmax.check("o", o[rows, h], want)
             softmax.check("lse", lse[rows, h], want)
+
+
+@pytest.mark.parametrize("dtype", [f32, bf16])
+@pytest.mark.parametrize("name", ["sm_scale", "softcap"])
+@pytest.mark.parametrize("value", [2.0 ** -100, 2.0 ** 100])
+def test_the_least_and_the_largest_scales_and_caps(name, value, dtype):
+    # with slopes, and with scales of 0 among others: what is left are the slopes' terms, the uncapped scores, or the largest score alone
+    B, H, G, N, d = 1, 2, 1, 200, 64
+    q, k, v, d_o = _inputs(B, H, G, N, d, dtype, seed=6)
+    c = 0.5 + torch.rand((B, H, N), generator=torch.Generator().manual_seed(1))
+    c[:, :, ::7] = 0.0
+    t = dict(alibi_slopes=torch.tensor([0.5, 0.03], device="cuda"), c_rows=c.cuda())
+    if name == "sm_scale" and value > 1:
+        k *= 2.0 ** -100                                          # (scores of order 8)
+    o, lse = binding.entmax_attn_softmax_fwd(q, k, v, True, **{name: value}, **t)
+    dq, dk, dv, dc, _ = binding.entmax_attn_softmax_bwd(q, k, v, o, lse, d_o, True, want_scale_rows=True, **{name: value}, **t)
+    cap, sm = (0.0, value) if name == "sm_scale" else (value, None)
+    args = (q.cpu(), k.cpu(), v.cpu(), True, None, None, None, None, c, t["alibi_slopes"].cpu())
+    want = softmax.problem(*args, cap, sm, d_o.cpu())
+    if cap > 1:
+        want = _bounds_without_a_cap(want, softmax.problem(*args, 0.0, None, d_o.cpu()))
+    for n, x in dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv, dc=dc).items():
+        softmax.check(n, x, want, "%s %g" % (name, value))
