@@ -483,9 +483,10 @@ int entmax_attn_row_ranges(int32_t batch, int32_t seq, int32_t docs, int32_t cau
  *   max_q_len, max_kv_len   the most new tokens and the longest kv_len of any sequence of the call (0: not known): they size the workspace and the
  *                 launches; a sequence beyond them is left out (ENTMAX_ATTN_FLAG_BAD_LENGTH)
  *   workspace     device scratch, 256-byte aligned, >= entmax_attn_softmax_paged_workspace_bytes(cache, params, cu_q == NULL) bytes
- * The rows of a sequence that is left out get O = 0, lse = -inf.  Slots past a sequence's length may hold anything.  A sequence with 64 rows at most
+ * The rows of a sequence that is left out get O = 0, lse = -inf.  Slots past a sequence's length may hold anything.  A sequence with few rows
  * (a row: a new token and one of the g = q_heads / kv_heads query heads of a K/V head, g <= 128) reads K and V once per K/V head, a longer chunk once for every
- * 128 new tokens and two of the query heads (g odd: 256 tokens and one).  Results are bitwise reproducible.  Errors as for entmax_attn_fwd; bf16 only. */
+ * 128 new tokens and two of the query heads (g odd: 256 tokens and one).  Few are 16, 32 or 64 rows: as many as the longest chunk the call allows fills, or,
+ * where that is more than 64, as the average one does (total_q / batch, rounded up).  Results are bitwise reproducible.  Errors as for entmax_attn_fwd; bf16 only. */
 typedef struct {
   int32_t total_q, q_heads;
   int32_t max_q_len, max_kv_len;
