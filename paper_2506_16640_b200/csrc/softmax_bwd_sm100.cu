@@ -18,8 +18,9 @@
 // five (16 heads x 8192 x 128, no mask: 667 us with one, 580 with two; forward and dK / dV, whose issuers' products depend on one another, lost by a
 // second one).  Every wait is bounded.
 //
-// Bound by a step's chain of barriers, TMEM loads, element code and products: 16 heads x 8192 x 128 causal 302 us for dQ (three products, 1.36 PFLOP/s) and 444 us for
-// dK and dV (four, 1.24); without a mask at 64 columns (4 x 16 x 4096) 472 and 695 us.  Short rows: 8 x 12 x 1024 x 64 50 and 61 us.
+// Bound by a step's chain of barriers, TMEM loads, element code and products: 16 heads x 8192 x 128 causal 294 us for dQ (three products, 1.40 PFLOP/s) and 444 us for
+// dK and dV (four, 1.24); without a mask at 64 columns (4 x 16 x 4096) 472 and 695 us.  Short rows: 8 x 12 x 1024 x 64 48 and 60 us, with a learned scale and its
+// gradient 73 and 65.  All threads have 96 registers: variants with caps, slopes or scales spill on the element path (dQ with everything 96 bytes stored, 236 read).
 #include <cuda.h>
 
 #include <type_traits>
@@ -177,7 +178,7 @@ __device__ __forceinline__ void dq_elements(const RowTerms& r, int j0, const flo
 }
 // CAP, SLOPE, FINE, DC known at compile time: see RowSoftmax.
 // FINE: calls with scales or slopes, whose maps are sharp.  A row of dS sums to zero, so dQ is what remains of a cancellation where its few keys weigh about the
-// same, and 2^-9 of every term is a part of that: dQ gets what the rounding of dS left over as a second product.  And dK gets D from the float32 probabilities.
+// same, and the rounding, up to 2^-8 of every term, is a part of that: dQ gets what the rounding of dS left over as a second product.  And dK gets D from the float32 probabilities.
 // (8 x 12 x 1024 x 64 with a learned scale: dQ 2.5e-3 off in norm without, 1.9e-3 with; the rounding of dQ itself is 1.7e-3.  Plain calls, 2.4e-3, would lose
 // 4 to 9 % of the backward pass.)
 template <int HD, bool CAP, bool SLOPE, bool FINE, bool DC>

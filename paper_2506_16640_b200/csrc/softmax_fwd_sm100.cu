@@ -5,14 +5,14 @@
 // scores first).  Per Q tile and K/V tile of 128 keys
 //   S = Q K^T        both operands in shared memory, S in TMEM;
 //   P = exp2(a x - a m)   a thread per row: its 128 scores in registers, running maximum m, running sum l of the float32 probabilities;
-//                         P as bf16 over S's own columns (2^-9 of a probability at most: what the product's input type holds);
+//                         P as bf16 over S's own columns (off by 2^-8 of a probability at most: what the product's input type holds);
 //   O += P V         P from TMEM, V with the head dim contiguous, O in TMEM.
 // O is not rescaled for every rise of the maximum: P may grow up to 2^8 above the m it is measured from before O and l are brought to a new one, exactly, so
 // that nothing is lost and the correction is rare.  While one tile's softmax runs the tensor core works on the other's O and next S.
 // Bound by the chain of one tile -- S from TMEM, maximum, 128 exponentials a thread (16384 a tile, 1024 cycles of the special-function unit), P to TMEM, then O and
 // the next S behind the other tile's -- of which two are under way.  Computing a part of the exponentials on the FMA pipe made it longer.
 // 16 heads x 16384 x 128 causal: 850 us, 1.29 PFLOP/s, 80 % of the measured rate of library products; 4 x 16 x 8192 x 64: 800 us; 8 x 12 x 1024 x 64, where starts and
-// ends of items count: 36 us.
+// ends of items count: 34 us (36 with a learned scale).  A cap makes the chain longer: 16 x 8192 x 128 causal 241 us, 376 with one.
 // CTA: warps 0..3 and 4..7 the rows of the two tiles, warp 8 MMA issuer, warp 9 TMA producer and scheduler (10, 11: idle, registers go by warpgroups).  Items are handed out by the hardware: a
 // running CTA takes over one that has not started (longest rows of a head first).  Every wait is bounded (see sm100_ptx.cuh).
 #include <cuda.h>

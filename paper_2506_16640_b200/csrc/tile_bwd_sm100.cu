@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kThreadsB, 1) tile_bwd_kernel(const __grid_con
             }
             // the rounding remainder of g dS as a second operand: the rows of dS sum to zero, so when a row's keys
             // are nearly equal vectors (retrieval: several copies of one key) dQ is what is left after a
-            // cancellation, and the bf16 rounding of dS alone (2^-9 of every term) would be a large part of it
+            // cancellation, and the bf16 rounding of dS alone (up to 2^-8 of every term) would be a large part of it
 #pragma unroll
             for (int kk = 0; kk < TN / 16; ++kk) {
               const uint32_t b_off = kk * ((16 * 128) >> 4);

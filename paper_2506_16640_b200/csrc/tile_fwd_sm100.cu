@@ -57,7 +57,7 @@ constexpr int kSampleSweepCap = 12;    // sampled sweeps at most
 constexpr float kSampleTol = 1e-2f;    // the sampled iteration stops at a step of this size, relative to |tau|
 // Mass sum_j p_ij at the threshold a sweep used, minus 1.  Within kNearMass before a Newton step: the step squares the
 // error, so the next sweep can be an output sweep.  Within kOutputMass in an output sweep: its O is the result (P is
-// rounded to bf16, 2^-9 relative, anyway), and the step its sums give makes the stored threshold exact to fp32.
+// rounded to bf16, 2^-8 relative at most, anyway), and the step its sums give makes the stored threshold exact to fp32.
 constexpr float kNearMass = 5e-2f, kOutputMass = 1e-3f;
 enum SweepKind : int { kSampleMax = 0, kSampleNewton = 1, kFullMax = 2, kFullNewton = 3, kOutput = 4 };
 constexpr int kPBytes = TM * TN * 2;
