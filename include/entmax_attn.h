@@ -415,7 +415,7 @@ int entmax_attn_paged_tables(const entmax_attn_paged_tables_params* params, cons
  *   z_ij = sm_scale <q_i, k_j>,   x_ij = softcap tanh(z_ij / softcap) - m_h |i - j|,   s_ij = c_i x_ij,
  *   p_ij = exp(s_ij - lse_i) over the keys the row sees,   O_i = sum_j p_ij v_j;   a row that sees none: O = 0, lse = -inf, no gradient.
  * Query heads g * kv_head .. g * kv_head + g - 1, g = heads / kv_heads, share a K/V head.
- *   seq           any length; row i sees the keys j <= i (causal = 1) or all, of those the ones in its range where ranges are given
+ *   seq           any length from 1 on (the dense calls refuse an empty batch or sequence); row i sees the keys j <= i (causal = 1) or all, of those the ones in its range where ranges are given
  *   softcap       0: scores are not capped; otherwise, like an sm_scale that is not 0, between 2^-100 and 2^100
  *   q, k, v, o    strides in elements, head_dim innermost (all 0: contiguous [batch, heads or kv_heads, seq, head_dim]); at least head_dim, multiples
  *                 of 8, where their dimension has more than one entry
