@@ -542,6 +542,7 @@ __global__ void __launch_bounds__(kDqThreads, 1) softmax_dq_kernel(const __grid_
           sum0 = fmaf(p, dp[e], sum0);
           sum1 += p;
         }
+        __syncwarp();                            // (with a cap rows may have gone different ways, and the store is all lanes')
         tmem_st2(lane_base + kDS + group * 16, __float_as_uint(sum0), __float_as_uint(sum1));
         tmem_st_wait();
         tc_fence_before();

@@ -534,7 +534,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) softmax_fwd_kernel(const __gri
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld_wait32(s[c]);
         const float grown = sm.take(a.cap_inv, s, k0, sees, edge);
-        if (j < hi - 1 && __any_sync(0xffffffffu, grown != 1.0f)) {
+        const bool rises = __any_sync(0xffffffffu, grown != 1.0f);    // (asked in every step: the warp's rows may have gone different ways, and the stores are all lanes')
+        if (j < hi - 1 && rises) {
 #pragma unroll
           for (int c = 0; c < HD / 16; ++c) {
             float v[16];

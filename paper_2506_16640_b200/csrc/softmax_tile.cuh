@@ -85,6 +85,7 @@ __device__ __forceinline__ void tanh_scores_of_rows(float inv, float (&s)[N]) {
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e) s[e] = tanh_full(s[e] * inv);
+    __syncwarp();                                // (the warp goes on together, as the TMEM instructions behind this want it)
   }
 }
 
